@@ -271,6 +271,85 @@ sata_status sata_decode_step_grouped(float* S, const void* q, const void* k, con
                                      sata_dtype dt, int B, int H_kv, int G, int d_k, int d_v, int P,
                                      void* y, void* stream);
 
+/* ---- Linear attention with a decay, and exact softmax attention ---------------
+ *
+ * The two attentions that stand beside Taylor attention in a stack: one with a
+ * d_k x d_v state that forgets, and the exact softmax that f_P approximates
+ * (Sec. 2.1).  Common to the calls below, besides the rules above:
+ *  - Grouped query heads throughout: q, y and their gradients are
+ *    [B][H_kv*G][n][d], k, v and theirs [B][H_kv][n][d]; query head g + G*h reads
+ *    key/value head h.  The gradients of k and v are sums over the group.
+ *  - Scores are scaled by c = 1 / sqrt(d_k).  Causality is inclusive.
+ *  - lengths: [B] int32 (device) or NULL.  Sequence b has lengths[b] tokens
+ *    (taken into 0..n; NULL: all have n).  Rows at and behind a length are not
+ *    used, whatever they hold, and their outputs and gradients are written as zero.
+ *  - 1 <= d_k, d_v <= 128 (SATA_ERR_UNSUPPORTED beyond), B*H_kv*G <= 65535 and
+ *    n <= 2^21 (SATA_ERR_TOO_LARGE beyond).
+ *  - Values that are not finite reach what depends on them only: not earlier
+ *    tokens' outputs, nor other sequences or heads.  */
+
+/* Causal linear attention with a decay: with lam = exp(log_decay[h]),
+ *     S_t = lam S_{t-1} + k_t (x) v_t,    y_t = c q_t S_t.
+ *   log_decay: [H_kv] float32 (device), at most 0; minus infinity keeps each token to itself
+ *   S_in : [B][H_kv][d_k][d_v] float32 (device), the state before the first token, or NULL for zero
+ *   y    : [B][H_kv*G][n][d_v], dtype dt (device, written)
+ *   S_out: [B][H_kv][d_k][d_v] float32 (device, written) or NULL: the state after
+ *          each sequence's last token, ready for sata_decay_step or as S_in of the
+ *          tokens that follow.  Must not be S_in.
+ * n = 0 writes S_out alone. */
+sata_status sata_decay_prefill(const void* q, const void* k, const void* v, const float* log_decay, sata_dtype dt, int B,
+                               int H_kv, int G, int n, int d_k, int d_v, const int32_t* lengths, const float* S_in,
+                               void* y, float* S_out, void* stream);
+
+/* One token of every sequence: S = lam S + k (x) v, then y = c q S.
+ *   S: [B][H_kv][d_k][d_v] float32 (device, read and written in place)
+ *   q: [B][H_kv*G][d_k], k: [B][H_kv][d_k], v: [B][H_kv][d_v], y: [B][H_kv*G][d_v] */
+sata_status sata_decay_step(float* S, const void* q, const void* k, const void* v, const float* log_decay,
+                            sata_dtype dt, int B, int H_kv, int G, int d_k, int d_v, void* y, void* stream);
+
+/* Gradients of sata_decay_prefill for dL/dy = dy and dL/dS_out = dS (NULL: zero):
+ *     U_t = lam U_{t+1} + c q_t (x) dy_t  (from U = dS / lam behind the last token),
+ *     dq_t = c S_t dy_t,   dk_t = U_t v_t,   dv_t = U_t^T k_t,   dS_in = lam U_0.
+ * The decay is a constant of the layer: it gets no gradient.
+ *   S_in : as given to the forward call, or NULL
+ *   dq, dk, dv: as q, k, v (device, written)
+ *   dS_in: [B][H_kv][d_k][d_v] float32 (device, written) or NULL.  Must not be dS. */
+sata_status sata_decay_backward(const void* q, const void* k, const void* v, const float* log_decay, const void* dy,
+                                sata_dtype dt, int B, int H_kv, int G, int n, int d_k, int d_v, const int32_t* lengths,
+                                const float* S_in, const float* dS, void* dq, void* dk, void* dv, float* dS_in,
+                                void* stream);
+
+/* Exact causal softmax attention (Sec. 2.1):
+ *     lse_t = log sum_{s<=t} exp(c q_t.k_s),   y_t = sum_{s<=t} exp(c q_t.k_s - lse_t) v_s.
+ *   y  : [B][H_kv*G][n][d_v], dtype dt (device, written)
+ *   lse: [B][H_kv*G][n] float32 (device, written) or NULL: what sata_softmax_backward
+ *        needs; minus infinity at and behind a sequence's length. */
+sata_status sata_softmax_prefill(const void* q, const void* k, const void* v, sata_dtype dt, int B, int H_kv, int G, int n,
+                                 int d_k, int d_v, const int32_t* lengths, void* y, float* lse, void* stream);
+
+/* Gradients of sata_softmax_prefill for dL/dy = dy, the probabilities computed
+ * again from the scores and lse (y and lse as the forward call wrote them):
+ *     p_ts = exp(c q_t.k_s - lse_t),   e_ts = c p_ts (dy_t.v_s - dy_t.y_t),
+ *     dq_t = sum_{s<=t} e_ts k_s,  dk_s = sum_{t>=s} e_ts q_t,  dv_s = sum_{t>=s} p_ts dy_t.
+ *   dq, dk, dv: as q, k, v (device, written)
+ * Workspace: 4 bytes per query head and token. */
+sata_status sata_softmax_backward(const void* q, const void* k, const void* v, const void* y, const float* lse,
+                                  const void* dy, sata_dtype dt, int B, int H_kv, int G, int n, int d_k, int d_v,
+                                  const int32_t* lengths, void* dq, void* dk, void* dv, void* stream);
+
+/* One token of every sequence over a cache: writes k and v as row lengths[b] of
+ * the cache, then y = softmax attention of q over rows 0..lengths[b].
+ *   K, V   : [B][H_kv][capacity][d_k] and [..][d_v], dtype dt (device; one row per head written)
+ *   lengths: [B] int32 (device): tokens in the cache before the call; not changed.
+ *            A sequence whose length is negative or not below the capacity is idle:
+ *            its cache is left as it is and its y is zero.
+ *   q: [B][H_kv*G][d_k], k: [B][H_kv][d_k], v: [B][H_kv][d_v], y: [B][H_kv*G][d_v]
+ * Rows behind lengths[b] are not used, whatever they hold.  The cache after a
+ * prompt is its k and v, in tensors of `capacity` rows; capacity <= 2^21. */
+sata_status sata_softmax_step(void* K, void* V, int capacity, const int32_t* lengths, const void* q, const void* k,
+                              const void* v, sata_dtype dt, int B, int H_kv, int G, int d_k, int d_v, void* y,
+                              void* stream);
+
 /* Static text for a status code. */
 const char* sata_status_string(sata_status s);
 

@@ -66,6 +66,19 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.sata_decode_step_compensated.restype = i32
     lib.sata_decode_step_grouped.argtypes = [vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, vp, vp]
     lib.sata_decode_step_grouped.restype = i32
+    lib.sata_decay_prefill.argtypes = [vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp]
+    lib.sata_decay_prefill.restype = i32
+    lib.sata_decay_step.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, vp, vp]
+    lib.sata_decay_step.restype = i32
+    lib.sata_decay_backward.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp,
+                                        vp, vp]
+    lib.sata_decay_backward.restype = i32
+    lib.sata_softmax_prefill.argtypes = [vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, vp, vp, vp, vp]
+    lib.sata_softmax_prefill.restype = i32
+    lib.sata_softmax_backward.argtypes = [vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp]
+    lib.sata_softmax_backward.restype = i32
+    lib.sata_softmax_step.argtypes = [vp, vp, i32, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, vp, vp]
+    lib.sata_softmax_step.restype = i32
     lib.sata_status_string.argtypes = [i32]
     lib.sata_status_string.restype = ctypes.c_char_p
     lib.sata_last_error.argtypes = []
@@ -412,6 +425,182 @@ def decode_step_grouped(S, q, k, v, P: int, y=None):
         _check(load_library().sata_decode_step_grouped(_ptr(S), _ptr(q), _ptr(k), _ptr(v), code, B, Hkv, G,
                                                        dk, dv, P, _ptr(y), _stream_ptr()),
                "sata_decode_step_grouped")
+    return y
+
+
+# ------------------------------------------------------------------ decay and softmax attention
+
+def _prompt_sizes(q, k, v):
+    """(dtype code, B, H_kv, G, n, d_k, d_v) of q [B, G*H_kv, n, d_k], k [B, H_kv, n, d_k], v [B, H_kv, n, d_v]."""
+    code = _dtype_code(q)
+    _check_same_dtype(q, k=k, v=v)
+    if q.dim() != 4 or k.dim() != 4 or v.dim() != 4:
+        raise ValueError("q [B, G*H_kv, n, d_k], k [B, H_kv, n, d_k], v [B, H_kv, n, d_v] expected")
+    B, Hq, n, dk = q.shape
+    Hkv, dv = k.shape[1], v.shape[-1]
+    if Hkv < 1 or Hq % Hkv:
+        raise ValueError("the query head count must be a multiple of the key/value head count")
+    _check_shape(k, "k", (B, Hkv, n, dk))
+    _check_shape(v, "v", (B, Hkv, n, dv))
+    return code, B, Hkv, Hq // Hkv, n, dk, dv
+
+
+def _token_sizes(q, k, v):
+    """(dtype code, B, H_kv, G, d_k, d_v) of q [B, G*H_kv, d_k], k [B, H_kv, d_k], v [B, H_kv, d_v]."""
+    code = _dtype_code(q)
+    _check_same_dtype(q, k=k, v=v)
+    if q.dim() != 3 or k.dim() != 3 or v.dim() != 3:
+        raise ValueError("q [B, G*H_kv, d_k], k [B, H_kv, d_k], v [B, H_kv, d_v] expected")
+    B, Hq, dk = q.shape
+    Hkv, dv = k.shape[1], v.shape[-1]
+    if Hkv < 1 or Hq % Hkv:
+        raise ValueError("the query head count must be a multiple of the key/value head count")
+    _check_shape(k, "k", (B, Hkv, dk))
+    _check_shape(v, "v", (B, Hkv, dv))
+    return code, B, Hkv, Hq // Hkv, dk, dv
+
+
+def _check_as(t, name: str, dtype, shape):
+    """Type and shape of an argument that may be left out."""
+    if t is None:
+        return
+    if t.dtype != dtype:
+        raise TypeError(f"{name} is {t.dtype}, expected {dtype}")
+    _check_shape(t, name, shape)
+
+
+def _check_tensors(device, **tensors):
+    for name, t in tensors.items():
+        if t is not None:
+            _check_tensor(t, name, device)
+
+
+def decay_prefill(q, k, v, log_decay, lengths=None, S_in=None, want_state: bool = True, y=None, S=None):
+    """Causal linear attention with a decay per key/value head: S_t = exp(log_decay) S_{t-1} + k_t (x) v_t,
+    y_t = q_t S_t / sqrt(d_k).
+
+    q: [B, H_q, n, d_k] with H_q = G * H_kv (query head g + G*h reads key/value head h); k: [B, H_kv, n, d_k];
+    v: [B, H_kv, n, d_v]; log_decay: [H_kv] float32, at most 0; lengths: [B] int32, the tokens of each
+    sequence (the rest is padding: y is zero there); S_in: the states to go on from.
+    Returns (y [B, H_q, n, d_v] in the input dtype, S [B, H_kv, d_k, d_v] float32 or None).
+    Preallocated outputs may be passed as y= and S=."""
+    torch = _torch()
+    code, B, H, G, n, dk, dv = _prompt_sizes(q, k, v)
+    _check_as(log_decay, "log_decay", torch.float32, (H,))
+    _check_as(lengths, "lengths", torch.int32, (B,))
+    _check_as(S_in, "S_in", torch.float32, (B, H, dk, dv))
+    _check_as(y, "y", q.dtype, (B, G * H, n, dv))
+    _check_as(S, "S", torch.float32, (B, H, dk, dv))
+    _check_tensors(q.device, q=q, k=k, v=v, log_decay=log_decay, lengths=lengths, S_in=S_in, y=y, S=S)
+    if y is None:
+        y = torch.empty(B, G * H, n, dv, dtype=q.dtype, device=q.device)
+    if want_state and S is None:
+        S = torch.empty(B, H, dk, dv, dtype=torch.float32, device=q.device)
+    with torch.cuda.device(q.device):
+        _check(load_library().sata_decay_prefill(_ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), code, B, H, G, n, dk, dv,
+                                                 _ptr(lengths), _ptr(S_in), _ptr(y), _ptr(S), _stream_ptr()),
+               "sata_decay_prefill")
+    return y, S
+
+
+def decay_step(S, q, k, v, log_decay, y=None):
+    """One token of every sequence, in place on S [B, H_kv, d_k, d_v]: S = exp(log_decay) S + k (x) v,
+    y = q S / sqrt(d_k).  q: [B, H_q, d_k]; k: [B, H_kv, d_k]; v: [B, H_kv, d_v].  Returns y [B, H_q, d_v]."""
+    torch = _torch()
+    code, B, H, G, dk, dv = _token_sizes(q, k, v)
+    _check_state(S, (B, H, dk, dv))
+    _check_as(log_decay, "log_decay", torch.float32, (H,))
+    _check_as(y, "y", q.dtype, (B, G * H, dv))
+    _check_tensors(q.device, S=S, q=q, k=k, v=v, log_decay=log_decay, y=y)
+    if y is None:
+        y = torch.empty(B, G * H, dv, dtype=q.dtype, device=q.device)
+    with torch.cuda.device(q.device):
+        _check(load_library().sata_decay_step(_ptr(S), _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), code, B, H, G, dk,
+                                              dv, _ptr(y), _stream_ptr()), "sata_decay_step")
+    return y
+
+
+def decay_backward(q, k, v, log_decay, dy, lengths=None, S_in=None, dS=None):
+    """Gradients of decay_prefill for dL/dy = dy [B, H_q, n, d_v] and dL/dS = dS [B, H_kv, d_k, d_v] (None: zero).
+    Returns (dq, dk, dv, dS_in): the first three in q's dtype, dS_in float32, or None without S_in.
+    The decay is a constant of the layer and gets no gradient."""
+    torch = _torch()
+    code, B, H, G, n, dk, dv = _prompt_sizes(q, k, v)
+    _check_as(log_decay, "log_decay", torch.float32, (H,))
+    _check_as(dy, "dy", q.dtype, (B, G * H, n, dv))
+    _check_as(lengths, "lengths", torch.int32, (B,))
+    _check_as(S_in, "S_in", torch.float32, (B, H, dk, dv))
+    _check_as(dS, "dS", torch.float32, (B, H, dk, dv))
+    _check_tensors(q.device, q=q, k=k, v=v, log_decay=log_decay, dy=dy, lengths=lengths, S_in=S_in, dS=dS)
+    dq, dkk, dvv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+    dS_in = torch.empty_like(S_in) if S_in is not None else None
+    with torch.cuda.device(q.device):
+        _check(load_library().sata_decay_backward(_ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(dy), code, B, H, G,
+                                                  n, dk, dv, _ptr(lengths), _ptr(S_in), _ptr(dS), _ptr(dq), _ptr(dkk),
+                                                  _ptr(dvv), _ptr(dS_in), _stream_ptr()), "sata_decay_backward")
+    return dq, dkk, dvv, dS_in
+
+
+def softmax_prefill(q, k, v, lengths=None, want_lse: bool = True, y=None):
+    """Exact causal softmax attention, the one that the Taylor series stands for.
+
+    q: [B, H_q, n, d_k] with H_q = G * H_kv; k: [B, H_kv, n, d_k]; v: [B, H_kv, n, d_v]; lengths: [B] int32, the
+    tokens of each sequence (the rest is padding: y is zero and lse minus infinity there).
+    Returns (y [B, H_q, n, d_v] in the input dtype, lse [B, H_q, n] float32, the logarithm of each row's sum of
+    exponentials, or None)."""
+    torch = _torch()
+    code, B, H, G, n, dk, dv = _prompt_sizes(q, k, v)
+    _check_as(lengths, "lengths", torch.int32, (B,))
+    _check_as(y, "y", q.dtype, (B, G * H, n, dv))
+    _check_tensors(q.device, q=q, k=k, v=v, lengths=lengths, y=y)
+    if y is None:
+        y = torch.empty(B, G * H, n, dv, dtype=q.dtype, device=q.device)
+    lse = torch.empty(B, G * H, n, dtype=torch.float32, device=q.device) if want_lse else None
+    with torch.cuda.device(q.device):
+        _check(load_library().sata_softmax_prefill(_ptr(q), _ptr(k), _ptr(v), code, B, H, G, n, dk, dv, _ptr(lengths),
+                                                   _ptr(y), _ptr(lse), _stream_ptr()), "sata_softmax_prefill")
+    return y, lse
+
+
+def softmax_backward(q, k, v, y, lse, dy, lengths=None):
+    """Gradients of softmax_prefill for dL/dy = dy, from its outputs y and lse; the probabilities are computed
+    again.  Returns (dq, dk, dv) in q's dtype."""
+    torch = _torch()
+    code, B, H, G, n, dk, dv = _prompt_sizes(q, k, v)
+    _check_as(y, "y", q.dtype, (B, G * H, n, dv))
+    _check_as(lse, "lse", torch.float32, (B, G * H, n))
+    _check_as(dy, "dy", q.dtype, (B, G * H, n, dv))
+    _check_as(lengths, "lengths", torch.int32, (B,))
+    _check_tensors(q.device, q=q, k=k, v=v, y=y, lse=lse, dy=dy, lengths=lengths)
+    dq, dkk, dvv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+    with torch.cuda.device(q.device):
+        _check(load_library().sata_softmax_backward(_ptr(q), _ptr(k), _ptr(v), _ptr(y), _ptr(lse), _ptr(dy), code, B,
+                                                    H, G, n, dk, dv, _ptr(lengths), _ptr(dq), _ptr(dkk), _ptr(dvv),
+                                                    _stream_ptr()), "sata_softmax_backward")
+    return dq, dkk, dvv
+
+
+def softmax_step(K, V, lengths, q, k, v, y=None):
+    """One token of every sequence over a cache K [B, H_kv, capacity, d_k], V [B, H_kv, capacity, d_v]: writes k and
+    v as row lengths[b], then attends over rows 0..lengths[b].  lengths: [B] int32, the tokens in the cache before
+    the call; it is not changed.  A sequence whose length is negative or not below the capacity is idle (its cache
+    stays, its y is zero).  q: [B, H_q, d_k]; k: [B, H_kv, d_k]; v: [B, H_kv, d_v].  Returns y [B, H_q, d_v]."""
+    torch = _torch()
+    code, B, H, G, dk, dv = _token_sizes(q, k, v)
+    _check_same_dtype(q, K=K, V=V)
+    if K.dim() != 4:
+        raise ValueError("K must be [B, H_kv, capacity, d_k]")
+    cap = K.shape[2]
+    _check_shape(K, "K", (B, H, cap, dk))
+    _check_shape(V, "V", (B, H, cap, dv))
+    _check_as(lengths, "lengths", torch.int32, (B,))
+    _check_as(y, "y", q.dtype, (B, G * H, dv))
+    _check_tensors(q.device, K=K, V=V, lengths=lengths, q=q, k=k, v=v, y=y)
+    if y is None:
+        y = torch.empty(B, G * H, dv, dtype=q.dtype, device=q.device)
+    with torch.cuda.device(q.device):
+        _check(load_library().sata_softmax_step(_ptr(K), _ptr(V), cap, _ptr(lengths), _ptr(q), _ptr(k), _ptr(v), code,
+                                                B, H, G, dk, dv, _ptr(y), _stream_ptr()), "sata_softmax_step")
     return y
 
 

@@ -198,6 +198,62 @@ hipError_t launch_backward_direct(const void* q, const void* k, const void* v, c
                                   void* dv, bool bf16, int BH, int n, int dk_, int dv_, int P, float* stat,
                                   hipStream_t s);
 
+// ---- linear attention with a decay, softmax attention -----------------------------
+constexpr int kMaxPairDim = 128;  // d_k and d_v
+
+// One scan over the tokens of `heads` key/value heads (decay.hip): with the state
+//     R_t = lam R_{t-1} + update b_t (x) w_t,   out_t = readout a_t R_t,
+// from the last token back where `reverse`; one of update and readout is the
+// scale of the scores, the other 1.  a holds ga members a head, b and w gb
+// (one of the two is 1).  Forward, the state starts as S_in and S_out is the
+// state after the last token; in reverse R starts as S_in / lam, and S_out is lam R
+// after the first token.
+struct DecayScan {
+  const void *a = nullptr, *b = nullptr, *w = nullptr;
+  void* out = nullptr;                            // may be null: the state alone
+  const float* S_in = nullptr;                    // [heads][da][dw] ([dw][da] where transposed) or null
+  float* S_out = nullptr;                         // the same or null
+  const float* log_decay = nullptr;               // [H]
+  const int* lengths = nullptr;                   // [heads / H] or null
+  int heads = 0, H = 0, n = 0, da = 0, dw = 0, ga = 1, gb = 1;
+  bool reverse = false, transposed = false;
+  float update = 1.f, readout = 1.f;
+};
+hipError_t launch_decay_scan(const DecayScan& s, bool bf16, hipStream_t st);
+hipError_t launch_decay_step(float* S, const void* q, const void* k, const void* v, const float* log_decay, void* y,
+                             bool bf16, int heads, int H, int G, int dk, int dv, float scale, hipStream_t st);
+
+struct SoftmaxArgs {
+  const void *q, *k, *v;
+  void* y;
+  float* lse;          // may be null
+  const int* lengths;  // may be null
+  int heads, H, G, n, dk_, dv_;
+  float scale;
+};
+hipError_t launch_softmax_prefill(const SoftmaxArgs& a, bool bf16, hipStream_t s);
+
+struct SoftmaxGradArgs {
+  const void *q, *k, *v, *y, *dy;
+  const float* lse;
+  void *dq, *dk, *dv;
+  float* delta;        // scratch, [heads * G][n]
+  const int* lengths;  // may be null
+  int heads, H, G, n, dk_, dv_;
+  float scale;
+};
+hipError_t launch_softmax_backward(const SoftmaxGradArgs& a, bool bf16, hipStream_t s);
+
+struct SoftmaxStepArgs {
+  void *K, *V;         // [heads][capacity][d]
+  const int* lengths;  // [heads / H]
+  const void *q, *k, *v;
+  void* y;
+  int heads, H, G, capacity, dk_, dv_;
+  float scale;
+};
+hipError_t launch_softmax_step(const SoftmaxStepArgs& a, bool bf16, hipStream_t s);
+
 // ---- helpers -----------------------------------------------------------------
 hipError_t launch_fill_zero(float* p, int64_t count, hipStream_t s);
 

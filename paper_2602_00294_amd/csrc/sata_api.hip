@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
@@ -689,6 +690,26 @@ sata_status backward(Way way, const void* q, const void* k, const void* v, const
   return ok();
 }
 
+// Longest sequences of the decay and softmax calls: a head's tensor is addressed
+// by 32-bit byte offsets (float32 at d = 128).
+constexpr int kMaxPairTokens = 1 << 21;
+
+sata_status check_pair_args(sata_dtype dt, int B, int H_kv, int G, int n, int d_k, int d_v) {
+  if (!valid_dtype(dt)) return fail(SATA_ERR_INVALID_ARG, "unknown dtype %d", (int)dt);
+  if (B < 1 || H_kv < 1 || G < 1) return fail(SATA_ERR_INVALID_ARG, "B=%d H_kv=%d G=%d must be >= 1", B, H_kv, G);
+  if (n < 0) return fail(SATA_ERR_INVALID_ARG, "n=%d < 0", n);
+  if (d_k < 1 || d_v < 1) return fail(SATA_ERR_INVALID_ARG, "d_k=%d d_v=%d must be >= 1", d_k, d_v);
+  if (d_k > sata::kMaxPairDim || d_v > sata::kMaxPairDim)
+    return fail(SATA_ERR_UNSUPPORTED, "d_k=%d d_v=%d; supported up to %d", d_k, d_v, sata::kMaxPairDim);
+  // (by division: the product of the three may overflow 64 bits)
+  if (H_kv > kMaxHeads / B || G > kMaxHeads / (B * H_kv))
+    return fail(SATA_ERR_TOO_LARGE, "B*H_kv*G of B=%d H_kv=%d G=%d exceeds %d", B, H_kv, G, kMaxHeads);
+  if (n > kMaxPairTokens) return fail(SATA_ERR_TOO_LARGE, "n=%d exceeds %d", n, kMaxPairTokens);
+  return SATA_OK;
+}
+
+float pair_scale(int d_k) { return (float)(1.0 / std::sqrt((double)d_k)); }
+
 }  // namespace
 
 extern "C" {
@@ -927,6 +948,116 @@ sata_status sata_decode_step_grouped(float* S, const void* q, const void* k, con
   hipError_t e = sata::launch_decode_grouped(S, q, k, v, y, dt == SATA_BF16, BH, d_k, d_v, t, plan, partial,
                                              counters, s);
   if (e != hipSuccess) return hip_fail(e, "grouped decode launch");
+  return ok();
+}
+
+sata_status sata_decay_prefill(const void* q, const void* k, const void* v, const float* log_decay, sata_dtype dt, int B,
+                               int H_kv, int G, int n, int d_k, int d_v, const int32_t* lengths, const float* S_in,
+                               void* y, float* S_out, void* stream) {
+  sata_status st = check_pair_args(dt, B, H_kv, G, n, d_k, d_v);
+  if (st != SATA_OK) return st;
+  if (!log_decay || (n > 0 && (!q || !k || !v || !y))) return fail(SATA_ERR_INVALID_ARG, "null tensor pointer");
+  if (S_in && S_in == S_out) return fail(SATA_ERR_INVALID_ARG, "S_out must not be S_in");
+  if (n == 0 && !S_out) return ok();
+  sata::DecayScan s;
+  s.a = q, s.b = k, s.w = v, s.out = y;
+  s.S_in = S_in, s.S_out = S_out, s.log_decay = log_decay, s.lengths = lengths;
+  s.heads = B * H_kv, s.H = H_kv, s.n = n, s.da = d_k, s.dw = d_v, s.ga = G;
+  s.readout = pair_scale(d_k);
+  hipError_t e = sata::launch_decay_scan(s, dt == SATA_BF16, (hipStream_t)stream);
+  if (e != hipSuccess) return hip_fail(e, "decay prefill launch");
+  return ok();
+}
+
+sata_status sata_decay_step(float* S, const void* q, const void* k, const void* v, const float* log_decay,
+                            sata_dtype dt, int B, int H_kv, int G, int d_k, int d_v, void* y, void* stream) {
+  sata_status st = check_pair_args(dt, B, H_kv, G, 1, d_k, d_v);
+  if (st != SATA_OK) return st;
+  if (!S || !q || !k || !v || !log_decay || !y) return fail(SATA_ERR_INVALID_ARG, "null tensor pointer");
+  hipError_t e = sata::launch_decay_step(S, q, k, v, log_decay, y, dt == SATA_BF16, B * H_kv, H_kv, G, d_k, d_v,
+                                         pair_scale(d_k), (hipStream_t)stream);
+  if (e != hipSuccess) return hip_fail(e, "decay step launch");
+  return ok();
+}
+
+sata_status sata_decay_backward(const void* q, const void* k, const void* v, const float* log_decay, const void* dy,
+                                sata_dtype dt, int B, int H_kv, int G, int n, int d_k, int d_v, const int32_t* lengths,
+                                const float* S_in, const float* dS, void* dq, void* dk, void* dv, float* dS_in,
+                                void* stream) {
+  sata_status st = check_pair_args(dt, B, H_kv, G, n, d_k, d_v);
+  if (st != SATA_OK) return st;
+  if (!log_decay || (n > 0 && (!q || !k || !v || !dy || !dq || !dk || !dv)))
+    return fail(SATA_ERR_INVALID_ARG, "null tensor pointer");
+  if (dS && dS == dS_in) return fail(SATA_ERR_INVALID_ARG, "dS_in must not be dS");
+  if (n == 0 && !dS_in) return ok();
+  const hipStream_t hs = (hipStream_t)stream;
+  const bool bf16 = dt == SATA_BF16;
+  const float c = pair_scale(d_k);
+  sata::DecayScan s;
+  s.log_decay = log_decay, s.lengths = lengths;
+  s.heads = B * H_kv, s.H = H_kv, s.n = n;
+  hipError_t e = hipSuccess;
+  if (n > 0) {
+    sata::DecayScan r = s;
+    r.a = dy, r.b = v, r.w = k, r.out = dq;
+    r.da = d_v, r.dw = d_k, r.ga = G;
+    r.S_in = S_in, r.transposed = true;
+    r.readout = c;
+    if ((e = sata::launch_decay_scan(r, bf16, hs)) != hipSuccess) return hip_fail(e, "decay backward (dq) launch");
+    r = s;
+    r.a = v, r.b = dy, r.w = q, r.out = dk;
+    r.da = d_v, r.dw = d_k, r.gb = G;
+    r.reverse = true, r.transposed = true;
+    r.S_in = dS, r.update = c;
+    if ((e = sata::launch_decay_scan(r, bf16, hs)) != hipSuccess) return hip_fail(e, "decay backward (dk) launch");
+  }
+  s.a = k, s.b = q, s.w = dy, s.out = dv;
+  s.da = d_k, s.dw = d_v, s.gb = G;
+  s.reverse = true;
+  s.S_in = dS, s.S_out = dS_in, s.update = c;
+  if ((e = sata::launch_decay_scan(s, bf16, hs)) != hipSuccess) return hip_fail(e, "decay backward (dv) launch");
+  return ok();
+}
+
+sata_status sata_softmax_prefill(const void* q, const void* k, const void* v, sata_dtype dt, int B, int H_kv, int G, int n,
+                                 int d_k, int d_v, const int32_t* lengths, void* y, float* lse, void* stream) {
+  sata_status st = check_pair_args(dt, B, H_kv, G, n, d_k, d_v);
+  if (st != SATA_OK) return st;
+  if (n == 0) return ok();
+  if (!q || !k || !v || !y) return fail(SATA_ERR_INVALID_ARG, "null tensor pointer");
+  const sata::SoftmaxArgs a{q, k, v, y, lse, lengths, B * H_kv, H_kv, G, n, d_k, d_v, pair_scale(d_k)};
+  hipError_t e = sata::launch_softmax_prefill(a, dt == SATA_BF16, (hipStream_t)stream);
+  if (e != hipSuccess) return hip_fail(e, "softmax prefill launch");
+  return ok();
+}
+
+sata_status sata_softmax_backward(const void* q, const void* k, const void* v, const void* y, const float* lse,
+                                  const void* dy, sata_dtype dt, int B, int H_kv, int G, int n, int d_k, int d_v,
+                                  const int32_t* lengths, void* dq, void* dk, void* dv, void* stream) {
+  sata_status st = check_pair_args(dt, B, H_kv, G, n, d_k, d_v);
+  if (st != SATA_OK) return st;
+  if (n == 0) return ok();
+  if (!q || !k || !v || !y || !lse || !dy || !dq || !dk || !dv) return fail(SATA_ERR_INVALID_ARG, "null tensor pointer");
+  const hipStream_t s = (hipStream_t)stream;
+  void* ws = nullptr;
+  if ((st = get_workspace(sizeof(float) * (size_t)B * H_kv * G * n, s, &ws)) != SATA_OK) return st;
+  const sata::SoftmaxGradArgs a{q,           k,    v, y, dy, lse, dq, dk, dv, (float*)ws, lengths, B * H_kv, H_kv, G, n, d_k, d_v,
+                                pair_scale(d_k)};
+  hipError_t e = sata::launch_softmax_backward(a, dt == SATA_BF16, s);
+  if (e != hipSuccess) return hip_fail(e, "softmax backward launch");
+  return ok();
+}
+
+sata_status sata_softmax_step(void* K, void* V, int capacity, const int32_t* lengths, const void* q, const void* k,
+                              const void* v, sata_dtype dt, int B, int H_kv, int G, int d_k, int d_v, void* y,
+                              void* stream) {
+  sata_status st = check_pair_args(dt, B, H_kv, G, capacity, d_k, d_v);
+  if (st != SATA_OK) return st;
+  if (capacity < 1) return fail(SATA_ERR_INVALID_ARG, "capacity=%d must be >= 1", capacity);
+  if (!K || !V || !lengths || !q || !k || !v || !y) return fail(SATA_ERR_INVALID_ARG, "null tensor pointer");
+  const sata::SoftmaxStepArgs a{K, V, lengths, q, k, v, y, B * H_kv, H_kv, G, capacity, d_k, d_v, pair_scale(d_k)};
+  hipError_t e = sata::launch_softmax_step(a, dt == SATA_BF16, (hipStream_t)stream);
+  if (e != hipSuccess) return hip_fail(e, "softmax step launch");
   return ok();
 }
 

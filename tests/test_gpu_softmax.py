@@ -1,0 +1,249 @@
+"""Exact softmax attention on the GPU against its definition in float64, element by
+element within derived bounds (pair_ref.py): prompts, gradients and single
+tokens over a cache; values that are not finite; streams and captured graphs."""
+import math
+import sys
+
+import pytest
+
+import pair_ref
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+@pytest.fixture(scope="module")
+def sata():
+    if not torch.cuda.is_available():
+        pytest.fail("no GPU visible")
+    import paper_2602_00294_amd as m
+    m.load_library()
+    return m
+
+
+def _say(*msg):
+    print(*msg, file=sys.stderr, flush=True)
+
+
+def _rand(seed, dtype, *shapes, offset=0, size=1.0):
+    g = torch.Generator().manual_seed(seed)
+    out = []
+    for s in shapes:
+        x = (torch.randn(*s, generator=g) * size).to(DT[dtype])
+        held = torch.empty(x.numel() + offset, dtype=x.dtype, device="cuda")
+        held[offset:] = x.reshape(-1).cuda()
+        out.append(held[offset:].view(*s))
+    return out
+
+
+def _prompt(seed, B, H, G, n, dk, dv, dtype, **more):
+    return _rand(seed, dtype, (B, H * G, n, dk), (B, H, n, dk), (B, H, n, dv), (B, H * G, n, dv), **more)
+
+
+def _lengths(x):
+    return None if x is None else torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+CASES = [  # B, H, G, n, dk, dv, dtype, lengths
+    (1, 1, 1, 1, 1, 1, "f32", None),
+    (1, 2, 1, 1, 64, 64, "bf16", None),
+    (2, 2, 1, 63, 16, 16, "bf16", None),
+    (1, 3, 2, 64, 32, 32, "bf16", None),
+    (1, 2, 1, 65, 32, 32, "f32", None),
+    (2, 2, 3, 130, 24, 40, "f32", [0, 130]),
+    (3, 2, 1, 129, 8, 5, "bf16", [1, 64, 128]),
+    (2, 3, 2, 200, 33, 31, "bf16", [199, 7]),
+    (1, 2, 1, 257, 128, 128, "bf16", None),
+    (1, 1, 2, 190, 128, 128, "f32", None),
+    (2, 1, 1, 150, 128, 16, "bf16", [150, 90]),
+    (2, 1, 1, 150, 16, 128, "f32", [-3, 1000]),
+    (1, 2, 4, 100, 100, 72, "f32", None),
+    (1, 1, 1, 1500, 64, 64, "bf16", None),
+    (2, 1, 2, 700, 96, 64, "f32", [650, 3]),
+    (1, 1, 8, 300, 17, 127, "bf16", None),
+    (1, 9, 2, 385, 64, 96, "bf16", None),
+]
+
+
+def _check_prompt(sata, q, k, v, dy, lengths):
+    lens = _lengths(lengths)
+    y, lse = sata.softmax_prefill(q, k, v, lens)
+    torch.cuda.synchronize()
+    ry, rl = pair_ref.softmax_prefill(q, k, v, lengths)
+    worst = [pair_ref.check(y, ry, "y"), pair_ref.check(lse, rl, "lse")]
+    again, none = sata.softmax_prefill(q, k, v, lens, want_lse=False)
+    assert none is None and torch.equal(again, y)
+    got = sata.softmax_backward(q, k, v, y, lse, dy, lens)
+    torch.cuda.synchronize()
+    want = pair_ref.softmax_backward(q, k, v, y, lse, dy, lengths)
+    worst += [pair_ref.check(a, w, name) for name, a, w in zip(("dq", "dk", "dv"), got, want)]
+    _say("  of the bounds: y, lse, dq, dk, dv", ["%.3f" % x for x in worst])
+
+
+@pytest.mark.parametrize("B,H,G,n,dk,dv,dtype,lengths", CASES)
+def test_prompt_and_gradients(sata, B, H, G, n, dk, dv, dtype, lengths):
+    _say("softmax prompt", B, H, G, n, dk, dv, dtype, lengths)
+    _check_prompt(sata, *_prompt(n + dk, B, H, G, n, dk, dv, dtype), lengths)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_unaligned_tensors(sata, dtype):
+    _say("softmax, tensors one element off", dtype)
+    _check_prompt(sata, *_prompt(3, 2, 2, 2, 77, 32, 64, dtype, offset=1), None)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_far_scores(sata, dtype):
+    """Scores of some hundreds: most weights vanish, the maximum moves late, and nothing overflows."""
+    _say("softmax, far scores", dtype)
+    q, k, v, dy = _prompt(4, 1, 2, 1, 300, 32, 32, dtype)
+    k = k * torch.linspace(0.1, 40.0, 300, device="cuda")[None, None, :, None].to(k.dtype)
+    _check_prompt(sata, q, k.contiguous(), v, dy, None)
+
+
+TOKENS = [  # B, H, G, capacity, dk, dv, dtype, lengths
+    (1, 1, 1, 1, 1, 1, "f32", [0]),
+    (2, 2, 1, 70, 64, 64, "bf16", [0, 69]),
+    (4, 2, 4, 300, 128, 128, "bf16", [299, 255, 1, 64]),
+    (3, 3, 2, 130, 33, 40, "f32", [129, 63, 5]),
+    (4, 1, 8, 200, 16, 16, "bf16", [-1, 200, 199, 100]),
+    (1, 2, 3, 5000, 64, 32, "f32", [4321]),
+    (2, 1, 1, 4099, 128, 128, "f32", [4098, 17]),
+    (1, 1, 20, 2600, 96, 100, "bf16", [2599]),
+    (2, 2, 1, 3001, 40, 24, "bf16", [3000, 2047]),
+]
+
+
+@pytest.mark.parametrize("B,H,G,cap,dk,dv,dtype,lengths", TOKENS)
+@pytest.mark.parametrize("offset", [0, 1])
+def test_token(sata, B, H, G, cap, dk, dv, dtype, lengths, offset):
+    _say("softmax token", B, H, G, cap, dk, dv, dtype, lengths, offset)
+    K, V, q, k, v = _rand(cap, dtype, (B, H, cap, dk), (B, H, cap, dv), (B, H * G, dk), (B, H, dk), (B, H, dv),
+                          offset=offset)
+    for b, e in enumerate(lengths):  # rows behind a sequence may hold anything
+        K[b, :, max(e, 0):], V[b, :, max(e, 0):] = math.nan, math.inf
+    at = _lengths(lengths)
+    ry, rK, rV = pair_ref.softmax_step(K, V, lengths, q, k, v)
+    y = sata.softmax_step(K, V, at, q, k, v)
+    torch.cuda.synchronize()
+    pair_ref.check(y, ry, "y")
+    assert torch.equal(K.cpu().nan_to_num(7.0), rK.nan_to_num(7.0)) and torch.equal(V.cpu(), rV)
+    assert at.tolist() == lengths
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_prompt_then_tokens(sata, dtype):
+    """Tokens over the cache of a prompt are the rows of the longer prompt."""
+    _say("softmax prompt, then tokens", dtype)
+    ends, n, steps = [60, 33], 60, 12
+    q, k, v, _ = _prompt(5, 2, 2, 2, n + steps, 32, 48, dtype)
+    K, V = torch.full_like(k, math.nan), torch.full_like(v, math.nan)
+    K[:, :, :n], V[:, :, :n] = k[:, :, :n], v[:, :, :n]
+    at = _lengths(ends)
+    ys = []
+    for t in range(steps):
+        row = lambda x: torch.stack([x[b, :, e + t] for b, e in enumerate(ends)])  # noqa: E731
+        ys.append(sata.softmax_step(K, V, at, row(q), row(k), row(v)))
+        at += 1
+    torch.cuda.synchronize()
+    ref = pair_ref.softmax_prefill(q, k, v)[0]
+    for t, y in enumerate(ys):
+        for b, e in enumerate(ends):
+            pair_ref.check(y[b], (ref[0][b, :, e + t], ref[1][b, :, e + t]), f"token {t} of {b}")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_values_that_are_not_finite(sata, dtype, bad):
+    n, ends, at = 200, [150, 200], 100
+    _say("softmax, not finite", dtype, bad)
+    q, k, v, dy = _prompt(6, 2, 2, 2, n, 40, 24, dtype)
+    lens = _lengths(ends)
+    y, lse = sata.softmax_prefill(q, k, v, lens)
+    grads = sata.softmax_backward(q, k, v, y, lse, dy, lens)
+    holes = [x.clone() for x in (q, k, v, dy, y, lse)]
+    for x in holes:
+        x[0, :, ends[0]:] = bad
+    y2, lse2 = sata.softmax_prefill(*holes[:3], lens)
+    assert torch.equal(y2, y) and torch.equal(lse2, lse)
+    for a, b in zip(sata.softmax_backward(*holes[:3], holes[4], holes[5], holes[3], lens), grads):
+        assert torch.equal(a, b)
+    for x in (1, 2):
+        args = [t.clone() for t in (q, k, v)]
+        args[x][1, 1, at, 3] = bad
+        y2, lse2 = sata.softmax_prefill(*args, lens)
+        assert torch.equal(y2[0], y[0]) and torch.equal(y2[1, :2], y[1, :2])
+        assert torch.equal(y2[1, 2:, :at], y[1, 2:, :at]) and torch.equal(lse2[1, 2:, :at], lse[1, 2:, :at])
+        assert not torch.isfinite(y2[1, 2:, at]).all()
+        dq = sata.softmax_backward(*args, y2, lse2, dy, lens)[0]
+        assert torch.equal(dq[1, 2:, :at], grads[0][1, 2:, :at]) and torch.equal(dq[1, :2], grads[0][1, :2])
+    args = [t.clone() for t in (q, dy)]
+    args[0][1, 3, at, 0] = bad
+    args[1][1, 3, at, 0] = bad
+    y2, lse2 = sata.softmax_prefill(args[0], k, v, lens)
+    keep = torch.arange(n, device="cuda") != at
+    assert torch.equal(y2[:, :, keep], y[:, :, keep]) and torch.equal(lse2[:, :, keep], lse[:, :, keep])
+    got = sata.softmax_backward(args[0], k, v, y2, lse2, args[1], lens)
+    assert torch.equal(got[0][:, :, keep], grads[0][:, :, keep])
+    for a, b in zip(got[1:], grads[1:]):
+        assert torch.equal(a[1, 1, at + 1:], b[1, 1, at + 1:]) and torch.equal(a[1, 0], b[1, 0]) and torch.equal(a[0], b[0])
+        assert not torch.isfinite(a[1, 1, at]).all()
+
+
+def test_streams_and_repeats(sata):
+    q, k, v, dy = _prompt(7, 2, 3, 2, 400, 64, 64, "bf16")
+    y, lse = sata.softmax_prefill(q, k, v)
+    want = [y, lse, *sata.softmax_backward(q, k, v, y, lse, dy)]
+    torch.cuda.synchronize()
+    streams, runs = [torch.cuda.Stream(), torch.cuda.Stream()], []
+    for _ in range(2):
+        for s in streams:
+            with torch.cuda.stream(s):
+                a, b = sata.softmax_prefill(q, k, v)
+                runs.append([a, b, *sata.softmax_backward(q, k, v, a, b, dy)])
+    torch.cuda.synchronize()
+    for r in runs:
+        assert all(torch.equal(a, b) for a, b in zip(r, want))
+
+
+def test_captured(sata):
+    """Prompt, gradients and tokens in one graph, replayed with other inputs and eager work in between; the
+    lengths move on inside the graph."""
+    make = lambda seed: _prompt(seed, 1, 2, 2, 300, 32, 64, "bf16")  # noqa: E731
+    held = make(8)
+    at = torch.tensor([100], dtype=torch.int32, device="cuda")
+    tok = [held[0][:, :, 5].contiguous(), held[1][:, :, 5].contiguous(), held[2][:, :, 5].contiguous()]
+    stream = torch.cuda.Stream()
+
+    def work(h, K, V, at):
+        y, lse = sata.softmax_prefill(*h[:3])
+        out = [y, lse, *sata.softmax_backward(*h[:3], y, lse, h[3])]
+        K.copy_(h[1])
+        V.copy_(h[2])
+        for _ in range(2):
+            out.append(sata.softmax_step(K, V, at, *tok))
+            at += 1
+        return out + [K, V]
+
+    K, V = torch.zeros_like(held[1]), torch.zeros_like(held[2])
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        work(held, K, V, at)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        out = work(held, K, V, at)
+    for seed in (9, 10, 11):
+        before = at.clone()
+        with torch.cuda.stream(stream):
+            for a, b in zip(held, make(seed)):
+                a.copy_(b)
+            graph.replay()
+        stream.synchronize()
+        assert at.item() == before.item() + 2
+        want = work(held, torch.zeros_like(K), torch.zeros_like(V), before)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want))
