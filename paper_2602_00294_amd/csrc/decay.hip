@@ -10,14 +10,11 @@
 
 #include "device_common.hpp"
 #include "kernels.hpp"
+#include "pair_tiles.hpp"
 
 namespace sata {
 
 namespace {
-
-__device__ __forceinline__ int tokens_of(const int* lengths, int b, int n) {
-  return lengths ? min(max(lengths[b], 0), n) : n;
-}
 
 // exp(g)^e as a float pair.  A single float would do for one factor, but the state is
 // multiplied by the same one at every step: its error (2^-25) would grow with the

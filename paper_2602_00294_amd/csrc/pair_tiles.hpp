@@ -1,0 +1,326 @@
+// Tiles of rows in LDS and 32 x 32 matrix products of them, for the kernels of
+// softmax attention and of linear attention with a decay.
+//
+// Products are v_mfma_f32_32x32x16_bf16.  Lane l (l31 = l % 32, h = l / 32) holds row
+// (left operand) or column (right operand) l31 of a 32 x 16 operand, entries 8 h .. +7
+// of the contraction, and column l31, rows 8 (i / 4) + 4 h + i % 4 of a result's 16
+// numbers.  So numbers 0..7 and 8..15 of a result are, lane by lane, the right (or
+// left) operands of a product that contracts over the result's rows 0..15 and
+// 16..31, with the rows in the order {4 h .. +3, 8 + 4 h .. +3}: load_transposed reads
+// the other operand in that order, and probabilities and states never leave their
+// lanes.
+//
+// A tile holds rows of a tensor as they lie in memory, bfloat16, float32 ones as three
+// bfloat16 numbers (planes) whose sum carries 24 bits; a product of two such numbers is
+// the six partial products of order 2^-16 and up, accumulated in float32.  Rows are
+// whole 64, 128 or 256 bytes; the 16-byte units of a row change places by
+// its number, so that both ways of reading, along 16 or more rows and transposed by
+// four rows of 64 bytes, meet every bank once.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include "device_common.hpp"
+#include "series.hpp"
+
+namespace sata {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+__device__ __forceinline__ f32x16 mfma32(const uint4& a, const uint4& b, const f32x16& c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0,
+                                                 0);
+}
+// sum of the products a[i] b[j] with i + j <= MAX, smallest first
+template <int MAX = 2, int NA, int NB>
+__device__ __forceinline__ f32x16 dot_planes32(const uint4 (&a)[NA], const uint4 (&b)[NB], f32x16 c) {
+#pragma unroll
+  for (int t = MAX; t >= 0; --t)
+#pragma unroll
+    for (int i = 0; i <= t; ++i)
+      if (i < NA && t - i < NB) c = mfma32(a[i], b[t - i], c);
+  return c;
+}
+__device__ __forceinline__ f32x16 zero16() {
+  f32x16 z;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) z[i] = 0.f;
+  return z;
+}
+// Idle cycles between a 32 x 32 matrix instruction and a branch behind which its
+// results are read or overwritten (see settle_mfma for the compiler's distance
+// across branches).
+__device__ __forceinline__ void settle_mfma32() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_nop 15\n\ts_nop 3");
+  __builtin_amdgcn_sched_barrier(0);
+}
+// Row of a result's number i.
+__device__ __forceinline__ int result_row(int i, int h) { return 8 * (i >> 2) + 4 * h + (i & 3); }
+
+// N values (a multiple of 8) as operands of PL planes each; x is used up.
+template <int PL, int N>
+__device__ __forceinline__ void to_planes(float (&x)[N], uint4 (&op)[N / 8][PL]) {
+#pragma unroll
+  for (int s = 0; s < N / 8; ++s)
+#pragma unroll
+    for (int p = 0; p < PL; ++p) {
+      op[s][p] = to_bf16(x + 8 * s);
+      if (p + 1 < PL) take_bf16(op[s][p], x + 8 * s);
+    }
+}
+
+// ROWS rows of up to 32 ND columns of type T (u16: bfloat16 bits, or float).
+template <typename T, int ND, int ROWS>
+struct PairTile {
+  static constexpr int kPl = sizeof(T) == 4 ? 3 : 1;
+  static constexpr int kUnits = ND == 1 ? 4 : ND == 2 ? 8 : 16;  // 16-byte units in a row of a plane
+  static constexpr int kRow = 8 * kUnits;                        // u16
+  static constexpr int kPlane = ROWS * kRow;
+  static constexpr int kElems = kPl * kPlane;
+  static constexpr int kBytes = 2 * kElems;
+
+  // Where a row's unit 0 is put; unit u is at u ^ swap(row).
+  __device__ static __forceinline__ int swap(int row) {
+    if constexpr (kUnits == 16) return ((row & 3) << 2) | ((row >> 2) & 3);
+    else if constexpr (kUnits == 8) return (((row >> 1) & 1) << 2) | ((row >> 2) & 3);
+    else return (row >> 2) & 3;
+  }
+  __device__ static __forceinline__ int at(int row, int col) { return row * kRow + 8 * ((col >> 3) ^ swap(row)) + (col & 7); }
+
+  // Operand of rows r0 .. r0 + 31 (r0 a multiple of 32), entries 16 s .. +15.
+  __device__ static __forceinline__ void load_rows(const u16* t, int r0, int s, uint4 (&op)[kPl]) {
+    const int lane = threadIdx.x & 63, l31 = lane & 31, h = lane >> 5;
+    const u16* const p = t + (r0 + l31) * kRow + 8 * ((2 * s + h) ^ swap(l31));
+#pragma unroll
+    for (int i = 0; i < kPl; ++i) op[i] = *(const uint4*)(p + i * kPlane);
+  }
+  // Operand of columns 32 j .. +31 over the 16 rows from r0 (a multiple of 16).
+  __device__ static __forceinline__ void load_transposed(const u16* t, int r0, int j, uint4 (&op)[kPl]) {
+    const int lane = threadIdx.x & 63, l15 = lane & 15, g = (lane >> 4) & 1, h = lane >> 5;
+    const int row = 4 * h + (l15 >> 2), unit = 4 * j + 2 * g + ((l15 & 3) >> 1), half = 4 * (l15 & 1);
+    const u16* const a = t + (r0 + row) * kRow + 8 * (unit ^ swap(row)) + half;
+    const u16* const b = t + (r0 + row + 8) * kRow + 8 * (unit ^ swap(row + 8)) + half;
+#pragma unroll
+    for (int i = 0; i < kPl; ++i) op[i] = read_transposed(a + i * kPlane, (int)(b - a));
+  }
+  __device__ static __forceinline__ float value(const u16* t, int row, int col) {
+    float x = 0.f;
+#pragma unroll
+    for (int i = kPl - 1; i >= 0; --i) x += __uint_as_float((uint32_t)t[i * kPlane + at(row, col)] << 16);
+    return x;
+  }
+};
+
+// The entries of a plane that are infinite or NaN, all bits of each set.
+__device__ __forceinline__ uint4 not_finite_entries(const uint4& w) {
+  auto wide = [](uint32_t x) { return ((((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u) >> 15) * 0xffffu; };
+  return uint4{wide(w.x), wide(w.y), wide(w.z), wide(w.w)};
+}
+
+// acc[j] += (rows r0 .. r0 + 31 of the tile, columns 32 j .. +31)^T times the 32 x 32 weights w.
+template <typename L, int ND>
+__device__ __forceinline__ void contract32(const u16* t, int r0, const uint4 (&w)[2][L::kPl], f32x16 (&acc)[ND]) {
+#pragma unroll
+  for (int j = 0; j < ND; ++j)
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      uint4 a[L::kPl];
+      L::load_transposed(t, r0 + 16 * s, j, a);
+      acc[j] = dot_planes32(a, w[s], acc[j]);
+    }
+}
+
+// Whether rows r0 .. r0 + 31 of the tile hold a value that is not finite (for the whole wave).
+template <typename L, int ND>
+__device__ __forceinline__ bool tile_not_finite(const u16* t, int r0) {
+  uint32_t bad = 0;
+#pragma unroll
+  for (int s = 0; s < 2 * ND; ++s) {
+    uint4 a[L::kPl];
+    L::load_rows(t, r0, s, a);
+    const uint4 m = not_finite_entries(a[0]);
+    bad |= m.x | m.y | m.z | m.w;
+  }
+  return __ballot(bad != 0) != 0;
+}
+
+// contract32 where w is zero for the rows that its columns do not see and some of the
+// values there are not finite, which would not be zero times 0.  They are left out of
+// the product, and a product of marks with the rows seen (allowed(row) of this lane's
+// column) tells which results have one: those are NaN.
+template <typename L, int ND, typename F>
+__device__ __forceinline__ void contract32_own(const u16* t, int r0, const uint4 (&w)[2][L::kPl], f32x16 (&acc)[ND],
+                                               F&& allowed) {
+  const int h = (threadIdx.x & 63) >> 5;
+  uint4 seen[2];
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = allowed(result_row(8 * s + i, h)) ? 1.f : 0.f;
+    seen[s] = to_bf16(x);
+  }
+#pragma unroll
+  for (int j = 0; j < ND; ++j) {
+    f32x16 count = zero16();
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      uint4 a[L::kPl];
+      L::load_transposed(t, r0 + 16 * s, j, a);
+      const uint4 m = not_finite_entries(a[0]);
+      count = mfma32(uint4{m.x & 0x3f803f80u, m.y & 0x3f803f80u, m.z & 0x3f803f80u, m.w & 0x3f803f80u}, seen[s], count);
+#pragma unroll
+      for (int i = 0; i < L::kPl; ++i) a[i].x &= ~m.x, a[i].y &= ~m.y, a[i].z &= ~m.z, a[i].w &= ~m.w;
+      acc[j] = dot_planes32(a, w[s], acc[j]);
+    }
+    settle_mfma32();
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[j][i] = count[i] > 0.f ? __uint_as_float(0x7fc00000u) : acc[j][i];
+  }
+}
+
+// A tensor's rows on their way to a tile of THREADS threads' workgroup: 16-byte vectors
+// where rows allow them (width a multiple of a vector, base aligned), else entries.  Rows
+// at and behind `rows` read as zero.  The columns behind the width are never written:
+// the tile is cleared once before.
+template <typename T, int ND, int ROWS, int THREADS>
+struct TileStage {
+  using L = PairTile<T, ND, ROWS>;
+  static constexpr int kEV = 16 / sizeof(T);
+  static constexpr int kIt = (ROWS * 32 * ND / kEV + THREADS - 1) / THREADS;
+  const T* base;
+  int rows, width, tid;
+  bool vec;
+  VectorReader read;
+  uint4 r[kIt];
+
+  __device__ void init(const T* p, int rows_, int width_, int tid_) {
+    base = p, rows = rows_, width = width_, tid = tid_;
+    vec = width % kEV == 0 && ((uintptr_t)p & 15) == 0;
+    read = VectorReader(p, vec ? (int64_t)rows * width * (int)sizeof(T) : 0);
+  }
+  // the chunk of ROWS rows from r0 (a whole number of vectors from the tensor's start where vec)
+  __device__ void fetch(int r0) {
+    const int total = ROWS * width / kEV;
+    const uint32_t start = (uint32_t)r0 * (uint32_t)(width * (int)sizeof(T));
+#pragma unroll
+    for (int i = 0; i < kIt; ++i) {
+      const int v = tid + i * THREADS;
+      r[i] = read(v < total ? start + 16u * v : kNoVector);
+    }
+  }
+  __device__ static void put_entry(u16* dst, T x) {
+    if constexpr (sizeof(T) == 4) {
+      float f = x;
+#pragma unroll
+      for (int i = 0; i < L::kPl; ++i) {
+        const uint32_t b = pack2(f, 0.f);
+        dst[i * L::kPlane] = (u16)b;
+        f -= lo_f32(b);
+      }
+    } else {
+      dst[0] = x;
+    }
+  }
+  __device__ void put(u16* t, int r0) const {
+    if (vec) {
+      const int nv = width / kEV;
+#pragma unroll
+      for (int i = 0; i < kIt; ++i) {
+        const int v = tid + i * THREADS, row = v / nv, col = (v - row * nv) * kEV;
+        if (row >= ROWS) continue;
+        u16* const dst = t + L::at(row, col);
+        if constexpr (sizeof(T) == 4) {
+          float x[4] = {__uint_as_float(r[i].x), __uint_as_float(r[i].y), __uint_as_float(r[i].z), __uint_as_float(r[i].w)};
+#pragma unroll
+          for (int pl = 0; pl < L::kPl; ++pl) {
+            const uint2 b = {pack2(x[0], x[1]), pack2(x[2], x[3])};
+            *(uint2*)(dst + pl * L::kPlane) = b;
+            x[0] -= lo_f32(b.x), x[1] -= hi_f32(b.x), x[2] -= lo_f32(b.y), x[3] -= hi_f32(b.y);
+          }
+        } else {
+          *(uint4*)dst = r[i];
+        }
+      }
+    } else {
+      for (int i = tid; i < ROWS * width; i += THREADS) {
+        const int row = i / width;
+        put_entry(t + L::at(row, i - row * width),
+                  r0 + row < rows ? base[(int64_t)r0 * width + i] : (T)0);
+      }
+    }
+  }
+};
+
+// Right (or left) operands of one row per lane pair: entries 16 s + 8 h .. +7, all planes;
+// zero past the width and where !ok.
+template <typename T, int ND>
+__device__ __forceinline__ void load_own32(const T* p, bool ok, int width, uint4 (&f)[2 * ND][sizeof(T) == 4 ? 3 : 1]) {
+  const int h = (threadIdx.x & 63) >> 5;
+  const bool vec = sizeof(T) == 2 && width % 8 == 0 && ((uintptr_t)p & 15) == 0;
+#pragma unroll
+  for (int s = 0; s < 2 * ND; ++s) {
+    const int c0 = 16 * s + 8 * h;
+    if constexpr (sizeof(T) == 4) {
+      float x[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = ok && c0 + j < width ? p[c0 + j] : 0.f;
+#pragma unroll
+      for (int i = 0; i < 3; ++i) {
+        f[s][i] = to_bf16(x);
+        take_bf16(f[s][i], x);
+      }
+    } else {
+      uint4 w = {0u, 0u, 0u, 0u};
+      if (vec) {
+        if (ok && c0 < width) w = *(const uint4*)(p + c0);
+      } else {
+        uint32_t u[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (ok && c0 + j < width) u[j >> 1] |= (uint32_t)p[c0 + j] << (16 * (j & 1));
+        w = uint4{u[0], u[1], u[2], u[3]};
+      }
+      f[s][0] = w;
+    }
+  }
+}
+
+// Four values of a row, columns c0 .. +3 (those below the width).
+template <typename T>
+__device__ __forceinline__ void store4(T* p, int c0, int width, const float (&x)[4], bool vec) {
+  if (vec) {
+    if (c0 < width) {
+      if constexpr (sizeof(T) == 4) *(float4*)(p + c0) = float4{x[0], x[1], x[2], x[3]};
+      else *(uint2*)(p + c0) = uint2{pack2(x[0], x[1]), pack2(x[2], x[3])};
+    }
+  } else {
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if (c0 + r < width) {
+        if constexpr (sizeof(T) == 4) p[c0 + r] = x[r];
+        else p[c0 + r] = (T)(pack2(x[r], 0.f) & 0xffffu);
+      }
+  }
+}
+// A lane's part of one output row: columns 32 j + 8 i + 4 h .. +3 of results acc[j], scaled.
+template <typename T, int ND>
+__device__ __forceinline__ void store_row32(T* p, int width, const f32x16 (&acc)[ND], float scale) {
+  const int h = (threadIdx.x & 63) >> 5;
+  const bool vec = width % 4 == 0 && ((uintptr_t)p & (4 * sizeof(T) - 1)) == 0;
+#pragma unroll
+  for (int j = 0; j < ND; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float x[4] = {acc[j][4 * i] * scale, acc[j][4 * i + 1] * scale, acc[j][4 * i + 2] * scale,
+                          acc[j][4 * i + 3] * scale};
+      store4(p, 32 * j + 8 * i + 4 * h, width, x, vec);
+    }
+}
+
+__device__ __forceinline__ int tokens_of(const int* lengths, int b, int n) {
+  return lengths ? min(max(lengths[b], 0), n) : n;
+}
+
+}  // namespace sata

@@ -6,16 +6,15 @@
 // and its single step over a cache.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "device_common.hpp"
 #include "kernels.hpp"
+#include "pair_tiles.hpp"
 
 namespace sata {
 
 namespace {
-
-__device__ __forceinline__ int tokens_of(const int* lengths, int b, int n) {
-  return lengths ? min(max(lengths[b], 0), n) : n;
-}
 
 __device__ __forceinline__ float wave_sum(float x) {
 #pragma unroll
@@ -58,16 +57,156 @@ __device__ __forceinline__ float attend(const T* q, const T* k, const T* v, int 
   return keys > 0 ? logf(l) + m : -INFINITY;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(64) softmax_prefill_kernel(SoftmaxArgs a) {
-  const int t = blockIdx.x;
-  const int64_t qh = blockIdx.y, kvh = qh / a.G;
-  const int len = tokens_of(a.lengths, (int)(kvh / a.H), a.n);
-  float2 y;
-  const float lse = attend((const T*)a.q + (qh * a.n + t) * a.dk_, (const T*)a.k + kvh * a.n * a.dk_,
-                           (const T*)a.v + kvh * a.n * a.dv_, t < len ? t + 1 : 0, a.dk_, a.dv_, a.scale, y);
-  put_row((T*)a.y + (qh * a.n + t) * a.dv_, a.dv_, y);
-  if (a.lse && threadIdx.x == 0) a.lse[qh * a.n + t] = lse;
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLn2 = 0.69314718055994530942f;
+
+// v_exp_f32: within 1 ulp, results below 2^-126 are zero.
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// Workgroups go to the 8 XCDs in turn.  With 8 heads or more each XCD takes whole
+// heads, one after the other, so that a head's rows are read through one L2.
+__device__ __forceinline__ bool locate(int heads, int blocks, int& head, int& blk) {
+  if (heads >= 8) {
+    const int j = blockIdx.x >> 3;
+    head = (j / blocks) * 8 + (int)(blockIdx.x & 7);
+    blk = j % blocks;
+    return head < heads;
+  }
+  head = blockIdx.x % heads;
+  blk = blockIdx.x / heads;
+  return true;
+}
+inline int64_t head_blocks(int heads, int blocks) {
+  return (int64_t)blocks * (heads >= 8 ? ((int64_t)heads + 7) / 8 * 8 : heads);
+}
+
+// One workgroup of W waves per 32 W queries of a head, 32 to a wave, which are the columns
+// of its scores and outputs; the keys are walked in tiles of 32.  The exponentials' base
+// moves only when a score passes it by 2^8 (in either half of the lanes), so the outputs are rarely scaled.
+template <typename T, int ND, int W>
+__global__ void __launch_bounds__(64 * W, sizeof(T) == 2 ? 2 : 1) softmax_prefill_kernel(SoftmaxArgs a, int blocks) {
+  constexpr int kWaves = W, kThreads = 64 * W;
+  constexpr int kKeys = sizeof(T) == 2 ? 64 : 32;  // keys staged at a time
+  using L = PairTile<T, ND, kKeys>;
+  extern __shared__ __attribute__((aligned(16))) u16 smem16[];
+  const int tid = threadIdx.x, lane = tid & 63, l31 = lane & 31, h = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  int qh, blk;
+  if (!locate(a.heads * a.G, blocks, qh, blk)) return;
+  blk = blocks - 1 - blk;  // the longest first
+  const int kvh = qh / a.G, n = a.n, dk = a.dk_, dv = a.dv_;
+  const int len = tokens_of(a.lengths, kvh / a.H, n);
+  const int q0 = 32 * (kWaves * blk + wave), row = q0 + l31;
+  T* const yp = (T*)a.y + ((int64_t)qh * n + row) * dv;
+  f32x16 o[ND];
+#pragma unroll
+  for (int j = 0; j < ND; ++j) o[j] = zero16();
+  float top = -3.4028234e38f, sum = 0.f;
+  const int end = min(len, 32 * kWaves * (blk + 1));  // keys that this workgroup sees
+  if (32 * kWaves * blk < len) {
+    for (int i = tid; i < 4 * L::kElems / 8; i += kThreads) ((uint4*)smem16)[i] = uint4{0u, 0u, 0u, 0u};
+    TileStage<T, ND, kKeys, kThreads> sk, sv;
+    sk.init((const T*)a.k + (int64_t)kvh * n * dk, len, dk, tid);
+    sv.init((const T*)a.v + (int64_t)kvh * n * dv, len, dv, tid);
+    uint4 qf[2 * ND][L::kPl];
+    load_own32<T, ND>((const T*)a.q + ((int64_t)qh * n + row) * dk, row < len, dk, qf);
+    const float c = a.scale * kLog2e;
+    // keys r0 .. +31 of a staged block; own: the queries' own tile, of which each sees its part
+    auto work = [&](const u16* kt, const u16* vt, int r0, bool own) {
+      f32x16 s = zero16();
+#pragma unroll
+      for (int i = 0; i < 2 * ND; ++i) {
+        uint4 f[L::kPl];
+        L::load_rows(kt, r0, i, f);
+        s = dot_planes32(f, qf[i], s);
+      }
+      settle_mfma32();
+      bool odd = false;
+      if (own) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = result_row(i, h) > l31 ? -INFINITY : s[i];
+        odd = tile_not_finite<L, ND>(vt, r0);
+      }
+      float z[16], most = -3.4028234e38f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        z[i] = s[i] * c;
+        most = fmaxf(most, z[i]);
+      }
+      if (__ballot(most > top + 8.f)) {
+        const float next = fmaxf(top, fmaxf(most, __shfl_xor(most, 32)));
+        const float keep = exp2_fast(top - next);
+        top = next;
+        sum *= keep;
+#pragma unroll
+        for (int j = 0; j < ND; ++j)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[j][i] *= keep;
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        z[i] = exp2_fast(z[i] - top);
+        sum += z[i];
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      uint4 w[2][L::kPl];
+      to_planes<L::kPl>(z, w);
+      if (__builtin_expect(odd, 0)) contract32_own<L, ND>(vt, r0, w, o, [&](int key) { return key <= l31; });
+      else contract32<L, ND>(vt, r0, w, o);
+    };
+    __syncthreads();
+    sk.fetch(0);
+    sv.fetch(0);
+    sk.put(smem16, 0);
+    sv.put(smem16 + L::kElems, 0);
+    __syncthreads();
+    const int steps = (end + kKeys - 1) / kKeys;
+    for (int st = 0; st < steps; ++st) {
+      const bool more = st + 1 < steps;
+      if (more) {
+        sk.fetch((st + 1) * kKeys);
+        sv.fetch((st + 1) * kKeys);
+      }
+      const u16* const kt = smem16 + (st & 1) * 2 * L::kElems;
+      const u16* const vt = kt + L::kElems;
+#pragma unroll 1
+      for (int r = 0; r < kKeys; r += 32) {
+        const int k0 = st * kKeys + r;
+        if (k0 <= q0) work(kt, vt, r, k0 == q0);
+      }
+      if (more) {
+        sk.put(smem16 + ((st + 1) & 1) * 2 * L::kElems, (st + 1) * kKeys);
+        sv.put(smem16 + ((st + 1) & 1) * 2 * L::kElems + L::kElems, (st + 1) * kKeys);
+      }
+      __syncthreads();
+    }
+    settle_mfma32();
+  }
+  if (row >= n) return;
+  sum += __shfl_xor(sum, 32);
+  store_row32<T, ND>(yp, dv, o, row < len ? 1.f / sum : 0.f);
+  if (a.lse && h == 0) a.lse[(int64_t)qh * n + row] = row < len ? top * kLn2 + logf(sum) : -INFINITY;
+}
+
+template <typename T, int ND, int W>
+hipError_t launch_prefill_w(const SoftmaxArgs& a, hipStream_t s) {
+  constexpr int kKeys = sizeof(T) == 2 ? 64 : 32;
+  constexpr int bytes = 4 * PairTile<T, ND, kKeys>::kBytes;
+  static_assert(bytes <= 160 * 1024, "LDS of one workgroup");
+  auto kern = softmax_prefill_kernel<T, ND, W>;
+  if (bytes > 64 * 1024) {
+    hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != hipSuccess) return e;
+  }
+  const int blocks = (a.n + 32 * W - 1) / (32 * W);
+  hipLaunchKernelGGL(kern, dim3((unsigned)head_blocks(a.heads * a.G, blocks)), dim3(64 * W), bytes, s, a, blocks);
+  return hipGetLastError();
+}
+
+template <typename T, int ND>
+hipError_t launch_prefill(const SoftmaxArgs& a, hipStream_t s) {
+  if (sizeof(T) == 2 && (int64_t)a.heads * a.G * ((a.n + 255) / 256) >= 256) return launch_prefill_w<T, ND, 8>(a, s);
+  return launch_prefill_w<T, ND, 4>(a, s);
 }
 
 template <typename T>
@@ -138,10 +277,12 @@ __global__ void __launch_bounds__(64) softmax_step_kernel(SoftmaxStepArgs a) {
 }  // namespace
 
 hipError_t launch_softmax_prefill(const SoftmaxArgs& a, bool bf16, hipStream_t s) {
-  const dim3 grid(a.n, a.heads * a.G);
-  if (bf16) hipLaunchKernelGGL(softmax_prefill_kernel<bf16_t>, grid, dim3(64), 0, s, a);
-  else hipLaunchKernelGGL(softmax_prefill_kernel<float>, grid, dim3(64), 0, s, a);
-  return hipGetLastError();
+  switch ((std::max(a.dk_, a.dv_) + 31) / 32) {
+    case 1: return bf16 ? launch_prefill<u16, 1>(a, s) : launch_prefill<float, 1>(a, s);
+    case 2: return bf16 ? launch_prefill<u16, 2>(a, s) : launch_prefill<float, 2>(a, s);
+    case 3: return bf16 ? launch_prefill<u16, 3>(a, s) : launch_prefill<float, 3>(a, s);
+    default: return bf16 ? launch_prefill<u16, 4>(a, s) : launch_prefill<float, 4>(a, s);
+  }
 }
 
 hipError_t launch_softmax_backward(const SoftmaxGradArgs& a, bool bf16, hipStream_t s) {
