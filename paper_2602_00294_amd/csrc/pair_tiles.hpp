@@ -304,19 +304,44 @@ __device__ __forceinline__ void store4(T* p, int c0, int width, const float (&x)
       }
   }
 }
-// A lane's part of one output row: columns 32 j + 8 i + 4 h .. +3 of results acc[j], scaled.
+// A lane's part of one output row: columns 32 j + 8 i + 4 h .. +3 of results acc[j], scaled,
+// or zeros.
 template <typename T, int ND>
-__device__ __forceinline__ void store_row32(T* p, int width, const f32x16 (&acc)[ND], float scale) {
+__device__ __forceinline__ void store_row32(T* p, int width, const f32x16 (&acc)[ND], float scale, bool zero) {
   const int h = (threadIdx.x & 63) >> 5;
   const bool vec = width % 4 == 0 && ((uintptr_t)p & (4 * sizeof(T) - 1)) == 0;
 #pragma unroll
   for (int j = 0; j < ND; ++j)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float x[4] = {acc[j][4 * i] * scale, acc[j][4 * i + 1] * scale, acc[j][4 * i + 2] * scale,
-                          acc[j][4 * i + 3] * scale};
+      float x[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) x[r] = zero ? 0.f : acc[j][4 * i + r] * scale;
       store4(p, 32 * j + 8 * i + 4 * h, width, x, vec);
     }
+}
+
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLn2 = 0.69314718055994530942f;
+
+// v_exp_f32: within 1 ulp, results below 2^-126 are zero.
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// Workgroups go to the 8 XCDs in turn.  With 8 heads or more each XCD takes whole
+// heads, one after the other, so that a head's rows are read through one L2.
+__device__ __forceinline__ bool locate(int heads, int blocks, int& head, int& blk) {
+  if (heads >= 8) {
+    const int j = blockIdx.x >> 3;
+    head = (j / blocks) * 8 + (int)(blockIdx.x & 7);
+    blk = j % blocks;
+    return head < heads;
+  }
+  head = blockIdx.x % heads;
+  blk = blockIdx.x / heads;
+  return true;
+}
+inline int64_t head_blocks(int heads, int blocks) {
+  return (int64_t)blocks * (heads >= 8 ? ((int64_t)heads + 7) / 8 * 8 : heads);
 }
 
 __device__ __forceinline__ int tokens_of(const int* lengths, int b, int n) {

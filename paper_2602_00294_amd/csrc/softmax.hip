@@ -1,8 +1,5 @@
 // Exact causal softmax attention: with c = 1 / sqrt(d_k),
 //     lse_t = log sum_{s<=t} exp(c q_t.k_s),  p_ts = exp(c q_t.k_s - lse_t),  y_t = sum_{s<=t} p_ts v_s,
-// its gradients with the probabilities computed again from lse,
-//     dv_s = sum_{t>=s} p_ts dy_t,   e_ts = c p_ts (dy_t.v_s - dy_t.y_t),
-//     dq_t = sum_{s<=t} e_ts k_s,    dk_s = sum_{t>=s} e_ts q_t,
 // and its single step over a cache.
 #include <hip/hip_runtime.h>
 
@@ -55,29 +52,6 @@ __device__ __forceinline__ float attend(const T* q, const T* k, const T* v, int 
   const float r = keys > 0 ? 1.f / l : 0.f;
   y.x *= r, y.y *= r;
   return keys > 0 ? logf(l) + m : -INFINITY;
-}
-
-constexpr float kLog2e = 1.44269504088896340736f;
-constexpr float kLn2 = 0.69314718055994530942f;
-
-// v_exp_f32: within 1 ulp, results below 2^-126 are zero.
-__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
-
-// Workgroups go to the 8 XCDs in turn.  With 8 heads or more each XCD takes whole
-// heads, one after the other, so that a head's rows are read through one L2.
-__device__ __forceinline__ bool locate(int heads, int blocks, int& head, int& blk) {
-  if (heads >= 8) {
-    const int j = blockIdx.x >> 3;
-    head = (j / blocks) * 8 + (int)(blockIdx.x & 7);
-    blk = j % blocks;
-    return head < heads;
-  }
-  head = blockIdx.x % heads;
-  blk = blockIdx.x / heads;
-  return true;
-}
-inline int64_t head_blocks(int heads, int blocks) {
-  return (int64_t)blocks * (heads >= 8 ? ((int64_t)heads + 7) / 8 * 8 : heads);
 }
 
 // One workgroup of W waves per 32 W queries of a head, 32 to a wave, which are the columns
@@ -184,7 +158,7 @@ __global__ void __launch_bounds__(64 * W, sizeof(T) == 2 ? 2 : 1) softmax_prefil
   }
   if (row >= n) return;
   sum += __shfl_xor(sum, 32);
-  store_row32<T, ND>(yp, dv, o, row < len ? 1.f / sum : 0.f);
+  store_row32<T, ND>(yp, dv, o, 1.f / sum, row >= len);
   if (a.lse && h == 0) a.lse[(int64_t)qh * n + row] = row < len ? top * kLn2 + logf(sum) : -INFINITY;
 }
 
@@ -207,52 +181,6 @@ template <typename T, int ND>
 hipError_t launch_prefill(const SoftmaxArgs& a, hipStream_t s) {
   if (sizeof(T) == 2 && (int64_t)a.heads * a.G * ((a.n + 255) / 256) >= 256) return launch_prefill_w<T, ND, 8>(a, s);
   return launch_prefill_w<T, ND, 4>(a, s);
-}
-
-template <typename T>
-__global__ void __launch_bounds__(64) softmax_rows_kernel(SoftmaxGradArgs a) {
-  const int t = blockIdx.x;
-  const int64_t qh = blockIdx.y, kvh = qh / a.G;
-  const int len = tokens_of(a.lengths, (int)(kvh / a.H), a.n);
-  float2 o = {0.f, 0.f};
-  if (t < len) {
-    const float2 x = row_of((const T*)a.q + (qh * a.n + t) * a.dk_, a.dk_);
-    const float2 d = row_of((const T*)a.dy + (qh * a.n + t) * a.dv_, a.dv_);
-    const float delta = dot(d, row_of((const T*)a.y + (qh * a.n + t) * a.dv_, a.dv_));
-    const float lse = a.lse[qh * a.n + t];
-    if (threadIdx.x == 0) a.delta[qh * a.n + t] = delta;
-    for (int s = 0; s <= t; ++s) {
-      const float2 k = row_of((const T*)a.k + (kvh * a.n + s) * a.dk_, a.dk_);
-      const float p = expf(a.scale * dot(x, k) - lse);
-      const float e = a.scale * p * (dot(d, row_of((const T*)a.v + (kvh * a.n + s) * a.dv_, a.dv_)) - delta);
-      o.x = fmaf(e, k.x, o.x);
-      o.y = fmaf(e, k.y, o.y);
-    }
-  }
-  put_row((T*)a.dq + (qh * a.n + t) * a.dk_, a.dk_, o);
-}
-
-template <typename T>
-__global__ void __launch_bounds__(64) softmax_cols_kernel(SoftmaxGradArgs a) {
-  const int s = blockIdx.x;
-  const int64_t kvh = blockIdx.y;
-  const int len = tokens_of(a.lengths, (int)(kvh / a.H), a.n);
-  float2 gk = {0.f, 0.f}, gv = {0.f, 0.f};
-  if (s < len) {
-    const float2 k = row_of((const T*)a.k + (kvh * a.n + s) * a.dk_, a.dk_);
-    const float2 v = row_of((const T*)a.v + (kvh * a.n + s) * a.dv_, a.dv_);
-    for (int64_t qh = kvh * a.G; qh < (kvh + 1) * a.G; ++qh)
-      for (int t = s; t < len; ++t) {
-        const float2 x = row_of((const T*)a.q + (qh * a.n + t) * a.dk_, a.dk_);
-        const float2 d = row_of((const T*)a.dy + (qh * a.n + t) * a.dv_, a.dv_);
-        const float p = expf(a.scale * dot(x, k) - a.lse[qh * a.n + t]);
-        const float e = a.scale * p * (dot(d, v) - a.delta[qh * a.n + t]);
-        gk.x = fmaf(e, x.x, gk.x), gk.y = fmaf(e, x.y, gk.y);
-        gv.x = fmaf(p, d.x, gv.x), gv.y = fmaf(p, d.y, gv.y);
-      }
-  }
-  put_row((T*)a.dk + (kvh * a.n + s) * a.dk_, a.dk_, gk);
-  put_row((T*)a.dv + (kvh * a.n + s) * a.dv_, a.dv_, gv);
 }
 
 // One wave per query head; the first member of a group writes the cache.
@@ -283,16 +211,6 @@ hipError_t launch_softmax_prefill(const SoftmaxArgs& a, bool bf16, hipStream_t s
     case 3: return bf16 ? launch_prefill<u16, 3>(a, s) : launch_prefill<float, 3>(a, s);
     default: return bf16 ? launch_prefill<u16, 4>(a, s) : launch_prefill<float, 4>(a, s);
   }
-}
-
-hipError_t launch_softmax_backward(const SoftmaxGradArgs& a, bool bf16, hipStream_t s) {
-  if (bf16) hipLaunchKernelGGL(softmax_rows_kernel<bf16_t>, dim3(a.n, a.heads * a.G), dim3(64), 0, s, a);
-  else hipLaunchKernelGGL(softmax_rows_kernel<float>, dim3(a.n, a.heads * a.G), dim3(64), 0, s, a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  if (bf16) hipLaunchKernelGGL(softmax_cols_kernel<bf16_t>, dim3(a.n, a.heads), dim3(64), 0, s, a);
-  else hipLaunchKernelGGL(softmax_cols_kernel<float>, dim3(a.n, a.heads), dim3(64), 0, s, a);
-  return hipGetLastError();
 }
 
 hipError_t launch_softmax_step(const SoftmaxStepArgs& a, bool bf16, hipStream_t s) {

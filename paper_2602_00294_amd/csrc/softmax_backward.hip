@@ -1,0 +1,284 @@
+// Gradients of causal softmax attention, the probabilities computed again from the
+// scores and lse: with c = 1 / sqrt(d_k),
+//     p_ts = exp(c q_t.k_s - lse_t),  e_ts = p_ts (dy_t.v_s - delta_t),  delta_t = dy_t.y_t,
+//     dq_t = c sum_{s<=t} e_ts k_s,   dk_s = c sum_{t>=s} e_ts q_t,      dv_s = sum_{t>=s} p_ts dy_t.
+//
+// Two launches, each sum in the registers of one wave in a fixed order:
+// softmax_rows walks the keys of its queries for dq (and leaves delta),
+// softmax_cols the queries of its keys, of all members of the group, for dk and dv.
+// The scores and dy.v are formed in both: seven products of d columns a pair instead of five, for
+// no sums of dq across workgroups.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "device_common.hpp"
+#include "kernels.hpp"
+#include "pair_tiles.hpp"
+
+namespace sata {
+
+namespace {
+
+template <typename T>
+constexpr int kStaged = sizeof(T) == 2 ? 64 : 32;  // rows staged at a time
+
+// This lane's part of the product of two rows (the other half of the lanes has the rest).
+template <int ND, int PL>
+__device__ __forceinline__ float dot_own(const uint4 (&a)[2 * ND][PL], const uint4 (&b)[2 * ND][PL]) {
+  float r = 0.f;
+#pragma unroll
+  for (int s = 0; s < 2 * ND; ++s) {
+    float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = PL - 1; i >= 0; --i) {
+      const uint32_t u[4] = {a[s][i].x, a[s][i].y, a[s][i].z, a[s][i].w}, w[4] = {b[s][i].x, b[s][i].y, b[s][i].z, b[s][i].w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        x[2 * j] += lo_f32(u[j]), x[2 * j + 1] += hi_f32(u[j]);
+        y[2 * j] += lo_f32(w[j]), y[2 * j + 1] += hi_f32(w[j]);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) r = fmaf(x[j], y[j], r);
+  }
+  return r;
+}
+
+// 32 x 32 products of the tile's rows r0 .. +31 with this wave's rows.
+template <typename L, int ND>
+__device__ __forceinline__ f32x16 dot_rows32(const u16* t, int r0, const uint4 (&own)[2 * ND][L::kPl]) {
+  f32x16 s = zero16();
+#pragma unroll
+  for (int i = 0; i < 2 * ND; ++i) {
+    uint4 f[L::kPl];
+    L::load_rows(t, r0, i, f);
+    s = dot_planes32(f, own[i], s);
+  }
+  return s;
+}
+
+template <typename T, int ND, int W>
+__global__ void __launch_bounds__(64 * W, sizeof(T) == 2 ? 2 : 1) softmax_rows(SoftmaxGradArgs a, int blocks) {
+  constexpr int kRows = kStaged<T>, kThreads = 64 * W;
+  using L = PairTile<T, ND, kRows>;
+  extern __shared__ __attribute__((aligned(16))) u16 smem16[];
+  const int tid = threadIdx.x, lane = tid & 63, l31 = lane & 31, h = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  int qh, blk;
+  if (!locate(a.heads * a.G, blocks, qh, blk)) return;
+  blk = blocks - 1 - blk;  // the longest first
+  const int kvh = qh / a.G, n = a.n, dk = a.dk_, dv = a.dv_;
+  const int len = tokens_of(a.lengths, kvh / a.H, n);
+  const int q0 = 32 * (W * blk + wave), row = q0 + l31;
+  const int64_t at = (int64_t)qh * n + row;
+  f32x16 acc[ND];
+#pragma unroll
+  for (int j = 0; j < ND; ++j) acc[j] = zero16();
+  if (32 * W * blk < len) {
+    for (int i = tid; i < 4 * L::kElems / 8; i += kThreads) ((uint4*)smem16)[i] = uint4{0u, 0u, 0u, 0u};
+    TileStage<T, ND, kRows, kThreads> sk, sv;
+    sk.init((const T*)a.k + (int64_t)kvh * n * dk, len, dk, tid);
+    sv.init((const T*)a.v + (int64_t)kvh * n * dv, len, dv, tid);
+    uint4 qf[2 * ND][L::kPl], df[2 * ND][L::kPl];
+    load_own32<T, ND>((const T*)a.y + at * dv, row < len, dv, qf);
+    load_own32<T, ND>((const T*)a.dy + at * dv, row < len, dv, df);
+    float delta = dot_own<ND>(qf, df);
+    delta += __shfl_xor(delta, 32);
+    if (row < len && h == 0) a.delta[at] = delta;
+    load_own32<T, ND>((const T*)a.q + at * dk, row < len, dk, qf);
+    const float c = a.scale * kLog2e, lse = row < len ? a.lse[at] * kLog2e : 0.f;
+    auto work = [&](const u16* kt, const u16* vt, int r0, bool own) {
+      f32x16 s = dot_rows32<L, ND>(kt, r0, qf), d = dot_rows32<L, ND>(vt, r0, df);
+      float e[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) e[i] = exp2_fast(fmaf(s[i], c, -lse)) * (d[i] - delta);
+      bool odd = false;
+      if (own) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) e[i] = result_row(i, h) > l31 ? 0.f : e[i];
+        odd = tile_not_finite<L, ND>(kt, r0);
+      }
+      uint4 w[2][L::kPl];
+      to_planes<L::kPl>(e, w);
+      if (__builtin_expect(odd, 0)) contract32_own<L, ND>(kt, r0, w, acc, [&](int key) { return key <= l31; });
+      else contract32<L, ND>(kt, r0, w, acc);
+    };
+    __syncthreads();
+    sk.fetch(0);
+    sv.fetch(0);
+    sk.put(smem16, 0);
+    sv.put(smem16 + L::kElems, 0);
+    __syncthreads();
+    const int steps = (min(len, 32 * W * (blk + 1)) + kRows - 1) / kRows;
+    for (int st = 0; st < steps; ++st) {
+      const bool more = st + 1 < steps;
+      if (more) {
+        sk.fetch((st + 1) * kRows);
+        sv.fetch((st + 1) * kRows);
+      }
+      const u16* const kt = smem16 + (st & 1) * 2 * L::kElems;
+#pragma unroll 1
+      for (int r = 0; r < kRows; r += 32) {
+        const int k0 = st * kRows + r;
+        if (k0 <= q0) work(kt, kt + L::kElems, r, k0 == q0);
+      }
+      if (more) {
+        sk.put(smem16 + ((st + 1) & 1) * 2 * L::kElems, (st + 1) * kRows);
+        sv.put(smem16 + ((st + 1) & 1) * 2 * L::kElems + L::kElems, (st + 1) * kRows);
+      }
+      __syncthreads();
+    }
+    settle_mfma32();
+  }
+  if (row < n) store_row32<T, ND>((T*)a.dq + at * dk, dk, acc, row < len ? a.scale : 0.f, row >= len);
+}
+
+template <typename T, int ND, int W>
+__global__ void __launch_bounds__(64 * W, sizeof(T) == 2 && ND <= 2 ? 2 : 1) softmax_cols(SoftmaxGradArgs a, int blocks) {
+  constexpr int kRows = kStaged<T>, kThreads = 64 * W;
+  using L = PairTile<T, ND, kRows>;
+  constexpr int kBuf = 2 * L::kElems + 4 * kRows;  // Q rows, dy rows, then lse and delta as float
+  extern __shared__ __attribute__((aligned(16))) u16 smem16[];
+  const int tid = threadIdx.x, lane = tid & 63, l31 = lane & 31, h = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  int kvh, blk;
+  if (!locate(a.heads, blocks, kvh, blk)) return;  // (the first keys have the longest sweeps)
+  const int n = a.n, dk = a.dk_, dv = a.dv_;
+  const int len = tokens_of(a.lengths, kvh / a.H, n);
+  const int k0 = 32 * (W * blk + wave), row = k0 + l31;
+  const int64_t at = (int64_t)kvh * n + row;
+  f32x16 gk[ND], gv[ND];
+#pragma unroll
+  for (int j = 0; j < ND; ++j) gk[j] = gv[j] = zero16();
+  if (32 * W * blk < len) {
+    for (int i = tid; i < 2 * kBuf / 8; i += kThreads) ((uint4*)smem16)[i] = uint4{0u, 0u, 0u, 0u};
+    uint4 kf[2 * ND][L::kPl], vf[2 * ND][L::kPl];
+    load_own32<T, ND>((const T*)a.k + at * dk, row < len, dk, kf);
+    load_own32<T, ND>((const T*)a.v + at * dv, row < len, dv, vf);
+    const float c = a.scale * kLog2e;
+    auto work = [&](const u16* qt, const u16* yt, const float* stat, int r0, bool own) {
+      f32x16 s = dot_rows32<L, ND>(qt, r0, kf), d = dot_rows32<L, ND>(yt, r0, vf);
+      float p[16], e[16];
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const float4 z4 = *(const float4*)(stat + r0 + 8 * g + 4 * h), d4 = *(const float4*)(stat + kRows + r0 + 8 * g + 4 * h);
+        const float z[4] = {z4.x, z4.y, z4.z, z4.w}, de[4] = {d4.x, d4.y, d4.z, d4.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          p[4 * g + i] = exp2_fast(fmaf(s[4 * g + i], c, -z[i]));
+          e[4 * g + i] = p[4 * g + i] * (d[4 * g + i] - de[i]);
+        }
+      }
+      bool odd_q = false, odd_y = false;
+      if (own) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          p[i] = result_row(i, h) < l31 ? 0.f : p[i];
+          e[i] = result_row(i, h) < l31 ? 0.f : e[i];
+        }
+        odd_q = tile_not_finite<L, ND>(qt, r0);
+        odd_y = tile_not_finite<L, ND>(yt, r0);
+      }
+      uint4 w[2][L::kPl];
+      auto seen = [&](int query) { return query >= l31; };
+      to_planes<L::kPl>(p, w);
+      if (__builtin_expect(odd_y, 0)) contract32_own<L, ND>(yt, r0, w, gv, seen);
+      else contract32<L, ND>(yt, r0, w, gv);
+      to_planes<L::kPl>(e, w);
+      if (__builtin_expect(odd_q, 0)) contract32_own<L, ND>(qt, r0, w, gk, seen);
+      else contract32<L, ND>(qt, r0, w, gk);
+    };
+    TileStage<T, ND, kRows, kThreads> sq, sy;
+    const int first = 32 * W * blk / kRows, steps = (len + kRows - 1) / kRows - first;
+    float st_ = 0.f;
+    int64_t base = 0;  // the member's first row
+    auto open = [&](int g) {
+      base = ((int64_t)kvh * a.G + g) * n;
+      sq.init((const T*)a.q + base * dk, len, dk, tid);
+      sy.init((const T*)a.dy + base * dv, len, dv, tid);
+    };
+    auto fetch = [&](int t0) {
+      sq.fetch(t0);
+      sy.fetch(t0);
+      if (tid < 2 * kRows) {
+        const int t = t0 + tid % kRows;
+        // (a row behind the sequence: probability zero)
+        if (tid < kRows) st_ = t < len ? a.lse[base + t] * kLog2e : INFINITY;
+        else st_ = t < len ? a.delta[base + t] : 0.f;
+      }
+    };
+    auto put = [&](int b, int t0) {
+      u16* const t = smem16 + b * kBuf;
+      sq.put(t, t0);
+      sy.put(t + L::kElems, t0);
+      if (tid < 2 * kRows) ((float*)(t + 2 * L::kElems))[tid] = st_;
+    };
+    __syncthreads();
+    open(0);
+    fetch(first * kRows);
+    put(0, first * kRows);
+    __syncthreads();
+    const int total = steps * a.G;
+    for (int u = 0, st = 0, g = 0; u < total; ++u) {
+      const bool more = u + 1 < total;
+      int next = st + 1;
+      if (next == steps) next = 0;
+      if (more) {
+        if (next == 0) open(++g);
+        fetch((first + next) * kRows);
+      }
+      const u16* const qt = smem16 + (u & 1) * kBuf;
+#pragma unroll 1
+      for (int r = 0; r < kRows; r += 32) {
+        const int t0 = (first + st) * kRows + r;
+        if (t0 >= k0) work(qt, qt + L::kElems, (const float*)(qt + 2 * L::kElems), r, t0 == k0);
+      }
+      if (more) put((u + 1) & 1, (first + next) * kRows);
+      st = next;
+      __syncthreads();
+    }
+    settle_mfma32();
+  }
+  if (row >= n) return;
+  store_row32<T, ND>((T*)a.dk + at * dk, dk, gk, a.scale, row >= len);
+  store_row32<T, ND>((T*)a.dv + at * dv, dv, gv, 1.f, row >= len);
+}
+
+template <typename T, int ND, int W>
+hipError_t launch_backward_w(const SoftmaxGradArgs& a, hipStream_t s) {
+  using L = PairTile<T, ND, kStaged<T>>;
+  constexpr int rows_bytes = 4 * L::kBytes, cols_bytes = 2 * (2 * L::kBytes + 8 * kStaged<T>);
+  static_assert(cols_bytes <= 160 * 1024, "LDS of one workgroup");
+  auto rows = softmax_rows<T, ND, W>;
+  auto cols = softmax_cols<T, ND, W>;
+  if (cols_bytes > 64 * 1024) {
+    hipError_t e = hipFuncSetAttribute((const void*)rows, hipFuncAttributeMaxDynamicSharedMemorySize, rows_bytes);
+    if (e == hipSuccess) e = hipFuncSetAttribute((const void*)cols, hipFuncAttributeMaxDynamicSharedMemorySize, cols_bytes);
+    if (e != hipSuccess) return e;
+  }
+  const int blocks = (a.n + 32 * W - 1) / (32 * W);
+  hipLaunchKernelGGL(rows, dim3((unsigned)head_blocks(a.heads * a.G, blocks)), dim3(64 * W), rows_bytes, s, a, blocks);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(cols, dim3((unsigned)head_blocks(a.heads, blocks)), dim3(64 * W), cols_bytes, s, a, blocks);
+  return hipGetLastError();
+}
+
+template <int ND>
+hipError_t launch_backward(const SoftmaxGradArgs& a, bool bf16, hipStream_t s) {
+  return bf16 ? launch_backward_w<u16, ND, 4>(a, s) : launch_backward_w<float, ND, 4>(a, s);
+}
+
+}  // namespace
+
+hipError_t launch_softmax_backward(const SoftmaxGradArgs& a, bool bf16, hipStream_t s) {
+  switch ((std::max(a.dk_, a.dv_) + 31) / 32) {
+    case 1: return launch_backward<1>(a, bf16, s);
+    case 2: return launch_backward<2>(a, bf16, s);
+    case 3: return launch_backward<3>(a, bf16, s);
+    default: return launch_backward<4>(a, bf16, s);
+  }
+}
+
+}  // namespace sata
