@@ -204,22 +204,29 @@ constexpr int kMaxPairDim = 128;  // d_k and d_v
 // One scan over the tokens of `heads` key/value heads (decay.hip): with the state
 //     R_t = lam R_{t-1} + update b_t (x) w_t,   out_t = readout a_t R_t,
 // from the last token back where `reverse`; one of update and readout is the
-// scale of the scores, the other 1.  a holds ga members a head, b and w gb
-// (one of the two is 1).  Forward, the state starts as S_in and S_out is the
+// scale of the scores, the other 1.  Of a group of G query heads, a (forward) or b and
+// w (reverse) hold a member each.  Forward, the state starts as S_in and S_out is the
 // state after the last token; in reverse R starts as S_in / lam, and S_out is lam R
 // after the first token.
 struct DecayScan {
   const void *a = nullptr, *b = nullptr, *w = nullptr;
-  void* out = nullptr;                            // may be null: the state alone
+  void* out = nullptr;
   const float* S_in = nullptr;                    // [heads][da][dw] ([dw][da] where transposed) or null
   float* S_out = nullptr;                         // the same or null
   const float* log_decay = nullptr;               // [H]
   const int* lengths = nullptr;                   // [heads / H] or null
-  int heads = 0, H = 0, n = 0, da = 0, dw = 0, ga = 1, gb = 1;
+  int heads = 0, H = 0, n = 0, da = 0, dw = 0, G = 1;
   bool reverse = false, transposed = false;
   float update = 1.f, readout = 1.f;
 };
-hipError_t launch_decay_scan(const DecayScan& s, bool bf16, hipStream_t st);
+// Parts of a head's sequence that run side by side (what they add to the state is
+// summed first); the scan's launch takes state_bytes of scratch.
+struct DecayScanPlan {
+  int parts = 1, part_len = 0;
+  size_t state_bytes = 0;
+};
+DecayScanPlan plan_decay_scan(int heads, int n, int da, int dw);
+hipError_t launch_decay_scan(const DecayScan& s, bool bf16, float* states, hipStream_t st);
 hipError_t launch_decay_step(float* S, const void* q, const void* k, const void* v, const float* log_decay, void* y,
                              bool bf16, int heads, int H, int G, int dk, int dv, float scale, hipStream_t st);
 

@@ -182,16 +182,20 @@ __device__ __forceinline__ void contract32_own(const u16* t, int r0, const uint4
 
 // A tensor's rows on their way to a tile of THREADS threads' workgroup: 16-byte vectors
 // where rows allow them (width a multiple of a vector, base aligned), else entries.  Rows
-// at and behind `rows` read as zero.  The columns behind the width are never written:
-// the tile is cleared once before.
+// at and behind `rows` and columns at and behind the width read as zero.  A thread has
+// one vector's place in a row, in every kPer-th row.
 template <typename T, int ND, int ROWS, int THREADS>
 struct TileStage {
   using L = PairTile<T, ND, ROWS>;
   static constexpr int kEV = 16 / sizeof(T);
-  static constexpr int kIt = (ROWS * 32 * ND / kEV + THREADS - 1) / THREADS;
+  static constexpr int kU = L::kRow / kEV;  // vectors in a row
+  static constexpr int kPer = THREADS / kU;
+  static constexpr int kIt = (ROWS + kPer - 1) / kPer;
+  static_assert(THREADS % kU == 0, "whole rows in a pass");
   const T* base;
   int rows, width, tid;
   bool vec;
+  uint32_t off;
   VectorReader read;
   uint4 r[kIt];
 
@@ -199,16 +203,13 @@ struct TileStage {
     base = p, rows = rows_, width = width_, tid = tid_;
     vec = width % kEV == 0 && ((uintptr_t)p & 15) == 0;
     read = VectorReader(p, vec ? (int64_t)rows * width * (int)sizeof(T) : 0);
+    const int row = tid / kU, col = tid % kU * kEV;
+    off = col < width && row < ROWS ? (uint32_t)(row * width + col) * (uint32_t)sizeof(T) : kNoVector;
   }
-  // the chunk of ROWS rows from r0 (a whole number of vectors from the tensor's start where vec)
+  // the rows from r0 on
   __device__ void fetch(int r0) {
-    const int total = ROWS * width / kEV;
-    const uint32_t start = (uint32_t)r0 * (uint32_t)(width * (int)sizeof(T));
 #pragma unroll
-    for (int i = 0; i < kIt; ++i) {
-      const int v = tid + i * THREADS;
-      r[i] = read(v < total ? start + 16u * v : kNoVector);
-    }
+    for (int i = 0; i < kIt; ++i) r[i] = read(off + (uint32_t)(r0 + i * kPer) * (uint32_t)(width * (int)sizeof(T)));
   }
   __device__ static void put_entry(u16* dst, T x) {
     if constexpr (sizeof(T) == 4) {
@@ -225,12 +226,11 @@ struct TileStage {
   }
   __device__ void put(u16* t, int r0) const {
     if (vec) {
-      const int nv = width / kEV;
 #pragma unroll
       for (int i = 0; i < kIt; ++i) {
-        const int v = tid + i * THREADS, row = v / nv, col = (v - row * nv) * kEV;
-        if (row >= ROWS) continue;
-        u16* const dst = t + L::at(row, col);
+        const int row = tid / kU + i * kPer;
+        if ((i + 1) * kPer > ROWS && row >= ROWS) continue;
+        u16* const dst = t + L::at(row, tid % kU * kEV);
         if constexpr (sizeof(T) == 4) {
           float x[4] = {__uint_as_float(r[i].x), __uint_as_float(r[i].y), __uint_as_float(r[i].z), __uint_as_float(r[i].w)};
 #pragma unroll
@@ -244,10 +244,10 @@ struct TileStage {
         }
       }
     } else {
-      for (int i = tid; i < ROWS * width; i += THREADS) {
-        const int row = i / width;
-        put_entry(t + L::at(row, i - row * width),
-                  r0 + row < rows ? base[(int64_t)r0 * width + i] : (T)0);
+#pragma unroll 1
+      for (int i = tid; i < ROWS * 32 * ND; i += THREADS) {
+        const int row = i / (32 * ND), col = i % (32 * ND);
+        put_entry(t + L::at(row, col), r0 + row < rows && col < width ? base[(int64_t)(r0 + row) * width + col] : (T)0);
       }
     }
   }

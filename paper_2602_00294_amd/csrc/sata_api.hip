@@ -708,6 +708,15 @@ sata_status check_pair_args(sata_dtype dt, int B, int H_kv, int G, int n, int d_
   return SATA_OK;
 }
 
+// Scratch for the states of a decay scan's parts (nothing for one part).
+sata_status get_decay_states(int heads, int n, int d_k, int d_v, hipStream_t stream, float** out) {
+  const size_t bytes = sata::plan_decay_scan(heads, n, d_k, d_v).state_bytes;
+  void* ws = nullptr;
+  sata_status st = bytes ? get_workspace(bytes, stream, &ws) : SATA_OK;
+  *out = (float*)ws;
+  return st;
+}
+
 float pair_scale(int d_k) { return (float)(1.0 / std::sqrt((double)d_k)); }
 
 }  // namespace
@@ -962,9 +971,13 @@ sata_status sata_decay_prefill(const void* q, const void* k, const void* v, cons
   sata::DecayScan s;
   s.a = q, s.b = k, s.w = v, s.out = y;
   s.S_in = S_in, s.S_out = S_out, s.log_decay = log_decay, s.lengths = lengths;
-  s.heads = B * H_kv, s.H = H_kv, s.n = n, s.da = d_k, s.dw = d_v, s.ga = G;
+  s.heads = B * H_kv, s.H = H_kv, s.n = n, s.da = d_k, s.dw = d_v, s.G = G;
   s.readout = pair_scale(d_k);
-  hipError_t e = sata::launch_decay_scan(s, dt == SATA_BF16, (hipStream_t)stream);
+  const hipStream_t hs = (hipStream_t)stream;
+  const bool bf16 = dt == SATA_BF16;
+  float* states = nullptr;
+  if ((st = get_decay_states(s.heads, n, d_k, d_v, hs, &states)) != SATA_OK) return st;
+  hipError_t e = sata::launch_decay_scan(s, bf16, states, hs);
   if (e != hipSuccess) return hip_fail(e, "decay prefill launch");
   return ok();
 }
@@ -993,6 +1006,8 @@ sata_status sata_decay_backward(const void* q, const void* k, const void* v, con
   const hipStream_t hs = (hipStream_t)stream;
   const bool bf16 = dt == SATA_BF16;
   const float c = pair_scale(d_k);
+  float* states = nullptr;
+  if ((st = get_decay_states(B * H_kv, n, d_k, d_v, hs, &states)) != SATA_OK) return st;
   sata::DecayScan s;
   s.log_decay = log_decay, s.lengths = lengths;
   s.heads = B * H_kv, s.H = H_kv, s.n = n;
@@ -1000,22 +1015,22 @@ sata_status sata_decay_backward(const void* q, const void* k, const void* v, con
   if (n > 0) {
     sata::DecayScan r = s;
     r.a = dy, r.b = v, r.w = k, r.out = dq;
-    r.da = d_v, r.dw = d_k, r.ga = G;
+    r.da = d_v, r.dw = d_k, r.G = G;
     r.S_in = S_in, r.transposed = true;
     r.readout = c;
-    if ((e = sata::launch_decay_scan(r, bf16, hs)) != hipSuccess) return hip_fail(e, "decay backward (dq) launch");
+    if ((e = sata::launch_decay_scan(r, bf16, states, hs)) != hipSuccess) return hip_fail(e, "decay backward (dq) launch");
     r = s;
     r.a = v, r.b = dy, r.w = q, r.out = dk;
-    r.da = d_v, r.dw = d_k, r.gb = G;
+    r.da = d_v, r.dw = d_k, r.G = G;
     r.reverse = true, r.transposed = true;
     r.S_in = dS, r.update = c;
-    if ((e = sata::launch_decay_scan(r, bf16, hs)) != hipSuccess) return hip_fail(e, "decay backward (dk) launch");
+    if ((e = sata::launch_decay_scan(r, bf16, states, hs)) != hipSuccess) return hip_fail(e, "decay backward (dk) launch");
   }
   s.a = k, s.b = q, s.w = dy, s.out = dv;
-  s.da = d_k, s.dw = d_v, s.gb = G;
+  s.da = d_k, s.dw = d_v, s.G = G;
   s.reverse = true;
   s.S_in = dS, s.S_out = dS_in, s.update = c;
-  if ((e = sata::launch_decay_scan(s, bf16, hs)) != hipSuccess) return hip_fail(e, "decay backward (dv) launch");
+  if ((e = sata::launch_decay_scan(s, bf16, states, hs)) != hipSuccess) return hip_fail(e, "decay backward (dv) launch");
   return ok();
 }
 

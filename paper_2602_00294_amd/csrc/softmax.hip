@@ -78,7 +78,6 @@ __global__ void __launch_bounds__(64 * W, sizeof(T) == 2 ? 2 : 1) softmax_prefil
   float top = -3.4028234e38f, sum = 0.f;
   const int end = min(len, 32 * kWaves * (blk + 1));  // keys that this workgroup sees
   if (32 * kWaves * blk < len) {
-    for (int i = tid; i < 4 * L::kElems / 8; i += kThreads) ((uint4*)smem16)[i] = uint4{0u, 0u, 0u, 0u};
     TileStage<T, ND, kKeys, kThreads> sk, sv;
     sk.init((const T*)a.k + (int64_t)kvh * n * dk, len, dk, tid);
     sv.init((const T*)a.v + (int64_t)kvh * n * dv, len, dv, tid);
@@ -128,7 +127,6 @@ __global__ void __launch_bounds__(64 * W, sizeof(T) == 2 ? 2 : 1) softmax_prefil
       if (__builtin_expect(odd, 0)) contract32_own<L, ND>(vt, r0, w, o, [&](int key) { return key <= l31; });
       else contract32<L, ND>(vt, r0, w, o);
     };
-    __syncthreads();
     sk.fetch(0);
     sv.fetch(0);
     sk.put(smem16, 0);

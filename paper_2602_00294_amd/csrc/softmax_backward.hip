@@ -76,7 +76,6 @@ __global__ void __launch_bounds__(64 * W, sizeof(T) == 2 ? 2 : 1) softmax_rows(S
 #pragma unroll
   for (int j = 0; j < ND; ++j) acc[j] = zero16();
   if (32 * W * blk < len) {
-    for (int i = tid; i < 4 * L::kElems / 8; i += kThreads) ((uint4*)smem16)[i] = uint4{0u, 0u, 0u, 0u};
     TileStage<T, ND, kRows, kThreads> sk, sv;
     sk.init((const T*)a.k + (int64_t)kvh * n * dk, len, dk, tid);
     sv.init((const T*)a.v + (int64_t)kvh * n * dv, len, dv, tid);
@@ -104,7 +103,6 @@ __global__ void __launch_bounds__(64 * W, sizeof(T) == 2 ? 2 : 1) softmax_rows(S
       if (__builtin_expect(odd, 0)) contract32_own<L, ND>(kt, r0, w, acc, [&](int key) { return key <= l31; });
       else contract32<L, ND>(kt, r0, w, acc);
     };
-    __syncthreads();
     sk.fetch(0);
     sv.fetch(0);
     sk.put(smem16, 0);
@@ -152,7 +150,6 @@ __global__ void __launch_bounds__(64 * W, sizeof(T) == 2 && ND <= 2 ? 2 : 1) sof
 #pragma unroll
   for (int j = 0; j < ND; ++j) gk[j] = gv[j] = zero16();
   if (32 * W * blk < len) {
-    for (int i = tid; i < 2 * kBuf / 8; i += kThreads) ((uint4*)smem16)[i] = uint4{0u, 0u, 0u, 0u};
     uint4 kf[2 * ND][L::kPl], vf[2 * ND][L::kPl];
     load_own32<T, ND>((const T*)a.k + at * dk, row < len, dk, kf);
     load_own32<T, ND>((const T*)a.v + at * dv, row < len, dv, vf);
@@ -214,7 +211,6 @@ __global__ void __launch_bounds__(64 * W, sizeof(T) == 2 && ND <= 2 ? 2 : 1) sof
       sy.put(t + L::kElems, t0);
       if (tid < 2 * kRows) ((float*)(t + 2 * L::kElems))[tid] = st_;
     };
-    __syncthreads();
     open(0);
     fetch(first * kRows);
     put(0, first * kRows);
