@@ -286,7 +286,18 @@ sata_status sata_decode_step_grouped(float* S, const void* q, const void* k, con
  *  - 1 <= d_k, d_v <= 128 (SATA_ERR_UNSUPPORTED beyond), B*H_kv*G <= 65535 and
  *    n <= 2^21 (SATA_ERR_TOO_LARGE beyond).
  *  - Values that are not finite reach what depends on them only: not earlier
- *    tokens' outputs, nor other sequences or heads.  */
+ *    tokens' outputs, nor other sequences or heads.
+ *  - scratch: device memory for the call's own use, 16-byte aligned, of at least as many
+ *    bytes as the query beside the call says (NULL where that is 0).  These calls allocate
+ *    nothing, upload nothing and wait for nothing, so any of them may be the first
+ *    on its stream or be captured into a graph; calls or graphs that may
+ *    overlap take separate scratch.  */
+
+/* Bytes of scratch (host only; -1 for sizes that the calls refuse): of sata_decay_prefill and
+ * sata_decay_backward, of sata_softmax_backward, and of sata_softmax_step. */
+int64_t sata_decay_scratch(int B, int H_kv, int n, int d_k, int d_v);
+int64_t sata_softmax_backward_scratch(int B, int H_kv, int G, int n);
+int64_t sata_softmax_step_scratch(int B, int H_kv, int G, int capacity, int d_v);
 
 /* Causal linear attention with a decay: with lam = exp(log_decay[h]),
  *     S_t = lam S_{t-1} + k_t (x) v_t,    y_t = c q_t S_t.
@@ -299,7 +310,7 @@ sata_status sata_decode_step_grouped(float* S, const void* q, const void* k, con
  * n = 0 writes S_out alone. */
 sata_status sata_decay_prefill(const void* q, const void* k, const void* v, const float* log_decay, sata_dtype dt, int B,
                                int H_kv, int G, int n, int d_k, int d_v, const int32_t* lengths, const float* S_in,
-                               void* y, float* S_out, void* stream);
+                               void* y, float* S_out, void* scratch, void* stream);
 
 /* One token of every sequence: S = lam S + k (x) v, then y = c q S.
  *   S: [B][H_kv][d_k][d_v] float32 (device, read and written in place)
@@ -317,7 +328,7 @@ sata_status sata_decay_step(float* S, const void* q, const void* k, const void* 
 sata_status sata_decay_backward(const void* q, const void* k, const void* v, const float* log_decay, const void* dy,
                                 sata_dtype dt, int B, int H_kv, int G, int n, int d_k, int d_v, const int32_t* lengths,
                                 const float* S_in, const float* dS, void* dq, void* dk, void* dv, float* dS_in,
-                                void* stream);
+                                void* scratch, void* stream);
 
 /* Exact causal softmax attention (Sec. 2.1):
  *     lse_t = log sum_{s<=t} exp(c q_t.k_s),   y_t = sum_{s<=t} exp(c q_t.k_s - lse_t) v_s.
@@ -331,11 +342,11 @@ sata_status sata_softmax_prefill(const void* q, const void* k, const void* v, sa
  * again from the scores and lse (y and lse as the forward call wrote them):
  *     p_ts = exp(c q_t.k_s - lse_t),   e_ts = c p_ts (dy_t.v_s - dy_t.y_t),
  *     dq_t = sum_{s<=t} e_ts k_s,  dk_s = sum_{t>=s} e_ts q_t,  dv_s = sum_{t>=s} p_ts dy_t.
- *   dq, dk, dv: as q, k, v (device, written)
- * Workspace: 4 bytes per query head and token. */
+ *   dq, dk, dv: as q, k, v (device, written) */
 sata_status sata_softmax_backward(const void* q, const void* k, const void* v, const void* y, const float* lse,
                                   const void* dy, sata_dtype dt, int B, int H_kv, int G, int n, int d_k, int d_v,
-                                  const int32_t* lengths, void* dq, void* dk, void* dv, void* stream);
+                                  const int32_t* lengths, void* dq, void* dk, void* dv, void* scratch,
+                                  void* stream);
 
 /* One token of every sequence over a cache: writes k and v as row lengths[b] of
  * the cache, then y = softmax attention of q over rows 0..lengths[b].
@@ -348,7 +359,7 @@ sata_status sata_softmax_backward(const void* q, const void* k, const void* v, c
  * prompt is its k and v, in tensors of `capacity` rows; capacity <= 2^21. */
 sata_status sata_softmax_step(void* K, void* V, int capacity, const int32_t* lengths, const void* q, const void* k,
                               const void* v, sata_dtype dt, int B, int H_kv, int G, int d_k, int d_v, void* y,
-                              void* stream);
+                              void* scratch, void* stream);
 
 /* Static text for a status code. */
 const char* sata_status_string(sata_status s);

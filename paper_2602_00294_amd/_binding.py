@@ -66,18 +66,25 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.sata_decode_step_compensated.restype = i32
     lib.sata_decode_step_grouped.argtypes = [vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, vp, vp]
     lib.sata_decode_step_grouped.restype = i32
-    lib.sata_decay_prefill.argtypes = [vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp]
+    lib.sata_decay_scratch.argtypes = [i32, i32, i32, i32, i32]
+    lib.sata_decay_scratch.restype = i64
+    lib.sata_softmax_backward_scratch.argtypes = [i32, i32, i32, i32]
+    lib.sata_softmax_backward_scratch.restype = i64
+    lib.sata_softmax_step_scratch.argtypes = [i32, i32, i32, i32, i32]
+    lib.sata_softmax_step_scratch.restype = i64
+    lib.sata_decay_prefill.argtypes = [vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp]
     lib.sata_decay_prefill.restype = i32
     lib.sata_decay_step.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, vp, vp]
     lib.sata_decay_step.restype = i32
     lib.sata_decay_backward.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp,
-                                        vp, vp]
+                                        vp, vp, vp]
     lib.sata_decay_backward.restype = i32
     lib.sata_softmax_prefill.argtypes = [vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, vp, vp, vp, vp]
     lib.sata_softmax_prefill.restype = i32
-    lib.sata_softmax_backward.argtypes = [vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp]
+    lib.sata_softmax_backward.argtypes = [vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp,
+                                          vp]
     lib.sata_softmax_backward.restype = i32
-    lib.sata_softmax_step.argtypes = [vp, vp, i32, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, vp, vp]
+    lib.sata_softmax_step.argtypes = [vp, vp, i32, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, vp, vp, vp]
     lib.sata_softmax_step.restype = i32
     lib.sata_status_string.argtypes = [i32]
     lib.sata_status_string.restype = ctypes.c_char_p
@@ -475,6 +482,12 @@ def _check_tensors(device, **tensors):
             _check_tensor(t, name, device)
 
 
+def _scratch(nbytes: int, device):
+    """The call's own device memory, from torch's allocator: on the current stream, and in the pool of the
+    graph that a call is captured into."""
+    return _torch().empty(nbytes, dtype=_torch().uint8, device=device) if nbytes > 0 else None
+
+
 def decay_prefill(q, k, v, log_decay, lengths=None, S_in=None, want_state: bool = True, y=None, S=None):
     """Causal linear attention with a decay per key/value head: S_t = exp(log_decay) S_{t-1} + k_t (x) v_t,
     y_t = q_t S_t / sqrt(d_k).
@@ -497,8 +510,10 @@ def decay_prefill(q, k, v, log_decay, lengths=None, S_in=None, want_state: bool 
     if want_state and S is None:
         S = torch.empty(B, H, dk, dv, dtype=torch.float32, device=q.device)
     with torch.cuda.device(q.device):
-        _check(load_library().sata_decay_prefill(_ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), code, B, H, G, n, dk, dv,
-                                                 _ptr(lengths), _ptr(S_in), _ptr(y), _ptr(S), _stream_ptr()),
+        lib = load_library()
+        scratch = _scratch(lib.sata_decay_scratch(B, H, n, dk, dv), q.device)
+        _check(lib.sata_decay_prefill(_ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), code, B, H, G, n, dk, dv,
+                                      _ptr(lengths), _ptr(S_in), _ptr(y), _ptr(S), _ptr(scratch), _stream_ptr()),
                "sata_decay_prefill")
     return y, S
 
@@ -535,9 +550,11 @@ def decay_backward(q, k, v, log_decay, dy, lengths=None, S_in=None, dS=None):
     dq, dkk, dvv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
     dS_in = torch.empty_like(S_in) if S_in is not None else None
     with torch.cuda.device(q.device):
-        _check(load_library().sata_decay_backward(_ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(dy), code, B, H, G,
-                                                  n, dk, dv, _ptr(lengths), _ptr(S_in), _ptr(dS), _ptr(dq), _ptr(dkk),
-                                                  _ptr(dvv), _ptr(dS_in), _stream_ptr()), "sata_decay_backward")
+        lib = load_library()
+        scratch = _scratch(lib.sata_decay_scratch(B, H, n, dk, dv), q.device)
+        _check(lib.sata_decay_backward(_ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(dy), code, B, H, G, n, dk, dv,
+                                       _ptr(lengths), _ptr(S_in), _ptr(dS), _ptr(dq), _ptr(dkk), _ptr(dvv),
+                                       _ptr(dS_in), _ptr(scratch), _stream_ptr()), "sata_decay_backward")
     return dq, dkk, dvv, dS_in
 
 
@@ -574,9 +591,11 @@ def softmax_backward(q, k, v, y, lse, dy, lengths=None):
     _check_tensors(q.device, q=q, k=k, v=v, y=y, lse=lse, dy=dy, lengths=lengths)
     dq, dkk, dvv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
     with torch.cuda.device(q.device):
-        _check(load_library().sata_softmax_backward(_ptr(q), _ptr(k), _ptr(v), _ptr(y), _ptr(lse), _ptr(dy), code, B,
-                                                    H, G, n, dk, dv, _ptr(lengths), _ptr(dq), _ptr(dkk), _ptr(dvv),
-                                                    _stream_ptr()), "sata_softmax_backward")
+        lib = load_library()
+        scratch = _scratch(lib.sata_softmax_backward_scratch(B, H, G, n), q.device)
+        _check(lib.sata_softmax_backward(_ptr(q), _ptr(k), _ptr(v), _ptr(y), _ptr(lse), _ptr(dy), code, B, H, G, n, dk,
+                                         dv, _ptr(lengths), _ptr(dq), _ptr(dkk), _ptr(dvv), _ptr(scratch),
+                                         _stream_ptr()), "sata_softmax_backward")
     return dq, dkk, dvv
 
 
@@ -599,8 +618,10 @@ def softmax_step(K, V, lengths, q, k, v, y=None):
     if y is None:
         y = torch.empty(B, G * H, dv, dtype=q.dtype, device=q.device)
     with torch.cuda.device(q.device):
-        _check(load_library().sata_softmax_step(_ptr(K), _ptr(V), cap, _ptr(lengths), _ptr(q), _ptr(k), _ptr(v), code,
-                                                B, H, G, dk, dv, _ptr(y), _stream_ptr()), "sata_softmax_step")
+        lib = load_library()
+        scratch = _scratch(lib.sata_softmax_step_scratch(B, H, G, cap, dv), q.device)
+        _check(lib.sata_softmax_step(_ptr(K), _ptr(V), cap, _ptr(lengths), _ptr(q), _ptr(k), _ptr(v), code, B, H, G,
+                                     dk, dv, _ptr(y), _ptr(scratch), _stream_ptr()), "sata_softmax_step")
     return y
 
 

@@ -1,7 +1,7 @@
 // Causal linear attention with a decay per head: with lam = exp(log_decay[h]) and
 // c = 1 / sqrt(d_k),
 //     S_t = lam S_{t-1} + k_t (x) v_t,   y_t = c q_t S_t,
-// its gradients and its single step.  All four sums over a sequence (y, dq, dk and
+// and its gradients.  All four sums over a sequence (y, dq, dk and
 // dv) are one scan with the tensors in other places,
 //     out_t = c sum_{s<=t} lam^(t-s) (a_t . b_s) w_s + (the state before the first token),
 //     y : a = q,  b = k,  w = v         dq: a = dy, b = v,  w = k
@@ -10,6 +10,7 @@
 
 #include <algorithm>
 
+#include "decay_power.hpp"
 #include "device_common.hpp"
 #include "kernels.hpp"
 #include "pair_tiles.hpp"
@@ -17,19 +18,6 @@
 namespace sata {
 
 namespace {
-
-// exp(g)^e as a float pair.  A single float would do for one factor, but the state is
-// multiplied by the same one at every step: its error (2^-25) would grow with the
-// number of steps, while the roundings of the products are independent.
-struct FloatPair {
-  float hi, lo;
-};
-__device__ __forceinline__ FloatPair decay_power(float g, int e) {
-  const double x = exp((double)fmaxf(g, -1e30f) * e);  // (no minus infinity: times 0 it is NaN)
-  const float hi = (float)x;
-  return FloatPair{hi, (float)(x - hi)};
-}
-__device__ __forceinline__ float times(float x, FloatPair p) { return fmaf(x, p.hi, x * p.lo); }
 
 // A stretch of one head's tokens per workgroup, in chunks of kChunk, the state in
 // registers: wave j holds columns 32 j .. +31 of it (and writes those of the output), its lanes one
@@ -331,29 +319,6 @@ __global__ void __launch_bounds__(256) decay_carry_kernel(DecayScan s, ScanParts
   if (s.S_out) s.S_out[head * size + at] = R;
 }
 
-// One workgroup per key/value head, one thread per column of the state.
-template <typename T>
-__global__ void __launch_bounds__(kMaxPairDim) decay_step_kernel(float* S, const T* q, const T* k, const T* v,
-                                                                const float* log_decay, T* y, int H, int G, int dk,
-                                                                int dv, float scale) {
-  const int64_t head = blockIdx.x;
-  const int j = threadIdx.x;
-  if (j >= dv) return;
-  const FloatPair lam = decay_power(log_decay[head % H], 1);
-  float* const s = S + head * dk * dv + j;
-  const float w = to_f32(v[head * dv + j]);
-  for (int i = 0; i < dk; ++i) s[i * dv] = fmaf(to_f32(k[head * dk + i]), w, times(s[i * dv], lam));
-  for (int g = 0; g < G; ++g) {
-    float o = 0.f;
-    for (int i = 0; i < dk; ++i) o = fmaf(to_f32(q[(head * G + g) * dk + i]), s[i * dv], o);
-    y[(head * G + g) * dv + j] = from_f32<T>(o * scale);
-  }
-}
-
-}  // namespace
-
-namespace {
-
 template <typename T, int ND, bool REV>
 hipError_t launch_scan(const DecayScan& s, float* states, hipStream_t st) {
   constexpr int bytes = 3 * PairTile<T, ND, kChunk>::kBytes + 4 * (2 * kChunk + 4);
@@ -406,17 +371,6 @@ hipError_t launch_decay_scan(const DecayScan& s, bool bf16, float* states, hipSt
     case 3: return launch_scan_n<3>(s, bf16, states, st);
     default: return launch_scan_n<4>(s, bf16, states, st);
   }
-}
-
-hipError_t launch_decay_step(float* S, const void* q, const void* k, const void* v, const float* log_decay, void* y,
-                             bool bf16, int heads, int H, int G, int dk, int dv, float scale, hipStream_t st) {
-  if (bf16)
-    hipLaunchKernelGGL(decay_step_kernel<bf16_t>, dim3(heads), dim3(kMaxPairDim), 0, st, S, (const bf16_t*)q,
-                       (const bf16_t*)k, (const bf16_t*)v, log_decay, (bf16_t*)y, H, G, dk, dv, scale);
-  else
-    hipLaunchKernelGGL(decay_step_kernel<float>, dim3(heads), dim3(kMaxPairDim), 0, st, S, (const float*)q,
-                       (const float*)k, (const float*)v, log_decay, (float*)y, H, G, dk, dv, scale);
-  return hipGetLastError();
 }
 
 }  // namespace sata

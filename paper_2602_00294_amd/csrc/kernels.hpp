@@ -251,11 +251,19 @@ struct SoftmaxGradArgs {
 };
 hipError_t launch_softmax_backward(const SoftmaxGradArgs& a, bool bf16, hipStream_t s);
 
+// A head's cache in stretches, a workgroup for each and every 32 members of a group;
+// their sums lie in `bytes` bytes of scratch.
+struct SoftmaxStepPlan {
+  int stretches = 1, stretch_len = 0, blocks = 1;
+  size_t bytes = 0;
+};
+SoftmaxStepPlan plan_softmax_step(int heads, int G, int capacity, int dv);
 struct SoftmaxStepArgs {
   void *K, *V;         // [heads][capacity][d]
   const int* lengths;  // [heads / H]
   const void *q, *k, *v;
   void* y;
+  float* scratch;
   int heads, H, G, capacity, dk_, dv_;
   float scale;
 };

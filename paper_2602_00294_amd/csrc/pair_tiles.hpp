@@ -287,6 +287,12 @@ __device__ __forceinline__ void load_own32(const T* p, bool ok, int width, uint4
   }
 }
 
+template <typename T>
+__device__ __forceinline__ T rounded(float x) {
+  if constexpr (sizeof(T) == 4) return x;
+  else return (T)(pack2(x, 0.f) & 0xffffu);
+}
+
 // Four values of a row, columns c0 .. +3 (those below the width).
 template <typename T>
 __device__ __forceinline__ void store4(T* p, int c0, int width, const float (&x)[4], bool vec) {
@@ -298,10 +304,7 @@ __device__ __forceinline__ void store4(T* p, int c0, int width, const float (&x)
   } else {
 #pragma unroll
     for (int r = 0; r < 4; ++r)
-      if (c0 + r < width) {
-        if constexpr (sizeof(T) == 4) p[c0 + r] = x[r];
-        else p[c0 + r] = (T)(pack2(x[r], 0.f) & 0xffffu);
-      }
+      if (c0 + r < width) p[c0 + r] = rounded<T>(x[r]);
   }
 }
 // A lane's part of one output row: columns 32 j + 8 i + 4 h .. +3 of results acc[j], scaled,

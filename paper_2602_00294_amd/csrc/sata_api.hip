@@ -708,13 +708,11 @@ sata_status check_pair_args(sata_dtype dt, int B, int H_kv, int G, int n, int d_
   return SATA_OK;
 }
 
-// Scratch for the states of a decay scan's parts (nothing for one part).
-sata_status get_decay_states(int heads, int n, int d_k, int d_v, hipStream_t stream, float** out) {
-  const size_t bytes = sata::plan_decay_scan(heads, n, d_k, d_v).state_bytes;
-  void* ws = nullptr;
-  sata_status st = bytes ? get_workspace(bytes, stream, &ws) : SATA_OK;
-  *out = (float*)ws;
-  return st;
+// The caller's scratch for a call that needs `bytes` of it.
+sata_status check_scratch(const void* scratch, size_t bytes) {
+  if (bytes && !scratch) return fail(SATA_ERR_INVALID_ARG, "null scratch; %zu bytes needed", bytes);
+  if (bytes && ((uintptr_t)scratch & 15)) return fail(SATA_ERR_INVALID_ARG, "scratch must be 16-byte aligned");
+  return SATA_OK;
 }
 
 float pair_scale(int d_k) { return (float)(1.0 / std::sqrt((double)d_k)); }
@@ -960,24 +958,36 @@ sata_status sata_decode_step_grouped(float* S, const void* q, const void* k, con
   return ok();
 }
 
+int64_t sata_decay_scratch(int B, int H_kv, int n, int d_k, int d_v) {
+  if (check_pair_args(SATA_F32, B, H_kv, 1, n, d_k, d_v) != SATA_OK) return -1;
+  return (int64_t)sata::plan_decay_scan(B * H_kv, n, d_k, d_v).state_bytes;
+}
+
+int64_t sata_softmax_backward_scratch(int B, int H_kv, int G, int n) {
+  if (check_pair_args(SATA_F32, B, H_kv, G, n, 1, 1) != SATA_OK) return -1;
+  return (int64_t)sizeof(float) * B * H_kv * G * n;
+}
+
+int64_t sata_softmax_step_scratch(int B, int H_kv, int G, int capacity, int d_v) {
+  if (check_pair_args(SATA_F32, B, H_kv, G, capacity, 1, d_v) != SATA_OK || capacity < 1) return -1;
+  return (int64_t)sata::plan_softmax_step(B * H_kv, G, capacity, d_v).bytes;
+}
+
 sata_status sata_decay_prefill(const void* q, const void* k, const void* v, const float* log_decay, sata_dtype dt, int B,
                                int H_kv, int G, int n, int d_k, int d_v, const int32_t* lengths, const float* S_in,
-                               void* y, float* S_out, void* stream) {
+                               void* y, float* S_out, void* scratch, void* stream) {
   sata_status st = check_pair_args(dt, B, H_kv, G, n, d_k, d_v);
   if (st != SATA_OK) return st;
   if (!log_decay || (n > 0 && (!q || !k || !v || !y))) return fail(SATA_ERR_INVALID_ARG, "null tensor pointer");
   if (S_in && S_in == S_out) return fail(SATA_ERR_INVALID_ARG, "S_out must not be S_in");
   if (n == 0 && !S_out) return ok();
+  if ((st = check_scratch(scratch, sata::plan_decay_scan(B * H_kv, n, d_k, d_v).state_bytes)) != SATA_OK) return st;
   sata::DecayScan s;
   s.a = q, s.b = k, s.w = v, s.out = y;
   s.S_in = S_in, s.S_out = S_out, s.log_decay = log_decay, s.lengths = lengths;
   s.heads = B * H_kv, s.H = H_kv, s.n = n, s.da = d_k, s.dw = d_v, s.G = G;
   s.readout = pair_scale(d_k);
-  const hipStream_t hs = (hipStream_t)stream;
-  const bool bf16 = dt == SATA_BF16;
-  float* states = nullptr;
-  if ((st = get_decay_states(s.heads, n, d_k, d_v, hs, &states)) != SATA_OK) return st;
-  hipError_t e = sata::launch_decay_scan(s, bf16, states, hs);
+  hipError_t e = sata::launch_decay_scan(s, dt == SATA_BF16, (float*)scratch, (hipStream_t)stream);
   if (e != hipSuccess) return hip_fail(e, "decay prefill launch");
   return ok();
 }
@@ -996,18 +1006,18 @@ sata_status sata_decay_step(float* S, const void* q, const void* k, const void* 
 sata_status sata_decay_backward(const void* q, const void* k, const void* v, const float* log_decay, const void* dy,
                                 sata_dtype dt, int B, int H_kv, int G, int n, int d_k, int d_v, const int32_t* lengths,
                                 const float* S_in, const float* dS, void* dq, void* dk, void* dv, float* dS_in,
-                                void* stream) {
+                                void* scratch, void* stream) {
   sata_status st = check_pair_args(dt, B, H_kv, G, n, d_k, d_v);
   if (st != SATA_OK) return st;
   if (!log_decay || (n > 0 && (!q || !k || !v || !dy || !dq || !dk || !dv)))
     return fail(SATA_ERR_INVALID_ARG, "null tensor pointer");
   if (dS && dS == dS_in) return fail(SATA_ERR_INVALID_ARG, "dS_in must not be dS");
   if (n == 0 && !dS_in) return ok();
+  if ((st = check_scratch(scratch, sata::plan_decay_scan(B * H_kv, n, d_k, d_v).state_bytes)) != SATA_OK) return st;
   const hipStream_t hs = (hipStream_t)stream;
   const bool bf16 = dt == SATA_BF16;
   const float c = pair_scale(d_k);
-  float* states = nullptr;
-  if ((st = get_decay_states(B * H_kv, n, d_k, d_v, hs, &states)) != SATA_OK) return st;
+  float* const states = (float*)scratch;
   sata::DecayScan s;
   s.log_decay = log_decay, s.lengths = lengths;
   s.heads = B * H_kv, s.H = H_kv, s.n = n;
@@ -1048,16 +1058,21 @@ sata_status sata_softmax_prefill(const void* q, const void* k, const void* v, sa
 
 sata_status sata_softmax_backward(const void* q, const void* k, const void* v, const void* y, const float* lse,
                                   const void* dy, sata_dtype dt, int B, int H_kv, int G, int n, int d_k, int d_v,
-                                  const int32_t* lengths, void* dq, void* dk, void* dv, void* stream) {
+                                  const int32_t* lengths, void* dq, void* dk, void* dv, void* scratch,
+                                  void* stream) {
   sata_status st = check_pair_args(dt, B, H_kv, G, n, d_k, d_v);
   if (st != SATA_OK) return st;
   if (n == 0) return ok();
   if (!q || !k || !v || !y || !lse || !dy || !dq || !dk || !dv) return fail(SATA_ERR_INVALID_ARG, "null tensor pointer");
+  if ((st = check_scratch(scratch, sizeof(float) * (size_t)B * H_kv * G * n)) != SATA_OK) return st;
   const hipStream_t s = (hipStream_t)stream;
-  void* ws = nullptr;
-  if ((st = get_workspace(sizeof(float) * (size_t)B * H_kv * G * n, s, &ws)) != SATA_OK) return st;
-  const sata::SoftmaxGradArgs a{q,           k,    v, y, dy, lse, dq, dk, dv, (float*)ws, lengths, B * H_kv, H_kv, G, n, d_k, d_v,
-                                pair_scale(d_k)};
+  sata::SoftmaxGradArgs a;
+  a.q = q, a.k = k, a.v = v, a.y = y, a.dy = dy, a.lse = lse;
+  a.dq = dq, a.dk = dk, a.dv = dv;
+  a.delta = (float*)scratch;
+  a.lengths = lengths;
+  a.heads = B * H_kv, a.H = H_kv, a.G = G, a.n = n, a.dk_ = d_k, a.dv_ = d_v;
+  a.scale = pair_scale(d_k);
   hipError_t e = sata::launch_softmax_backward(a, dt == SATA_BF16, s);
   if (e != hipSuccess) return hip_fail(e, "softmax backward launch");
   return ok();
@@ -1065,12 +1080,14 @@ sata_status sata_softmax_backward(const void* q, const void* k, const void* v, c
 
 sata_status sata_softmax_step(void* K, void* V, int capacity, const int32_t* lengths, const void* q, const void* k,
                               const void* v, sata_dtype dt, int B, int H_kv, int G, int d_k, int d_v, void* y,
-                              void* stream) {
+                              void* scratch, void* stream) {
   sata_status st = check_pair_args(dt, B, H_kv, G, capacity, d_k, d_v);
   if (st != SATA_OK) return st;
   if (capacity < 1) return fail(SATA_ERR_INVALID_ARG, "capacity=%d must be >= 1", capacity);
   if (!K || !V || !lengths || !q || !k || !v || !y) return fail(SATA_ERR_INVALID_ARG, "null tensor pointer");
-  const sata::SoftmaxStepArgs a{K, V, lengths, q, k, v, y, B * H_kv, H_kv, G, capacity, d_k, d_v, pair_scale(d_k)};
+  if ((st = check_scratch(scratch, sata::plan_softmax_step(B * H_kv, G, capacity, d_v).bytes)) != SATA_OK) return st;
+  const sata::SoftmaxStepArgs a{K, V, lengths, q, k, v, y, (float*)scratch, B * H_kv, H_kv, G, capacity, d_k, d_v,
+                                pair_scale(d_k)};
   hipError_t e = sata::launch_softmax_step(a, dt == SATA_BF16, (hipStream_t)stream);
   if (e != hipSuccess) return hip_fail(e, "softmax step launch");
   return ok();

@@ -1,6 +1,5 @@
 // Exact causal softmax attention: with c = 1 / sqrt(d_k),
-//     lse_t = log sum_{s<=t} exp(c q_t.k_s),  p_ts = exp(c q_t.k_s - lse_t),  y_t = sum_{s<=t} p_ts v_s,
-// and its single step over a cache.
+//     lse_t = log sum_{s<=t} exp(c q_t.k_s),  p_ts = exp(c q_t.k_s - lse_t),  y_t = sum_{s<=t} p_ts v_s.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -12,47 +11,6 @@
 namespace sata {
 
 namespace {
-
-__device__ __forceinline__ float wave_sum(float x) {
-#pragma unroll
-  for (int i = 32; i >= 1; i >>= 1) x += __shfl_xor(x, i);
-  return x;
-}
-
-// A row of up to 128 entries over a wave: entries lane and lane + 64.
-template <typename T>
-__device__ __forceinline__ float2 row_of(const T* p, int d) {
-  const int l = threadIdx.x;
-  return float2{l < d ? to_f32(p[l]) : 0.f, l + 64 < d ? to_f32(p[l + 64]) : 0.f};
-}
-template <typename T>
-__device__ __forceinline__ void put_row(T* p, int d, float2 x) {
-  const int l = threadIdx.x;
-  if (l < d) p[l] = from_f32<T>(x.x);
-  if (l + 64 < d) p[l + 64] = from_f32<T>(x.y);
-}
-__device__ __forceinline__ float dot(float2 a, float2 b) { return wave_sum(fmaf(a.x, b.x, a.y * b.y)); }
-
-// One wave per query: keys one after the other, running maximum and sum.
-template <typename T>
-__device__ __forceinline__ float attend(const T* q, const T* k, const T* v, int keys, int dk, int dv, float c, float2& y) {
-  const float2 x = row_of(q, dk);
-  float m = -INFINITY, l = 0.f;
-  y = float2{0.f, 0.f};
-  for (int s = 0; s < keys; ++s) {
-    const float z = c * dot(x, row_of(k + (int64_t)s * dk, dk));
-    const float top = fmaxf(m, z), base = top == -INFINITY ? 0.f : top;
-    const float keep = expf(m - base), p = expf(z - base);
-    const float2 w = row_of(v + (int64_t)s * dv, dv);
-    l = l * keep + p;
-    y.x = y.x * keep + p * w.x;
-    y.y = y.y * keep + p * w.y;
-    m = top;
-  }
-  const float r = keys > 0 ? 1.f / l : 0.f;
-  y.x *= r, y.y *= r;
-  return keys > 0 ? logf(l) + m : -INFINITY;
-}
 
 // One workgroup of W waves per 32 W queries of a head, 32 to a wave, which are the columns
 // of its scores and outputs; the keys are walked in tiles of 32.  The exponentials' base
@@ -181,25 +139,6 @@ hipError_t launch_prefill(const SoftmaxArgs& a, hipStream_t s) {
   return launch_prefill_w<T, ND, 4>(a, s);
 }
 
-// One wave per query head; the first member of a group writes the cache.
-template <typename T>
-__global__ void __launch_bounds__(64) softmax_step_kernel(SoftmaxStepArgs a) {
-  const int64_t kvh = blockIdx.x;
-  const int at = a.lengths[kvh / a.H];
-  const bool on = at >= 0 && at < a.capacity;
-  T* const K = (T*)a.K + kvh * a.capacity * a.dk_;
-  T* const V = (T*)a.V + kvh * a.capacity * a.dv_;
-  if (on) {
-    put_row(K + (int64_t)at * a.dk_, a.dk_, row_of((const T*)a.k + kvh * a.dk_, a.dk_));
-    put_row(V + (int64_t)at * a.dv_, a.dv_, row_of((const T*)a.v + kvh * a.dv_, a.dv_));
-  }
-  for (int64_t qh = kvh * a.G; qh < (kvh + 1) * a.G; ++qh) {
-    float2 y;
-    attend((const T*)a.q + qh * a.dk_, K, V, on ? at + 1 : 0, a.dk_, a.dv_, a.scale, y);
-    put_row((T*)a.y + qh * a.dv_, a.dv_, y);
-  }
-}
-
 }  // namespace
 
 hipError_t launch_softmax_prefill(const SoftmaxArgs& a, bool bf16, hipStream_t s) {
@@ -209,12 +148,6 @@ hipError_t launch_softmax_prefill(const SoftmaxArgs& a, bool bf16, hipStream_t s
     case 3: return bf16 ? launch_prefill<u16, 3>(a, s) : launch_prefill<float, 3>(a, s);
     default: return bf16 ? launch_prefill<u16, 4>(a, s) : launch_prefill<float, 4>(a, s);
   }
-}
-
-hipError_t launch_softmax_step(const SoftmaxStepArgs& a, bool bf16, hipStream_t s) {
-  if (bf16) hipLaunchKernelGGL(softmax_step_kernel<bf16_t>, dim3(a.heads), dim3(64), 0, s, a);
-  else hipLaunchKernelGGL(softmax_step_kernel<float>, dim3(a.heads), dim3(64), 0, s, a);
-  return hipGetLastError();
 }
 
 }  // namespace sata

@@ -147,11 +147,11 @@ def lib():
 def test_sizes_refused(lib, sizes, code):
     dt, B, H, G, n, dk, dv = sizes
     F = FAKE
-    calls = [lib.sata_decay_prefill(F, F, F, F, *sizes, NULL, NULL, F, NULL, NULL),
-             lib.sata_decay_backward(F, F, F, F, F, *sizes, NULL, NULL, NULL, F, F, F, NULL, NULL),
+    calls = [lib.sata_decay_prefill(F, F, F, F, *sizes, NULL, NULL, F, NULL, F, NULL),
+             lib.sata_decay_backward(F, F, F, F, F, *sizes, NULL, NULL, NULL, F, F, F, NULL, F, NULL),
              lib.sata_softmax_prefill(F, F, F, *sizes, NULL, F, F, NULL),
-             lib.sata_softmax_backward(F, F, F, F, F, F, *sizes, NULL, F, F, F, NULL),
-             lib.sata_softmax_step(F, F, n, F, F, F, F, dt, B, H, G, dk, dv, F, NULL)]
+             lib.sata_softmax_backward(F, F, F, F, F, F, *sizes, NULL, F, F, F, F, NULL),
+             lib.sata_softmax_step(F, F, n, F, F, F, F, dt, B, H, G, dk, dv, F, F, NULL)]
     if n == 8:
         calls.append(lib.sata_decay_step(F, F, F, F, F, dt, B, H, G, dk, dv, F, NULL))
     assert calls == [code] * len(calls)
@@ -164,15 +164,15 @@ def test_pointers_refused(lib):
     for at in range(4):
         p = [F] * 4
         p[at] = N
-        assert lib.sata_decay_prefill(*p, *ok, N, N, F, N, N) == -1
-    assert lib.sata_decay_prefill(F, F, F, F, *ok, N, N, N, N, N) == -1
-    assert lib.sata_decay_prefill(F, F, F, F, *ok, N, F, F, F, N) == -1      # S_out is S_in
+        assert lib.sata_decay_prefill(*p, *ok, N, N, F, N, F, N) == -1
+    assert lib.sata_decay_prefill(F, F, F, F, *ok, N, N, N, N, F, N) == -1
+    assert lib.sata_decay_prefill(F, F, F, F, *ok, N, F, F, F, F, N) == -1      # S_out is S_in
     for at in range(5):
         p = [F] * 5
         p[at] = N
-        assert lib.sata_decay_backward(*p, *ok, N, N, N, F, F, F, N, N) == -1
-    assert lib.sata_decay_backward(F, F, F, F, F, *ok, N, N, F, F, F, F, F, N) == -1  # dS_in is dS
-    assert lib.sata_decay_backward(F, F, F, F, F, *ok, N, N, N, F, N, F, N, N) == -1
+        assert lib.sata_decay_backward(*p, *ok, N, N, N, F, F, F, N, F, N) == -1
+    assert lib.sata_decay_backward(F, F, F, F, F, *ok, N, N, F, F, F, F, F, F, N) == -1  # dS_in is dS
+    assert lib.sata_decay_backward(F, F, F, F, F, *ok, N, N, N, F, N, F, N, F, N) == -1
     for at in range(5):
         p = [F] * 5
         p[at] = N
@@ -181,16 +181,36 @@ def test_pointers_refused(lib):
     for at in range(6):
         p = [F] * 6
         p[at] = N
-        assert lib.sata_softmax_backward(*p, *ok, N, F, F, F, N) == -1
-    assert lib.sata_softmax_backward(F, F, F, F, F, F, *ok, N, F, F, N, N) == -1
-    assert lib.sata_softmax_step(F, F, 8, N, F, F, F, 0, 1, 1, 1, 4, 4, F, N) == -1
-    assert lib.sata_softmax_step(F, F, 0, F, F, F, F, 0, 1, 1, 1, 4, 4, F, N) == -1
+        assert lib.sata_softmax_backward(*p, *ok, N, F, F, F, F, N) == -1
+    assert lib.sata_softmax_backward(F, F, F, F, F, F, *ok, N, F, F, N, F, N) == -1
+    assert lib.sata_softmax_step(F, F, 8, N, F, F, F, 0, 1, 1, 1, 4, 4, F, F, N) == -1
+    assert lib.sata_softmax_step(F, F, 0, F, F, F, F, 0, 1, 1, 1, 4, 4, F, F, N) == -1
     # no tokens: nothing to do without a state
     empty = (0, 1, 1, 1, 0, 4, 4)
-    assert lib.sata_decay_prefill(N, N, N, F, *empty, N, N, N, N, N) == 0
-    assert lib.sata_decay_backward(N, N, N, F, N, *empty, N, N, N, N, N, N, N, N) == 0
+    assert lib.sata_decay_prefill(N, N, N, F, *empty, N, N, N, N, N, N) == 0
+    assert lib.sata_decay_backward(N, N, N, F, N, *empty, N, N, N, N, N, N, N, N, N) == 0
     assert lib.sata_softmax_prefill(N, N, N, *empty, N, N, N, N) == 0
-    assert lib.sata_softmax_backward(N, N, N, N, N, N, *empty, N, N, N, N, N) == 0
+    assert lib.sata_softmax_backward(N, N, N, N, N, N, *empty, N, N, N, N, N, N) == 0
+
+
+def test_scratch(lib):
+    F, N = FAKE, NULL
+    odd = ctypes.c_void_p(0x1008)
+    # long heads and few of them work in parts or stretches, whose sums need room
+    assert lib.sata_decay_scratch(1, 2, 4096, 64, 32) > 0 and lib.sata_decay_scratch(64, 64, 4096, 64, 32) == 0
+    assert lib.sata_softmax_backward_scratch(2, 3, 4, 5) == 4 * 2 * 3 * 4 * 5
+    assert lib.sata_softmax_step_scratch(1, 2, 4, 8192, 64) > 0 and lib.sata_softmax_step_scratch(64, 64, 1, 8192, 64) == 0
+    for bad in ((0, 1, 1, 1, 1), (1, 1, -1, 1, 1), (1, 1, 1, 129, 1), (1, 65536, 1, 1, 1)):
+        assert lib.sata_decay_scratch(*bad) == -1
+    assert lib.sata_softmax_backward_scratch(1, 1, 0, 5) == -1
+    assert lib.sata_softmax_step_scratch(1, 1, 1, 0, 5) == -1
+    sizes = (0, 1, 2, 1, 4096, 64, 32)
+    for s in (N, odd):
+        assert lib.sata_decay_prefill(F, F, F, F, *sizes, N, N, F, N, s, N) == -1
+        assert lib.sata_decay_backward(F, F, F, F, F, *sizes, N, N, N, F, F, F, N, s, N) == -1
+        assert lib.sata_softmax_backward(F, F, F, F, F, F, *sizes, N, F, F, F, s, N) == -1
+        assert lib.sata_softmax_step(F, F, 8192, F, F, F, F, 0, 1, 2, 1, 64, 64, F, s, N) == -1
+        assert "scratch" in lib.sata_last_error().decode()
 
 
 class TestBindingRefuses:
