@@ -119,14 +119,23 @@ __device__ __forceinline__ uint4 not_finite_entries(const uint4& w) {
 }
 
 // acc[j] += (rows r0 .. r0 + 31 of the tile, columns 32 j .. +31)^T times the 32 x 32 weights w.
-template <typename L, int ND>
+// CLEAN: values of the tile that are not finite count as zero: w is zero for rows that
+// its columns do not see, and not finite times 0 would not be.  mark_not_finite then
+// gives the others their due.
+template <typename L, int ND, bool CLEAN = false>
 __device__ __forceinline__ void contract32(const u16* t, int r0, const uint4 (&w)[2][L::kPl], f32x16 (&acc)[ND]) {
 #pragma unroll
   for (int j = 0; j < ND; ++j)
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
+      if (CLEAN) __builtin_amdgcn_sched_barrier(0);  // (rare: one at a time takes fewer registers)
       uint4 a[L::kPl];
       L::load_transposed(t, r0 + 16 * s, j, a);
+      if constexpr (CLEAN) {
+        const uint4 m = not_finite_entries(a[0]);
+#pragma unroll
+        for (int i = 0; i < L::kPl; ++i) a[i].x &= ~m.x, a[i].y &= ~m.y, a[i].z &= ~m.z, a[i].w &= ~m.w;
+      }
       acc[j] = dot_planes32(a, w[s], acc[j]);
     }
 }
@@ -145,39 +154,24 @@ __device__ __forceinline__ bool tile_not_finite(const u16* t, int r0) {
   return __ballot(bad != 0) != 0;
 }
 
-// contract32 where w is zero for the rows that its columns do not see and some of the
-// values there are not finite, which would not be zero times 0.  They are left out of
-// the product, and a product of marks with the rows seen (allowed(row) of this lane's
-// column) tells which results have one: those are NaN.
-template <typename L, int ND, typename F>
-__device__ __forceinline__ void contract32_own(const u16* t, int r0, const uint4 (&w)[2][L::kPl], f32x16 (&acc)[ND],
-                                               F&& allowed) {
+// Makes NaN of the results in whose columns one of the rows first .. last of p (those that this
+// lane's column sees of its own tile) is not finite.
+template <typename T, int ND>
+__device__ __forceinline__ void mark_not_finite(const T* p, int width, int first, int last, f32x16 (&acc)[ND]) {
   const int h = (threadIdx.x & 63) >> 5;
-  uint4 seen[2];
+#pragma unroll 1
+  for (int r = first; r <= last; ++r)
 #pragma unroll
-  for (int s = 0; s < 2; ++s) {
-    float x[8];
+    for (int j = 0; j < ND; ++j)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = allowed(result_row(8 * s + i, h)) ? 1.f : 0.f;
-    seen[s] = to_bf16(x);
-  }
-#pragma unroll
-  for (int j = 0; j < ND; ++j) {
-    f32x16 count = zero16();
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      uint4 a[L::kPl];
-      L::load_transposed(t, r0 + 16 * s, j, a);
-      const uint4 m = not_finite_entries(a[0]);
-      count = mfma32(uint4{m.x & 0x3f803f80u, m.y & 0x3f803f80u, m.z & 0x3f803f80u, m.w & 0x3f803f80u}, seen[s], count);
-#pragma unroll
-      for (int i = 0; i < L::kPl; ++i) a[i].x &= ~m.x, a[i].y &= ~m.y, a[i].z &= ~m.z, a[i].w &= ~m.w;
-      acc[j] = dot_planes32(a, w[s], acc[j]);
-    }
-    settle_mfma32();
-#pragma unroll
-    for (int i = 0; i < 16; ++i) acc[j][i] = count[i] > 0.f ? __uint_as_float(0x7fc00000u) : acc[j][i];
-  }
+      for (int i = 0; i < 16; ++i) {
+        const int col = 32 * j + result_row(i, h);
+        if (col >= width) continue;
+        float x;
+        if constexpr (sizeof(T) == 4) x = p[(int64_t)r * width + col];
+        else x = __uint_as_float((uint32_t)p[(int64_t)r * width + col] << 16);
+        if (!(fabsf(x) <= 3.4028235e38f)) acc[j][i] = __uint_as_float(0x7fc00000u);
+      }
 }
 
 // A tensor's rows on their way to a tile of THREADS threads' workgroup: 16-byte vectors
@@ -199,7 +193,7 @@ struct TileStage {
   VectorReader read;
   uint4 r[kIt];
 
-  __device__ void init(const T* p, int rows_, int width_, int tid_) {
+  __device__ __forceinline__ void init(const T* p, int rows_, int width_, int tid_) {
     base = p, rows = rows_, width = width_, tid = tid_;
     vec = width % kEV == 0 && ((uintptr_t)p & 15) == 0;
     read = VectorReader(p, vec ? (int64_t)rows * width * (int)sizeof(T) : 0);
@@ -207,7 +201,7 @@ struct TileStage {
     off = col < width && row < ROWS ? (uint32_t)(row * width + col) * (uint32_t)sizeof(T) : kNoVector;
   }
   // the rows from r0 on
-  __device__ void fetch(int r0) {
+  __device__ __forceinline__ void fetch(int r0) {
 #pragma unroll
     for (int i = 0; i < kIt; ++i) r[i] = read(off + (uint32_t)(r0 + i * kPer) * (uint32_t)(width * (int)sizeof(T)));
   }
@@ -224,7 +218,7 @@ struct TileStage {
       dst[0] = x;
     }
   }
-  __device__ void put(u16* t, int r0) const {
+  __device__ __forceinline__ void put(u16* t, int r0) const {
     if (vec) {
 #pragma unroll
       for (int i = 0; i < kIt; ++i) {
@@ -248,6 +242,60 @@ struct TileStage {
       for (int i = tid; i < ROWS * 32 * ND; i += THREADS) {
         const int row = i / (32 * ND), col = i % (32 * ND);
         put_entry(t + L::at(row, col), r0 + row < rows && col < width ? base[(int64_t)(r0 + row) * width + col] : (T)0);
+      }
+    }
+  }
+};
+
+// Two tensors x and y walked together, ROWS rows at a time, through two LDS buffers of two tiles
+// (x, then y) each.  work(buffer, r0) is called for every 32 rows; the next rows are on their way
+// meanwhile: with two calls a step x's during the first and y's during the second, so
+// that the registers of one tensor do for both.
+template <typename T, int ND, int ROWS, int THREADS>
+struct PairStage {
+  using S = TileStage<T, ND, ROWS, THREADS>;
+  using L = typename S::L;
+  static_assert(ROWS == 32 || ROWS == 64, "one or two calls a step");
+  const T *x, *y;
+  int x_width, y_width, rows, tid;
+  S a, b;
+
+  __device__ __forceinline__ void open(const T* x_, int x_width_, const T* y_, int y_width_, int rows_, int tid_) {
+    x = x_, x_width = x_width_, y = y_, y_width = y_width_, rows = rows_, tid = tid_;
+  }
+  // both tensors' rows from r0 on, into a buffer
+  __device__ __forceinline__ void load(u16* buf, int r0) {
+    a.init(x, rows, x_width, tid);
+    b.init(y, rows, y_width, tid);
+    a.fetch(r0);
+    b.fetch(r0);
+    a.put(buf, r0);
+    b.put(buf + L::kElems, r0);
+  }
+  // the work on a buffer, while the rows from `next` on (none where !more) go to `other`
+  template <typename F>
+  __device__ __forceinline__ void step(const u16* buf, u16* other, bool more, int next, F&& work) {
+    if constexpr (ROWS == 64) {
+#pragma unroll 1
+      for (int r = 0; r < 64; r += 32) {
+        if (more) {
+          a.init(r ? y : x, rows, r ? y_width : x_width, tid);
+          a.fetch(next);
+        }
+        work(buf, r);
+        if (more) a.put(other + (r ? L::kElems : 0), next);
+      }
+    } else {
+      if (more) {
+        a.init(x, rows, x_width, tid);
+        b.init(y, rows, y_width, tid);
+        a.fetch(next);
+        b.fetch(next);
+      }
+      work(buf, 0);
+      if (more) {
+        a.put(other, next);
+        b.put(other + L::kElems, next);
       }
     }
   }

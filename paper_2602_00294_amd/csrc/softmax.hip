@@ -36,12 +36,10 @@ __global__ void __launch_bounds__(64 * W, sizeof(T) == 2 ? 2 : 1) softmax_prefil
   float top = -3.4028234e38f, sum = 0.f;
   const int end = min(len, 32 * kWaves * (blk + 1));  // keys that this workgroup sees
   if (32 * kWaves * blk < len) {
-    TileStage<T, ND, kKeys, kThreads> sk, sv;
-    sk.init((const T*)a.k + (int64_t)kvh * n * dk, len, dk, tid);
-    sv.init((const T*)a.v + (int64_t)kvh * n * dv, len, dv, tid);
     uint4 qf[2 * ND][L::kPl];
     load_own32<T, ND>((const T*)a.q + ((int64_t)qh * n + row) * dk, row < len, dk, qf);
     const float c = a.scale * kLog2e;
+    bool odd = false;  // whether the own tile holds values that are not finite
     // keys r0 .. +31 of a staged block; own: the queries' own tile, of which each sees its part
     auto work = [&](const u16* kt, const u16* vt, int r0, bool own) {
       f32x16 s = zero16();
@@ -52,7 +50,6 @@ __global__ void __launch_bounds__(64 * W, sizeof(T) == 2 ? 2 : 1) softmax_prefil
         s = dot_planes32(f, qf[i], s);
       }
       settle_mfma32();
-      bool odd = false;
       if (own) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = result_row(i, h) > l31 ? -INFINITY : s[i];
@@ -82,35 +79,27 @@ __global__ void __launch_bounds__(64 * W, sizeof(T) == 2 ? 2 : 1) softmax_prefil
       __builtin_amdgcn_sched_barrier(0);
       uint4 w[2][L::kPl];
       to_planes<L::kPl>(z, w);
-      if (__builtin_expect(odd, 0)) contract32_own<L, ND>(vt, r0, w, o, [&](int key) { return key <= l31; });
+      // (the own tile is the last one that a wave works on)
+      if (__builtin_expect(odd, 0)) contract32<L, ND, true>(vt, r0, w, o);
       else contract32<L, ND>(vt, r0, w, o);
     };
-    sk.fetch(0);
-    sv.fetch(0);
-    sk.put(smem16, 0);
-    sv.put(smem16 + L::kElems, 0);
+    PairStage<T, ND, kKeys, kThreads> stage;
+    stage.open((const T*)a.k + (int64_t)kvh * n * dk, dk, (const T*)a.v + (int64_t)kvh * n * dv, dv, len, tid);
+    stage.load(smem16, 0);
     __syncthreads();
     const int steps = (end + kKeys - 1) / kKeys;
     for (int st = 0; st < steps; ++st) {
-      const bool more = st + 1 < steps;
-      if (more) {
-        sk.fetch((st + 1) * kKeys);
-        sv.fetch((st + 1) * kKeys);
-      }
-      const u16* const kt = smem16 + (st & 1) * 2 * L::kElems;
-      const u16* const vt = kt + L::kElems;
-#pragma unroll 1
-      for (int r = 0; r < kKeys; r += 32) {
+      u16* const now = smem16 + (st & 1) * 2 * L::kElems;
+      u16* const next = smem16 + ((st + 1) & 1) * 2 * L::kElems;
+      stage.step(now, next, st + 1 < steps, (st + 1) * kKeys, [&](const u16* buf, int r) {
         const int k0 = st * kKeys + r;
-        if (k0 <= q0) work(kt, vt, r, k0 == q0);
-      }
-      if (more) {
-        sk.put(smem16 + ((st + 1) & 1) * 2 * L::kElems, (st + 1) * kKeys);
-        sv.put(smem16 + ((st + 1) & 1) * 2 * L::kElems + L::kElems, (st + 1) * kKeys);
-      }
+        if (k0 <= q0) work(buf, buf + L::kElems, r, k0 == q0);
+      });
       __syncthreads();
     }
     settle_mfma32();
+    if (__builtin_expect(odd, 0))
+      mark_not_finite((const T*)a.v + ((int64_t)kvh * n + q0) * dv, dv, 0, row < len ? l31 : -1, o);
   }
   if (row >= n) return;
   sum += __shfl_xor(sum, 32);
@@ -135,7 +124,8 @@ hipError_t launch_prefill_w(const SoftmaxArgs& a, hipStream_t s) {
 
 template <typename T, int ND>
 hipError_t launch_prefill(const SoftmaxArgs& a, hipStream_t s) {
-  if (sizeof(T) == 2 && (int64_t)a.heads * a.G * ((a.n + 255) / 256) >= 256) return launch_prefill_w<T, ND, 8>(a, s);
+  if constexpr (sizeof(T) == 2)
+    if ((int64_t)a.heads * a.G * ((a.n + 255) / 256) >= 256) return launch_prefill_w<T, ND, 8>(a, s);
   return launch_prefill_w<T, ND, 4>(a, s);
 }
 

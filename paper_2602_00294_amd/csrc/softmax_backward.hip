@@ -76,9 +76,6 @@ __global__ void __launch_bounds__(64 * W, sizeof(T) == 2 ? 2 : 1) softmax_rows(S
 #pragma unroll
   for (int j = 0; j < ND; ++j) acc[j] = zero16();
   if (32 * W * blk < len) {
-    TileStage<T, ND, kRows, kThreads> sk, sv;
-    sk.init((const T*)a.k + (int64_t)kvh * n * dk, len, dk, tid);
-    sv.init((const T*)a.v + (int64_t)kvh * n * dv, len, dv, tid);
     uint4 qf[2 * ND][L::kPl], df[2 * ND][L::kPl];
     load_own32<T, ND>((const T*)a.y + at * dv, row < len, dv, qf);
     load_own32<T, ND>((const T*)a.dy + at * dv, row < len, dv, df);
@@ -87,12 +84,12 @@ __global__ void __launch_bounds__(64 * W, sizeof(T) == 2 ? 2 : 1) softmax_rows(S
     if (row < len && h == 0) a.delta[at] = delta;
     load_own32<T, ND>((const T*)a.q + at * dk, row < len, dk, qf);
     const float c = a.scale * kLog2e, lse = row < len ? a.lse[at] * kLog2e : 0.f;
+    bool odd = false;  // whether the own tile holds values that are not finite
     auto work = [&](const u16* kt, const u16* vt, int r0, bool own) {
       f32x16 s = dot_rows32<L, ND>(kt, r0, qf), d = dot_rows32<L, ND>(vt, r0, df);
       float e[16];
 #pragma unroll
       for (int i = 0; i < 16; ++i) e[i] = exp2_fast(fmaf(s[i], c, -lse)) * (d[i] - delta);
-      bool odd = false;
       if (own) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) e[i] = result_row(i, h) > l31 ? 0.f : e[i];
@@ -100,170 +97,192 @@ __global__ void __launch_bounds__(64 * W, sizeof(T) == 2 ? 2 : 1) softmax_rows(S
       }
       uint4 w[2][L::kPl];
       to_planes<L::kPl>(e, w);
-      if (__builtin_expect(odd, 0)) contract32_own<L, ND>(kt, r0, w, acc, [&](int key) { return key <= l31; });
+      // (the own tile is the last one that a wave works on)
+      if (__builtin_expect(odd, 0)) contract32<L, ND, true>(kt, r0, w, acc);
       else contract32<L, ND>(kt, r0, w, acc);
     };
-    sk.fetch(0);
-    sv.fetch(0);
-    sk.put(smem16, 0);
-    sv.put(smem16 + L::kElems, 0);
+    PairStage<T, ND, kRows, kThreads> stage;
+    stage.open((const T*)a.k + (int64_t)kvh * n * dk, dk, (const T*)a.v + (int64_t)kvh * n * dv, dv, len, tid);
+    stage.load(smem16, 0);
     __syncthreads();
     const int steps = (min(len, 32 * W * (blk + 1)) + kRows - 1) / kRows;
     for (int st = 0; st < steps; ++st) {
-      const bool more = st + 1 < steps;
-      if (more) {
-        sk.fetch((st + 1) * kRows);
-        sv.fetch((st + 1) * kRows);
-      }
-      const u16* const kt = smem16 + (st & 1) * 2 * L::kElems;
-#pragma unroll 1
-      for (int r = 0; r < kRows; r += 32) {
+      u16* const now = smem16 + (st & 1) * 2 * L::kElems;
+      u16* const next = smem16 + ((st + 1) & 1) * 2 * L::kElems;
+      stage.step(now, next, st + 1 < steps, (st + 1) * kRows, [&](const u16* buf, int r) {
         const int k0 = st * kRows + r;
-        if (k0 <= q0) work(kt, kt + L::kElems, r, k0 == q0);
-      }
-      if (more) {
-        sk.put(smem16 + ((st + 1) & 1) * 2 * L::kElems, (st + 1) * kRows);
-        sv.put(smem16 + ((st + 1) & 1) * 2 * L::kElems + L::kElems, (st + 1) * kRows);
-      }
+        if (k0 <= q0) work(buf, buf + L::kElems, r, k0 == q0);
+      });
       __syncthreads();
     }
     settle_mfma32();
+    if (__builtin_expect(odd, 0))
+      mark_not_finite((const T*)a.k + ((int64_t)kvh * n + q0) * dk, dk, 0, row < len ? l31 : -1, acc);
   }
   if (row < n) store_row32<T, ND>((T*)a.dq + at * dk, dk, acc, row < len ? a.scale : 0.f, row >= len);
 }
 
-template <typename T, int ND, int W>
-__global__ void __launch_bounds__(64 * W, sizeof(T) == 2 && ND <= 2 ? 2 : 1) softmax_cols(SoftmaxGradArgs a, int blocks) {
-  constexpr int kRows = kStaged<T>, kThreads = 64 * W;
+// SPLIT: the sums of dk and of dv, 32 ND numbers a lane each, go to two waves with the same keys, wave
+// w of the first half dv, of the second half dk: both in one wave would leave it no
+// registers at ND >= 3 (they moved through the accumulation registers: 487 vector instructions a tile
+// instead of 150).  The scores are formed twice then.
+template <typename T, int ND, int W, bool SPLIT>
+__global__ void __launch_bounds__(64 * W, sizeof(T) == 2 ? 2 : 1) softmax_cols(SoftmaxGradArgs a, int blocks) {
+  constexpr int kRows = kStaged<T>, kThreads = 64 * W, kTiles = SPLIT ? W / 2 : W;
   using L = PairTile<T, ND, kRows>;
   constexpr int kBuf = 2 * L::kElems + 4 * kRows;  // Q rows, dy rows, then lse and delta as float
   extern __shared__ __attribute__((aligned(16))) u16 smem16[];
   const int tid = threadIdx.x, lane = tid & 63, l31 = lane & 31, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const bool for_k = !SPLIT || wave >= kTiles;
   int kvh, blk;
   if (!locate(a.heads, blocks, kvh, blk)) return;  // (the first keys have the longest sweeps)
   const int n = a.n, dk = a.dk_, dv = a.dv_;
   const int len = tokens_of(a.lengths, kvh / a.H, n);
-  const int k0 = 32 * (W * blk + wave), row = k0 + l31;
+  const int k0 = 32 * (kTiles * blk + wave % kTiles), row = k0 + l31;
   const int64_t at = (int64_t)kvh * n + row;
-  f32x16 gk[ND], gv[ND];
+  f32x16 acc[SPLIT ? 1 : 2][ND];  // dv (or dk), dk
 #pragma unroll
-  for (int j = 0; j < ND; ++j) gk[j] = gv[j] = zero16();
-  if (32 * W * blk < len) {
+  for (int i = 0; i < (SPLIT ? 1 : 2); ++i)
+#pragma unroll
+    for (int j = 0; j < ND; ++j) acc[i][j] = zero16();
+  if (32 * kTiles * blk < len) {
     uint4 kf[2 * ND][L::kPl], vf[2 * ND][L::kPl];
     load_own32<T, ND>((const T*)a.k + at * dk, row < len, dk, kf);
-    load_own32<T, ND>((const T*)a.v + at * dv, row < len, dv, vf);
+    load_own32<T, ND>((const T*)a.v + at * dv, row < len && for_k, dv, vf);
     const float c = a.scale * kLog2e;
-    auto work = [&](const u16* qt, const u16* yt, const float* stat, int r0, bool own) {
-      f32x16 s = dot_rows32<L, ND>(qt, r0, kf), d = dot_rows32<L, ND>(yt, r0, vf);
+    bool odd_q = false, odd_y = false;  // whether own tiles held values that are not finite
+    auto work = [&](const u16* qt, const float* stat, int r0, bool own) {
+      const u16* const yt = qt + L::kElems;
+      f32x16 s = dot_rows32<L, ND>(qt, r0, kf);
       float p[16], e[16];
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
-        const float4 z4 = *(const float4*)(stat + r0 + 8 * g + 4 * h), d4 = *(const float4*)(stat + kRows + r0 + 8 * g + 4 * h);
-        const float z[4] = {z4.x, z4.y, z4.z, z4.w}, de[4] = {d4.x, d4.y, d4.z, d4.w};
+        const float4 z4 = *(const float4*)(stat + r0 + 8 * g + 4 * h);
+        const float z[4] = {z4.x, z4.y, z4.z, z4.w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          p[4 * g + i] = exp2_fast(fmaf(s[4 * g + i], c, -z[i]));
-          e[4 * g + i] = p[4 * g + i] * (d[4 * g + i] - de[i]);
-        }
+        for (int i = 0; i < 4; ++i) p[4 * g + i] = exp2_fast(fmaf(s[4 * g + i], c, -z[i]));
       }
-      bool odd_q = false, odd_y = false;
+      if (for_k) {
+        const f32x16 d = dot_rows32<L, ND>(yt, r0, vf);
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const float4 d4 = *(const float4*)(stat + kRows + r0 + 8 * g + 4 * h);
+          const float de[4] = {d4.x, d4.y, d4.z, d4.w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) e[4 * g + i] = p[4 * g + i] * (d[4 * g + i] - de[i]);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) e[i] = p[i];
+      }
       if (own) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          p[i] = result_row(i, h) < l31 ? 0.f : p[i];
+          if (!SPLIT) p[i] = result_row(i, h) < l31 ? 0.f : p[i];
           e[i] = result_row(i, h) < l31 ? 0.f : e[i];
         }
-        odd_q = tile_not_finite<L, ND>(qt, r0);
-        odd_y = tile_not_finite<L, ND>(yt, r0);
       }
       uint4 w[2][L::kPl];
-      auto seen = [&](int query) { return query >= l31; };
-      to_planes<L::kPl>(p, w);
-      if (__builtin_expect(odd_y, 0)) contract32_own<L, ND>(yt, r0, w, gv, seen);
-      else contract32<L, ND>(yt, r0, w, gv);
-      to_planes<L::kPl>(e, w);
-      if (__builtin_expect(odd_q, 0)) contract32_own<L, ND>(qt, r0, w, gk, seen);
-      else contract32<L, ND>(qt, r0, w, gk);
+      if constexpr (SPLIT) {
+        const u16* const t = for_k ? qt : yt;
+        const bool odd = own && tile_not_finite<L, ND>(t, r0);
+        odd_q |= odd;
+        to_planes<L::kPl>(e, w);
+        if (__builtin_expect(odd, 0)) contract32<L, ND, true>(t, r0, w, acc[0]);
+        else contract32<L, ND>(t, r0, w, acc[0]);
+      } else {
+        const bool bad_y = own && tile_not_finite<L, ND>(yt, r0), bad_q = own && tile_not_finite<L, ND>(qt, r0);
+        odd_y |= bad_y;
+        odd_q |= bad_q;
+        to_planes<L::kPl>(p, w);
+        if (__builtin_expect(bad_y, 0)) contract32<L, ND, true>(yt, r0, w, acc[0]);
+        else contract32<L, ND>(yt, r0, w, acc[0]);
+        to_planes<L::kPl>(e, w);
+        if (__builtin_expect(bad_q, 0)) contract32<L, ND, true>(qt, r0, w, acc[1]);
+        else contract32<L, ND>(qt, r0, w, acc[1]);
+      }
     };
-    TileStage<T, ND, kRows, kThreads> sq, sy;
-    const int first = 32 * W * blk / kRows, steps = (len + kRows - 1) / kRows - first;
-    float st_ = 0.f;
+    PairStage<T, ND, kRows, kThreads> stage;
+    const int first = 32 * kTiles * blk / kRows, steps = (len + kRows - 1) / kRows - first;
     int64_t base = 0;  // the member's first row
     auto open = [&](int g) {
       base = ((int64_t)kvh * a.G + g) * n;
-      sq.init((const T*)a.q + base * dk, len, dk, tid);
-      sy.init((const T*)a.dy + base * dv, len, dv, tid);
+      stage.open((const T*)a.q + base * dk, dk, (const T*)a.dy + base * dv, dv, len, tid);
     };
-    auto fetch = [&](int t0) {
-      sq.fetch(t0);
-      sy.fetch(t0);
-      if (tid < 2 * kRows) {
-        const int t = t0 + tid % kRows;
-        // (a row behind the sequence: probability zero)
-        if (tid < kRows) st_ = t < len ? a.lse[base + t] * kLog2e : INFINITY;
-        else st_ = t < len ? a.delta[base + t] : 0.f;
-      }
-    };
-    auto put = [&](int b, int t0) {
-      u16* const t = smem16 + b * kBuf;
-      sq.put(t, t0);
-      sy.put(t + L::kElems, t0);
-      if (tid < 2 * kRows) ((float*)(t + 2 * L::kElems))[tid] = st_;
+    auto stat_of = [&](int t0) {  // lse and delta of the staged rows, one or the other for each thread
+      const int t = t0 + tid % kRows;
+      if (tid >= 2 * kRows) return 0.f;
+      // (a row behind the sequence: probability zero)
+      if (tid < kRows) return t < len ? a.lse[base + t] * kLog2e : INFINITY;
+      return t < len ? a.delta[base + t] : 0.f;
     };
     open(0);
-    fetch(first * kRows);
-    put(0, first * kRows);
+    const float st0 = stat_of(first * kRows);
+    stage.load(smem16, first * kRows);
+    if (tid < 2 * kRows) ((float*)(smem16 + 2 * L::kElems))[tid] = st0;
     __syncthreads();
     const int total = steps * a.G;
     for (int u = 0, st = 0, g = 0; u < total; ++u) {
+      u16* const now = smem16 + (u & 1) * kBuf;
+      u16* const then = smem16 + ((u + 1) & 1) * kBuf;
       const bool more = u + 1 < total;
       int next = st + 1;
       if (next == steps) next = 0;
-      if (more) {
-        if (next == 0) open(++g);
-        fetch((first + next) * kRows);
-      }
-      const u16* const qt = smem16 + (u & 1) * kBuf;
-#pragma unroll 1
-      for (int r = 0; r < kRows; r += 32) {
+      if (more && next == 0) open(++g);
+      const float stat = more ? stat_of((first + next) * kRows) : 0.f;
+      stage.step(now, then, more, (first + next) * kRows, [&](const u16* buf, int r) {
         const int t0 = (first + st) * kRows + r;
-        if (t0 >= k0) work(qt, qt + L::kElems, (const float*)(qt + 2 * L::kElems), r, t0 == k0);
-      }
-      if (more) put((u + 1) & 1, (first + next) * kRows);
+        if (t0 >= k0) work(buf, (const float*)(buf + 2 * L::kElems), r, t0 == k0);
+      });
+      if (more && tid < 2 * kRows) ((float*)(then + 2 * L::kElems))[tid] = stat;
       st = next;
       __syncthreads();
     }
     settle_mfma32();
+    if (__builtin_expect(odd_q || odd_y, 0)) {
+      const int last = row < len ? min(31, len - 1 - k0) : -1;
+      for (int g = 0; g < a.G; ++g) {
+        const int64_t own = ((int64_t)kvh * a.G + g) * n + k0;
+        if (for_k) mark_not_finite((const T*)a.q + own * dk, dk, l31, last, acc[SPLIT ? 0 : 1]);
+        if (!SPLIT || !for_k) mark_not_finite((const T*)a.dy + own * dv, dv, l31, last, acc[0]);
+      }
+    }
   }
   if (row >= n) return;
-  store_row32<T, ND>((T*)a.dk + at * dk, dk, gk, a.scale, row >= len);
-  store_row32<T, ND>((T*)a.dv + at * dv, dv, gv, 1.f, row >= len);
+  if (for_k) store_row32<T, ND>((T*)a.dk + at * dk, dk, acc[SPLIT ? 0 : 1], a.scale, row >= len);
+  if (!SPLIT || !for_k) store_row32<T, ND>((T*)a.dv + at * dv, dv, acc[0], 1.f, row >= len);
 }
 
-template <typename T, int ND, int W>
+// WR, WC: waves of a workgroup of the two kernels.
+template <typename T, int ND, int WR, int WC, bool SPLIT>
 hipError_t launch_backward_w(const SoftmaxGradArgs& a, hipStream_t s) {
   using L = PairTile<T, ND, kStaged<T>>;
   constexpr int rows_bytes = 4 * L::kBytes, cols_bytes = 2 * (2 * L::kBytes + 8 * kStaged<T>);
   static_assert(cols_bytes <= 160 * 1024, "LDS of one workgroup");
-  auto rows = softmax_rows<T, ND, W>;
-  auto cols = softmax_cols<T, ND, W>;
+  auto rows = softmax_rows<T, ND, WR>;
+  auto cols = softmax_cols<T, ND, WC, SPLIT>;
   if (cols_bytes > 64 * 1024) {
     hipError_t e = hipFuncSetAttribute((const void*)rows, hipFuncAttributeMaxDynamicSharedMemorySize, rows_bytes);
     if (e == hipSuccess) e = hipFuncSetAttribute((const void*)cols, hipFuncAttributeMaxDynamicSharedMemorySize, cols_bytes);
     if (e != hipSuccess) return e;
   }
-  const int blocks = (a.n + 32 * W - 1) / (32 * W);
-  hipLaunchKernelGGL(rows, dim3((unsigned)head_blocks(a.heads * a.G, blocks)), dim3(64 * W), rows_bytes, s, a, blocks);
+  const int row_blocks = (a.n + 32 * WR - 1) / (32 * WR);
+  hipLaunchKernelGGL(rows, dim3((unsigned)head_blocks(a.heads * a.G, row_blocks)), dim3(64 * WR), rows_bytes, s, a,
+                     row_blocks);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(cols, dim3((unsigned)head_blocks(a.heads, blocks)), dim3(64 * W), cols_bytes, s, a, blocks);
+  constexpr int keys = 32 * (SPLIT ? WC / 2 : WC);
+  const int col_blocks = (a.n + keys - 1) / keys;
+  hipLaunchKernelGGL(cols, dim3((unsigned)head_blocks(a.heads, col_blocks)), dim3(64 * WC), cols_bytes, s, a, col_blocks);
   return hipGetLastError();
 }
 
 template <int ND>
 hipError_t launch_backward(const SoftmaxGradArgs& a, bool bf16, hipStream_t s) {
-  return bf16 ? launch_backward_w<u16, ND, 4>(a, s) : launch_backward_w<float, ND, 4>(a, s);
+  constexpr bool wide = ND >= 3;
+  if (!bf16) return launch_backward_w<float, ND, 4, 4, (ND >= 2)>(a, s);
+  return launch_backward_w<u16, ND, wide ? 8 : 4, wide ? 8 : 4, wide>(a, s);
 }
 
 }  // namespace
