@@ -55,6 +55,13 @@ __device__ __forceinline__ void settle_mfma32() {
   asm volatile("s_nop 15\n\ts_nop 3");
   __builtin_amdgcn_sched_barrier(0);
 }
+// Keeps what follows inside its branch: the compiler would rather compute both ways (the test of a tile
+// for values that are not finite, 170 instructions, for every tile instead of one).
+__device__ __forceinline__ void stay_in_branch() { asm volatile(""); }
+
+__device__ __forceinline__ float entry_of(const float* p, int64_t i) { return p[i]; }
+__device__ __forceinline__ float entry_of(const u16* p, int64_t i) { return __uint_as_float((uint32_t)p[i] << 16); }
+
 // Row of a result's number i.
 __device__ __forceinline__ int result_row(int i, int h) { return 8 * (i >> 2) + 4 * h + (i & 3); }
 
@@ -119,30 +126,66 @@ __device__ __forceinline__ uint4 not_finite_entries(const uint4& w) {
 }
 
 // acc[j] += (rows r0 .. r0 + 31 of the tile, columns 32 j .. +31)^T times the 32 x 32 weights w.
-// CLEAN: values of the tile that are not finite count as zero: w is zero for rows that
-// its columns do not see, and not finite times 0 would not be.  mark_not_finite then
-// gives the others their due.
-template <typename L, int ND, bool CLEAN = false>
+template <typename L, int ND>
 __device__ __forceinline__ void contract32(const u16* t, int r0, const uint4 (&w)[2][L::kPl], f32x16 (&acc)[ND]) {
 #pragma unroll
   for (int j = 0; j < ND; ++j)
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-      if (CLEAN) __builtin_amdgcn_sched_barrier(0);  // (rare: one at a time takes fewer registers)
       uint4 a[L::kPl];
       L::load_transposed(t, r0 + 16 * s, j, a);
-      if constexpr (CLEAN) {
-        const uint4 m = not_finite_entries(a[0]);
-#pragma unroll
-        for (int i = 0; i < L::kPl; ++i) a[i].x &= ~m.x, a[i].y &= ~m.y, a[i].z &= ~m.z, a[i].w &= ~m.w;
-      }
       acc[j] = dot_planes32(a, w[s], acc[j]);
     }
 }
 
+// A tile on the diagonal has masked pairs, and a masked weight's zero times a value that is not
+// finite would be no zero.  So such a tile (tile_not_finite) stays out of the
+// products, and the wave goes over its rows one by one at the end with these two:
+// this lane's column times a row, and acc += weight times a row.
+template <typename T, int ND, int PL>
+__device__ __forceinline__ float dot_row(const uint4 (&own)[2 * ND][PL], const T* row, int width) {
+  const int h = (threadIdx.x & 63) >> 5;
+  float r = 0.f;
+#pragma unroll
+  for (int s = 0; s < 2 * ND; ++s) {
+    __builtin_amdgcn_sched_barrier(0);  // (a few entries at a time: registers)
+    float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = PL - 1; i >= 0; --i) {
+      uint32_t w[4] = {own[s][i].x, own[s][i].y, own[s][i].z, own[s][i].w};
+      // (unpacked for each row anew: all of them, kept over the loop, would take the sweep's registers)
+      asm volatile("" : "+v"(w[0]), "+v"(w[1]), "+v"(w[2]), "+v"(w[3]));
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[2 * j] += lo_f32(w[j]), x[2 * j + 1] += hi_f32(w[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int col = 16 * s + 8 * h + j;
+      if (col < width) r = fmaf(x[j], entry_of(row, col), r);
+    }
+  }
+  return r + __shfl_xor(r, 32);
+}
+template <typename T, int ND>
+__device__ __forceinline__ void add_row(const T* row, int width, float weight, f32x16 (&acc)[ND]) {
+  const int h = (threadIdx.x & 63) >> 5;
+#pragma unroll
+  for (int j = 0; j < ND; ++j)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int col = 32 * j + result_row(i, h);
+      if (i % 4 == 0) __builtin_amdgcn_sched_barrier(0);
+      if (col < width) acc[j][i] = fmaf(weight, entry_of(row, col), acc[j][i]);
+    }
+}
+
+// (a float32 value beyond bfloat16's range is an infinity in its first plane)
+__device__ __forceinline__ bool bf16_finite(float x) { return (pack2(x, 0.f) & 0x7f80u) != 0x7f80u; }
+
 // Whether rows r0 .. r0 + 31 of the tile hold a value that is not finite (for the whole wave).
 template <typename L, int ND>
 __device__ __forceinline__ bool tile_not_finite(const u16* t, int r0) {
+  stay_in_branch();
   uint32_t bad = 0;
 #pragma unroll
   for (int s = 0; s < 2 * ND; ++s) {
@@ -152,26 +195,6 @@ __device__ __forceinline__ bool tile_not_finite(const u16* t, int r0) {
     bad |= m.x | m.y | m.z | m.w;
   }
   return __ballot(bad != 0) != 0;
-}
-
-// Makes NaN of the results in whose columns one of the rows first .. last of p (those that this
-// lane's column sees of its own tile) is not finite.
-template <typename T, int ND>
-__device__ __forceinline__ void mark_not_finite(const T* p, int width, int first, int last, f32x16 (&acc)[ND]) {
-  const int h = (threadIdx.x & 63) >> 5;
-#pragma unroll 1
-  for (int r = first; r <= last; ++r)
-#pragma unroll
-    for (int j = 0; j < ND; ++j)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int col = 32 * j + result_row(i, h);
-        if (col >= width) continue;
-        float x;
-        if constexpr (sizeof(T) == 4) x = p[(int64_t)r * width + col];
-        else x = __uint_as_float((uint32_t)p[(int64_t)r * width + col] << 16);
-        if (!(fabsf(x) <= 3.4028235e38f)) acc[j][i] = __uint_as_float(0x7fc00000u);
-      }
 }
 
 // A tensor's rows on their way to a tile of THREADS threads' workgroup: 16-byte vectors

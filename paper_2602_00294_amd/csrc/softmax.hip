@@ -51,16 +51,16 @@ __global__ void __launch_bounds__(64 * W, sizeof(T) == 2 ? 2 : 1) softmax_prefil
       }
       settle_mfma32();
       if (own) {
+        stay_in_branch();
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = result_row(i, h) > l31 ? -INFINITY : s[i];
         odd = tile_not_finite<L, ND>(vt, r0);
+        if (odd) return;
       }
-      float z[16], most = -3.4028234e38f;
+      float most = s[0];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        z[i] = s[i] * c;
-        most = fmaxf(most, z[i]);
-      }
+      for (int i = 1; i < 16; ++i) most = fmaxf(most, s[i]);
+      most *= c;
       if (__ballot(most > top + 8.f)) {
         const float next = fmaxf(top, fmaxf(most, __shfl_xor(most, 32)));
         const float keep = exp2_fast(top - next);
@@ -71,17 +71,16 @@ __global__ void __launch_bounds__(64 * W, sizeof(T) == 2 ? 2 : 1) softmax_prefil
 #pragma unroll
           for (int i = 0; i < 16; ++i) o[j][i] *= keep;
       }
+      float z[16];
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        z[i] = exp2_fast(z[i] - top);
+        z[i] = exp2_fast(fmaf(s[i], c, -top));
         sum += z[i];
       }
       __builtin_amdgcn_sched_barrier(0);
       uint4 w[2][L::kPl];
       to_planes<L::kPl>(z, w);
-      // (the own tile is the last one that a wave works on)
-      if (__builtin_expect(odd, 0)) contract32<L, ND, true>(vt, r0, w, o);
-      else contract32<L, ND>(vt, r0, w, o);
+      contract32<L, ND>(vt, r0, w, o);
     };
     PairStage<T, ND, kKeys, kThreads> stage;
     stage.open((const T*)a.k + (int64_t)kvh * n * dk, dk, (const T*)a.v + (int64_t)kvh * n * dv, dv, len, tid);
@@ -98,8 +97,22 @@ __global__ void __launch_bounds__(64 * W, sizeof(T) == 2 ? 2 : 1) softmax_prefil
       __syncthreads();
     }
     settle_mfma32();
-    if (__builtin_expect(odd, 0))
-      mark_not_finite((const T*)a.v + ((int64_t)kvh * n + q0) * dv, dv, 0, row < len ? l31 : -1, o);
+    if (__builtin_expect(odd, 0)) {
+#pragma unroll 1
+      for (int r = 0; r < min(32, len - q0); ++r) {
+        const int64_t key = (int64_t)kvh * n + q0 + r;
+        const float z = c * dot_row<T, ND>(qf, (const T*)a.k + key * dk, dk);
+        if (r > l31) continue;
+        const float next = fmaxf(top, z), keep = exp2_fast(top - next), p = exp2_fast(z - next);
+        top = next;
+        sum = sum * keep + (h == 0 ? p : 0.f);
+#pragma unroll
+        for (int j = 0; j < ND; ++j)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[j][i] *= keep;
+        add_row((const T*)a.v + key * dv, dv, p, o);
+      }
+    }
   }
   if (row >= n) return;
   sum += __shfl_xor(sum, 32);

@@ -91,15 +91,15 @@ __global__ void __launch_bounds__(64 * W, sizeof(T) == 2 ? 2 : 1) softmax_rows(S
 #pragma unroll
       for (int i = 0; i < 16; ++i) e[i] = exp2_fast(fmaf(s[i], c, -lse)) * (d[i] - delta);
       if (own) {
+        stay_in_branch();
 #pragma unroll
         for (int i = 0; i < 16; ++i) e[i] = result_row(i, h) > l31 ? 0.f : e[i];
         odd = tile_not_finite<L, ND>(kt, r0);
+        if (odd) return;
       }
       uint4 w[2][L::kPl];
       to_planes<L::kPl>(e, w);
-      // (the own tile is the last one that a wave works on)
-      if (__builtin_expect(odd, 0)) contract32<L, ND, true>(kt, r0, w, acc);
-      else contract32<L, ND>(kt, r0, w, acc);
+      contract32<L, ND>(kt, r0, w, acc);
     };
     PairStage<T, ND, kRows, kThreads> stage;
     stage.open((const T*)a.k + (int64_t)kvh * n * dk, dk, (const T*)a.v + (int64_t)kvh * n * dv, dv, len, tid);
@@ -116,8 +116,15 @@ __global__ void __launch_bounds__(64 * W, sizeof(T) == 2 ? 2 : 1) softmax_rows(S
       __syncthreads();
     }
     settle_mfma32();
-    if (__builtin_expect(odd, 0))
-      mark_not_finite((const T*)a.k + ((int64_t)kvh * n + q0) * dk, dk, 0, row < len ? l31 : -1, acc);
+    if (__builtin_expect(odd, 0)) {
+#pragma unroll 1
+      for (int r = 0; r < min(32, len - q0); ++r) {
+        const int64_t key = (int64_t)kvh * n + q0 + r;
+        const float z = dot_row<T, ND>(qf, (const T*)a.k + key * dk, dk);
+        const float d = dot_row<T, ND>(df, (const T*)a.v + key * dv, dv);
+        if (r <= l31) add_row((const T*)a.k + key * dk, dk, exp2_fast(fmaf(z, c, -lse)) * (d - delta), acc);
+      }
+    }
   }
   if (row < n) store_row32<T, ND>((T*)a.dq + at * dk, dk, acc, row < len ? a.scale : 0.f, row >= len);
 }
@@ -151,7 +158,7 @@ __global__ void __launch_bounds__(64 * W, sizeof(T) == 2 ? 2 : 1) softmax_cols(S
     load_own32<T, ND>((const T*)a.k + at * dk, row < len, dk, kf);
     load_own32<T, ND>((const T*)a.v + at * dv, row < len && for_k, dv, vf);
     const float c = a.scale * kLog2e;
-    bool odd_q = false, odd_y = false;  // whether own tiles held values that are not finite
+    bool odd = false;  // whether own tiles hold values that are not finite: such a member's is left out
     auto work = [&](const u16* qt, const float* stat, int r0, bool own) {
       const u16* const yt = qt + L::kElems;
       f32x16 s = dot_rows32<L, ND>(qt, r0, kf);
@@ -177,30 +184,26 @@ __global__ void __launch_bounds__(64 * W, sizeof(T) == 2 ? 2 : 1) softmax_cols(S
         for (int i = 0; i < 16; ++i) e[i] = p[i];
       }
       if (own) {
+        stay_in_branch();
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           if (!SPLIT) p[i] = result_row(i, h) < l31 ? 0.f : p[i];
           e[i] = result_row(i, h) < l31 ? 0.f : e[i];
         }
+        if (tile_not_finite<L, ND>(qt, r0) || tile_not_finite<L, ND>(yt, r0)) {
+          odd = true;
+          return;
+        }
       }
       uint4 w[2][L::kPl];
       if constexpr (SPLIT) {
-        const u16* const t = for_k ? qt : yt;
-        const bool odd = own && tile_not_finite<L, ND>(t, r0);
-        odd_q |= odd;
         to_planes<L::kPl>(e, w);
-        if (__builtin_expect(odd, 0)) contract32<L, ND, true>(t, r0, w, acc[0]);
-        else contract32<L, ND>(t, r0, w, acc[0]);
+        contract32<L, ND>(for_k ? qt : yt, r0, w, acc[0]);
       } else {
-        const bool bad_y = own && tile_not_finite<L, ND>(yt, r0), bad_q = own && tile_not_finite<L, ND>(qt, r0);
-        odd_y |= bad_y;
-        odd_q |= bad_q;
         to_planes<L::kPl>(p, w);
-        if (__builtin_expect(bad_y, 0)) contract32<L, ND, true>(yt, r0, w, acc[0]);
-        else contract32<L, ND>(yt, r0, w, acc[0]);
+        contract32<L, ND>(yt, r0, w, acc[0]);
         to_planes<L::kPl>(e, w);
-        if (__builtin_expect(bad_q, 0)) contract32<L, ND, true>(qt, r0, w, acc[1]);
-        else contract32<L, ND>(qt, r0, w, acc[1]);
+        contract32<L, ND>(qt, r0, w, acc[1]);
       }
     };
     PairStage<T, ND, kRows, kThreads> stage;
@@ -240,12 +243,25 @@ __global__ void __launch_bounds__(64 * W, sizeof(T) == 2 ? 2 : 1) softmax_cols(S
       __syncthreads();
     }
     settle_mfma32();
-    if (__builtin_expect(odd_q || odd_y, 0)) {
-      const int last = row < len ? min(31, len - 1 - k0) : -1;
+    if (__builtin_expect(odd, 0)) {
+      const int rows = min(32, len - k0);
+#pragma unroll 1
       for (int g = 0; g < a.G; ++g) {
-        const int64_t own = ((int64_t)kvh * a.G + g) * n + k0;
-        if (for_k) mark_not_finite((const T*)a.q + own * dk, dk, l31, last, acc[SPLIT ? 0 : 1]);
-        if (!SPLIT || !for_k) mark_not_finite((const T*)a.dy + own * dv, dv, l31, last, acc[0]);
+        const int64_t t0 = ((int64_t)kvh * a.G + g) * n + k0;
+        const T* const q = (const T*)a.q + t0 * dk;
+        const T* const dy = (const T*)a.dy + t0 * dv;
+        uint32_t bad = 0;
+        for (int i = lane; i < rows * dk; i += 64) bad |= (uint32_t)!bf16_finite(entry_of(q, i));
+        for (int i = lane; i < rows * dv; i += 64) bad |= (uint32_t)!bf16_finite(entry_of(dy, i));
+        if (__ballot(bad != 0) == 0) continue;
+#pragma unroll 1
+        for (int r = 0; r < rows; ++r) {
+          const float p = exp2_fast(fmaf(dot_row<T, ND>(kf, q + r * dk, dk), c, -kLog2e * a.lse[t0 + r]));
+          const float e = for_k ? p * (dot_row<T, ND>(vf, dy + r * dv, dv) - a.delta[t0 + r]) : 0.f;
+          if (r < l31) continue;
+          if (for_k) add_row(q + r * dk, dk, e, acc[SPLIT ? 0 : 1]);
+          if (!SPLIT || !for_k) add_row(dy + r * dv, dv, p, acc[0]);
+        }
       }
     }
   }

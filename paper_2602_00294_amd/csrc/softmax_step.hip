@@ -99,12 +99,13 @@ softmax_step_kernel(SoftmaxStepArgs a, SoftmaxStepPlan p) {
       L::load_rows(tile, 0, i, f);
       s = dot_planes32(f, qf[i], s);
     }
-    float z[16], most = -3.4028234e38f;
+    float most = -INFINITY;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      z[i] = r0 + result_row(i, h) > at ? -INFINITY : s[i] * c;
-      most = fmaxf(most, z[i]);
+      s[i] = r0 + result_row(i, h) > at ? -INFINITY : s[i];
+      most = fmaxf(most, s[i]);
     }
+    most *= c;
     stage(sv, r0, vn, dv);
     if (r0 + kStep < end) sv.fetch(r0 + kStep);
     if (__ballot(most > top + 8.f)) {
@@ -117,9 +118,10 @@ softmax_step_kernel(SoftmaxStepArgs a, SoftmaxStepPlan p) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[j][i] *= keep;
     }
+    float z[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      z[i] = exp2_fast(z[i] - top);
+      z[i] = exp2_fast(fmaf(s[i], c, -top));
       sum += z[i];
     }
     uint4 w[2][L::kPl];
