@@ -298,28 +298,17 @@ struct PairStage {
   // the work on a buffer, while the rows from `next` on (none where !more) go to `other`
   template <typename F>
   __device__ __forceinline__ void step(const u16* buf, u16* other, bool more, int next, F&& work) {
-    if constexpr (ROWS == 64) {
+    if (more) {
+      a.init(x, rows, x_width, tid);
+      b.init(y, rows, y_width, tid);
+      a.fetch(next);
+      b.fetch(next);
+    }
 #pragma unroll 1
-      for (int r = 0; r < 64; r += 32) {
-        if (more) {
-          a.init(r ? y : x, rows, r ? y_width : x_width, tid);
-          a.fetch(next);
-        }
-        work(buf, r);
-        if (more) a.put(other + (r ? L::kElems : 0), next);
-      }
-    } else {
-      if (more) {
-        a.init(x, rows, x_width, tid);
-        b.init(y, rows, y_width, tid);
-        a.fetch(next);
-        b.fetch(next);
-      }
-      work(buf, 0);
-      if (more) {
-        a.put(other, next);
-        b.put(other + L::kElems, next);
-      }
+    for (int r = 0; r < ROWS; r += 32) work(buf, r);
+    if (more) {
+      a.put(other, next);
+      b.put(other + L::kElems, next);
     }
   }
 };
