@@ -19,22 +19,40 @@ namespace sata {
 
 namespace {
 
-// A stretch of one head's tokens per workgroup, in chunks of kChunk, the state in
-// registers: wave j holds columns 32 j .. +31 of it (and writes those of the output), its lanes one
-// column each.  With r a row of a chunk of m tokens and R the state before it (forward)
+// A workgroup takes W tiles of 32 columns of the state (and the output) of a stretch of one head's
+// tokens, in chunks of 32: wave j has the state's columns 32 j .. +31 in registers, one in
+// each lane pair.  With r a row of a chunk of m tokens and R the state before it (forward)
 //     out_r = readout lam^(r+1) a_r R + sum_{s<=r} update readout lam^(r-s) (a_r.b_s) w_s
 //     R     = lam^m R + sum_s update lam^(m-1-s) b_s (x) w_s
 // and in reverse the same with lam^(m-1-r), lam^(s-r) and lam^(s+1).
 //
-// Precision: bfloat16 inputs are exact operands; the pairs' weights are rounded to
-// bfloat16 as the output is; the state is read out as two bfloat16 numbers and what is
-// added to it carries 24 bits (w times its power as three), so that the state is a float32 one.
-// float32 inputs, weights and states: three bfloat16 numbers each.
+// Bound: memory (a, b, w read and out written once), where there are heads enough; per
+// chunk and wave 8 + 4 + 8 + 24 matrix instructions at d = 128 in bfloat16 and about 320 vector instructions.
+//
+// The state lies in units of f = lam^(tokens since ...): lam^m goes into f, which enters the readout's
+// factor and, inverted, the update's; only when f falls below 2^-8 are all entries
+// multiplied (with an entry's product at every chunk: 128 vector instructions more of 740).
+//
+// Precision: bfloat16 inputs are exact operands.  The pairs' weights inside a chunk are carried as two
+// bfloat16 numbers; the state's entries are rounded to one for the readout (as every term of the
+// output is rounded once, by half a step of the output's type, before the output is), but what is
+// added to the state carries 24 bits (w times its power as three), so that the state is a
+// float32 one.  float32 inputs, weights and states: three bfloat16 numbers each.
 constexpr int kChunk = 32;
 
+// Parts of a head's sequence side by side: states[head][part] holds what each adds (written
+// by the sums) and then what it starts from, as [d_k][d_v]; null: one part.
 struct ScanParts {
-  int parts, part_len;  // stretches per head, tokens in each (a multiple of the chunk)
-  float* states;        // [heads][parts][da][dw]: what each adds (written) or starts from (read); null: one part
+  int parts, part_len;  // (tokens: a multiple of the chunk)
+  float* states;
+};
+struct ScanJob {
+  DecayScan s;
+  ScanParts p;
+};
+struct ScanJobs {
+  ScanJob job[3];
+  int jobs, splits;  // splits: workgroups that share the state's columns
 };
 
 // Entries 16 s + 4 h .. +3 and 16 s + 8 + 4 h .. +3 of rows r0 .. r0 + 31: the order of a result's
@@ -52,51 +70,68 @@ __device__ __forceinline__ void load_rows_as_results(const u16* t, int r0, int s
   }
 }
 
+template <typename T, int ND, int W>
+struct ScanLds {
+  using L = PairTile<T, ND, kChunk>;
+  using LW = PairTile<T, W, kChunk>;
+  static constexpr int kPowers = 2 * L::kElems + LW::kElems;  // (u16 before them)
+  static constexpr int kBytes = 2 * kPowers + 4 * (4 * kChunk + 4);
+};
+
 // REV: from the last token back.  The members of a group (G) vary in a forward, and in b
 // and w in reverse.  SUMS: only what the part adds to the state, from zero.
-template <typename T, int ND, bool REV, bool SUMS>
-__global__ void __launch_bounds__(64 * ND, sizeof(T) == 2 ? 2 : 1) decay_scan_kernel(DecayScan s, ScanParts p) {
-  constexpr int C = kChunk, kThreads = 64 * ND, kTiles = C / 32;
-  using L = PairTile<T, ND, C>;
-  constexpr int PS = sizeof(T) == 2 ? 2 : 3;  // numbers of a state's entry in its readout
-  extern __shared__ __attribute__((aligned(16))) u16 smem16[];
-  u16* const ta = smem16;
-  u16* const tb = smem16 + L::kElems;
-  u16* const tw = smem16 + 2 * L::kElems;
-  // lam^0 .. lam^C, behind C zeros (a power's place is a lane's number plus a constant)
-  float* const power = (float*)(smem16 + 3 * L::kElems) + C;
+template <typename T, int ND, int W, bool REV, bool SUMS>
+__device__ __forceinline__ void scan_part(const DecayScan& s, const ScanParts& p, int head, int part, int tile0,
+                                          u16* smem) {
+  constexpr int C = kChunk, kThreads = 64 * W;
+  using D = ScanLds<T, ND, W>;
+  using L = typename D::L;
+  using LW = typename D::LW;
+  constexpr int PS = sizeof(T) == 2 ? 1 : 3;  // numbers of a state's entry in its readout
+  constexpr int PA = sizeof(T) == 2 ? 2 : 3;  // of a pair's weight
+  u16* const ta = smem;
+  u16* const tb = smem + L::kElems;
+  u16* const tw = tb + L::kElems;
+  // lam^0 .. lam^C, behind C zeros (a power's place is a lane's number plus a constant), and
+  // the same times the scale of the scores
+  float* const power = (float*)(smem + D::kPowers) + C;
+  float* const scaled = power + 2 * C;
   const int tid = threadIdx.x, lane = tid & 63, l31 = lane & 31, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int head = blockIdx.x / p.parts, part = blockIdx.x % p.parts;
   const int len = tokens_of(s.lengths, head / s.H, s.n);
   const int first = part * p.part_len, last = min(first + p.part_len, s.n), end = max(first, min(last, len));
   const int chunks = (end - first + C - 1) / C;
-  const int col = 32 * wave + l31;
-  const float rate = s.log_decay[head % s.H];
+  const int col0 = 32 * tile0, col = col0 + 32 * wave + l31;
+  const double rate = decay_rate(s.log_decay[head % s.H]);
   for (int e = tid; e <= C; e += kThreads) {
-    power[e] = decay_power(rate, e).hi;
+    power[e] = (float)exp(rate * e);
+    if (e < C) scaled[e] = power[e] * (s.update * s.readout);
     if (e > 0) power[-e] = 0.f;
+    if (e > 0 && e < C) scaled[-e] = 0.f;
   }
-  // (only the chunk at the sequence's end has fewer tokens)
-  const FloatPair whole = decay_power(rate, C), tail = decay_power(rate, end - first - (chunks - 1) * C);
 
   f32x16 S[ND];
-  auto state_at = [&](int j, int i, bool transposed) {
+  auto state_at = [&](int j, int i) {
     const int r = 32 * j + result_row(i, h);
-    return transposed ? (int64_t)col * s.da + r : (int64_t)r * s.dw + col;
+    return s.transposed ? (int64_t)col * s.da + r : (int64_t)r * s.dw + col;
   };
   auto has = [&](int j, int i) { return 32 * j + result_row(i, h) < s.da && col < s.dw; };
   const int64_t size = (int64_t)s.da * s.dw;
-  const float* const from = SUMS ? nullptr : p.states ? p.states + ((int64_t)head * p.parts + part) * size
-                                           : s.S_in ? s.S_in + head * size : nullptr;
+  float* const states = p.states ? p.states + ((int64_t)head * p.parts + part) * size : nullptr;
+  const float* const from = SUMS ? nullptr : states ? states : s.S_in ? s.S_in + head * size : nullptr;
 #pragma unroll
   for (int j = 0; j < ND; ++j)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) S[j][i] = from && has(j, i) ? from[state_at(j, i, !p.states && s.transposed)] : 0.f;
+    for (int i = 0; i < 16; ++i) S[j][i] = from && has(j, i) ? from[state_at(j, i)] : 0.f;
+  double f = 1.0, inv = 1.0;  // the state is f S; 1 / f
 
   if (chunks > 0) {
     const int G = SUMS && !REV ? 1 : s.G, units = chunks * G;
-    TileStage<T, ND, C, kThreads> sa, sb, sw;
+    // (only the chunk at the sequence's end has fewer tokens)
+    const int rest = end - first - (chunks - 1) * C;
+    const double lam_c = exp(rate * C), lam_r = exp(rate * rest), inv_c = exp(-rate * C), inv_r = exp(-rate * rest);
+    TileStage<T, ND, C, kThreads> sa, sb;
+    TileStage<T, W, C, kThreads> sw;
     auto row_of = [&](int c) { return first + (REV ? chunks - 1 - c : c) * C; };
     // tiles that unit (c, g) needs anew
     auto new_a = [&](int g) { return !SUMS && (!REV || g == 0); };
@@ -109,14 +144,13 @@ __global__ void __launch_bounds__(64 * ND, sizeof(T) == 2 ? 2 : 1) decay_scan_ke
       if (new_b(g)) {
         const int64_t m = (int64_t)head * (REV ? s.G : 1) + (REV ? g : 0);
         sb.init((const T*)s.b + m * s.n * s.da, len, s.da, tid);
-        sw.init((const T*)s.w + m * s.n * s.dw, len, s.dw, tid);
+        sw.init((const T*)s.w + m * s.n * s.dw, len, min(32 * W, s.dw - col0), tid, s.dw, col0);
         sb.fetch(t0);
         sw.fetch(t0);
       }
     };
-    const float scale = s.update * s.readout;
     fetch(0, row_of(0));
-    f32x16 o[kTiles];
+    f32x16 o;
     for (int u = 0, c = 0, g = 0; u < units; ++u) {
       const int t0 = row_of(c), m = min(C, end - t0);
       const bool opens = g == 0, closes = g + 1 == G;
@@ -139,116 +173,110 @@ __global__ void __launch_bounds__(64 * ND, sizeof(T) == 2 ? 2 : 1) decay_scan_ke
       uint32_t bad = 0;
 #pragma unroll
       for (int x = 0; x < C / 16; ++x) {
-        L::load_transposed(tw, 16 * x, wave, wf[x]);
-        const uint4 b = not_finite_entries(wf[x][0]);
-        bad |= b.x | b.y | b.z | b.w;
+        LW::load_transposed(tw, 16 * x, wave, wf[x]);
+        bad |= not_finite_bits(wf[x][0]);
       }
       if constexpr (!SUMS) {
         if (!REV || opens) {
-#pragma unroll
-          for (int q = 0; q < kTiles; ++q) o[q] = zero16();
+          o = zero16();
 #pragma unroll
           for (int x = 0; x < 2 * ND; ++x) {
             float v[8];
-            uint4 st[1][PS];
+            uint4 st[1][PS], e[L::kPl];
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = S[x / 2][8 * (x & 1) + i];
             to_planes<PS>(v, st);
-#pragma unroll
-            for (int q = 0; q < kTiles; ++q) {
-              uint4 f[L::kPl];
-              load_rows_as_results<L>(ta, 32 * q, x, f);
-              o[q] = dot_planes32(st[0], f, o[q]);
-            }
+            load_rows_as_results<L>(ta, 0, x, e);
+            o = dot_planes32(st[0], e, o);
           }
+          const float k = s.readout * (float)f * (REV ? late(l31) : early(l31));
 #pragma unroll
-          for (int q = 0; q < kTiles; ++q) {
-            const int r = 32 * q + l31;
-            const float k = s.readout * (REV ? late(r) : early(r));
+          for (int i = 0; i < 16; ++i) o[i] *= k;
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        f32x16 acc = zero16();
 #pragma unroll
-            for (int i = 0; i < 16; ++i) o[q][i] *= k;
+        for (int x = 0; x < 2 * ND; ++x) {
+          uint4 e[L::kPl], own[L::kPl];
+          L::load_rows(ta, 0, x, own);
+          L::load_rows(tb, 0, x, e);
+          acc = dot_planes32(e, own, acc);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        float z[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int far = l31 - result_row(i, h), e = REV ? -far : far;
+          float x = scaled[e];
+          asm volatile("" : "+v"(x));  // (read by all lanes, not in 16 branches)
+          z[i] = e >= 0 ? acc[i] * x : 0.f;  // (a select: not finite times 0 is no zero)
+        }
+        uint4 w[2][PA];
+        to_planes<PA>(z, w);
+        uint4 wc[2][L::kPl];
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int i = 0; i < L::kPl; ++i) wc[x][i] = wf[x][i];
+        const bool odd = __ballot(bad != 0) != 0;
+        if (__builtin_expect(odd, 0)) {
+          // Values of w that are not finite are left out: weights of pairs that are masked are zero, and
+          // the product would not be.
+          stay_in_branch();
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            const uint4 b = not_finite_entries(wf[x][0]);
+#pragma unroll
+            for (int i = 0; i < L::kPl; ++i) wc[x][i].x &= ~b.x, wc[x][i].y &= ~b.y, wc[x][i].z &= ~b.z, wc[x][i].w &= ~b.w;
           }
         }
 #pragma unroll
-        for (int q = 0; q < kTiles; ++q)
+        for (int x = 0; x < 2; ++x) o = dot_planes32(wc[x], w[x], o);
+        if (__builtin_expect(odd, 0)) {
+          // They get their due here: a product of marks with the pairs that are not masked tells which
+          // outputs have one, and those are NaN.
+          settle_mfma32();
+          f32x16 count = zero16();
 #pragma unroll
-          for (int k = REV ? q : 0; k < (REV ? kTiles : q + 1); ++k) {
-            __builtin_amdgcn_sched_barrier(0);
-            f32x16 acc = zero16();
+          for (int x = 0; x < 2; ++x) {
+            float y[8];
 #pragma unroll
-            for (int x = 0; x < 2 * ND; ++x) {
-              uint4 f[L::kPl], own[L::kPl];
-              L::load_rows(ta, 32 * q, x, own);
-              L::load_rows(tb, 32 * k, x, f);
-              acc = dot_planes32(f, own, acc);
+            for (int i = 0; i < 8; ++i) {
+              const int row = result_row(8 * x + i, h);
+              y[i] = (REV ? row >= l31 : row <= l31) ? 1.f : 0.f;
             }
-            __builtin_amdgcn_sched_barrier(0);
-            float z[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const int far = 32 * (q - k) + l31 - result_row(i, h), e = REV ? -far : far;
-              z[i] = acc[i] * (scale * power[e]);
-              if (q == k) z[i] = e >= 0 ? z[i] : 0.f;  // (not finite times 0 is no zero)
-            }
-            uint4 w[2][L::kPl];
-            to_planes<L::kPl>(z, w);
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-              uint4 f[L::kPl];
-#pragma unroll
-              for (int i = 0; i < L::kPl; ++i) f[i] = wf[2 * k + x][i];
-              if (k == q) {  // (not finite times a masked 0 is no zero)
-                const uint4 b = not_finite_entries(f[0]);
-#pragma unroll
-                for (int i = 0; i < L::kPl; ++i) f[i].x &= ~b.x, f[i].y &= ~b.y, f[i].z &= ~b.z, f[i].w &= ~b.w;
-              }
-              o[q] = dot_planes32(f, w[x], o[q]);
-            }
+            const uint4 b = not_finite_entries(wf[x][0]);
+            count = mfma32(uint4{b.x & 0x3f803f80u, b.y & 0x3f803f80u, b.z & 0x3f803f80u, b.w & 0x3f803f80u}, to_bf16(y),
+                           count);
           }
-        if (__builtin_expect(__ballot(bad != 0) != 0, 0)) {
-          // values that are not finite, left out of the own tiles: as in contract32_own
           settle_mfma32();
 #pragma unroll
-          for (int q = 0; q < kTiles; ++q) {
-            f32x16 count = zero16();
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-              float y[8];
-#pragma unroll
-              for (int i = 0; i < 8; ++i) {
-                const int row = result_row(8 * x + i, h);
-                y[i] = (REV ? row >= l31 : row <= l31) ? 1.f : 0.f;
-              }
-              const uint4 b = not_finite_entries(wf[2 * q + x][0]);
-              count = mfma32(uint4{b.x & 0x3f803f80u, b.y & 0x3f803f80u, b.z & 0x3f803f80u, b.w & 0x3f803f80u}, to_bf16(y),
-                             count);
-            }
-            settle_mfma32();
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[q][i] = count[i] > 0.f ? __uint_as_float(0x7fc00000u) : o[q][i];
-          }
+          for (int i = 0; i < 16; ++i) o[i] = count[i] > 0.f ? __uint_as_float(0x7fc00000u) : o[i];
         }
         if (!REV || closes) {
           settle_mfma32();
-#pragma unroll
-          for (int q = 0; q < kTiles; ++q) {
-            const int r = 32 * q + l31;
-            if (r >= m) continue;
-            T* const out = (T*)s.out + (((int64_t)head * (REV ? 1 : s.G) + (REV ? 0 : member)) * s.n + t0 + r) * s.dw;
-            const f32x16 one[1] = {o[q]};
-            store_row32<T, 1>(out + 32 * wave, s.dw - 32 * wave, one, 1.f, false);
+          if (l31 < m) {
+            T* const out = (T*)s.out + (((int64_t)head * (REV ? 1 : s.G) + (REV ? 0 : member)) * s.n + t0 + l31) * s.dw;
+            const f32x16 one[1] = {o};
+            store_row32<T, 1>(out + col0 + 32 * wave, s.dw - col0 - 32 * wave, one, 1.f, false);
           }
         }
       }
       __builtin_amdgcn_sched_barrier(0);
       if (REV ? opens : closes) {
-        const float hi = m == C ? whole.hi : tail.hi, lo = m == C ? whole.lo : tail.lo;
+        f *= m == C ? lam_c : lam_r;
+        inv *= m == C ? inv_c : inv_r;
+        if (f < 0x1p-8) {
+          const float k = (float)f;
 #pragma unroll
-        for (int j = 0; j < ND; ++j)
+          for (int j = 0; j < ND; ++j)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) S[j][i] = times(S[j][i], FloatPair{hi, lo});
+            for (int i = 0; i < 16; ++i) S[j][i] *= k;
+          f = inv = 1.0;
+        }
       }
       if (REV || closes) {
+        const float up = s.update * (float)inv;
 #pragma unroll
         for (int x = 0; x < C / 16; ++x) {
           __builtin_amdgcn_sched_barrier(0);
@@ -264,112 +292,167 @@ __global__ void __launch_bounds__(64 * ND, sizeof(T) == 2 ? 2 : 1) decay_scan_ke
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             const int r = 16 * x + result_row(i, h);
-            v[i] *= s.update * (REV ? early(r) : late(r));
+            v[i] *= up * (REV ? early(r) : late(r));
           }
           uint4 w3[1][3];
           to_planes<3>(v, w3);
 #pragma unroll
           for (int j = 0; j < ND; ++j) {
-            uint4 f[L::kPl];
-            L::load_transposed(tb, 16 * x, j, f);
-            S[j] = dot_planes32(f, w3[0], S[j]);
+            uint4 e[L::kPl];
+            L::load_transposed(tb, 16 * x, j, e);
+            S[j] = dot_planes32(e, w3[0], S[j]);
           }
         }
         settle_mfma32();
       }
     }
   }
-  float* const to = SUMS ? p.states + ((int64_t)head * p.parts + part) * size
-                         : !p.states && s.S_out ? s.S_out + head * size : nullptr;
+  float* const to = SUMS ? states : !states && s.S_out ? s.S_out + head * size : nullptr;
   if (to) {
+    const float k = (float)f;
 #pragma unroll
     for (int j = 0; j < ND; ++j)
 #pragma unroll
       for (int i = 0; i < 16; ++i)
-        if (has(j, i)) to[state_at(j, i, !p.states && s.transposed)] = S[j][i];
+        if (has(j, i)) to[state_at(j, i)] = S[j][i] * k;
   }
-  if (!SUMS && s.out) {
-    const int pad = last - end;  // rows behind the sequence
+  if (!SUMS) {
+    const int cols = min(32 * W, s.dw - col0);  // rows behind the sequence
     for (int g = 0; g < (REV ? 1 : s.G); ++g) {
-      T* const out = (T*)s.out + (((int64_t)head * (REV ? 1 : s.G) + g) * s.n + end) * s.dw;
-      for (int64_t i = tid; i < (int64_t)pad * s.dw; i += kThreads) out[i] = (T)0;
+      T* const out = (T*)s.out + (((int64_t)head * (REV ? 1 : s.G) + g) * s.n + end) * s.dw + col0;
+      for (int i = tid; i < (last - end) * cols; i += kThreads) out[(int64_t)(i / cols) * s.dw + i % cols] = (T)0;
     }
   }
 }
 
-// What each part adds becomes what it starts from; one thread per entry of a state.
-__global__ void __launch_bounds__(256) decay_carry_kernel(DecayScan s, ScanParts p) {
-  const int head = blockIdx.y;
-  const int64_t size = (int64_t)s.da * s.dw;
-  const int i = blockIdx.x * 256 + threadIdx.x;
-  const int len = tokens_of(s.lengths, head / s.H, s.n);
-  const float g = s.log_decay[head % s.H];
-  const FloatPair whole = decay_power(g, p.part_len);
-  if (i >= size) return;
-  const int row = i / s.dw, at = s.transposed ? (i - row * s.dw) * s.da + row : i;
-  float* const states = p.states + (int64_t)head * p.parts * size + i;
-  float R = s.S_in ? s.S_in[head * size + at] : 0.f;
-  for (int c = 0; c < p.parts; ++c) {
-    const int part = s.reverse ? p.parts - 1 - c : c;
-    const int tokens = min(max(len - part * p.part_len, 0), p.part_len);
-    const float add = states[part * size];
-    states[part * size] = R;
-    R = times(R, tokens == p.part_len ? whole : decay_power(g, tokens)) + add;
+template <typename T, int ND, int W, bool SUMS>
+__global__ void __launch_bounds__(64 * W, sizeof(T) == 2 ? 2 : 1) decay_scan_kernel(ScanJobs a) {
+  extern __shared__ __attribute__((aligned(16))) u16 smem16[];
+  const DecayScan& s0 = a.job[0].s;
+  // An XCD takes whole heads: what the jobs, parts and columns of a head read is read through one L2.
+  const int each = a.jobs * a.job[0].p.parts * a.splits;
+  int head, unit;
+  if (s0.heads >= 8) {
+    const int j = blockIdx.x >> 3;
+    head = j / each * 8 + (int)(blockIdx.x & 7);
+    unit = j % each;
+    if (head >= s0.heads) return;
+  } else {
+    head = blockIdx.x / each;
+    unit = blockIdx.x % each;
   }
-  if (s.S_out) s.S_out[head * size + at] = R;
+  const int split = unit % a.splits, job = unit / a.splits % a.jobs, part = unit / a.splits / a.jobs;
+  const DecayScan& s = a.job[job].s;
+  const ScanParts& p = a.job[job].p;
+  if (32 * W * split >= s.dw) return;  // (d_k and d_v may differ)
+  if (s.reverse) scan_part<T, ND, W, true, SUMS>(s, p, head, part, W * split, smem16);
+  else scan_part<T, ND, W, false, SUMS>(s, p, head, part, W * split, smem16);
 }
 
-template <typename T, int ND, bool REV>
-hipError_t launch_scan(const DecayScan& s, float* states, hipStream_t st) {
-  constexpr int bytes = 3 * PairTile<T, ND, kChunk>::kBytes + 4 * (2 * kChunk + 4);
+// What each part adds becomes what it starts from; one thread per entry of a state.
+__global__ void __launch_bounds__(256) decay_carry_kernel(ScanJobs a) {
+  const DecayScan& s = a.job[blockIdx.z].s;
+  const ScanParts& p = a.job[blockIdx.z].p;
+  const int head = blockIdx.y, i = blockIdx.x * 256 + threadIdx.x;
+  const int64_t size = (int64_t)s.da * s.dw;
+  const int len = tokens_of(s.lengths, head / s.H, s.n);
+  const double rate = decay_rate(s.log_decay[head % s.H]);
+  const FloatPair whole = float_pair(exp(rate * p.part_len)), rest = float_pair(exp(rate * (len % p.part_len)));
+  if (i >= size) return;
+  float* const states = p.states + (int64_t)head * p.parts * size + i;
+  float R = s.S_in ? s.S_in[head * size + i] : 0.f;
+  constexpr int kAhead = 8;  // parts read at once
+  for (int c0 = 0; c0 < p.parts; c0 += kAhead) {
+    float add[kAhead];
+#pragma unroll
+    for (int x = 0; x < kAhead; ++x) {
+      const int part = s.reverse ? p.parts - 1 - c0 - x : c0 + x;
+      add[x] = c0 + x < p.parts ? states[part * size] : 0.f;
+    }
+#pragma unroll
+    for (int x = 0; x < kAhead; ++x) {
+      if (c0 + x >= p.parts) break;
+      const int part = s.reverse ? p.parts - 1 - c0 - x : c0 + x;
+      states[part * size] = R;
+      const int tokens = len - part * p.part_len;
+      if (tokens >= p.part_len) R = times(R, whole) + add[x];
+      else if (tokens > 0) R = times(R, rest) + add[x];
+    }
+  }
+  if (s.S_out) s.S_out[head * size + i] = R;
+}
+
+template <typename T, int ND, int W, bool SUMS>
+hipError_t launch_jobs(ScanJobs a, hipStream_t st) {
+  constexpr int bytes = ScanLds<T, ND, W>::kBytes;
   static_assert(bytes <= 160 * 1024, "LDS of one workgroup");
-  auto scan = decay_scan_kernel<T, ND, REV, false>;
-  auto sums = decay_scan_kernel<T, ND, REV, true>;
+  auto kern = decay_scan_kernel<T, ND, W, SUMS>;
   if (bytes > 64 * 1024) {
-    hipError_t e = hipFuncSetAttribute((const void*)scan, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (e == hipSuccess) e = hipFuncSetAttribute((const void*)sums, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != hipSuccess) return e;
   }
-  ScanParts p{1, s.n, nullptr};
-  const DecayScanPlan plan = plan_decay_scan(s.heads, s.n, s.da, s.dw);
-  if (plan.parts > 1) {
-    p = ScanParts{plan.parts, plan.part_len, states};
-    hipLaunchKernelGGL(sums, dim3(s.heads * p.parts), dim3(64 * ND), bytes, st, s, p);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(decay_carry_kernel, dim3((s.da * s.dw + 255) / 256, s.heads), dim3(256), 0, st, s, p);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-  }
-  hipLaunchKernelGGL(scan, dim3(s.heads * p.parts), dim3(64 * ND), bytes, st, s, p);
+  a.splits = (ND + W - 1) / W;
+  const int heads = a.job[0].s.heads;
+  const int64_t grid = (int64_t)(heads >= 8 ? (heads + 7) / 8 * 8 : heads) * a.jobs * a.job[0].p.parts * a.splits;
+  hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(64 * W), bytes, st, a);
   return hipGetLastError();
 }
 
+template <typename T, int ND>
+hipError_t launch_scan(const DecayScan* scans, int count, const DecayScan* sums, int sum_count, float* states,
+                       const DecayScanPlan& plan, hipStream_t st) {
+  const int64_t size = (int64_t)scans[0].da * scans[0].dw;
+  ScanJobs a{};
+  if (plan.parts > 1) {
+    a.jobs = sum_count;
+    for (int i = 0; i < sum_count; ++i)
+      a.job[i] = ScanJob{sums[i], {plan.parts, plan.part_len, states + i * scans[0].heads * plan.parts * size}};
+    hipError_t e = launch_jobs<T, ND, ND, true>(a, st);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(decay_carry_kernel, dim3((unsigned)((size + 255) / 256), scans[0].heads, sum_count), dim3(256), 0, st, a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  a.jobs = count;
+  for (int i = 0; i < count; ++i)
+    a.job[i] = ScanJob{scans[i], {plan.parts, plan.part_len,
+                                  plan.parts > 1 ? states + (scans[i].reverse ? sum_count - 1 : 0) * scans[0].heads * plan.parts * size
+                                                 : nullptr}};
+  if constexpr (ND % 2 == 0)
+    if (plan.split) return launch_jobs<T, ND, ND / 2, false>(a, st);
+  return launch_jobs<T, ND, ND, false>(a, st);
+}
+
 template <int ND>
-hipError_t launch_scan_n(const DecayScan& s, bool bf16, float* states, hipStream_t st) {
-  if (s.reverse) return bf16 ? launch_scan<u16, ND, true>(s, states, st) : launch_scan<float, ND, true>(s, states, st);
-  return bf16 ? launch_scan<u16, ND, false>(s, states, st) : launch_scan<float, ND, false>(s, states, st);
+hipError_t launch_scan_t(const DecayScan* scans, int count, const DecayScan* sums, int sum_count, bool bf16, float* states,
+                         const DecayScanPlan& plan, hipStream_t st) {
+  return bf16 ? launch_scan<u16, ND>(scans, count, sums, sum_count, states, plan, st)
+              : launch_scan<float, ND>(scans, count, sums, sum_count, states, plan, st);
 }
 
 }  // namespace
 
-DecayScanPlan plan_decay_scan(int heads, int n, int da, int dw) {
-  const int tiles = (std::max(da, dw) + 31) / 32;
+DecayScanPlan plan_decay_scan(int heads, int n, int da, int dw, int jobs) {
   DecayScanPlan p;
-  const int64_t want = std::max<int64_t>(1, 2048 / tiles / heads);  // (8 waves on each of 256 compute units)
-  const int chunks = (n + kChunk - 1) / kChunk;
-  const int each = (int)std::max<int64_t>(1, (chunks + want - 1) / want);
+  const int tiles = (std::max(da, dw) + 31) / 32, chunks = (n + kChunk - 1) / kChunk;
+  const int64_t waves = (int64_t)heads * tiles * jobs;
+  const int64_t want = std::max<int64_t>(1, 2048 / waves);
+  const int each = (int)std::max<int64_t>(std::max(1, std::min(chunks, 4)), (chunks + want - 1) / want);
   p.parts = std::max(1, (chunks + each - 1) / each);
   p.part_len = each * kChunk;
+  p.split = p.parts == 1 && waves <= 1024;
   p.state_bytes = p.parts > 1 ? sizeof(float) * (size_t)heads * p.parts * da * dw : 0;
   return p;
 }
 
-hipError_t launch_decay_scan(const DecayScan& s, bool bf16, float* states, hipStream_t st) {
+hipError_t launch_decay_scan(const DecayScan* scans, int count, const DecayScan* sums, int sum_count, bool bf16,
+                             float* states, hipStream_t st) {
+  const DecayScan& s = scans[0];
+  const DecayScanPlan plan = plan_decay_scan(s.heads, s.n, s.da, s.dw, count);
   switch ((std::max(s.da, s.dw) + 31) / 32) {
-    case 1: return launch_scan_n<1>(s, bf16, states, st);
-    case 2: return launch_scan_n<2>(s, bf16, states, st);
-    case 3: return launch_scan_n<3>(s, bf16, states, st);
-    default: return launch_scan_n<4>(s, bf16, states, st);
+    case 1: return launch_scan_t<1>(scans, count, sums, sum_count, bf16, states, plan, st);
+    case 2: return launch_scan_t<2>(scans, count, sums, sum_count, bf16, states, plan, st);
+    case 3: return launch_scan_t<3>(scans, count, sums, sum_count, bf16, states, plan, st);
+    default: return launch_scan_t<4>(scans, count, sums, sum_count, bf16, states, plan, st);
   }
 }
 

@@ -48,7 +48,7 @@ __global__ void __launch_bounds__(kStepThreads) decay_step_kernel(float* __restr
   }
 #pragma unroll
   for (int x = 0; x < V; ++x) w[x] = on ? to_f32(v_[head * dv + c0 + x]) : 0.f;
-  const FloatPair lam = decay_power(log_decay[head % H], 1);
+  const FloatPair lam = float_pair(exp(decay_rate(log_decay[head % H])));
 #pragma unroll
   for (int i = 0; i < R; ++i) {
     const int row = rg + i * groups;

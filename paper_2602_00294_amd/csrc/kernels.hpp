@@ -219,14 +219,19 @@ struct DecayScan {
   bool reverse = false, transposed = false;
   float update = 1.f, readout = 1.f;
 };
-// Parts of a head's sequence that run side by side (what they add to the state is
-// summed first); the scan's launch takes state_bytes of scratch.
+// Parts of a head's sequence that run side by side, where one part for a head would leave
+// compute units without work (what each part adds to the state is summed first), and
+// whether two workgroups share the state's columns.
 struct DecayScanPlan {
   int parts = 1, part_len = 0;
-  size_t state_bytes = 0;
+  bool split = false;
+  size_t state_bytes = 0;  // scratch for the states of one sum
 };
-DecayScanPlan plan_decay_scan(int heads, int n, int da, int dw);
-hipError_t launch_decay_scan(const DecayScan& s, bool bf16, float* states, hipStream_t st);
+DecayScanPlan plan_decay_scan(int heads, int n, int da, int dw, int jobs);
+// Up to three scans over the same heads in one launch; `sums`: the scans (of layout [d_k][d_v]) whose
+// states the parts start from, the forward one first, the reverse one last.
+hipError_t launch_decay_scan(const DecayScan* scans, int count, const DecayScan* sums, int sum_count, bool bf16,
+                             float* states, hipStream_t st);
 hipError_t launch_decay_step(float* S, const void* q, const void* k, const void* v, const float* log_decay, void* y,
                              bool bf16, int heads, int H, int G, int dk, int dv, float scale, hipStream_t st);
 

@@ -179,6 +179,12 @@ __device__ __forceinline__ void add_row(const T* row, int width, float weight, f
     }
 }
 
+// Whether there are any (bits set).
+__device__ __forceinline__ uint32_t not_finite_bits(const uint4& w) {
+  return ((((w.x & 0x7f807f80u) + 0x00800080u) | ((w.y & 0x7f807f80u) + 0x00800080u)) |
+          (((w.z & 0x7f807f80u) + 0x00800080u) | ((w.w & 0x7f807f80u) + 0x00800080u))) & 0x80008000u;
+}
+
 // (a float32 value beyond bfloat16's range is an infinity in its first plane)
 __device__ __forceinline__ bool bf16_finite(float x) { return (pack2(x, 0.f) & 0x7f80u) != 0x7f80u; }
 
@@ -191,8 +197,7 @@ __device__ __forceinline__ bool tile_not_finite(const u16* t, int r0) {
   for (int s = 0; s < 2 * ND; ++s) {
     uint4 a[L::kPl];
     L::load_rows(t, r0, s, a);
-    const uint4 m = not_finite_entries(a[0]);
-    bad |= m.x | m.y | m.z | m.w;
+    bad |= not_finite_bits(a[0]);
   }
   return __ballot(bad != 0) != 0;
 }
@@ -210,23 +215,25 @@ struct TileStage {
   static constexpr int kIt = (ROWS + kPer - 1) / kPer;
   static_assert(THREADS % kU == 0, "whole rows in a pass");
   const T* base;
-  int rows, width, tid;
+  int rows, width, pitch, tid;
   bool vec;
   uint32_t off;
   VectorReader read;
   uint4 r[kIt];
 
-  __device__ __forceinline__ void init(const T* p, int rows_, int width_, int tid_) {
-    base = p, rows = rows_, width = width_, tid = tid_;
-    vec = width % kEV == 0 && ((uintptr_t)p & 15) == 0;
-    read = VectorReader(p, vec ? (int64_t)rows * width * (int)sizeof(T) : 0);
+  // `width` columns from column `col0` on of rows of `pitch` entries at p
+  __device__ __forceinline__ void init(const T* p, int rows_, int width_, int tid_, int pitch_, int col0) {
+    base = p + col0, rows = rows_, width = width_, pitch = pitch_, tid = tid_;
+    vec = pitch % kEV == 0 && ((uintptr_t)p & 15) == 0;
+    read = VectorReader(base, vec ? ((int64_t)rows * pitch - col0) * (int)sizeof(T) : 0);
     const int row = tid / kU, col = tid % kU * kEV;
-    off = col < width && row < ROWS ? (uint32_t)(row * width + col) * (uint32_t)sizeof(T) : kNoVector;
+    off = col < width && row < ROWS ? (uint32_t)(row * pitch + col) * (uint32_t)sizeof(T) : kNoVector;
   }
+  __device__ __forceinline__ void init(const T* p, int rows_, int width_, int tid_) { init(p, rows_, width_, tid_, width_, 0); }
   // the rows from r0 on
   __device__ __forceinline__ void fetch(int r0) {
 #pragma unroll
-    for (int i = 0; i < kIt; ++i) r[i] = read(off + (uint32_t)(r0 + i * kPer) * (uint32_t)(width * (int)sizeof(T)));
+    for (int i = 0; i < kIt; ++i) r[i] = read(off + (uint32_t)(r0 + i * kPer) * (uint32_t)(pitch * (int)sizeof(T)));
   }
   __device__ static void put_entry(u16* dst, T x) {
     if constexpr (sizeof(T) == 4) {
@@ -264,7 +271,7 @@ struct TileStage {
 #pragma unroll 1
       for (int i = tid; i < ROWS * 32 * ND; i += THREADS) {
         const int row = i / (32 * ND), col = i % (32 * ND);
-        put_entry(t + L::at(row, col), r0 + row < rows && col < width ? base[(int64_t)(r0 + row) * width + col] : (T)0);
+        put_entry(t + L::at(row, col), r0 + row < rows && col < width ? base[(int64_t)(r0 + row) * pitch + col] : (T)0);
       }
     }
   }

@@ -960,7 +960,8 @@ sata_status sata_decode_step_grouped(float* S, const void* q, const void* k, con
 
 int64_t sata_decay_scratch(int B, int H_kv, int n, int d_k, int d_v) {
   if (check_pair_args(SATA_F32, B, H_kv, 1, n, d_k, d_v) != SATA_OK) return -1;
-  return (int64_t)sata::plan_decay_scan(B * H_kv, n, d_k, d_v).state_bytes;
+  return (int64_t)std::max(sata::plan_decay_scan(B * H_kv, n, d_k, d_v, 1).state_bytes,
+                           2 * sata::plan_decay_scan(B * H_kv, n, d_k, d_v, 3).state_bytes);
 }
 
 int64_t sata_softmax_backward_scratch(int B, int H_kv, int G, int n) {
@@ -981,13 +982,13 @@ sata_status sata_decay_prefill(const void* q, const void* k, const void* v, cons
   if (!log_decay || (n > 0 && (!q || !k || !v || !y))) return fail(SATA_ERR_INVALID_ARG, "null tensor pointer");
   if (S_in && S_in == S_out) return fail(SATA_ERR_INVALID_ARG, "S_out must not be S_in");
   if (n == 0 && !S_out) return ok();
-  if ((st = check_scratch(scratch, sata::plan_decay_scan(B * H_kv, n, d_k, d_v).state_bytes)) != SATA_OK) return st;
+  if ((st = check_scratch(scratch, sata::plan_decay_scan(B * H_kv, n, d_k, d_v, 1).state_bytes)) != SATA_OK) return st;
   sata::DecayScan s;
   s.a = q, s.b = k, s.w = v, s.out = y;
   s.S_in = S_in, s.S_out = S_out, s.log_decay = log_decay, s.lengths = lengths;
   s.heads = B * H_kv, s.H = H_kv, s.n = n, s.da = d_k, s.dw = d_v, s.G = G;
   s.readout = pair_scale(d_k);
-  hipError_t e = sata::launch_decay_scan(s, dt == SATA_BF16, (float*)scratch, (hipStream_t)stream);
+  hipError_t e = sata::launch_decay_scan(&s, 1, &s, 1, dt == SATA_BF16, (float*)scratch, (hipStream_t)stream);
   if (e != hipSuccess) return hip_fail(e, "decay prefill launch");
   return ok();
 }
@@ -1013,34 +1014,27 @@ sata_status sata_decay_backward(const void* q, const void* k, const void* v, con
     return fail(SATA_ERR_INVALID_ARG, "null tensor pointer");
   if (dS && dS == dS_in) return fail(SATA_ERR_INVALID_ARG, "dS_in must not be dS");
   if (n == 0 && !dS_in) return ok();
-  if ((st = check_scratch(scratch, sata::plan_decay_scan(B * H_kv, n, d_k, d_v).state_bytes)) != SATA_OK) return st;
-  const hipStream_t hs = (hipStream_t)stream;
-  const bool bf16 = dt == SATA_BF16;
+  if ((st = check_scratch(scratch, 2 * sata::plan_decay_scan(B * H_kv, n, d_k, d_v, 3).state_bytes)) != SATA_OK) return st;
   const float c = pair_scale(d_k);
-  float* const states = (float*)scratch;
   sata::DecayScan s;
   s.log_decay = log_decay, s.lengths = lengths;
-  s.heads = B * H_kv, s.H = H_kv, s.n = n;
-  hipError_t e = hipSuccess;
-  if (n > 0) {
-    sata::DecayScan r = s;
-    r.a = dy, r.b = v, r.w = k, r.out = dq;
-    r.da = d_v, r.dw = d_k, r.G = G;
-    r.S_in = S_in, r.transposed = true;
-    r.readout = c;
-    if ((e = sata::launch_decay_scan(r, bf16, states, hs)) != hipSuccess) return hip_fail(e, "decay backward (dq) launch");
-    r = s;
-    r.a = v, r.b = dy, r.w = q, r.out = dk;
-    r.da = d_v, r.dw = d_k, r.G = G;
-    r.reverse = true, r.transposed = true;
-    r.S_in = dS, r.update = c;
-    if ((e = sata::launch_decay_scan(r, bf16, states, hs)) != hipSuccess) return hip_fail(e, "decay backward (dk) launch");
-  }
-  s.a = k, s.b = q, s.w = dy, s.out = dv;
-  s.da = d_k, s.dw = d_v, s.G = G;
-  s.reverse = true;
-  s.S_in = dS, s.S_out = dS_in, s.update = c;
-  if ((e = sata::launch_decay_scan(s, bf16, states, hs)) != hipSuccess) return hip_fail(e, "decay backward (dv) launch");
+  s.heads = B * H_kv, s.H = H_kv, s.n = n, s.G = G;
+  sata::DecayScan scans[3] = {s, s, s}, sums[2] = {s, s};
+  sata::DecayScan &gq = scans[0], &gk = scans[1], &gv = scans[2];
+  gq.a = dy, gq.b = v, gq.w = k, gq.out = dq;
+  gq.da = d_v, gq.dw = d_k;
+  gq.S_in = S_in, gq.transposed = true, gq.readout = c;
+  gk.a = v, gk.b = dy, gk.w = q, gk.out = dk;
+  gk.da = d_v, gk.dw = d_k;
+  gk.S_in = dS, gk.transposed = true, gk.reverse = true, gk.update = c;
+  gv.a = k, gv.b = q, gv.w = dy, gv.out = dv;
+  gv.da = d_k, gv.dw = d_v;
+  gv.S_in = dS, gv.S_out = dS_in, gv.reverse = true, gv.update = c;
+  sums[0].b = k, sums[0].w = v, sums[0].S_in = S_in;
+  sums[0].da = d_k, sums[0].dw = d_v;
+  sums[1] = gv;
+  hipError_t e = sata::launch_decay_scan(scans, 3, sums, 2, dt == SATA_BF16, (float*)scratch, (hipStream_t)stream);
+  if (e != hipSuccess) return hip_fail(e, "decay backward launch");
   return ok();
 }
 

@@ -9,9 +9,11 @@ half step of the output's type (2^-8 bfloat16, 2^-24 float32):
                                     r = 2^-8 for bfloat16 inputs, 2^-22 for float32 ones
                                     (three bfloat16 numbers carry 24 bits; their product
                                     leaves out partial products below 2^-24, three of them);
-  N 2^-23 sum |terms|               float32 sums of N terms and the factors of a term;
-  2^-15 sum |terms| (bfloat16)      states as pairs of bfloat16 numbers (2^-17 twice) with
-                                    the pairs' products.
+  r sum |a| |R|                     one rounding of the entries of a state R to the operands' type
+                                    where it is read out, at the start of a chunk of 32 tokens
+                                    (from the other end in the gradients of k and v);
+  N 2^-23 sum |terms|               float32 sums of N terms and the factors of a term.
+A weight inside a chunk is carried as two bfloat16 numbers (2^-17), for which r is more than enough.
 """
 import math
 
@@ -19,7 +21,7 @@ import torch
 
 HALF = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8}
 WEIGHT = {torch.float32: 2.0 ** -22, torch.bfloat16: 2.0 ** -8}
-STATE = {torch.float32: 2.0 ** -22, torch.bfloat16: 2.0 ** -15}
+CHUNK = 32
 
 
 def _ends(lengths, B, n):
@@ -37,9 +39,26 @@ def _pairs(g, n):
     return _power(g, t[:, None] - t[None, :])
 
 
+def _readout(a, b, w, g, R, c, reverse=False):
+    """sum |a| |R| of each row: R the state before (reverse: behind) the row's chunk, by whole chunks.
+    a, b [e, i], w [e, j], in reverse R already times exp(g) (as the state behind the last token is given)."""
+    e = a.shape[0]
+    out = torch.zeros(e, w.shape[1], dtype=torch.float64)
+    starts = list(range(0, e, CHUNK))
+    for p in reversed(starts) if reverse else starts:
+        q = min(e, p + CHUNK)
+        t = torch.arange(q - p, dtype=torch.float64)
+        far = (q - p - 1 - t) if reverse else t + 1
+        out[p:q] = (a[p:q].abs() * _power(g, far)[:, None]) @ R.abs() * c
+        late = t + 1 if reverse else q - p - 1 - t
+        R = _power(g, torch.tensor(float(q - p), dtype=torch.float64)) * R + (b[p:q] * _power(g, late)[:, None]).T @ w[p:q]
+    return out
+
+
 def _bounded(value, dtype, weights, terms, count):
-    """weights: sum |w| |x| of the rounded weights; terms: sum of all factors' sizes."""
-    f = HALF[dtype] * value.abs() + 1.01 * WEIGHT[dtype] * weights + (count * 2.0 ** -23 + STATE[dtype]) * terms
+    """weights: sum |w| |x| of the rounded weights and sum |a| |R| of the rounded states; terms: sum of all
+    factors' sizes."""
+    f = HALF[dtype] * value.abs() + 1.01 * WEIGHT[dtype] * weights + count * 2.0 ** -23 * terms
     return value, f + 1e-30
 
 
@@ -65,7 +84,7 @@ def decay_prefill(q, k, v, log_decay, lengths=None, S_in=None):
                 Q = q[b, i, :e]
                 w = Q @ K.T * D * c
                 out[0][b, i, :e] = w @ V + (Q * first) @ S0 * c
-                out[1][b, i, :e] = w.abs() @ V.abs()
+                out[1][b, i, :e] = w.abs() @ V.abs() + _readout(Q, K, V, g, S0, c)
                 out[2][b, i, :e] = (Q.abs() @ K.abs().T * D * c) @ V.abs() + (Q.abs() * first) @ S0.abs() * c
             late = _power(g, e - 1 - t)[:, None]
             last = _power(g, torch.tensor(float(e), dtype=torch.float64))
@@ -107,13 +126,13 @@ def decay_backward(q, k, v, log_decay, dy, lengths=None, S_in=None, dS=None):
                 a, w = Y @ V.T * D * c, Q @ K.T * D * c
                 aa, ww = Y.abs() @ V.abs().T * D * c, Q.abs() @ K.abs().T * D * c
                 gq[0][b, i, :e] = a @ K + (Y * first) @ S0.T * c
-                gq[1][b, i, :e] = a.abs() @ K.abs()
+                gq[1][b, i, :e] = a.abs() @ K.abs() + _readout(Y, V, K, g, S0.T, c)
                 gq[2][b, i, :e] = aa @ K.abs() + (Y.abs() * first) @ S0.abs().T * c
                 gk[0][b, h, :e] += a.T @ Q
-                gk[1][b, h, :e] += a.abs().T @ Q.abs()
+                gk[1][b, h, :e] += a.abs().T @ Q.abs() + _readout(V, Y * c, Q, g, Ue.T / G, 1.0, True)
                 gk[2][b, h, :e] += aa.T @ Q.abs()
                 gv[0][b, h, :e] += w.T @ Y
-                gv[1][b, h, :e] += w.abs().T @ Y.abs()
+                gv[1][b, h, :e] += w.abs().T @ Y.abs() + _readout(K, Q * c, Y, g, Ue / G, 1.0, True)
                 gv[2][b, h, :e] += ww.T @ Y.abs()
                 gS[0][b, h] += (Q * first).T @ Y * c
                 gS[1][b, h] += (Q.abs() * first).T @ Y.abs() * c

@@ -24,7 +24,7 @@ def _inputs(seed, B, H, G, n, dk, dv):
 
 @pytest.fixture(autouse=True)
 def _f64(monkeypatch):
-    for table in (pair_ref.HALF, pair_ref.WEIGHT, pair_ref.STATE):
+    for table in (pair_ref.HALF, pair_ref.WEIGHT):
         monkeypatch.setitem(table, torch.float64, 2.0 ** -50)
 
 
