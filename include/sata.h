@@ -295,7 +295,7 @@ sata_status sata_decode_step_grouped(float* S, const void* q, const void* k, con
 
 /* Bytes of scratch (host only; -1 for sizes that the calls refuse): of sata_decay_prefill and
  * sata_decay_backward, of sata_softmax_backward, and of sata_softmax_step. */
-int64_t sata_decay_scratch(int B, int H_kv, int n, int d_k, int d_v);
+int64_t sata_decay_scratch(int B, int H_kv, int G, int n, int d_k, int d_v);
 int64_t sata_softmax_backward_scratch(int B, int H_kv, int G, int n);
 int64_t sata_softmax_step_scratch(int B, int H_kv, int G, int capacity, int d_v);
 

@@ -66,7 +66,7 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.sata_decode_step_compensated.restype = i32
     lib.sata_decode_step_grouped.argtypes = [vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, vp, vp]
     lib.sata_decode_step_grouped.restype = i32
-    lib.sata_decay_scratch.argtypes = [i32, i32, i32, i32, i32]
+    lib.sata_decay_scratch.argtypes = [i32, i32, i32, i32, i32, i32]
     lib.sata_decay_scratch.restype = i64
     lib.sata_softmax_backward_scratch.argtypes = [i32, i32, i32, i32]
     lib.sata_softmax_backward_scratch.restype = i64
@@ -527,7 +527,7 @@ def decay_prefill(q, k, v, log_decay, lengths=None, S_in=None, want_state: bool 
         y = torch.empty(B, G * H, n, dv, dtype=q.dtype, device=q.device)
     if want_state and S is None:
         S = torch.empty(B, H, dk, dv, dtype=torch.float32, device=q.device)
-    scratch = _scratch(load_library().sata_decay_scratch(B, H, n, dk, dv), q.device)
+    scratch = _scratch(load_library().sata_decay_scratch(B, H, G, n, dk, dv), q.device)
     _invoke("sata_decay_prefill", q.device, _at(q), _at(k), _at(v), _at(log_decay), code, B, H, G, n, dk, dv,
             _at(lengths), _at(S_in), _at(y), _at(S), _at(scratch))
     return y, S
@@ -563,7 +563,7 @@ def decay_backward(q, k, v, log_decay, dy, lengths=None, S_in=None, dS=None):
     _check_tensors(q.device, q=q, k=k, v=v, log_decay=log_decay, dy=dy, lengths=lengths, S_in=S_in, dS=dS)
     dq, dkk, dvv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
     dS_in = torch.empty_like(S_in) if S_in is not None else None
-    scratch = _scratch(load_library().sata_decay_scratch(B, H, n, dk, dv), q.device)
+    scratch = _scratch(load_library().sata_decay_scratch(B, H, G, n, dk, dv), q.device)
     _invoke("sata_decay_backward", q.device, _at(q), _at(k), _at(v), _at(log_decay), _at(dy), code, B, H, G, n, dk,
             dv, _at(lengths), _at(S_in), _at(dS), _at(dq), _at(dkk), _at(dvv), _at(dS_in), _at(scratch))
     return dq, dkk, dvv, dS_in

@@ -40,8 +40,8 @@ namespace {
 // float32 one.  float32 inputs, weights and states: three bfloat16 numbers each.
 constexpr int kChunk = 32;
 
-// Parts of a head's sequence side by side: states[head][part] holds what each adds (written
-// by the sums) and then what it starts from, as [d_k][d_v]; null: one part.
+// Parts of a head's sequence side by side: states[head][part], as [d_k][d_v], is what each adds to the
+// state (written by the sums) and then what it starts from.
 struct ScanParts {
   int parts, part_len;  // (tokens: a multiple of the chunk)
   float* states;
@@ -75,7 +75,7 @@ struct ScanLds {
   using L = PairTile<T, ND, kChunk>;
   using LW = PairTile<T, W, kChunk>;
   static constexpr int kPowers = 2 * L::kElems + LW::kElems;  // (u16 before them)
-  static constexpr int kBytes = 2 * kPowers + 4 * (4 * kChunk + 4);
+  static constexpr int kBytes = 2 * kPowers + 4 * (4 * kChunk + 8);
 };
 
 // REV: from the last token back.  The members of a group (G) vary in a forward, and in b
@@ -92,10 +92,11 @@ __device__ __forceinline__ void scan_part(const DecayScan& s, const ScanParts& p
   u16* const ta = smem;
   u16* const tb = smem + L::kElems;
   u16* const tw = tb + L::kElems;
-  // lam^0 .. lam^C, behind C zeros (a power's place is a lane's number plus a constant), and
-  // the same times the scale of the scores
-  float* const power = (float*)(smem + D::kPowers) + C;
-  float* const scaled = power + 2 * C;
+  // Powers of lam at C + exponent, zeros below, and the same times the scale of the scores.  An exponent
+  // is a lane's number (at least -4) plus a constant: the lanes' pointers start 4 further
+  // on, so that the constants are the instructions' offsets (they took an address register each).
+  float* const power = (float*)(smem + D::kPowers);
+  float* const scaled = power + 2 * C + 4;
   const int tid = threadIdx.x, lane = tid & 63, l31 = lane & 31, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int len = tokens_of(s.lengths, head / s.H, s.n);
@@ -104,10 +105,10 @@ __device__ __forceinline__ void scan_part(const DecayScan& s, const ScanParts& p
   const int col0 = 32 * tile0, col = col0 + 32 * wave + l31;
   const double rate = decay_rate(s.log_decay[head % s.H]);
   for (int e = tid; e <= C; e += kThreads) {
-    power[e] = (float)exp(rate * e);
-    if (e < C) scaled[e] = power[e] * (s.update * s.readout);
-    if (e > 0) power[-e] = 0.f;
-    if (e > 0 && e < C) scaled[-e] = 0.f;
+    const float x = (float)exp(rate * e);
+    power[C + e] = x;
+    scaled[C + e] = x * (s.update * s.readout);
+    if (e < C) power[e] = scaled[e] = 0.f;
   }
 
   f32x16 S[ND];
@@ -117,7 +118,7 @@ __device__ __forceinline__ void scan_part(const DecayScan& s, const ScanParts& p
   };
   auto has = [&](int j, int i) { return 32 * j + result_row(i, h) < s.da && col < s.dw; };
   const int64_t size = (int64_t)s.da * s.dw;
-  float* const states = p.states ? p.states + ((int64_t)head * p.parts + part) * size : nullptr;
+  float* const states = p.parts > 1 ? p.states + ((int64_t)head * p.parts + part) * size : nullptr;
   const float* const from = SUMS ? nullptr : states ? states : s.S_in ? s.S_in + head * size : nullptr;
 #pragma unroll
   for (int j = 0; j < ND; ++j)
@@ -166,8 +167,11 @@ __device__ __forceinline__ void scan_part(const DecayScan& s, const ScanParts& p
       else ++g;
       if (u + 1 < units) fetch(g, row_of(c));
 
-      auto early = [&](int r) { return power[r + 1]; };
-      auto late = [&](int r) { return power[m - 1 - r]; };
+      // of the rows result_row(i, h) of a chunk's 32 (i a constant)
+      const float* const early = power + 4 * h;
+      const float* const late = power + m - 1 + 4 - 4 * h;
+      auto early_of = [&](int i) { return early[C + 1 + result_row(i, 0)]; };
+      auto late_of = [&](int i) { return late[C - 4 - result_row(i, 0)]; };
       // this wave's columns of w: operands of rows 16 x .. +15
       uint4 wf[C / 16][L::kPl];
       uint32_t bad = 0;
@@ -189,7 +193,7 @@ __device__ __forceinline__ void scan_part(const DecayScan& s, const ScanParts& p
             load_rows_as_results<L>(ta, 0, x, e);
             o = dot_planes32(st[0], e, o);
           }
-          const float k = s.readout * (float)f * (REV ? late(l31) : early(l31));
+          const float k = s.readout * (float)f * (REV ? power[C + m - 1 - l31] : power[C + 1 + l31]);
 #pragma unroll
           for (int i = 0; i < 16; ++i) o[i] *= k;
         }
@@ -203,13 +207,15 @@ __device__ __forceinline__ void scan_part(const DecayScan& s, const ScanParts& p
           acc = dot_planes32(e, own, acc);
         }
         __builtin_amdgcn_sched_barrier(0);
+        const float* const ahead = scaled + l31 + 4 - 4 * h;
+        const float* const behind = scaled + 32 + 4 * h - l31;
         float z[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const int far = l31 - result_row(i, h), e = REV ? -far : far;
-          float x = scaled[e];
+          const bool sees = REV ? result_row(i, h) >= l31 : result_row(i, h) <= l31;
+          float x = REV ? behind[C - 32 + result_row(i, 0)] : ahead[C - 4 - result_row(i, 0)];
           asm volatile("" : "+v"(x));  // (read by all lanes, not in 16 branches)
-          z[i] = e >= 0 ? acc[i] * x : 0.f;  // (a select: not finite times 0 is no zero)
+          z[i] = sees ? acc[i] * x : 0.f;  // (a select: not finite times 0 is no zero)
         }
         uint4 w[2][PA];
         to_planes<PA>(z, w);
@@ -282,17 +288,17 @@ __device__ __forceinline__ void scan_part(const DecayScan& s, const ScanParts& p
           __builtin_amdgcn_sched_barrier(0);
           float v[8];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) v[i] = 0.f;
-#pragma unroll
           for (int i = L::kPl - 1; i >= 0; --i) {
             const uint32_t u4[4] = {wf[x][i].x, wf[x][i].y, wf[x][i].z, wf[x][i].w};
 #pragma unroll
-            for (int y = 0; y < 4; ++y) v[2 * y] += lo_f32(u4[y]), v[2 * y + 1] += hi_f32(u4[y]);
+            for (int y = 0; y < 4; ++y) {
+              v[2 * y] = i == L::kPl - 1 ? lo_f32(u4[y]) : v[2 * y] + lo_f32(u4[y]);
+              v[2 * y + 1] = i == L::kPl - 1 ? hi_f32(u4[y]) : v[2 * y + 1] + hi_f32(u4[y]);
+            }
           }
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            const int r = 16 * x + result_row(i, h);
-            v[i] *= up * (REV ? early(r) : late(r));
+            v[i] *= up * (REV ? early_of(8 * x + i) : late_of(8 * x + i));
           }
           uint4 w3[1][3];
           to_planes<3>(v, w3);
@@ -307,7 +313,8 @@ __device__ __forceinline__ void scan_part(const DecayScan& s, const ScanParts& p
       }
     }
   }
-  float* const to = SUMS ? states : !states && s.S_out ? s.S_out + head * size : nullptr;
+  float* const to = SUMS ? states
+                         : s.S_out && part == (REV ? 0 : p.parts - 1) ? s.S_out + head * size : nullptr;
   if (to) {
     const float k = (float)f;
 #pragma unroll
@@ -330,7 +337,8 @@ __global__ void __launch_bounds__(64 * W, sizeof(T) == 2 ? 2 : 1) decay_scan_ker
   extern __shared__ __attribute__((aligned(16))) u16 smem16[];
   const DecayScan& s0 = a.job[0].s;
   // An XCD takes whole heads: what the jobs, parts and columns of a head read is read through one L2.
-  const int each = a.jobs * a.job[0].p.parts * a.splits;
+  // (nobody reads what the last part adds, in reverse the first)
+  const int parts = a.job[0].p.parts - (SUMS ? 1 : 0), each = a.jobs * parts * a.splits;
   int head, unit;
   if (s0.heads >= 8) {
     const int j = blockIdx.x >> 3;
@@ -341,8 +349,9 @@ __global__ void __launch_bounds__(64 * W, sizeof(T) == 2 ? 2 : 1) decay_scan_ker
     head = blockIdx.x / each;
     unit = blockIdx.x % each;
   }
-  const int split = unit % a.splits, job = unit / a.splits % a.jobs, part = unit / a.splits / a.jobs;
+  const int split = unit % a.splits, job = unit / a.splits % a.jobs;
   const DecayScan& s = a.job[job].s;
+  const int part = unit / a.splits / a.jobs + (SUMS && s.reverse ? 1 : 0);
   const ScanParts& p = a.job[job].p;
   if (32 * W * split >= s.dw) return;  // (d_k and d_v may differ)
   if (s.reverse) scan_part<T, ND, W, true, SUMS>(s, p, head, part, W * split, smem16);
@@ -355,10 +364,10 @@ __global__ void __launch_bounds__(256) decay_carry_kernel(ScanJobs a) {
   const ScanParts& p = a.job[blockIdx.z].p;
   const int head = blockIdx.y, i = blockIdx.x * 256 + threadIdx.x;
   const int64_t size = (int64_t)s.da * s.dw;
+  if (i >= size) return;
   const int len = tokens_of(s.lengths, head / s.H, s.n);
   const double rate = decay_rate(s.log_decay[head % s.H]);
   const FloatPair whole = float_pair(exp(rate * p.part_len)), rest = float_pair(exp(rate * (len % p.part_len)));
-  if (i >= size) return;
   float* const states = p.states + (int64_t)head * p.parts * size + i;
   float R = s.S_in ? s.S_in[head * size + i] : 0.f;
   constexpr int kAhead = 8;  // parts read at once
@@ -367,19 +376,17 @@ __global__ void __launch_bounds__(256) decay_carry_kernel(ScanJobs a) {
 #pragma unroll
     for (int x = 0; x < kAhead; ++x) {
       const int part = s.reverse ? p.parts - 1 - c0 - x : c0 + x;
-      add[x] = c0 + x < p.parts ? states[part * size] : 0.f;
+      add[x] = c0 + x + 1 < p.parts ? states[part * size] : 0.f;  // (of the last part: not there, nor needed)
     }
 #pragma unroll
     for (int x = 0; x < kAhead; ++x) {
       if (c0 + x >= p.parts) break;
-      const int part = s.reverse ? p.parts - 1 - c0 - x : c0 + x;
+      const int part = s.reverse ? p.parts - 1 - c0 - x : c0 + x, tokens = len - part * p.part_len;
       states[part * size] = R;
-      const int tokens = len - part * p.part_len;
       if (tokens >= p.part_len) R = times(R, whole) + add[x];
       else if (tokens > 0) R = times(R, rest) + add[x];
     }
   }
-  if (s.S_out) s.S_out[head * size + i] = R;
 }
 
 template <typename T, int ND, int W, bool SUMS>
@@ -393,7 +400,8 @@ hipError_t launch_jobs(ScanJobs a, hipStream_t st) {
   }
   a.splits = (ND + W - 1) / W;
   const int heads = a.job[0].s.heads;
-  const int64_t grid = (int64_t)(heads >= 8 ? (heads + 7) / 8 * 8 : heads) * a.jobs * a.job[0].p.parts * a.splits;
+  const int64_t grid = (int64_t)(heads >= 8 ? (heads + 7) / 8 * 8 : heads) * a.jobs * (a.job[0].p.parts - (SUMS ? 1 : 0)) *
+                       a.splits;
   hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(64 * W), bytes, st, a);
   return hipGetLastError();
 }
@@ -417,8 +425,6 @@ hipError_t launch_scan(const DecayScan* scans, int count, const DecayScan* sums,
     a.job[i] = ScanJob{scans[i], {plan.parts, plan.part_len,
                                   plan.parts > 1 ? states + (scans[i].reverse ? sum_count - 1 : 0) * scans[0].heads * plan.parts * size
                                                  : nullptr}};
-  if constexpr (ND % 2 == 0)
-    if (plan.split) return launch_jobs<T, ND, ND / 2, false>(a, st);
   return launch_jobs<T, ND, ND, false>(a, st);
 }
 
@@ -431,23 +437,40 @@ hipError_t launch_scan_t(const DecayScan* scans, int count, const DecayScan* sum
 
 }  // namespace
 
-DecayScanPlan plan_decay_scan(int heads, int n, int da, int dw, int jobs) {
-  DecayScanPlan p;
-  const int tiles = (std::max(da, dw) + 31) / 32, chunks = (n + kChunk - 1) / kChunk;
-  const int64_t waves = (int64_t)heads * tiles * jobs;
-  const int64_t want = std::max<int64_t>(1, 2048 / waves);
-  const int each = (int)std::max<int64_t>(std::max(1, std::min(chunks, 4)), (chunks + want - 1) / want);
-  p.parts = std::max(1, (chunks + each - 1) / each);
-  p.part_len = each * kChunk;
-  p.split = p.parts == 1 && waves <= 1024;
-  p.state_bytes = p.parts > 1 ? sizeof(float) * (size_t)heads * p.parts * da * dw : 0;
-  return p;
+// The number of parts with the least estimated time, in us on an MI355X: chunks one after the other
+// in a workgroup, workgroups side by side as far as there are slots (8 waves a compute unit, float32 4), the sums at
+// 0.45 of a scan's chunk or the time of their bytes, two launches more and the states read and written.
+DecayScanPlan plan_decay_scan(bool bf16, int heads, int G, int n, int da, int dw, int jobs) {
+  const int tiles = (std::max(da, dw) + 31) / 32, chunks = std::max(1, (n + kChunk - 1) / kChunk);
+  const double unit = bf16 ? 1.6 + 0.6 * tiles : 2.0 + 1.3 * tiles, slots = (bf16 ? 2048.0 : 1024.0) / tiles;
+  const int sums = jobs > 1 ? 2 : 1;
+  const double bytes = (double)heads * n * (da + dw) * (bf16 ? 2 : 4) * (sums > 1 ? 0.5 * (1 + G) : 1.0);
+  DecayScanPlan best;
+  double least = 0.0;
+  for (int each = chunks; each >= 1; each = each > 8 ? (each + 1) / 2 : each - 1) {
+    const int parts = (chunks + each - 1) / each;
+    const double wgs = (double)heads * jobs * parts;
+    double t = std::max(1.0, wgs / slots) * each * G * unit;
+    if (parts > 1) {
+      const double work = std::max(1.0, (double)heads * sums * (parts - 1) / slots) * each * (sums > 1 ? 0.5 * (1 + G) : 1.0);
+      t += 10.0 + std::max(0.45 * unit * work, bytes * (parts - 1) / parts / 4.5e6) +
+           16.0 * sums * heads * parts * da * dw / 4.5e6;
+    }
+    if (best.part_len == 0 || t < least) {
+      least = t;
+      best.parts = parts;
+      best.part_len = each * kChunk;
+    }
+    if (each == 1) break;
+  }
+  best.state_bytes = best.parts > 1 ? sizeof(float) * (size_t)heads * best.parts * da * dw : 0;
+  return best;
 }
 
 hipError_t launch_decay_scan(const DecayScan* scans, int count, const DecayScan* sums, int sum_count, bool bf16,
                              float* states, hipStream_t st) {
   const DecayScan& s = scans[0];
-  const DecayScanPlan plan = plan_decay_scan(s.heads, s.n, s.da, s.dw, count);
+  const DecayScanPlan plan = plan_decay_scan(bf16, s.heads, s.G, s.n, s.da, s.dw, count);
   switch ((std::max(s.da, s.dw) + 31) / 32) {
     case 1: return launch_scan_t<1>(scans, count, sums, sum_count, bf16, states, plan, st);
     case 2: return launch_scan_t<2>(scans, count, sums, sum_count, bf16, states, plan, st);

@@ -220,14 +220,12 @@ struct DecayScan {
   float update = 1.f, readout = 1.f;
 };
 // Parts of a head's sequence that run side by side, where one part for a head would leave
-// compute units without work (what each part adds to the state is summed first), and
-// whether two workgroups share the state's columns.
+// compute units without work (what each part adds to the state is summed first).
 struct DecayScanPlan {
   int parts = 1, part_len = 0;
-  bool split = false;
   size_t state_bytes = 0;  // scratch for the states of one sum
 };
-DecayScanPlan plan_decay_scan(int heads, int n, int da, int dw, int jobs);
+DecayScanPlan plan_decay_scan(bool bf16, int heads, int G, int n, int da, int dw, int jobs);
 // Up to three scans over the same heads in one launch; `sums`: the scans (of layout [d_k][d_v]) whose
 // states the parts start from, the forward one first, the reverse one last.
 hipError_t launch_decay_scan(const DecayScan* scans, int count, const DecayScan* sums, int sum_count, bool bf16,

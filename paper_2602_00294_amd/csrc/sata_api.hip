@@ -958,10 +958,13 @@ sata_status sata_decode_step_grouped(float* S, const void* q, const void* k, con
   return ok();
 }
 
-int64_t sata_decay_scratch(int B, int H_kv, int n, int d_k, int d_v) {
-  if (check_pair_args(SATA_F32, B, H_kv, 1, n, d_k, d_v) != SATA_OK) return -1;
-  return (int64_t)std::max(sata::plan_decay_scan(B * H_kv, n, d_k, d_v, 1).state_bytes,
-                           2 * sata::plan_decay_scan(B * H_kv, n, d_k, d_v, 3).state_bytes);
+int64_t sata_decay_scratch(int B, int H_kv, int G, int n, int d_k, int d_v) {
+  if (check_pair_args(SATA_F32, B, H_kv, G, n, d_k, d_v) != SATA_OK) return -1;
+  size_t bytes = 0;
+  for (bool bf16 : {false, true})
+    bytes = std::max({bytes, sata::plan_decay_scan(bf16, B * H_kv, G, n, d_k, d_v, 1).state_bytes,
+                      2 * sata::plan_decay_scan(bf16, B * H_kv, G, n, d_k, d_v, 3).state_bytes});
+  return (int64_t)bytes;
 }
 
 int64_t sata_softmax_backward_scratch(int B, int H_kv, int G, int n) {
@@ -982,7 +985,7 @@ sata_status sata_decay_prefill(const void* q, const void* k, const void* v, cons
   if (!log_decay || (n > 0 && (!q || !k || !v || !y))) return fail(SATA_ERR_INVALID_ARG, "null tensor pointer");
   if (S_in && S_in == S_out) return fail(SATA_ERR_INVALID_ARG, "S_out must not be S_in");
   if (n == 0 && !S_out) return ok();
-  if ((st = check_scratch(scratch, sata::plan_decay_scan(B * H_kv, n, d_k, d_v, 1).state_bytes)) != SATA_OK) return st;
+  if ((st = check_scratch(scratch, sata::plan_decay_scan(dt == SATA_BF16, B * H_kv, G, n, d_k, d_v, 1).state_bytes)) != SATA_OK) return st;
   sata::DecayScan s;
   s.a = q, s.b = k, s.w = v, s.out = y;
   s.S_in = S_in, s.S_out = S_out, s.log_decay = log_decay, s.lengths = lengths;
@@ -1014,7 +1017,7 @@ sata_status sata_decay_backward(const void* q, const void* k, const void* v, con
     return fail(SATA_ERR_INVALID_ARG, "null tensor pointer");
   if (dS && dS == dS_in) return fail(SATA_ERR_INVALID_ARG, "dS_in must not be dS");
   if (n == 0 && !dS_in) return ok();
-  if ((st = check_scratch(scratch, 2 * sata::plan_decay_scan(B * H_kv, n, d_k, d_v, 3).state_bytes)) != SATA_OK) return st;
+  if ((st = check_scratch(scratch, 2 * sata::plan_decay_scan(dt == SATA_BF16, B * H_kv, G, n, d_k, d_v, 3).state_bytes)) != SATA_OK) return st;
   const float c = pair_scale(d_k);
   sata::DecayScan s;
   s.log_decay = log_decay, s.lengths = lengths;
