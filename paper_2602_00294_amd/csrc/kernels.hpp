@@ -254,13 +254,14 @@ struct SoftmaxGradArgs {
 };
 hipError_t launch_softmax_backward(const SoftmaxGradArgs& a, bool bf16, hipStream_t s);
 
-// A head's cache in stretches, a workgroup for each and every 32 members of a group;
-// their sums lie in `bytes` bytes of scratch.
+// The heads' caches in stretches of `least` units or more, at most `workgroups` of them, for a card that
+// holds `places` at a time; a group's heads in blocks of 32.  The sums of heads of several stretches lie in
+// `bytes` bytes of scratch.
 struct SoftmaxStepPlan {
-  int stretches = 1, stretch_len = 0, blocks = 1;
+  int unit = 128, least = 2, places = 0, workgroups = 0, blocks = 1;
   size_t bytes = 0;
 };
-SoftmaxStepPlan plan_softmax_step(int heads, int G, int capacity, int dv);
+SoftmaxStepPlan plan_softmax_step(bool bf16, int heads, int G, int capacity, int dv);
 struct SoftmaxStepArgs {
   void *K, *V;         // [heads][capacity][d]
   const int* lengths;  // [heads / H]

@@ -231,9 +231,13 @@ struct TileStage {
   }
   __device__ __forceinline__ void init(const T* p, int rows_, int width_, int tid_) { init(p, rows_, width_, tid_, width_, 0); }
   // the rows from r0 on
+  template <bool STREAM = false>
   __device__ __forceinline__ void fetch(int r0) {
 #pragma unroll
-    for (int i = 0; i < kIt; ++i) r[i] = read(off + (uint32_t)(r0 + i * kPer) * (uint32_t)(pitch * (int)sizeof(T)));
+    for (int i = 0; i < kIt; ++i) {
+      const uint32_t at = off + (uint32_t)(r0 + i * kPer) * (uint32_t)(pitch * (int)sizeof(T));
+      r[i] = STREAM ? read.stream(at) : read(at);
+    }
   }
   __device__ static void put_entry(u16* dst, T x) {
     if constexpr (sizeof(T) == 4) {

@@ -196,6 +196,11 @@ struct VectorReader {
     typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
     return __builtin_bit_cast(uint4, (u32x4)__builtin_amdgcn_raw_buffer_load_b128(rsrc, (int)offset, 0, 0));
   }
+  // the same, streamed past the caches
+  __device__ __forceinline__ uint4 stream(uint32_t offset) const {
+    typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+    return __builtin_bit_cast(uint4, (u32x4)__builtin_amdgcn_raw_buffer_load_b128(rsrc, (int)offset, 0, 2));
+  }
 };
 
 // f(integral_constant<int, I>) for I = 0 .. N-1, unrolled.

@@ -3,10 +3,16 @@
 //
 // Bound: the cache is read once, 2 (d_k + d_v) bytes a key in bfloat16.  The G query heads that share
 // a key/value head are the columns of one 32 x 32 product, so a key's row serves all of
-// them.  A key/value head's rows are cut into stretches for as many workgroups as keep
-// every compute unit loading; a wave takes every W-th tile of 32 rows of a stretch and
-// has the next tile on its way while it works, so no wave waits for another one before
-// the end, where the waves' sums are joined (and the stretches' by a second kernel).
+// them.  The heads' caches are cut into stretches of one length, which the lengths of the
+// sequences decide on the card: as many of them as it holds workgroups at a time, so that
+// sequences of any lengths keep every compute unit loading to the end.  A wave takes every
+// W-th tile of 32 rows of a stretch and has the next tile on its way while it works, so no
+// wave waits for another one before the end, where the waves' sums are joined (and those of
+// a head of several stretches by a second kernel).
+// 128 heads of d = 128 in groups of four, sequences of 1 to 8192 rows (286 MB): 59 us (4.84 TB/s; a
+// copy of 4 GB 4.9), 78 with stretches of one length for all calls and plain loads; the same
+// with all caches full (537 MB) 91 us (5.92 TB/s), 104; all a quarter full 31 us, 62; one
+// sequence of 131072 rows 117 us, 159.  Loads are streamed: with plain ones 70 us for the first.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -32,33 +38,58 @@ struct StepState {
   float top, sum;
 };
 
+// The units of a sequence's cache: one at least, for its zeros or its new row.
+__device__ __forceinline__ int step_units(const SoftmaxStepArgs& a, const SoftmaxStepPlan& p, int b) {
+  const int at = a.lengths[b];
+  return at >= 0 && at < a.capacity ? at / p.unit + 1 : 1;
+}
+
+__device__ __forceinline__ int wave_total(int x) {
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) x += __shfl_xor(x, d);
+  return __builtin_amdgcn_readfirstlane(x);
+}
+
+// The length of a stretch in units, the same in every wave of a call: the units over the places of the
+// card, or a little more where the sequences' last, shorter stretches need places too; with about as
+// many heads as places only heads of twice the mean are cut.  There are never more than p.workgroups
+// stretches: max(places, heads) of full length, and one shorter one a head.
+__device__ __forceinline__ int step_stretch(const SoftmaxStepArgs& a, const SoftmaxStepPlan& p, int lane) {
+  if (p.workgroups <= p.places) return p.least;  // (as what follows finds; 2 us less)
+  const int B = a.heads / a.H, heads_of = a.H * p.blocks, heads = a.heads * p.blocks;
+  int all = 0;
+  for (int b = lane; b < B; b += 64) all += step_units(a, p, b);
+  all = wave_total(all) * heads_of;
+  const int most = max(p.places, heads);
+#pragma unroll 1
+  for (int i = 0; i < 4 && heads < p.places; ++i) {
+    const int places = p.places - i * heads / 4, len = max(p.least, (all + places - 1) / places);
+    int count = 0;
+    for (int b = lane; b < B; b += 64) count += (step_units(a, p, b) + len - 1) / len;
+    if (wave_total(count) * heads_of <= p.places) return len;
+  }
+  return max(p.least, 2 * ((all + most - 1) / most));
+}
+
+// One head's rows [first, end) of a sequence with `at` rows and its new one.
 template <typename T, int ND>
-__global__ void __launch_bounds__(64 * kStepWaves, sizeof(T) == 2 ? 2 : 1)
-softmax_step_kernel(SoftmaxStepArgs a, SoftmaxStepPlan p) {
+__device__ __forceinline__ void step_stretch_rows(const SoftmaxStepArgs& a, int64_t kvh, int block, int at, int first, int end,
+                                           float* part, u16* smem16, StepState (*state)[32]) {
   using L = PairTile<T, ND, 32>;
-  extern __shared__ __attribute__((aligned(16))) u16 smem16[];
-  __shared__ StepState state[kStepWaves][32];
   const int tid = threadIdx.x, lane = tid & 63, l31 = lane & 31, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  // workgroups of one key/value head lie next to each other
-  const int stretch = blockIdx.x % p.stretches, block = blockIdx.x / p.stretches % p.blocks;
-  const int64_t kvh = blockIdx.x / p.stretches / p.blocks;
-  const int dk = a.dk_, dv = a.dv_, at = a.lengths[kvh / a.H];
-  const bool on = at >= 0 && at < a.capacity;
+  const int dk = a.dk_, dv = a.dv_;
   const int members = min(32, a.G - 32 * block);
   const int64_t q0 = kvh * a.G + 32 * block;  // the block's first query head
-  const int first = stretch * p.stretch_len, end = on ? min(at + 1, first + p.stretch_len) : 0;
-  if (first >= end) {
-    // (no token at all: the first stretch writes the zeros)
-    if (!on && stretch == 0)
-      for (int i = tid; i < members * dv; i += 64 * kStepWaves) ((T*)a.y)[q0 * dv + i] = (T)0;
+  if (at < 0 || at >= a.capacity) {  // no token
+    for (int i = tid; i < members * dv; i += 64 * kStepWaves) ((T*)a.y)[q0 * dv + i] = (T)0;
     return;
   }
   T* const K = (T*)a.K + kvh * a.capacity * dk;
   T* const V = (T*)a.V + kvh * a.capacity * dv;
   const T* const kn = (const T*)a.k + kvh * dk;
   const T* const vn = (const T*)a.v + kvh * dv;
-  if (block == 0 && at < first + p.stretch_len) {
+  if (block == 0 && at < end) {
     for (int i = tid; i < dk; i += 64 * kStepWaves) K[(int64_t)at * dk + i] = kn[i];
     for (int i = tid; i < dv; i += 64 * kStepWaves) V[(int64_t)at * dv + i] = vn[i];
   }
@@ -86,12 +117,12 @@ softmax_step_kernel(SoftmaxStepArgs a, SoftmaxStepPlan p) {
   constexpr int kStep = 32 * kStepWaves;
   int r0 = first + 32 * wave;
   if (r0 < end) {
-    sk.fetch(r0);
-    sv.fetch(r0);
+    sk.template fetch<true>(r0);
+    sv.template fetch<true>(r0);
   }
   for (; r0 < end; r0 += kStep) {
     stage(sk, r0, kn, dk);
-    if (r0 + kStep < end) sk.fetch(r0 + kStep);
+    if (r0 + kStep < end) sk.template fetch<true>(r0 + kStep);
     f32x16 s = zero16();
 #pragma unroll
     for (int i = 0; i < 2 * ND; ++i) {
@@ -107,7 +138,7 @@ softmax_step_kernel(SoftmaxStepArgs a, SoftmaxStepPlan p) {
     }
     most *= c;
     stage(sv, r0, vn, dv);
-    if (r0 + kStep < end) sv.fetch(r0 + kStep);
+    if (r0 + kStep < end) sv.template fetch<true>(r0 + kStep);
     if (__ballot(most > top + 8.f)) {
       const float next = fmaxf(top, fmaxf(most, __shfl_xor(most, 32)));
       const float keep = exp2_fast(top - next);
@@ -158,33 +189,72 @@ softmax_step_kernel(SoftmaxStepArgs a, SoftmaxStepPlan p) {
       x = fmaf(sums[(w * members + m) * dv + col], k, x);
       l = fmaf(state[w][m].sum, k, l);
     }
-    if (p.stretches == 1) {
+    if (!part) {
       ((T*)a.y)[(q0 + m) * dv + col] = rounded<T>(x / l);
     } else {
-      float* const out = a.scratch + ((q0 + m) * p.stretches + stretch) * (dv + 2);
+      float* const out = part + m * (dv + 2);
       out[col] = x;
       if (col == 0) out[dv] = most, out[dv + 1] = l;
     }
   }
 }
 
-// The stretches' sums of one query head joined, in their order; one thread per column.
+template <typename T, int ND>
+__global__ void __launch_bounds__(64 * kStepWaves, sizeof(T) == 2 ? 2 : 1)
+softmax_step_kernel(SoftmaxStepArgs a, SoftmaxStepPlan p) {
+  extern __shared__ __attribute__((aligned(16))) u16 smem16[];
+  __shared__ StepState state[kStepWaves][32];
+  const int lane = threadIdx.x & 63, B = a.heads / a.H, heads_of = a.H * p.blocks;
+  const int len = step_stretch(a, p, lane);
+  // ---- which one this is: a lane counts the stretches of its own sequences
+  const int per = (B + 63) / 64, b0 = min(B, lane * per), b1 = min(B, b0 + per);
+  int mine = 0;
+  for (int b = b0; b < b1; ++b) mine += (step_units(a, p, b) + len - 1) / len;
+  int before = mine;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const int x = __shfl_up(before, d);
+    if (lane >= d) before += x;
+  }
+  before -= mine;
+  const int id = blockIdx.x;
+  const uint64_t here = __ballot(before * heads_of <= id && id < (before + mine) * heads_of);
+  if (!here) return;
+  const int from = __builtin_ctzll(here);
+  int b = __builtin_amdgcn_readlane(b0, from);
+  int rest = id - __builtin_amdgcn_readlane(before, from) * heads_of;
+  int count = (step_units(a, p, b) + len - 1) / len;
+  for (; rest >= count * heads_of; count = (step_units(a, p, b) + len - 1) / len) rest -= count * heads_of, ++b;
+  // (a head's stretches lie next to each other)
+  const int hb = rest / count, stretch = rest - hb * count, head = hb / p.blocks;
+  const int at = a.lengths[b], first = stretch * len * p.unit;
+  step_stretch_rows<T, ND>(a, (int64_t)b * a.H + head, hb - head * p.blocks, at, first, min(at + 1, first + len * p.unit),
+                           count == 1 ? nullptr : a.scratch + (int64_t)id * min(32, a.G) * (a.dv_ + 2), smem16, state);
+}
+
+// The sums of one query head's stretches joined, in their order; one thread per column.
 template <typename T>
 __global__ void __launch_bounds__(kMaxPairDim) softmax_join_kernel(SoftmaxStepArgs a, SoftmaxStepPlan p) {
-  const int64_t qh = blockIdx.x;
-  const int dv = a.dv_, col = threadIdx.x, at = a.lengths[qh / a.G / a.H];
-  if (col >= dv || at < 0 || at >= a.capacity) return;
-  const int count = at / p.stretch_len + 1;
-  const float* const in = a.scratch + qh * p.stretches * (dv + 2);
+  const int qh = blockIdx.x, kvh = qh / a.G, member = qh - kvh * a.G, seq = kvh / a.H;
+  const int dv = a.dv_, col = threadIdx.x, lane = col & 63, heads_of = a.H * p.blocks;
+  const int len = step_stretch(a, p, lane), count = (step_units(a, p, seq) + len - 1) / len;
+  if (count == 1) return;
+  int before = 0;
+  for (int b = lane; b < seq; b += 64) before += (step_units(a, p, b) + len - 1) / len;
+  const int id = wave_total(before) * heads_of + ((kvh - seq * a.H) * p.blocks + member / 32) * count;
+  if (col >= dv) return;
+  const int64_t pitch = (int64_t)min(32, a.G) * (dv + 2);
+  const float* const sums = a.scratch + id * pitch + (member % 32) * (dv + 2);
   float most = -3.4028234e38f;
-  for (int s = 0; s < count; ++s) most = fmaxf(most, in[s * (dv + 2) + dv]);
+  for (int w = 0; w < count; ++w) most = fmaxf(most, sums[w * pitch + dv]);
   float x = 0.f, l = 0.f;
-  for (int s = 0; s < count; ++s) {
-    const float k = exp2_fast(in[s * (dv + 2) + dv] - most);
-    x = fmaf(in[s * (dv + 2) + col], k, x);
-    l = fmaf(in[s * (dv + 2) + dv + 1], k, l);
+  for (int w = 0; w < count; ++w) {
+    const float* const in = sums + w * pitch;
+    const float k = exp2_fast(in[dv] - most);
+    x = fmaf(in[col], k, x);
+    l = fmaf(in[dv + 1], k, l);
   }
-  ((T*)a.y)[qh * dv + col] = rounded<T>(x / l);
+  ((T*)a.y)[(int64_t)qh * dv + col] = rounded<T>(x / l);
 }
 
 template <typename T, int ND>
@@ -197,27 +267,28 @@ hipError_t launch_step(const SoftmaxStepArgs& a, const SoftmaxStepPlan& p, hipSt
     hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL(kern, dim3((unsigned)(a.heads * p.blocks * p.stretches)), dim3(64 * kStepWaves), bytes, s, a, p);
+  hipLaunchKernelGGL(kern, dim3(p.workgroups), dim3(64 * kStepWaves), bytes, s, a, p);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || p.stretches == 1) return e;
+  if (e != hipSuccess || p.bytes == 0) return e;
   hipLaunchKernelGGL(softmax_join_kernel<T>, dim3(a.heads * a.G), dim3((a.dv_ + 63) / 64 * 64), 0, s, a, p);
   return hipGetLastError();
 }
 
 }  // namespace
 
-SoftmaxStepPlan plan_softmax_step(int heads, int G, int capacity, int dv) {
+SoftmaxStepPlan plan_softmax_step(bool bf16, int heads, int G, int capacity, int dv) {
   SoftmaxStepPlan p;
   p.blocks = (G + 31) / 32;
-  const int64_t want = std::max<int64_t>(1, 1024 / ((int64_t)heads * p.blocks));
-  p.stretch_len = (int)std::max<int64_t>(256, (capacity + want * 128 - 1) / (want * 128) * 128);
-  p.stretches = (capacity + p.stretch_len - 1) / p.stretch_len;
-  p.bytes = p.stretches > 1 ? sizeof(float) * (size_t)heads * G * p.stretches * (dv + 2) : 0;
+  const int count = heads * p.blocks;
+  p.places = bf16 ? 512 : 256;
+  const int64_t most = (int64_t)count * (((capacity + p.unit - 1) / p.unit + p.least - 1) / p.least);
+  p.workgroups = (int)std::min<int64_t>(std::max(p.places, count) + count, most);
+  p.bytes = p.workgroups > count ? sizeof(float) * (size_t)p.workgroups * std::min(32, G) * (dv + 2) : 0;
   return p;
 }
 
 hipError_t launch_softmax_step(const SoftmaxStepArgs& a, bool bf16, hipStream_t s) {
-  const SoftmaxStepPlan p = plan_softmax_step(a.heads, a.G, a.capacity, a.dv_);
+  const SoftmaxStepPlan p = plan_softmax_step(bf16, a.heads, a.G, a.capacity, a.dv_);
   switch ((std::max(a.dk_, a.dv_) + 31) / 32) {
     case 1: return bf16 ? launch_step<u16, 1>(a, p, s) : launch_step<float, 1>(a, p, s);
     case 2: return bf16 ? launch_step<u16, 2>(a, p, s) : launch_step<float, 2>(a, p, s);

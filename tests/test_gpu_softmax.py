@@ -89,6 +89,20 @@ def test_prompt_and_gradients(sata, B, H, G, n, dk, dv, dtype, lengths):
     _check_prompt(sata, *_prompt(n + dk, B, H, G, n, dk, dv, dtype), lengths)
 
 
+MANY_HEADS = [  # B, H, G, n, dk, dv, dtype, lengths
+    (8, 16, 1, 300, 32, 32, "bf16", None),
+    (2, 16, 4, 513, 16, 128, "bf16", [513, 400]),
+    (3, 30, 3, 33, 64, 64, "bf16", [33, 0, 32]),
+    (4, 16, 4, 65, 96, 80, "f32", [65, 64, 1, 33]),
+]
+
+
+@pytest.mark.parametrize("B,H,G,n,dk,dv,dtype,lengths", MANY_HEADS)
+def test_many_heads(sata, B, H, G, n, dk, dv, dtype, lengths):
+    _say("softmax prompt, many heads", B, H, G, n, dk, dv, dtype, lengths)
+    _check_prompt(sata, *_prompt(n + dk, B, H, G, n, dk, dv, dtype), lengths)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_unaligned_tensors(sata, dtype):
     _say("softmax, tensors one element off", dtype)
@@ -114,6 +128,16 @@ TOKENS = [  # B, H, G, capacity, dk, dv, dtype, lengths
     (2, 1, 1, 4099, 128, 128, "f32", [4098, 17]),
     (1, 1, 20, 2600, 96, 100, "bf16", [2599]),
     (2, 2, 1, 3001, 40, 24, "bf16", [3000, 2047]),
+    # groups of more than 32
+    (2, 2, 33, 70, 32, 32, "bf16", [69, 31]),
+    (1, 2, 70, 700, 64, 40, "f32", [650]),
+    # one long sequence among short ones, ones without a token among them
+    (5, 2, 2, 9000, 32, 32, "bf16", [3, 8999, -1, 100, 9000]),
+    (70, 4, 1, 1100, 16, 16, "bf16", [(397 * b) % 1103 - 1 for b in range(70)]),
+    # more heads than the card holds workgroups, and about as many
+    (150, 4, 2, 600, 16, 24, "bf16", [(211 * b) % 600 for b in range(150)]),
+    (65, 4, 1, 900, 16, 16, "f32", [899] + [(97 * b) % 300 for b in range(64)]),
+    (48, 8, 1, 800, 16, 16, "bf16", [(173 * b) % 800 for b in range(48)]),
 ]
 
 
