@@ -281,15 +281,13 @@ struct TileStage {
   }
 };
 
-// Two tensors x and y walked together, ROWS rows at a time, through two LDS buffers of two tiles
-// (x, then y) each.  work(buffer, r0) is called for every 32 rows; the next rows are on their way
-// meanwhile: with two calls a step x's during the first and y's during the second, so
-// that the registers of one tensor do for both.
+// Two tensors x and y walked together, ROWS rows at a time, through LDS buffers of two tiles (x,
+// then y) each: rows are fetched a whole step before they are put into the buffer that the step
+// does not read.
 template <typename T, int ND, int ROWS, int THREADS>
 struct PairStage {
   using S = TileStage<T, ND, ROWS, THREADS>;
   using L = typename S::L;
-  static_assert(ROWS == 32 || ROWS == 64, "one or two calls a step");
   const T *x, *y;
   int x_width, y_width, rows, tid;
   S a, b;
@@ -297,30 +295,29 @@ struct PairStage {
   __device__ __forceinline__ void open(const T* x_, int x_width_, const T* y_, int y_width_, int rows_, int tid_) {
     x = x_, x_width = x_width_, y = y_, y_width = y_width_, rows = rows_, tid = tid_;
   }
-  // both tensors' rows from r0 on, into a buffer
-  __device__ __forceinline__ void load(u16* buf, int r0) {
+  // both tensors' rows from r0 on, on their way
+  __device__ __forceinline__ void fetch(int r0) {
     a.init(x, rows, x_width, tid);
     b.init(y, rows, y_width, tid);
     a.fetch(r0);
     b.fetch(r0);
+  }
+  // and there
+  __device__ __forceinline__ void put(u16* buf, int r0) const {
     a.put(buf, r0);
     b.put(buf + L::kElems, r0);
   }
-  // the work on a buffer, while the rows from `next` on (none where !more) go to `other`
+  __device__ __forceinline__ void load(u16* buf, int r0) {
+    fetch(r0);
+    put(buf, r0);
+  }
+  // work(buffer, r) for every 32 rows of a buffer, while the rows from `next` on (none where !more) go to `other`
   template <typename F>
   __device__ __forceinline__ void step(const u16* buf, u16* other, bool more, int next, F&& work) {
-    if (more) {
-      a.init(x, rows, x_width, tid);
-      b.init(y, rows, y_width, tid);
-      a.fetch(next);
-      b.fetch(next);
-    }
+    if (more) fetch(next);
 #pragma unroll 1
     for (int r = 0; r < ROWS; r += 32) work(buf, r);
-    if (more) {
-      a.put(other, next);
-      b.put(other + L::kElems, next);
-    }
+    if (more) put(other, next);
   }
 };
 

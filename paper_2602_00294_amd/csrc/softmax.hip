@@ -82,12 +82,64 @@ __global__ void __launch_bounds__(64 * W, sizeof(T) == 2 ? 2 : 1) softmax_prefil
       to_planes<L::kPl>(z, w);
       contract32<L, ND>(vt, r0, w, o);
     };
+    // a staged block that every query of the workgroup sees whole
+    auto whole = [&](const u16* kt, const u16* vt) {
+      constexpr int kSub = kKeys / 32;
+      f32x16 s[kSub];
+#pragma unroll
+      for (int r = 0; r < kSub; ++r) s[r] = zero16();
+#pragma unroll
+      for (int i = 0; i < 2 * ND; ++i)
+#pragma unroll
+        for (int r = 0; r < kSub; ++r) {
+          uint4 f[L::kPl];
+          L::load_rows(kt, 32 * r, i, f);
+          s[r] = dot_planes32(f, qf[i], s[r]);
+        }
+      settle_mfma32();
+      float most = s[0][0];
+#pragma unroll
+      for (int i = 1; i < 16 * kSub; ++i) most = fmaxf(most, s[i / 16][i % 16]);
+      most *= c;
+      if (__ballot(most > top + 8.f)) {
+        const float next = fmaxf(top, fmaxf(most, __shfl_xor(most, 32)));
+        const float keep = exp2_fast(top - next);
+        top = next;
+        sum *= keep;
+#pragma unroll
+        for (int j = 0; j < ND; ++j)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[j][i] *= keep;
+      }
+#pragma unroll
+      for (int r = 0; r < kSub; ++r) {
+        float z[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          z[i] = exp2_fast(fmaf(s[r][i], c, -top));
+          sum += z[i];
+        }
+        uint4 w[2][L::kPl];
+        to_planes<L::kPl>(z, w);
+        contract32<L, ND>(vt, 32 * r, w, o);
+      }
+    };
     PairStage<T, ND, kKeys, kThreads> stage;
     stage.open((const T*)a.k + (int64_t)kvh * n * dk, dk, (const T*)a.v + (int64_t)kvh * n * dv, dv, len, tid);
     stage.load(smem16, 0);
     __syncthreads();
     const int steps = (end + kKeys - 1) / kKeys;
-    for (int st = 0; st < steps; ++st) {
+    const int all_see = 32 * kWaves * blk / kKeys;
+    int st = 0;
+    for (; st < all_see; ++st) {
+      u16* const now = smem16 + (st & 1) * 2 * L::kElems;
+      u16* const next = smem16 + ((st + 1) & 1) * 2 * L::kElems;
+      stage.fetch((st + 1) * kKeys);
+      whole(now, now + L::kElems);
+      stage.put(next, (st + 1) * kKeys);
+      __syncthreads();
+    }
+    for (; st < steps; ++st) {
       u16* const now = smem16 + (st & 1) * 2 * L::kElems;
       u16* const next = smem16 + ((st + 1) & 1) * 2 * L::kElems;
       stage.step(now, next, st + 1 < steps, (st + 1) * kKeys, [&](const u16* buf, int r) {

@@ -11,6 +11,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "device_common.hpp"
 #include "kernels.hpp"
@@ -106,7 +107,19 @@ __global__ void __launch_bounds__(64 * W, sizeof(T) == 2 ? 2 : 1) softmax_rows(S
     stage.load(smem16, 0);
     __syncthreads();
     const int steps = (min(len, 32 * W * (blk + 1)) + kRows - 1) / kRows;
-    for (int st = 0; st < steps; ++st) {
+    // (blocks that every query of the workgroup sees whole)
+    const int all_see = 32 * W * blk / kRows;
+    int st = 0;
+    for (; st < all_see; ++st) {
+      u16* const now = smem16 + (st & 1) * 2 * L::kElems;
+      u16* const next = smem16 + ((st + 1) & 1) * 2 * L::kElems;
+      stage.fetch((st + 1) * kRows);
+#pragma unroll
+      for (int r = 0; r < kRows; r += 32) work(now, now + L::kElems, r, false);
+      stage.put(next, (st + 1) * kRows);
+      __syncthreads();
+    }
+    for (; st < steps; ++st) {
       u16* const now = smem16 + (st & 1) * 2 * L::kElems;
       u16* const next = smem16 + ((st + 1) & 1) * 2 * L::kElems;
       stage.step(now, next, st + 1 < steps, (st + 1) * kRows, [&](const u16* buf, int r) {
@@ -129,83 +142,35 @@ __global__ void __launch_bounds__(64 * W, sizeof(T) == 2 ? 2 : 1) softmax_rows(S
   if (row < n) store_row32<T, ND>((T*)a.dq + at * dk, dk, acc, row < len ? a.scale : 0.f, row >= len);
 }
 
-// SPLIT: the sums of dk and of dv, 32 ND numbers a lane each, go to two waves with the same keys, wave
-// w of the first half dv, of the second half dk: both in one wave would leave it no
-// registers at ND >= 3 (they moved through the accumulation registers: 487 vector instructions a tile
-// instead of 150).  The scores are formed twice then.
-template <typename T, int ND, int W, bool SPLIT>
+// A tile of 32 keys has two waves, which share its pairs: wave t of the first half forms the scores, the
+// probabilities and dv, wave t of the second dy.v, e and dk, 4 ND matrix instructions each a pair of tiles;
+// the probabilities go from one to the other through LDS, in float32, behind a barrier in the
+// middle of each step.
+template <typename T, int ND, int W>
 __global__ void __launch_bounds__(64 * W, sizeof(T) == 2 ? 2 : 1) softmax_cols(SoftmaxGradArgs a, int blocks) {
-  constexpr int kRows = kStaged<T>, kThreads = 64 * W, kTiles = SPLIT ? W / 2 : W;
+  constexpr int kRows = kStaged<T>, kThreads = 64 * W, kTiles = W / 2, kSub = kRows / 32;
   using L = PairTile<T, ND, kRows>;
   constexpr int kBuf = 2 * L::kElems + 4 * kRows;  // Q rows, dy rows, then lse and delta as float
   extern __shared__ __attribute__((aligned(16))) u16 smem16[];
   const int tid = threadIdx.x, lane = tid & 63, l31 = lane & 31, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const bool for_k = !SPLIT || wave >= kTiles;
+  const bool for_k = wave >= kTiles;
+  // this pair of waves' probabilities: 16 numbers of a lane, four at a time
+  float4* const shared_p = (float4*)(smem16 + 2 * kBuf) + wave % kTiles * kSub * 4 * 64 + lane;
   int kvh, blk;
   if (!locate(a.heads, blocks, kvh, blk)) return;  // (the first keys have the longest sweeps)
   const int n = a.n, dk = a.dk_, dv = a.dv_;
   const int len = tokens_of(a.lengths, kvh / a.H, n);
   const int k0 = 32 * (kTiles * blk + wave % kTiles), row = k0 + l31;
   const int64_t at = (int64_t)kvh * n + row;
-  f32x16 acc[SPLIT ? 1 : 2][ND];  // dv (or dk), dk
+  f32x16 acc[ND];  // dv or dk
 #pragma unroll
-  for (int i = 0; i < (SPLIT ? 1 : 2); ++i)
-#pragma unroll
-    for (int j = 0; j < ND; ++j) acc[i][j] = zero16();
+  for (int j = 0; j < ND; ++j) acc[j] = zero16();
   if (32 * kTiles * blk < len) {
-    uint4 kf[2 * ND][L::kPl], vf[2 * ND][L::kPl];
-    load_own32<T, ND>((const T*)a.k + at * dk, row < len, dk, kf);
-    load_own32<T, ND>((const T*)a.v + at * dv, row < len && for_k, dv, vf);
+    uint4 own[2 * ND][L::kPl];  // k or v
+    load_own32<T, ND>(for_k ? (const T*)a.v + at * dv : (const T*)a.k + at * dk, row < len, for_k ? dv : dk, own);
     const float c = a.scale * kLog2e;
     bool odd = false;  // whether own tiles hold values that are not finite: such a member's is left out
-    auto work = [&](const u16* qt, const float* stat, int r0, bool own) {
-      const u16* const yt = qt + L::kElems;
-      f32x16 s = dot_rows32<L, ND>(qt, r0, kf);
-      float p[16], e[16];
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const float4 z4 = *(const float4*)(stat + r0 + 8 * g + 4 * h);
-        const float z[4] = {z4.x, z4.y, z4.z, z4.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) p[4 * g + i] = exp2_fast(fmaf(s[4 * g + i], c, -z[i]));
-      }
-      if (for_k) {
-        const f32x16 d = dot_rows32<L, ND>(yt, r0, vf);
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const float4 d4 = *(const float4*)(stat + kRows + r0 + 8 * g + 4 * h);
-          const float de[4] = {d4.x, d4.y, d4.z, d4.w};
-#pragma unroll
-          for (int i = 0; i < 4; ++i) e[4 * g + i] = p[4 * g + i] * (d[4 * g + i] - de[i]);
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) e[i] = p[i];
-      }
-      if (own) {
-        stay_in_branch();
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          if (!SPLIT) p[i] = result_row(i, h) < l31 ? 0.f : p[i];
-          e[i] = result_row(i, h) < l31 ? 0.f : e[i];
-        }
-        if (tile_not_finite<L, ND>(qt, r0) || tile_not_finite<L, ND>(yt, r0)) {
-          odd = true;
-          return;
-        }
-      }
-      uint4 w[2][L::kPl];
-      if constexpr (SPLIT) {
-        to_planes<L::kPl>(e, w);
-        contract32<L, ND>(for_k ? qt : yt, r0, w, acc[0]);
-      } else {
-        to_planes<L::kPl>(p, w);
-        contract32<L, ND>(yt, r0, w, acc[0]);
-        to_planes<L::kPl>(e, w);
-        contract32<L, ND>(qt, r0, w, acc[1]);
-      }
-    };
     PairStage<T, ND, kRows, kThreads> stage;
     const int first = 32 * kTiles * blk / kRows, steps = (len + kRows - 1) / kRows - first;
     int64_t base = 0;  // the member's first row
@@ -226,25 +191,85 @@ __global__ void __launch_bounds__(64 * W, sizeof(T) == 2 ? 2 : 1) softmax_cols(S
     if (tid < 2 * kRows) ((float*)(smem16 + 2 * L::kElems))[tid] = st0;
     __syncthreads();
     const int total = steps * a.G;
-    for (int u = 0, st = 0, g = 0; u < total; ++u) {
+    int u = 0, st = 0, g = 0;
+    auto step = [&](auto whole) {
+      constexpr bool kWhole = decltype(whole)::value;
       u16* const now = smem16 + (u & 1) * kBuf;
       u16* const then = smem16 + ((u + 1) & 1) * kBuf;
+      const float* const stats = (const float*)(now + 2 * L::kElems) + 4 * h;
       const bool more = u + 1 < total;
       int next = st + 1;
       if (next == steps) next = 0;
       if (more && next == 0) open(++g);
       const float stat = more ? stat_of((first + next) * kRows) : 0.f;
-      stage.step(now, then, more, (first + next) * kRows, [&](const u16* buf, int r) {
-        const int t0 = (first + st) * kRows + r;
-        if (t0 >= k0) work(buf, (const float*)(buf + 2 * L::kElems), r, t0 == k0);
-      });
-      if (more && tid < 2 * kRows) ((float*)(then + 2 * L::kElems))[tid] = stat;
-      st = next;
+      const int t0 = (first + st) * kRows;
+      if (more) stage.fetch((first + next) * kRows);
+      f32x16 x[kSub];  // scores, then probabilities; or dy.v, then e
+#pragma unroll
+      for (int r = 0; r < kSub; ++r) {
+        if (!kWhole && t0 + 32 * r < k0) continue;
+        x[r] = dot_rows32<L, ND>(now + (for_k ? L::kElems : 0), 32 * r, own);
+        if (!for_k) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float4 z = *(const float4*)(stats + 32 * r + 8 * i);
+            x[r][4 * i] = exp2_fast(fmaf(x[r][4 * i], c, -z.x));
+            x[r][4 * i + 1] = exp2_fast(fmaf(x[r][4 * i + 1], c, -z.y));
+            x[r][4 * i + 2] = exp2_fast(fmaf(x[r][4 * i + 2], c, -z.z));
+            x[r][4 * i + 3] = exp2_fast(fmaf(x[r][4 * i + 3], c, -z.w));
+            shared_p[(4 * r + i) * 64] = float4{x[r][4 * i], x[r][4 * i + 1], x[r][4 * i + 2], x[r][4 * i + 3]};
+          }
+        }
+      }
+      settle_mfma32();
       __syncthreads();
+#pragma unroll
+      for (int r = 0; r < kSub; ++r) {
+        if (!kWhole && t0 + 32 * r < k0) continue;
+        float e[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) e[i] = x[r][i];
+        if (for_k) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float4 p = shared_p[(4 * r + i) * 64], z = *(const float4*)(stats + kRows + 32 * r + 8 * i);
+            e[4 * i] = p.x * (e[4 * i] - z.x);
+            e[4 * i + 1] = p.y * (e[4 * i + 1] - z.y);
+            e[4 * i + 2] = p.z * (e[4 * i + 2] - z.z);
+            e[4 * i + 3] = p.w * (e[4 * i + 3] - z.w);
+          }
+        }
+        if (!kWhole && t0 + 32 * r == k0) {
+          stay_in_branch();
+#pragma unroll
+          for (int i = 0; i < 16; ++i) e[i] = result_row(i, h) < l31 ? 0.f : e[i];
+          if (tile_not_finite<L, ND>(now, 32 * r) || tile_not_finite<L, ND>(now + L::kElems, 32 * r)) {
+            odd = true;
+            continue;
+          }
+        }
+        uint4 w[2][L::kPl];
+        to_planes<L::kPl>(e, w);
+        contract32<L, ND>(now + (for_k ? 0 : L::kElems), 32 * r, w, acc);
+      }
+      if (more) {
+        stage.put(then, (first + next) * kRows);
+        if (tid < 2 * kRows) ((float*)(then + 2 * L::kElems))[tid] = stat;
+      }
+      st = next;
+      ++u;
+      __syncthreads();
+    };
+    constexpr int kOwn = 32 * kTiles / kRows;  // steps with own tiles of the workgroup
+    while (u < total) {
+      for (int i = min(kOwn, steps); i > 0; --i) step(std::false_type{});
+      for (int i = steps - kOwn; i > 0; --i) step(std::true_type{});
     }
     settle_mfma32();
     if (__builtin_expect(odd, 0)) {
       const int rows = min(32, len - k0);
+      uint4 kf[2 * ND][L::kPl];
+      load_own32<T, ND>((const T*)a.k + at * dk, row < len, dk, kf);
 #pragma unroll 1
       for (int g = 0; g < a.G; ++g) {
         const int64_t t0 = ((int64_t)kvh * a.G + g) * n + k0;
@@ -257,27 +282,27 @@ __global__ void __launch_bounds__(64 * W, sizeof(T) == 2 ? 2 : 1) softmax_cols(S
 #pragma unroll 1
         for (int r = 0; r < rows; ++r) {
           const float p = exp2_fast(fmaf(dot_row<T, ND>(kf, q + r * dk, dk), c, -kLog2e * a.lse[t0 + r]));
-          const float e = for_k ? p * (dot_row<T, ND>(vf, dy + r * dv, dv) - a.delta[t0 + r]) : 0.f;
+          const float d = dot_row<T, ND>(own, dy + r * dv, for_k ? dv : 0);
           if (r < l31) continue;
-          if (for_k) add_row(q + r * dk, dk, e, acc[SPLIT ? 0 : 1]);
-          if (!SPLIT || !for_k) add_row(dy + r * dv, dv, p, acc[0]);
+          if (for_k) add_row(q + r * dk, dk, p * (d - a.delta[t0 + r]), acc);
+          else add_row(dy + r * dv, dv, p, acc);
         }
       }
     }
   }
   if (row >= n) return;
-  if (for_k) store_row32<T, ND>((T*)a.dk + at * dk, dk, acc[SPLIT ? 0 : 1], a.scale, row >= len);
-  if (!SPLIT || !for_k) store_row32<T, ND>((T*)a.dv + at * dv, dv, acc[0], 1.f, row >= len);
+  store_row32<T, ND>(for_k ? (T*)a.dk + at * dk : (T*)a.dv + at * dv, for_k ? dk : dv, acc, for_k ? a.scale : 1.f, row >= len);
 }
 
 // WR, WC: waves of a workgroup of the two kernels.
-template <typename T, int ND, int WR, int WC, bool SPLIT>
+template <typename T, int ND, int WR, int WC>
 hipError_t launch_backward_w(const SoftmaxGradArgs& a, hipStream_t s) {
   using L = PairTile<T, ND, kStaged<T>>;
-  constexpr int rows_bytes = 4 * L::kBytes, cols_bytes = 2 * (2 * L::kBytes + 8 * kStaged<T>);
+  constexpr int rows_bytes = 4 * L::kBytes, 
+                cols_bytes = 2 * (2 * L::kBytes + 8 * kStaged<T>) + WC / 2 * kStaged<T> * 128;
   static_assert(cols_bytes <= 160 * 1024, "LDS of one workgroup");
   auto rows = softmax_rows<T, ND, WR>;
-  auto cols = softmax_cols<T, ND, WC, SPLIT>;
+  auto cols = softmax_cols<T, ND, WC>;
   if (cols_bytes > 64 * 1024) {
     hipError_t e = hipFuncSetAttribute((const void*)rows, hipFuncAttributeMaxDynamicSharedMemorySize, rows_bytes);
     if (e == hipSuccess) e = hipFuncSetAttribute((const void*)cols, hipFuncAttributeMaxDynamicSharedMemorySize, cols_bytes);
@@ -288,7 +313,7 @@ hipError_t launch_backward_w(const SoftmaxGradArgs& a, hipStream_t s) {
                      row_blocks);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  constexpr int keys = 32 * (SPLIT ? WC / 2 : WC);
+  constexpr int keys = 16 * WC;
   const int col_blocks = (a.n + keys - 1) / keys;
   hipLaunchKernelGGL(cols, dim3((unsigned)head_blocks(a.heads, col_blocks)), dim3(64 * WC), cols_bytes, s, a, col_blocks);
   return hipGetLastError();
@@ -296,9 +321,8 @@ hipError_t launch_backward_w(const SoftmaxGradArgs& a, hipStream_t s) {
 
 template <int ND>
 hipError_t launch_backward(const SoftmaxGradArgs& a, bool bf16, hipStream_t s) {
-  constexpr bool wide = ND >= 3;
-  if (!bf16) return launch_backward_w<float, ND, 4, 4, (ND >= 2)>(a, s);
-  return launch_backward_w<u16, ND, wide ? 8 : 4, wide ? 8 : 4, wide>(a, s);
+  if (!bf16) return launch_backward_w<float, ND, 4, 4>(a, s);
+  return launch_backward_w<u16, ND, ND >= 3 ? 8 : 4, 8>(a, s);
 }
 
 }  // namespace
