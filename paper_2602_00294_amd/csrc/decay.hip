@@ -19,9 +19,8 @@ namespace sata {
 
 namespace {
 
-// A workgroup takes W tiles of 32 columns of the state (and the output) of a stretch of one head's
-// tokens, in chunks of 32: wave j has the state's columns 32 j .. +31 in registers, one in
-// each lane pair.  With r a row of a chunk of m tokens and R the state before it (forward)
+// A workgroup of ND waves takes a part of one head's tokens, in chunks of 32: wave j has the
+// state's (and the output's) columns 32 j .. +31 in registers, one in each lane pair.  With r a row of a chunk of m tokens and R the state before it (forward)
 //     out_r = readout lam^(r+1) a_r R + sum_{s<=r} update readout lam^(r-s) (a_r.b_s) w_s
 //     R     = lam^m R + sum_s update lam^(m-1-s) b_s (x) w_s
 // and in reverse the same with lam^(m-1-r), lam^(s-r) and lam^(s+1).
@@ -52,7 +51,7 @@ struct ScanJob {
 };
 struct ScanJobs {
   ScanJob job[3];
-  int jobs, splits;  // splits: workgroups that share the state's columns
+  int jobs;
 };
 
 // Entries 16 s + 4 h .. +3 and 16 s + 8 + 4 h .. +3 of rows r0 .. r0 + 31: the order of a result's
@@ -70,23 +69,20 @@ __device__ __forceinline__ void load_rows_as_results(const u16* t, int r0, int s
   }
 }
 
-template <typename T, int ND, int W>
+template <typename T, int ND>
 struct ScanLds {
   using L = PairTile<T, ND, kChunk>;
-  using LW = PairTile<T, W, kChunk>;
-  static constexpr int kPowers = 2 * L::kElems + LW::kElems;  // (u16 before them)
+  static constexpr int kPowers = 3 * L::kElems;  // (u16 before them)
   static constexpr int kBytes = 2 * kPowers + 4 * (4 * kChunk + 8);
 };
 
 // REV: from the last token back.  The members of a group (G) vary in a forward, and in b
 // and w in reverse.  SUMS: only what the part adds to the state, from zero.
-template <typename T, int ND, int W, bool REV, bool SUMS>
-__device__ __forceinline__ void scan_part(const DecayScan& s, const ScanParts& p, int head, int part, int tile0,
-                                          u16* smem) {
-  constexpr int C = kChunk, kThreads = 64 * W;
-  using D = ScanLds<T, ND, W>;
+template <typename T, int ND, bool REV, bool SUMS>
+__device__ __forceinline__ void scan_part(const DecayScan& s, const ScanParts& p, int head, int part, u16* smem) {
+  constexpr int C = kChunk, kThreads = 64 * ND;
+  using D = ScanLds<T, ND>;
   using L = typename D::L;
-  using LW = typename D::LW;
   constexpr int PS = sizeof(T) == 2 ? 1 : 3;  // numbers of a state's entry in its readout
   constexpr int PA = sizeof(T) == 2 ? 2 : 3;  // of a pair's weight
   u16* const ta = smem;
@@ -102,7 +98,7 @@ __device__ __forceinline__ void scan_part(const DecayScan& s, const ScanParts& p
   const int len = tokens_of(s.lengths, head / s.H, s.n);
   const int first = part * p.part_len, last = min(first + p.part_len, s.n), end = max(first, min(last, len));
   const int chunks = (end - first + C - 1) / C;
-  const int col0 = 32 * tile0, col = col0 + 32 * wave + l31;
+  const int col = 32 * wave + l31;
   const double rate = decay_rate(s.log_decay[head % s.H]);
   for (int e = tid; e <= C; e += kThreads) {
     const float x = (float)exp(rate * e);
@@ -131,8 +127,7 @@ __device__ __forceinline__ void scan_part(const DecayScan& s, const ScanParts& p
     // (only the chunk at the sequence's end has fewer tokens)
     const int rest = end - first - (chunks - 1) * C;
     const double lam_c = exp(rate * C), lam_r = exp(rate * rest), inv_c = exp(-rate * C), inv_r = exp(-rate * rest);
-    TileStage<T, ND, C, kThreads> sa, sb;
-    TileStage<T, W, C, kThreads> sw;
+    TileStage<T, ND, C, kThreads> sa, sb, sw;
     auto row_of = [&](int c) { return first + (REV ? chunks - 1 - c : c) * C; };
     // tiles that unit (c, g) needs anew
     auto new_a = [&](int g) { return !SUMS && (!REV || g == 0); };
@@ -145,7 +140,7 @@ __device__ __forceinline__ void scan_part(const DecayScan& s, const ScanParts& p
       if (new_b(g)) {
         const int64_t m = (int64_t)head * (REV ? s.G : 1) + (REV ? g : 0);
         sb.init((const T*)s.b + m * s.n * s.da, len, s.da, tid);
-        sw.init((const T*)s.w + m * s.n * s.dw, len, min(32 * W, s.dw - col0), tid, s.dw, col0);
+        sw.init((const T*)s.w + m * s.n * s.dw, len, s.dw, tid);
         sb.fetch(t0);
         sw.fetch(t0);
       }
@@ -177,7 +172,7 @@ __device__ __forceinline__ void scan_part(const DecayScan& s, const ScanParts& p
       uint32_t bad = 0;
 #pragma unroll
       for (int x = 0; x < C / 16; ++x) {
-        LW::load_transposed(tw, 16 * x, wave, wf[x]);
+        L::load_transposed(tw, 16 * x, wave, wf[x]);
         bad |= not_finite_bits(wf[x][0]);
       }
       if constexpr (!SUMS) {
@@ -264,7 +259,7 @@ __device__ __forceinline__ void scan_part(const DecayScan& s, const ScanParts& p
           if (l31 < m) {
             T* const out = (T*)s.out + (((int64_t)head * (REV ? 1 : s.G) + (REV ? 0 : member)) * s.n + t0 + l31) * s.dw;
             const f32x16 one[1] = {o};
-            store_row32<T, 1>(out + col0 + 32 * wave, s.dw - col0 - 32 * wave, one, 1.f, false);
+            store_row32<T, 1>(out + 32 * wave, s.dw - 32 * wave, one, 1.f, false);
           }
         }
       }
@@ -324,21 +319,20 @@ __device__ __forceinline__ void scan_part(const DecayScan& s, const ScanParts& p
         if (has(j, i)) to[state_at(j, i)] = S[j][i] * k;
   }
   if (!SUMS) {
-    const int cols = min(32 * W, s.dw - col0);  // rows behind the sequence
-    for (int g = 0; g < (REV ? 1 : s.G); ++g) {
-      T* const out = (T*)s.out + (((int64_t)head * (REV ? 1 : s.G) + g) * s.n + end) * s.dw + col0;
-      for (int i = tid; i < (last - end) * cols; i += kThreads) out[(int64_t)(i / cols) * s.dw + i % cols] = (T)0;
+    for (int g = 0; g < (REV ? 1 : s.G); ++g) {  // rows behind the sequence
+      T* const out = (T*)s.out + (((int64_t)head * (REV ? 1 : s.G) + g) * s.n + end) * s.dw;
+      for (int i = tid; i < (last - end) * s.dw; i += kThreads) out[i] = (T)0;
     }
   }
 }
 
-template <typename T, int ND, int W, bool SUMS>
-__global__ void __launch_bounds__(64 * W, sizeof(T) == 2 ? 2 : 1) decay_scan_kernel(ScanJobs a) {
+template <typename T, int ND, bool SUMS>
+__global__ void __launch_bounds__(64 * ND, sizeof(T) == 2 ? 2 : 1) decay_scan_kernel(ScanJobs a) {
   extern __shared__ __attribute__((aligned(16))) u16 smem16[];
   const DecayScan& s0 = a.job[0].s;
-  // An XCD takes whole heads: what the jobs, parts and columns of a head read is read through one L2.
+  // An XCD takes whole heads: what the jobs and parts of a head read is read through one L2.
   // (nobody reads what the last part adds, in reverse the first)
-  const int parts = a.job[0].p.parts - (SUMS ? 1 : 0), each = a.jobs * parts * a.splits;
+  const int parts = a.job[0].p.parts - (SUMS ? 1 : 0), each = a.jobs * parts;
   int head, unit;
   if (s0.heads >= 8) {
     const int j = blockIdx.x >> 3;
@@ -349,13 +343,12 @@ __global__ void __launch_bounds__(64 * W, sizeof(T) == 2 ? 2 : 1) decay_scan_ker
     head = blockIdx.x / each;
     unit = blockIdx.x % each;
   }
-  const int split = unit % a.splits, job = unit / a.splits % a.jobs;
+  const int job = unit % a.jobs;
   const DecayScan& s = a.job[job].s;
-  const int part = unit / a.splits / a.jobs + (SUMS && s.reverse ? 1 : 0);
+  const int part = unit / a.jobs + (SUMS && s.reverse ? 1 : 0);
   const ScanParts& p = a.job[job].p;
-  if (32 * W * split >= s.dw) return;  // (d_k and d_v may differ)
-  if (s.reverse) scan_part<T, ND, W, true, SUMS>(s, p, head, part, W * split, smem16);
-  else scan_part<T, ND, W, false, SUMS>(s, p, head, part, W * split, smem16);
+  if (s.reverse) scan_part<T, ND, true, SUMS>(s, p, head, part, smem16);
+  else scan_part<T, ND, false, SUMS>(s, p, head, part, smem16);
 }
 
 // What each part adds becomes what it starts from; one thread per entry of a state.
@@ -389,20 +382,18 @@ __global__ void __launch_bounds__(256) decay_carry_kernel(ScanJobs a) {
   }
 }
 
-template <typename T, int ND, int W, bool SUMS>
-hipError_t launch_jobs(ScanJobs a, hipStream_t st) {
-  constexpr int bytes = ScanLds<T, ND, W>::kBytes;
+template <typename T, int ND, bool SUMS>
+hipError_t launch_jobs(const ScanJobs& a, hipStream_t st) {
+  constexpr int bytes = ScanLds<T, ND>::kBytes;
   static_assert(bytes <= 160 * 1024, "LDS of one workgroup");
-  auto kern = decay_scan_kernel<T, ND, W, SUMS>;
+  auto kern = decay_scan_kernel<T, ND, SUMS>;
   if (bytes > 64 * 1024) {
     hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != hipSuccess) return e;
   }
-  a.splits = (ND + W - 1) / W;
   const int heads = a.job[0].s.heads;
-  const int64_t grid = (int64_t)(heads >= 8 ? (heads + 7) / 8 * 8 : heads) * a.jobs * (a.job[0].p.parts - (SUMS ? 1 : 0)) *
-                       a.splits;
-  hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(64 * W), bytes, st, a);
+  const int64_t grid = (int64_t)(heads >= 8 ? (heads + 7) / 8 * 8 : heads) * a.jobs * (a.job[0].p.parts - (SUMS ? 1 : 0));
+  hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(64 * ND), bytes, st, a);
   return hipGetLastError();
 }
 
@@ -415,7 +406,7 @@ hipError_t launch_scan(const DecayScan* scans, int count, const DecayScan* sums,
     a.jobs = sum_count;
     for (int i = 0; i < sum_count; ++i)
       a.job[i] = ScanJob{sums[i], {plan.parts, plan.part_len, states + i * scans[0].heads * plan.parts * size}};
-    hipError_t e = launch_jobs<T, ND, ND, true>(a, st);
+    hipError_t e = launch_jobs<T, ND, true>(a, st);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(decay_carry_kernel, dim3((unsigned)((size + 255) / 256), scans[0].heads, sum_count), dim3(256), 0, st, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
@@ -425,7 +416,7 @@ hipError_t launch_scan(const DecayScan* scans, int count, const DecayScan* sums,
     a.job[i] = ScanJob{scans[i], {plan.parts, plan.part_len,
                                   plan.parts > 1 ? states + (scans[i].reverse ? sum_count - 1 : 0) * scans[0].heads * plan.parts * size
                                                  : nullptr}};
-  return launch_jobs<T, ND, ND, false>(a, st);
+  return launch_jobs<T, ND, false>(a, st);
 }
 
 template <int ND>

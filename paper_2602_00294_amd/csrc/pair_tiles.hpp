@@ -111,18 +111,25 @@ struct PairTile {
 #pragma unroll
     for (int i = 0; i < kPl; ++i) op[i] = read_transposed(a + i * kPlane, (int)(b - a));
   }
-  __device__ static __forceinline__ float value(const u16* t, int row, int col) {
-    float x = 0.f;
-#pragma unroll
-    for (int i = kPl - 1; i >= 0; --i) x += __uint_as_float((uint32_t)t[i * kPlane + at(row, col)] << 16);
-    return x;
-  }
 };
 
 // The entries of a plane that are infinite or NaN, all bits of each set.
 __device__ __forceinline__ uint4 not_finite_entries(const uint4& w) {
   auto wide = [](uint32_t x) { return ((((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u) >> 15) * 0xffffu; };
   return uint4{wide(w.x), wide(w.y), wide(w.z), wide(w.w)};
+}
+
+// 32 x 32 products of the tile's rows r0 .. +31 with this wave's rows.
+template <typename L, int ND>
+__device__ __forceinline__ f32x16 dot_rows32(const u16* t, int r0, const uint4 (&own)[2 * ND][L::kPl]) {
+  f32x16 s = zero16();
+#pragma unroll
+  for (int i = 0; i < 2 * ND; ++i) {
+    uint4 f[L::kPl];
+    L::load_rows(t, r0, i, f);
+    s = dot_planes32(f, own[i], s);
+  }
+  return s;
 }
 
 // acc[j] += (rows r0 .. r0 + 31 of the tile, columns 32 j .. +31)^T times the 32 x 32 weights w.
@@ -215,27 +222,25 @@ struct TileStage {
   static constexpr int kIt = (ROWS + kPer - 1) / kPer;
   static_assert(THREADS % kU == 0, "whole rows in a pass");
   const T* base;
-  int rows, width, pitch, tid;
+  int rows, width, tid;
   bool vec;
   uint32_t off;
   VectorReader read;
   uint4 r[kIt];
 
-  // `width` columns from column `col0` on of rows of `pitch` entries at p
-  __device__ __forceinline__ void init(const T* p, int rows_, int width_, int tid_, int pitch_, int col0) {
-    base = p + col0, rows = rows_, width = width_, pitch = pitch_, tid = tid_;
-    vec = pitch % kEV == 0 && ((uintptr_t)p & 15) == 0;
-    read = VectorReader(base, vec ? ((int64_t)rows * pitch - col0) * (int)sizeof(T) : 0);
+  __device__ __forceinline__ void init(const T* p, int rows_, int width_, int tid_) {
+    base = p, rows = rows_, width = width_, tid = tid_;
+    vec = width % kEV == 0 && ((uintptr_t)p & 15) == 0;
+    read = VectorReader(base, vec ? (int64_t)rows * width * (int)sizeof(T) : 0);
     const int row = tid / kU, col = tid % kU * kEV;
-    off = col < width && row < ROWS ? (uint32_t)(row * pitch + col) * (uint32_t)sizeof(T) : kNoVector;
+    off = col < width && row < ROWS ? (uint32_t)(row * width + col) * (uint32_t)sizeof(T) : kNoVector;
   }
-  __device__ __forceinline__ void init(const T* p, int rows_, int width_, int tid_) { init(p, rows_, width_, tid_, width_, 0); }
   // the rows from r0 on
   template <bool STREAM = false>
   __device__ __forceinline__ void fetch(int r0) {
 #pragma unroll
     for (int i = 0; i < kIt; ++i) {
-      const uint32_t at = off + (uint32_t)(r0 + i * kPer) * (uint32_t)(pitch * (int)sizeof(T));
+      const uint32_t at = off + (uint32_t)(r0 + i * kPer) * (uint32_t)(width * (int)sizeof(T));
       r[i] = STREAM ? read.stream(at) : read(at);
     }
   }
@@ -275,7 +280,7 @@ struct TileStage {
 #pragma unroll 1
       for (int i = tid; i < ROWS * 32 * ND; i += THREADS) {
         const int row = i / (32 * ND), col = i % (32 * ND);
-        put_entry(t + L::at(row, col), r0 + row < rows && col < width ? base[(int64_t)(r0 + row) * pitch + col] : (T)0);
+        put_entry(t + L::at(row, col), r0 + row < rows && col < width ? base[(int64_t)(r0 + row) * width + col] : (T)0);
       }
     }
   }
@@ -320,6 +325,12 @@ struct PairStage {
     if (more) put(other, next);
   }
 };
+
+// A wave's own stores to LDS before its lanes' loads.
+__device__ __forceinline__ void wave_lds_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
 
 // Right (or left) operands of one row per lane pair: entries 16 s + 8 h .. +7, all planes;
 // zero past the width and where !ok.
@@ -392,17 +403,64 @@ __device__ __forceinline__ void store_row32(T* p, int width, const f32x16 (&acc)
     }
 }
 
+// The sums of WAVES = 4 waves with the same rows, in the waves' order: x[j] has columns 32 j + 8 wave + 4 h
+// .. +3 of this lane's row.  buf: 1024 ND float4 of LDS that no wave reads any more when all
+// have come here.
+template <int ND>
+__device__ __forceinline__ void join_waves(const f32x16 (&acc)[ND], float4* buf, float (&x)[ND][4]) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < ND; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      buf[((wave * ND + j) * 4 + i) * 64 + lane] = float4{acc[j][4 * i], acc[j][4 * i + 1], acc[j][4 * i + 2], acc[j][4 * i + 3]};
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < ND; ++j) {
+    x[j][0] = x[j][1] = x[j][2] = x[j][3] = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float4 y = buf[((w * ND + j) * 4 + wave) * 64 + lane];
+      x[j][0] += y.x, x[j][1] += y.y, x[j][2] += y.z, x[j][3] += y.w;
+    }
+  }
+}
+// A lane's part of an output row so joined, scaled, or zeros.
+template <typename T, int ND>
+__device__ __forceinline__ void store_joined(T* p, int width, float (&x)[ND][4], float scale, bool zero) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const bool vec = width % 4 == 0 && ((uintptr_t)p & (4 * sizeof(T) - 1)) == 0;
+#pragma unroll
+  for (int j = 0; j < ND; ++j) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) x[j][r] = zero ? 0.f : x[j][r] * scale;
+    store4(p, 32 * j + 8 * wave + 4 * (lane >> 5), width, x[j], vec);
+  }
+}
+
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
 
 // v_exp_f32: within 1 ulp, results below 2^-126 are zero.
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// Whether `heads` heads of n tokens make so few workgroups of 128 rows that sweeps are the longest thing in the
+// call, and a workgroup for every 32 rows, whose waves share one sweep, is faster.  Prompts / gradients in us,
+// that way and with workgroups of 128 rows or more, bfloat16 unless said: d = 64, 16 heads of 1000 tokens
+// 12.9 / 34 and 20.1 / 57, 16 of 2000 28 / 75 and 35 / 102, 32 of 2000 50 / 139 and 44 / 119; d = 128, 1 of 8000
+// 88 / 244 and 169 / 620, 16 of 1000 23 / 61 and 30 / 101, 16 of 2000 62 / 174 and 52 / 179, 128 of 128
+// 13.0 / 35 and 10.9 / 31; float32, d = 64, 16 of 1000 38 / 114 and 57 / 156, 16 of 2000 114 / 332 and 103 / 289.
+template <typename T, int ND>
+inline bool few_sweeps(int64_t heads, int n) {
+  return n > 128 && heads * ((n + 127) / 128) <= (sizeof(T) == 2 && ND <= 2 ? 256 : 128);
+}
+
 // Workgroups go to the 8 XCDs in turn.  With 8 heads or more each XCD takes whole
 // heads, so that a head's rows are read through one L2, in sets of as many heads as make
 // two rounds of workgroups on its 32 compute units: block by block within a set, so that a
 // set ends with short sweeps everywhere (one head after the other left a third of the units
-// idle at the end: n = 4096, 16 blocks, 4 heads an XCD, rows 360 -> 265 us), and one
+// idle at the end: n = 4096, 16 blocks, 4 heads an XCD, gradients 784 -> 662 us), and one
 // after the other, so that few heads' rows compete for the L2.
 __device__ __forceinline__ bool locate(int heads, int blocks, int& head, int& blk) {
   if (heads >= 8) {

@@ -12,6 +12,26 @@ namespace sata {
 
 namespace {
 
+// The queries' own tile row by row (see dot_row): `rows` keys and values from k and v on.
+template <typename T, int ND, int PL>
+__device__ __forceinline__ void masked_rows(const T* k, int dk, const T* v, int dv, int rows, float c,
+                                            const uint4 (&qf)[2 * ND][PL], f32x16 (&o)[ND], float& top, float& sum) {
+  const int lane = threadIdx.x & 63, l31 = lane & 31, h = lane >> 5;
+#pragma unroll 1
+  for (int r = 0; r < rows; ++r) {
+    const float z = c * dot_row<T, ND>(qf, k + (int64_t)r * dk, dk);
+    if (r > l31) continue;
+    const float next = fmaxf(top, z), keep = exp2_fast(top - next), p = exp2_fast(z - next);
+    top = next;
+    sum = sum * keep + (h == 0 ? p : 0.f);
+#pragma unroll
+    for (int j = 0; j < ND; ++j)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[j][i] *= keep;
+    add_row(v + (int64_t)r * dv, dv, p, o);
+  }
+}
+
 // One workgroup of W waves per 32 W queries of a head, 32 to a wave, which are the columns
 // of its scores and outputs; the keys are walked in tiles of 32.  The exponentials' base
 // moves only when a score passes it by 2^8 (in either half of the lanes), so the outputs are rarely scaled.
@@ -42,13 +62,7 @@ __global__ void __launch_bounds__(64 * W, sizeof(T) == 2 ? 2 : 1) softmax_prefil
     bool odd = false;  // whether the own tile holds values that are not finite
     // keys r0 .. +31 of a staged block; own: the queries' own tile, of which each sees its part
     auto work = [&](const u16* kt, const u16* vt, int r0, bool own) {
-      f32x16 s = zero16();
-#pragma unroll
-      for (int i = 0; i < 2 * ND; ++i) {
-        uint4 f[L::kPl];
-        L::load_rows(kt, r0, i, f);
-        s = dot_planes32(f, qf[i], s);
-      }
+      f32x16 s = dot_rows32<L, ND>(kt, r0, qf);
       settle_mfma32();
       if (own) {
         stay_in_branch();
@@ -150,26 +164,120 @@ __global__ void __launch_bounds__(64 * W, sizeof(T) == 2 ? 2 : 1) softmax_prefil
     }
     settle_mfma32();
     if (__builtin_expect(odd, 0)) {
-#pragma unroll 1
-      for (int r = 0; r < min(32, len - q0); ++r) {
-        const int64_t key = (int64_t)kvh * n + q0 + r;
-        const float z = c * dot_row<T, ND>(qf, (const T*)a.k + key * dk, dk);
-        if (r > l31) continue;
-        const float next = fmaxf(top, z), keep = exp2_fast(top - next), p = exp2_fast(z - next);
-        top = next;
-        sum = sum * keep + (h == 0 ? p : 0.f);
-#pragma unroll
-        for (int j = 0; j < ND; ++j)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) o[j][i] *= keep;
-        add_row((const T*)a.v + key * dv, dv, p, o);
-      }
+      const int64_t key = (int64_t)kvh * n + q0;
+      masked_rows<T, ND>((const T*)a.k + key * dk, dk, (const T*)a.v + key * dv, dv, min(32, len - q0), c, qf, o, top, sum);
     }
   }
   if (row >= n) return;
   sum += __shfl_xor(sum, 32);
   store_row32<T, ND>(yp, dv, o, 1.f / sum, row >= len);
   if (a.lse && h == 0) a.lse[(int64_t)qh * n + row] = row < len ? top * kLn2 + logf(sum) : -INFINITY;
+}
+
+// One workgroup of four waves per 32 queries, for calls with few of them: a wave takes every fourth tile
+// of keys, through LDS of its own, so no wave waits for another one before the sums are joined.
+template <typename T, int ND>
+__global__ void __launch_bounds__(256, 1) softmax_prefill_few(SoftmaxArgs a, int blocks) {
+  using L = PairTile<T, ND, 32>;
+  extern __shared__ __attribute__((aligned(16))) u16 smem16[];
+  __shared__ float2 state[4][32];  // a wave's exponentials' base and their sum
+  const int tid = threadIdx.x, lane = tid & 63, l31 = lane & 31, h = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  int qh, blk;
+  if (!locate(a.heads * a.G, blocks, qh, blk)) return;
+  blk = blocks - 1 - blk;  // the longest first
+  const int kvh = qh / a.G, n = a.n, dk = a.dk_, dv = a.dv_;
+  const int len = tokens_of(a.lengths, kvh / a.H, n);
+  const int row = 32 * blk + l31;
+  T* const yp = (T*)a.y + ((int64_t)qh * n + row) * dv;
+  float* const lse = a.lse ? a.lse + (int64_t)qh * n + row : nullptr;
+  const bool last = wave == 0 && h == 0 && row < n;  // the lane that writes a row's lse
+  float x[ND][4];
+  if (32 * blk >= len) {
+#pragma unroll
+    for (int j = 0; j < ND; ++j) x[j][0] = x[j][1] = x[j][2] = x[j][3] = 0.f;
+    if (row < n) store_joined<T, ND>(yp, dv, x, 0.f, true);
+    if (lse && last) *lse = -INFINITY;
+    return;
+  }
+  f32x16 o[ND];
+#pragma unroll
+  for (int j = 0; j < ND; ++j) o[j] = zero16();
+  float top = -3.4028234e38f, sum = 0.f;
+  uint4 qf[2 * ND][L::kPl];
+  load_own32<T, ND>((const T*)a.q + ((int64_t)qh * n + row) * dk, row < len, dk, qf);
+  const float c = a.scale * kLog2e;
+  bool odd = false;  // whether the own tile holds values that are not finite
+  u16* const tile = smem16 + wave * L::kElems;
+  TileStage<T, ND, 32, 64> sk, sv;
+  sk.init((const T*)a.k + (int64_t)kvh * n * dk, len, dk, lane);
+  sv.init((const T*)a.v + (int64_t)kvh * n * dv, len, dv, lane);
+  int t = wave;
+  if (t <= blk) sk.fetch(32 * t), sv.fetch(32 * t);
+  for (; t <= blk; t += 4) {
+    wave_lds_fence();
+    sk.put(tile, 32 * t);
+    wave_lds_fence();
+    if (t + 4 <= blk) sk.fetch(32 * (t + 4));
+    f32x16 s = dot_rows32<L, ND>(tile, 0, qf);
+    settle_mfma32();
+    if (t == blk) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = result_row(i, h) > l31 ? -INFINITY : s[i];
+    }
+    float most = s[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) most = fmaxf(most, s[i]);
+    most *= c;
+    wave_lds_fence();
+    sv.put(tile, 32 * t);
+    wave_lds_fence();
+    if (t + 4 <= blk) sv.fetch(32 * (t + 4));
+    if (t == blk) {
+      odd = tile_not_finite<L, ND>(tile, 0);
+      if (odd) break;
+    }
+    if (__ballot(most > top + 8.f)) {
+      const float next = fmaxf(top, fmaxf(most, __shfl_xor(most, 32)));
+      const float keep = exp2_fast(top - next);
+      top = next;
+      sum *= keep;
+#pragma unroll
+      for (int j = 0; j < ND; ++j)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[j][i] *= keep;
+    }
+    float z[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      z[i] = exp2_fast(fmaf(s[i], c, -top));
+      sum += z[i];
+    }
+    uint4 w[2][L::kPl];
+    to_planes<L::kPl>(z, w);
+    contract32<L, ND>(tile, 0, w, o);
+  }
+  settle_mfma32();
+  if (__builtin_expect(odd, 0))
+    masked_rows<T, ND>((const T*)a.k + ((int64_t)kvh * n + 32 * blk) * dk, dk, (const T*)a.v + ((int64_t)kvh * n + 32 * blk) * dv,
+                       dv, min(32, len - 32 * blk), c, qf, o, top, sum);
+  sum += __shfl_xor(sum, 32);
+  if (h == 0) state[wave][l31] = float2{top, sum};
+  __syncthreads();
+  float most = state[0][l31].x, total = 0.f;
+#pragma unroll
+  for (int w = 1; w < 4; ++w) most = fmaxf(most, state[w][l31].x);
+#pragma unroll
+  for (int w = 0; w < 4; ++w) total = fmaf(state[w][l31].y, exp2_fast(state[w][l31].x - most), total);
+  const float keep = exp2_fast(top - most);
+#pragma unroll
+  for (int j = 0; j < ND; ++j)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[j][i] *= keep;
+  join_waves<ND>(o, (float4*)smem16, x);
+  if (row >= n) return;
+  store_joined<T, ND>(yp, dv, x, 1.f / total, row >= len);
+  if (lse && last) *lse = row < len ? most * kLn2 + logf(total) : -INFINITY;
 }
 
 template <typename T, int ND, int W>
@@ -188,7 +296,21 @@ hipError_t launch_prefill_w(const SoftmaxArgs& a, hipStream_t s) {
 }
 
 template <typename T, int ND>
+hipError_t launch_prefill_few(const SoftmaxArgs& a, hipStream_t s) {
+  constexpr int bytes = std::max(4 * PairTile<T, ND, 32>::kBytes, 1024 * ND * (int)sizeof(float4));
+  auto kern = softmax_prefill_few<T, ND>;
+  if (bytes > 64 * 1024 - 1024) {
+    hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != hipSuccess) return e;
+  }
+  const int blocks = (a.n + 31) / 32;
+  hipLaunchKernelGGL(kern, dim3((unsigned)head_blocks(a.heads * a.G, blocks)), dim3(256), bytes, s, a, blocks);
+  return hipGetLastError();
+}
+
+template <typename T, int ND>
 hipError_t launch_prefill(const SoftmaxArgs& a, hipStream_t s) {
+  if (few_sweeps<T, ND>((int64_t)a.heads * a.G, a.n)) return launch_prefill_few<T, ND>(a, s);
   if constexpr (sizeof(T) == 2)
     if ((int64_t)a.heads * a.G * ((a.n + 255) / 256) >= 256) return launch_prefill_w<T, ND, 8>(a, s);
   return launch_prefill_w<T, ND, 4>(a, s);

@@ -46,17 +46,26 @@ __device__ __forceinline__ float dot_own(const uint4 (&a)[2 * ND][PL], const uin
   return r;
 }
 
-// 32 x 32 products of the tile's rows r0 .. +31 with this wave's rows.
-template <typename L, int ND>
-__device__ __forceinline__ f32x16 dot_rows32(const u16* t, int r0, const uint4 (&own)[2 * ND][L::kPl]) {
-  f32x16 s = zero16();
-#pragma unroll
-  for (int i = 0; i < 2 * ND; ++i) {
-    uint4 f[L::kPl];
-    L::load_rows(t, r0, i, f);
-    s = dot_planes32(f, own[i], s);
+// A query tile's own keys row by row (see dot_row): `rows` of them from k and v on.
+template <typename T, int ND, int PL>
+__device__ __forceinline__ void masked_keys(const T* k, int dk, const T* v, int dv, int rows, float c, float lse,
+                                            float delta, const uint4 (&qf)[2 * ND][PL], const uint4 (&df)[2 * ND][PL],
+                                            f32x16 (&acc)[ND]) {
+  const int l31 = threadIdx.x & 31;
+#pragma unroll 1
+  for (int r = 0; r < rows; ++r) {
+    const float z = dot_row<T, ND>(qf, k + (int64_t)r * dk, dk);
+    const float d = dot_row<T, ND>(df, v + (int64_t)r * dv, dv);
+    if (r <= l31) add_row(k + (int64_t)r * dk, dk, exp2_fast(fmaf(z, c, -lse)) * (d - delta), acc);
   }
-  return s;
+}
+// Whether rows of q and dy hold a value that is not finite (for the whole wave).
+template <typename T>
+__device__ __forceinline__ bool rows_not_finite(const T* q, int dk, const T* dy, int dv, int rows) {
+  bool bad = false;
+  for (int i = threadIdx.x & 63; i < rows * dk; i += 64) bad |= !bf16_finite(entry_of(q, i));
+  for (int i = threadIdx.x & 63; i < rows * dv; i += 64) bad |= !bf16_finite(entry_of(dy, i));
+  return __ballot(bad) != 0;
 }
 
 template <typename T, int ND, int W>
@@ -130,13 +139,8 @@ __global__ void __launch_bounds__(64 * W, sizeof(T) == 2 ? 2 : 1) softmax_rows(S
     }
     settle_mfma32();
     if (__builtin_expect(odd, 0)) {
-#pragma unroll 1
-      for (int r = 0; r < min(32, len - q0); ++r) {
-        const int64_t key = (int64_t)kvh * n + q0 + r;
-        const float z = dot_row<T, ND>(qf, (const T*)a.k + key * dk, dk);
-        const float d = dot_row<T, ND>(df, (const T*)a.v + key * dv, dv);
-        if (r <= l31) add_row((const T*)a.k + key * dk, dk, exp2_fast(fmaf(z, c, -lse)) * (d - delta), acc);
-      }
+      const int64_t key = (int64_t)kvh * n + q0;
+      masked_keys<T, ND>((const T*)a.k + key * dk, dk, (const T*)a.v + key * dv, dv, min(32, len - q0), c, lse, delta, qf, df, acc);
     }
   }
   if (row < n) store_row32<T, ND>((T*)a.dq + at * dk, dk, acc, row < len ? a.scale : 0.f, row >= len);
@@ -275,10 +279,7 @@ __global__ void __launch_bounds__(64 * W, sizeof(T) == 2 ? 2 : 1) softmax_cols(S
         const int64_t t0 = ((int64_t)kvh * a.G + g) * n + k0;
         const T* const q = (const T*)a.q + t0 * dk;
         const T* const dy = (const T*)a.dy + t0 * dv;
-        uint32_t bad = 0;
-        for (int i = lane; i < rows * dk; i += 64) bad |= (uint32_t)!bf16_finite(entry_of(q, i));
-        for (int i = lane; i < rows * dv; i += 64) bad |= (uint32_t)!bf16_finite(entry_of(dy, i));
-        if (__ballot(bad != 0) == 0) continue;
+        if (!rows_not_finite(q, dk, dy, dv, rows)) continue;
 #pragma unroll 1
         for (int r = 0; r < rows; ++r) {
           const float p = exp2_fast(fmaf(dot_row<T, ND>(kf, q + r * dk, dk), c, -kLog2e * a.lse[t0 + r]));
@@ -294,45 +295,254 @@ __global__ void __launch_bounds__(64 * W, sizeof(T) == 2 ? 2 : 1) softmax_cols(S
   store_row32<T, ND>(for_k ? (T*)a.dk + at * dk : (T*)a.dv + at * dv, for_k ? dk : dv, acc, for_k ? a.scale : 1.f, row >= len);
 }
 
-// WR, WC: waves of a workgroup of the two kernels.
-template <typename T, int ND, int WR, int WC>
-hipError_t launch_backward_w(const SoftmaxGradArgs& a, hipStream_t s) {
-  using L = PairTile<T, ND, kStaged<T>>;
-  constexpr int rows_bytes = 4 * L::kBytes, 
-                cols_bytes = 2 * (2 * L::kBytes + 8 * kStaged<T>) + WC / 2 * kStaged<T> * 128;
-  static_assert(cols_bytes <= 160 * 1024, "LDS of one workgroup");
-  auto rows = softmax_rows<T, ND, WR>;
-  auto cols = softmax_cols<T, ND, WC>;
-  if (cols_bytes > 64 * 1024) {
-    hipError_t e = hipFuncSetAttribute((const void*)rows, hipFuncAttributeMaxDynamicSharedMemorySize, rows_bytes);
-    if (e == hipSuccess) e = hipFuncSetAttribute((const void*)cols, hipFuncAttributeMaxDynamicSharedMemorySize, cols_bytes);
+// The same sums for calls with few workgroups: one of four waves per 32 queries (keys), of
+// which a wave takes every fourth tile of keys (queries), through LDS of its own, so that no wave
+// waits for another one before the sums are joined.
+template <typename T, int ND>
+__global__ void __launch_bounds__(256, 1) softmax_rows_few(SoftmaxGradArgs a, int blocks) {
+  using L = PairTile<T, ND, 32>;
+  extern __shared__ __attribute__((aligned(16))) u16 smem16[];
+  const int tid = threadIdx.x, lane = tid & 63, l31 = lane & 31, h = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  int qh, blk;
+  if (!locate(a.heads * a.G, blocks, qh, blk)) return;
+  blk = blocks - 1 - blk;  // the longest first
+  const int kvh = qh / a.G, n = a.n, dk = a.dk_, dv = a.dv_;
+  const int len = tokens_of(a.lengths, kvh / a.H, n);
+  const int row = 32 * blk + l31;
+  const int64_t at = (int64_t)qh * n + row;
+  f32x16 acc[ND];
+#pragma unroll
+  for (int j = 0; j < ND; ++j) acc[j] = zero16();
+  if (32 * blk < len) {
+    u16* const tile = smem16 + wave * L::kElems;
+    TileStage<T, ND, 32, 64> sk, sv;
+    sk.init((const T*)a.k + (int64_t)kvh * n * dk, len, dk, lane);
+    sv.init((const T*)a.v + (int64_t)kvh * n * dv, len, dv, lane);
+    int t = wave;
+    if (t <= blk) sv.fetch(32 * t), sk.fetch(32 * t);
+    uint4 qf[2 * ND][L::kPl], df[2 * ND][L::kPl];
+    load_own32<T, ND>((const T*)a.y + at * dv, row < len, dv, qf);
+    load_own32<T, ND>((const T*)a.dy + at * dv, row < len, dv, df);
+    float delta = dot_own<ND>(qf, df);
+    delta += __shfl_xor(delta, 32);
+    if (row < len && h == 0 && wave == 0) a.delta[at] = delta;
+    load_own32<T, ND>((const T*)a.q + at * dk, row < len, dk, qf);
+    const float c = a.scale * kLog2e, lse = row < len ? a.lse[at] * kLog2e : 0.f;
+    bool odd = false;  // whether the own tile holds values that are not finite
+    for (; t <= blk; t += 4) {
+      wave_lds_fence();
+      sv.put(tile, 32 * t);
+      wave_lds_fence();
+      if (t + 4 <= blk) sv.fetch(32 * (t + 4));
+      const f32x16 d = dot_rows32<L, ND>(tile, 0, df);
+      wave_lds_fence();
+      sk.put(tile, 32 * t);
+      wave_lds_fence();
+      if (t + 4 <= blk) sk.fetch(32 * (t + 4));
+      const f32x16 s = dot_rows32<L, ND>(tile, 0, qf);
+      float e[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) e[i] = exp2_fast(fmaf(s[i], c, -lse)) * (d[i] - delta);
+      if (t == blk) {
+        stay_in_branch();
+#pragma unroll
+        for (int i = 0; i < 16; ++i) e[i] = result_row(i, h) > l31 ? 0.f : e[i];
+        odd = tile_not_finite<L, ND>(tile, 0);
+        if (odd) break;
+      }
+      uint4 w[2][L::kPl];
+      to_planes<L::kPl>(e, w);
+      contract32<L, ND>(tile, 0, w, acc);
+    }
+    settle_mfma32();
+    if (__builtin_expect(odd, 0)) {
+      const int64_t key = (int64_t)kvh * n + 32 * blk;
+      masked_keys<T, ND>((const T*)a.k + key * dk, dk, (const T*)a.v + key * dv, dv, min(32, len - 32 * blk), c, lse, delta,
+                         qf, df, acc);
+    }
+  }
+  float x[ND][4];
+  join_waves<ND>(acc, (float4*)smem16, x);
+  if (row < n) store_joined<T, ND>((T*)a.dq + at * dk, dk, x, row < len ? a.scale : 0.f, row >= len);
+}
+
+template <typename T, int ND>
+__global__ void __launch_bounds__(256, 1) softmax_cols_few(SoftmaxGradArgs a, int blocks) {
+  using L = PairTile<T, ND, 32>;
+  extern __shared__ __attribute__((aligned(16))) u16 smem16[];
+  __shared__ float stats[4][64];  // a wave's queries' lse, then delta
+  const int tid = threadIdx.x, lane = tid & 63, l31 = lane & 31, h = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  int kvh, blk;
+  if (!locate(a.heads, blocks, kvh, blk)) return;  // (the first keys have the longest sweeps)
+  const int n = a.n, dk = a.dk_, dv = a.dv_;
+  const int len = tokens_of(a.lengths, kvh / a.H, n);
+  const int row = 32 * blk + l31;
+  const int64_t at = (int64_t)kvh * n + row;
+  f32x16 sum_v[ND], sum_k[ND];
+#pragma unroll
+  for (int j = 0; j < ND; ++j) sum_v[j] = sum_k[j] = zero16();
+  if (32 * blk < len) {
+    u16* const qt = smem16 + wave * 2 * L::kElems;
+    u16* const yt = qt + L::kElems;
+    // units of work: the members' tiles from this one on
+    const int tiles = (len + 31) / 32 - blk, units = tiles * a.G;
+    TileStage<T, ND, 32, 64> sq, sy;
+    float stat = 0.f;
+    int t0 = 0;
+    auto fetch = [&](int u) {
+      const int g = u / tiles;
+      t0 = 32 * (blk + u - g * tiles);
+      const int64_t base = ((int64_t)kvh * a.G + g) * n;
+      sq.init((const T*)a.q + base * dk, len, dk, lane);
+      sy.init((const T*)a.dy + base * dv, len, dv, lane);
+      sq.fetch(t0);
+      sy.fetch(t0);
+      const int t = t0 + l31;
+      // (a row behind the sequence: probability zero)
+      if (h == 0) stat = t < len ? a.lse[base + t] * kLog2e : INFINITY;
+      else stat = t < len ? a.delta[base + t] : 0.f;
+    };
+    int u = wave;
+    if (u < units) fetch(u);
+    uint4 kf[2 * ND][L::kPl], vf[2 * ND][L::kPl];
+    load_own32<T, ND>((const T*)a.k + at * dk, row < len, dk, kf);
+    load_own32<T, ND>((const T*)a.v + at * dv, row < len, dv, vf);
+    const float c = a.scale * kLog2e;
+    bool odd = false;  // whether own tiles hold values that are not finite: such a member's is left out
+    for (; u < units; u += 4) {
+      const bool own = u % tiles == 0;
+      wave_lds_fence();
+      sq.put(qt, t0);
+      sy.put(yt, t0);
+      stats[wave][lane] = stat;
+      wave_lds_fence();
+      if (u + 4 < units) fetch(u + 4);
+      const f32x16 s = dot_rows32<L, ND>(qt, 0, kf), d = dot_rows32<L, ND>(yt, 0, vf);
+      float p[16], e[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        p[i] = exp2_fast(fmaf(s[i], c, -stats[wave][result_row(i, h)]));
+        e[i] = p[i] * (d[i] - stats[wave][32 + result_row(i, h)]);
+      }
+      if (own) {
+        stay_in_branch();
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          p[i] = result_row(i, h) < l31 ? 0.f : p[i];
+          e[i] = result_row(i, h) < l31 ? 0.f : e[i];
+        }
+        if (tile_not_finite<L, ND>(qt, 0) || tile_not_finite<L, ND>(yt, 0)) {
+          odd = true;
+          continue;
+        }
+      }
+      uint4 w[2][L::kPl];
+      to_planes<L::kPl>(p, w);
+      contract32<L, ND>(yt, 0, w, sum_v);
+      to_planes<L::kPl>(e, w);
+      contract32<L, ND>(qt, 0, w, sum_k);
+    }
+    settle_mfma32();
+    if (__builtin_expect(odd, 0)) {
+      const int rows = min(32, len - 32 * blk);
+#pragma unroll 1
+      for (int g = 0; g < a.G; ++g) {
+        const int64_t t0 = ((int64_t)kvh * a.G + g) * n + 32 * blk;
+        const T* const q = (const T*)a.q + t0 * dk;
+        const T* const dy = (const T*)a.dy + t0 * dv;
+        if (g * tiles % 4 != wave || !rows_not_finite(q, dk, dy, dv, rows)) continue;
+#pragma unroll 1
+        for (int r = 0; r < rows; ++r) {
+          const float p = exp2_fast(fmaf(dot_row<T, ND>(kf, q + r * dk, dk), c, -kLog2e * a.lse[t0 + r]));
+          const float e = p * (dot_row<T, ND>(vf, dy + r * dv, dv) - a.delta[t0 + r]);
+          if (r < l31) continue;
+          add_row(q + r * dk, dk, e, sum_k);
+          add_row(dy + r * dv, dv, p, sum_v);
+        }
+      }
+    }
+  }
+  float x[ND][4];
+  join_waves<ND>(sum_k, (float4*)smem16, x);
+  if (row < n) store_joined<T, ND>((T*)a.dk + at * dk, dk, x, a.scale, row >= len);
+  join_waves<ND>(sum_v, (float4*)smem16, x);
+  if (row < n) store_joined<T, ND>((T*)a.dv + at * dv, dv, x, 1.f, row >= len);
+}
+
+template <typename T, int ND>
+hipError_t launch_rows_few(const SoftmaxGradArgs& a, hipStream_t s) {
+  constexpr int bytes = std::max(4 * PairTile<T, ND, 32>::kBytes, 1024 * ND * (int)sizeof(float4));
+  auto kern = softmax_rows_few<T, ND>;
+  if (bytes > 64 * 1024) {
+    hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != hipSuccess) return e;
   }
-  const int row_blocks = (a.n + 32 * WR - 1) / (32 * WR);
-  hipLaunchKernelGGL(rows, dim3((unsigned)head_blocks(a.heads * a.G, row_blocks)), dim3(64 * WR), rows_bytes, s, a,
-                     row_blocks);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  constexpr int keys = 16 * WC;
-  const int col_blocks = (a.n + keys - 1) / keys;
-  hipLaunchKernelGGL(cols, dim3((unsigned)head_blocks(a.heads, col_blocks)), dim3(64 * WC), cols_bytes, s, a, col_blocks);
+  const int blocks = (a.n + 31) / 32;
+  hipLaunchKernelGGL(kern, dim3((unsigned)head_blocks(a.heads * a.G, blocks)), dim3(256), bytes, s, a, blocks);
   return hipGetLastError();
 }
 
-template <int ND>
-hipError_t launch_backward(const SoftmaxGradArgs& a, bool bf16, hipStream_t s) {
-  if (!bf16) return launch_backward_w<float, ND, 4, 4>(a, s);
-  return launch_backward_w<u16, ND, ND >= 3 ? 8 : 4, 8>(a, s);
+template <typename T, int ND>
+hipError_t launch_cols_few(const SoftmaxGradArgs& a, hipStream_t s) {
+  constexpr int bytes = std::max(8 * PairTile<T, ND, 32>::kBytes, 1024 * ND * (int)sizeof(float4));
+  static_assert(bytes <= 159 * 1024, "LDS of one workgroup");
+  auto kern = softmax_cols_few<T, ND>;
+  if (bytes > 63 * 1024) {
+    hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != hipSuccess) return e;
+  }
+  const int blocks = (a.n + 31) / 32;
+  hipLaunchKernelGGL(kern, dim3((unsigned)head_blocks(a.heads, blocks)), dim3(256), bytes, s, a, blocks);
+  return hipGetLastError();
+}
+
+template <typename T, int ND, int W>
+hipError_t launch_rows(const SoftmaxGradArgs& a, hipStream_t s) {
+  constexpr int bytes = 4 * PairTile<T, ND, kStaged<T>>::kBytes;
+  auto kern = softmax_rows<T, ND, W>;
+  if (bytes > 64 * 1024) {
+    hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != hipSuccess) return e;
+  }
+  const int blocks = (a.n + 32 * W - 1) / (32 * W);
+  hipLaunchKernelGGL(kern, dim3((unsigned)head_blocks(a.heads * a.G, blocks)), dim3(64 * W), bytes, s, a, blocks);
+  return hipGetLastError();
+}
+
+template <typename T, int ND, int W>
+hipError_t launch_cols(const SoftmaxGradArgs& a, hipStream_t s) {
+  constexpr int bytes = 2 * (2 * PairTile<T, ND, kStaged<T>>::kBytes + 8 * kStaged<T>) + W / 2 * kStaged<T> * 128;
+  static_assert(bytes <= 160 * 1024, "LDS of one workgroup");
+  auto kern = softmax_cols<T, ND, W>;
+  if (bytes > 64 * 1024) {
+    hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != hipSuccess) return e;
+  }
+  const int blocks = (a.n + 16 * W - 1) / (16 * W);
+  hipLaunchKernelGGL(kern, dim3((unsigned)head_blocks(a.heads, blocks)), dim3(64 * W), bytes, s, a, blocks);
+  return hipGetLastError();
+}
+
+template <typename T, int ND>
+hipError_t launch_backward(const SoftmaxGradArgs& a, hipStream_t s) {
+  constexpr bool bf16 = sizeof(T) == 2;
+  hipError_t e = few_sweeps<T, ND>((int64_t)a.heads * a.G, a.n) ? launch_rows_few<T, ND>(a, s) : launch_rows<T, ND, bf16 && ND >= 3 ? 8 : 4>(a, s);
+  if (e != hipSuccess) return e;
+  if constexpr (bf16 || ND <= 2)  // (four waves' tiles of two wide float32 tensors, 192 KB, are more than the LDS)
+    if (few_sweeps<T, ND>(a.heads, a.n)) return launch_cols_few<T, ND>(a, s);
+  return launch_cols<T, ND, bf16 ? 8 : 4>(a, s);
 }
 
 }  // namespace
 
 hipError_t launch_softmax_backward(const SoftmaxGradArgs& a, bool bf16, hipStream_t s) {
   switch ((std::max(a.dk_, a.dv_) + 31) / 32) {
-    case 1: return launch_backward<1>(a, bf16, s);
-    case 2: return launch_backward<2>(a, bf16, s);
-    case 3: return launch_backward<3>(a, bf16, s);
-    default: return launch_backward<4>(a, bf16, s);
+    case 1: return bf16 ? launch_backward<u16, 1>(a, s) : launch_backward<float, 1>(a, s);
+    case 2: return bf16 ? launch_backward<u16, 2>(a, s) : launch_backward<float, 2>(a, s);
+    case 3: return bf16 ? launch_backward<u16, 3>(a, s) : launch_backward<float, 3>(a, s);
+    default: return bf16 ? launch_backward<u16, 4>(a, s) : launch_backward<float, 4>(a, s);
   }
 }
 

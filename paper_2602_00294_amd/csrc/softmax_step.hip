@@ -27,12 +27,6 @@ namespace {
 
 constexpr int kStepWaves = 4;
 
-// A wave's own stores to LDS before its lanes' loads.
-__device__ __forceinline__ void wave_lds_fence() {
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-}
-
 // What a stretch (or a wave) leaves for a query head: the sums times 2^-top, scores in units of log 2.
 struct StepState {
   float top, sum;
@@ -123,13 +117,7 @@ __device__ __forceinline__ void step_stretch_rows(const SoftmaxStepArgs& a, int6
   for (; r0 < end; r0 += kStep) {
     stage(sk, r0, kn, dk);
     if (r0 + kStep < end) sk.template fetch<true>(r0 + kStep);
-    f32x16 s = zero16();
-#pragma unroll
-    for (int i = 0; i < 2 * ND; ++i) {
-      uint4 f[L::kPl];
-      L::load_rows(tile, 0, i, f);
-      s = dot_planes32(f, qf[i], s);
-    }
+    f32x16 s = dot_rows32<L, ND>(tile, 0, qf);
     float most = -INFINITY;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {

@@ -94,6 +94,14 @@ MANY_HEADS = [  # B, H, G, n, dk, dv, dtype, lengths
     (2, 16, 4, 513, 16, 128, "bf16", [513, 400]),
     (3, 30, 3, 33, 64, 64, "bf16", [33, 0, 32]),
     (4, 16, 4, 65, 96, 80, "f32", [65, 64, 1, 33]),
+    (5, 30, 1, 200, 24, 32, "f32", None),
+    (5, 30, 1, 200, 64, 40, "f32", [200, 130, 1, 0, 150]),
+    (5, 30, 1, 161, 96, 96, "f32", [161, 96, 97, 64, 31]),
+    (5, 30, 1, 160, 128, 100, "f32", None),
+    (5, 30, 1, 130, 33, 31, "bf16", [130, 129, 128, 127, -4]),
+    (5, 30, 1, 200, 64, 40, "bf16", [64, 200, 193, 32, 192]),
+    (5, 30, 1, 290, 96, 72, "bf16", [289, 290, 1, 256, 225]),
+    (2, 80, 2, 257, 128, 128, "bf16", None),
 ]
 
 
@@ -181,14 +189,15 @@ def test_prompt_then_tokens(sata, dtype):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("bad", [math.nan, math.inf])
-def test_values_that_are_not_finite(sata, dtype, bad):
+@pytest.mark.parametrize("H,G", [(2, 2), (70, 1)])
+def test_values_that_are_not_finite(sata, dtype, bad, H, G):
     """Padding rows may hold anything; a token's values reach later rows only, its query and gradient earlier keys
     only.  What does not depend on the value is the same in bits in other heads, sequences and rows further off;
     in the value's own 32 rows the pairs are summed in another way, so that both ways are held to the bound of the
     exact result."""
     n, ends, at = 200, [150, 200], 100
-    _say("softmax, not finite", dtype, bad)
-    q, k, v, dy = _prompt(6, 2, 2, 2, n, 40, 24, dtype)
+    _say("softmax, not finite", dtype, bad, H, G)
+    q, k, v, dy = _prompt(6, 2, H, G, n, 40, 24, dtype)
     lens = _lengths(ends)
     y, lse = sata.softmax_prefill(q, k, v, lens)
     grads = sata.softmax_backward(q, k, v, y, lse, dy, lens)
@@ -213,17 +222,19 @@ def test_values_that_are_not_finite(sata, dtype, bad):
         args = [t.clone() for t in (q, k, v)]
         args[x][1, 1, at, 3] = bad
         y2, lse2 = sata.softmax_prefill(*args, lens)
-        assert torch.equal(y2[0], y[0]) and torch.equal(y2[1, :2], y[1, :2])
+        assert torch.equal(y2[0], y[0]) and torch.equal(y2[1, :G], y[1, :G])
         dq = sata.softmax_backward(*args, y2, lse2, dy, lens)[0]
-        assert torch.equal(dq[0], grads[0][0]) and torch.equal(dq[1, :2], grads[0][1, :2])
-        for head in (2, 3):
+        assert torch.equal(dq[0], grads[0][0]) and torch.equal(dq[1, :G], grads[0][1, :G])
+        for head in range(G, 2 * G):
             same(y2, y, exact[0], head, slice(0, at), range(tile, at))
             same(lse2, lse, exact[1], head, slice(0, at), range(tile, at))
             same(dq, grads[0], exact_grads[0], head, slice(0, at), range(tile, at))
-        assert not torch.isfinite(y2[1, 2:, at]).all()
+        for head in range(G, 2 * G):  # (a key with +inf where the query is below 0: score -inf, exp(-inf) = 0, no weight)
+            if x == 2 or math.isnan(bad) or q[1, head, at, 3] > 0:
+                assert not torch.isfinite(y2[1, head, at]).all()
     args = [t.clone() for t in (q, dy)]
-    args[0][1, 3, at, 0] = bad
-    args[1][1, 3, at, 0] = bad
+    args[0][1, 2 * G - 1, at, 0] = bad
+    args[1][1, 2 * G - 1, at, 0] = bad
     y2, lse2 = sata.softmax_prefill(args[0], k, v, lens)
     keep = torch.arange(n, device="cuda") != at
     assert torch.equal(y2[:, :, keep], y[:, :, keep]) and torch.equal(lse2[:, :, keep], lse[:, :, keep])
