@@ -20,17 +20,22 @@ namespace sata {
 namespace {
 
 // A workgroup of ND waves takes a part of one head's tokens, in chunks of 32: wave j has the
-// state's (and the output's) columns 32 j .. +31 in registers, one in each lane pair.  With r a row of a chunk of m tokens and R the state before it (forward)
+// state's (and the output's) columns 32 j .. +31 in registers, one in each lane pair.  With r a row
+// of a chunk of m tokens and R the state before it (forward)
 //     out_r = readout lam^(r+1) a_r R + sum_{s<=r} update readout lam^(r-s) (a_r.b_s) w_s
 //     R     = lam^m R + sum_s update lam^(m-1-s) b_s (x) w_s
 // and in reverse the same with lam^(m-1-r), lam^(s-r) and lam^(s+1).
 //
-// Bound: memory (a, b, w read and out written once), where there are heads enough; per
-// chunk and wave 8 + 4 + 8 + 24 matrix instructions at d = 128 in bfloat16 and about 320 vector instructions.
+// Bound: memory (a, b, w read and out written once) is the floor; what it runs at is the chain of a chunk, in
+// a wave 8 + 8 + 4 + 24 matrix instructions at d = 128 in bfloat16, some 360 vector instructions
+// and two barriers, with two waves a SIMD.  B = 8, H = 16, n = 8192, d = 128 in bfloat16: 438 us
+// (2.45 TB/s of 4.9), a third of it the sums; gradients of B = 8, H = 32, n = 2048, d = 64: 192 us
+// (2.4 TB/s).  Short prompts and few heads: a part's chunks one after the other, and the launches of the
+// sums and the carry.
 //
 // The state lies in units of f = lam^(tokens since ...): lam^m goes into f, which enters the readout's
 // factor and, inverted, the update's; only when f falls below 2^-8 are all entries
-// multiplied (with an entry's product at every chunk: 128 vector instructions more of 740).
+// multiplied (not 16 ND products at every chunk).
 //
 // Precision: bfloat16 inputs are exact operands.  The pairs' weights inside a chunk are carried as two
 // bfloat16 numbers; the state's entries are rounded to one for the readout (as every term of the

@@ -403,7 +403,7 @@ __device__ __forceinline__ void store_row32(T* p, int width, const f32x16 (&acc)
     }
 }
 
-// The sums of WAVES = 4 waves with the same rows, in the waves' order: x[j] has columns 32 j + 8 wave + 4 h
+// The sums of a workgroup's four waves with the same rows, in the waves' order: x[j] has columns 32 j + 8 wave + 4 h
 // .. +3 of this lane's row.  buf: 1024 ND float4 of LDS that no wave reads any more when all
 // have come here.
 template <int ND>

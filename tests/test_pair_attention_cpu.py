@@ -196,10 +196,10 @@ def test_pointers_refused(lib):
 def test_scratch(lib):
     F, N = FAKE, NULL
     odd = ctypes.c_void_p(0x1008)
-    # long heads and few of them work in parts or stretches, whose sums need room
+    # long heads and few of them work in parts, and long caches in stretches, whose sums need room
     assert lib.sata_decay_scratch(1, 2, 1, 4096, 64, 32) > 0 and lib.sata_decay_scratch(64, 64, 1, 4096, 64, 32) == 0
     assert lib.sata_softmax_backward_scratch(2, 3, 4, 5) == 4 * 2 * 3 * 4 * 5
-    assert lib.sata_softmax_step_scratch(1, 2, 4, 8192, 64) > 0 and lib.sata_softmax_step_scratch(64, 64, 1, 8192, 64) == 0
+    assert lib.sata_softmax_step_scratch(1, 2, 4, 8192, 64) > 0 and lib.sata_softmax_step_scratch(64, 64, 1, 256, 64) == 0
     for bad in ((0, 1, 1, 1, 1, 1), (1, 1, 1, -1, 1, 1), (1, 1, 1, 1, 129, 1), (1, 65536, 1, 1, 1, 1), (1, 1, 0, 1, 1, 1)):
         assert lib.sata_decay_scratch(*bad) == -1
     assert lib.sata_softmax_backward_scratch(1, 1, 0, 5) == -1
