@@ -255,8 +255,8 @@ struct SoftmaxGradArgs {
 hipError_t launch_softmax_backward(const SoftmaxGradArgs& a, bool bf16, hipStream_t s);
 
 // The heads' caches in stretches of `least` units or more, at most `workgroups` of them, for a card that
-// holds `places` at a time; a group's heads in blocks of 32.  The sums of heads of several stretches lie in
-// `bytes` bytes of scratch.
+// holds `places` at a time; a group's heads in blocks of 32.  Where a head's stretches are found and the sums of heads of
+// several lie in `bytes` bytes of scratch.
 struct SoftmaxStepPlan {
   int unit = 128, least = 2, places = 0, workgroups = 0, blocks = 1;
   size_t bytes = 0;

@@ -9,7 +9,7 @@
 // W-th tile of 32 rows of a stretch and has the next tile on its way while it works, so no
 // wave waits for another one before the end, where the waves' sums are joined (and those of
 // a head of several stretches by a second kernel).
-// 128 heads of d = 128 in groups of four, sequences of 1 to 8192 rows (286 MB): 59 us (4.84 TB/s; a
+// 128 heads of d = 128 in groups of four, sequences of 1 to 8192 rows (286 MB): 57 us (4.99 TB/s; a
 // copy of 4 GB 4.9), 78 with stretches of one length for all calls and plain loads; the same
 // with all caches full (537 MB) 91 us (5.92 TB/s), 104; all a quarter full 31 us, 62; one
 // sequence of 131072 rows 117 us, 159.  Loads are streamed: with plain ones 70 us for the first.
@@ -216,31 +216,37 @@ softmax_step_kernel(SoftmaxStepArgs a, SoftmaxStepPlan p) {
   // (a head's stretches lie next to each other)
   const int hb = rest / count, stretch = rest - hb * count, head = hb / p.blocks;
   const int at = a.lengths[b], first = stretch * len * p.unit;
+  const int64_t place = ((int64_t)b * a.H + head) * p.blocks + hb - head * p.blocks;
+  int2* const found = (int2*)a.scratch;
+  float* const sums = (float*)(found + (int64_t)a.heads * p.blocks);
+  if (p.bytes && stretch == 0 && threadIdx.x == 0) found[place] = int2{id, count};
   step_stretch_rows<T, ND>(a, (int64_t)b * a.H + head, hb - head * p.blocks, at, first, min(at + 1, first + len * p.unit),
-                           count == 1 ? nullptr : a.scratch + (int64_t)id * min(32, a.G) * (a.dv_ + 2), smem16, state);
+                           count == 1 ? nullptr : sums + (int64_t)id * min(32, a.G) * (a.dv_ + 2), smem16, state);
 }
 
-// The sums of one query head's stretches joined, in their order; one thread per column.
+// The sums of one query head's stretches joined, in their order; one thread per column.  (Each wave has all
+// tops at once and four stretches' sums on their way: 512 query heads of up to 12
+// stretches 4.6 us, where each block counting stretches and loading one sum after the other took 7.6.)
 template <typename T>
 __global__ void __launch_bounds__(kMaxPairDim) softmax_join_kernel(SoftmaxStepArgs a, SoftmaxStepPlan p) {
-  const int qh = blockIdx.x, kvh = qh / a.G, member = qh - kvh * a.G, seq = kvh / a.H;
-  const int dv = a.dv_, col = threadIdx.x, lane = col & 63, heads_of = a.H * p.blocks;
-  const int len = step_stretch(a, p, lane), count = (step_units(a, p, seq) + len - 1) / len;
-  if (count == 1) return;
-  int before = 0;
-  for (int b = lane; b < seq; b += 64) before += (step_units(a, p, b) + len - 1) / len;
-  const int id = wave_total(before) * heads_of + ((kvh - seq * a.H) * p.blocks + member / 32) * count;
-  if (col >= dv) return;
+  const int qh = blockIdx.x, kvh = qh / a.G, member = qh - kvh * a.G;
+  const int dv = a.dv_, col = threadIdx.x, lane = col & 63;
+  const int2* const found = (const int2*)a.scratch;
+  const int2 first = found[(int64_t)kvh * p.blocks + member / 32];  // its first stretch, and how many there are
+  if (first.y == 1) return;
   const int64_t pitch = (int64_t)min(32, a.G) * (dv + 2);
-  const float* const sums = a.scratch + id * pitch + (member % 32) * (dv + 2);
+  const float* const in = (const float*)(found + (int64_t)a.heads * p.blocks) + first.x * pitch + (member % 32) * (dv + 2);
   float most = -3.4028234e38f;
-  for (int w = 0; w < count; ++w) most = fmaxf(most, sums[w * pitch + dv]);
+  for (int w = lane; w < first.y; w += 64) most = fmaxf(most, in[w * pitch + dv]);
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
+  if (col >= dv) return;
   float x = 0.f, l = 0.f;
-  for (int w = 0; w < count; ++w) {
-    const float* const in = sums + w * pitch;
-    const float k = exp2_fast(in[dv] - most);
-    x = fmaf(in[col], k, x);
-    l = fmaf(in[dv + 1], k, l);
+#pragma unroll 4
+  for (int w = 0; w < first.y; ++w) {
+    const float k = exp2_fast(in[w * pitch + dv] - most);
+    x = fmaf(in[w * pitch + col], k, x);
+    l = fmaf(in[w * pitch + dv + 1], k, l);
   }
   ((T*)a.y)[(int64_t)qh * dv + col] = rounded<T>(x / l);
 }
@@ -271,7 +277,9 @@ SoftmaxStepPlan plan_softmax_step(bool bf16, int heads, int G, int capacity, int
   p.places = bf16 ? 512 : 256;
   const int64_t most = (int64_t)count * (((capacity + p.unit - 1) / p.unit + p.least - 1) / p.least);
   p.workgroups = (int)std::min<int64_t>(std::max(p.places, count) + count, most);
-  p.bytes = p.workgroups > count ? sizeof(float) * (size_t)p.workgroups * std::min(32, G) * (dv + 2) : 0;
+  p.bytes = p.workgroups > count
+                ? sizeof(int2) * (size_t)count + sizeof(float) * (size_t)p.workgroups * std::min(32, G) * (dv + 2)
+                : 0;
   return p;
 }
 
