@@ -356,7 +356,9 @@ sata_status sata_softmax_backward(const void* q, const void* k, const void* v, c
  *            its cache is left as it is and its y is zero.
  *   q: [B][H_kv*G][d_k], k: [B][H_kv][d_k], v: [B][H_kv][d_v], y: [B][H_kv*G][d_v]
  * Rows behind lengths[b] are not used, whatever they hold.  The cache after a
- * prompt is its k and v, in tensors of `capacity` rows; capacity <= 2^21. */
+ * prompt is its k and v, in tensors of `capacity` rows; capacity <= 2^21.  Where
+ * a sequence's sums are cut depends on all lengths: the same call gives the same
+ * bits, but a sequence's last bits may change with the others' lengths. */
 sata_status sata_softmax_step(void* K, void* V, int capacity, const int32_t* lengths, const void* q, const void* k,
                               const void* v, sata_dtype dt, int B, int H_kv, int G, int d_k, int d_v, void* y,
                               void* scratch, void* stream);

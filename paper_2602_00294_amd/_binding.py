@@ -610,7 +610,8 @@ def softmax_step(K, V, lengths, q, k, v, y=None):
     """One token of every sequence over a cache K [B, H_kv, capacity, d_k], V [B, H_kv, capacity, d_v]: writes k and
     v as row lengths[b], then attends over rows 0..lengths[b].  lengths: [B] int32, the tokens in the cache before
     the call; it is not changed.  A sequence whose length is negative or not below the capacity is idle (its cache
-    stays, its y is zero).  q: [B, H_q, d_k]; k: [B, H_kv, d_k]; v: [B, H_kv, d_v].  Returns y [B, H_q, d_v]."""
+    stays, its y is zero).  q: [B, H_q, d_k]; k: [B, H_kv, d_k]; v: [B, H_kv, d_v].  Returns y [B, H_q, d_v], whose
+    last bits may change with the other sequences' lengths (the sums are cut by all of them)."""
     torch = _torch()
     code, B, H, G, dk, dv = _token_sizes(q, k, v)
     _check_same_dtype(q, K=K, V=V)
