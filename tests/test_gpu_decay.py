@@ -257,3 +257,29 @@ def test_captured(sata):
         want = work(held, torch.zeros_like(S))
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out, want))
+
+
+def test_offsets_past_32_bits(sata):
+    """Tensors of more than 2^31 entries: the last head's rows lie behind them."""
+    H, n, d, end = 17, 1 << 20, 128, 70
+    _say("decay, offsets past 32 bits")
+    gen = torch.Generator().manual_seed(13)
+    small = [torch.randn(1, 1, end, d, generator=gen).bfloat16().cuda() for _ in range(4)]
+    big = [torch.zeros(1, H, n, d, dtype=torch.bfloat16, device="cuda") for _ in range(4)]
+    assert big[0].numel() > 2 ** 31
+    for x, part in zip(big, small):
+        x[:, -1:, :end] = part
+    g, lens = torch.full((H,), -0.02, device="cuda"), torch.tensor([end], dtype=torch.int32, device="cuda")
+    q, k, v, dy = big
+    y, S = sata.decay_prefill(q, k, v, g, lens)
+    torch.cuda.synchronize()
+    ry, rS = pair_ref.decay_prefill(*small[:3], g[:1])
+    pair_ref.check(y[:, -1:, :end], ry, "y")
+    pair_ref.check(S[:, -1:], rS, "S")
+    assert not y[:, -1, end:].any()
+    del y
+    grads = sata.decay_backward(q, k, v, g, dy, lens)[:3]
+    torch.cuda.synchronize()
+    for name, a, w in zip(("dq", "dk", "dv"), grads, pair_ref.decay_backward(*small[:3], g[:1], small[3])):
+        pair_ref.check(a[:, -1:, :end], w, name)
+        assert not a[:, -1, end:].any()

@@ -300,3 +300,36 @@ def test_captured(sata):
         want = work(held, torch.zeros_like(K), torch.zeros_like(V), before)
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out, want))
+
+
+def test_offsets_past_32_bits(sata):
+    """Tensors of more than 2^31 entries: the last head's rows lie behind them."""
+    H, n, d, end = 17, 1 << 20, 128, 70
+    _say("softmax, offsets past 32 bits")
+    last = _prompt(12, 1, 1, 1, end + 1, d, d, "bf16")
+    q, k, v, dy = (torch.zeros(1, H, n, d, dtype=torch.bfloat16, device="cuda") for _ in range(4))
+    assert q.numel() > 2 ** 31
+    for x, part in zip((q, k, v, dy), last):
+        x[:, -1:, :end] = part[:, :, :end]
+    lens = _lengths([end])
+    tokens = [x[:, :, end].contiguous().expand(1, H, d).contiguous() for x in last[:3]]
+    ry, rK, rV = pair_ref.softmax_step(k[:, -1:, :end + 2].clone(), v[:, -1:, :end + 2].clone(), [end], *(x[:, -1:] for x in tokens))
+    small = [x[:, -1:, :end].contiguous() for x in (q, k, v, dy)]
+    y, lse = sata.softmax_prefill(q, k, v, lens)
+    torch.cuda.synchronize()
+    ref_y, ref_lse = pair_ref.softmax_prefill(*small[:3])
+    pair_ref.check(y[:, -1:, :end], ref_y, "y")
+    pair_ref.check(lse[:, -1:, :end], ref_lse, "lse")
+    assert not y[:, -1, end:].any()
+    grads = sata.softmax_backward(q, k, v, y, lse, dy, lens)
+    torch.cuda.synchronize()
+    want = pair_ref.softmax_backward(*small[:3], y[:, -1:, :end].contiguous(), lse[:, -1:, :end].contiguous(), small[3])
+    for name, a, w in zip(("dq", "dk", "dv"), grads, want):
+        pair_ref.check(a[:, -1:, :end], w, name)
+        assert not a[:, -1, end:].any()
+    del grads, y
+    got = sata.softmax_step(k, v, lens, *tokens)
+    torch.cuda.synchronize()
+    pair_ref.check(got[:, -1:], ry, "token")
+    assert torch.equal(k[:, -1:, :end + 2].cpu(), rK) and torch.equal(v[:, -1:, :end + 2].cpu(), rV)
+    assert not k[:, -1, end + 2:].any()
