@@ -255,13 +255,14 @@ struct SoftmaxGradArgs {
 hipError_t launch_softmax_backward(const SoftmaxGradArgs& a, bool bf16, hipStream_t s);
 
 // The heads' caches in stretches of `least` units or more, at most `workgroups` of them, for a card that
-// holds `places` at a time; a group's heads in blocks of 32.  Where a head's stretches are found and the sums of heads of
-// several lie in `bytes` bytes of scratch.
+// holds `places` at a time; a group's heads in blocks of 32.  Where `fixed`, each head has that many
+// stretches of fixed_len units (those behind its rows stay without work).  Where a head's stretches are
+// found and the sums of heads of several lie in `bytes` bytes of scratch.
 struct SoftmaxStepPlan {
-  int unit = 128, least = 2, places = 0, workgroups = 0, blocks = 1;
+  int unit = 128, least = 2, places = 0, workgroups = 0, blocks = 1, fixed = 0, fixed_len = 0;
   size_t bytes = 0;
 };
-SoftmaxStepPlan plan_softmax_step(bool bf16, int heads, int G, int capacity, int dv);
+SoftmaxStepPlan plan_softmax_step(bool bf16, int heads, int H, int G, int capacity, int dv);
 struct SoftmaxStepArgs {
   void *K, *V;         // [heads][capacity][d]
   const int* lengths;  // [heads / H]

@@ -974,8 +974,8 @@ int64_t sata_softmax_backward_scratch(int B, int H_kv, int G, int n) {
 
 int64_t sata_softmax_step_scratch(int B, int H_kv, int G, int capacity, int d_v) {
   if (check_pair_args(SATA_F32, B, H_kv, G, capacity, 1, d_v) != SATA_OK || capacity < 1) return -1;
-  // (bfloat16's workgroups are the more)
-  return (int64_t)sata::plan_softmax_step(true, B * H_kv, G, capacity, d_v).bytes;
+  return (int64_t)std::max(sata::plan_softmax_step(true, B * H_kv, H_kv, G, capacity, d_v).bytes,
+                           sata::plan_softmax_step(false, B * H_kv, H_kv, G, capacity, d_v).bytes);
 }
 
 sata_status sata_decay_prefill(const void* q, const void* k, const void* v, const float* log_decay, sata_dtype dt, int B,
@@ -1083,7 +1083,7 @@ sata_status sata_softmax_step(void* K, void* V, int capacity, const int32_t* len
   if (st != SATA_OK) return st;
   if (capacity < 1) return fail(SATA_ERR_INVALID_ARG, "capacity=%d must be >= 1", capacity);
   if (!K || !V || !lengths || !q || !k || !v || !y) return fail(SATA_ERR_INVALID_ARG, "null tensor pointer");
-  if ((st = check_scratch(scratch, sata::plan_softmax_step(dt == SATA_BF16, B * H_kv, G, capacity, d_v).bytes)) != SATA_OK) return st;
+  if ((st = check_scratch(scratch, sata::plan_softmax_step(dt == SATA_BF16, B * H_kv, H_kv, G, capacity, d_v).bytes)) != SATA_OK) return st;
   const sata::SoftmaxStepArgs a{K, V, lengths, q, k, v, y, (float*)scratch, B * H_kv, H_kv, G, capacity, d_k, d_v,
                                 pair_scale(d_k)};
   hipError_t e = sata::launch_softmax_step(a, dt == SATA_BF16, (hipStream_t)stream);

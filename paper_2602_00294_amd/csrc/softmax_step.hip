@@ -5,14 +5,16 @@
 // a key/value head are the columns of one 32 x 32 product, so a key's row serves all of
 // them.  The heads' caches are cut into stretches of one length, which the lengths of the
 // sequences decide on the card: as many of them as it holds workgroups at a time, so that
-// sequences of any lengths keep every compute unit loading to the end.  A wave takes every
+// sequences of any lengths keep every compute unit loading to the end.  (With very many sequences the
+// capacity decides.)  A wave takes every
 // W-th tile of 32 rows of a stretch and has the next tile on its way while it works, so no
 // wave waits for another one before the end, where the waves' sums are joined (and those of
 // a head of several stretches by a second kernel).
-// 128 heads of d = 128 in groups of four, sequences of 1 to 8192 rows (286 MB): 57 us (4.99 TB/s; a
+// 128 heads of d = 128 in groups of four, sequences of 1 to 8192 rows (286 MB): 56 us (5.12 TB/s; a
 // copy of 4 GB 4.9), 78 with stretches of one length for all calls and plain loads; the same
 // with all caches full (537 MB) 91 us (5.92 TB/s), 104; all a quarter full 31 us, 62; one
-// sequence of 131072 rows 117 us, 159.  Loads are streamed: with plain ones 70 us for the first.
+// sequence of 131072 rows 93 us, 159.
+// Loads are streamed: an earlier form took 62 us with and 70 without.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -49,7 +51,6 @@ __device__ __forceinline__ int wave_total(int x) {
 // many heads as places only heads of twice the mean are cut.  There are never more than p.workgroups
 // stretches: max(places, heads) of full length, and one shorter one a head.
 __device__ __forceinline__ int step_stretch(const SoftmaxStepArgs& a, const SoftmaxStepPlan& p, int lane) {
-  if (p.workgroups <= p.places) return p.least;  // (as what follows finds; 2 us less)
   const int B = a.heads / a.H, heads_of = a.H * p.blocks, heads = a.heads * p.blocks;
   int all = 0;
   for (int b = lane; b < B; b += 64) all += step_units(a, p, b);
@@ -192,31 +193,39 @@ __global__ void __launch_bounds__(64 * kStepWaves, sizeof(T) == 2 ? 2 : 1)
 softmax_step_kernel(SoftmaxStepArgs a, SoftmaxStepPlan p) {
   extern __shared__ __attribute__((aligned(16))) u16 smem16[];
   __shared__ StepState state[kStepWaves][32];
-  const int lane = threadIdx.x & 63, B = a.heads / a.H, heads_of = a.H * p.blocks;
-  const int len = step_stretch(a, p, lane);
-  // ---- which one this is: a lane counts the stretches of its own sequences
-  const int per = (B + 63) / 64, b0 = min(B, lane * per), b1 = min(B, b0 + per);
-  int mine = 0;
-  for (int b = b0; b < b1; ++b) mine += (step_units(a, p, b) + len - 1) / len;
-  int before = mine;
+  const int id = blockIdx.x, heads_of = a.H * p.blocks;
+  int b, hb, stretch, count, len = p.fixed_len;
+  if (p.fixed) {
+    const int place = id / p.fixed;
+    stretch = id - place * p.fixed, b = place / heads_of, hb = place - b * heads_of;
+    count = (step_units(a, p, b) + len - 1) / len;
+    if (stretch >= count) return;
+  } else {
+    const int lane = threadIdx.x & 63, B = a.heads / a.H;
+    len = step_stretch(a, p, lane);
+    // ---- which one this is: a lane counts the stretches of its own sequences
+    const int per = (B + 63) / 64, b0 = min(B, lane * per), b1 = min(B, b0 + per);
+    int mine = 0;
+    for (int i = b0; i < b1; ++i) mine += (step_units(a, p, i) + len - 1) / len;
+    int before = mine;
 #pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const int x = __shfl_up(before, d);
-    if (lane >= d) before += x;
+    for (int d = 1; d < 64; d *= 2) {
+      const int x = __shfl_up(before, d);
+      if (lane >= d) before += x;
+    }
+    before -= mine;
+    const uint64_t here = __ballot(before * heads_of <= id && id < (before + mine) * heads_of);
+    if (!here) return;
+    const int from = __builtin_ctzll(here);
+    b = __builtin_amdgcn_readlane(b0, from);
+    int rest = id - __builtin_amdgcn_readlane(before, from) * heads_of;
+    count = (step_units(a, p, b) + len - 1) / len;
+    for (; rest >= count * heads_of; count = (step_units(a, p, b) + len - 1) / len) rest -= count * heads_of, ++b;
+    // (a head's stretches lie next to each other)
+    hb = rest / count, stretch = rest - hb * count;
   }
-  before -= mine;
-  const int id = blockIdx.x;
-  const uint64_t here = __ballot(before * heads_of <= id && id < (before + mine) * heads_of);
-  if (!here) return;
-  const int from = __builtin_ctzll(here);
-  int b = __builtin_amdgcn_readlane(b0, from);
-  int rest = id - __builtin_amdgcn_readlane(before, from) * heads_of;
-  int count = (step_units(a, p, b) + len - 1) / len;
-  for (; rest >= count * heads_of; count = (step_units(a, p, b) + len - 1) / len) rest -= count * heads_of, ++b;
-  // (a head's stretches lie next to each other)
-  const int hb = rest / count, stretch = rest - hb * count, head = hb / p.blocks;
-  const int at = a.lengths[b], first = stretch * len * p.unit;
-  const int64_t place = ((int64_t)b * a.H + head) * p.blocks + hb - head * p.blocks;
+  const int head = hb / p.blocks, at = a.lengths[b], first = stretch * len * p.unit;
+  const int64_t place = (int64_t)b * heads_of + hb;
   int2* const found = (int2*)a.scratch;
   float* const sums = (float*)(found + (int64_t)a.heads * p.blocks);
   if (p.bytes && stretch == 0 && threadIdx.x == 0) found[place] = int2{id, count};
@@ -270,13 +279,24 @@ hipError_t launch_step(const SoftmaxStepArgs& a, const SoftmaxStepPlan& p, hipSt
 
 }  // namespace
 
-SoftmaxStepPlan plan_softmax_step(bool bf16, int heads, int G, int capacity, int dv) {
+SoftmaxStepPlan plan_softmax_step(bool bf16, int heads, int H, int G, int capacity, int dv) {
   SoftmaxStepPlan p;
   p.blocks = (G + 31) / 32;
-  const int count = heads * p.blocks;
+  const int count = heads * p.blocks, units = (capacity + p.unit - 1) / p.unit, B = heads / H;
   p.places = bf16 ? 512 : 256;
-  const int64_t most = (int64_t)count * (((capacity + p.unit - 1) / p.unit + p.least - 1) / p.least);
-  p.workgroups = (int)std::min<int64_t>(std::max(p.places, count) + count, most);
+  if ((int64_t)count * ((units + p.least - 1) / p.least) <= p.places) {
+    p.fixed_len = p.least;  // (all find a place)
+  } else if (B > 384) {
+    // (each workgroup reads all lengths, in steps of 64: us with stretches cut by them and by the capacity, 256 sequences
+    // of 8 heads and up to 2048 rows 176 and 199, 300 of one of up to 4096 68 and 83, 1000 of one of up to 2048 112
+    // and 113, 512 of 8 of up to 1024 228 and 174, 2000 of 8 of up to 256 746 and 247)
+    const int most = std::min(8, std::max(4, (4 * p.places + count - 1) / count));
+    p.fixed_len = std::max(8, (units + most - 1) / most);
+  }
+  if (p.fixed_len) p.fixed = (units + p.fixed_len - 1) / p.fixed_len;
+  p.workgroups = p.fixed ? count * p.fixed
+                         : (int)std::min<int64_t>(std::max(p.places, count) + count,
+                                                  (int64_t)count * ((units + p.least - 1) / p.least));
   p.bytes = p.workgroups > count
                 ? sizeof(int2) * (size_t)count + sizeof(float) * (size_t)p.workgroups * std::min(32, G) * (dv + 2)
                 : 0;
@@ -284,7 +304,7 @@ SoftmaxStepPlan plan_softmax_step(bool bf16, int heads, int G, int capacity, int
 }
 
 hipError_t launch_softmax_step(const SoftmaxStepArgs& a, bool bf16, hipStream_t s) {
-  const SoftmaxStepPlan p = plan_softmax_step(bf16, a.heads, a.G, a.capacity, a.dv_);
+  const SoftmaxStepPlan p = plan_softmax_step(bf16, a.heads, a.H, a.G, a.capacity, a.dv_);
   switch ((std::max(a.dk_, a.dv_) + 31) / 32) {
     case 1: return bf16 ? launch_step<u16, 1>(a, p, s) : launch_step<float, 1>(a, p, s);
     case 2: return bf16 ? launch_step<u16, 2>(a, p, s) : launch_step<float, 2>(a, p, s);

@@ -146,6 +146,9 @@ TOKENS = [  # B, H, G, capacity, dk, dv, dtype, lengths
     (150, 4, 2, 600, 16, 24, "bf16", [(211 * b) % 600 for b in range(150)]),
     (65, 4, 1, 900, 16, 16, "f32", [899] + [(97 * b) % 300 for b in range(64)]),
     (48, 8, 1, 800, 16, 16, "bf16", [(173 * b) % 800 for b in range(48)]),
+    # very many sequences
+    (400, 1, 2, 3000, 16, 8, "bf16", [(457 * b) % 3003 - 1 for b in range(400)]),
+    (390, 2, 1, 270, 32, 32, "f32", [(97 * b) % 270 for b in range(390)]),
 ]
 
 
