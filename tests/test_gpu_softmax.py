@@ -336,3 +336,36 @@ def test_offsets_past_32_bits(sata):
     pair_ref.check(got[:, -1:], ry, "token")
     assert torch.equal(k[:, -1:, :end + 2].cpu(), rK) and torch.equal(v[:, -1:, :end + 2].cpu(), rV)
     assert not k[:, -1, end + 2:].any()
+
+
+def test_two_graphs_at_once(sata):
+    """Two captured graphs, replayed side by side on two streams, share no scratch."""
+    _say("softmax, two graphs at once")
+    graphs, outs, wants, streams = [], [], [], [torch.cuda.Stream() for _ in range(2)]
+    for i, stream in enumerate(streams):
+        h = _prompt(20 + i, 2, 2, 2, 1200, 64, 64, "bf16")
+        K, V, at = h[1].clone(), h[2].clone(), _lengths([1100, 700])
+        tok = [h[0][:, :, 5].contiguous(), h[1][:, :, 5].contiguous(), h[2][:, :, 5].contiguous()]
+
+        def work(h=h, K=K, V=V, at=at, tok=tok):
+            y, lse = sata.softmax_prefill(*h[:3])
+            return [y, lse, *sata.softmax_backward(*h[:3], y, lse, h[3]), sata.softmax_step(K, V, at, *tok)]
+
+        stream.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(stream):
+            wants.append([x.clone() for x in work()])
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            outs.append(work())
+        graphs.append((graph, work))
+    for _ in range(3):
+        for (graph, _), stream in zip(graphs, streams):
+            with torch.cuda.stream(stream):
+                graph.replay()
+        torch.cuda.synchronize()
+        for got, want in zip(outs, wants):
+            assert all(torch.equal(a, b) for a, b in zip(got, want))
+            for x in got:
+                x.zero_()
+        torch.cuda.synchronize()
