@@ -456,6 +456,12 @@ inline bool few_sweeps(int64_t heads, int n) {
   return n > 128 && heads * ((n + 127) / 128) <= (sizeof(T) == 2 && ND <= 2 ? 256 : 128);
 }
 
+// Whether a bfloat16 call's workgroups take 256 rows, with eight waves, instead of 128: a staged tile serves
+// twice as many rows, but there have to be two rounds of workgroups for the card.  Prompts in us with eight
+// and four waves, d = 128: 32 heads of 8192 tokens (1024 workgroups) 548 and 586, 64 of 2000 (512) 90 and 91, 32
+// of 2000 (256) 67 and 57; gradients, rows of 256 and 128: 2220 and 2265, 337 and 337, 198 and 193.
+inline bool eight_waves(int64_t heads, int n) { return heads * ((n + 255) / 256) >= 512; }
+
 // Workgroups go to the 8 XCDs in turn.  With 8 heads or more each XCD takes whole
 // heads, so that a head's rows are read through one L2, in sets of as many heads as make
 // two rounds of workgroups on its 32 compute units: block by block within a set, so that a

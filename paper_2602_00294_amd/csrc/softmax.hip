@@ -325,7 +325,7 @@ template <typename T, int ND>
 hipError_t launch_prefill(const SoftmaxArgs& a, hipStream_t s) {
   if (few_sweeps<T, ND>((int64_t)a.heads * a.G, a.n)) return launch_prefill_few<T, ND>(a, s);
   if constexpr (sizeof(T) == 2)
-    if ((int64_t)a.heads * a.G * ((a.n + 255) / 256) >= 256) return launch_prefill_w<T, ND, 8>(a, s);
+    if (eight_waves((int64_t)a.heads * a.G, a.n)) return launch_prefill_w<T, ND, 8>(a, s);
   return launch_prefill_w<T, ND, 4>(a, s);
 }
 

@@ -537,7 +537,10 @@ hipError_t launch_cols(const SoftmaxGradArgs& a, hipStream_t s) {
 template <typename T, int ND>
 hipError_t launch_backward(const SoftmaxGradArgs& a, hipStream_t s) {
   constexpr bool bf16 = sizeof(T) == 2;
-  hipError_t e = few_sweeps<T, ND>((int64_t)a.heads * a.G, a.n) ? launch_rows_few<T, ND>(a, s) : launch_rows<T, ND, bf16 && ND >= 3 ? 8 : 4>(a, s);
+  const int64_t heads = (int64_t)a.heads * a.G;
+  hipError_t e = few_sweeps<T, ND>(heads, a.n)         ? launch_rows_few<T, ND>(a, s)
+                 : bf16 && eight_waves(heads, a.n) ? launch_rows<T, ND, bf16 ? 8 : 4>(a, s)
+                                                   : launch_rows<T, ND, 4>(a, s);
   if (e != hipSuccess) return e;
   if constexpr (bf16 || ND <= 2)  // (four waves' tiles of two wide float32 tensors, 192 KB, are more than the LDS)
     if (few_sweeps<T, ND>(a.heads, a.n)) return launch_cols_few<T, ND>(a, s);

@@ -102,6 +102,10 @@ MANY_HEADS = [  # B, H, G, n, dk, dv, dtype, lengths
     (5, 30, 1, 200, 64, 40, "bf16", [64, 200, 193, 32, 192]),
     (5, 30, 1, 290, 96, 72, "bf16", [289, 290, 1, 256, 225]),
     (2, 80, 2, 257, 128, 128, "bf16", None),
+    (8, 32, 1, 300, 32, 32, "bf16", None),
+    (4, 64, 1, 270, 64, 40, "bf16", [270, 257, 256, 0]),
+    (2, 66, 2, 300, 96, 72, "bf16", [289, 300]),
+    (2, 33, 4, 513, 16, 128, "bf16", [513, 400]),
 ]
 
 
