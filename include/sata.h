@@ -301,7 +301,8 @@ int64_t sata_softmax_step_scratch(int B, int H_kv, int G, int capacity, int d_v)
 
 /* Causal linear attention with a decay: with lam = exp(log_decay[h]),
  *     S_t = lam S_{t-1} + k_t (x) v_t,    y_t = c q_t S_t.
- *   log_decay: [H_kv] float32 (device), at most 0; minus infinity keeps each token to itself
+ *   log_decay: [H_kv] float32 (device), at most 0; minus infinity keeps each token to itself,
+ *          NaN makes NaN of whatever a power of lam enters
  *   S_in : [B][H_kv][d_k][d_v] float32 (device), the state before the first token, or NULL for zero
  *   y    : [B][H_kv*G][n][d_v], dtype dt (device, written)
  *   S_out: [B][H_kv][d_k][d_v] float32 (device, written) or NULL: the state after

@@ -106,7 +106,7 @@ __device__ __forceinline__ void scan_part(const DecayScan& s, const ScanParts& p
   const int col = 32 * wave + l31;
   const double rate = decay_rate(s.log_decay[head % s.H]);
   for (int e = tid; e <= C; e += kThreads) {
-    const float x = (float)exp(rate * e);
+    const float x = (float)decay_power(rate, e);
     power[C + e] = x;
     scaled[C + e] = x * (s.update * s.readout);
     if (e < C) power[e] = scaled[e] = 0.f;
@@ -216,6 +216,11 @@ __device__ __forceinline__ void scan_part(const DecayScan& s, const ScanParts& p
           float x = REV ? behind[C - 32 + result_row(i, 0)] : ahead[C - 4 - result_row(i, 0)];
           asm volatile("" : "+v"(x));  // (read by all lanes, not in 16 branches)
           z[i] = sees ? acc[i] * x : 0.f;  // (a select: not finite times 0 is no zero)
+        }
+        if (REV && m < C) {  // (nor are rows behind the sequence, which are zeros, if the decay is not finite)
+          stay_in_branch();
+#pragma unroll
+          for (int i = 0; i < 16; ++i) z[i] = result_row(i, h) < m ? z[i] : 0.f;
         }
         uint4 w[2][PA];
         to_planes<PA>(z, w);
@@ -365,7 +370,7 @@ __global__ void __launch_bounds__(256) decay_carry_kernel(ScanJobs a) {
   if (i >= size) return;
   const int len = tokens_of(s.lengths, head / s.H, s.n);
   const double rate = decay_rate(s.log_decay[head % s.H]);
-  const FloatPair whole = float_pair(exp(rate * p.part_len)), rest = float_pair(exp(rate * (len % p.part_len)));
+  const FloatPair whole = float_pair(decay_power(rate, p.part_len)), rest = float_pair(decay_power(rate, len % p.part_len));
   float* const states = p.states + (int64_t)head * p.parts * size + i;
   float R = s.S_in ? s.S_in[head * size + i] : 0.f;
   constexpr int kAhead = 8;  // parts read at once

@@ -283,3 +283,39 @@ def test_offsets_past_32_bits(sata):
     for name, a, w in zip(("dq", "dk", "dv"), grads, pair_ref.decay_backward(*small[:3], g[:1], small[3])):
         pair_ref.check(a[:, -1:, :end], w, name)
         assert not a[:, -1, end:].any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,lengths", [(100, [100, 37]), (700, [700, 1])])
+def test_a_decay_that_is_no_number(sata, dtype, n, lengths):
+    """NaN as a head's decay: what its powers enter is NaN, what they do not (the last token's share of its own
+    gradients, states that no token follows, other heads) is what it was."""
+    _say("decay of NaN", dtype, n, lengths)
+    q, k, v, dy, S_in, dS, _ = _make(21, 2, 2, 2, n, 24, 40, dtype)
+    g = torch.tensor([math.nan, -0.1], device="cuda")
+    lens = _lengths(lengths)
+
+    def same(name, got, ref):
+        got, (want, bound) = got.double().cpu(), ref
+        gone = torch.isnan(want)
+        assert torch.equal(torch.isnan(got), gone), f"{name}: NaN in {int(torch.isnan(got).sum())}, not {int(gone.sum())} places"
+        assert ((got - want).abs()[~gone] <= bound[~gone]).all(), name
+
+    for S0 in (None, S_in):
+        y, S = sata.decay_prefill(q, k, v, g, lens, S0)
+        torch.cuda.synchronize()
+        ry, rS = pair_ref.decay_prefill(q, k, v, g, lengths, S0)
+        assert torch.isnan(ry[0][:, :2, 0]).all() and torch.isnan(rS[0][:, 0]).all() and not torch.isnan(ry[0][:, 2:]).any()
+        same("y", y, ry)
+        same("S", S, rS)
+    grads = sata.decay_backward(q, k, v, g, dy, lens, S_in, dS)
+    torch.cuda.synchronize()
+    for name, a, w in zip(("dq", "dk", "dv", "dS_in"), grads, pair_ref.decay_backward(q, k, v, g, dy, lengths, S_in, dS)):
+        assert torch.isnan(w[0]).any()
+        same(name, a, w)
+    row = [x[:, :, 0].contiguous() for x in (q, k, v)]
+    ry, rS = pair_ref.decay_step(S_in, *row, g)
+    y = sata.decay_step(S_in, *row, g)
+    torch.cuda.synchronize()
+    same("token's y", y, ry)
+    same("token's S", S_in, rS)
