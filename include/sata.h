@@ -286,7 +286,10 @@ sata_status sata_decode_step_grouped(float* S, const void* q, const void* k, con
  *  - 1 <= d_k, d_v <= 128 (SATA_ERR_UNSUPPORTED beyond), B*H_kv*G <= 65535 and
  *    n <= 2^21 (SATA_ERR_TOO_LARGE beyond).
  *  - Values that are not finite reach what depends on them only: not earlier
- *    tokens' outputs, nor other sequences or heads.
+ *    tokens' outputs, nor other sequences or heads.  In softmax attention an infinity
+ *    counts as in float32 arithmetic: a key whose score is minus infinity has no
+ *    weight, and an infinite entry of v is an infinity in the outputs' column.  In
+ *    the decay's sums the outputs and states that it reaches are infinite or NaN.
  *  - scratch: device memory for the call's own use, 16-byte aligned, of at least as many
  *    bytes as the query beside the call says (NULL where that is 0).  These calls allocate
  *    nothing, upload nothing and wait for nothing, so any of them may be the first

@@ -178,7 +178,7 @@ __device__ __forceinline__ void scan_part(const DecayScan& s, const ScanParts& p
 #pragma unroll
       for (int x = 0; x < C / 16; ++x) {
         L::load_transposed(tw, 16 * x, wave, wf[x]);
-        bad |= not_finite_bits(wf[x][0]);
+        bad |= not_finite_bits(wf[x][L::kPl - 1]);
       }
       if constexpr (!SUMS) {
         if (!REV || opens) {
@@ -236,7 +236,7 @@ __device__ __forceinline__ void scan_part(const DecayScan& s, const ScanParts& p
           stay_in_branch();
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
-            const uint4 b = not_finite_entries(wf[x][0]);
+            const uint4 b = not_finite_entries(wf[x][L::kPl - 1]);
 #pragma unroll
             for (int i = 0; i < L::kPl; ++i) wc[x][i].x &= ~b.x, wc[x][i].y &= ~b.y, wc[x][i].z &= ~b.z, wc[x][i].w &= ~b.w;
           }
@@ -256,7 +256,7 @@ __device__ __forceinline__ void scan_part(const DecayScan& s, const ScanParts& p
               const int row = result_row(8 * x + i, h);
               y[i] = (REV ? row >= l31 : row <= l31) ? 1.f : 0.f;
             }
-            const uint4 b = not_finite_entries(wf[x][0]);
+            const uint4 b = not_finite_entries(wf[x][L::kPl - 1]);
             count = mfma32(uint4{b.x & 0x3f803f80u, b.y & 0x3f803f80u, b.z & 0x3f803f80u, b.w & 0x3f803f80u}, to_bf16(y),
                            count);
           }

@@ -12,13 +12,16 @@
 //
 // A tile holds rows of a tensor as they lie in memory, bfloat16, float32 ones as three
 // bfloat16 numbers (planes) whose sum carries 24 bits; a product of two such numbers is
-// the six partial products of order 2^-16 and up, accumulated in float32.  Rows are
+// the six partial products of order 2^-16 and up, accumulated in float32.  (Those beyond
+// bfloat16's range, infinities among them: far_part.)  Rows are
 // whole 64, 128 or 256 bytes; the 16-byte units of a row change places by
 // its number, so that both ways of reading, along 16 or more rows and transposed by
 // four rows of 64 bytes, meet every bank once.
 #pragma once
 
 #include <hip/hip_runtime.h>
+
+#include <type_traits>
 
 #include "device_common.hpp"
 #include "series.hpp"
@@ -65,7 +68,23 @@ __device__ __forceinline__ float entry_of(const u16* p, int64_t i) { return __ui
 // Row of a result's number i.
 __device__ __forceinline__ int result_row(int i, int h) { return 8 * (i >> 2) + 4 * h + (i & 3); }
 
-// N values (a multiple of 8) as operands of PL planes each; x is used up.
+// Float32 values beyond bfloat16's largest number, 3.39e38, do not split as others do: rounded they would be
+// infinite, and an infinity leaves NaN.  A finite one's first plane is that number; an infinity is (1, 0, infinity) with
+// its sign, so that of the partial products with another value's planes one is infinite, the one with
+// the other's first plane, whose sign and zero are the value's.  Tiles are looked over for such values behind their stores
+// and put once more where there are some: 16 heads of 1000 tokens, d = 64, float32, prompts 41 -> 42 us and gradients
+// 119 -> 121, of 2000 tokens 101 -> 108 and 288 -> 295; 32 heads of 2000, d = 128, 214 -> 217 and 826 -> 845; the same
+// by the decay 151 -> 154 and 313 -> 324 (looked over before the stores: 220 and 855, 155 and 320).
+// far_part: plane `plane` of what the planes before it left.
+constexpr float kLargestBf16 = 0x1.fep127f;
+__device__ __forceinline__ float far_part(float x, int plane) {
+  if (plane == 2) return x;
+  if (fabsf(x) == INFINITY) return plane == 0 ? copysignf(1.f, x) : 0.f;
+  return fabsf(x) > kLargestBf16 ? copysignf(kLargestBf16, x) : x;
+}
+
+// N values (a multiple of 8) as operands of PL planes each; x is used up.  (For weights and states: an
+// infinite one of several planes becomes NaN.)
 template <int PL, int N>
 __device__ __forceinline__ void to_planes(float (&x)[N], uint4 (&op)[N / 8][PL]) {
 #pragma unroll
@@ -113,7 +132,7 @@ struct PairTile {
   }
 };
 
-// The entries of a plane that are infinite or NaN, all bits of each set.
+// The entries of a plane that are infinite or NaN, all bits of each set.  (A value's last plane is, where the value is.)
 __device__ __forceinline__ uint4 not_finite_entries(const uint4& w) {
   auto wide = [](uint32_t x) { return ((((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u) >> 15) * 0xffffu; };
   return uint4{wide(w.x), wide(w.y), wide(w.z), wide(w.w)};
@@ -192,10 +211,8 @@ __device__ __forceinline__ uint32_t not_finite_bits(const uint4& w) {
           (((w.z & 0x7f807f80u) + 0x00800080u) | ((w.w & 0x7f807f80u) + 0x00800080u))) & 0x80008000u;
 }
 
-// (a float32 value beyond bfloat16's range is an infinity in its first plane)
-__device__ __forceinline__ bool bf16_finite(float x) { return (pack2(x, 0.f) & 0x7f80u) != 0x7f80u; }
-
-// Whether rows r0 .. r0 + 31 of the tile hold a value that is not finite (for the whole wave).
+// Whether rows r0 .. r0 + 31 of the tile hold a value that is not finite, which its last plane tells (for
+// the whole wave).
 template <typename L, int ND>
 __device__ __forceinline__ bool tile_not_finite(const u16* t, int r0) {
   stay_in_branch();
@@ -204,7 +221,7 @@ __device__ __forceinline__ bool tile_not_finite(const u16* t, int r0) {
   for (int s = 0; s < 2 * ND; ++s) {
     uint4 a[L::kPl];
     L::load_rows(t, r0, s, a);
-    bad |= not_finite_bits(a[0]);
+    bad |= not_finite_bits(a[L::kPl - 1]);
   }
   return __ballot(bad != 0) != 0;
 }
@@ -249,7 +266,7 @@ struct TileStage {
       float f = x;
 #pragma unroll
       for (int i = 0; i < L::kPl; ++i) {
-        const uint32_t b = pack2(f, 0.f);
+        const uint32_t b = pack2(far_part(f, i), 0.f);
         dst[i * L::kPlane] = (u16)b;
         f -= lo_f32(b);
       }
@@ -257,24 +274,39 @@ struct TileStage {
       dst[0] = x;
     }
   }
+  // FAR: some values of the vectors are beyond bfloat16's range
+  template <bool FAR>
+  __device__ __forceinline__ void put_vectors(u16* t) const {
+#pragma unroll
+    for (int i = 0; i < kIt; ++i) {
+      const int row = tid / kU + i * kPer;
+      if ((i + 1) * kPer > ROWS && row >= ROWS) continue;
+      u16* const dst = t + L::at(row, tid % kU * kEV);
+      if constexpr (sizeof(T) == 4) {
+        float x[4] = {__uint_as_float(r[i].x), __uint_as_float(r[i].y), __uint_as_float(r[i].z), __uint_as_float(r[i].w)};
+#pragma unroll
+        for (int pl = 0; pl < L::kPl; ++pl) {
+          auto part = [&](int j) { return FAR ? far_part(x[j], pl) : x[j]; };
+          const uint2 b = {pack2(part(0), part(1)), pack2(part(2), part(3))};
+          *(uint2*)(dst + pl * L::kPlane) = b;
+          x[0] -= lo_f32(b.x), x[1] -= hi_f32(b.x), x[2] -= lo_f32(b.y), x[3] -= hi_f32(b.y);
+        }
+      } else {
+        *(uint4*)dst = r[i];
+      }
+    }
+  }
   __device__ __forceinline__ void put(u16* t, int r0) const {
     if (vec) {
+      put_vectors<false>(t);
+      if constexpr (sizeof(T) == 4) {
+        float most = 0.f;
 #pragma unroll
-      for (int i = 0; i < kIt; ++i) {
-        const int row = tid / kU + i * kPer;
-        if ((i + 1) * kPer > ROWS && row >= ROWS) continue;
-        u16* const dst = t + L::at(row, tid % kU * kEV);
-        if constexpr (sizeof(T) == 4) {
-          float x[4] = {__uint_as_float(r[i].x), __uint_as_float(r[i].y), __uint_as_float(r[i].z), __uint_as_float(r[i].w)};
-#pragma unroll
-          for (int pl = 0; pl < L::kPl; ++pl) {
-            const uint2 b = {pack2(x[0], x[1]), pack2(x[2], x[3])};
-            *(uint2*)(dst + pl * L::kPlane) = b;
-            x[0] -= lo_f32(b.x), x[1] -= hi_f32(b.x), x[2] -= lo_f32(b.y), x[3] -= hi_f32(b.y);
-          }
-        } else {
-          *(uint4*)dst = r[i];
+        for (int i = 0; i < kIt; ++i) {
+          most = fmaxf(fmaxf(most, fabsf(__uint_as_float(r[i].x))), fabsf(__uint_as_float(r[i].y)));
+          most = fmaxf(fmaxf(most, fabsf(__uint_as_float(r[i].z))), fabsf(__uint_as_float(r[i].w)));
         }
+        if (__builtin_expect(most > kLargestBf16, 0)) put_vectors<true>(t);  // (once more)
       }
     } else {
 #pragma unroll 1
@@ -334,23 +366,40 @@ __device__ __forceinline__ void wave_lds_fence() {
 
 // Right (or left) operands of one row per lane pair: entries 16 s + 8 h .. +7, all planes;
 // zero past the width and where !ok.
-template <typename T, int ND>
-__device__ __forceinline__ void load_own32(const T* p, bool ok, int width, uint4 (&f)[2 * ND][sizeof(T) == 4 ? 3 : 1]) {
+template <int ND, bool FAR>
+__device__ __forceinline__ float split_own32(const float* p, bool ok, int width, uint4 (&f)[2 * ND][3]) {
   const int h = (threadIdx.x & 63) >> 5;
-  const bool vec = sizeof(T) == 2 && width % 8 == 0 && ((uintptr_t)p & 15) == 0;
+  float most = 0.f;
 #pragma unroll
   for (int s = 0; s < 2 * ND; ++s) {
     const int c0 = 16 * s + 8 * h;
-    if constexpr (sizeof(T) == 4) {
-      float x[8];
+    float x[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] = ok && c0 + j < width ? p[c0 + j] : 0.f;
+    for (int j = 0; j < 8; ++j) x[j] = ok && c0 + j < width ? p[c0 + j] : 0.f;
 #pragma unroll
-      for (int i = 0; i < 3; ++i) {
-        f[s][i] = to_bf16(x);
-        take_bf16(f[s][i], x);
-      }
-    } else {
+    for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf(x[j]));
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      float y[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) y[j] = FAR ? far_part(x[j], i) : x[j];
+      f[s][i] = to_bf16(y);
+      take_bf16(f[s][i], x);
+    }
+  }
+  return most;
+}
+template <typename T, int ND>
+__device__ __forceinline__ void load_own32(const T* p, bool ok, int width, uint4 (&f)[2 * ND][sizeof(T) == 4 ? 3 : 1]) {
+  if constexpr (sizeof(T) == 4) {
+    // (read once more where some are: a branch for every eight values would wait for each one's loads)
+    if (__builtin_expect(split_own32<ND, false>(p, ok, width, f) > kLargestBf16, 0)) split_own32<ND, true>(p, ok, width, f);
+  } else {
+    const int h = (threadIdx.x & 63) >> 5;
+    const bool vec = width % 8 == 0 && ((uintptr_t)p & 15) == 0;
+#pragma unroll
+    for (int s = 0; s < 2 * ND; ++s) {
+      const int c0 = 16 * s + 8 * h;
       uint4 w = {0u, 0u, 0u, 0u};
       if (vec) {
         if (ok && c0 < width) w = *(const uint4*)(p + c0);

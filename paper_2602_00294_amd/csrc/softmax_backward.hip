@@ -72,8 +72,8 @@ __device__ __forceinline__ void masked_keys(const T* k, int dk, const T* v, int 
 template <typename T>
 __device__ __forceinline__ bool rows_not_finite(const T* q, int dk, const T* dy, int dv, int rows) {
   bool bad = false;
-  for (int i = threadIdx.x & 63; i < rows * dk; i += 64) bad |= !bf16_finite(entry_of(q, i));
-  for (int i = threadIdx.x & 63; i < rows * dv; i += 64) bad |= !bf16_finite(entry_of(dy, i));
+  for (int i = threadIdx.x & 63; i < rows * dk; i += 64) bad |= !isfinite(entry_of(q, i));
+  for (int i = threadIdx.x & 63; i < rows * dv; i += 64) bad |= !isfinite(entry_of(dy, i));
   return __ballot(bad) != 0;
 }
 

@@ -373,3 +373,116 @@ def test_two_graphs_at_once(sata):
             for x in got:
                 x.zero_()
         torch.cuda.synchronize()
+
+
+def _by_rows(q, k, v, lengths):
+    """y and lse row by row in float64, so that a row meets the keys it sees and no others: (value, bound) pairs
+    with pair_ref's bounds, counted over what is finite."""
+    dt = q.dtype
+    q, k, v = q.double().cpu(), k.double().cpu(), v.double().cpu()
+    B, Hq, n, dk = q.shape
+    G, dv = Hq // k.shape[1], v.shape[-1]
+    y, yb = (torch.zeros(B, Hq, n, dv, dtype=torch.float64) for _ in range(2))
+    lse, lb = torch.full((B, Hq, n), -math.inf, dtype=torch.float64), torch.zeros(B, Hq, n, dtype=torch.float64)
+    for b, e in enumerate(lengths):
+        for i in range(Hq):
+            for t in range(e):
+                K, V, x = k[b, i // G, :t + 1], v[b, i // G, :t + 1], q[b, i, t]
+                s = K @ x / math.sqrt(dk)
+                z = torch.logsumexp(s, 0)
+                p = torch.exp(s - z)
+                off = ((dk + 8) * 2.0 ** -23 / math.sqrt(dk) * (K.abs() @ x.abs())).masked_fill(p == 0, 0.0)
+                y[b, i, t], lse[b, i, t] = p @ V, z
+                rel = 2 * off + 2 * (p * off).sum() + (n + 32) * 2.0 ** -23
+                yb[b, i, t] = pair_ref.HALF[dt] * y[b, i, t].abs() + (p * (1.01 * pair_ref.WEIGHT[dt] + rel)) @ V.abs() + 1e-30
+                lb[b, i, t] = 2.0 ** -22 * z.abs() + (p * off).sum() + (n + 16) * 2.0 ** -23
+    return (y, yb), (lse, lb)
+
+
+# few workgroups, four waves a workgroup, and (bfloat16) eight
+INFINITE = [("f32", 1, 2, 2, 150, 0), ("f32", 1, 2, 2, 150, 1), ("f32", 70, 1, 2, 70, 0), ("f32", 70, 1, 2, 70, 1),
+            ("bf16", 1, 2, 2, 150, 0), ("bf16", 70, 1, 2, 70, 0), ("bf16", 256, 2, 1, 33, 0), ("bf16", 256, 2, 1, 33, 1)]
+
+
+@pytest.mark.parametrize("dtype,H,G,B,end,offset", INFINITE)
+def test_infinite_values(sata, dtype, H, G, B, end, offset):
+    """An infinite entry of v is an infinity in its column of every row that sees it, and nowhere else; dv,
+    which v does not enter, keeps its bits (from the same lse)."""
+    n, at = end + 7, min(end - 20, 100)
+    _say("softmax, infinite values", dtype, H, G, B, end, offset)
+    q, k, v, dy = _prompt(31, B, H, G, n, 40, 24, dtype, offset=offset)
+    lengths = [end] + [n] * (B - 1)
+    y, lse = sata.softmax_prefill(q, k, v, _lengths(lengths))
+    dv = sata.softmax_backward(q, k, v, y, lse, dy, _lengths(lengths))[2]
+    v2 = v.clone() if not offset else _prompt(31, B, H, G, n, 40, 24, dtype, offset=offset)[2]
+    v2[0, 0, at, 3], v2[0, 0, at - 3, 5] = math.inf, -math.inf
+    y2, lse2 = sata.softmax_prefill(q, k, v2, _lengths(lengths))
+    dv2 = sata.softmax_backward(q, k, v2, y2, lse, dy, _lengths(lengths))[2]
+    torch.cuda.synchronize()
+    want = y.clone()
+    want[0, :G, at:end, 3], want[0, :G, at - 3:end, 5] = math.inf, -math.inf
+    hit = torch.isinf(want)
+    assert torch.equal(y2[hit], want[hit]) and torch.isfinite(y2[~hit]).all()
+    off = (lse2 - lse)[0, :, :end].abs().max()
+    assert off <= 1e-5 and torch.equal(dv2, dv)
+    ry, rl = _by_rows(q[:1, :G], k[:1, :1], v2[:1, :1], lengths[:1])
+    pair_ref.check(y2[:1, :G], ry, "y")
+    pair_ref.check(lse2[:1, :G], rl, "lse")
+
+
+@pytest.mark.parametrize("dtype,H,G,B,end,offset", INFINITE)
+def test_keys_without_weight(sata, dtype, H, G, B, end, offset):
+    """A key whose score is minus infinity has no weight: the rows that see it are those without it."""
+    n, at = end + 7, min(end - 20, 100)
+    _say("softmax, keys without weight", dtype, H, G, B, end, offset)
+    q, k, v, _ = _prompt(32, B, H, G, n, 40, 24, dtype, offset=offset)
+    q[..., 3] = -q[..., 3].abs() - 0.125
+    lengths = [end] + [n] * (B - 1)
+    k[0, 0, at, 3] = math.inf
+    y, lse = sata.softmax_prefill(q, k, v, _lengths(lengths))
+    torch.cuda.synchronize()
+    ry, rl = _by_rows(q[:1, :G], k[:1, :1], v[:1, :1], lengths[:1])
+    assert torch.isfinite(ry[0]).all()
+    pair_ref.check(y[:1, :G], ry, "y")
+    pair_ref.check(lse[:1, :G], rl, "lse")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_infinities_in_the_cache(sata, dtype):
+    _say("softmax token, infinities in the cache", dtype)
+    K, V, q, k, v = _rand(33, dtype, (2, 2, 900, 40), (2, 2, 900, 24), (2, 4, 40), (2, 2, 40), (2, 2, 24))
+    q[..., 3] = -q[..., 3].abs() - 0.125
+    K[0, 0, 77, 3] = math.inf          # no weight
+    V[1, 1, 500, 7] = -math.inf        # an infinity in its column
+    at = [860, 700]
+    rows = lambda x, new: [torch.cat([x[b, :, :e], new[b, :, None]], 1)[None] for b, e in enumerate(at)]  # noqa: E731
+    rK, rV = rows(K, k), rows(V, v)
+    y = sata.softmax_step(K, V, _lengths(at), q, k, v)
+    torch.cuda.synchronize()
+    for b, e in enumerate(at):
+        for h in range(4):
+            s = rK[b][0, h // 2].double().cpu() @ q[b, h].double().cpu() / math.sqrt(40)
+            p, vv = torch.softmax(s, 0), rV[b][0, h // 2].double().cpu()
+            assert torch.isfinite(s).all() or (b, h // 2) == (0, 0)
+            rel = 1.01 * pair_ref.WEIGHT[DT[dtype]] + (2 * 48 * 40 + e + 32) * 2.0 ** -23  # (|q||k| below 40)
+            ref = p @ vv
+            pair_ref.check(y[b, h], (ref, pair_ref.HALF[DT[dtype]] * ref.abs() + rel * (p @ vv.abs()) + 1e-30), f"y {b} {h}")
+    assert torch.isneginf(y[1, 2:, 7]).all() and torch.isfinite(y[0]).all()
+
+
+def test_largest_float32_values(sata):
+    """Float32 numbers beyond bfloat16's largest (3.39e38) are numbers like others."""
+    _say("softmax, largest values")
+    n, at = 150, 70
+    q, k, v, dy = _prompt(34, 1, 2, 1, n, 40, 24, "f32")
+    v[0, 0, at, 3], v[0, 0, at, 4] = 3.4e38, -3.4e38
+    q[..., 5] = 2.0 ** -125
+    k[0, 1, at, 5] = 3.4e38            # (a score of 8 / sqrt(40))
+    y, lse = sata.softmax_prefill(q, k, v)
+    K, V = k.clone(), v.clone()
+    last = sata.softmax_step(K, V, _lengths([n - 1]), q[:, :, -1].contiguous(), k[:, :, -1].contiguous(), v[:, :, -1].contiguous())
+    torch.cuda.synchronize()
+    ry, rl = _by_rows(q, k, v, [n])
+    pair_ref.check(y, ry, "y")
+    pair_ref.check(lse, rl, "lse")
+    pair_ref.check(last, (ry[0][:, :, -1], ry[1][:, :, -1]), "token")
