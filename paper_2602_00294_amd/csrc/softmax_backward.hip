@@ -155,6 +155,22 @@ __global__ void __launch_bounds__(64 * W, sizeof(T) == 2 ? 2 : 1) softmax_rows(S
   if (row < n) store_row32<T, ND>((T*)a.dq + at * dk, dk, acc, row < len ? a.scale : 0.f, row >= len);
 }
 
+// Rows behind the sequence are zeros of probability zero, but a key or value that is not finite makes NaN of
+// them: for such keys (rare) they are taken out of a tile's weights x of rows t0 .. +31.
+template <int ND, int PL>
+__device__ __forceinline__ bool own_not_finite(const uint4 (&own)[2 * ND][PL]) {
+  uint32_t bad = 0;
+#pragma unroll
+  for (int s = 0; s < 2 * ND; ++s) bad |= not_finite_bits(own[s][PL - 1]);
+  return __ballot(bad != 0) != 0;
+}
+template <typename X>
+__device__ __forceinline__ void without_padding(X& x, int t0, int len) {
+  stay_in_branch();
+#pragma unroll
+  for (int i = 0; i < 16; ++i) x[i] = t0 + result_row(i, (threadIdx.x & 63) >> 5) < len ? x[i] : 0.f;
+}
+
 // A tile of 32 keys has two waves, which share its pairs: wave t of the first half forms the scores, the
 // probabilities and dv, wave t of the second dy.v, e and dk, 4 ND matrix instructions each a pair of tiles;
 // the probabilities go from one to the other through LDS, in float32, behind a barrier in the
@@ -182,6 +198,7 @@ __global__ void __launch_bounds__(64 * W, sizeof(T) == 2 ? 2 : 1) softmax_cols(S
   if (32 * kTiles * blk < len) {
     uint4 own[2 * ND][L::kPl];  // k or v
     load_own32<T, ND>(for_k ? (const T*)a.v + at * dv : (const T*)a.k + at * dk, row < len, for_k ? dv : dk, own);
+    const bool strange = own_not_finite<ND>(own);
     const float c = a.scale * kLog2e;
     bool odd = false;  // whether own tiles hold values that are not finite: such a member's is left out
     PairStage<T, ND, kRows, kThreads> stage;
@@ -232,6 +249,12 @@ __global__ void __launch_bounds__(64 * W, sizeof(T) == 2 ? 2 : 1) softmax_cols(S
             x[r][4 * i + 3] = exp2_fast(fmaf(x[r][4 * i + 3], c, -z.w));
             shared_p[(4 * r + i) * 64] = float4{x[r][4 * i], x[r][4 * i + 1], x[r][4 * i + 2], x[r][4 * i + 3]};
           }
+          if (__builtin_expect(strange && t0 + 32 * r + 32 > len, 0)) {
+            without_padding(x[r], t0 + 32 * r, len);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              shared_p[(4 * r + i) * 64] = float4{x[r][4 * i], x[r][4 * i + 1], x[r][4 * i + 2], x[r][4 * i + 3]};
+          }
         }
       }
       settle_mfma32();
@@ -251,6 +274,7 @@ __global__ void __launch_bounds__(64 * W, sizeof(T) == 2 ? 2 : 1) softmax_cols(S
             e[4 * i + 2] = p.z * (e[4 * i + 2] - z.z);
             e[4 * i + 3] = p.w * (e[4 * i + 3] - z.w);
           }
+          if (__builtin_expect(strange && t0 + 32 * r + 32 > len, 0)) without_padding(e, t0 + 32 * r, len);
         }
         if (!kWhole && t0 + 32 * r == k0) {
           stay_in_branch();
@@ -421,7 +445,7 @@ __global__ void __launch_bounds__(256, 1) softmax_cols_few(SoftmaxGradArgs a, in
     const float c = a.scale * kLog2e;
     bool odd = false;  // whether own tiles hold values that are not finite: such a member's is left out
     for (; u < units; u += 4) {
-      const bool own = u % tiles == 0;
+      const bool own = u % tiles == 0, ends = t0 + 32 > len;
       wave_lds_fence();
       sq.put(qt, t0);
       sy.put(yt, t0);
@@ -434,6 +458,13 @@ __global__ void __launch_bounds__(256, 1) softmax_cols_few(SoftmaxGradArgs a, in
       for (int i = 0; i < 16; ++i) {
         p[i] = exp2_fast(fmaf(s[i], c, -stats[wave][result_row(i, h)]));
         e[i] = p[i] * (d[i] - stats[wave][32 + result_row(i, h)]);
+      }
+      if (__builtin_expect(ends, 0)) {
+        stay_in_branch();
+        if (__builtin_expect(own_not_finite<ND>(kf) || own_not_finite<ND>(vf), 0)) {
+          without_padding(p, len / 32 * 32, len);
+          without_padding(e, len / 32 * 32, len);
+        }
       }
       if (own) {
         stay_in_branch();

@@ -432,19 +432,32 @@ def test_infinite_values(sata, dtype, H, G, B, end, offset):
 
 @pytest.mark.parametrize("dtype,H,G,B,end,offset", INFINITE)
 def test_keys_without_weight(sata, dtype, H, G, B, end, offset):
-    """A key whose score is minus infinity has no weight: the rows that see it are those without it."""
+    """A key whose score is minus infinity has no weight: the rows that see it are those without it, and so
+    are all gradients of k and v, its own being zero (0 times its infinity makes dq NaN)."""
     n, at = end + 7, min(end - 20, 100)
     _say("softmax, keys without weight", dtype, H, G, B, end, offset)
-    q, k, v, _ = _prompt(32, B, H, G, n, 40, 24, dtype, offset=offset)
+    q, k, v, dy = _prompt(32, B, H, G, n, 40, 24, dtype, offset=offset)
     q[..., 3] = -q[..., 3].abs() - 0.125
     lengths = [end] + [n] * (B - 1)
     k[0, 0, at, 3] = math.inf
     y, lse = sata.softmax_prefill(q, k, v, _lengths(lengths))
+    grads = sata.softmax_backward(q, k, v, y, lse, dy, _lengths(lengths))
     torch.cuda.synchronize()
     ry, rl = _by_rows(q[:1, :G], k[:1, :1], v[:1, :1], lengths[:1])
     assert torch.isfinite(ry[0]).all()
     pair_ref.check(y[:1, :G], ry, "y")
     pair_ref.check(lse[:1, :G], rl, "lse")
+    # a key of -2^60 in its place is the same, in finite numbers
+    far = k.clone()
+    far[0, 0, at, 3] = 2.0 ** 60
+    want = pair_ref.softmax_backward(q[:1, :G], far[:1, :1], v[:1, :1], y[:1, :G], lse[:1, :G], dy[:1, :G], lengths[:1])
+    for name, a, (w, bound) in zip(("dk", "dv"), grads[1:], want[1:]):
+        assert not w[0, 0, at].any() and torch.isfinite(a).all(), name
+        keep = torch.arange(n) != at
+        pair_ref.check(a[:1, :1, keep], (w[:, :, keep], bound[:, :, keep]), name)
+        assert not a[0, 0, at].any(), name
+    assert torch.isfinite(grads[0][:1, :G, :at]).all()
+    pair_ref.check(grads[0][:1, :G, :at], (want[0][0][:, :, :at], want[0][1][:, :, :at]), "dq")
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
