@@ -266,7 +266,7 @@ hipError_t launch_step(const SoftmaxStepArgs& a, const SoftmaxStepPlan& p, hipSt
   const int bytes = std::max<int>(kStepWaves * PairTile<T, ND, 32>::kBytes,
                                   kStepWaves * std::min(32, a.G) * a.dv_ * (int)sizeof(float));
   auto kern = softmax_step_kernel<T, ND>;
-  if (bytes > 64 * 1024) {
+  if (bytes > 63 * 1024) {  // (1 KB is static)
     hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != hipSuccess) return e;
   }

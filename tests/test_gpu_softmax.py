@@ -499,3 +499,17 @@ def test_largest_float32_values(sata):
     pair_ref.check(y, ry, "y")
     pair_ref.check(lse, rl, "lse")
     pair_ref.check(last, (ry[0][:, :, -1], ry[1][:, :, -1]), "token")
+
+
+@pytest.mark.parametrize("G", [32, 33])
+@pytest.mark.parametrize("dv", [127, 128])
+@pytest.mark.parametrize("cap,end", [(100, 99), (3000, 2500)])
+def test_token_of_wide_groups(sata, G, dv, cap, end):
+    """The waves' sums of 32 query heads of 128 columns are 64 KB of LDS."""
+    _say("softmax token, wide groups", G, dv, cap, end)
+    K, V, q, k, v = _rand(35, "bf16", (1, 2, cap, 128), (1, 2, cap, dv), (1, 2 * G, 128), (1, 2, 128), (1, 2, dv))
+    ry, rK, rV = pair_ref.softmax_step(K, V, [end], q, k, v)
+    y = sata.softmax_step(K, V, _lengths([end]), q, k, v)
+    torch.cuda.synchronize()
+    pair_ref.check(y, ry, "y")
+    assert torch.equal(K.cpu(), rK) and torch.equal(V.cpu(), rV)
