@@ -328,7 +328,7 @@ sata_status sata_decay_step(float* S, const void* q, const void* k, const void* 
  * The decay is a constant of the layer: it gets no gradient.
  *   S_in : as given to the forward call, or NULL
  *   dq, dk, dv: as q, k, v (device, written)
- *   dS_in: [B][H_kv][d_k][d_v] float32 (device, written) or NULL.  Must not be dS. */
+ *   dS_in: [B][H_kv][d_k][d_v] float32 (device, written) or NULL.  Must be neither dS nor S_in. */
 sata_status sata_decay_backward(const void* q, const void* k, const void* v, const float* log_decay, const void* dy,
                                 sata_dtype dt, int B, int H_kv, int G, int n, int d_k, int d_v, const int32_t* lengths,
                                 const float* S_in, const float* dS, void* dq, void* dk, void* dv, float* dS_in,

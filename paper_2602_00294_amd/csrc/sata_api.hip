@@ -1017,6 +1017,8 @@ sata_status sata_decay_backward(const void* q, const void* k, const void* v, con
   if (!log_decay || (n > 0 && (!q || !k || !v || !dy || !dq || !dk || !dv)))
     return fail(SATA_ERR_INVALID_ARG, "null tensor pointer");
   if (dS && dS == dS_in) return fail(SATA_ERR_INVALID_ARG, "dS_in must not be dS");
+  // (one launch forms all gradients: the workgroups for dq read S_in while those for dv write dS_in)
+  if (S_in && S_in == dS_in) return fail(SATA_ERR_INVALID_ARG, "dS_in must not be S_in");
   if (n == 0 && !dS_in) return ok();
   if ((st = check_scratch(scratch, 2 * sata::plan_decay_scan(dt == SATA_BF16, B * H_kv, G, n, d_k, d_v, 3).state_bytes)) != SATA_OK) return st;
   const float c = pair_scale(d_k);

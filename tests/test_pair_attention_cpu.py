@@ -193,6 +193,19 @@ def test_pointers_refused(lib):
     assert lib.sata_softmax_backward(N, N, N, N, N, N, *empty, N, N, N, N, N, N) == 0
 
 
+def test_states_that_alias(lib):
+    """One workgroup would write dS_in while another reads S_in or dS."""
+    F, N = FAKE, NULL
+    A, B, C = (ctypes.c_void_p(0x1000 * i) for i in (2, 3, 4))
+    for sizes in ((0, 1, 1, 1, 8, 4, 4), (1, 2, 3, 2, 4096, 64, 32)):
+        assert lib.sata_decay_backward(F, F, F, F, F, *sizes, N, A, B, F, F, F, A, F, N) == -1
+        assert "S_in" in lib.sata_last_error().decode()
+        assert lib.sata_decay_backward(F, F, F, F, F, *sizes, N, A, B, F, F, F, B, F, N) == -1
+    # (other states: only the missing scratch is in the way)
+    assert lib.sata_decay_backward(F, F, F, F, F, *sizes, N, A, B, F, F, F, C, N, N) == -1
+    assert "scratch" in lib.sata_last_error().decode()
+
+
 def test_scratch(lib):
     F, N = FAKE, NULL
     odd = ctypes.c_void_p(0x1008)
