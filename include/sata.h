@@ -284,7 +284,8 @@ sata_status sata_decode_step_grouped(float* S, const void* q, const void* k, con
  *    (taken into 0..n; NULL: all have n).  Rows at and behind a length are not
  *    used, whatever they hold, and their outputs and gradients are written as zero.
  *  - 1 <= d_k, d_v <= 128 (SATA_ERR_UNSUPPORTED beyond), B*H_kv*G <= 65535 and
- *    n <= 2^21 (SATA_ERR_TOO_LARGE beyond).
+ *    n <= 2^21 (SATA_ERR_TOO_LARGE beyond).  Softmax prompts and gradients: B*H_kv*G*n <= 2e9,
+ *    gradients also B*H_kv*n <= 1e9 (what one launch holds).
  *  - Values that are not finite reach what depends on them only: not earlier
  *    tokens' outputs, nor other sequences or heads.  In softmax attention an infinity
  *    counts as in float32 arithmetic: a key whose score is minus infinity has no

@@ -708,6 +708,19 @@ sata_status check_pair_args(sata_dtype dt, int B, int H_kv, int G, int n, int d_
   return SATA_OK;
 }
 
+// A launch has fewer than 2^32 threads: the kernels of softmax prompts take two a query and those of the gradients four a
+// key as well, of heads rounded up to a multiple of 8 and tokens to one of 256 (at these sizes under 2% in all).
+constexpr int64_t kMaxPromptTokens = 2000000000, kMaxGradientTokens = 1000000000;
+
+sata_status check_softmax_tokens(int B, int H_kv, int G, int n, bool gradients) {
+  const int64_t keys = (int64_t)B * H_kv * n;
+  if (keys * G > kMaxPromptTokens)
+    return fail(SATA_ERR_TOO_LARGE, "B*H_kv*G*n=%lld tokens exceed %lld", (long long)(keys * G), (long long)kMaxPromptTokens);
+  if (gradients && keys > kMaxGradientTokens)
+    return fail(SATA_ERR_TOO_LARGE, "B*H_kv*n=%lld tokens exceed %lld", (long long)keys, (long long)kMaxGradientTokens);
+  return SATA_OK;
+}
+
 // The caller's scratch for a call that needs `bytes` of it.
 sata_status check_scratch(const void* scratch, size_t bytes) {
   if (bytes && !scratch) return fail(SATA_ERR_INVALID_ARG, "null scratch; %zu bytes needed", bytes);
@@ -969,6 +982,7 @@ int64_t sata_decay_scratch(int B, int H_kv, int G, int n, int d_k, int d_v) {
 
 int64_t sata_softmax_backward_scratch(int B, int H_kv, int G, int n) {
   if (check_pair_args(SATA_F32, B, H_kv, G, n, 1, 1) != SATA_OK) return -1;
+  if (check_softmax_tokens(B, H_kv, G, n, true) != SATA_OK) return -1;
   return (int64_t)sizeof(float) * B * H_kv * G * n;
 }
 
@@ -1048,6 +1062,7 @@ sata_status sata_softmax_prefill(const void* q, const void* k, const void* v, sa
                                  int d_k, int d_v, const int32_t* lengths, void* y, float* lse, void* stream) {
   sata_status st = check_pair_args(dt, B, H_kv, G, n, d_k, d_v);
   if (st != SATA_OK) return st;
+  if ((st = check_softmax_tokens(B, H_kv, G, n, false)) != SATA_OK) return st;
   if (n == 0) return ok();
   if (!q || !k || !v || !y) return fail(SATA_ERR_INVALID_ARG, "null tensor pointer");
   const sata::SoftmaxArgs a{q, k, v, y, lse, lengths, B * H_kv, H_kv, G, n, d_k, d_v, pair_scale(d_k)};
@@ -1062,6 +1077,7 @@ sata_status sata_softmax_backward(const void* q, const void* k, const void* v, c
                                   void* stream) {
   sata_status st = check_pair_args(dt, B, H_kv, G, n, d_k, d_v);
   if (st != SATA_OK) return st;
+  if ((st = check_softmax_tokens(B, H_kv, G, n, true)) != SATA_OK) return st;
   if (n == 0) return ok();
   if (!q || !k || !v || !y || !lse || !dy || !dq || !dk || !dv) return fail(SATA_ERR_INVALID_ARG, "null tensor pointer");
   if ((st = check_scratch(scratch, sizeof(float) * (size_t)B * H_kv * G * n)) != SATA_OK) return st;

@@ -513,3 +513,31 @@ def test_token_of_wide_groups(sata, G, dv, cap, end):
     torch.cuda.synchronize()
     pair_ref.check(y, ry, "y")
     assert torch.equal(K.cpu(), rK) and torch.equal(V.cpu(), rV)
+
+
+def test_as_many_tokens_as_a_launch_holds(sata):
+    """The largest prompts and gradients by their number of heads and tokens: a sequence of 70 tokens in the
+    last head, none elsewhere."""
+    _say("softmax, the largest launches")
+    end, n = 70, 1 << 21
+    for H, grads in ((953, False), (476, True)):
+        last = _prompt(36, 1, 1, 1, end, 1, 1, "bf16")
+        q, k, v, dy = (torch.zeros(H, 1, n, 1, dtype=torch.bfloat16, device="cuda") for _ in range(4))
+        for x, part in zip((q, k, v, dy), last):
+            x[-1:, :, :end] = part
+        lens = torch.zeros(H, dtype=torch.int32, device="cuda")
+        lens[-1] = end
+        y, lse = sata.softmax_prefill(q, k, v, lens)
+        torch.cuda.synchronize()
+        ref_y, ref_lse = pair_ref.softmax_prefill(*last[:3])
+        pair_ref.check(y[-1:, :, :end], ref_y, "y")
+        pair_ref.check(lse[-1:, :, :end], ref_lse, "lse")
+        assert not y[-1, :, end:].any() and not y[0].any() and torch.isneginf(lse[-1, :, end:]).all()
+        if not grads:
+            continue
+        got = sata.softmax_backward(q, k, v, y, lse, dy, lens)
+        torch.cuda.synchronize()
+        want = pair_ref.softmax_backward(*last[:3], y[-1:, :, :end], lse[-1:, :, :end], last[3])
+        for name, a, w in zip(("dq", "dk", "dv"), got, want):
+            pair_ref.check(a[-1:, :, :end], w, name)
+            assert not a[-1, :, end:].any() and not a[0].any()

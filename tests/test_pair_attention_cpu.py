@@ -193,6 +193,26 @@ def test_pointers_refused(lib):
     assert lib.sata_softmax_backward(N, N, N, N, N, N, *empty, N, N, N, N, N, N) == 0
 
 
+def test_more_tokens_than_a_launch_holds(lib):
+    """A launch has fewer than 2^32 threads; softmax prompts take two a query and gradients four a key."""
+    F, N = FAKE, NULL
+    big = 2 ** 21
+    prompt = lambda B, H, G, n: lib.sata_softmax_prefill(F, F, F, 1, B, H, G, n, 1, 1, N, N if n == 0 else F, F, N)  # noqa: E731
+    # (null scratch: refused next, so that nothing is launched)
+    grads = lambda B, H, G, n: lib.sata_softmax_backward(F, F, F, F, F, F, 1, B, H, G, n, 1, 1, N, F, F, F, N, N)  # noqa: E731
+    too_large = lambda got: got == -3 and "tokens" in lib.sata_last_error().decode()  # noqa: E731
+    for B, H, G, n in ((1, 954, 1, big), (2, 10, 100, 1000001), (65535, 1, 1, 30519), (5, 1, 13107, 32768)):
+        assert B * H * G * n > 2 * 10 ** 9 and too_large(prompt(B, H, G, n)) and too_large(grads(B, H, G, n))
+        assert lib.sata_softmax_backward_scratch(B, H, G, n) == -1
+    for B, H, G, n in ((1, 477, 1, big), (500, 2, 2, 1000001), (65535, 1, 1, 15260)):
+        assert B * H * n > 10 ** 9 and too_large(grads(B, H, G, n))
+        assert lib.sata_softmax_backward_scratch(B, H, G, n) == -1
+    for B, H, G, n in ((1, 476, 2, big), (1, 1, 953, big), (65535, 1, 1, 15258)):
+        assert B * H * n <= 10 ** 9 and B * H * G * n <= 2 * 10 ** 9
+        assert grads(B, H, G, n) == -1 and "scratch" in lib.sata_last_error().decode()
+        assert lib.sata_softmax_backward_scratch(B, H, G, n) == 4 * B * H * G * n
+
+
 def test_states_that_alias(lib):
     """One workgroup would write dS_in while another reads S_in or dS."""
     F, N = FAKE, NULL
