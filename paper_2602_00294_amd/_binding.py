@@ -455,6 +455,13 @@ def decode_step_grouped(S, q, k, v, P: int, y=None):
 
 # ------------------------------------------------------------------ decay and softmax attention
 
+def _check_sizes(*sizes):
+    """ctypes hands the library the low 32 bits of a size, whatever it is."""
+    for size in sizes:
+        if size >= 1 << 31:
+            raise ValueError(f"a size of {size} does not fit in 32 bits")
+
+
 def _prompt_sizes(q, k, v):
     """(dtype code, B, H_kv, G, n, d_k, d_v) of q [B, G*H_kv, n, d_k], k [B, H_kv, n, d_k], v [B, H_kv, n, d_v]."""
     code = _dtype_code(q)
@@ -467,6 +474,7 @@ def _prompt_sizes(q, k, v):
         raise ValueError("the query head count must be a multiple of the key/value head count")
     _check_shape(k, "k", (B, Hkv, n, dk))
     _check_shape(v, "v", (B, Hkv, n, dv))
+    _check_sizes(B, Hq, n, dk, dv)
     return code, B, Hkv, Hq // Hkv, n, dk, dv
 
 
@@ -482,6 +490,7 @@ def _token_sizes(q, k, v):
         raise ValueError("the query head count must be a multiple of the key/value head count")
     _check_shape(k, "k", (B, Hkv, dk))
     _check_shape(v, "v", (B, Hkv, dv))
+    _check_sizes(B, Hq, dk, dv)
     return code, B, Hkv, Hq // Hkv, dk, dv
 
 
@@ -618,6 +627,7 @@ def softmax_step(K, V, lengths, q, k, v, y=None):
     if K.dim() != 4:
         raise ValueError("K must be [B, H_kv, capacity, d_k]")
     cap = K.shape[2]
+    _check_sizes(cap)
     _check_shape(K, "K", (B, H, cap, dk))
     _check_shape(V, "V", (B, H, cap, dv))
     _check_as(lengths, "lengths", torch.int32, (B,))

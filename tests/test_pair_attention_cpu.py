@@ -324,3 +324,26 @@ class TestBindingRefuses:
             bnd.softmax_step(K[0], V, at, q, k, v)
         with pytest.raises(ValueError, match="GPU"):
             bnd.softmax_step(K, V, at, q, k, v)
+
+    def test_sizes_beyond_32_bits(self):
+        """They would reach the library cut to their low 32 bits: 2^32 + 4 tokens would be taken for 4."""
+        far = 2 ** 32 + 4
+        long = lambda *s: torch.zeros(1, dtype=torch.bfloat16).expand(*s)  # noqa: E731
+        f32 = lambda *s: torch.zeros(1).expand(*s)  # noqa: E731
+        at = torch.zeros(1, dtype=torch.int32)
+        sizes = [(1, 1, far, 1, 1), (1, far, 1, 1, 1), (1, 1, 1, far, 1), (1, 1, 1, 1, far), (far, 1, 1, 1, 1)]
+        for B, H, n, dk, dv in sizes:
+            q, k, v, y = long(B, H, n, dk), long(B, H, n, dk), long(B, H, n, dv), long(B, H, n, dv)
+            g, lse = f32(H), f32(B, H, n)
+            for call in (lambda: bnd.decay_prefill(q, k, v, g), lambda: bnd.decay_backward(q, k, v, g, y),
+                         lambda: bnd.softmax_prefill(q, k, v), lambda: bnd.softmax_backward(q, k, v, y, lse, y)):
+                with pytest.raises(ValueError, match="32 bits"):
+                    call()
+            if n == 1:
+                t = [x[:, :, 0] for x in (q, k, v)]
+                with pytest.raises(ValueError, match="32 bits"):
+                    bnd.decay_step(f32(B, H, dk, dv), *t, g)
+                with pytest.raises(ValueError, match="32 bits"):
+                    bnd.softmax_step(long(B, H, 9, dk), long(B, H, 9, dv), at.expand(B), *t)
+        with pytest.raises(ValueError, match="32 bits"):
+            bnd.softmax_step(long(1, 1, far, 4), long(1, 1, far, 4), at, *(long(1, 1, 4) for _ in range(3)))
