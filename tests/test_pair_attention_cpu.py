@@ -347,3 +347,26 @@ class TestBindingRefuses:
                     bnd.softmax_step(long(B, H, 9, dk), long(B, H, 9, dv), at.expand(B), *t)
         with pytest.raises(ValueError, match="32 bits"):
             bnd.softmax_step(long(1, 1, far, 4), long(1, 1, far, 4), at, *(long(1, 1, 4) for _ in range(3)))
+
+
+def test_the_stream_without_torchs_private_function(monkeypatch):
+    """The current stream's handle is the same whether or not this torch has the function that gives it directly."""
+    class Stream:
+        def __init__(self, device):
+            self.cuda_stream = 1000 + device
+
+    handed = []
+
+    class Library:
+        def call(self, *args):
+            handed.append(args)
+            return 0
+
+    monkeypatch.setattr(torch.cuda, "current_stream", Stream)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 3)
+    monkeypatch.setattr(bnd, "load_library", Library)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda index: 2000 + index, raising=False)
+    bnd._invoke("call", torch.device("cuda", 3), 7)
+    monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream")
+    bnd._invoke("call", torch.device("cuda", 3), 7)
+    assert handed == [(7, 2003), (7, 1003)]
