@@ -33,6 +33,11 @@ sata_status sata_testing_scan_route(sata_dtype dt, int B, int H_kv, int n, int d
 sata_status sata_testing_backward_route(sata_dtype dt, int B, int H, int n, int d_k, int d_v, int P, int chunk,
                                         sata_route* route);
 
+/* Into how many parts sata_decay_prefill, or sata_decay_backward (gradients != 0), cuts a
+ * sequence, and their tokens (host only; the calls' own validation). */
+sata_status sata_testing_decay_parts(int gradients, sata_dtype dt, int B, int H_kv, int G, int n, int d_k, int d_v,
+                                     int* parts, int* part_len);
+
 /* sata_prefill_grouped and sata_backward pair by pair (pairs != 0;
  * SATA_ERR_UNSUPPORTED where those kernels do not cover the shape) or by the
  * scans (pairs = 0), whatever the estimates say. */

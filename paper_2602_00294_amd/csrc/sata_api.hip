@@ -992,6 +992,17 @@ int64_t sata_softmax_step_scratch(int B, int H_kv, int G, int capacity, int d_v)
                            sata::plan_softmax_step(false, B * H_kv, H_kv, G, capacity, d_v).bytes);
 }
 
+sata_status sata_testing_decay_parts(int gradients, sata_dtype dt, int B, int H_kv, int G, int n, int d_k, int d_v,
+                                     int* parts, int* part_len) {
+  sata_status st = check_pair_args(dt, B, H_kv, G, n, d_k, d_v);
+  if (st != SATA_OK) return st;
+  if (!parts || !part_len) return fail(SATA_ERR_INVALID_ARG, "null result pointer");
+  const sata::DecayScanPlan plan = sata::plan_decay_scan(dt == SATA_BF16, B * H_kv, G, n, d_k, d_v, gradients ? 3 : 1);
+  *parts = plan.parts;
+  *part_len = plan.part_len;
+  return ok();
+}
+
 sata_status sata_decay_prefill(const void* q, const void* k, const void* v, const float* log_decay, sata_dtype dt, int B,
                                int H_kv, int G, int n, int d_k, int d_v, const int32_t* lengths, const float* S_in,
                                void* y, float* S_out, void* scratch, void* stream) {

@@ -12,6 +12,7 @@ def _lib():
     lib.sata_testing_prefill_route.argtypes = [_I] * 10 + [ctypes.POINTER(_I)]
     lib.sata_testing_scan_route.argtypes = [_I] * 8 + [ctypes.POINTER(_I)]
     lib.sata_testing_backward_route.argtypes = [_I] * 8 + [ctypes.POINTER(_I)]
+    lib.sata_testing_decay_parts.argtypes = [_I] * 8 + [ctypes.POINTER(_I)] * 2
     lib.sata_testing_prefill.argtypes = [_I] + [_VP] * 3 + [_I] * 9 + [_VP] * 3
     lib.sata_testing_backward.argtypes = [_I] + [_VP] * 4 + [_I] * 8 + [_VP] * 4
     return lib
@@ -79,3 +80,11 @@ def backward_by(pairs, q, k, v, dy, P, chunk=64):
     _check(_lib().sata_testing_backward(int(pairs), _p(q), _p(k), _p(v), _p(dy), int(q.dtype == torch.bfloat16), B, H,
                                         n, dk, dv, P, chunk, *(_p(t) for t in out), _stream()))
     return out
+
+
+def decay_parts(gradients, dtype, B, H_kv, G, n, dk, dv):
+    """(parts, tokens of a part) of sata.decay_prefill or decay_backward (host only)."""
+    parts, part_len = _I(-1), _I(-1)
+    _check(_lib().sata_testing_decay_parts(int(gradients), int(dtype == "bf16"), B, H_kv, G, n, dk, dv,
+                                           ctypes.byref(parts), ctypes.byref(part_len)))
+    return parts.value, part_len.value

@@ -8,6 +8,7 @@ import sys
 import pytest
 
 import pair_ref
+import routes
 
 pytestmark = pytest.mark.gpu
 
@@ -319,3 +320,52 @@ def test_a_decay_that_is_no_number(sata, dtype, n, lengths):
     torch.cuda.synchronize()
     same("token's y", y, ry)
     same("token's S", S_in, rS)
+
+
+PARTS = [  # dtype, B, H, G, n, dk, dv: sequences in several parts of several chunks, of more than 8 heads
+    ("bf16", 3, 3, 2, 1600, 128, 128), ("bf16", 2, 9, 1, 1000, 96, 96), ("bf16", 2, 20, 2, 900, 96, 72),
+    ("f32", 4, 16, 1, 600, 128, 100), ("bf16", 2, 25, 1, 500, 96, 96), ("f32", 2, 9, 1, 700, 64, 64),
+    ("bf16", 3, 40, 1, 600, 32, 32), ("bf16", 4, 16, 1, 1200, 96, 96),
+]
+
+
+@pytest.mark.parametrize("dtype,B,H,G,n,dk,dv", PARTS)
+@pytest.mark.parametrize("offset", [0, 1])
+def test_parts_of_several_chunks(sata, dtype, B, H, G, n, dk, dv, offset):
+    """Lengths that end inside a chunk, at a part's border and in a part in the middle; decays that take the state's
+    unit below 2^-8 never, in each chunk and after some chunks of a part."""
+    plans = [routes.decay_parts(gradients, dtype, B, H, G, n, dk, dv) for gradients in (False, True)]
+    _say("decay in parts", dtype, B, H, G, n, dk, dv, plans, offset)
+    length = max(length for parts, length in plans if parts > 1)
+    assert length >= 64 and B * H > 8
+    q, k, v, dy, S_in, dS, _ = _make(n + dv, B, H, G, n, dk, dv, dtype, offset)
+    rates = [0.0, -0.02, -0.1, -0.7, -1e-4, -0.06, -25.0, -math.inf]
+    g = torch.tensor([rates[h % 8] for h in range(H)], device="cuda")
+    for lengths in (None, [n - 7, length * 2 + 37, length, 0][:B]):
+        y, S = sata.decay_prefill(q, k, v, g, _lengths(lengths), S_in)
+        got = sata.decay_backward(q, k, v, g, dy, _lengths(lengths), S_in, dS)
+        torch.cuda.synchronize()
+        ry, rS = pair_ref.decay_prefill(q, k, v, g, lengths, S_in)
+        worst = [pair_ref.check(y, ry, "y"), pair_ref.check(S, rS, "S")]
+        worst += [pair_ref.check(a, w, name) for name, a, w in
+                  zip(("dq", "dk", "dv", "dS_in"), got, pair_ref.decay_backward(q, k, v, g, dy, lengths, S_in, dS))]
+        _say("  of the bounds: y, S, dq, dk, dv, dS_in", ["%.3f" % x for x in worst])
+        if offset:
+            break
+
+
+@pytest.mark.parametrize("dk,dv", [(96, 96), (72, 96), (96, 65)])
+@pytest.mark.parametrize("offset", [0, 1])
+def test_three_tiles_of_columns(sata, dk, dv, offset):
+    """d of 65 to 96 in bfloat16: a staging pass covers 12 rows, the third one more than the tile has."""
+    _say("decay, three tiles of columns", dk, dv, offset)
+    n, lengths = 203, [203, 97]
+    q, k, v, dy, S_in, dS, g = _make(dk + dv, 2, 6, 2, n, dk, dv, "bf16", offset)
+    y, S = sata.decay_prefill(q, k, v, g, _lengths(lengths), S_in)
+    got = sata.decay_backward(q, k, v, g, dy, _lengths(lengths), S_in, dS)
+    torch.cuda.synchronize()
+    ry, rS = pair_ref.decay_prefill(q, k, v, g, lengths, S_in)
+    pair_ref.check(y, ry, "y")
+    pair_ref.check(S, rS, "S")
+    for name, a, w in zip(("dq", "dk", "dv", "dS_in"), got, pair_ref.decay_backward(q, k, v, g, dy, lengths, S_in, dS)):
+        pair_ref.check(a, w, name)
