@@ -246,6 +246,22 @@ def softmax_step(K, V, lengths, q, k, v):
     return (y, yb), K, V
 
 
+def one_entry_a_row(seed, n, dk, dv):
+    """q, k, v, dy [1, 1, n, d] in bfloat16 with one entry a row, in column t % d, so that an element of a result is a sum of
+    about n / d terms.  q and dy grow with t as the weights shrink, so that all terms of a sum are of
+    like size: one that is left out, or one too many, is then well beyond 2^-8 of their sum."""
+    g = torch.Generator().manual_seed(seed)
+    t = torch.arange(n)
+
+    def make(d, low, high, grow):
+        a = (torch.rand(n, generator=g) * (high - low) + low) * (torch.randint(0, 2, (n,), generator=g) * 2 - 1)
+        x = torch.zeros(n, d)
+        x[t, t % d] = a * (t + 1) / grow if grow else a
+        return x.bfloat16()[None, None]
+
+    return make(dk, 0.5, 1.0, 16), make(dk, 0.125, 0.25, 0), make(dv, 0.5, 2.0, 0), make(dv, 0.5, 2.0, 64)
+
+
 def check(got, ref, label=""):
     """Every element of a result within its bound (infinities equal)."""
     value, bound = ref

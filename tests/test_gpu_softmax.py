@@ -541,3 +541,81 @@ def test_as_many_tokens_as_a_launch_holds(sata):
         for name, a, w in zip(("dq", "dk", "dv"), got, want):
             pair_ref.check(a[-1:, :, :end], w, name)
             assert not a[-1, :, end:].any() and not a[0].any()
+
+
+@pytest.mark.parametrize("heads,n,d", [(1, 600, 128), (60, 600, 128), (180, 600, 128), (1, 600, 64), (60, 600, 64),
+                                       (180, 600, 64), (1, 300, 32), (100, 300, 32), (260, 300, 32)])
+def test_one_entry_a_row(sata, heads, n, d):
+    """Inputs whose bounds feel every single key and query in bfloat16: few workgroups, four and eight waves."""
+    _say("softmax, one entry a row", heads, n, d)
+    one = pair_ref.one_entry_a_row(1, n, d, d)
+    q, k, v, dy = (x.cuda().expand(1, heads, n, d).contiguous() for x in one)
+    y, lse = sata.softmax_prefill(q, k, v)
+    grads = sata.softmax_backward(q, k, v, y, lse, dy)
+    torch.cuda.synchronize()
+    ref_y, ref_lse = pair_ref.softmax_prefill(*one[:3])
+    pair_ref.check(y[:, :1], ref_y, "y")
+    pair_ref.check(lse[:, :1], ref_lse, "lse")
+    want = pair_ref.softmax_backward(*one[:3], y[:, :1], lse[:, :1], one[3])
+    for name, a, w in zip(("dq", "dk", "dv"), grads, want):
+        pair_ref.check(a[:, :1], w, name)
+    for x in (y, lse, *grads):  # all heads hold the same
+        assert torch.equal(x, x[:, :1].expand_as(x))
+
+
+@pytest.mark.parametrize("end", [31, 127, 128, 2047, 2900])
+def test_token_of_one_entry_a_row(sata, end):
+    """Nearly equal weights over values of one entry a row: a row of the cache lost or read twice is felt."""
+    _say("softmax token, one entry a row", end)
+    K, q, k = _rand(37, "bf16", (1, 2, 3000, 128), (1, 2, 128), (1, 2, 128))
+    q *= 2.0 ** -6
+    rows = pair_ref.one_entry_a_row(2, end + 1, 128, 128)[2].cuda()
+    V = torch.full((1, 2, 3000, 128), math.nan, dtype=torch.bfloat16, device="cuda")
+    V[:, :, :end] = rows[:, :, :end]
+    v = rows[:, :, end].expand(1, 2, 128).contiguous()
+    ref, _, _ = pair_ref.softmax_step(K, V, [end], q, k, v)
+    # a weight is near 1 / (end + 1), the least entry 1/2, and the bound below that: a row more or less is beyond it
+    assert ref[1].max() < 0.4 / (end + 1)
+    y = sata.softmax_step(K, V, _lengths([end]), q, k, v)
+    torch.cuda.synchronize()
+    pair_ref.check(y, ref, "y")
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_values_that_are_not_finite_by_eight_waves(sata, bad):
+    test_values_that_are_not_finite(sata, "bf16", bad, 256, 1)
+
+
+@pytest.mark.parametrize("at", [100, 255, 256, 300])
+def test_not_finite_in_later_blocks_of_eight_waves(sata, at):
+    """NaN in the first or a later block of 256 rows, whose keys other blocks see whole."""
+    _say("softmax by eight waves, NaN at", at)
+    H, n = 256, 330
+    q, k, v, dy = _prompt(38, 1, H, 1, n, 40, 24, "bf16")
+    y, lse = sata.softmax_prefill(q, k, v)
+    grads = sata.softmax_backward(q, k, v, y, lse, dy)
+    ry, rl = pair_ref.softmax_prefill(q[:, :1], k[:, :1], v[:, :1])
+    rg = pair_ref.softmax_backward(q[:, :1], k[:, :1], v[:, :1], y[:, :1], lse[:, :1], dy[:, :1])
+    cut = lambda ref, rows: tuple(x[:, :, rows] for x in ref)  # noqa: E731
+    before, behind = slice(0, at), slice(at + 1, n)
+    for x in (1, 2):
+        args = [q, k.clone(), v.clone()]
+        args[x][0, 0, at, 3] = math.nan
+        y2, lse2 = sata.softmax_prefill(*args)
+        dq = sata.softmax_backward(*args, y2, lse2, dy)[0]
+        torch.cuda.synchronize()
+        for a, was in ((y2, y), (lse2, lse), (dq, grads[0])):
+            assert torch.equal(a[:, 1:], was[:, 1:])
+        pair_ref.check(y2[:, :1, before], cut(ry, before), "y")
+        pair_ref.check(lse2[:, :1, before], cut(rl, before), "lse")
+        pair_ref.check(dq[:, :1, before], cut(rg[0], before), "dq")
+        assert torch.isnan(y2[0, 0, at:]).any(1).all() and torch.isnan(dq[0, 0, at:]).any(1).all()
+    for x in (0, 1):
+        args = [q.clone(), dy.clone()]
+        args[x][0, 0, at, 3] = math.nan
+        got = sata.softmax_backward(args[0], k, v, y, lse, args[1])
+        torch.cuda.synchronize()
+        for name, a, was, ref in zip(("dk", "dv"), got[1:], grads[1:], rg[1:]):
+            assert torch.equal(a[:, 1:], was[:, 1:])
+            pair_ref.check(a[:, :1, behind], cut(ref, behind), name)
+        assert torch.isnan(got[1][0, 0, :at + 1]).any(1).all() and torch.isnan(got[2][0, 0, :at + 1]).any(1).all()

@@ -128,6 +128,29 @@ def test_gradients_by_differences(which):
             assert abs((moved[0] - moved[1]) / (2 * step) - gx.reshape(-1)[j].item()) < 1e-7, (which, at, j)
 
 
+@pytest.mark.parametrize("n,d", [(600, 128), (600, 64), (300, 32)])
+def test_bfloat16_bounds_feel_every_pair(n, d):
+    """With one entry a row the bounds of bfloat16 results tell a key lost, or one seen too early, at any place of
+    any row: for dv every pair of a query and a key, for the others all but a few, where a row's few keys hold nearly the
+    same as the one lost or added, or a pair's term is nearly zero."""
+    q, k, v, dy = pair_ref.one_entry_a_row(1, n, d, d)
+    (y, y_bound), (lse, _) = pair_ref.softmax_prefill(q, k, v)
+    grads = pair_ref.softmax_backward(q, k, v, y.bfloat16(), lse.float(), dy)
+    Q, K, V, Y = (x[0, 0].double() for x in (q, k, v, dy))
+    t, c = torch.arange(n), 1 / math.sqrt(d)
+    col = t % d
+    p = torch.exp(Q @ K.T * c - lse[0, 0][:, None])
+    # a row without its key s, or with one behind it: the weights of the others change with it
+    was, add = y[0, 0][:, col], V[t, col]
+    now = torch.where(t[:, None] >= t[None, :], (was - p * add) / (1 - p), (was + p * add) / (1 + p))
+    now[0, 0] = math.inf  # (a row without its only key)
+    assert ((now - was).abs() > y_bound[0, 0][:, col]).double().mean() > 0.9999
+    e = c * p * (Y @ V.T - (Y * y[0, 0]).sum(1, keepdim=True))
+    felt = [((term.abs() > bound[0, 0][:, col]).double().mean().item())
+            for term, (_, bound) in zip((e * K[t, col], e.T * Q[t, col], p.T * Y[t, col]), grads)]
+    assert felt[0] > 0.999 and felt[1] > 0.96 and felt[2] == 1.0, felt
+
+
 # ------------------------------------------------------------------ refusals
 
 SIZES = [  # (dtype, B, H_kv, G, n, d_k, d_v), status
