@@ -261,15 +261,19 @@ struct TileStage {
       r[i] = STREAM ? read.stream(at) : read(at);
     }
   }
+  template <bool FAR>
+  __device__ static __forceinline__ void put_planes(u16* dst, float f) {
+#pragma unroll
+    for (int i = 0; i < L::kPl; ++i) {
+      const uint32_t b = pack2(FAR ? far_part(f, i) : f, 0.f);
+      dst[i * L::kPlane] = (u16)b;
+      f -= lo_f32(b);
+    }
+  }
   __device__ static void put_entry(u16* dst, T x) {
     if constexpr (sizeof(T) == 4) {
-      float f = x;
-#pragma unroll
-      for (int i = 0; i < L::kPl; ++i) {
-        const uint32_t b = pack2(far_part(f, i), 0.f);
-        dst[i * L::kPlane] = (u16)b;
-        f -= lo_f32(b);
-      }
+      put_planes<false>(dst, x);
+      if (__builtin_expect(fabsf(x) > kLargestBf16, 0)) put_planes<true>(dst, x);  // (once more)
     } else {
       dst[0] = x;
     }
@@ -309,12 +313,25 @@ struct TileStage {
         if (__builtin_expect(most > kLargestBf16, 0)) put_vectors<true>(t);  // (once more)
       }
     } else {
+      if (put_entries<false>(t, r0) > kLargestBf16) put_entries<true>(t, r0);  // (once more)
+    }
+  }
+  // the same entry by entry; the largest size (float32)
+  template <bool FAR>
+  __device__ __forceinline__ float put_entries(u16* t, int r0) const {
+    float most = 0.f;
 #pragma unroll 1
-      for (int i = tid; i < ROWS * 32 * ND; i += THREADS) {
-        const int row = i / (32 * ND), col = i % (32 * ND);
-        put_entry(t + L::at(row, col), r0 + row < rows && col < width ? base[(int64_t)(r0 + row) * width + col] : (T)0);
+    for (int i = tid; i < ROWS * 32 * ND; i += THREADS) {
+      const int row = i / (32 * ND), col = i % (32 * ND);
+      const T x = r0 + row < rows && col < width ? base[(int64_t)(r0 + row) * width + col] : (T)0;
+      if constexpr (sizeof(T) == 4) {
+        put_planes<FAR>(t + L::at(row, col), x);
+        most = fmaxf(most, fabsf(x));
+      } else {
+        put_entry(t + L::at(row, col), x);
       }
     }
+    return most;
   }
 };
 
