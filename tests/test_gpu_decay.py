@@ -369,3 +369,23 @@ def test_three_tiles_of_columns(sata, dk, dv, offset):
     pair_ref.check(S, rS, "S")
     for name, a, w in zip(("dq", "dk", "dv", "dS_in"), got, pair_ref.decay_backward(q, k, v, g, dy, lengths, S_in, dS)):
         pair_ref.check(a, w, name)
+
+
+@pytest.mark.parametrize("B,H,G,n,dk,dv,lengths", [(1, 6, 2, 300, 64, 64, None), (2, 9, 1, 700, 128, 100, [700, 333]),
+                                                   (2, 3, 2, 190, 24, 40, [190, 1])])
+def test_bfloat16_sums_carry_sixteen_bits(sata, monkeypatch, B, H, G, n, dk, dv, lengths):
+    """Sums of signed terms cancel, so the weights and the state's entries of bfloat16 calls are two bfloat16
+    numbers each, 2^-17 of them off, not one; what is rounded to bfloat16 is the result."""
+    _say("decay, sixteen bits", B, H, G, n, dk, dv, lengths)
+    monkeypatch.setitem(pair_ref.WEIGHT, torch.bfloat16, 2.0 ** -17)
+    q, k, v, dy, S_in, dS, g = _make(n + dk, B, H, G, n, dk, dv, "bf16")
+    S_in[:, :, ::2] += 1000.0  # (large entries that cancel in the readout)
+    S_in[:, :, 1::2] -= 1000.0
+    y, S = sata.decay_prefill(q, k, v, g, _lengths(lengths), S_in)
+    got = sata.decay_backward(q, k, v, g, dy, _lengths(lengths), S_in, dS)
+    torch.cuda.synchronize()
+    ry, rS = pair_ref.decay_prefill(q, k, v, g, lengths, S_in)
+    pair_ref.check(y, ry, "y")
+    pair_ref.check(S, rS, "S")
+    for name, a, w in zip(("dq", "dk", "dv", "dS_in"), got, pair_ref.decay_backward(q, k, v, g, dy, lengths, S_in, dS)):
+        pair_ref.check(a, w, name)
