@@ -151,9 +151,9 @@ __device__ __forceinline__ f32x16 dot_rows32(const u16* t, int r0, const uint4 (
   return s;
 }
 
-// acc[j] += (rows r0 .. r0 + 31 of the tile, columns 32 j .. +31)^T times the 32 x 32 weights w.
-template <typename L, int ND>
-__device__ __forceinline__ void contract32(const u16* t, int r0, const uint4 (&w)[2][L::kPl], f32x16 (&acc)[ND]) {
+// acc[j] += (rows r0 .. r0 + 31 of the tile, columns 32 j .. +31)^T times the 32 x 32 weights w (of PW numbers each).
+template <typename L, int ND, int PW>
+__device__ __forceinline__ void contract32(const u16* t, int r0, const uint4 (&w)[2][PW], f32x16 (&acc)[ND]) {
 #pragma unroll
   for (int j = 0; j < ND; ++j)
 #pragma unroll

@@ -15,6 +15,11 @@
 // with all caches full (537 MB) 91 us (5.92 TB/s), 104; all a quarter full 31 us, 62; one
 // sequence of 131072 rows 93 us, 159.
 // Loads are streamed: an earlier form took 62 us with and 70 without.
+//
+// Precision: scores, statistics and sums are float32; a weight is two bfloat16 numbers for its product with v in
+// bfloat16 calls (three in float32 ones).  With one, outputs were 0.0023 off the exact ones, relative,
+// instead of 0.0017, the rounding of the outputs; the second number costs 55.7 -> 56.4 us
+// of the case above, at most 5% of others.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -66,11 +71,33 @@ __device__ __forceinline__ int step_stretch(const SoftmaxStepArgs& a, const Soft
   return max(p.least, 2 * ((all + most - 1) / most));
 }
 
+// Weights x >= 0 as two bfloat16 numbers, 2^-15 of them off at most, both above zero where x is (from 2^-117 on): an
+// infinite v times either is the same infinity (a second number below zero, or zero, would make NaN of it).  The
+// first is x less 2^-9 of it, cut off; what is left is at least that 2^-9.
+__device__ __forceinline__ void to_positive_pairs(const float (&x)[16], uint4 (&op)[2][2]) {
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    uint32_t first[4];
+    float rest[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t a = __float_as_uint(x[8 * s + 2 * i] * (1.f - 0x1p-9f));
+      const uint32_t b = __float_as_uint(x[8 * s + 2 * i + 1] * (1.f - 0x1p-9f));
+      first[i] = __builtin_amdgcn_perm(b, a, 0x07060302);
+      rest[2 * i] = x[8 * s + 2 * i] - __uint_as_float(a & 0xffff0000u);
+      rest[2 * i + 1] = x[8 * s + 2 * i + 1] - __uint_as_float(b & 0xffff0000u);
+    }
+    op[s][0] = uint4{first[0], first[1], first[2], first[3]};
+    op[s][1] = to_bf16(rest);
+  }
+}
+
 // One head's rows [first, end) of a sequence with `at` rows and its new one.
 template <typename T, int ND>
 __device__ __forceinline__ void step_stretch_rows(const SoftmaxStepArgs& a, int64_t kvh, int block, int at, int first, int end,
                                            float* part, u16* smem16, StepState (*state)[32]) {
   using L = PairTile<T, ND, 32>;
+  constexpr int kWeight = sizeof(T) == 2 ? 2 : 3;  // numbers of a weight
   const int tid = threadIdx.x, lane = tid & 63, l31 = lane & 31, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int dk = a.dk_, dv = a.dv_;
@@ -144,8 +171,9 @@ __device__ __forceinline__ void step_stretch_rows(const SoftmaxStepArgs& a, int6
       z[i] = exp2_fast(fmaf(s[i], c, -top));
       sum += z[i];
     }
-    uint4 w[2][L::kPl];
-    to_planes<L::kPl>(z, w);
+    uint4 w[2][kWeight];
+    if constexpr (kWeight == 2) to_positive_pairs(z, w);
+    else to_planes<3>(z, w);
     contract32<L, ND>(tile, 0, w, o);
   }
   settle_mfma32();

@@ -619,3 +619,17 @@ def test_not_finite_in_later_blocks_of_eight_waves(sata, at):
             assert torch.equal(a[:, 1:], was[:, 1:])
             pair_ref.check(a[:, :1, behind], cut(ref, behind), name)
         assert torch.isnan(got[1][0, 0, :at + 1]).any(1).all() and torch.isnan(got[2][0, 0, :at + 1]).any(1).all()
+
+
+@pytest.mark.parametrize("B,H,G,cap,dk,dv,lengths", [(2, 2, 4, 300, 128, 128, [299, 100]), (1, 2, 3, 5000, 64, 40, [4321]),
+                                                     (3, 2, 33, 700, 33, 100, [650, 3, 0])])
+def test_token_weights_carry_fifteen_bits(sata, monkeypatch, B, H, G, cap, dk, dv, lengths):
+    """A token's weights are two bfloat16 numbers in bfloat16 calls: cut off below 2^-7 + 2^-9 of the weight and then
+    rounded by 2^-9 of that rest, 2^-15.6 in all."""
+    _say("softmax token, fifteen bits", B, H, G, cap, dk, dv, lengths)
+    monkeypatch.setitem(pair_ref.WEIGHT, torch.bfloat16, 2.0 ** -15)
+    K, V, q, k, v = _rand(cap + 1, "bf16", (B, H, cap, dk), (B, H, cap, dv), (B, H * G, dk), (B, H, dk), (B, H, dv))
+    ry, _, _ = pair_ref.softmax_step(K, V, lengths, q, k, v)
+    y = sata.softmax_step(K, V, _lengths(lengths), q, k, v)
+    torch.cuda.synchronize()
+    pair_ref.check(y, ry, "y")
