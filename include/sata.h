@@ -291,6 +291,12 @@ sata_status sata_decode_step_grouped(float* S, const void* q, const void* k, con
  *    counts as in float32 arithmetic: a key whose score is minus infinity has no
  *    weight, and an infinite entry of v is an infinity in the outputs' column.  In
  *    the decay's sums the outputs and states that it reaches are infinite or NaN.
+ *  - float32 calls carry 24 bits throughout: inputs, weights, states and sums.  In bfloat16
+ *    calls states, scores, statistics and sums are float32 and outputs are rounded
+ *    once; the decay's weights and states enter products with 16 bits, a single softmax
+ *    token's weights with 15, and the weights of softmax prompts and gradients (p_ts and e_ts
+ *    below) are rounded to bfloat16 for them, which leaves outputs 0.002 off the exact
+ *    ones, relative, where their own rounding is 0.0017.  Pass float32 for more.
  *  - scratch: device memory for the call's own use, 16-byte aligned, of at least as many
  *    bytes as the query beside the call says (NULL where that is 0).  These calls allocate
  *    nothing, upload nothing and wait for nothing, so any of them may be the first

@@ -27,10 +27,10 @@ namespace {
 // and in reverse the same with lam^(m-1-r), lam^(s-r) and lam^(s+1).
 //
 // Bound: memory (a, b, w read and out written once) is the floor; what it runs at is the chain of a chunk, in
-// a wave 8 + 8 + 4 + 24 matrix instructions at d = 128 in bfloat16, some 360 vector instructions
-// and two barriers, with two waves a SIMD.  B = 8, H = 16, n = 8192, d = 128 in bfloat16: 438 us
-// (2.45 TB/s of 4.9), a third of it the sums; gradients of B = 8, H = 32, n = 2048, d = 64: 192 us
-// (2.4 TB/s).  Short prompts and few heads: a part's chunks one after the other, and the launches of the
+// a wave 16 + 8 + 4 + 24 matrix instructions at d = 128 in bfloat16, some 510 vector instructions
+// and two barriers, with two waves a SIMD.  B = 8, H = 16, n = 8192, d = 128 in bfloat16: 468 us
+// (2.33 TB/s of 4.9), 0.3 of it the sums; gradients of B = 8, H = 32, n = 2048, d = 64: 210 us
+// (2.24 TB/s).  Short prompts and few heads: a part's chunks one after the other, and the launches of the
 // sums and the carry.
 //
 // The state lies in units of f = lam^(tokens since ...): lam^m goes into f, which enters the readout's
@@ -40,7 +40,8 @@ namespace {
 // Precision: bfloat16 inputs are exact operands.  The pairs' weights inside a chunk and the state's entries
 // in their readout are two bfloat16 numbers, 2^-17 of them off, for the sums have terms of both signs, which may
 // cancel (with one number for the state's entries outputs were 0.0023 off the exact ones, relative,
-// instead of 0.0017, the rounding of the output, and the calls above took 436 and 192 us); what is
+// instead of 0.0017, the rounding of the output, and the calls above took 9% less: 437 us where these took
+// 481, 192 where 213); what is
 // added to the state carries 24 bits (w times its power as three), so that the state is a
 // float32 one.  float32 inputs, weights and states: three bfloat16 numbers each.
 constexpr int kChunk = 32;

@@ -513,10 +513,10 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 
 // Whether `heads` heads of n tokens make so few workgroups of 128 rows that sweeps are the longest thing in the
 // call, and a workgroup for every 32 rows, whose waves share one sweep, is faster.  Prompts / gradients in us,
-// that way and with workgroups of 128 rows or more, bfloat16 unless said: d = 64, 16 heads of 1000 tokens
-// 12.9 / 34 and 20.1 / 57, 16 of 2000 28 / 75 and 35 / 102, 32 of 2000 50 / 139 and 44 / 119; d = 128, 1 of 8000
-// 88 / 244 and 169 / 620, 16 of 1000 23 / 61 and 30 / 101, 16 of 2000 62 / 174 and 52 / 179, 128 of 128
-// 13.0 / 35 and 10.9 / 31; float32, d = 64, 16 of 1000 38 / 114 and 57 / 156, 16 of 2000 114 / 332 and 103 / 289.
+// that way and with workgroups of 128 rows or more (on one card in turn), bfloat16 unless said: d = 64, 16 heads of
+// 1000 tokens 13.6 / 35 and 20.2 / 58, 16 of 2000 29 / 76 and 34 / 102, 32 of 2000 50 / 140 and 36 / 118; d = 128, 1 of
+// 8000 86 / 241 and 168 / 592, 16 of 1000 23 / 62 and 30 / 95, 16 of 2000 62 / 178 and 51 / 169, 128 of 128
+// 12.8 / 37 and 11.0 / 30; float32, d = 64, 16 of 1000 41 / 118 and 60 / 162, 16 of 2000 119 / 345 and 108 / 300.
 template <typename T, int ND>
 inline bool few_sweeps(int64_t heads, int n) {
   return n > 128 && heads * ((n + 127) / 128) <= (sizeof(T) == 2 && ND <= 2 ? 256 : 128);
@@ -524,8 +524,8 @@ inline bool few_sweeps(int64_t heads, int n) {
 
 // Whether a bfloat16 call's workgroups take 256 rows, with eight waves, instead of 128: a staged tile serves
 // twice as many rows, but there have to be two rounds of workgroups for the card.  Prompts in us with eight
-// and four waves, d = 128: 32 heads of 8192 tokens (1024 workgroups) 548 and 586, 64 of 2000 (512) 90 and 91, 32
-// of 2000 (256) 67 and 57; gradients, rows of 256 and 128: 2220 and 2265, 337 and 337, 198 and 193.
+// and four waves (on one card in turn), d = 128: 32 heads of 8192 tokens (1024 workgroups) 569 and 608, 64 of 2000
+// (512) 89 and 91, 32 of 2000 (256) 66 and 57; gradients, rows of 256 and 128: 2255 and 2305, 336 and 339, 198 and 193.
 inline bool eight_waves(int64_t heads, int n) { return heads * ((n + 255) / 256) >= 512; }
 
 // Workgroups go to the 8 XCDs in turn.  With 8 heads or more each XCD takes whole

@@ -38,14 +38,16 @@ __device__ __forceinline__ void masked_rows(const T* k, int dk, const T* v, int 
 //
 // Bound: matrix instructions (4 ND a tile) and vector instructions (32 lanes' 16 weights: a multiply-add,
 // an exponential at a quarter of the rate, a sum, a maximum, half a conversion) in equal parts:
-// n = 8192, 32 heads of d = 128: 565 us (975 TFLOP/s; a large library product 1346), each busy 46% of the
+// n = 8192, 32 heads of d = 128: 566 us (971 TFLOP/s; a large library product 1346), each busy 46% of the
 // cycles.  Blocks that the whole workgroup sees go without branches, their tiles' products side
-// by side: 623 -> 565 us.  Half of the waves half a step behind the others: 586 us; waves of higher
-// priority in their products: no change; four waves instead of eight: 593 us.
+// by side: a tenth of the time less.  Half of the waves half a step behind the others: 4% more; waves of higher
+// priority in their products: no change; four waves instead of eight: see eight_waves.
 //
 // Precision: scores, statistics and sums are float32.  A bfloat16 call's weights are rounded to
 // bfloat16 for their product with v, as v's entries are (half a step each); their sum takes them
-// unrounded.  float32 ones are three bfloat16 numbers each.
+// unrounded.  As two numbers each they would take the outputs from 0.0022 off the exact ones, relative, to 0.0016, the
+// rounding of the outputs, and the case above from 570 to 771 us, 16 heads of 1000 with d = 64 from 13.6 to 14.4; they
+// are positive, so that nothing cancels.  float32 ones are three bfloat16 numbers each.
 template <typename T, int ND, int W>
 __global__ void __launch_bounds__(64 * W, sizeof(T) == 2 ? 2 : 1) softmax_prefill_kernel(SoftmaxArgs a, int blocks) {
   constexpr int kWaves = W, kThreads = 64 * W;

@@ -317,7 +317,11 @@ SoftmaxStepPlan plan_softmax_step(bool bf16, int heads, int H, int G, int capaci
   } else if (B > 384) {
     // (each workgroup reads all lengths, in steps of 64: us with stretches cut by them and by the capacity, 256 sequences
     // of 8 heads and up to 2048 rows 176 and 199, 300 of one of up to 4096 68 and 83, 1000 of one of up to 2048 112
-    // and 113, 512 of 8 of up to 1024 228 and 174, 2000 of 8 of up to 256 746 and 247)
+    // and 113, 512 of 8 of up to 1024 228 and 174, 2000 of 8 of up to 256 746 and 247.  In long caches, d = 64, lengths
+    // of all sizes / one sequence full among short ones: 400 of one of up to 131072 1506 / 45 and 1134 / 204, 400 of 8 of
+    // up to 32768 2143 / 74 and 2454 / 108, 1000 of one of up to 16384 400 / 40 and 396 / 50, 4000 of one of up to 32768
+    // 2593 / 342 and 3005 / 113: what the capacity loses where one sequence is much longer than the others it
+    // gains elsewhere, and it never takes the time of the full caches)
     const int most = std::min(8, std::max(4, (4 * p.places + count - 1) / count));
     p.fixed_len = std::max(8, (units + most - 1) / most);
   }
