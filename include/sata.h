@@ -374,6 +374,118 @@ sata_status sata_softmax_step(void* K, void* V, int capacity, const int32_t* len
                               const void* v, sata_dtype dt, int B, int H_kv, int G, int d_k, int d_v, void* y,
                               void* scratch, void* stream);
 
+/* ---- The gated delta rule ------------------------------------------------------
+ *
+ * Linear attention whose state overwrites what it holds under a key: for every
+ * value head, with a log decay g_t and a rate beta_t for each token,
+ *     S' = exp(g_t) S_{t-1},  u_t = beta_t (v_t - k_t S'),  S_t = S' + k_t (x) u_t,  y_t = c q_t S_t.
+ * The rules of the calls above hold (c, lengths, padding, sizes, scratch, streams and graphs), and:
+ *  - Value heads share queries and keys: q, k and their gradients are [B][H_qk][n][d_k]; v, y and theirs
+ *    [B][H_qk*G][n][d_v]; value head g + G*h reads query and key head h, whose gradients are sums over its
+ *    value heads.  Each value head has its state, its g and its beta:
+ *    g, beta and their gradients are [B][H_qk*G][n] float32.
+ *  - g at most 0, as a layer makes it; below -200 it counts as -200 (nothing of a state is left), NaN makes NaN of
+ *    what follows.  beta and the keys are the caller's to bound: a state grows where
+ *    beta |k|^2 exceeds 2, and then so do roundings.
+ *  - B*H_qk*G <= 65535, n <= 2^21, B*H_qk*G*n <= 1e9.
+ *  - Prompts: values that are not finite reach the outputs of their own token and of later ones of their heads, of v
+ *    in their own column only.  Gradients: where a
+ *    sequence holds one, all gradients of its heads may be NaN; other sequences and heads do not feel it.
+ *  - States and sums are float32 and carry 24 bits through every product also in bfloat16 calls, where
+ *    the outputs' own products take 16 and outputs are rounded once.  */
+
+/* Bytes of scratch (host only; -1 for sizes that the calls refuse) of sata_delta_prefill, or with
+ * gradients != 0 of sata_delta_backward. */
+int64_t sata_delta_scratch(int gradients, sata_dtype dt, int B, int H_qk, int G, int n, int d_k, int d_v);
+
+/*   S_in : [B][H_qk*G][d_k][d_v] float32 (device), the state before the first token, or NULL for zero
+ *   y    : [B][H_qk*G][n][d_v], dtype dt (device, written)
+ *   S_out: as S_in (device, written) or NULL: the state after each sequence's last token, for
+ *          sata_delta_step or as S_in of the tokens that follow.  Must not be S_in.
+ * n = 0 writes S_out alone. */
+sata_status sata_delta_prefill(const void* q, const void* k, const void* v, const float* g, const float* beta,
+                               sata_dtype dt, int B, int H_qk, int G, int n, int d_k, int d_v, const int32_t* lengths,
+                               const float* S_in, void* y, float* S_out, void* scratch, void* stream);
+
+/* One token of every sequence.
+ *   S: [B][H_qk*G][d_k][d_v] float32 (device, read and written in place)
+ *   q, k: [B][H_qk][d_k], v, y: [B][H_qk*G][d_v], g, beta: [B][H_qk*G] */
+sata_status sata_delta_step(float* S, const void* q, const void* k, const void* v, const float* g, const float* beta,
+                            sata_dtype dt, int B, int H_qk, int G, int d_k, int d_v, void* y, void* stream);
+
+/* Gradients of sata_delta_prefill for dL/dy = dy and dL/dS_out = dS (NULL: zero).  With U the gradient of the state
+ * behind a token (from U = dS), e_t = v_t - k_t S' and S' as above, from the last token back:
+ *     U += c q_t (x) dy_t,   dq_t = c S_t dy_t,   z_t = U^T k_t,   dbeta_t = z_t.e_t,   dv_t = beta_t z_t,
+ *     dk_t = U u_t - S' dv_t,   U -= k_t (x) dv_t,   dg_t = <U, S'>,   U = exp(g_t) U;   dS_in = U at the end.
+ *   S_in : as given to the forward call, or NULL
+ *   dq, dk, dv: as q, k, v, dg, dbeta: as g, beta (device, written; zero at padding)
+ *   dS_in: as S_in (device, written) or NULL.  Must be neither dS nor S_in. */
+sata_status sata_delta_backward(const void* q, const void* k, const void* v, const float* g, const float* beta,
+                                const void* dy, sata_dtype dt, int B, int H_qk, int G, int n, int d_k, int d_v,
+                                const int32_t* lengths, const float* S_in, const float* dS, void* dq, void* dk, void* dv,
+                                float* dg, float* dbeta, float* dS_in, void* scratch, void* stream);
+
+/* ---- Rotary positions ------------------------------------------------------------
+ *
+ * The positions of queries and keys for softmax attention, whose scores then depend
+ * on distances: the first 2*pairs entries of a row are pairs (a, b), and pair i is turned by x = position * inv_freq[i],
+ *     (a, b) -> scale * (a cos x - b sin x, b cos x + a sin x);
+ * entries behind them stay as they are.  A pair is entries i and pairs + i, or with `interleaved` 2 i and 2 i + 1.
+ *   q, k: [B][H_q][n][d] and [B][H_k][n][d], dtype dt (device); H_k = 0 and k = k_out = NULL: q alone
+ *   positions: [B][n] int32 (device), of any sign; inv_freq: [pairs] float32 (device)
+ *   back != 0: turned by -x, the transposed map: what takes gradients of the outputs to those of q and k
+ *   q_out, k_out: as q and k (device, written); may be q and k themselves
+ * 1 <= pairs <= d / 2, d <= 128 (SATA_ERR_UNSUPPORTED beyond), B*H <= 65535, n <= 2^21.  Angles are formed in 64
+ * bits, the rest in 32, outputs are rounded once. */
+sata_status sata_rotary(const void* q, const void* k, const int32_t* positions, const float* inv_freq, sata_dtype dt, int B,
+                        int H_q, int H_k, int n, int d, int pairs, int interleaved, float scale, int back, void* q_out,
+                        void* k_out, void* stream);
+
+/* Frequencies base^(-i / pairs), and those for contexts `factor` times as long as the `original` tokens that a model was
+ * trained with. */
+typedef enum {
+  SATA_ROTARY_PLAIN = 0,   /* as they are                                                        */
+  SATA_ROTARY_LINEAR = 1,  /* all divided by the factor (positions brought closer together)        */
+  SATA_ROTARY_BASE = 2,    /* base * factor^(pairs / (pairs - 1)): the slowest divided by the factor */
+  SATA_ROTARY_BY_TURNS = 3 /* those of 32 turns and more in `original` tokens as they are, of one and
+                              fewer divided by the factor, in between in proportion; scale 0.1 ln factor + 1 */
+} sata_rotary_scaling;
+/* Host only.  inv_freq: [pairs] and scale: [1] (host, written), for sata_rotary; scale is 1 but BY_TURNS. */
+sata_status sata_rotary_frequencies(int pairs, double base, sata_rotary_scaling scaling, double factor, double original,
+                                    float* inv_freq, float* scale);
+
+/* ---- Caches of 4 bits an entry ------------------------------------------------------
+ *
+ * sata_softmax_step over caches that hold a row of d entries in sata_packed_row_bytes(d) bytes: 20 (d <= 32), 40 (<= 64) or
+ * 80.  With G = 1, 2 or 4 groups of 32 entries, byte a G + g (a = 0..15) holds the codes of entry 32 g + a in its low four
+ * bits and of entry 32 g + 16 + a in its high ones; from byte 16 G on follow for each group its scale and its least value
+ * in bfloat16.  An entry stands for least + scale * code (rounded once to float32).  For entries x of a group,
+ *     least = bf16(min x),  scale = bf16((max x / 2 - min x / 2) / 7.5),  code = nearest of (x - least) / scale in 0..15
+ * (0 where scale is 0), ties to the even one.  A group with an entry that is not finite or beyond 2^120 in size stands
+ * for NaN.  Entries and groups behind d are zero.
+ * A cache is [B][H_kv][capacity][row bytes], aligned to 4 G bytes (SATA_ERR_INVALID_ARG otherwise). */
+int64_t sata_packed_row_bytes(int d);
+
+/* Rows t = 0 .. n - 1 of sequence b into rows first[b] + t of its caches, those with t < counts[b].
+ *   k: [B][H_kv][n][d_k], v: [..][d_v], dtype dt (device); V and v may both be NULL
+ *   first, counts: [B] int32 (device) or NULL (zero; all n)
+ * Rows that lie outside of 0 .. capacity - 1 are left out, all other rows stay as they are. */
+sata_status sata_packed_write(void* K, void* V, int capacity, const int32_t* first, const void* k, const void* v,
+                              const int32_t* counts, sata_dtype dt, int B, int H_kv, int n, int d_k, int d_v, void* stream);
+
+/* What rows first[b] .. first[b] + n - 1 of a cache stand for, x: [B][H_kv][n][d], dtype dt (device, written);
+ * zero for rows outside of 0 .. capacity - 1. */
+sata_status sata_packed_read(const void* cache, int capacity, const int32_t* first, sata_dtype dt, int B, int H_kv, int n, int d,
+                             void* x, void* stream);
+
+/* sata_softmax_step over such caches, the new rows among them: k and v count as what their four bits stand for.  Idle
+ * sequences, unused rows, sizes and scratch as there; scratch of sata_softmax_step_packed_scratch bytes.  (A weight
+ * times a scale enters its product with 16 bits in bfloat16 calls.)  A row's NaN makes NaN of the outputs that see it. */
+int64_t sata_softmax_step_packed_scratch(int B, int H_kv, int G, int capacity, int d_v);
+sata_status sata_softmax_step_packed(void* K, void* V, int capacity, const int32_t* lengths, const void* q, const void* k,
+                                     const void* v, sata_dtype dt, int B, int H_kv, int G, int d_k, int d_v, void* y,
+                                     void* scratch, void* stream);
+
 /* Static text for a status code. */
 const char* sata_status_string(sata_status s);
 

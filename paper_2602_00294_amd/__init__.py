@@ -8,11 +8,15 @@ libsata.so); this package is the thin Python binding over it.
     y_t = decode_step(S, q_t, k_t, v_t, P=4)     # S updated in place
 """
 from ._binding import (SataError, backward, decay_backward, decay_prefill, decay_step, decode_step,
-                       decode_step_compensated, decode_step_grouped, feature_count, feature_index, feature_map,
-                       load_library, prefill, prefill_grouped, prefill_operands, prefill_parts, release,
-                       residual_elems, softmax_backward, softmax_prefill, softmax_step, state_elems)
+                       decode_step_compensated, decode_step_grouped, delta_backward, delta_prefill, delta_step,
+                       feature_count, feature_index, feature_map, load_library, packed_read, packed_row_bytes,
+                       packed_write, prefill, prefill_grouped, prefill_operands, prefill_parts, release, residual_elems,
+                       rotary, rotary_backward, rotary_frequencies, softmax_backward, softmax_prefill, softmax_step,
+                       softmax_step_packed, state_elems)
 
 __all__ = ["SataError", "backward", "decay_backward", "decay_prefill", "decay_step", "decode_step",
-           "decode_step_compensated", "decode_step_grouped", "feature_count", "feature_index", "feature_map",
-           "load_library", "prefill", "prefill_grouped", "prefill_operands", "prefill_parts", "release",
-           "residual_elems", "softmax_backward", "softmax_prefill", "softmax_step", "state_elems"]
+           "decode_step_compensated", "decode_step_grouped", "delta_backward", "delta_prefill", "delta_step",
+           "feature_count", "feature_index", "feature_map", "load_library", "packed_read", "packed_row_bytes",
+           "packed_write", "prefill", "prefill_grouped", "prefill_operands", "prefill_parts", "release",
+           "residual_elems", "rotary", "rotary_backward", "rotary_frequencies", "softmax_backward", "softmax_prefill",
+           "softmax_step", "softmax_step_packed", "state_elems"]

@@ -86,6 +86,30 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.sata_softmax_backward.restype = i32
     lib.sata_softmax_step.argtypes = [vp, vp, i32, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, vp, vp, vp]
     lib.sata_softmax_step.restype = i32
+    f32, f64 = ctypes.c_float, ctypes.c_double
+    lib.sata_delta_scratch.argtypes = [i32, i32, i32, i32, i32, i32, i32, i32]
+    lib.sata_delta_scratch.restype = i64
+    lib.sata_delta_prefill.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp]
+    lib.sata_delta_prefill.restype = i32
+    lib.sata_delta_step.argtypes = [vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, vp, vp]
+    lib.sata_delta_step.restype = i32
+    lib.sata_delta_backward.argtypes = [vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp,
+                                        vp, vp, vp, vp, vp]
+    lib.sata_delta_backward.restype = i32
+    lib.sata_rotary.argtypes = [vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, i32, f32, i32, vp, vp, vp]
+    lib.sata_rotary.restype = i32
+    lib.sata_rotary_frequencies.argtypes = [i32, f64, i32, f64, f64, ctypes.POINTER(f32), ctypes.POINTER(f32)]
+    lib.sata_rotary_frequencies.restype = i32
+    lib.sata_packed_row_bytes.argtypes = [i32]
+    lib.sata_packed_row_bytes.restype = i64
+    lib.sata_packed_write.argtypes = [vp, vp, i32, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, vp]
+    lib.sata_packed_write.restype = i32
+    lib.sata_packed_read.argtypes = [vp, i32, vp, i32, i32, i32, i32, i32, vp, vp]
+    lib.sata_packed_read.restype = i32
+    lib.sata_softmax_step_packed_scratch.argtypes = [i32, i32, i32, i32, i32]
+    lib.sata_softmax_step_packed_scratch.restype = i64
+    lib.sata_softmax_step_packed.argtypes = [vp, vp, i32, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, vp, vp, vp]
+    lib.sata_softmax_step_packed.restype = i32
     lib.sata_status_string.argtypes = [i32]
     lib.sata_status_string.restype = ctypes.c_char_p
     lib.sata_last_error.argtypes = []
@@ -648,6 +672,253 @@ def softmax_step(K, V, lengths, q, k, v, y=None):
         y = torch.empty(B, G * H, dv, dtype=q.dtype, device=q.device)
     scratch = _scratch(load_library().sata_softmax_step_scratch(B, H, G, cap, dv), q.device)
     _invoke("sata_softmax_step", q.device, _at(K), _at(V), cap, _at(lengths), _at(q), _at(k), _at(v), code, B, H, G,
+            dk, dv, _at(y), _at(scratch))
+    return y
+
+
+# ------------------------------------------------------------------ the gated delta rule
+
+def _delta_sizes(q, k, v, dims: int):
+    """(dtype code, B, H_qk, G, n, d_k, d_v) of q, k [B, H_qk(, n), d_k] and v [B, G*H_qk(, n), d_v] of `dims` dimensions."""
+    code = _dtype_code(q)
+    _check_same_dtype(q, k=k, v=v)
+    rows = ", n" if dims == 4 else ""
+    if q.dim() != dims or k.dim() != dims or v.dim() != dims:
+        raise ValueError(f"q, k [B, H_qk{rows}, d_k] and v [B, G*H_qk{rows}, d_v] expected")
+    B, H, dk = q.shape[0], q.shape[1], q.shape[-1]
+    Hv, dv = v.shape[1], v.shape[-1]
+    if H < 1 or Hv % H or Hv < H:
+        raise ValueError("the value head count must be a multiple of the query and key head count")
+    n = q.shape[2] if dims == 4 else 1
+    tokens = (n,) if dims == 4 else ()
+    _check_shape(k, "k", (B, H, *tokens, dk))
+    _check_shape(v, "v", (B, Hv, *tokens, dv))
+    _check_sizes(B, Hv, n, dk, dv)
+    return code, B, H, Hv // H, n, dk, dv
+
+
+def delta_prefill(q, k, v, g, beta, lengths=None, S_in=None, want_state: bool = True, y=None, S=None):
+    """Linear attention by the gated delta rule: S' = exp(g_t) S_{t-1}, S_t = S' + k_t (x) beta_t (v_t - k_t S'),
+    y_t = q_t S_t / sqrt(d_k).
+
+    q, k: [B, H, n, d_k]; v: [B, H_v, n, d_v] with H_v = G * H (value head g + G*h reads query and key head h);
+    g (at most 0), beta: [B, H_v, n] float32; lengths: [B] int32, the tokens of each sequence (the rest is padding: y is
+    zero there); S_in: the states to go on from.  Keys should be of length one or beta |k|^2 at most 2: states grow otherwise.
+    Returns (y [B, H_v, n, d_v] in the input dtype, S [B, H_v, d_k, d_v] float32 or None).
+    Preallocated outputs may be passed as y= and S=."""
+    torch = _torch()
+    code, B, H, G, n, dk, dv = _delta_sizes(q, k, v, 4)
+    _check_as(g, "g", torch.float32, (B, G * H, n))
+    _check_as(beta, "beta", torch.float32, (B, G * H, n))
+    _check_as(lengths, "lengths", torch.int32, (B,))
+    _check_as(S_in, "S_in", torch.float32, (B, G * H, dk, dv))
+    _check_as(y, "y", q.dtype, (B, G * H, n, dv))
+    _check_as(S, "S", torch.float32, (B, G * H, dk, dv))
+    _check_tensors(q.device, q=q, k=k, v=v, g=g, beta=beta, lengths=lengths, S_in=S_in, y=y, S=S)
+    if y is None:
+        y = torch.empty(B, G * H, n, dv, dtype=q.dtype, device=q.device)
+    if want_state and S is None:
+        S = torch.empty(B, G * H, dk, dv, dtype=torch.float32, device=q.device)
+    scratch = _scratch(load_library().sata_delta_scratch(0, code, B, H, G, n, dk, dv), q.device)
+    _invoke("sata_delta_prefill", q.device, _at(q), _at(k), _at(v), _at(g), _at(beta), code, B, H, G, n, dk, dv,
+            _at(lengths), _at(S_in), _at(y), _at(S), _at(scratch))
+    return y, S
+
+
+def delta_step(S, q, k, v, g, beta, y=None):
+    """One token of every sequence by the gated delta rule, in place on S [B, H_v, d_k, d_v].  q, k: [B, H, d_k];
+    v: [B, H_v, d_v]; g, beta: [B, H_v] float32.  Returns y [B, H_v, d_v]."""
+    torch = _torch()
+    code, B, H, G, _, dk, dv = _delta_sizes(q, k, v, 3)
+    _check_state(S, (B, G * H, dk, dv))
+    _check_as(g, "g", torch.float32, (B, G * H))
+    _check_as(beta, "beta", torch.float32, (B, G * H))
+    _check_as(y, "y", q.dtype, (B, G * H, dv))
+    _check_tensors(q.device, S=S, q=q, k=k, v=v, g=g, beta=beta, y=y)
+    if y is None:
+        y = torch.empty(B, G * H, dv, dtype=q.dtype, device=q.device)
+    _invoke("sata_delta_step", q.device, _at(S), _at(q), _at(k), _at(v), _at(g), _at(beta), code, B, H, G, dk, dv, _at(y))
+    return y
+
+
+def delta_backward(q, k, v, g, beta, dy, lengths=None, S_in=None, dS=None):
+    """Gradients of delta_prefill for dL/dy = dy [B, H_v, n, d_v] and dL/dS = dS [B, H_v, d_k, d_v] (None: zero).
+    Returns (dq, dk, dv, dg, dbeta, dS_in): the first three in q's dtype, the others float32, dS_in None without S_in."""
+    torch = _torch()
+    code, B, H, G, n, dk, dv = _delta_sizes(q, k, v, 4)
+    _check_as(g, "g", torch.float32, (B, G * H, n))
+    _check_as(beta, "beta", torch.float32, (B, G * H, n))
+    _check_as(dy, "dy", q.dtype, (B, G * H, n, dv))
+    _check_as(lengths, "lengths", torch.int32, (B,))
+    _check_as(S_in, "S_in", torch.float32, (B, G * H, dk, dv))
+    _check_as(dS, "dS", torch.float32, (B, G * H, dk, dv))
+    _check_tensors(q.device, q=q, k=k, v=v, g=g, beta=beta, dy=dy, lengths=lengths, S_in=S_in, dS=dS)
+    dq, dkk, dvv, dg, db = (torch.empty_like(x) for x in (q, k, v, g, beta))
+    dS_in = torch.empty_like(S_in) if S_in is not None else None
+    scratch = _scratch(load_library().sata_delta_scratch(1, code, B, H, G, n, dk, dv), q.device)
+    _invoke("sata_delta_backward", q.device, _at(q), _at(k), _at(v), _at(g), _at(beta), _at(dy), code, B, H, G, n, dk, dv,
+            _at(lengths), _at(S_in), _at(dS), _at(dq), _at(dkk), _at(dvv), _at(dg), _at(db), _at(dS_in), _at(scratch))
+    return dq, dkk, dvv, dg, db, dS_in
+
+
+# ------------------------------------------------------------------ rotary positions
+
+ROTARY_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "by_turns": 3}
+
+
+def rotary_frequencies(pairs: int, base: float = 10000.0, scaling: str = "plain", factor: float = 1.0,
+                       original: float = 0.0, device="cuda"):
+    """Frequencies base^(-i / pairs) of `pairs` pairs, [pairs] float32 on `device`, and the outputs' scale, for rotary().
+    scaling, for contexts `factor` times as long as trained: "linear" divides all by the factor; "base" raises the
+    base so that the slowest is divided by it; "by_turns" keeps those of 32 turns and more in `original` tokens, divides those
+    of one and fewer, goes from the ones to the others in proportion, and scales by 0.1 ln(factor) + 1."""
+    if scaling not in ROTARY_SCALINGS:
+        raise ValueError(f"unknown scaling {scaling!r}; one of {', '.join(ROTARY_SCALINGS)}")
+    _check_sizes(pairs)
+    freq, scale = (ctypes.c_float * max(1, pairs))(), ctypes.c_float()
+    _check(load_library().sata_rotary_frequencies(pairs, base, ROTARY_SCALINGS[scaling], factor, original, freq,
+                                                  ctypes.byref(scale)), "sata_rotary_frequencies")
+    return _torch().tensor(list(freq), dtype=_torch().float32).to(device), scale.value
+
+
+def _turn(q, k, positions, inv_freq, interleaved, scale, back, q_out, k_out):
+    torch = _torch()
+    code = _dtype_code(q)
+    if q.dim() not in (3, 4):
+        raise ValueError("q must be [B, H, n, d] or, for one token of every sequence, [B, H, d]")
+    rows = q.shape[2:-1]
+    B, Hq, n, d = q.shape[0], q.shape[1], rows[0] if rows else 1, q.shape[-1]
+    Hk = 0
+    if k is not None:
+        _check_same_dtype(q, k=k)
+        if k.dim() != q.dim():
+            raise ValueError("k must have as many dimensions as q")
+        Hk = k.shape[1]
+        _check_shape(k, "k", (B, Hk, *rows, d))
+    elif k_out is not None:
+        raise ValueError("k_out without k")
+    _check_as(positions, "positions", torch.int32, (B, *rows))
+    if inv_freq.dim() != 1:
+        raise ValueError("inv_freq must be [pairs]")
+    _check_as(inv_freq, "inv_freq", torch.float32, inv_freq.shape)
+    _check_as(q_out, "q_out", q.dtype, q.shape)
+    _check_as(k_out, "k_out", q.dtype, k.shape if k is not None else ())
+    pairs = inv_freq.shape[0]
+    _check_sizes(B, Hq, Hk, n, d, pairs)
+    _check_tensors(q.device, q=q, k=k, positions=positions, inv_freq=inv_freq, q_out=q_out, k_out=k_out)
+    q_out = torch.empty_like(q) if q_out is None else q_out
+    if Hk:
+        k_out = torch.empty_like(k) if k_out is None else k_out
+    elif k is not None:  # (no heads)
+        k_out = torch.empty_like(k) if k_out is None else k_out
+    _invoke("sata_rotary", q.device, _at(q), _at(k), _at(positions), _at(inv_freq), code, B, Hq, Hk, n, d, pairs,
+            int(bool(interleaved)), float(scale), int(back), _at(q_out), _at(k_out))
+    return q_out, k_out
+
+
+def rotary(q, k, positions, inv_freq, interleaved: bool = False, scale: float = 1.0, q_out=None, k_out=None):
+    """Queries and keys turned by their positions: pair i of the first 2 * len(inv_freq) entries of a row, entries i and
+    len(inv_freq) + i, or 2 i and 2 i + 1 where interleaved, by the angle position * inv_freq[i], times scale;
+    the entries behind them stay.
+
+    q: [B, H_q, n, d] and k: [B, H_k, n, d] (or None) with positions [B, n] int32, or [B, H, d] with positions [B] for one
+    token of every sequence; inv_freq: float32.  q_out and k_out may be q and k themselves.  Returns (q_out, k_out)."""
+    return _turn(q, k, positions, inv_freq, interleaved, scale, False, q_out, k_out)
+
+
+def rotary_backward(dq, dk, positions, inv_freq, interleaved: bool = False, scale: float = 1.0, q_out=None, k_out=None):
+    """Gradients of rotary's inputs from those of its outputs: turned back by the same angles, times scale.
+    Arguments and results as in rotary."""
+    return _turn(dq, dk, positions, inv_freq, interleaved, scale, True, q_out, k_out)
+
+
+# ------------------------------------------------------------------ caches of 4 bits an entry
+
+def packed_row_bytes(d: int) -> int:
+    """Bytes of a row of d entries (1 to 128) in a cache of 4 bits an entry, a scale and a least value for every 32."""
+    _check_sizes(d)
+    size = int(load_library().sata_packed_row_bytes(d))
+    if size < 0:
+        raise ValueError(f"rows of {d} entries; 1 to 128 are supported")
+    return size
+
+
+def _check_packed(cache, name: str, B, H, d):
+    torch = _torch()
+    if cache.dtype != torch.uint8:
+        raise TypeError(f"{name} is {cache.dtype}, expected torch.uint8")
+    if cache.dim() != 4:
+        raise ValueError(f"{name} must be [B, H_kv, capacity, row bytes]")
+    _check_sizes(cache.shape[2])
+    _check_shape(cache, name, (B, H, cache.shape[2], packed_row_bytes(d)))
+
+
+def packed_write(K, V, first, k, v, counts=None):
+    """Rows k [B, H, n, d_k] and v [B, H, n, d_v] into rows first[b] on of the caches K and V [B, H, capacity,
+    packed_row_bytes(d)] uint8, the first counts[b] of them (None: all).  first, counts: [B] int32; first may be None
+    (zero), V and v may both be None.  Rows outside of the caches are left out."""
+    torch = _torch()
+    code = _dtype_code(k)
+    if k.dim() != 4:
+        raise ValueError("k must be [B, H_kv, n, d_k]")
+    B, H, n, dk = k.shape
+    _check_sizes(B, H, n, dk)
+    _check_packed(K, "K", B, H, dk)
+    if (V is None) != (v is None):
+        raise ValueError("V and v come together")
+    dv = 1
+    if v is not None:
+        _check_same_dtype(k, v=v)
+        dv = v.shape[-1]
+        _check_shape(v, "v", (B, H, n, dv))
+        _check_packed(V, "V", B, H, dv)
+        if V.shape[2] != K.shape[2]:
+            raise ValueError("K and V must have the same capacity")
+    _check_as(first, "first", torch.int32, (B,))
+    _check_as(counts, "counts", torch.int32, (B,))
+    _check_tensors(k.device, K=K, V=V, first=first, k=k, v=v, counts=counts)
+    _invoke("sata_packed_write", k.device, _at(K), _at(V), K.shape[2], _at(first), _at(k), _at(v), _at(counts), code, B, H,
+            n, dk, dv)
+
+
+def packed_read(cache, first, n: int, d: int, dtype, x=None):
+    """What rows first[b] .. first[b] + n - 1 (first None: from 0) of a cache [B, H, capacity, packed_row_bytes(d)] stand
+    for, [B, H, n, d] in dtype; zero for rows outside of the cache."""
+    torch = _torch()
+    if cache.dim() != 4:
+        raise ValueError("cache must be [B, H_kv, capacity, row bytes]")
+    B, H = cache.shape[:2]
+    if n < 0:
+        raise ValueError(f"n={n} < 0")
+    _check_sizes(B, H, n)
+    _check_packed(cache, "cache", B, H, d)
+    _check_as(first, "first", torch.int32, (B,))
+    _check_as(x, "x", dtype, (B, H, n, d))
+    _check_tensors(cache.device, cache=cache, first=first, x=x)
+    if x is None:
+        x = torch.empty(B, H, n, d, dtype=dtype, device=cache.device)
+    _invoke("sata_packed_read", cache.device, _at(cache), cache.shape[2], _at(first), _dtype_code(x), B, H, n, d, _at(x))
+    return x
+
+
+def softmax_step_packed(K, V, lengths, q, k, v, y=None):
+    """softmax_step over caches of 4 bits an entry, K and V [B, H_kv, capacity, packed_row_bytes(d)] uint8: k and v are
+    written as row lengths[b] in those bits and count as what they stand for, then q attends over rows 0..lengths[b].
+    Arguments and result otherwise as there."""
+    torch = _torch()
+    code, B, H, G, dk, dv = _token_sizes(q, k, v)
+    _check_packed(K, "K", B, H, dk)
+    _check_packed(V, "V", B, H, dv)
+    cap = K.shape[2]
+    if V.shape[2] != cap:
+        raise ValueError("K and V must have the same capacity")
+    _check_as(lengths, "lengths", torch.int32, (B,))
+    _check_as(y, "y", q.dtype, (B, G * H, dv))
+    _check_tensors(q.device, K=K, V=V, lengths=lengths, q=q, k=k, v=v, y=y)
+    if y is None:
+        y = torch.empty(B, G * H, dv, dtype=q.dtype, device=q.device)
+    scratch = _scratch(load_library().sata_softmax_step_packed_scratch(B, H, G, cap, dv), q.device)
+    _invoke("sata_softmax_step_packed", q.device, _at(K), _at(V), cap, _at(lengths), _at(q), _at(k), _at(v), code, B, H, G,
             dk, dv, _at(y), _at(scratch))
     return y
 

@@ -255,14 +255,14 @@ struct SoftmaxGradArgs {
 hipError_t launch_softmax_backward(const SoftmaxGradArgs& a, bool bf16, hipStream_t s);
 
 // The heads' caches in stretches of `least` units or more, at most `workgroups` of them, for a card that
-// holds `places` at a time; a group's heads in blocks of 32.  Where `fixed`, each head has that many
+// holds `places` at a time; a group's heads in blocks of `members`.  Where `fixed`, each head has that many
 // stretches of fixed_len units (those behind its rows stay without work).  Where a head's stretches are
 // found and the sums of heads of several lie in `bytes` bytes of scratch.
 struct SoftmaxStepPlan {
-  int unit = 128, least = 2, places = 0, workgroups = 0, blocks = 1, fixed = 0, fixed_len = 0;
+  int unit = 128, least = 2, places = 0, workgroups = 0, blocks = 1, members = 32, fixed = 0, fixed_len = 0;
   size_t bytes = 0;
 };
-SoftmaxStepPlan plan_softmax_step(bool bf16, int heads, int H, int G, int capacity, int dv);
+SoftmaxStepPlan plan_softmax_step(bool bf16, int heads, int H, int G, int capacity, int dv, int members = 32);
 struct SoftmaxStepArgs {
   void *K, *V;         // [heads][capacity][d]
   const int* lengths;  // [heads / H]
@@ -273,6 +273,59 @@ struct SoftmaxStepArgs {
   float scale;
 };
 hipError_t launch_softmax_step(const SoftmaxStepArgs& a, bool bf16, hipStream_t s);
+// K and V: caches of 4 bits an entry.
+constexpr int kPackedMembers = 16;
+SoftmaxStepPlan plan_softmax_step_packed(bool bf16, int heads, int H, int G, int capacity, int dv);
+hipError_t launch_softmax_step_packed(const SoftmaxStepArgs& a, bool bf16, hipStream_t s);
+
+// ---- rotary positions ---------------------------------------------------------
+struct RotaryArgs {
+  const void *q, *k;      // [B][heads][n][d]
+  void *q_out, *k_out;    // the same, or q and k themselves
+  const int* positions;   // [B][n]
+  const float* freq;      // [pairs]
+  int B, Hq, Hk, n, d, pairs;
+  bool interleaved, back;
+  float scale;
+};
+hipError_t launch_rotary(const RotaryArgs& a, bool bf16, hipStream_t s);
+
+// ---- caches of 4 bits an entry --------------------------------------------------
+// Groups of 32 entries in a row, padded to 1, 2 or 4.
+constexpr int packed_groups(int d) { return d <= 32 ? 1 : d <= 64 ? 2 : 4; }
+constexpr int packed_row_bytes(int d) { return 20 * packed_groups(d); }
+struct PackedRows {
+  uint8_t* cache;         // [heads][capacity][row bytes]
+  void* x;                // [heads][n][d]
+  int d;
+};
+struct PackedArgs {
+  PackedRows rows[2];     // (one or two tensors)
+  int tensors;
+  const int* first;       // [heads / H]
+  const int* counts;      // may be null
+  int heads, H, n, capacity;
+};
+hipError_t launch_packed_write(const PackedArgs& a, bool bf16, hipStream_t s);
+hipError_t launch_packed_read(const PackedArgs& a, bool bf16, hipStream_t s);
+
+// ---- the gated delta rule ---------------------------------------------------------
+// heads: value heads, [B][Hk * G]; head h reads queries and keys of head h / G.
+struct DeltaArgs {
+  const void *q, *k, *v, *dy;
+  const float *g, *beta;        // [heads][n]
+  const int* lengths;           // [heads / (Hk G)] or null
+  const float *S_in, *dS;       // [heads][dk][dv] or null
+  void *y, *dq, *dk_out, *dv_out;
+  float *S_out, *dg, *dbeta, *dS_in;
+  int heads, Hk, G, n, dk, dv;
+  float scale;
+};
+hipError_t launch_delta_prefill(const DeltaArgs& a, bool bf16, void* scratch, hipStream_t s);
+size_t delta_prefill_scratch(bool bf16, int heads, int G, int n, int dk, int dv);
+hipError_t launch_delta_step(const DeltaArgs& a, float* S, bool bf16, hipStream_t s);
+hipError_t launch_delta_backward(const DeltaArgs& a, bool bf16, void* scratch, hipStream_t s);
+size_t delta_backward_scratch(bool bf16, int heads, int G, int n, int dk, int dv);
 
 // ---- helpers -----------------------------------------------------------------
 hipError_t launch_fill_zero(float* p, int64_t count, hipStream_t s);

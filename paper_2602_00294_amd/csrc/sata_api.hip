@@ -730,6 +730,33 @@ sata_status check_scratch(const void* scratch, size_t bytes) {
 
 float pair_scale(int d_k) { return (float)(1.0 / std::sqrt((double)d_k)); }
 
+// The delta rule's calls: value heads, G to a query and key head.
+sata_status check_delta_args(sata_dtype dt, int B, int H_qk, int G, int n, int d_k, int d_v) {
+  if (H_qk < 1) return fail(SATA_ERR_INVALID_ARG, "H_qk=%d must be >= 1", H_qk);
+  sata_status st = check_pair_args(dt, B, H_qk, G, n, d_k, d_v);
+  if (st != SATA_OK) return st;
+  const int64_t tokens = (int64_t)B * H_qk * G * n;
+  if (tokens > kMaxGradientTokens)
+    return fail(SATA_ERR_TOO_LARGE, "B*H_qk*G*n=%lld tokens exceed %lld", (long long)tokens, (long long)kMaxGradientTokens);
+  return SATA_OK;
+}
+
+sata::DeltaArgs delta_args(const void* q, const void* k, const void* v, const float* g, const float* beta, int B, int H_qk,
+                           int G, int n, int d_k, int d_v, const int32_t* lengths) {
+  sata::DeltaArgs a{};
+  a.q = q, a.k = k, a.v = v, a.g = g, a.beta = beta, a.lengths = lengths;
+  a.heads = B * H_qk * G, a.Hk = H_qk, a.G = G, a.n = n, a.dk = d_k, a.dv = d_v;
+  a.scale = pair_scale(d_k);
+  return a;
+}
+
+// Caches of 4 bits an entry: rows are read by 4, 8 or 16 bytes.
+sata_status check_packed(const void* cache, int d) {
+  if ((uintptr_t)cache & (4 * sata::packed_groups(d) - 1))
+    return fail(SATA_ERR_INVALID_ARG, "a cache of rows of d=%d must be %d-byte aligned", d, 4 * sata::packed_groups(d));
+  return SATA_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -1117,6 +1144,173 @@ sata_status sata_softmax_step(void* K, void* V, int capacity, const int32_t* len
                                 pair_scale(d_k)};
   hipError_t e = sata::launch_softmax_step(a, dt == SATA_BF16, (hipStream_t)stream);
   if (e != hipSuccess) return hip_fail(e, "softmax step launch");
+  return ok();
+}
+
+int64_t sata_delta_scratch(int gradients, sata_dtype dt, int B, int H_qk, int G, int n, int d_k, int d_v) {
+  if (check_delta_args(dt, B, H_qk, G, n, d_k, d_v) != SATA_OK) return -1;
+  const int heads = B * H_qk * G;
+  return (int64_t)(gradients ? sata::delta_backward_scratch(dt == SATA_BF16, heads, G, n, d_k, d_v)
+                             : sata::delta_prefill_scratch(dt == SATA_BF16, heads, G, n, d_k, d_v));
+}
+
+sata_status sata_delta_prefill(const void* q, const void* k, const void* v, const float* g, const float* beta,
+                               sata_dtype dt, int B, int H_qk, int G, int n, int d_k, int d_v, const int32_t* lengths,
+                               const float* S_in, void* y, float* S_out, void* scratch, void* stream) {
+  sata_status st = check_delta_args(dt, B, H_qk, G, n, d_k, d_v);
+  if (st != SATA_OK) return st;
+  if (n > 0 && (!q || !k || !v || !g || !beta || !y)) return fail(SATA_ERR_INVALID_ARG, "null tensor pointer");
+  if (S_in && S_in == S_out) return fail(SATA_ERR_INVALID_ARG, "S_out must not be S_in");
+  if (n == 0 && !S_out) return ok();
+  sata::DeltaArgs a = delta_args(q, k, v, g, beta, B, H_qk, G, n, d_k, d_v, lengths);
+  if ((st = check_scratch(scratch, sata::delta_prefill_scratch(dt == SATA_BF16, a.heads, G, n, d_k, d_v))) != SATA_OK) return st;
+  a.S_in = S_in, a.y = y, a.S_out = S_out;
+  hipError_t e = sata::launch_delta_prefill(a, dt == SATA_BF16, scratch, (hipStream_t)stream);
+  if (e != hipSuccess) return hip_fail(e, "delta prefill launch");
+  return ok();
+}
+
+sata_status sata_delta_step(float* S, const void* q, const void* k, const void* v, const float* g, const float* beta,
+                            sata_dtype dt, int B, int H_qk, int G, int d_k, int d_v, void* y, void* stream) {
+  sata_status st = check_delta_args(dt, B, H_qk, G, 1, d_k, d_v);
+  if (st != SATA_OK) return st;
+  if (!S || !q || !k || !v || !g || !beta || !y) return fail(SATA_ERR_INVALID_ARG, "null tensor pointer");
+  sata::DeltaArgs a = delta_args(q, k, v, g, beta, B, H_qk, G, 1, d_k, d_v, nullptr);
+  a.y = y;
+  hipError_t e = sata::launch_delta_step(a, S, dt == SATA_BF16, (hipStream_t)stream);
+  if (e != hipSuccess) return hip_fail(e, "delta step launch");
+  return ok();
+}
+
+sata_status sata_delta_backward(const void* q, const void* k, const void* v, const float* g, const float* beta,
+                                const void* dy, sata_dtype dt, int B, int H_qk, int G, int n, int d_k, int d_v,
+                                const int32_t* lengths, const float* S_in, const float* dS, void* dq, void* dk, void* dv,
+                                float* dg, float* dbeta, float* dS_in, void* scratch, void* stream) {
+  sata_status st = check_delta_args(dt, B, H_qk, G, n, d_k, d_v);
+  if (st != SATA_OK) return st;
+  if (n > 0 && (!q || !k || !v || !g || !beta || !dy || !dq || !dk || !dv || !dg || !dbeta))
+    return fail(SATA_ERR_INVALID_ARG, "null tensor pointer");
+  if (dS && dS == dS_in) return fail(SATA_ERR_INVALID_ARG, "dS_in must not be dS");
+  if (S_in && S_in == dS_in) return fail(SATA_ERR_INVALID_ARG, "dS_in must not be S_in");
+  if (n == 0 && !dS_in) return ok();
+  sata::DeltaArgs a = delta_args(q, k, v, g, beta, B, H_qk, G, n, d_k, d_v, lengths);
+  if ((st = check_scratch(scratch, sata::delta_backward_scratch(dt == SATA_BF16, a.heads, G, n, d_k, d_v))) != SATA_OK) return st;
+  a.dy = dy, a.S_in = S_in, a.dS = dS;
+  a.dq = dq, a.dk_out = dk, a.dv_out = dv, a.dg = dg, a.dbeta = dbeta, a.dS_in = dS_in;
+  hipError_t e = sata::launch_delta_backward(a, dt == SATA_BF16, scratch, (hipStream_t)stream);
+  if (e != hipSuccess) return hip_fail(e, "delta backward launch");
+  return ok();
+}
+
+sata_status sata_rotary_frequencies(int pairs, double base, sata_rotary_scaling scaling, double factor, double original,
+                                    float* inv_freq, float* scale) {
+  if (!inv_freq || !scale) return fail(SATA_ERR_INVALID_ARG, "null output pointer");
+  if (pairs < 1 || pairs > sata::kMaxPairDim / 2) return fail(SATA_ERR_INVALID_ARG, "pairs=%d not in 1..%d", pairs, sata::kMaxPairDim / 2);
+  if (!(base > 1.0) || !std::isfinite(base)) return fail(SATA_ERR_INVALID_ARG, "base=%g must be above 1", base);
+  if (scaling < SATA_ROTARY_PLAIN || scaling > SATA_ROTARY_BY_TURNS)
+    return fail(SATA_ERR_INVALID_ARG, "unknown scaling %d", (int)scaling);
+  if (scaling != SATA_ROTARY_PLAIN && (!(factor >= 1.0) || !std::isfinite(factor)))
+    return fail(SATA_ERR_INVALID_ARG, "factor=%g must be at least 1", factor);
+  if (scaling == SATA_ROTARY_BY_TURNS && (!(original >= 1.0) || !std::isfinite(original)))
+    return fail(SATA_ERR_INVALID_ARG, "original=%g must be at least 1", original);
+  if (scaling == SATA_ROTARY_BASE && pairs < 2) return fail(SATA_ERR_INVALID_ARG, "a scaled base takes two pairs at least");
+  if (scaling == SATA_ROTARY_BASE) base *= std::pow(factor, (double)pairs / (pairs - 1));
+  for (int i = 0; i < pairs; ++i) {
+    double f = std::pow(base, -(double)i / pairs);
+    if (scaling == SATA_ROTARY_LINEAR) f /= factor;
+    if (scaling == SATA_ROTARY_BY_TURNS) {
+      const double turns = original * f / 6.283185307179586, keep = std::min(1.0, std::max(0.0, (turns - 1.0) / 31.0));
+      f *= keep + (1.0 - keep) / factor;
+    }
+    inv_freq[i] = (float)f;
+  }
+  *scale = scaling == SATA_ROTARY_BY_TURNS ? (float)(0.1 * std::log(factor) + 1.0) : 1.f;
+  return ok();
+}
+
+sata_status sata_rotary(const void* q, const void* k, const int32_t* positions, const float* inv_freq, sata_dtype dt, int B,
+                        int H_q, int H_k, int n, int d, int pairs, int interleaved, float scale, int back, void* q_out,
+                        void* k_out, void* stream) {
+  if (!valid_dtype(dt)) return fail(SATA_ERR_INVALID_ARG, "unknown dtype %d", (int)dt);
+  if (B < 1 || H_q < 1 || H_k < 0) return fail(SATA_ERR_INVALID_ARG, "B=%d H_q=%d must be >= 1, H_k=%d >= 0", B, H_q, H_k);
+  if (n < 0) return fail(SATA_ERR_INVALID_ARG, "n=%d < 0", n);
+  if (d < 1 || pairs < 1 || pairs > d / 2) return fail(SATA_ERR_INVALID_ARG, "pairs=%d not in 1..d/2 of d=%d", pairs, d);
+  if (d > sata::kMaxPairDim) return fail(SATA_ERR_UNSUPPORTED, "d=%d; supported up to %d", d, sata::kMaxPairDim);
+  if (H_q > kMaxHeads / B || H_k > kMaxHeads / B)
+    return fail(SATA_ERR_TOO_LARGE, "B*H of B=%d H_q=%d H_k=%d exceeds %d", B, H_q, H_k, kMaxHeads);
+  if (n > kMaxPairTokens) return fail(SATA_ERR_TOO_LARGE, "n=%d exceeds %d", n, kMaxPairTokens);
+  if (n == 0) return ok();
+  if (!q || !q_out || !positions || !inv_freq || (H_k > 0 && (!k || !k_out))) return fail(SATA_ERR_INVALID_ARG, "null tensor pointer");
+  if (H_k > 0 && (q_out == k_out || q_out == k || k_out == q))
+    return fail(SATA_ERR_INVALID_ARG, "an output must be its own input or a tensor of its own");
+  const sata::RotaryArgs a{q, k, q_out, k_out, positions, inv_freq, B, H_q, H_k, n, d, pairs, interleaved != 0, back != 0, scale};
+  hipError_t e = sata::launch_rotary(a, dt == SATA_BF16, (hipStream_t)stream);
+  if (e != hipSuccess) return hip_fail(e, "rotary launch");
+  return ok();
+}
+
+int64_t sata_packed_row_bytes(int d) { return d < 1 || d > sata::kMaxPairDim ? -1 : sata::packed_row_bytes(d); }
+
+sata_status sata_packed_write(void* K, void* V, int capacity, const int32_t* first, const void* k, const void* v,
+                              const int32_t* counts, sata_dtype dt, int B, int H_kv, int n, int d_k, int d_v, void* stream) {
+  const bool both = V || v;
+  sata_status st = check_pair_args(dt, B, H_kv, 1, n, d_k, both ? d_v : 1);
+  if (st != SATA_OK) return st;
+  if (capacity < 1) return fail(SATA_ERR_INVALID_ARG, "capacity=%d must be >= 1", capacity);
+  if (capacity > kMaxPairTokens) return fail(SATA_ERR_TOO_LARGE, "capacity=%d exceeds %d", capacity, kMaxPairTokens);
+  if (n == 0) return ok();
+  if (!K || !k || (both && (!V || !v))) return fail(SATA_ERR_INVALID_ARG, "null tensor pointer");
+  if (both && K == V) return fail(SATA_ERR_INVALID_ARG, "K and V must be caches of their own");
+  if ((st = check_packed(K, d_k)) != SATA_OK || (both && (st = check_packed(V, d_v)) != SATA_OK)) return st;
+  sata::PackedArgs a{};
+  a.rows[0] = {(uint8_t*)K, const_cast<void*>(k), d_k};
+  a.rows[1] = {(uint8_t*)V, const_cast<void*>(v), d_v};
+  a.tensors = both ? 2 : 1, a.first = first, a.counts = counts;
+  a.heads = B * H_kv, a.H = H_kv, a.n = n, a.capacity = capacity;
+  hipError_t e = sata::launch_packed_write(a, dt == SATA_BF16, (hipStream_t)stream);
+  if (e != hipSuccess) return hip_fail(e, "packed write launch");
+  return ok();
+}
+
+sata_status sata_packed_read(const void* cache, int capacity, const int32_t* first, sata_dtype dt, int B, int H_kv, int n, int d,
+                             void* x, void* stream) {
+  sata_status st = check_pair_args(dt, B, H_kv, 1, n, d, 1);
+  if (st != SATA_OK) return st;
+  if (capacity < 1) return fail(SATA_ERR_INVALID_ARG, "capacity=%d must be >= 1", capacity);
+  if (capacity > kMaxPairTokens) return fail(SATA_ERR_TOO_LARGE, "capacity=%d exceeds %d", capacity, kMaxPairTokens);
+  if (n == 0) return ok();
+  if (!cache || !x) return fail(SATA_ERR_INVALID_ARG, "null tensor pointer");
+  if ((st = check_packed(cache, d)) != SATA_OK) return st;
+  sata::PackedArgs a{};
+  a.rows[0] = {(uint8_t*)const_cast<void*>(cache), x, d};
+  a.tensors = 1, a.first = first;
+  a.heads = B * H_kv, a.H = H_kv, a.n = n, a.capacity = capacity;
+  hipError_t e = sata::launch_packed_read(a, dt == SATA_BF16, (hipStream_t)stream);
+  if (e != hipSuccess) return hip_fail(e, "packed read launch");
+  return ok();
+}
+
+int64_t sata_softmax_step_packed_scratch(int B, int H_kv, int G, int capacity, int d_v) {
+  if (check_pair_args(SATA_F32, B, H_kv, G, capacity, 1, d_v) != SATA_OK || capacity < 1) return -1;
+  return (int64_t)std::max(sata::plan_softmax_step_packed(true, B * H_kv, H_kv, G, capacity, d_v).bytes,
+                           sata::plan_softmax_step_packed(false, B * H_kv, H_kv, G, capacity, d_v).bytes);
+}
+
+sata_status sata_softmax_step_packed(void* K, void* V, int capacity, const int32_t* lengths, const void* q, const void* k,
+                                     const void* v, sata_dtype dt, int B, int H_kv, int G, int d_k, int d_v, void* y,
+                                     void* scratch, void* stream) {
+  sata_status st = check_pair_args(dt, B, H_kv, G, capacity, d_k, d_v);
+  if (st != SATA_OK) return st;
+  if (capacity < 1) return fail(SATA_ERR_INVALID_ARG, "capacity=%d must be >= 1", capacity);
+  if (!K || !V || !lengths || !q || !k || !v || !y) return fail(SATA_ERR_INVALID_ARG, "null tensor pointer");
+  if (K == V) return fail(SATA_ERR_INVALID_ARG, "K and V must be caches of their own");
+  if ((st = check_packed(K, d_k)) != SATA_OK || (st = check_packed(V, d_v)) != SATA_OK) return st;
+  if ((st = check_scratch(scratch, sata::plan_softmax_step_packed(dt == SATA_BF16, B * H_kv, H_kv, G, capacity, d_v).bytes)) != SATA_OK)
+    return st;
+  const sata::SoftmaxStepArgs a{K, V, lengths, q, k, v, y, (float*)scratch, B * H_kv, H_kv, G, capacity, d_k, d_v,
+                                pair_scale(d_k)};
+  hipError_t e = sata::launch_softmax_step_packed(a, dt == SATA_BF16, (hipStream_t)stream);
+  if (e != hipSuccess) return hip_fail(e, "packed softmax step launch");
   return ok();
 }
 

@@ -1,0 +1,376 @@
+// One token of causal softmax attention over caches of 4 bits an entry (packed_rows.hpp): row lengths[b] of the
+// caches becomes k and v in those bits, then y = sum_{s<=lengths[b]} p_s v_s with p = softmax(c q.k_s), k_s and v_s
+// being what the caches' rows stand for.
+//
+// Rows are never unpacked into numbers of their own.  A bfloat16 with the code's four bits on top of its
+// fraction, 0x4180 | code << 3, is 16 + code, exactly, so two codes become operands of a product by a shift and
+// one and-or.  With s and m a group's scale and least value, X the sums over such operands,
+//     q.k_t = sum_g s_tg X_tg + (m_tg - 16 s_tg) (sum of q's entries in g),   X_tg = sum_i (16 + code_ti) q_i
+//     y     = sum_t (p_t s_tg) (16 + code_tj) + sum_t p_t (m_tg - 16 s_tg).
+// Products are v_mfma_f32_16x16x32_bf16 with the query heads of a group as columns: of keys a group of 32 entries
+// at a time, rows being 16 tokens; of values 16 columns at a time over 32 tokens.  A lane reads of a key's row the bytes of
+// four a (packed_rows.hpp), of a value's row those of one; scores' tokens, four a lane, are the
+// weights' places in the second product, so they never leave their lanes.
+//
+// Bound: the cache is read once, 5 (d_k + d_v) / 8 bytes a key.
+//
+// Precision: codes, scales and least values are exact operands; scores, statistics and sums are float32; a weight times a
+// scale is two bfloat16 numbers in bfloat16 calls, three in float32 ones.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "device_common.hpp"
+#include "kernels.hpp"
+#include "packed_rows.hpp"
+#include "pair_tiles.hpp"
+#include "softmax_stretches.hpp"
+
+namespace sata {
+
+namespace {
+
+// G bytes for each of four a, as they lie in a key's row.
+template <int G>
+struct KeyCodes {
+  uint32_t w[G];
+};
+template <int G>
+__device__ __forceinline__ KeyCodes<G> load_key(const uint8_t* p) {
+  KeyCodes<G> c;
+  if constexpr (G == 4) {
+    const uint4 x = *(const uint4*)p;
+    c.w[0] = x.x, c.w[1] = x.y, c.w[2] = x.z, c.w[3] = x.w;
+  } else if constexpr (G == 2) {
+    const uint2 x = *(const uint2*)p;
+    c.w[0] = x.x, c.w[1] = x.y;
+  } else {
+    c.w[0] = *(const uint32_t*)p;
+  }
+  return c;
+}
+// a row's scales and least values
+template <int G>
+__device__ __forceinline__ KeyCodes<G> load_params(const uint8_t* row) {
+  return load_key<G>(row + 16 * G);
+}
+
+// Bytes `g` of four a's, two at a time in the low bytes of the halves of a dword.
+template <int G>
+__device__ __forceinline__ void group_bytes(const KeyCodes<G>& c, int g, uint32_t& first, uint32_t& second) {
+  if constexpr (G == 4) {
+    const uint32_t sel = 0x0c000c04u + 0x00010001u * g;  // byte g of the second and of the first
+    first = __builtin_amdgcn_perm(c.w[0], c.w[1], 0x0c000c04u + 0x00010001u * g);
+    second = __builtin_amdgcn_perm(c.w[2], c.w[3], sel);
+  } else if constexpr (G == 2) {
+    first = g ? (c.w[0] >> 8) & 0x00ff00ffu : c.w[0] & 0x00ff00ffu;
+    second = g ? (c.w[1] >> 8) & 0x00ff00ffu : c.w[1] & 0x00ff00ffu;
+  } else {
+    first = __builtin_amdgcn_perm(0u, c.w[0], 0x0c010c00u);
+    second = __builtin_amdgcn_perm(0u, c.w[0], 0x0c030c02u);
+  }
+}
+// 16 + the code in bits 0..3 (or 4..7) of each half
+__device__ __forceinline__ uint32_t low_codes(uint32_t x) { return ((x << 3) & 0x00780078u) | 0x41804180u; }
+__device__ __forceinline__ uint32_t high_codes(uint32_t x) { return ((x >> 1) & 0x00780078u) | 0x41804180u; }
+
+__device__ __forceinline__ f32x4 zero4() { return f32x4{0.f, 0.f, 0.f, 0.f}; }
+
+// GK, GV: groups of keys and values.
+template <typename T, int GK, int GV>
+__device__ __forceinline__ void packed_stretch_rows(const SoftmaxStepArgs& a, int64_t kvh, int block, int at, int first, int end,
+                                                    float* part, float* sums, StepState (*state)[kPackedMembers],
+                                                    uint8_t* fresh) {
+  constexpr int kPl = sizeof(T) == 4 ? 3 : 1;    // numbers of a query's entry
+  constexpr int kWeight = sizeof(T) == 4 ? 3 : 2;  // of a weight
+  constexpr int kKey = 20 * GK, kValue = 20 * GV, kThreads = 64 * kStepWaves;
+  const int tid = threadIdx.x, lane = tid & 63, l15 = lane & 15, t4 = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int dk = a.dk_, dv = a.dv_;
+  const int members = min(kPackedMembers, a.G - kPackedMembers * block);
+  const int64_t q0 = kvh * a.G + kPackedMembers * block;  // the block's first query head
+  if (at < 0 || at >= a.capacity) {  // no token
+    for (int i = tid; i < members * dv; i += kThreads) ((T*)a.y)[q0 * dv + i] = (T)0;
+    return;
+  }
+  uint8_t* const K = (uint8_t*)a.K + kvh * a.capacity * kKey;
+  uint8_t* const V = (uint8_t*)a.V + kvh * a.capacity * kValue;
+  // ---- the new row, in LDS for this workgroup (whoever writes the cache's) and in the cache
+  if (at < end) {
+    if (wave == 0) {
+      const bool key = lane < 16;
+      if (lane < 32) {
+        if (key) {
+          uint32_t params[GK];
+          const T* const x = (const T*)a.k + kvh * dk;
+          const uint32_t codes = pack_row<GK>(l15, dk, [&](int e) { return entry_of(x, e); }, params);
+          store_packed<GK>(fresh, l15, codes, params);
+          if (block == 0) store_packed<GK>(K + (int64_t)at * kKey, l15, codes, params);
+        } else {
+          uint32_t params[GV];
+          const T* const x = (const T*)a.v + kvh * dv;
+          const uint32_t codes = pack_row<GV>(l15, dv, [&](int e) { return entry_of(x, e); }, params);
+          store_packed<GV>(fresh + 80, l15, codes, params);
+          if (block == 0) store_packed<GV>(V + (int64_t)at * kValue, l15, codes, params);
+        }
+      }
+    }
+    __syncthreads();
+  }
+  // ---- the query heads: operands of entries 32 g + 4 t4 .. +3 and 32 g + 16 + 4 t4 .. +3, in the codes' order, and
+  // the sums over the groups as three bfloat16 numbers, one in each of the first three fours of
+  // lanes
+  uint4 qf[GK][kPl], qsum;
+  {
+    const T* const q = (const T*)a.q + (q0 + l15) * dk;
+    float total[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int g = 0; g < GK; ++g) {
+      float x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        // (dwords in the order of the products' operands: low codes of a = 0, 1, then of 2, 3, then the high ones)
+        const int e = 32 * g + 4 * t4 + (i & 3) + 16 * (i >> 2);
+        x[i] = l15 < members && e < dk ? entry_of(q, e) : 0.f;
+        total[g] += x[i];
+      }
+      total[g] += __shfl_xor(total[g], 16);
+      total[g] += __shfl_xor(total[g], 32);
+      uint4 w[1][kPl];
+      to_planes<kPl>(x, w);
+#pragma unroll
+      for (int p = 0; p < kPl; ++p) qf[g][p] = w[0][p];
+    }
+    float x[8];
+#pragma unroll
+    for (int g = 0; g < 4; ++g) x[2 * g] = g < GK ? -16.f * total[g] : 0.f, x[2 * g + 1] = g < GK ? total[g] : 0.f;
+    uint4 w[1][3];
+    to_planes<3>(x, w);
+    qsum = t4 == 0 ? w[0][0] : t4 == 1 ? w[0][1] : t4 == 2 ? w[0][2] : uint4{0u, 0u, 0u, 0u};
+  }
+  f32x4 o[2 * GV];
+  float base[GV];
+#pragma unroll
+  for (int j = 0; j < 2 * GV; ++j) o[j] = zero4();
+#pragma unroll
+  for (int g = 0; g < GV; ++g) base[g] = 0.f;
+  float top = -3.4028234e38f, sum = 0.f;
+  const float c = a.scale * kLog2e;
+  constexpr int kStep = 32 * kStepWaves;
+#pragma unroll 1
+  for (int r0 = first + 32 * wave; r0 < end; r0 += kStep) {
+    // Rows behind the last one are read as the last one, and the last one, which others may be writing, from LDS.
+    const bool last = at < r0 + 32;
+    auto key_row = [&](int r) -> const uint8_t* { return K + (int64_t)min(r, at) * kKey; };
+    auto value_row = [&](int r) -> const uint8_t* { return V + (int64_t)min(r, at) * kValue; };
+    KeyCodes<GK> kc[2], kp[2], ks[2][4];
+    uint32_t vc[8];
+    KeyCodes<GV> vp[8];
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const uint8_t* const row = key_row(r0 + 16 * x + l15);
+      kc[x] = load_key<GK>(row + 4 * GK * t4);
+      kp[x] = load_params<GK>(row);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) ks[x][i] = load_params<GK>(key_row(r0 + 16 * x + 4 * t4 + i));
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint8_t* const row = value_row(r0 + 4 * t4 + 16 * (i >> 2) + (i & 3));
+      vc[i] = load_packed<GV>(row, l15);
+      vp[i] = load_params<GV>(row);
+    }
+    if (last) {
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        if (r0 + 16 * x + l15 >= at) kc[x] = load_key<GK>(fresh + 4 * GK * t4), kp[x] = load_params<GK>(fresh);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (r0 + 16 * x + 4 * t4 + i >= at) ks[x][i] = load_params<GK>(fresh);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (r0 + 4 * t4 + 16 * (i >> 2) + (i & 3) >= at) vc[i] = load_packed<GV>(fresh + 80, l15), vp[i] = load_params<GV>(fresh + 80);
+    }
+    // ---- scores of tokens 4 t4 .. +3 and 16 + 4 t4 .. +3 with query head l15
+    float s[8];
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      uint4 m = {0u, 0u, 0u, 0u};
+      m.x = kp[x].w[0];
+      if constexpr (GK >= 2) m.y = kp[x].w[1];
+      if constexpr (GK == 4) m.z = kp[x].w[2], m.w = kp[x].w[3];
+      f32x4 score = mfma_bf16(m, qsum, zero4());
+#pragma unroll
+      for (int g = 0; g < GK; ++g) {
+        uint32_t u, w;
+        group_bytes<GK>(kc[x], g, u, w);
+        const uint4 e = {low_codes(u), low_codes(w), high_codes(u), high_codes(w)};
+        f32x4 acc = zero4();
+#pragma unroll
+        for (int p = kPl - 1; p >= 0; --p) acc = mfma_bf16(e, qf[g][p], acc);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) score[i] = fmaf(lo_f32(ks[x][i].w[g]), acc[i], score[i]);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[4 * x + i] = score[i];
+    }
+    float most = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      s[i] = r0 + 4 * t4 + 16 * (i >> 2) + (i & 3) > at ? -INFINITY : s[i];
+      most = fmaxf(most, s[i]);
+    }
+    most *= c;
+    if (__ballot(most > top + 8.f)) {
+      float next = fmaxf(most, __shfl_xor(most, 16));
+      next = fmaxf(top, fmaxf(next, __shfl_xor(next, 32)));
+      const float keep = exp2_fast(top - next);
+      top = next;
+      sum *= keep;
+#pragma unroll
+      for (int j = 0; j < 2 * GV; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[j][i] *= keep;
+#pragma unroll
+      for (int g = 0; g < GV; ++g) base[g] *= keep;
+    }
+    // ---- weights, times the scales, and the values
+    float z[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      z[i] = exp2_fast(fmaf(s[i], c, -top));
+      sum += z[i];
+    }
+    uint32_t pairs[4][2];  // bytes of tokens 2 i and 2 i + 1, groups 0, 1 and 2, 3
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      pairs[i][0] = __builtin_amdgcn_perm(vc[2 * i + 1], vc[2 * i], 0x05040100);
+      pairs[i][1] = __builtin_amdgcn_perm(vc[2 * i + 1], vc[2 * i], 0x07060302);
+    }
+#pragma unroll
+    for (int g = 0; g < GV; ++g) {
+      float y[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float scale = lo_f32(vp[i].w[g]);
+        y[i] = z[i] * scale;
+        base[g] = fmaf(z[i], fmaf(-16.f, scale, hi_f32(vp[i].w[g])), base[g]);
+      }
+      uint4 w[1][kWeight];
+      to_planes<kWeight>(y, w);
+      uint32_t lo[4], hi[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t x = pairs[i][g >> 1] >> (8 * (g & 1));
+        lo[i] = low_codes(x), hi[i] = high_codes(x);
+      }
+#pragma unroll
+      for (int p = kWeight - 1; p >= 0; --p) {
+        o[2 * g] = mfma_bf16(uint4{lo[0], lo[1], lo[2], lo[3]}, w[0][p], o[2 * g]);
+        o[2 * g + 1] = mfma_bf16(uint4{hi[0], hi[1], hi[2], hi[3]}, w[0][p], o[2 * g + 1]);
+      }
+    }
+  }
+  settle_mfma32();
+  sum += __shfl_xor(sum, 16);
+  sum += __shfl_xor(sum, 32);
+#pragma unroll
+  for (int g = 0; g < GV; ++g) {
+    base[g] += __shfl_xor(base[g], 16);
+    base[g] += __shfl_xor(base[g], 32);
+  }
+
+  // ---- the waves' sums joined, in their order
+  if (t4 == 0) state[wave][l15] = StepState{top, sum};
+  if (l15 < members) {
+    float* const row = sums + (wave * members + l15) * dv;
+#pragma unroll
+    for (int j = 0; j < 2 * GV; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int col = 16 * j + 4 * t4 + i;
+        if (col < dv) row[col] = o[j][i] + base[j / 2];
+      }
+  }
+  __syncthreads();
+  for (int i = tid; i < members * dv; i += kThreads) {
+    const int m = i / dv, col = i - m * dv;
+    float most = state[0][m].top;
+#pragma unroll
+    for (int w = 1; w < kStepWaves; ++w) most = fmaxf(most, state[w][m].top);
+    float x = 0.f, l = 0.f;
+#pragma unroll
+    for (int w = 0; w < kStepWaves; ++w) {
+      const float k = exp2_fast(state[w][m].top - most);
+      x = fmaf(sums[(w * members + m) * dv + col], k, x);
+      l = fmaf(state[w][m].sum, k, l);
+    }
+    if (!part) {
+      ((T*)a.y)[(q0 + m) * dv + col] = rounded<T>(x / l);
+    } else {
+      float* const out = part + m * (dv + 2);
+      out[col] = x;
+      if (col == 0) out[dv] = most, out[dv + 1] = l;
+    }
+  }
+}
+
+template <typename T, int GK, int GV>
+__global__ void __launch_bounds__(64 * kStepWaves, 2) softmax_step_packed_kernel(SoftmaxStepArgs a, SoftmaxStepPlan p) {
+  extern __shared__ float sums_of[];  // [wave][member][dv]
+  __shared__ StepState state[kStepWaves][kPackedMembers];
+  __shared__ __attribute__((aligned(16))) uint8_t fresh[160];  // the new rows
+  StepPlace f;
+  if (!find_stretch(a, p, f)) return;
+  const int id = blockIdx.x, heads_of = a.H * p.blocks, head = f.hb / p.blocks;
+  const int at = a.lengths[f.b], first = f.stretch * f.len * p.unit;
+  const int64_t place = (int64_t)f.b * heads_of + f.hb;
+  int2* const found = (int2*)a.scratch;
+  float* const sums = (float*)(found + (int64_t)a.heads * p.blocks);
+  if (p.bytes && f.stretch == 0 && threadIdx.x == 0) found[place] = int2{id, f.count};
+  packed_stretch_rows<T, GK, GV>(a, (int64_t)f.b * a.H + head, f.hb - head * p.blocks, at, first,
+                                 min(at + 1, first + f.len * p.unit),
+                                 f.count == 1 ? nullptr : sums + (int64_t)id * min(kPackedMembers, a.G) * (a.dv_ + 2), sums_of,
+                                 state, fresh);
+}
+
+template <typename T, int GK, int GV>
+hipError_t launch_step(const SoftmaxStepArgs& a, const SoftmaxStepPlan& p, hipStream_t s) {
+  const int bytes = kStepWaves * std::min(kPackedMembers, a.G) * a.dv_ * (int)sizeof(float);  // (32 KB at most)
+  hipLaunchKernelGGL((softmax_step_packed_kernel<T, GK, GV>), dim3(p.workgroups), dim3(64 * kStepWaves), bytes, s, a, p);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.bytes == 0) return e;
+  hipLaunchKernelGGL(softmax_join_kernel<T>, dim3(a.heads * a.G), dim3((a.dv_ + 63) / 64 * 64), 0, s, a, p);
+  return hipGetLastError();
+}
+
+template <typename T, int GK>
+hipError_t launch_values(const SoftmaxStepArgs& a, const SoftmaxStepPlan& p, hipStream_t s) {
+  switch (packed_groups(a.dv_)) {
+    case 1: return launch_step<T, GK, 1>(a, p, s);
+    case 2: return launch_step<T, GK, 2>(a, p, s);
+    default: return launch_step<T, GK, 4>(a, p, s);
+  }
+}
+template <typename T>
+hipError_t launch_keys(const SoftmaxStepArgs& a, const SoftmaxStepPlan& p, hipStream_t s) {
+  switch (packed_groups(a.dk_)) {
+    case 1: return launch_values<T, 1>(a, p, s);
+    case 2: return launch_values<T, 2>(a, p, s);
+    default: return launch_values<T, 4>(a, p, s);
+  }
+}
+
+}  // namespace
+
+SoftmaxStepPlan plan_softmax_step_packed(bool bf16, int heads, int H, int G, int capacity, int dv) {
+  return plan_softmax_step(bf16, heads, H, G, capacity, dv, kPackedMembers);
+}
+
+hipError_t launch_softmax_step_packed(const SoftmaxStepArgs& a, bool bf16, hipStream_t s) {
+  const SoftmaxStepPlan p = plan_softmax_step_packed(bf16, a.heads, a.H, a.G, a.capacity, a.dv_);
+  return bf16 ? launch_keys<u16>(a, p, s) : launch_keys<float>(a, p, s);
+}
+
+}  // namespace sata
