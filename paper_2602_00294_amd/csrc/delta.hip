@@ -5,6 +5,7 @@
 #include <algorithm>
 
 #include "decay_power.hpp"
+#include "delta_tiles.hpp"
 #include "device_common.hpp"
 #include "kernels.hpp"
 #include "pair_tiles.hpp"
@@ -84,12 +85,308 @@ hipError_t launch_tokens(const DeltaArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
+// ---- chunk by chunk
+//
+// A wave has 16 columns of the state, S[j] rows 16 j + 4 t4 .. +3 of column l15, for a head's whole sequence; four waves
+// make a workgroup and share the staged queries and keys.  For a chunk (delta_tiles.hpp)
+//     R = k S,  r = v - early R,  E = inverse r,  y = c early q S + P E,  S = whole S + k^T (late E),
+// each a product whose right operand is what the one before left in this lane.
+constexpr int kScanWaves = 4;
+
+// One of the buffers in LDS: a chunk's keys, queries and what its pairs left.
+template <typename T, int ND>
+struct DeltaLds {
+  using L = PairTile<T, ND, kDeltaChunk>;
+  using Data = DeltaChunkData<sizeof(T) == 2>;
+  static constexpr int kBuffers = sizeof(T) == 2 ? 2 : 1;
+  static constexpr int kBuffer = 2 * L::kBytes + (int)sizeof(Data);
+  static constexpr int kBytes = kBuffers * kBuffer;
+};
+
+// `sizeof(D)` bytes on their way into LDS.
+template <typename D, int THREADS>
+struct DataStage {
+  static_assert(sizeof(D) % 16 == 0, "whole vectors");
+  static constexpr int kVectors = sizeof(D) / 16, kIt = (kVectors + THREADS - 1) / THREADS;
+  uint4 r[kIt];
+  __device__ __forceinline__ void fetch(const D* d, int tid) {
+#pragma unroll
+    for (int i = 0; i < kIt; ++i)
+      if (tid + i * THREADS < kVectors) r[i] = ((const uint4*)d)[tid + i * THREADS];
+  }
+  __device__ __forceinline__ void put(D* d, int tid) const {
+#pragma unroll
+    for (int i = 0; i < kIt; ++i)
+      if (tid + i * THREADS < kVectors) ((uint4*)d)[tid + i * THREADS] = r[i];
+  }
+};
+
+// Entries of rows 16 x + 4 t4 .. +3 (x = 0, 1) of this lane's column, zero behind `rows`.
+template <typename T>
+__device__ __forceinline__ void fetch_column(const T* p, int rows, int pitch, bool on, T (&v)[8]) {
+  const int t4 = (threadIdx.x & 63) >> 4;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const int r = 16 * (e >> 2) + 4 * t4 + (e & 3);
+    v[e] = on && r < rows ? p[(int64_t)r * pitch] : (T)0;
+  }
+}
+
+// A chunk's tokens one by one, for chunks in which something is not finite: products would take it to earlier tokens,
+// whose weights of it are zero.
+template <typename T, int ND>
+__device__ __forceinline__ void delta_one_by_one(const DeltaArgs& a, int head, int64_t shared, int t0, int m, int col, bool on,
+                                                 f32x4 (&S)[2 * ND], T* y, float* errors) {
+  const int t4 = (threadIdx.x & 63) >> 4;
+  const T* const q = (const T*)a.q + shared * a.n * a.dk;
+  const T* const k = (const T*)a.k + shared * a.n * a.dk;
+  for (int t = t0; t < t0 + m; ++t) {
+    const float lam = (float)exp(delta_rate(a.g[(int64_t)head * a.n + t])), beta = a.beta[(int64_t)head * a.n + t];
+    float p = 0.f;
+#pragma unroll 1
+    for (int j = 0; j < 2 * ND; ++j) {
+      f32x4 s = S[0];
+#pragma unroll
+      for (int x = 1; x < 2 * ND; ++x) s = j == x ? S[x] : s;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int row = 16 * j + 4 * t4 + i;
+        s[i] *= lam;
+        p = row < a.dk ? fmaf(entry_of(k, (int64_t)t * a.dk + row), s[i], p) : p;
+      }
+#pragma unroll
+      for (int x = 0; x < 2 * ND; ++x) S[x] = j == x ? s : S[x];
+    }
+    p += __shfl_xor(p, 16);
+    p += __shfl_xor(p, 32);
+    const float e = on ? entry_of((const T*)a.v, ((int64_t)head * a.n + t) * a.dv + col) - p : 0.f;
+    const float u = on ? beta * e : 0.f;
+    if (errors && on && t4 == 0) errors[((int64_t)head * a.n + t) * a.dv + col] = e;
+    p = 0.f;
+#pragma unroll 1
+    for (int j = 0; j < 2 * ND; ++j) {
+      f32x4 s = S[0];
+#pragma unroll
+      for (int x = 1; x < 2 * ND; ++x) s = j == x ? S[x] : s;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int row = 16 * j + 4 * t4 + i;
+        s[i] = row < a.dk ? fmaf(entry_of(k, (int64_t)t * a.dk + row), u, s[i]) : s[i];
+        p = row < a.dk ? fmaf(entry_of(q, (int64_t)t * a.dk + row), s[i], p) : p;
+      }
+#pragma unroll
+      for (int x = 0; x < 2 * ND; ++x) S[x] = j == x ? s : S[x];
+    }
+    p += __shfl_xor(p, 16);
+    p += __shfl_xor(p, 32);
+    if (y && on && t4 == 0) y[(int64_t)t * a.dv + col] = rounded<T>(p * a.scale);
+  }
+}
+
+// GRAD: no outputs, but the errors and the states before every block.
+template <typename T, int ND, bool GRAD>
+__global__ void __launch_bounds__(64 * kScanWaves, 2) delta_scan_kernel(DeltaArgs a, const void* data_, float* states, float* errors,
+                                                                        int slices) {
+  extern __shared__ __attribute__((aligned(16))) u16 smem16[];
+  constexpr bool BF16 = sizeof(T) == 2;
+  constexpr int C = kDeltaChunk, kThreads = 64 * kScanWaves;
+  using D = DeltaLds<T, ND>;
+  using L = typename D::L;
+  using Data = DeltaChunkData<BF16>;
+  constexpr int PE = Data::kPair, PY = BF16 ? 2 : 3;  // numbers of an error and of a state's entry in the outputs
+  int head, slice;
+  if (!delta_place(a.heads, slices, head, slice)) return;
+  const int tid = threadIdx.x, lane = tid & 63, l15 = lane & 15, t4 = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int64_t shared = head / a.G;
+  const int len = tokens_of(a.lengths, head / (a.Hk * a.G), a.n), chunks = (len + C - 1) / C;
+  const int c0 = 16 * (kScanWaves * slice + wave), col = c0 + l15;
+  const bool on = col < a.dv;
+  const int64_t size = (int64_t)a.dk * a.dv;
+  f32x4 S[2 * ND];
+#pragma unroll
+  for (int j = 0; j < 2 * ND; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int row = 16 * j + 4 * t4 + i;
+      S[j][i] = a.S_in && on && row < a.dk ? a.S_in[head * size + (int64_t)row * a.dv + col] : 0.f;
+    }
+  auto put_state = [&](float* to) {
+#pragma unroll
+    for (int j = 0; j < 2 * ND; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int row = 16 * j + 4 * t4 + i;
+        if (on && row < a.dk) to[(int64_t)row * a.dv + col] = S[j][i];
+      }
+  };
+  const T* const v = (const T*)a.v + (int64_t)head * a.n * a.dv + col;
+  T* const y = GRAD ? nullptr : (T*)a.y + (int64_t)head * a.n * a.dv;
+  const bool vec = a.dv % 4 == 0 && ((uintptr_t)y & (4 * sizeof(T) - 1)) == 0;
+  if (chunks > 0) {
+    const Data* const data = (const Data*)data_ + (int64_t)head * ((a.n + C - 1) / C);
+    TileStage<T, ND, C, kThreads> sq, sk;
+    sq.init((const T*)a.q + shared * a.n * a.dk, len, a.dk, tid);
+    sk.init((const T*)a.k + shared * a.n * a.dk, len, a.dk, tid);
+    DataStage<Data, kThreads> sd;
+    T next[8];
+    sk.fetch(0);
+    if (!GRAD) sq.fetch(0);
+    sd.fetch(data, tid);
+    fetch_column(v, len, a.dv, on, next);
+    for (int c = 0; c < chunks; ++c) {
+      const int t0 = c * C;
+      u16* const tk = smem16 + (D::kBuffers == 2 && (c & 1) ? D::kBuffer / 2 : 0);
+      u16* const tq = tk + L::kElems;
+      Data& d = *(Data*)(tq + L::kElems);
+      if (D::kBuffers == 1) __syncthreads();
+      sk.put(tk, t0);
+      if (!GRAD) sq.put(tq, t0);
+      sd.put(&d, tid);
+      __syncthreads();
+      float r[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) r[e] = entry_of(&next[e], 0);
+      if (c + 1 < chunks) {
+        sk.fetch(t0 + C);
+        if (!GRAD) sq.fetch(t0 + C);
+        sd.fetch(data + c + 1, tid);
+        fetch_column(v + (int64_t)(t0 + C) * a.dv, len - t0 - C, a.dv, on, next);
+      }
+      if (GRAD && c % (kDeltaBlock / C) == 0)
+        put_state(states + ((int64_t)head * ((a.n + kDeltaBlock - 1) / kDeltaBlock) + c / (kDeltaBlock / C)) * size);
+      f32x4 R[2] = {zero4(), zero4()}, o[2] = {zero4(), zero4()};
+#pragma unroll
+      for (int b = 0; b < ND; ++b) {
+        uint4 st[3];
+        operand_of<3>(S[2 * b], S[2 * b + 1], st);
+        uint4 so[PY];
+#pragma unroll
+        for (int p = 0; p < PY; ++p) so[p] = st[p];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          uint4 e[L::kPl];
+          rows16_as_results<L>(tk, 16 * x, b, e);
+          R[x] = dot_planes16(e, st, R[x]);
+          if (!GRAD) {
+            rows16_as_results<L>(tq, 16 * x, b, e);
+            o[x] = dot_planes16(so, e, o[x]);
+          }
+        }
+      }
+      float most = 0.f;
+      f32x4 early[2] = {*(const f32x4*)(d.early + 4 * t4), *(const f32x4*)(d.early + 16 + 4 * t4)};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        r[e] = fmaf(-early[e >> 2][e & 3], R[e >> 2][e & 3], r[e]);
+        most = r[e] - r[e] == 0.f ? most : 1.f;  // (an infinity's difference with itself is no number)
+      }
+      uint4 rp[3];
+      operand_of<3>(r, rp);
+      f32x4 E[2];
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        uint4 inv[Data::kInverse];
+#pragma unroll
+        for (int p = 0; p < Data::kInverse; ++p) inv[p] = d.inverse[p][x][lane];
+        E[x] = dot_planes16(inv, rp, zero4());
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) most = E[e >> 2][e & 3] - E[e >> 2][e & 3] == 0.f ? most : 1.f;
+      settle_mfma();
+      if (__builtin_expect(__ballot(most != 0.f) != 0, 0)) {
+        delta_one_by_one<T, ND>(a, head, shared, t0, min(C, len - t0), col, on, S, y, GRAD ? errors : nullptr);
+        continue;
+      }
+      if (GRAD) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int t = t0 + 16 * (e >> 2) + 4 * t4 + (e & 3);
+          if (on && t < len) errors[((int64_t)head * a.n + t) * a.dv + col] = E[e >> 2][e & 3];
+        }
+      } else {
+        uint4 ep[PE];
+        operand_of<PE>(E[0], E[1], ep);
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[x][i] *= d.early[16 * x + l15] * a.scale;
+          uint4 pairs[PE];
+#pragma unroll
+          for (int p = 0; p < PE; ++p) pairs[p] = d.pairs[p][x][lane];
+          o[x] = dot_planes16(ep, pairs, o[x]);
+        }
+      }
+      float w[8];
+      f32x4 late[2] = {*(const f32x4*)(d.late + 4 * t4), *(const f32x4*)(d.late + 16 + 4 * t4)};
+      const float whole = d.whole[0];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[e] = E[e >> 2][e & 3] * late[e >> 2][e & 3];
+      uint4 wp[3];
+      operand_of<3>(w, wp);
+#pragma unroll
+      for (int j = 0; j < 2 * ND; ++j) {
+        uint4 e[L::kPl];
+        columns16<L>(tk, 0, j, e);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) S[j][i] *= whole;
+        S[j] = dot_planes16(e, wp, S[j]);
+      }
+      if (!GRAD) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const int t = t0 + 16 * x + l15;
+          const float z[4] = {o[x][0], o[x][1], o[x][2], o[x][3]};
+          if (t < len) store4<T>(y + (int64_t)t * a.dv, c0 + 4 * t4, a.dv, z, vec);
+        }
+      }
+      settle_mfma();
+    }
+  }
+  if (!GRAD && a.S_out) put_state(a.S_out + head * size);
+  if (!GRAD && on) {  // rows behind the sequence
+    for (int t = len + t4; t < a.n; t += 4) y[(int64_t)t * a.dv + col] = (T)0;
+  }
+}
+
+template <typename T, int ND, bool GRAD>
+hipError_t launch_scan(const DeltaArgs& a, const void* data, float* states, float* errors, hipStream_t s) {
+  constexpr int bytes = DeltaLds<T, ND>::kBytes;
+  auto kern = delta_scan_kernel<T, ND, GRAD>;
+  if (bytes > 64 * 1024) {
+    hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != hipSuccess) return e;
+  }
+  const int slices = (a.dv + 16 * kScanWaves - 1) / (16 * kScanWaves);
+  hipLaunchKernelGGL(kern, dim3(delta_grid(a.heads, slices)), dim3(64 * kScanWaves), bytes, s, a, data, states, errors, slices);
+  return hipGetLastError();
+}
+
+template <typename T, bool GRAD>
+hipError_t launch_scan_t(const DeltaArgs& a, const void* data, float* states, float* errors, hipStream_t s) {
+  switch ((a.dk + 31) / 32) {
+    case 1: return launch_scan<T, 1, GRAD>(a, data, states, errors, s);
+    case 2: return launch_scan<T, 2, GRAD>(a, data, states, errors, s);
+    case 3: return launch_scan<T, 3, GRAD>(a, data, states, errors, s);
+    default: return launch_scan<T, 4, GRAD>(a, data, states, errors, s);
+  }
+}
+
 }  // namespace
 
-size_t delta_prefill_scratch(bool, int, int, int, int, int) { return 0; }
+size_t delta_prefill_scratch(bool bf16, int heads, int, int n, int, int) {
+  return delta_data_bytes(bf16, heads, n);
+}
 
-hipError_t launch_delta_prefill(const DeltaArgs& a, bool bf16, void*, hipStream_t s) {
-  return bf16 ? launch_tokens<u16>(a, s) : launch_tokens<float>(a, s);
+hipError_t launch_delta_prefill(const DeltaArgs& a, bool bf16, void* scratch, hipStream_t s) {
+  if (a.n == 0) return bf16 ? launch_tokens<u16>(a, s) : launch_tokens<float>(a, s);
+  hipError_t e = launch_delta_pairs(a, bf16, scratch, nullptr, s);
+  if (e != hipSuccess) return e;
+  return bf16 ? launch_scan_t<u16, false>(a, scratch, nullptr, nullptr, s) : launch_scan_t<float, false>(a, scratch, nullptr, nullptr, s);
+}
+
+hipError_t launch_delta_states(const DeltaArgs& a, bool bf16, const void* data, float* states, float* errors, hipStream_t s) {
+  return bf16 ? launch_scan_t<u16, true>(a, data, states, errors, s) : launch_scan_t<float, true>(a, data, states, errors, s);
 }
 
 }  // namespace sata
