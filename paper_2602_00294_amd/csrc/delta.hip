@@ -103,35 +103,6 @@ struct DeltaLds {
   static constexpr int kBytes = kBuffers * kBuffer;
 };
 
-// `sizeof(D)` bytes on their way into LDS.
-template <typename D, int THREADS>
-struct DataStage {
-  static_assert(sizeof(D) % 16 == 0, "whole vectors");
-  static constexpr int kVectors = sizeof(D) / 16, kIt = (kVectors + THREADS - 1) / THREADS;
-  uint4 r[kIt];
-  __device__ __forceinline__ void fetch(const D* d, int tid) {
-#pragma unroll
-    for (int i = 0; i < kIt; ++i)
-      if (tid + i * THREADS < kVectors) r[i] = ((const uint4*)d)[tid + i * THREADS];
-  }
-  __device__ __forceinline__ void put(D* d, int tid) const {
-#pragma unroll
-    for (int i = 0; i < kIt; ++i)
-      if (tid + i * THREADS < kVectors) ((uint4*)d)[tid + i * THREADS] = r[i];
-  }
-};
-
-// Entries of rows 16 x + 4 t4 .. +3 (x = 0, 1) of this lane's column, zero behind `rows`.
-template <typename T>
-__device__ __forceinline__ void fetch_column(const T* p, int rows, int pitch, bool on, T (&v)[8]) {
-  const int t4 = (threadIdx.x & 63) >> 4;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const int r = 16 * (e >> 2) + 4 * t4 + (e & 3);
-    v[e] = on && r < rows ? p[(int64_t)r * pitch] : (T)0;
-  }
-}
-
 // A chunk's tokens one by one, for chunks in which something is not finite: products would take it to earlier tokens,
 // whose weights of it are zero.
 template <typename T, int ND>

@@ -1,6 +1,647 @@
+// Gradients of the gated delta rule, in four passes: what the chunks' pairs leave (delta_pairs.hip), forward for the
+// states before every 64 tokens and the errors E = v - k S' (delta.hip), backward for the states' gradients U
+// and z = dL/du, and then, all blocks of 64 tokens side by side, what a block's tokens
+// make of these.  With G_i the sums of the log decays in a chunk, L and the letters of delta_tiles.hpp, D = -beta z,
+// S the state before the chunk and U the gradient behind it:
+//     du  = P0^T dy + exp(G_C - G) (k U),   P0_ij = c exp(G_i - G_j) q_i.k_j (j <= i)
+//     z   = (I + beta L)^-T du,   dv = beta z,   dbeta = z.E
+//     U   = exp(G_C) U + (c exp(G) q)^T dy + (exp(G) k)^T D
+//     dq  = c exp(G) dy S^T + one k,                 one_ij = c exp(G_i - G_j) dy_i.u_j (j <= i)
+//     dk  = asked + kept,  asked = exp(G) D S^T + two k,   two_ij = exp(G_i - G_j) D_i.u_j (j < i)
+//                          kept  = one^T q + two^T k + exp(G_C - G) u U^T
+//     dg_t = sum_{i>=t} (q.dq + k.asked - k.kept)_i + <U, S behind the block>:
+// every term that grows with G_i counts for it, every one that falls against it.
 #include <hip/hip_runtime.h>
-#include "kernels.hpp"
+
+#include <algorithm>
+
+#include "delta_tiles.hpp"
+
 namespace sata {
-size_t delta_backward_scratch(bool, int, int, int, int, int) { return 0; }
-hipError_t launch_delta_backward(const DeltaArgs&, bool, void*, hipStream_t) { return hipErrorNotSupported; }
+
+namespace {
+
+constexpr int C = kDeltaChunk, kBlock = kDeltaBlock;
+constexpr int kBackWaves = 4, kBackThreads = 64 * kBackWaves;
+
+// ---- from the last token back: a wave has 16 columns of U, as the forward scan of S
+template <typename T, int ND>
+struct BackLds {
+  using L = PairTile<T, ND, C>;
+  using Data = DeltaChunkBack<sizeof(T) == 2>;
+  static constexpr int kBuffers = sizeof(T) == 2 ? 2 : 1;
+  static constexpr int kBuffer = 2 * L::kBytes + (int)sizeof(Data);
+  static constexpr int kBytes = kBuffers * kBuffer;
+};
+
+template <typename T, int ND>
+__global__ void __launch_bounds__(kBackThreads, 2) delta_back_kernel(DeltaArgs a, const void* data_, float* behind, float* zs, int slices) {
+  extern __shared__ __attribute__((aligned(16))) u16 smem16[];
+  using D = BackLds<T, ND>;
+  using L = typename D::L;
+  using Data = typename D::Data;
+  int head, slice;
+  if (!delta_place(a.heads, slices, head, slice)) return;
+  const int tid = threadIdx.x, lane = tid & 63, l15 = lane & 15, t4 = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int64_t shared = head / a.G;
+  const int len = tokens_of(a.lengths, head / (a.Hk * a.G), a.n), chunks = (len + C - 1) / C;
+  const int col = 16 * (kBackWaves * slice + wave) + l15;
+  const bool on = col < a.dv;
+  const int64_t size = (int64_t)a.dk * a.dv;
+  f32x4 U[2 * ND];
+#pragma unroll
+  for (int j = 0; j < 2 * ND; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int row = 16 * j + 4 * t4 + i;
+      U[j][i] = a.dS && on && row < a.dk ? a.dS[head * size + (int64_t)row * a.dv + col] : 0.f;
+    }
+  auto put_state = [&](float* to) {
+#pragma unroll
+    for (int j = 0; j < 2 * ND; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int row = 16 * j + 4 * t4 + i;
+        if (on && row < a.dk) to[(int64_t)row * a.dv + col] = U[j][i];
+      }
+  };
+  T* const dv = (T*)a.dv_out + (int64_t)head * a.n * a.dv + col;
+  if (chunks > 0) {
+    const Data* const data = (const Data*)data_ + (int64_t)head * ((a.n + C - 1) / C);
+    const T* const dy = (const T*)a.dy + (int64_t)head * a.n * a.dv + col;
+    float* const z_out = zs + (int64_t)head * a.n * a.dv + col;
+    TileStage<T, ND, C, kBackThreads> sq, sk;
+    sq.init((const T*)a.q + shared * a.n * a.dk, len, a.dk, tid);
+    sk.init((const T*)a.k + shared * a.n * a.dk, len, a.dk, tid);
+    DataStage<Data, kBackThreads> sd;
+    T next[8];
+    auto fetch = [&](int c) {
+      sk.fetch(c * C);
+      sq.fetch(c * C);
+      sd.fetch(data + c, tid);
+      fetch_column(dy + (int64_t)c * C * a.dv, len - c * C, a.dv, on, next);
+    };
+    fetch(chunks - 1);
+    for (int c = chunks - 1; c >= 0; --c) {
+      const int t0 = c * C;
+      u16* const tk = smem16 + (D::kBuffers == 2 && (c & 1) ? D::kBuffer / 2 : 0);
+      u16* const tq = tk + L::kElems;
+      Data& d = *(Data*)(tq + L::kElems);
+      if (D::kBuffers == 1) __syncthreads();
+      sk.put(tk, t0);
+      sq.put(tq, t0);
+      sd.put(&d, tid);
+      __syncthreads();
+      float y[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = entry_of(&next[e], 0);
+      if (c > 0) fetch(c - 1);
+      if (c == chunks - 1 || c % (kBlock / C) == kBlock / C - 1)
+        put_state(behind + ((int64_t)head * ((a.n + kBlock - 1) / kBlock) + c / (kBlock / C)) * size);
+      f32x4 R[2] = {zero4(), zero4()}, du[2];
+#pragma unroll
+      for (int b = 0; b < ND; ++b) {
+        uint4 st[3];
+        operand_of<3>(U[2 * b], U[2 * b + 1], st);
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          uint4 e[L::kPl];
+          rows16_as_results<L>(tk, 16 * x, b, e);
+          R[x] = dot_planes16(e, st, R[x]);
+        }
+      }
+      const f32x4 early[2] = {*(const f32x4*)(d.early + 4 * t4), *(const f32x4*)(d.early + 16 + 4 * t4)};
+      const f32x4 late[2] = {*(const f32x4*)(d.late + 4 * t4), *(const f32x4*)(d.late + 16 + 4 * t4)};
+      const f32x4 beta[2] = {*(const f32x4*)(d.beta + 4 * t4), *(const f32x4*)(d.beta + 16 + 4 * t4)};
+      const float whole = d.whole[0];
+      {
+        float x8[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x8[e] = y[e];
+        uint4 yp[L::kPl];
+        operand_of<L::kPl>(x8, yp);
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          uint4 p[3];
+#pragma unroll
+          for (int i = 0; i < 3; ++i) p[i] = d.pairs[i][x][lane];
+          du[x] = dot_planes16(p, yp, zero4());
+#pragma unroll
+          for (int i = 0; i < 4; ++i) du[x][i] = fmaf(late[x][i], R[x][i], du[x][i]);
+        }
+      }
+      uint4 dp[3];
+      operand_of<3>(du[0], du[1], dp);
+      f32x4 z[2];
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        uint4 p[3];
+#pragma unroll
+        for (int i = 0; i < 3; ++i) p[i] = d.inverse[i][x][lane];
+        z[x] = dot_planes16(p, dp, zero4());
+      }
+      float w[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int x = e >> 2, i = e & 3, t = t0 + 16 * x + 4 * t4 + i;
+        w[e] = beta[x][i] * z[x][i];
+        if (on && t < len) {
+          z_out[(int64_t)t * a.dv] = z[x][i];
+          dv[(int64_t)t * a.dv] = rounded<T>(w[e]);
+        }
+        w[e] *= -early[x][i];
+        y[e] *= early[x][i] * a.scale;
+      }
+      uint4 wp[3], yp[3];
+      operand_of<3>(w, wp);
+      operand_of<3>(y, yp);
+#pragma unroll
+      for (int j = 0; j < 2 * ND; ++j) {
+        uint4 e[L::kPl];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) U[j][i] *= whole;
+        columns16<L>(tk, 0, j, e);
+        U[j] = dot_planes16(e, wp, U[j]);
+        columns16<L>(tq, 0, j, e);
+        U[j] = dot_planes16(e, yp, U[j]);
+      }
+      settle_mfma();
+    }
+  }
+  if (a.dS_in) put_state(a.dS_in + head * size);
+  if (on)
+    for (int t = len + t4; t < a.n; t += 4) dv[(int64_t)t * a.dv] = (T)0;
+}
+
+// ---- block by block: a wave has 16 of 64 tokens, and of their dq, asked and kept all columns
+template <typename T, int ND>
+struct BlockLds {
+  using W = PairTile<float, ND, kBlock>;  // errors, z, or gradients of the outputs
+  using L = PairTile<T, ND, kBlock>;      // queries or keys
+  using Half = PairTile<float, ND, 32>;   // 32 rows of a state (two of them in the place of W)
+  static_assert(2 * Half::kBytes <= W::kBytes, "the states' rows lie in the errors' place");
+  static constexpr int kBytes = W::kBytes + L::kBytes;
+};
+
+// A row's entries 32 s + 8 t4 .. +7 as operands
+template <typename T, int ND>
+__device__ __forceinline__ void load_own16(const T* p, bool ok, int width, uint4 (&f)[ND][sizeof(T) == 4 ? 3 : 1]) {
+  constexpr int kPl = sizeof(T) == 4 ? 3 : 1, kEV = 16 / sizeof(T);
+  const int t4 = (threadIdx.x & 63) >> 4;
+  const bool vec = width % kEV == 0 && ((uintptr_t)p & 15) == 0;
+#pragma unroll
+  for (int s = 0; s < ND; ++s) {
+    const int c0 = 32 * s + 8 * t4;
+    if constexpr (sizeof(T) == 4) {
+      float x[8];
+#pragma unroll
+      for (int h = 0; h < 8; h += 4) {
+        float4 w = {0.f, 0.f, 0.f, 0.f};
+        if (vec) {
+          if (ok && c0 + h < width) w = *(const float4*)(p + c0 + h);
+        } else if (ok) {
+          if (c0 + h < width) w.x = p[c0 + h];
+          if (c0 + h + 1 < width) w.y = p[c0 + h + 1];
+          if (c0 + h + 2 < width) w.z = p[c0 + h + 2];
+          if (c0 + h + 3 < width) w.w = p[c0 + h + 3];
+        }
+        x[h] = w.x, x[h + 1] = w.y, x[h + 2] = w.z, x[h + 3] = w.w;
+      }
+      operand_of<kPl>(x, f[s]);
+    } else {
+      uint4 w = {0u, 0u, 0u, 0u};
+      if (vec) {
+        if (ok && c0 < width) w = *(const uint4*)(p + c0);
+      } else if (ok) {
+        uint32_t u[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (c0 + j < width) u[j >> 1] |= (uint32_t)p[c0 + j] << (16 * (j & 1));
+        w = uint4{u[0], u[1], u[2], u[3]};
+      }
+      f[s][0] = w;
+    }
+  }
+}
+
+template <typename T, int ND, bool MANY>
+__global__ void __launch_bounds__(kBackThreads, sizeof(T) == 2 ? 2 : 1)
+delta_blocks_kernel(DeltaArgs a, const float* states, const float* behind, const float* errors, const float* zs) {
+  extern __shared__ __attribute__((aligned(16))) u16 smem16[];
+  using D = BlockLds<T, ND>;
+  using W = typename D::W;
+  using L = typename D::L;
+  using Half = typename D::Half;
+  constexpr int kPl = L::kPl;
+  __shared__ double sums[kBlock];
+  __shared__ float rates[kBlock], terms[kBlock], parts[2 * kBackWaves];
+  u16* const ta = smem16;               // errors, z, gradients of outputs; rows of states
+  u16* const tb = smem16 + W::kElems;   // queries or keys
+  const int tid = threadIdx.x, lane = tid & 63, l15 = lane & 15, t4 = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int blocks = (a.n + kBlock - 1) / kBlock, block = blockIdx.x, shared = blockIdx.y, t0 = block * kBlock;
+  const int len = tokens_of(a.lengths, shared / a.Hk, a.n), own = 16 * wave, last = min(a.n, t0 + kBlock);
+  const int64_t size = (int64_t)a.dk * a.dv, row0 = (int64_t)shared * a.n;
+  T* const dq_out = (T*)a.dq + row0 * a.dk;
+  T* const dk_out = (T*)a.dk_out + row0 * a.dk;
+  // rows behind the sequence
+  for (int i = tid; i < (last - max(t0, min(len, last))) * a.dk; i += kBackThreads) {
+    const int64_t at = (int64_t)max(t0, min(len, last)) * a.dk + i;
+    dq_out[at] = dk_out[at] = (T)0;
+  }
+  if (t0 + tid < last && tid < kBlock && t0 + tid >= len)
+    for (int v = 0; v < a.G; ++v) {
+      const int64_t at = ((int64_t)shared * a.G + v) * a.n + t0 + tid;
+      a.dg[at] = a.dbeta[at] = 0.f;
+    }
+  if (t0 >= len) return;
+  const T* const q = (const T*)a.q + row0 * a.dk;
+  const T* const k = (const T*)a.k + row0 * a.dk;
+  TileStage<float, ND, kBlock, kBackThreads> sa;
+  TileStage<T, ND, kBlock, kBackThreads> sb;
+  auto stage_keys = [&](const T* x) {
+    sb.init(x, len, a.dk, tid);
+    sb.fetch(t0);
+  };
+  f32x4 all_q[MANY ? 2 * ND : 1], all_k[MANY ? 2 * ND : 1];
+#pragma unroll
+  for (int j = 0; j < (MANY ? 2 * ND : 1); ++j) all_q[j] = all_k[j] = zero4();
+  for (int v = 0; v < a.G; ++v) {
+    const int64_t head = (int64_t)shared * a.G + v, row = head * a.n;
+    const float* const E = errors + row * a.dv;
+    const float* const Z = zs + row * a.dv;
+    const T* const dy = (const T*)a.dy + row * a.dv;
+    __syncthreads();  // (the last value head's readers are done)
+    if (wave == 0) {
+      const bool there = t0 + lane < len;
+      double sum = there ? delta_rate(a.g[row + t0 + lane]) : 0.0;
+#pragma unroll
+      for (int d = 1; d < 64; d *= 2) {
+        const uint64_t u = __builtin_bit_cast(uint64_t, sum);
+        const uint32_t lo = __shfl_up((uint32_t)u, d), hi = __shfl_up((uint32_t)(u >> 32), d);
+        if (lane >= d) sum += __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+      }
+      sums[lane] = sum;
+      rates[lane] = there ? a.beta[row + t0 + lane] : 0.f;
+    }
+    sa.init(E, len, a.dv, tid);
+    sa.fetch(t0);
+    stage_keys(k);
+    sa.put(ta, t0);
+    sb.put(tb, t0);
+    __syncthreads();
+    f32x4 dq[2 * ND], asked[2 * ND], kept[2 * ND];
+#pragma unroll
+    for (int j = 0; j < 2 * ND; ++j) dq[j] = asked[j] = kept[j] = zero4();
+    const int mine = own + l15;  // a token of this wave's, in the block
+    const bool there = t0 + mine < len;
+    const double my_sum = sums[mine];
+    const float my_rate = rates[mine];
+    auto decay = [&](double d) { return exp2_fast((float)(d * 1.4426950408889634)); };
+
+    // ---- pairs of this wave's tokens i with j <= i: rows of one and two
+    {
+      uint4 y[ND][kPl], z[ND][3];
+      load_own16<T, ND>(dy + (int64_t)(t0 + mine) * a.dv, there, a.dv, y);
+      load_own16<float, ND>(Z + (int64_t)(t0 + mine) * a.dv, there, a.dv, z);
+#pragma unroll 1
+      for (int jb = 0; 32 * jb <= own; ++jb) {
+        float one[8], two[8];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          f32x4 p = zero4(), r = zero4();
+#pragma unroll
+          for (int s = 0; s < ND; ++s) {
+            uint4 e[3];
+            rows16<W>(ta, 32 * jb + 16 * x, s, e);
+            p = dot_planes16(e, y[s], p);
+            r = dot_planes16(e, z[s], r);
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int j = 32 * jb + 16 * x + 4 * t4 + i;
+            const float d = decay(my_sum - sums[j]) * rates[j];
+            one[4 * x + i] = j <= mine ? p[i] * d * a.scale : 0.f;
+            two[4 * x + i] = j < mine ? -(r[i] * d * my_rate) : 0.f;
+          }
+        }
+        uint4 op[3], tp[3];
+        operand_of<3>(one, op);
+        operand_of<3>(two, tp);
+#pragma unroll
+        for (int j = 0; j < 2 * ND; ++j) {
+          uint4 e[kPl];
+          columns16<L>(tb, 32 * jb, j, e);
+          dq[j] = dot_planes16(op, e, dq[j]);
+          asked[j] = dot_planes16(tp, e, asked[j]);
+        }
+        settle_mfma();
+      }
+    }
+    // ---- pairs of tokens i with this wave's j <= i: columns of one, then of two
+    uint4 e_own[ND][3];
+    load_own16<float, ND>(E + (int64_t)(t0 + mine) * a.dv, there, a.dv, e_own);
+    {
+      TileStage<T, ND, kBlock, kBackThreads> sy;
+      sy.init(dy, len, a.dv, tid);
+      sy.fetch(t0);
+      stage_keys(q);
+      __syncthreads();
+      sy.put(ta, t0);
+      sb.put(tb, t0);
+      __syncthreads();
+#pragma unroll 1
+      for (int ib = own / 32; ib < 2; ++ib) {
+        float one[8];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          f32x4 p = zero4();
+#pragma unroll
+          for (int s = 0; s < ND; ++s) {
+            uint4 e[kPl];
+            rows16<L>(ta, 32 * ib + 16 * x, s, e);
+            p = dot_planes16(e, e_own[s], p);
+          }
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int i = 32 * ib + 16 * x + 4 * t4 + r;
+            one[4 * x + r] = i >= mine ? p[r] * decay(sums[i] - my_sum) * (my_rate * a.scale) : 0.f;
+          }
+        }
+        uint4 op[3];
+        operand_of<3>(one, op);
+#pragma unroll
+        for (int j = 0; j < 2 * ND; ++j) {
+          uint4 e[kPl];
+          columns16<L>(tb, 32 * ib, j, e);
+          kept[j] = dot_planes16(op, e, kept[j]);
+        }
+        settle_mfma();
+      }
+      sa.init(Z, len, a.dv, tid);
+      sa.fetch(t0);
+      stage_keys(k);
+      __syncthreads();
+      sa.put(ta, t0);
+      sb.put(tb, t0);
+      __syncthreads();
+#pragma unroll 1
+      for (int ib = own / 32; ib < 2; ++ib) {
+        float two[8];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          f32x4 p = zero4();
+#pragma unroll
+          for (int s = 0; s < ND; ++s) {
+            uint4 e[3];
+            rows16<W>(ta, 32 * ib + 16 * x, s, e);
+            p = dot_planes16(e, e_own[s], p);
+          }
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int i = 32 * ib + 16 * x + 4 * t4 + r;
+            two[4 * x + r] = i > mine ? -(p[r] * decay(sums[i] - my_sum) * (my_rate * rates[i])) : 0.f;
+          }
+        }
+        uint4 op[3];
+        operand_of<3>(two, op);
+#pragma unroll
+        for (int j = 0; j < 2 * ND; ++j) {
+          uint4 e[kPl];
+          columns16<L>(tb, 32 * ib, j, e);
+          kept[j] = dot_planes16(op, e, kept[j]);
+        }
+        settle_mfma();
+      }
+    }
+    // ---- the states, 32 rows at a time
+    float inner = 0.f, late_terms = 0.f;
+    {
+      uint4 y[ND][kPl], z[ND][3];
+      load_own16<T, ND>(dy + (int64_t)(t0 + mine) * a.dv, there, a.dv, y);
+      load_own16<float, ND>(Z + (int64_t)(t0 + mine) * a.dv, there, a.dv, z);
+      const double end = sums[kBlock - 1];
+      float early[4], late[4], rate[4];  // of tokens own + 4 t4 .. +3
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int i = own + 4 * t4 + r;
+        early[r] = decay(sums[i]), late[r] = decay(end - sums[i]), rate[r] = rates[i];
+      }
+      const float* const S = states + (head * blocks + block) * size;
+      const float* const U = behind + (head * blocks + block) * size;
+      TileStage<float, ND, 32, kBackThreads> ss, su;
+      ss.init(S, a.dk, a.dv, tid);
+      su.init(U, a.dk, a.dv, tid);
+      u16* const tu = ta + Half::kElems;
+#pragma unroll 1
+      for (int b = 0; 32 * b < a.dk; ++b) {
+        ss.fetch(32 * b);
+        su.fetch(32 * b);
+        __syncthreads();
+        ss.put(ta, 32 * b);
+        su.put(tu, 32 * b);
+        for (int i = tid; i < 32 * a.dv; i += kBackThreads) {
+          const int64_t at = (int64_t)32 * b * a.dv + i;
+          if (at < size) inner = fmaf(S[at], U[at], inner);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          f32x4 of_y = zero4(), of_z = zero4(), of_e = zero4();
+#pragma unroll
+          for (int s = 0; s < ND; ++s) {
+            uint4 e[3];
+            rows16<Half>(ta, 16 * x, s, e);
+            of_y = dot_planes16(y[s], e, of_y);
+            of_z = dot_planes16(z[s], e, of_z);
+            rows16<Half>(tu, 16 * x, s, e);
+            of_e = dot_planes16(e_own[s], e, of_e);
+          }
+          const int col = 32 * b + 16 * x + l15;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int i = own + 4 * t4 + r;
+            const float ue = of_e[r] * (late[r] * rate[r]), ye = of_y[r] * (early[r] * a.scale), ze = of_z[r] * (early[r] * rate[r]);
+            if (col < a.dk && t0 + i < len) late_terms = fmaf(entry_of(k, (int64_t)(t0 + i) * a.dk + col), ue, late_terms);
+#pragma unroll
+            for (int j = 0; j < 2 * ND; ++j)
+              if (j == 2 * b + x) kept[j][r] += ue, dq[j][r] += ye, asked[j][r] -= ze;
+          }
+        }
+      }
+      settle_mfma();
+      inner *= decay(end);
+    }
+    // ---- the gradients of g and beta
+    float at[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < 2 * ND; ++j) {
+      const int col = 16 * j + l15;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int t = t0 + own + 4 * t4 + r;
+        if (col < a.dk && t < len) {
+          const int64_t i = (int64_t)t * a.dk + col;
+          at[r] = fmaf(entry_of(q, i), dq[j][r], fmaf(entry_of(k, i), asked[j][r] - kept[j][r], at[r]));
+        }
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+#pragma unroll
+      for (int d = 1; d < 16; d *= 2) at[r] += __shfl_xor(at[r], d);
+      if (l15 == r) terms[own + 4 * t4 + r] = at[r];
+    }
+    inner += late_terms;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) inner += __shfl_xor(inner, d);
+    if (lane == 0) parts[wave] = inner;
+    {
+      float dot = 0.f;
+      if (there)
+        for (int i = t4; i < a.dv; i += 4) {
+          const int64_t x = (int64_t)(t0 + mine) * a.dv + i;
+          dot = fmaf(Z[x], E[x], dot);
+        }
+      dot += __shfl_xor(dot, 16);
+      dot += __shfl_xor(dot, 32);
+      if (t4 == 0 && there) a.dbeta[row + t0 + mine] = dot;
+    }
+    __syncthreads();
+    if (wave == 0) {
+      double sum = terms[lane];
+#pragma unroll
+      for (int d = 1; d < 64; d *= 2) {
+        const uint64_t u = __builtin_bit_cast(uint64_t, sum);
+        const uint32_t lo = __shfl_down((uint32_t)u, d), hi = __shfl_down((uint32_t)(u >> 32), d);
+        if (lane + d < 64) sum += __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+      }
+      double rest = 0.0;
+#pragma unroll
+      for (int w = 0; w < kBackWaves; ++w) rest += parts[w];
+      if (t0 + lane < len) a.dg[row + t0 + lane] = (float)(sum + rest);
+    }
+    // ---- dq and dk, over the group's value heads
+#pragma unroll
+    for (int j = 0; j < 2 * ND; ++j) {
+      f32x4 gq = dq[j], gk;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) gk[r] = asked[j][r] + kept[j][r];
+      if constexpr (MANY) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) all_q[j][r] += gq[r], all_k[j][r] += gk[r];
+        gq = all_q[j], gk = all_k[j];
+      }
+      if (!MANY || v + 1 == a.G) {
+        const int col = 16 * j + l15;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int t = t0 + own + 4 * t4 + r;
+          if (col < a.dk && t < len) {
+            dq_out[(int64_t)t * a.dk + col] = rounded<T>(gq[r]);
+            dk_out[(int64_t)t * a.dk + col] = rounded<T>(gk[r]);
+          }
+        }
+      }
+    }
+  }
+}
+
+// Where a call's scratch goes.
+struct Places {
+  size_t data, back, states, behind, errors, zs, bytes;
+};
+Places places_of(bool bf16, int heads, int n, int dk, int dv) {
+  const size_t chunks = (size_t)heads * ((n + C - 1) / C), blocks = (size_t)heads * ((n + kBlock - 1) / kBlock);
+  auto whole = [](size_t x) { return (x + 255) / 256 * 256; };
+  Places p;
+  p.data = 0;
+  p.back = whole(delta_data_bytes(bf16, heads, n));
+  p.states = p.back + whole(chunks * (bf16 ? sizeof(DeltaChunkBack<true>) : sizeof(DeltaChunkBack<false>)));
+  p.behind = p.states + whole(blocks * dk * dv * sizeof(float));
+  p.errors = p.behind + whole(blocks * dk * dv * sizeof(float));
+  p.zs = p.errors + whole((size_t)heads * n * dv * sizeof(float));
+  p.bytes = p.zs + whole((size_t)heads * n * dv * sizeof(float));
+  return p;
+}
+
+template <typename F>
+hipError_t raise_lds(F kern, int bytes) {
+  return bytes > 60 * 1024 ? hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) : hipSuccess;
+}
+
+template <typename T, int ND>
+hipError_t launch_back(const DeltaArgs& a, const void* data, float* behind, float* zs, hipStream_t s) {
+  constexpr int bytes = BackLds<T, ND>::kBytes;
+  auto kern = delta_back_kernel<T, ND>;
+  hipError_t e = raise_lds(kern, bytes);
+  if (e != hipSuccess) return e;
+  const int slices = (a.dv + 16 * kBackWaves - 1) / (16 * kBackWaves);
+  hipLaunchKernelGGL(kern, dim3(delta_grid(a.heads, slices)), dim3(kBackThreads), bytes, s, a, data, behind, zs, slices);
+  return hipGetLastError();
+}
+
+template <typename T, int ND, bool MANY>
+hipError_t launch_blocks_of(const DeltaArgs& a, const float* states, const float* behind, const float* errors, const float* zs,
+                            hipStream_t s) {
+  constexpr int bytes = BlockLds<T, ND>::kBytes;
+  static_assert(bytes <= 158 * 1024, "LDS of one workgroup");
+  auto kern = delta_blocks_kernel<T, ND, MANY>;
+  hipError_t e = raise_lds(kern, bytes);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(kern, dim3((a.n + kBlock - 1) / kBlock, a.heads / a.G), dim3(kBackThreads), bytes, s, a, states, behind, errors, zs);
+  return hipGetLastError();
+}
+template <typename T, int ND>
+hipError_t launch_blocks(const DeltaArgs& a, const float* states, const float* behind, const float* errors, const float* zs,
+                         hipStream_t s) {
+  return a.G > 1 ? launch_blocks_of<T, ND, true>(a, states, behind, errors, zs, s)
+                 : launch_blocks_of<T, ND, false>(a, states, behind, errors, zs, s);
+}
+
+template <typename T>
+hipError_t launch(const DeltaArgs& a, char* scratch, hipStream_t s) {
+  const Places p = places_of(sizeof(T) == 2, a.heads, a.n, a.dk, a.dv);
+  float *states = (float*)(scratch + p.states), *behind = (float*)(scratch + p.behind);
+  float *errors = (float*)(scratch + p.errors), *zs = (float*)(scratch + p.zs);
+  hipError_t e = launch_delta_pairs(a, sizeof(T) == 2, scratch + p.data, scratch + p.back, s);
+  if (e == hipSuccess) e = launch_delta_states(a, sizeof(T) == 2, scratch + p.data, states, errors, s);
+  if (e != hipSuccess) return e;
+  switch ((a.dk + 31) / 32) {
+    case 1: e = launch_back<T, 1>(a, scratch + p.back, behind, zs, s); break;
+    case 2: e = launch_back<T, 2>(a, scratch + p.back, behind, zs, s); break;
+    case 3: e = launch_back<T, 3>(a, scratch + p.back, behind, zs, s); break;
+    default: e = launch_back<T, 4>(a, scratch + p.back, behind, zs, s); break;
+  }
+  if (e != hipSuccess) return e;
+  switch ((std::max(a.dk, a.dv) + 31) / 32) {
+    case 1: return launch_blocks<T, 1>(a, states, behind, errors, zs, s);
+    case 2: return launch_blocks<T, 2>(a, states, behind, errors, zs, s);
+    case 3: return launch_blocks<T, 3>(a, states, behind, errors, zs, s);
+    default: return launch_blocks<T, 4>(a, states, behind, errors, zs, s);
+  }
+}
+
+// No tokens: the states' gradients as they are.
+__global__ void __launch_bounds__(256) delta_no_tokens_kernel(const float* dS, float* dS_in, int64_t count) {
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < count; i += (int64_t)gridDim.x * 256) dS_in[i] = dS ? dS[i] : 0.f;
+}
+
+}  // namespace
+
+size_t delta_backward_scratch(bool bf16, int heads, int, int n, int dk, int dv) {
+  return n == 0 ? 0 : places_of(bf16, heads, n, dk, dv).bytes;
+}
+
+hipError_t launch_delta_backward(const DeltaArgs& a, bool bf16, void* scratch, hipStream_t s) {
+  if (a.n == 0) {
+    const int64_t count = (int64_t)a.heads * a.dk * a.dv;
+    hipLaunchKernelGGL(delta_no_tokens_kernel, dim3((unsigned)std::min<int64_t>((count + 255) / 256, 65536)), dim3(256), 0, s, a.dS,
+                       a.dS_in, count);
+    return hipGetLastError();
+  }
+  return bf16 ? launch<u16>(a, (char*)scratch, s) : launch<float>(a, (char*)scratch, s);
+}
+
 }  // namespace sata

@@ -105,6 +105,35 @@ struct DeltaChunkBack {
   float whole[4];
 };
 
+// `sizeof(D)` bytes on their way into LDS.
+template <typename D, int THREADS>
+struct DataStage {
+  static_assert(sizeof(D) % 16 == 0, "whole vectors");
+  static constexpr int kVectors = sizeof(D) / 16, kIt = (kVectors + THREADS - 1) / THREADS;
+  uint4 r[kIt];
+  __device__ __forceinline__ void fetch(const D* d, int tid) {
+#pragma unroll
+    for (int i = 0; i < kIt; ++i)
+      if (tid + i * THREADS < kVectors) r[i] = ((const uint4*)d)[tid + i * THREADS];
+  }
+  __device__ __forceinline__ void put(D* d, int tid) const {
+#pragma unroll
+    for (int i = 0; i < kIt; ++i)
+      if (tid + i * THREADS < kVectors) ((uint4*)d)[tid + i * THREADS] = r[i];
+  }
+};
+
+// Entries of rows 16 x + 4 t4 .. +3 (x = 0, 1) of this lane's column, zero behind `rows`.
+template <typename T>
+__device__ __forceinline__ void fetch_column(const T* p, int rows, int pitch, bool on, T (&v)[8]) {
+  const int t4 = (threadIdx.x & 63) >> 4;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const int r = 16 * (e >> 2) + 4 * t4 + (e & 3);
+    v[e] = on && r < rows ? p[(int64_t)r * pitch] : (T)0;
+  }
+}
+
 // Workgroups to heads and slices of columns: an XCD takes whole heads, whose queries and keys are then read through one L2.
 __device__ __forceinline__ bool delta_place(int heads, int slices, int& head, int& slice) {
   if (heads >= 8) {

@@ -258,3 +258,177 @@ def test_refusals(sata):
     wide = torch.zeros(1, 1, 2, 129, device="cuda")
     with pytest.raises(sata.SataError):
         sata.delta_prefill(wide, wide, wide, torch.zeros(1, 1, 2, device="cuda"), torch.zeros(1, 1, 2, device="cuda"))
+
+
+# ------------------------------------------------------------------ gradients
+
+GRADIENTS = [  # B, Hk, G, n, dk, dv, dtype, lengths, state
+    (1, 1, 1, 1, 16, 16, "f32", None, False),
+    (1, 1, 1, 33, 32, 32, "f32", None, True),
+    (2, 2, 1, 64, 64, 64, "bf16", None, True),
+    (2, 1, 3, 97, 40, 24, "f32", [97, 30], True),
+    (1, 2, 2, 65, 128, 128, "bf16", None, True),
+    (1, 1, 2, 130, 128, 128, "f32", None, False),
+    (3, 1, 1, 50, 1, 3, "f32", [0, 1, 50], True),
+    (2, 1, 1, 129, 33, 65, "bf16", [128, 64], False),
+    (1, 3, 1, 31, 96, 100, "bf16", None, True),
+    (2, 1, 2, 200, 17, 128, "f32", [200, 160], False),
+    (1, 1, 1, 150, 128, 7, "bf16", None, True),
+    (1, 1, 4, 70, 64, 96, "f32", [69], True),
+]
+
+
+def gradient_reference(q, k, v, g, beta, dy, L, S0, dS):
+    """The gradients in float64, and for every token the sizes of the sums that they are."""
+    x = ref.to64(q, k, v, g, beta) + ([S0.double()] if S0 is not None else [])
+    leaves = [a.clone().requires_grad_() for a in x]
+    y, S, states = ref.delta(*leaves[:5], L, leaves[5] if S0 is not None else None)
+    loss = (y * dy.double()).sum() + ((S * dS.double()).sum() if dS is not None else 0.0)
+    out = torch.autograd.grad(loss, leaves + states, allow_unused=True)
+    grads = [torch.zeros_like(l) if o is None else o for l, o in zip(leaves, out)]
+    n, dk = q.shape[2], q.shape[3]
+    zero = torch.zeros_like(states[0])
+    norm = lambda a: a.detach().flatten(2).norm(dim=-1)  # noqa: E731
+    U = torch.stack([norm(zero if o is None else o) for o in out[len(leaves):]], -1)   # [B, H, n]
+    before = torch.stack([norm(s) for s in states], -1)
+    first = norm(leaves[5]) if S0 is not None else torch.zeros_like(before[..., 0])
+    before = torch.maximum(before, torch.cat((first[..., None], before[..., :-1]), -1))
+    values, rate = x[2].norm(dim=-1), x[4]
+    size = {"dq": before * dy.double().norm(dim=-1) / math.sqrt(dk), "dv": U * rate, "dbeta": U * (values + before),
+            "dk": 2 * U * rate * (values + before), "dg": U * before}
+    return grads, size
+
+
+def check_gradients(got, want, size, n, dk, dv, dtype, G):
+    """Each row's error against its rounding and, as states and gradients of states carry their own error
+    (state_tol) into every sum, twice that of the sum's size; a chunk's inverse and the sums over a block's tokens
+    double it again."""
+    eps = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -24
+    off = 4 * state_tol(n, max(dk, dv))
+    for i, name in enumerate(("dq", "dk", "dv", "dg", "dbeta")):
+        w, s = want[i], size[name]
+        a = got[i].double().cpu()
+        assert a.shape == w.shape
+        if name in ("dq", "dk"):
+            s = s.reshape(s.shape[0], -1, G, s.shape[-1]).sum(2)
+        err, mag = ((a - w).norm(dim=-1), w.norm(dim=-1)) if w.dim() == 4 else ((a - w).abs(), w.abs())
+        tol = (eps if w.dim() == 4 else 2.0 ** -24) * mag + off * s.amax(-1, keepdim=True) * (1 if name == "dg" else 0) + off * s
+        assert (err <= tol + 1e-300).all(), (name, (err / (tol + 1e-300)).max())
+    if len(want) > 5:
+        S = want[5]
+        err = (got[5].double().cpu() - S).flatten(2).norm(dim=-1)
+        assert (err <= off * S.flatten(2).norm(dim=-1) + off * size["dv"].amax(-1) + 1e-300).all()
+
+
+@pytest.mark.parametrize("case", GRADIENTS, ids=str)
+def test_gradients(sata, case):
+    B, Hk, G, n, dk, dv, dtype, lengths, state = case
+    print("gradients", case, file=sys.stderr, flush=True)
+    q, k, v, g, beta, S0 = ref.draw(n + dk + 1, B, Hk, G, n, dk, dv, dtype, state=state)
+    gen = torch.Generator().manual_seed(n)
+    dy = torch.randn(B, Hk * G, n, dv, generator=gen).to(q.dtype)
+    dS = torch.randn(B, Hk * G, dk, dv, generator=gen) if state else None
+    L = torch.tensor(lengths, dtype=torch.int32) if lengths else None
+    if lengths:
+        for b, e in enumerate(lengths):
+            dy[b, :, e:] = 0.0
+    want, size = gradient_reference(q, k, v, g, beta, dy, L, S0, dS)
+    if lengths:  # (padding is not used, whatever it holds)
+        for b, e in enumerate(lengths):
+            for x in (q, k, v, g, beta, dy):
+                x[b, :, e:] = math.nan
+    got = sata.delta_backward(*_cuda(q, k, v, g, beta, dy), lengths=_cuda(L)[0], S_in=_cuda(S0)[0], dS=_cuda(dS)[0])
+    assert (got[5] is None) == (not state)
+    check_gradients(got, want, size, n, dk, dv, dtype, G)
+    if lengths:
+        for b, e in enumerate(lengths):
+            assert all((x[b, :, e:] == 0).all() for x in got[:5])
+
+
+def test_gradients_of_a_state_alone(sata):
+    """dS without an earlier state, and an earlier state without dS."""
+    q, k, v, g, beta, S0 = ref.draw(91, 1, 2, 1, 40, 24, 16, "f32", state=True)
+    gen = torch.Generator().manual_seed(92)
+    dy, dS = torch.randn(1, 2, 40, 16, generator=gen), torch.randn(1, 2, 24, 16, generator=gen)
+    for s, d in ((S0, None), (None, dS)):
+        want, size = gradient_reference(q, k, v, g, beta, dy, None, s, d)
+        got = sata.delta_backward(*_cuda(q, k, v, g, beta, dy), S_in=_cuda(s)[0], dS=_cuda(d)[0])
+        check_gradients(got, want, size, 40, 24, 16, "f32", 1)
+
+
+def test_gradients_at_rates_of_zero_and_strong_decays(sata):
+    """beta 0 has a gradient of its own; a decay of minus infinity cuts the sequence in two."""
+    n, d = 100, 32
+    q, k, v, g, beta, S0 = ref.draw(93, 1, 1, 1, n, d, d, "f32", state=True)
+    beta[..., ::3], beta[..., 1::7] = 0.0, 1.0
+    g[..., 10], g[..., 40], g[..., 70] = -300.0, -150.0, -1e30
+    g[..., 45:50] = -30.0
+    gen = torch.Generator().manual_seed(94)
+    dy, dS = torch.randn(1, 1, n, d, generator=gen), torch.randn(1, 1, d, d, generator=gen)
+    want, size = gradient_reference(q, k, v, g.clamp(min=-1000.0), beta, dy, None, S0, dS)
+    g[..., 70] = -math.inf
+    got = sata.delta_backward(*_cuda(q, k, v, g, beta, dy), S_in=S0.cuda(), dS=dS.cuda())
+    check_gradients(got, want, size, n, d, d, "f32", 1)
+
+
+def test_gradients_by_differences(sata):
+    """The forward call's own slope along random directions, in float32: differences over a step of 2^-6 lose
+    14 bits to it and as many to the third derivative's share; 2^-9 of the gradients' sizes are left."""
+    x = list(ref.draw(95, 1, 1, 2, 45, 16, 12, "f32", state=True))
+    gen = torch.Generator().manual_seed(96)
+    w, wS = torch.randn(1, 2, 45, 12, generator=gen), torch.randn(1, 2, 16, 12, generator=gen)
+    grads = sata.delta_backward(*_cuda(*x[:5], w), S_in=x[5].cuda(), dS=wS.cuda())
+
+    def loss(*a):
+        y, S = sata.delta_prefill(*_cuda(*a[:5]), S_in=a[5].cuda())
+        return (y.cpu().double() * w).sum() + (S.cpu().double() * wS).sum()
+
+    h = 2.0 ** -6
+    for i, grad in enumerate(grads):
+        e = torch.randn(x[i].shape, generator=gen)
+        e = e / e.norm()
+        at = lambda s: loss(*(a + s * e if j == i else a for j, a in enumerate(x)))  # noqa: E731
+        slope = (at(h) - at(-h)) / (2 * h)
+        # (the losses are sums of some 700 terms, of float32's error each)
+        assert abs(slope - (grad.cpu().double() * e).sum()) <= 2.0 ** -9 * grad.double().norm().item() + 2.0 ** -24 * 700 / h, i
+
+
+def test_gradients_of_bad_values_stay_in_their_sequence_and_head(sata):
+    q, k, v, g, beta, _ = ref.draw(97, 2, 2, 2, 70, 32, 32, "bf16")
+    dy = torch.randn(2, 4, 70, 32, generator=torch.Generator().manual_seed(98)).bfloat16()
+    clean = sata.delta_backward(*_cuda(q, k, v, g, beta, dy))
+    k[1, 0, 30, 3], v[0, 3, 11, 2], dy[0, 2, 69, 0] = math.nan, math.inf, math.nan
+    got = sata.delta_backward(*_cuda(q, k, v, g, beta, dy))
+    for i, (a, b) in enumerate(zip(got[:5], clean[:5])):
+        # heads that hold none: of queries and keys (0, 0) and (1, 1), of values their two each
+        for bb, h in (((0, 0), (1, 1)) if i < 2 else ((0, 0), (0, 1), (1, 2), (1, 3))):
+            assert torch.equal(a[bb, h], b[bb, h])
+
+
+def test_gradients_twice_and_captured(sata):
+    q, k, v, g, beta, S0 = _cuda(*ref.draw(99, 2, 2, 2, 100, 64, 64, "bf16", state=True))
+    dy, dS = torch.randn_like(v), torch.randn_like(S0)
+    first = sata.delta_backward(q, k, v, g, beta, dy, S_in=S0, dS=dS)
+    second = sata.delta_backward(q, k, v, g, beta, dy, S_in=S0, dS=dS)
+    assert all(torch.equal(a, b) for a, b in zip(first, second))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = sata.delta_backward(q, k, v, g, beta, dy, S_in=S0, dS=dS)
+    for _ in range(4):
+        dy.mul_(0.5)
+        graph.replay()
+        want = sata.delta_backward(q, k, v, g, beta, dy, S_in=S0, dS=dS)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(held, want))
+
+
+def test_gradients_of_empty_prompts(sata):
+    q, k, v, g, beta, S0 = _cuda(*ref.draw(100, 2, 1, 2, 4, 16, 8, "f32", state=True))
+    e = [x[:, :, :0].contiguous() for x in (q, k, v, g, beta)]
+    dS = torch.randn_like(S0)
+    out = sata.delta_backward(*e, torch.zeros_like(e[2]), S_in=S0, dS=dS)
+    assert torch.equal(out[5], dS) and out[0].shape == (2, 1, 0, 16)
+    L = torch.zeros(2, dtype=torch.int32, device="cuda")
+    out = sata.delta_backward(q, k, v, g, beta, torch.ones_like(v), lengths=L, S_in=S0, dS=dS)
+    assert torch.equal(out[5], dS) and all((x == 0).all() for x in out[:5])
+    assert (sata.delta_backward(q, k, v, g, beta, torch.ones_like(v), lengths=L, S_in=S0)[5] == 0).all()
