@@ -191,7 +191,6 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2) delta_scan_kernel(DeltaArg
         if (on && row < a.dk) to[(int64_t)row * a.dv + col] = S[j][i];
       }
   };
-  const T* const v = (const T*)a.v + (int64_t)head * a.n * a.dv + col;
   T* const y = GRAD ? nullptr : (T*)a.y + (int64_t)head * a.n * a.dv;
   const bool vec = a.dv % 4 == 0 && ((uintptr_t)y & (4 * sizeof(T) - 1)) == 0;
   if (chunks > 0) {
@@ -200,11 +199,15 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2) delta_scan_kernel(DeltaArg
     sq.init((const T*)a.q + shared * a.n * a.dk, len, a.dk, tid);
     sk.init((const T*)a.k + shared * a.n * a.dk, len, a.dk, tid);
     DataStage<Data, kThreads> sd;
-    T next[8];
+    ColumnStage<T> sv;
+    ColumnStage<float> se;
+    sd.init(data, chunks, tid);
+    sv.init((const T*)a.v + (int64_t)head * a.n * a.dv, len, a.dv, col);
+    if (GRAD) se.init(errors + (int64_t)head * a.n * a.dv, len, a.dv, col);
     sk.fetch(0);
     if (!GRAD) sq.fetch(0);
-    sd.fetch(data, tid);
-    fetch_column(v, len, a.dv, on, next);
+    sd.fetch(0);
+    sv.fetch(0);
     for (int c = 0; c < chunks; ++c) {
       const int t0 = c * C;
       u16* const tk = smem16 + (D::kBuffers == 2 && (c & 1) ? D::kBuffer / 2 : 0);
@@ -213,16 +216,16 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2) delta_scan_kernel(DeltaArg
       if (D::kBuffers == 1) __syncthreads();
       sk.put(tk, t0);
       if (!GRAD) sq.put(tq, t0);
-      sd.put(&d, tid);
+      sd.put(&d);
       __syncthreads();
       float r[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) r[e] = entry_of(&next[e], 0);
+      for (int e = 0; e < 8; ++e) r[e] = sv.value(e);
       if (c + 1 < chunks) {
         sk.fetch(t0 + C);
         if (!GRAD) sq.fetch(t0 + C);
-        sd.fetch(data + c + 1, tid);
-        fetch_column(v + (int64_t)(t0 + C) * a.dv, len - t0 - C, a.dv, on, next);
+        sd.fetch(c + 1);
+        sv.fetch(t0 + C);
       }
       if (GRAD && c % (kDeltaBlock / C) == 0)
         put_state(states + ((int64_t)head * ((a.n + kDeltaBlock - 1) / kDeltaBlock) + c / (kDeltaBlock / C)) * size);
@@ -271,10 +274,7 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2) delta_scan_kernel(DeltaArg
       }
       if (GRAD) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int t = t0 + 16 * (e >> 2) + 4 * t4 + (e & 3);
-          if (on && t < len) errors[((int64_t)head * a.n + t) * a.dv + col] = E[e >> 2][e & 3];
-        }
+        for (int e = 0; e < 8; ++e) se.store(t0, e, E[e >> 2][e & 3]);
       } else {
         uint4 ep[PE];
         operand_of<PE>(E[0], E[1], ep);

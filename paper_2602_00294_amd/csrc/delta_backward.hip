@@ -69,18 +69,22 @@ __global__ void __launch_bounds__(kBackThreads, 2) delta_back_kernel(DeltaArgs a
   T* const dv = (T*)a.dv_out + (int64_t)head * a.n * a.dv + col;
   if (chunks > 0) {
     const Data* const data = (const Data*)data_ + (int64_t)head * ((a.n + C - 1) / C);
-    const T* const dy = (const T*)a.dy + (int64_t)head * a.n * a.dv + col;
-    float* const z_out = zs + (int64_t)head * a.n * a.dv + col;
     TileStage<T, ND, C, kBackThreads> sq, sk;
     sq.init((const T*)a.q + shared * a.n * a.dk, len, a.dk, tid);
     sk.init((const T*)a.k + shared * a.n * a.dk, len, a.dk, tid);
     DataStage<Data, kBackThreads> sd;
-    T next[8];
+    ColumnStage<T> sy, sv;
+    ColumnStage<float> sz;
+    const int64_t head0 = (int64_t)head * a.n * a.dv;
+    sd.init(data, chunks, tid);
+    sy.init((const T*)a.dy + head0, len, a.dv, col);
+    sv.init((const T*)a.dv_out + head0, len, a.dv, col);
+    sz.init(zs + head0, len, a.dv, col);
     auto fetch = [&](int c) {
       sk.fetch(c * C);
       sq.fetch(c * C);
-      sd.fetch(data + c, tid);
-      fetch_column(dy + (int64_t)c * C * a.dv, len - c * C, a.dv, on, next);
+      sd.fetch(c);
+      sy.fetch(c * C);
     };
     fetch(chunks - 1);
     for (int c = chunks - 1; c >= 0; --c) {
@@ -91,11 +95,11 @@ __global__ void __launch_bounds__(kBackThreads, 2) delta_back_kernel(DeltaArgs a
       if (D::kBuffers == 1) __syncthreads();
       sk.put(tk, t0);
       sq.put(tq, t0);
-      sd.put(&d, tid);
+      sd.put(&d);
       __syncthreads();
       float y[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = entry_of(&next[e], 0);
+      for (int e = 0; e < 8; ++e) y[e] = sy.value(e);
       if (c > 0) fetch(c - 1);
       if (c == chunks - 1 || c % (kBlock / C) == kBlock / C - 1)
         put_state(behind + ((int64_t)head * ((a.n + kBlock - 1) / kBlock) + c / (kBlock / C)) * size);
@@ -144,12 +148,10 @@ __global__ void __launch_bounds__(kBackThreads, 2) delta_back_kernel(DeltaArgs a
       float w[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const int x = e >> 2, i = e & 3, t = t0 + 16 * x + 4 * t4 + i;
+        const int x = e >> 2, i = e & 3;
         w[e] = beta[x][i] * z[x][i];
-        if (on && t < len) {
-          z_out[(int64_t)t * a.dv] = z[x][i];
-          dv[(int64_t)t * a.dv] = rounded<T>(w[e]);
-        }
+        sz.store(t0, e, z[x][i]);
+        sv.store(t0, e, w[e]);
         w[e] *= -early[x][i];
         y[e] *= early[x][i] * a.scale;
       }
@@ -174,20 +176,39 @@ __global__ void __launch_bounds__(kBackThreads, 2) delta_back_kernel(DeltaArgs a
     for (int t = len + t4; t < a.n; t += 4) dv[(int64_t)t * a.dv] = (T)0;
 }
 
-// ---- block by block: a wave has 16 of 64 tokens, and of their dq, asked and kept all columns
+// ---- block by block: a wave has 16 of 64 tokens and all columns of their dq and dk
+//
+// First dq and asked, which take what lies before a token (pairs with tokens j <= i, the state before the block); then, on top
+// of asked, kept, which takes what lies behind (pairs with i >= j, the gradient of the state behind the block).  A pair's
+// weight is formed in both places, once for each side's rows, so that it is an operand where it is formed.
 template <typename T, int ND>
 struct BlockLds {
-  using W = PairTile<float, ND, kBlock>;  // errors, z, or gradients of the outputs
+  using W = PairTile<float, ND, kBlock>;  // errors, z, or gradients of the outputs; rows of a state
   using L = PairTile<T, ND, kBlock>;      // queries or keys
-  using Half = PairTile<float, ND, 32>;   // 32 rows of a state (two of them in the place of W)
-  static_assert(2 * Half::kBytes <= W::kBytes, "the states' rows lie in the errors' place");
+  using Half = PairTile<float, ND, 32>;
   static constexpr int kBytes = W::kBytes + L::kBytes;
 };
 
+// Entries 32 s + 8 t4 .. +7 of a row in float32, zero behind `width`.
+__device__ __forceinline__ void load_eight(const float* p, int c0, bool ok, int width, bool vec, float (&x)[8]) {
+#pragma unroll
+  for (int h = 0; h < 8; h += 4) {
+    float4 w = {0.f, 0.f, 0.f, 0.f};
+    if (vec) {
+      if (ok && c0 + h < width) w = *(const float4*)(p + c0 + h);
+    } else if (ok) {
+      if (c0 + h < width) w.x = p[c0 + h];
+      if (c0 + h + 1 < width) w.y = p[c0 + h + 1];
+      if (c0 + h + 2 < width) w.z = p[c0 + h + 2];
+      if (c0 + h + 3 < width) w.w = p[c0 + h + 3];
+    }
+    x[h] = w.x, x[h + 1] = w.y, x[h + 2] = w.z, x[h + 3] = w.w;
+  }
+}
 // A row's entries 32 s + 8 t4 .. +7 as operands
 template <typename T, int ND>
 __device__ __forceinline__ void load_own16(const T* p, bool ok, int width, uint4 (&f)[ND][sizeof(T) == 4 ? 3 : 1]) {
-  constexpr int kPl = sizeof(T) == 4 ? 3 : 1, kEV = 16 / sizeof(T);
+  constexpr int kEV = 16 / sizeof(T);
   const int t4 = (threadIdx.x & 63) >> 4;
   const bool vec = width % kEV == 0 && ((uintptr_t)p & 15) == 0;
 #pragma unroll
@@ -195,20 +216,8 @@ __device__ __forceinline__ void load_own16(const T* p, bool ok, int width, uint4
     const int c0 = 32 * s + 8 * t4;
     if constexpr (sizeof(T) == 4) {
       float x[8];
-#pragma unroll
-      for (int h = 0; h < 8; h += 4) {
-        float4 w = {0.f, 0.f, 0.f, 0.f};
-        if (vec) {
-          if (ok && c0 + h < width) w = *(const float4*)(p + c0 + h);
-        } else if (ok) {
-          if (c0 + h < width) w.x = p[c0 + h];
-          if (c0 + h + 1 < width) w.y = p[c0 + h + 1];
-          if (c0 + h + 2 < width) w.z = p[c0 + h + 2];
-          if (c0 + h + 3 < width) w.w = p[c0 + h + 3];
-        }
-        x[h] = w.x, x[h + 1] = w.y, x[h + 2] = w.z, x[h + 3] = w.w;
-      }
-      operand_of<kPl>(x, f[s]);
+      load_eight(p, c0, ok, width, vec, x);
+      operand_of<3>(x, f[s]);
     } else {
       uint4 w = {0u, 0u, 0u, 0u};
       if (vec) {
@@ -225,6 +234,29 @@ __device__ __forceinline__ void load_own16(const T* p, bool ok, int width, uint4
   }
 }
 
+// Sums over the lanes up to (or from) a lane's own.
+__device__ __forceinline__ double sum_up_to(double x) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, x);
+    const uint32_t lo = __shfl_up((uint32_t)u, d), hi = __shfl_up((uint32_t)(u >> 32), d);
+    if (lane >= d) x += __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+  }
+  return x;
+}
+__device__ __forceinline__ double sum_from(double x) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, x);
+    const uint32_t lo = __shfl_down((uint32_t)u, d), hi = __shfl_down((uint32_t)(u >> 32), d);
+    if (lane + d < 64) x += __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+  }
+  return x;
+}
+
+// MANY: several value heads to a query and key head, whose dq and dk are summed.
 template <typename T, int ND, bool MANY>
 __global__ void __launch_bounds__(kBackThreads, sizeof(T) == 2 ? 2 : 1)
 delta_blocks_kernel(DeltaArgs a, const float* states, const float* behind, const float* errors, const float* zs) {
@@ -235,22 +267,21 @@ delta_blocks_kernel(DeltaArgs a, const float* states, const float* behind, const
   using Half = typename D::Half;
   constexpr int kPl = L::kPl;
   __shared__ double sums[kBlock];
-  __shared__ float rates[kBlock], terms[kBlock], parts[2 * kBackWaves];
-  u16* const ta = smem16;               // errors, z, gradients of outputs; rows of states
-  u16* const tb = smem16 + W::kElems;   // queries or keys
+  __shared__ float rates[kBlock], terms[kBlock], parts[kBackWaves];
+  u16* const ta = smem16;
+  u16* const tb = smem16 + W::kElems;
   const int tid = threadIdx.x, lane = tid & 63, l15 = lane & 15, t4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int blocks = (a.n + kBlock - 1) / kBlock, block = blockIdx.x, shared = blockIdx.y, t0 = block * kBlock;
   const int len = tokens_of(a.lengths, shared / a.Hk, a.n), own = 16 * wave, last = min(a.n, t0 + kBlock);
   const int64_t size = (int64_t)a.dk * a.dv, row0 = (int64_t)shared * a.n;
-  T* const dq_out = (T*)a.dq + row0 * a.dk;
-  T* const dk_out = (T*)a.dk_out + row0 * a.dk;
   // rows behind the sequence
-  for (int i = tid; i < (last - max(t0, min(len, last))) * a.dk; i += kBackThreads) {
-    const int64_t at = (int64_t)max(t0, min(len, last)) * a.dk + i;
-    dq_out[at] = dk_out[at] = (T)0;
+  const int rest = max(t0, min(len, last));
+  for (int i = tid; i < (last - rest) * a.dk; i += kBackThreads) {
+    const int64_t at = (row0 + rest) * a.dk + i;
+    ((T*)a.dq)[at] = ((T*)a.dk_out)[at] = (T)0;
   }
-  if (t0 + tid < last && tid < kBlock && t0 + tid >= len)
+  if (tid < kBlock && t0 + tid < last && t0 + tid >= len)
     for (int v = 0; v < a.G; ++v) {
       const int64_t at = ((int64_t)shared * a.G + v) * a.n + t0 + tid;
       a.dg[at] = a.dbeta[at] = 0.f;
@@ -258,9 +289,14 @@ delta_blocks_kernel(DeltaArgs a, const float* states, const float* behind, const
   if (t0 >= len) return;
   const T* const q = (const T*)a.q + row0 * a.dk;
   const T* const k = (const T*)a.k + row0 * a.dk;
-  TileStage<float, ND, kBlock, kBackThreads> sa;
+  // (a column of queries, keys and their gradients, as results have it)
+  ColumnStage<T> cq, ck, gq, gk;
+  cq.init(q, len, a.dk, l15);
+  ck.init(k, len, a.dk, l15);
+  gq.init((T*)a.dq + row0 * a.dk, len, a.dk, l15);
+  gk.init((T*)a.dk_out + row0 * a.dk, len, a.dk, l15);
   TileStage<T, ND, kBlock, kBackThreads> sb;
-  auto stage_keys = [&](const T* x) {
+  auto fetch_keys = [&](const T* x) {
     sb.init(x, len, a.dk, tid);
     sb.fetch(t0);
   };
@@ -272,39 +308,41 @@ delta_blocks_kernel(DeltaArgs a, const float* states, const float* behind, const
     const float* const E = errors + row * a.dv;
     const float* const Z = zs + row * a.dv;
     const T* const dy = (const T*)a.dy + row * a.dv;
+    const float* const S = states + (head * blocks + block) * size;
+    const float* const U = behind + (head * blocks + block) * size;
+    TileStage<float, ND, kBlock, kBackThreads> sa;
+    sa.init(E, len, a.dv, tid);
+    sa.fetch(t0);
+    fetch_keys(k);
     __syncthreads();  // (the last value head's readers are done)
     if (wave == 0) {
       const bool there = t0 + lane < len;
-      double sum = there ? delta_rate(a.g[row + t0 + lane]) : 0.0;
-#pragma unroll
-      for (int d = 1; d < 64; d *= 2) {
-        const uint64_t u = __builtin_bit_cast(uint64_t, sum);
-        const uint32_t lo = __shfl_up((uint32_t)u, d), hi = __shfl_up((uint32_t)(u >> 32), d);
-        if (lane >= d) sum += __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
-      }
-      sums[lane] = sum;
+      sums[lane] = sum_up_to(there ? delta_rate(a.g[row + t0 + lane]) : 0.0);
       rates[lane] = there ? a.beta[row + t0 + lane] : 0.f;
     }
-    sa.init(E, len, a.dv, tid);
-    sa.fetch(t0);
-    stage_keys(k);
     sa.put(ta, t0);
     sb.put(tb, t0);
     __syncthreads();
-    f32x4 dq[2 * ND], asked[2 * ND], kept[2 * ND];
-#pragma unroll
-    for (int j = 0; j < 2 * ND; ++j) dq[j] = asked[j] = kept[j] = zero4();
     const int mine = own + l15;  // a token of this wave's, in the block
     const bool there = t0 + mine < len;
     const double my_sum = sums[mine];
     const float my_rate = rates[mine];
     auto decay = [&](double d) { return exp2_fast((float)(d * 1.4426950408889634)); };
-
-    // ---- pairs of this wave's tokens i with j <= i: rows of one and two
+    float rate[4];  // of tokens own + 4 t4 .. +3
+#pragma unroll
+    for (int r = 0; r < 4; ++r) rate[r] = rates[own + 4 * t4 + r];
+    float at[4] = {0.f, 0.f, 0.f, 0.f};  // what counts for a token's sum of log decays
+    f32x4 sum_k[2 * ND];
+#pragma unroll
+    for (int j = 0; j < 2 * ND; ++j) sum_k[j] = zero4();
     {
+      f32x4 dq[2 * ND];
+#pragma unroll
+      for (int j = 0; j < 2 * ND; ++j) dq[j] = zero4();
       uint4 y[ND][kPl], z[ND][3];
       load_own16<T, ND>(dy + (int64_t)(t0 + mine) * a.dv, there, a.dv, y);
       load_own16<float, ND>(Z + (int64_t)(t0 + mine) * a.dv, there, a.dv, z);
+      // ---- pairs of this wave's tokens i with j <= i: rows of one and two
 #pragma unroll 1
       for (int jb = 0; 32 * jb <= own; ++jb) {
         float one[8], two[8];
@@ -334,158 +372,207 @@ delta_blocks_kernel(DeltaArgs a, const float* states, const float* behind, const
           uint4 e[kPl];
           columns16<L>(tb, 32 * jb, j, e);
           dq[j] = dot_planes16(op, e, dq[j]);
-          asked[j] = dot_planes16(tp, e, asked[j]);
+          sum_k[j] = dot_planes16(tp, e, sum_k[j]);
         }
         settle_mfma();
+      }
+      // ---- the state before the block, 32 rows at a time
+      float early[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) early[r] = decay(sums[own + 4 * t4 + r]);
+      TileStage<float, ND, 32, kBackThreads> ss;
+      ss.init(S, a.dk, a.dv, tid);
+      ss.fetch(0);
+#pragma unroll
+      for (int b = 0; b < ND; ++b)
+        if (32 * b < a.dk) {
+          __syncthreads();
+          ss.put(ta, 32 * b);
+          __syncthreads();
+          if (32 * b + 32 < a.dk) ss.fetch(32 * b + 32);
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            f32x4 of_y = zero4(), of_z = zero4();
+#pragma unroll
+            for (int s = 0; s < ND; ++s) {
+              uint4 e[3];
+              rows16<Half>(ta, 16 * x, s, e);
+              of_y = dot_planes16(y[s], e, of_y);
+              of_z = dot_planes16(z[s], e, of_z);
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              dq[2 * b + x][r] = fmaf(of_y[r], early[r] * a.scale, dq[2 * b + x][r]);
+              sum_k[2 * b + x][r] = fmaf(-of_z[r], early[r] * rate[r], sum_k[2 * b + x][r]);
+            }
+          }
+          settle_mfma();
+        }
+      // (asked counts twice here: with kept it is taken off once)
+#pragma unroll
+      for (int j = 0; j < 2 * ND; ++j) {
+        cq.template fetch<4>(t0 + own, 16 * j);
+        ck.template fetch<4>(t0 + own, 16 * j);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) at[r] = fmaf(cq.value(r), dq[j][r], fmaf(2.f * ck.value(r), sum_k[j][r], at[r]));
+        if constexpr (MANY) {
+#pragma unroll
+          for (int r = 0; r < 4; ++r) all_q[j][r] += dq[j][r];
+          dq[j] = all_q[j];
+        }
+        if (!MANY || v + 1 == a.G)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) gq.store(t0 + own, r, dq[j][r], 16 * j);
       }
     }
     // ---- pairs of tokens i with this wave's j <= i: columns of one, then of two
     uint4 e_own[ND][3];
-    load_own16<float, ND>(E + (int64_t)(t0 + mine) * a.dv, there, a.dv, e_own);
     {
       TileStage<T, ND, kBlock, kBackThreads> sy;
       sy.init(dy, len, a.dv, tid);
       sy.fetch(t0);
-      stage_keys(q);
+      fetch_keys(q);
+      const float* const pe = E + (int64_t)(t0 + mine) * a.dv;
+      const float* const pz = Z + (int64_t)(t0 + mine) * a.dv;
+      const bool vec = a.dv % 4 == 0 && (((uintptr_t)pe | (uintptr_t)pz) & 15) == 0;
+      float dot = 0.f;
+#pragma unroll
+      for (int s = 0; s < ND; ++s) {
+        float x[8], w[8];
+        load_eight(pe, 32 * s + 8 * t4, there, a.dv, vec, x);
+        load_eight(pz, 32 * s + 8 * t4, there, a.dv, vec, w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dot = fmaf(x[i], w[i], dot);
+        operand_of<3>(x, e_own[s]);
+      }
+      dot += __shfl_xor(dot, 16);
+      dot += __shfl_xor(dot, 32);
+      if (t4 == 0 && there) a.dbeta[row + t0 + mine] = dot;
       __syncthreads();
       sy.put(ta, t0);
       sb.put(tb, t0);
       __syncthreads();
+    }
 #pragma unroll 1
-      for (int ib = own / 32; ib < 2; ++ib) {
-        float one[8];
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          f32x4 p = zero4();
-#pragma unroll
-          for (int s = 0; s < ND; ++s) {
-            uint4 e[kPl];
-            rows16<L>(ta, 32 * ib + 16 * x, s, e);
-            p = dot_planes16(e, e_own[s], p);
-          }
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int i = 32 * ib + 16 * x + 4 * t4 + r;
-            one[4 * x + r] = i >= mine ? p[r] * decay(sums[i] - my_sum) * (my_rate * a.scale) : 0.f;
-          }
-        }
-        uint4 op[3];
-        operand_of<3>(one, op);
-#pragma unroll
-        for (int j = 0; j < 2 * ND; ++j) {
-          uint4 e[kPl];
-          columns16<L>(tb, 32 * ib, j, e);
-          kept[j] = dot_planes16(op, e, kept[j]);
-        }
-        settle_mfma();
+    for (int turn = 0; turn < 2; ++turn) {
+      if (turn == 1) {
+        sa.init(Z, len, a.dv, tid);
+        sa.fetch(t0);
+        fetch_keys(k);
+        __syncthreads();
+        sa.put(ta, t0);
+        sb.put(tb, t0);
+        __syncthreads();
       }
-      sa.init(Z, len, a.dv, tid);
-      sa.fetch(t0);
-      stage_keys(k);
-      __syncthreads();
-      sa.put(ta, t0);
-      sb.put(tb, t0);
-      __syncthreads();
 #pragma unroll 1
       for (int ib = own / 32; ib < 2; ++ib) {
-        float two[8];
+        float w[8];
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
           f32x4 p = zero4();
+          if (turn == 0) {
 #pragma unroll
-          for (int s = 0; s < ND; ++s) {
-            uint4 e[3];
-            rows16<W>(ta, 32 * ib + 16 * x, s, e);
-            p = dot_planes16(e, e_own[s], p);
+            for (int s = 0; s < ND; ++s) {
+              uint4 e[kPl];
+              rows16<L>(ta, 32 * ib + 16 * x, s, e);
+              p = dot_planes16(e, e_own[s], p);
+            }
+          } else {
+#pragma unroll
+            for (int s = 0; s < ND; ++s) {
+              uint4 e[3];
+              rows16<W>(ta, 32 * ib + 16 * x, s, e);
+              p = dot_planes16(e, e_own[s], p);
+            }
           }
+          settle_mfma();
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             const int i = 32 * ib + 16 * x + 4 * t4 + r;
-            two[4 * x + r] = i > mine ? -(p[r] * decay(sums[i] - my_sum) * (my_rate * rates[i])) : 0.f;
+            const float d = p[r] * (decay(sums[i] - my_sum) * my_rate);
+            w[4 * x + r] = turn == 0 ? (i >= mine ? d * a.scale : 0.f) : i > mine ? -(d * rates[i]) : 0.f;
           }
         }
         uint4 op[3];
-        operand_of<3>(two, op);
+        operand_of<3>(w, op);
 #pragma unroll
         for (int j = 0; j < 2 * ND; ++j) {
           uint4 e[kPl];
           columns16<L>(tb, 32 * ib, j, e);
-          kept[j] = dot_planes16(op, e, kept[j]);
+          sum_k[j] = dot_planes16(op, e, sum_k[j]);
         }
         settle_mfma();
       }
     }
-    // ---- the states, 32 rows at a time
+    // ---- the gradient of the state behind the block
     float inner = 0.f, late_terms = 0.f;
     {
-      uint4 y[ND][kPl], z[ND][3];
-      load_own16<T, ND>(dy + (int64_t)(t0 + mine) * a.dv, there, a.dv, y);
-      load_own16<float, ND>(Z + (int64_t)(t0 + mine) * a.dv, there, a.dv, z);
       const double end = sums[kBlock - 1];
-      float early[4], late[4], rate[4];  // of tokens own + 4 t4 .. +3
+      float late[4];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int i = own + 4 * t4 + r;
-        early[r] = decay(sums[i]), late[r] = decay(end - sums[i]), rate[r] = rates[i];
-      }
-      const float* const S = states + (head * blocks + block) * size;
-      const float* const U = behind + (head * blocks + block) * size;
+      for (int r = 0; r < 4; ++r) late[r] = decay(end - sums[own + 4 * t4 + r]) * rate[r];
       TileStage<float, ND, 32, kBackThreads> ss, su;
       ss.init(S, a.dk, a.dv, tid);
       su.init(U, a.dk, a.dv, tid);
-      u16* const tu = ta + Half::kElems;
-#pragma unroll 1
-      for (int b = 0; 32 * b < a.dk; ++b) {
-        ss.fetch(32 * b);
-        su.fetch(32 * b);
-        __syncthreads();
-        ss.put(ta, 32 * b);
-        su.put(tu, 32 * b);
-        for (int i = tid; i < 32 * a.dv; i += kBackThreads) {
-          const int64_t at = (int64_t)32 * b * a.dv + i;
-          if (at < size) inner = fmaf(S[at], U[at], inner);
-        }
-        __syncthreads();
+      su.fetch(0);
+      ss.fetch(0);
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          f32x4 of_y = zero4(), of_z = zero4(), of_e = zero4();
+      for (int b = 0; b < ND; ++b)
+        if (32 * b < a.dk) {
+          __syncthreads();
+          su.put(ta, 32 * b);
+          if (su.vec && ss.vec) {
 #pragma unroll
-          for (int s = 0; s < ND; ++s) {
-            uint4 e[3];
-            rows16<Half>(ta, 16 * x, s, e);
-            of_y = dot_planes16(y[s], e, of_y);
-            of_z = dot_planes16(z[s], e, of_z);
-            rows16<Half>(tu, 16 * x, s, e);
-            of_e = dot_planes16(e_own[s], e, of_e);
+            for (int i = 0; i < su.kIt; ++i) {
+              inner = fmaf(__uint_as_float(ss.r[i].x), __uint_as_float(su.r[i].x), inner);
+              inner = fmaf(__uint_as_float(ss.r[i].y), __uint_as_float(su.r[i].y), inner);
+              inner = fmaf(__uint_as_float(ss.r[i].z), __uint_as_float(su.r[i].z), inner);
+              inner = fmaf(__uint_as_float(ss.r[i].w), __uint_as_float(su.r[i].w), inner);
+            }
+          } else {
+            for (int i = tid; i < min(32, a.dk - 32 * b) * a.dv; i += kBackThreads)
+              inner = fmaf(S[(int64_t)32 * b * a.dv + i], U[(int64_t)32 * b * a.dv + i], inner);
           }
-          const int col = 32 * b + 16 * x + l15;
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int i = own + 4 * t4 + r;
-            const float ue = of_e[r] * (late[r] * rate[r]), ye = of_y[r] * (early[r] * a.scale), ze = of_z[r] * (early[r] * rate[r]);
-            if (col < a.dk && t0 + i < len) late_terms = fmaf(entry_of(k, (int64_t)(t0 + i) * a.dk + col), ue, late_terms);
-#pragma unroll
-            for (int j = 0; j < 2 * ND; ++j)
-              if (j == 2 * b + x) kept[j][r] += ue, dq[j][r] += ye, asked[j][r] -= ze;
+          __syncthreads();
+          if (32 * b + 32 < a.dk) {
+            su.fetch(32 * b + 32);
+            ss.fetch(32 * b + 32);
           }
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            f32x4 of_e = zero4();
+#pragma unroll
+            for (int s = 0; s < ND; ++s) {
+              uint4 e[3];
+              rows16<Half>(ta, 16 * x, s, e);
+              of_e = dot_planes16(e_own[s], e, of_e);
+            }
+            ck.template fetch<4>(t0 + own, 32 * b + 16 * x);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const float e = of_e[r] * late[r];
+              late_terms = fmaf(ck.value(r), e, late_terms);
+              sum_k[2 * b + x][r] += e;
+            }
+          }
+          settle_mfma();
         }
-      }
-      settle_mfma();
       inner *= decay(end);
     }
-    // ---- the gradients of g and beta
-    float at[4] = {0.f, 0.f, 0.f, 0.f};
+    // ---- dk, and the gradient of g
 #pragma unroll
     for (int j = 0; j < 2 * ND; ++j) {
-      const int col = 16 * j + l15;
+      ck.template fetch<4>(t0 + own, 16 * j);
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int t = t0 + own + 4 * t4 + r;
-        if (col < a.dk && t < len) {
-          const int64_t i = (int64_t)t * a.dk + col;
-          at[r] = fmaf(entry_of(q, i), dq[j][r], fmaf(entry_of(k, i), asked[j][r] - kept[j][r], at[r]));
-        }
+      for (int r = 0; r < 4; ++r) at[r] = fmaf(-ck.value(r), sum_k[j][r], at[r]);
+      if constexpr (MANY) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) all_k[j][r] += sum_k[j][r];
+        sum_k[j] = all_k[j];
       }
+      if (!MANY || v + 1 == a.G)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) gk.store(t0 + own, r, sum_k[j][r], 16 * j);
     }
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
@@ -497,53 +584,12 @@ delta_blocks_kernel(DeltaArgs a, const float* states, const float* behind, const
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) inner += __shfl_xor(inner, d);
     if (lane == 0) parts[wave] = inner;
-    {
-      float dot = 0.f;
-      if (there)
-        for (int i = t4; i < a.dv; i += 4) {
-          const int64_t x = (int64_t)(t0 + mine) * a.dv + i;
-          dot = fmaf(Z[x], E[x], dot);
-        }
-      dot += __shfl_xor(dot, 16);
-      dot += __shfl_xor(dot, 32);
-      if (t4 == 0 && there) a.dbeta[row + t0 + mine] = dot;
-    }
     __syncthreads();
     if (wave == 0) {
-      double sum = terms[lane];
+      double sum = sum_from(terms[lane]);
 #pragma unroll
-      for (int d = 1; d < 64; d *= 2) {
-        const uint64_t u = __builtin_bit_cast(uint64_t, sum);
-        const uint32_t lo = __shfl_down((uint32_t)u, d), hi = __shfl_down((uint32_t)(u >> 32), d);
-        if (lane + d < 64) sum += __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
-      }
-      double rest = 0.0;
-#pragma unroll
-      for (int w = 0; w < kBackWaves; ++w) rest += parts[w];
-      if (t0 + lane < len) a.dg[row + t0 + lane] = (float)(sum + rest);
-    }
-    // ---- dq and dk, over the group's value heads
-#pragma unroll
-    for (int j = 0; j < 2 * ND; ++j) {
-      f32x4 gq = dq[j], gk;
-#pragma unroll
-      for (int r = 0; r < 4; ++r) gk[r] = asked[j][r] + kept[j][r];
-      if constexpr (MANY) {
-#pragma unroll
-        for (int r = 0; r < 4; ++r) all_q[j][r] += gq[r], all_k[j][r] += gk[r];
-        gq = all_q[j], gk = all_k[j];
-      }
-      if (!MANY || v + 1 == a.G) {
-        const int col = 16 * j + l15;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int t = t0 + own + 4 * t4 + r;
-          if (col < a.dk && t < len) {
-            dq_out[(int64_t)t * a.dk + col] = rounded<T>(gq[r]);
-            dk_out[(int64_t)t * a.dk + col] = rounded<T>(gk[r]);
-          }
-        }
-      }
+      for (int w = 0; w < kBackWaves; ++w) sum += parts[w];
+      if (t0 + lane < len) a.dg[row + t0 + lane] = (float)sum;
     }
   }
 }

@@ -105,34 +105,63 @@ struct DeltaChunkBack {
   float whole[4];
 };
 
-// `sizeof(D)` bytes on their way into LDS.
+// The records of a head's chunks on their way into LDS.  (Loads have no branches: behind a branch the compiler waits for
+// all that are on their way.)
 template <typename D, int THREADS>
 struct DataStage {
   static_assert(sizeof(D) % 16 == 0, "whole vectors");
   static constexpr int kVectors = sizeof(D) / 16, kIt = (kVectors + THREADS - 1) / THREADS;
+  VectorReader read;
+  int tid;
   uint4 r[kIt];
-  __device__ __forceinline__ void fetch(const D* d, int tid) {
-#pragma unroll
-    for (int i = 0; i < kIt; ++i)
-      if (tid + i * THREADS < kVectors) r[i] = ((const uint4*)d)[tid + i * THREADS];
+  __device__ __forceinline__ void init(const D* records, int count, int tid_) {
+    read = VectorReader(records, (int64_t)count * sizeof(D));
+    tid = tid_;
   }
-  __device__ __forceinline__ void put(D* d, int tid) const {
+  __device__ __forceinline__ void fetch(int c) {
+#pragma unroll
+    for (int i = 0; i < kIt; ++i) r[i] = read((uint32_t)c * (uint32_t)sizeof(D) + 16u * (uint32_t)(tid + i * THREADS));
+  }
+  __device__ __forceinline__ void put(D* d) const {
 #pragma unroll
     for (int i = 0; i < kIt; ++i)
-      if (tid + i * THREADS < kVectors) ((uint4*)d)[tid + i * THREADS] = r[i];
+      if ((i + 1) * THREADS <= kVectors || tid + i * THREADS < kVectors) ((uint4*)d)[tid + i * THREADS] = r[i];
   }
 };
 
-// Entries of rows 16 x + 4 t4 .. +3 (x = 0, 1) of this lane's column, zero behind `rows`.
+// One column of a head's [rows][pitch] entries, a lane its own: entries of rows t0 + 16 x + 4 t4 .. +3 (x = 0, 1), zero behind
+// the last row and where the lane has no column.  Stores there are dropped.
 template <typename T>
-__device__ __forceinline__ void fetch_column(const T* p, int rows, int pitch, bool on, T (&v)[8]) {
-  const int t4 = (threadIdx.x & 63) >> 4;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const int r = 16 * (e >> 2) + 4 * t4 + (e & 3);
-    v[e] = on && r < rows ? p[(int64_t)r * pitch] : (T)0;
+struct ColumnStage {
+  __amdgpu_buffer_rsrc_t rsrc;
+  uint32_t off, pitch;
+  int left;  // columns from this lane's on
+  uint32_t r[8];
+  __device__ __forceinline__ void init(const T* head, int rows, int width, int col) {
+    rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(head), 0, rows * width * (int)sizeof(T), 0x00020000);
+    pitch = (uint32_t)(width * (int)sizeof(T));
+    left = width - col;
+    off = (uint32_t)((threadIdx.x & 63) >> 4) * 4u * pitch + (uint32_t)(col * (int)sizeof(T));
   }
-}
+  // (of the column `ahead` further on, of which the lane may have none)
+  __device__ __forceinline__ uint32_t at(int t0, int e, int ahead) const {
+    const uint32_t place = off + (uint32_t)(t0 + 16 * (e >> 2) + (e & 3)) * pitch + (uint32_t)(ahead * (int)sizeof(T));
+    return ahead < left ? place : kNoVector;
+  }
+  template <int COUNT = 8>
+  __device__ __forceinline__ void fetch(int t0, int ahead = 0) {
+#pragma unroll
+    for (int e = 0; e < COUNT; ++e) {
+      if constexpr (sizeof(T) == 4) r[e] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rsrc, (int)at(t0, e, ahead), 0, 0);
+      else r[e] = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rsrc, (int)at(t0, e, ahead), 0, 0);
+    }
+  }
+  __device__ __forceinline__ float value(int e) const { return __uint_as_float(sizeof(T) == 4 ? r[e] : r[e] << 16); }
+  __device__ __forceinline__ void store(int t0, int e, float x, int ahead = 0) const {
+    if constexpr (sizeof(T) == 4) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(x), rsrc, (int)at(t0, e, ahead), 0, 0);
+    else __builtin_amdgcn_raw_buffer_store_b16((unsigned short)(pack2(x, 0.f) & 0xffffu), rsrc, (int)at(t0, e, ahead), 0, 0);
+  }
+};
 
 // Workgroups to heads and slices of columns: an XCD takes whole heads, whose queries and keys are then read through one L2.
 __device__ __forceinline__ bool delta_place(int heads, int slices, int& head, int& slice) {
