@@ -85,25 +85,27 @@ hipError_t launch_tokens(const DeltaArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-// ---- chunk by chunk
+// ---- block by block
 //
 // A wave has 16 columns of the state, S[j] rows 16 j + 4 t4 .. +3 of column l15, for a head's whole sequence; four waves
-// make a workgroup and share the staged queries and keys.  For a chunk (delta_tiles.hpp)
-//     R = k S,  r = v - early R,  E = inverse r,  y = c early q S + P E,  S = whole S + k^T (late E),
+// make a workgroup and share the staged queries and keys.  For a block (delta_tiles.hpp)
+//     R = k S,  r = v - early R - (L_21 E_1 in the second half),  E = inverse r,
+//     y = c early q S + P E,  S = whole S + k^T (late E),
 // each a product whose right operand is what the one before left in this lane.
 constexpr int kScanWaves = 4;
 
-// One of the buffers in LDS: a chunk's keys, queries and what its pairs left.
+// One of the buffers in LDS: a block's keys, queries and what its pairs left.
 template <typename T, int ND>
 struct DeltaLds {
-  using L = PairTile<T, ND, kDeltaChunk>;
-  using Data = DeltaChunkData<sizeof(T) == 2>;
+  using L = PairTile<T, ND, kDeltaBlock>;
+  using Data = DeltaForward<sizeof(T) == 2>;
   static constexpr int kBuffers = sizeof(T) == 2 ? 2 : 1;
   static constexpr int kBuffer = 2 * L::kBytes + (int)sizeof(Data);
   static constexpr int kBytes = kBuffers * kBuffer;
+  static_assert(kBytes <= 160 * 1024, "LDS of one workgroup");
 };
 
-// A chunk's tokens one by one, for chunks in which something is not finite: products would take it to earlier tokens,
+// A block's tokens one by one, for blocks in which something is not finite: products would take it to earlier tokens,
 // whose weights of it are zero.
 template <typename T, int ND>
 __device__ __forceinline__ void delta_one_by_one(const DeltaArgs& a, int head, int64_t shared, int t0, int m, int col, bool on,
@@ -156,21 +158,21 @@ __device__ __forceinline__ void delta_one_by_one(const DeltaArgs& a, int head, i
 
 // GRAD: no outputs, but the errors and the states before every block.
 template <typename T, int ND, bool GRAD>
-__global__ void __launch_bounds__(64 * kScanWaves, 2) delta_scan_kernel(DeltaArgs a, const void* data_, float* states, float* errors,
+__global__ void __launch_bounds__(64 * kScanWaves, 1) delta_scan_kernel(DeltaArgs a, const void* data_, float* states, float* errors,
                                                                         int slices) {
   extern __shared__ __attribute__((aligned(16))) u16 smem16[];
   constexpr bool BF16 = sizeof(T) == 2;
-  constexpr int C = kDeltaChunk, kThreads = 64 * kScanWaves;
+  constexpr int C = kDeltaBlock, kThreads = 64 * kScanWaves;
   using D = DeltaLds<T, ND>;
   using L = typename D::L;
-  using Data = DeltaChunkData<BF16>;
+  using Data = typename D::Data;
   constexpr int PE = Data::kPair, PY = BF16 ? 2 : 3;  // numbers of an error and of a state's entry in the outputs
   int head, slice;
   if (!delta_place(a.heads, slices, head, slice)) return;
   const int tid = threadIdx.x, lane = tid & 63, l15 = lane & 15, t4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t shared = head / a.G;
-  const int len = tokens_of(a.lengths, head / (a.Hk * a.G), a.n), chunks = (len + C - 1) / C;
+  const int len = tokens_of(a.lengths, head / (a.Hk * a.G), a.n), blocks = (len + C - 1) / C;
   const int c0 = 16 * (kScanWaves * slice + wave), col = c0 + l15;
   const bool on = col < a.dv;
   const int64_t size = (int64_t)a.dk * a.dv;
@@ -193,7 +195,7 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2) delta_scan_kernel(DeltaArg
   };
   T* const y = GRAD ? nullptr : (T*)a.y + (int64_t)head * a.n * a.dv;
   const bool vec = a.dv % 4 == 0 && ((uintptr_t)y & (4 * sizeof(T) - 1)) == 0;
-  if (chunks > 0) {
+  if (blocks > 0) {
     const Data* const data = (const Data*)data_ + (int64_t)head * ((a.n + C - 1) / C);
     TileStage<T, ND, C, kThreads> sq, sk;
     sq.init((const T*)a.q + shared * a.n * a.dk, len, a.dk, tid);
@@ -201,14 +203,14 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2) delta_scan_kernel(DeltaArg
     DataStage<Data, kThreads> sd;
     ColumnStage<T> sv;
     ColumnStage<float> se;
-    sd.init(data, chunks, tid);
+    sd.init(data, blocks, tid);
     sv.init((const T*)a.v + (int64_t)head * a.n * a.dv, len, a.dv, col);
     if (GRAD) se.init(errors + (int64_t)head * a.n * a.dv, len, a.dv, col);
     sk.fetch(0);
     if (!GRAD) sq.fetch(0);
     sd.fetch(0);
     sv.fetch(0);
-    for (int c = 0; c < chunks; ++c) {
+    for (int c = 0; c < blocks; ++c) {
       const int t0 = c * C;
       u16* const tk = smem16 + (D::kBuffers == 2 && (c & 1) ? D::kBuffer / 2 : 0);
       u16* const tq = tk + L::kElems;
@@ -218,94 +220,135 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2) delta_scan_kernel(DeltaArg
       if (!GRAD) sq.put(tq, t0);
       sd.put(&d);
       __syncthreads();
-      float r[8];
+      float r[16];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) r[e] = sv.value(e);
-      if (c + 1 < chunks) {
+      for (int e = 0; e < 16; ++e) r[e] = sv.value(e);
+      if (c + 1 < blocks) {
         sk.fetch(t0 + C);
         if (!GRAD) sq.fetch(t0 + C);
         sd.fetch(c + 1);
         sv.fetch(t0 + C);
       }
-      if (GRAD && c % (kDeltaBlock / C) == 0)
-        put_state(states + ((int64_t)head * ((a.n + kDeltaBlock - 1) / kDeltaBlock) + c / (kDeltaBlock / C)) * size);
-      f32x4 R[2] = {zero4(), zero4()}, o[2] = {zero4(), zero4()};
+      if (GRAD) put_state(states + ((int64_t)head * ((a.n + C - 1) / C) + c) * size);
+      // Operands are loaded well ahead of their products: with one wave a SIMD nothing else hides LDS's latency.
+      f32x4 early[4], late[4];
 #pragma unroll
-      for (int b = 0; b < ND; ++b) {
-        uint4 st[3];
-        operand_of<3>(S[2 * b], S[2 * b + 1], st);
-        uint4 so[PY];
+      for (int x = 0; x < 4; ++x) {
+        early[x] = *(const f32x4*)(d.early + 16 * x + 4 * t4);
+        late[x] = *(const f32x4*)(d.late + 16 * x + 4 * t4);
+      }
+      const float whole = d.whole[0];
+      auto operand = [&](const DeltaOperand* p, int x, auto& op) {
 #pragma unroll
-        for (int p = 0; p < PY; ++p) so[p] = st[p];
+        for (int i = 0; i < (int)(sizeof(op) / sizeof(op[0])); ++i) op[i] = p[i][x][lane];
+      };
+      uint4 st[ND][3];
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
+      for (int b = 0; b < ND; ++b) operand_of<3>(S[2 * b], S[2 * b + 1], st[b]);
+      f32x4 R[4], o[4], E[4];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        R[x] = zero4();
+#pragma unroll
+        for (int b = 0; b < ND; ++b) {
           uint4 e[L::kPl];
           rows16_as_results<L>(tk, 16 * x, b, e);
-          R[x] = dot_planes16(e, st, R[x]);
-          if (!GRAD) {
+          R[x] = dot_planes16(e, st[b], R[x]);
+        }
+      }
+      if constexpr (!GRAD) {
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          o[x] = zero4();
+#pragma unroll
+          for (int b = 0; b < ND; ++b) {
+            uint4 so[PY], e[L::kPl];
+#pragma unroll
+            for (int p = 0; p < PY; ++p) so[p] = st[b][p];
             rows16_as_results<L>(tq, 16 * x, b, e);
             o[x] = dot_planes16(so, e, o[x]);
           }
         }
       }
-      float most = 0.f;
-      f32x4 early[2] = {*(const f32x4*)(d.early + 4 * t4), *(const f32x4*)(d.early + 16 + 4 * t4)};
+      float bad = 0.f;  // (an infinity or NaN times zero is NaN)
+      uint4 ep[2][3];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        r[e] = fmaf(-early[e >> 2][e & 3], R[e >> 2][e & 3], r[e]);
-        most = r[e] - r[e] == 0.f ? most : 1.f;  // (an infinity's difference with itself is no number)
+      for (int h = 0; h < 2; ++h) {
+        uint4 inv[2][3];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) operand(d.inverse[h], x, inv[x]);
+        f32x4 before[2] = {zero4(), zero4()};
+        if (h == 1) {
+          uint4 below[2][3];
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            operand(d.below, x, below[x]);
+            before[x] = dot_planes16(below[x], ep[0], before[x]);
+          }
+        }
+        float z[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          z[e] = fmaf(-early[2 * h + (e >> 2)][e & 3], R[2 * h + (e >> 2)][e & 3], r[8 * h + e]);
+          if (h == 1) z[e] -= before[e >> 2][e & 3];
+          bad = fmaf(z[e], 0.f, bad);
+        }
+        uint4 rp[3];
+        operand_of<3>(z, rp);
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          E[2 * h + x] = dot_planes16(inv[x], rp, zero4());
+#pragma unroll
+          for (int i = 0; i < 4; ++i) bad = fmaf(E[2 * h + x][i], 0.f, bad);
+        }
+        operand_of<3>(E[2 * h], E[2 * h + 1], ep[h]);
       }
-      uint4 rp[3];
-      operand_of<3>(r, rp);
-      f32x4 E[2];
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        uint4 inv[Data::kInverse];
-#pragma unroll
-        for (int p = 0; p < Data::kInverse; ++p) inv[p] = d.inverse[p][x][lane];
-        E[x] = dot_planes16(inv, rp, zero4());
-      }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) most = E[e >> 2][e & 3] - E[e >> 2][e & 3] == 0.f ? most : 1.f;
       settle_mfma();
-      if (__builtin_expect(__ballot(most != 0.f) != 0, 0)) {
+      if (__builtin_expect(__ballot(!(bad == 0.f)) != 0, 0)) {
         delta_one_by_one<T, ND>(a, head, shared, t0, min(C, len - t0), col, on, S, y, GRAD ? errors : nullptr);
         continue;
       }
+      uint4 wp[2][3];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float w[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = E[2 * h + (e >> 2)][e & 3] * late[2 * h + (e >> 2)][e & 3];
+        operand_of<3>(w, wp[h]);
+      }
       if (GRAD) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) se.store(t0, e, E[e >> 2][e & 3]);
+        for (int e = 0; e < 16; ++e) se.store(t0, e, E[e >> 2][e & 3]);
       } else {
-        uint4 ep[PE];
-        operand_of<PE>(E[0], E[1], ep);
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
+        for (int x = 0; x < 4; ++x) {
+          const float readout = d.early[16 * x + l15] * a.scale;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) o[x][i] *= d.early[16 * x + l15] * a.scale;
-          uint4 pairs[PE];
+          for (int i = 0; i < 4; ++i) o[x][i] *= readout;
 #pragma unroll
-          for (int p = 0; p < PE; ++p) pairs[p] = d.pairs[p][x][lane];
-          o[x] = dot_planes16(ep, pairs, o[x]);
+          for (int h = 0; h <= x / 2; ++h) {
+            uint4 pairs[PE], e[PE];
+            operand(d.pairs[x / 2 + h], x & 1, pairs);
+#pragma unroll
+            for (int p = 0; p < PE; ++p) e[p] = ep[h][p];
+            o[x] = dot_planes16<PE - 1>(e, pairs, o[x]);
+          }
         }
       }
-      float w[8];
-      f32x4 late[2] = {*(const f32x4*)(d.late + 4 * t4), *(const f32x4*)(d.late + 16 + 4 * t4)};
-      const float whole = d.whole[0];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) w[e] = E[e >> 2][e & 3] * late[e >> 2][e & 3];
-      uint4 wp[3];
-      operand_of<3>(w, wp);
 #pragma unroll
       for (int j = 0; j < 2 * ND; ++j) {
-        uint4 e[L::kPl];
-        columns16<L>(tk, 0, j, e);
 #pragma unroll
         for (int i = 0; i < 4; ++i) S[j][i] *= whole;
-        S[j] = dot_planes16(e, wp, S[j]);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          uint4 e[L::kPl];
+          columns16<L>(tk, 32 * h, j, e);
+          S[j] = dot_planes16(e, wp[h], S[j]);
+        }
       }
       if (!GRAD) {
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
+        for (int x = 0; x < 4; ++x) {
           const int t = t0 + 16 * x + l15;
           const float z[4] = {o[x][0], o[x][1], o[x][2], o[x][3]};
           if (t < len) store4<T>(y + (int64_t)t * a.dv, c0 + 4 * t4, a.dv, z, vec);
@@ -346,7 +389,7 @@ hipError_t launch_scan_t(const DeltaArgs& a, const void* data, float* states, fl
 }  // namespace
 
 size_t delta_prefill_scratch(bool bf16, int heads, int, int n, int, int) {
-  return delta_data_bytes(bf16, heads, n);
+  return delta_forward_bytes(bf16, heads, n);
 }
 
 hipError_t launch_delta_prefill(const DeltaArgs& a, bool bf16, void* scratch, hipStream_t s) {

@@ -1,10 +1,9 @@
-// Gradients of the gated delta rule, in four passes: what the chunks' pairs leave (delta_pairs.hip), forward for the
+// Gradients of the gated delta rule, in four passes: what the blocks' pairs leave (delta_pairs.hip), forward for the
 // states before every 64 tokens and the errors E = v - k S' (delta.hip), backward for the states' gradients U
 // and z = dL/du, and then, all blocks of 64 tokens side by side, what a block's tokens
-// make of these.  With G_i the sums of the log decays in a chunk, L and the letters of delta_tiles.hpp, D = -beta z,
-// S the state before the chunk and U the gradient behind it:
-//     du  = P0^T dy + exp(G_C - G) (k U),   P0_ij = c exp(G_i - G_j) q_i.k_j (j <= i)
-//     z   = (I + beta L)^-T du,   dv = beta z,   dbeta = z.E
+// make of these.  With the letters of delta_tiles.hpp, D = -beta z, S the state before a block and U the gradient behind it:
+//     du  = P^T dy + exp(G_C - G) (k U),   P_ij = c exp(G_i - G_j) q_i.k_j (j <= i)
+//     z   = (I + M)^-T du,   M_ij = exp(G_i - G_j) beta_i k_i.k_j (j < i),   dv = beta z,   dbeta = z.E
 //     U   = exp(G_C) U + (c exp(G) q)^T dy + (exp(G) k)^T D
 //     dq  = c exp(G) dy S^T + one k,                 one_ij = c exp(G_i - G_j) dy_i.u_j (j <= i)
 //     dk  = asked + kept,  asked = exp(G) D S^T + two k,   two_ij = exp(G_i - G_j) D_i.u_j (j < i)
@@ -21,31 +20,31 @@ namespace sata {
 
 namespace {
 
-constexpr int C = kDeltaChunk, kBlock = kDeltaBlock;
+constexpr int kBlock = kDeltaBlock;
 constexpr int kBackWaves = 4, kBackThreads = 64 * kBackWaves;
 
 // ---- from the last token back: a wave has 16 columns of U, as the forward scan of S
 template <typename T, int ND>
 struct BackLds {
-  using L = PairTile<T, ND, C>;
-  using Data = DeltaChunkBack<sizeof(T) == 2>;
+  using L = PairTile<T, ND, kBlock>;
   static constexpr int kBuffers = sizeof(T) == 2 ? 2 : 1;
-  static constexpr int kBuffer = 2 * L::kBytes + (int)sizeof(Data);
+  static constexpr int kBuffer = 2 * L::kBytes + (int)sizeof(DeltaBackward);
   static constexpr int kBytes = kBuffers * kBuffer;
+  static_assert(kBytes <= 160 * 1024, "LDS of one workgroup");
 };
 
 template <typename T, int ND>
-__global__ void __launch_bounds__(kBackThreads, 2) delta_back_kernel(DeltaArgs a, const void* data_, float* behind, float* zs, int slices) {
+__global__ void __launch_bounds__(kBackThreads, 1) delta_back_kernel(DeltaArgs a, const void* data_, float* behind, float* zs, int slices) {
   extern __shared__ __attribute__((aligned(16))) u16 smem16[];
   using D = BackLds<T, ND>;
   using L = typename D::L;
-  using Data = typename D::Data;
+  using Data = DeltaBackward;
   int head, slice;
   if (!delta_place(a.heads, slices, head, slice)) return;
   const int tid = threadIdx.x, lane = tid & 63, l15 = lane & 15, t4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t shared = head / a.G;
-  const int len = tokens_of(a.lengths, head / (a.Hk * a.G), a.n), chunks = (len + C - 1) / C;
+  const int len = tokens_of(a.lengths, head / (a.Hk * a.G), a.n), blocks = (len + kBlock - 1) / kBlock;
   const int col = 16 * (kBackWaves * slice + wave) + l15;
   const bool on = col < a.dv;
   const int64_t size = (int64_t)a.dk * a.dv;
@@ -66,29 +65,28 @@ __global__ void __launch_bounds__(kBackThreads, 2) delta_back_kernel(DeltaArgs a
         if (on && row < a.dk) to[(int64_t)row * a.dv + col] = U[j][i];
       }
   };
-  T* const dv = (T*)a.dv_out + (int64_t)head * a.n * a.dv + col;
-  if (chunks > 0) {
-    const Data* const data = (const Data*)data_ + (int64_t)head * ((a.n + C - 1) / C);
-    TileStage<T, ND, C, kBackThreads> sq, sk;
+  const int64_t all_blocks = (a.n + kBlock - 1) / kBlock;
+  if (blocks > 0) {
+    TileStage<T, ND, kBlock, kBackThreads> sq, sk;
     sq.init((const T*)a.q + shared * a.n * a.dk, len, a.dk, tid);
     sk.init((const T*)a.k + shared * a.n * a.dk, len, a.dk, tid);
     DataStage<Data, kBackThreads> sd;
     ColumnStage<T> sy, sv;
     ColumnStage<float> sz;
     const int64_t head0 = (int64_t)head * a.n * a.dv;
-    sd.init(data, chunks, tid);
+    sd.init((const Data*)data_ + head * all_blocks, blocks, tid);
     sy.init((const T*)a.dy + head0, len, a.dv, col);
     sv.init((const T*)a.dv_out + head0, len, a.dv, col);
     sz.init(zs + head0, len, a.dv, col);
     auto fetch = [&](int c) {
-      sk.fetch(c * C);
-      sq.fetch(c * C);
+      sk.fetch(c * kBlock);
+      sq.fetch(c * kBlock);
       sd.fetch(c);
-      sy.fetch(c * C);
+      sy.fetch(c * kBlock);
     };
-    fetch(chunks - 1);
-    for (int c = chunks - 1; c >= 0; --c) {
-      const int t0 = c * C;
+    fetch(blocks - 1);
+    for (int c = blocks - 1; c >= 0; --c) {
+      const int t0 = c * kBlock;
       u16* const tk = smem16 + (D::kBuffers == 2 && (c & 1) ? D::kBuffer / 2 : 0);
       u16* const tq = tk + L::kElems;
       Data& d = *(Data*)(tq + L::kElems);
@@ -97,83 +95,115 @@ __global__ void __launch_bounds__(kBackThreads, 2) delta_back_kernel(DeltaArgs a
       sq.put(tq, t0);
       sd.put(&d);
       __syncthreads();
-      float y[8];
+      float y[16];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = sy.value(e);
+      for (int e = 0; e < 16; ++e) y[e] = sy.value(e);
       if (c > 0) fetch(c - 1);
-      if (c == chunks - 1 || c % (kBlock / C) == kBlock / C - 1)
-        put_state(behind + ((int64_t)head * ((a.n + kBlock - 1) / kBlock) + c / (kBlock / C)) * size);
-      f32x4 R[2] = {zero4(), zero4()}, du[2];
+      put_state(behind + (head * all_blocks + c) * size);
+      auto operand = [&](const DeltaOperand* p, int x, uint4 (&op)[3]) {
 #pragma unroll
-      for (int b = 0; b < ND; ++b) {
-        uint4 st[3];
-        operand_of<3>(U[2 * b], U[2 * b + 1], st);
+        for (int i = 0; i < 3; ++i) op[i] = p[i][x][lane];
+      };
+      f32x4 early[4], late[4], beta[4];
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
+      for (int x = 0; x < 4; ++x) {
+        early[x] = *(const f32x4*)(d.early + 16 * x + 4 * t4);
+        late[x] = *(const f32x4*)(d.late + 16 * x + 4 * t4);
+        beta[x] = *(const f32x4*)(d.beta + 16 * x + 4 * t4);
+      }
+      const float whole = d.whole[0];
+      uint4 st[ND][3];
+#pragma unroll
+      for (int b = 0; b < ND; ++b) operand_of<3>(U[2 * b], U[2 * b + 1], st[b]);
+      f32x4 R[4], z[4];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        R[x] = zero4();
+#pragma unroll
+        for (int b = 0; b < ND; ++b) {
           uint4 e[L::kPl];
           rows16_as_results<L>(tk, 16 * x, b, e);
-          R[x] = dot_planes16(e, st, R[x]);
+          R[x] = dot_planes16(e, st[b], R[x]);
         }
       }
-      const f32x4 early[2] = {*(const f32x4*)(d.early + 4 * t4), *(const f32x4*)(d.early + 16 + 4 * t4)};
-      const f32x4 late[2] = {*(const f32x4*)(d.late + 4 * t4), *(const f32x4*)(d.late + 16 + 4 * t4)};
-      const f32x4 beta[2] = {*(const f32x4*)(d.beta + 4 * t4), *(const f32x4*)(d.beta + 16 + 4 * t4)};
-      const float whole = d.whole[0];
-      {
-        float x8[8];
+      uint4 yp[2][L::kPl], ep[2][3], zp[3], wp[2][3];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x8[e] = y[e];
-        uint4 yp[L::kPl];
-        operand_of<L::kPl>(x8, yp);
+      for (int h = 0; h < 2; ++h) {
+        float x8[8], e8[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          x8[e] = y[8 * h + e];
+          e8[e] = x8[e] * (early[2 * h + (e >> 2)][e & 3] * a.scale);
+        }
+        operand_of<L::kPl>(x8, yp[h]);
+        operand_of<3>(e8, ep[h]);
+      }
+      // the second half first: the first one's updates are seen by its keys
+#pragma unroll
+      for (int h = 1; h >= 0; --h) {
+        f32x4 du[2];
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
           uint4 p[3];
+          operand(d.pairs[2 * h], x, p);
+          du[x] = dot_planes16(p, yp[h], zero4());
+          if (h == 0) {
+            operand(d.pairs[1], x, p);
+            du[x] = dot_planes16(p, yp[1], du[x]);
+          }
 #pragma unroll
-          for (int i = 0; i < 3; ++i) p[i] = d.pairs[i][x][lane];
-          du[x] = dot_planes16(p, yp, zero4());
+          for (int i = 0; i < 4; ++i) du[x][i] = fmaf(late[2 * h + x][i], R[2 * h + x][i], du[x][i]);
+          if (h == 0) {
+            operand(d.below, x, p);
+            const f32x4 m = dot_planes16(p, zp, zero4());
 #pragma unroll
-          for (int i = 0; i < 4; ++i) du[x][i] = fmaf(late[x][i], R[x][i], du[x][i]);
+            for (int i = 0; i < 4; ++i) du[x][i] -= m[i];
+          }
         }
-      }
-      uint4 dp[3];
-      operand_of<3>(du[0], du[1], dp);
-      f32x4 z[2];
+        uint4 dp[3];
+        operand_of<3>(du[0], du[1], dp);
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        uint4 p[3];
-#pragma unroll
-        for (int i = 0; i < 3; ++i) p[i] = d.inverse[i][x][lane];
-        z[x] = dot_planes16(p, dp, zero4());
+        for (int x = 0; x < 2; ++x) {
+          uint4 p[3];
+          operand(d.inverse[h], x, p);
+          z[2 * h + x] = dot_planes16(p, dp, zero4());
+        }
+        if (h == 1) operand_of<3>(z[2], z[3], zp);
       }
-      float w[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int x = e >> 2, i = e & 3;
-        w[e] = beta[x][i] * z[x][i];
-        sz.store(t0, e, z[x][i]);
-        sv.store(t0, e, w[e]);
-        w[e] *= -early[x][i];
-        y[e] *= early[x][i] * a.scale;
+      for (int h = 0; h < 2; ++h) {
+        float w[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int x = 2 * h + (e >> 2), i = e & 3;
+          w[e] = beta[x][i] * z[x][i];
+          sz.store(t0, 8 * h + e, z[x][i]);
+          sv.store(t0, 8 * h + e, w[e]);
+          w[e] *= -early[x][i];
+        }
+        operand_of<3>(w, wp[h]);
       }
-      uint4 wp[3], yp[3];
-      operand_of<3>(w, wp);
-      operand_of<3>(y, yp);
 #pragma unroll
       for (int j = 0; j < 2 * ND; ++j) {
-        uint4 e[L::kPl];
 #pragma unroll
         for (int i = 0; i < 4; ++i) U[j][i] *= whole;
-        columns16<L>(tk, 0, j, e);
-        U[j] = dot_planes16(e, wp, U[j]);
-        columns16<L>(tq, 0, j, e);
-        U[j] = dot_planes16(e, yp, U[j]);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          uint4 e[L::kPl];
+          columns16<L>(tq, 32 * h, j, e);
+          U[j] = dot_planes16(e, ep[h], U[j]);
+          columns16<L>(tk, 32 * h, j, e);
+          U[j] = dot_planes16(e, wp[h], U[j]);
+        }
       }
       settle_mfma();
     }
   }
   if (a.dS_in) put_state(a.dS_in + head * size);
-  if (on)
+  if (on) {
+    T* const dv = (T*)a.dv_out + (int64_t)head * a.n * a.dv + col;
     for (int t = len + t4; t < a.n; t += 4) dv[(int64_t)t * a.dv] = (T)0;
+  }
 }
 
 // ---- block by block: a wave has 16 of 64 tokens and all columns of their dq and dk
@@ -599,12 +629,12 @@ struct Places {
   size_t data, back, states, behind, errors, zs, bytes;
 };
 Places places_of(bool bf16, int heads, int n, int dk, int dv) {
-  const size_t chunks = (size_t)heads * ((n + C - 1) / C), blocks = (size_t)heads * ((n + kBlock - 1) / kBlock);
+  const size_t blocks = (size_t)heads * ((n + kBlock - 1) / kBlock);
   auto whole = [](size_t x) { return (x + 255) / 256 * 256; };
   Places p;
   p.data = 0;
-  p.back = whole(delta_data_bytes(bf16, heads, n));
-  p.states = p.back + whole(chunks * (bf16 ? sizeof(DeltaChunkBack<true>) : sizeof(DeltaChunkBack<false>)));
+  p.back = whole(delta_forward_bytes(bf16, heads, n));
+  p.states = p.back + whole(blocks * sizeof(DeltaBackward));
   p.behind = p.states + whole(blocks * dk * dv * sizeof(float));
   p.errors = p.behind + whole(blocks * dk * dv * sizeof(float));
   p.zs = p.errors + whole((size_t)heads * n * dv * sizeof(float));

@@ -1,10 +1,11 @@
-// What the pairs of a chunk's tokens leave for the delta rule's scans (delta_tiles.hpp): the products of its keys and
-// queries, weighted by the decays, and the inverse of a unit lower triangular matrix.
+// What the pairs of a block's tokens leave for the delta rule's scans (delta_tiles.hpp): the products of its keys and
+// queries, weighted by the decays, and the inverses of unit lower triangular matrices.
 //
-// A wave takes a chunk of 32 tokens of one query and key head: k.k and q.k once, then for each of its value heads the
-// decays' sums (in 64 bits: differences of large sums keep their digits), the weights, and the inverse by
-// forward substitution of the two 16 x 16 blocks on the diagonal, a column a lane, and
-// -X22 A21 X11 below.  All chunks side by side: the scans, which cannot be, have only products left.
+// Three waves to a block of 64 tokens of a query and key head: one for the pairs within each half, one for those
+// across.  A wave forms k.k and q.k once, then for each value head the decays' sums (in 64 bits: differences
+// of large sums keep their digits), the weights, and for a half the inverse, by
+// forward substitution of the two 16 x 16 blocks on the diagonal, a column a lane, and -X22 A21 X11 below.
+// All blocks side by side: the scans, which cannot be, have only products left.
 #include <hip/hip_runtime.h>
 
 #include "delta_tiles.hpp"
@@ -13,7 +14,7 @@ namespace sata {
 
 namespace {
 
-constexpr int C = kDeltaChunk;
+constexpr int C = 32;  // tokens of a half
 constexpr int kPitch = C + 4;  // floats of a row in LDS
 
 __device__ __forceinline__ double shuffle_up(double x, int d) {
@@ -77,7 +78,7 @@ __device__ __forceinline__ void invert(const float* A, float* X, float* Y) {
 
 // A 32 x 32 matrix in LDS as operands of its rows (or its columns), entries in the order of a result's rows.
 template <int PL, bool TRANSPOSED>
-__device__ __forceinline__ void put_operand(const float* m, uint4 (*out)[2][64]) {
+__device__ __forceinline__ void put_operand(const float* m, DeltaOperand* out) {
   const int lane = threadIdx.x & 63, l15 = lane & 15, t4 = lane >> 4;
 #pragma unroll
   for (int x = 0; x < 2; ++x) {
@@ -95,108 +96,134 @@ __device__ __forceinline__ void put_operand(const float* m, uint4 (*out)[2][64])
 }
 
 template <typename T, int ND, bool BACK>
-__global__ void __launch_bounds__(64) delta_pairs_kernel(DeltaArgs a, void* data_, void* back_) {
+__global__ void __launch_bounds__(64) delta_pairs_kernel(DeltaArgs a, void* forward_, void* backward_) {
   constexpr bool BF16 = sizeof(T) == 2;
   constexpr int kPl = BF16 ? 1 : 3;
+  using Forward = DeltaForward<BF16>;
   __shared__ __attribute__((aligned(16))) float A[C * kPitch], X[C * kPitch], W[C * kPitch];
-  __shared__ double sums[C];
-  __shared__ float rates[C];
+  __shared__ double sums[kDeltaBlock];
+  __shared__ float rates[kDeltaBlock];
   const int lane = threadIdx.x & 63, l31 = lane & 31, h = lane >> 5;
-  const int chunks = (a.n + C - 1) / C, chunk = blockIdx.x, shared = blockIdx.y, t0 = chunk * C;
-  const int len = tokens_of(a.lengths, shared / a.Hk, a.n);
+  const int blocks = (a.n + kDeltaBlock - 1) / kDeltaBlock, block = blockIdx.x / 3, part = blockIdx.x % 3, shared = blockIdx.y;
+  const int t0 = block * kDeltaBlock, len = tokens_of(a.lengths, shared / a.Hk, a.n);
   if (t0 >= len) return;
-  const bool there = t0 + l31 < len;
-  f32x16 kk = zero16(), qk = zero16();  // of key result_row(i, h) with key and query l31
+  const int i0 = part == 0 ? 0 : C, j0 = part == 1 ? C : 0;  // the halves of queries (and later keys), and of keys
+  f32x16 kk = zero16(), qk = zero16();  // of key j0 + result_row(i, h) with key and query i0 + l31
   {
-    uint4 k[2 * ND][kPl], q[2 * ND][kPl];
-    const int64_t row = (int64_t)shared * a.n + t0 + l31;
-    load_own32<T, ND>((const T*)a.k + row * a.dk, there, a.dk, k);
-    load_own32<T, ND>((const T*)a.q + row * a.dk, there, a.dk, q);
+    uint4 kj[2 * ND][kPl], x[2 * ND][kPl];
+    auto load = [&](const void* p, int r, uint4 (&to)[2 * ND][kPl]) {
+      load_own32<T, ND>((const T*)p + ((int64_t)shared * a.n + t0 + r + l31) * a.dk, t0 + r + l31 < len, a.dk, to);
+    };
+    load(a.k, j0, kj);
+    load(a.q, i0, x);
 #pragma unroll
-    for (int s = 0; s < 2 * ND; ++s) {
-      kk = dot_planes32(k[s], k[s], kk);
-      qk = dot_planes32(k[s], q[s], qk);
-    }
+    for (int s = 0; s < 2 * ND; ++s) qk = dot_planes32(kj[s], x[s], qk);
+    if (part == 2) load(a.k, i0, x);
+    else
+#pragma unroll
+      for (int s = 0; s < 2 * ND; ++s)
+#pragma unroll
+        for (int p = 0; p < kPl; ++p) x[s][p] = kj[s][p];
+#pragma unroll
+    for (int s = 0; s < 2 * ND; ++s) kk = dot_planes32(kj[s], x[s], kk);
     settle_mfma32();
   }
   for (int v = 0; v < a.G; ++v) {
-    const int64_t head = (int64_t)shared * a.G + v, at = head * a.n + t0 + l31;
+    const int64_t head = (int64_t)shared * a.G + v, at = head * a.n + t0 + lane;
+    const bool there = t0 + lane < len;
     double sum = there ? delta_rate(a.g[at]) : 0.0;
     const float beta = there ? a.beta[at] : 0.f;
 #pragma unroll
-    for (int d = 1; d < C; d *= 2) {
+    for (int d = 1; d < 64; d *= 2) {
       const double x = shuffle_up(sum, d);
-      if (l31 >= d) sum += x;
+      if (lane >= d) sum += x;
     }
     wave_lds_fence();  // (the last value head's readers are done)
-    if (h == 0) sums[l31] = sum, rates[l31] = beta;
+    sums[lane] = sum, rates[lane] = beta;
     wave_lds_fence();
-    const double last = sums[C - 1];
-    const float early = (float)exp(sum), late = (float)exp(last - sum), whole = (float)exp(last);
-    auto* const data = (DeltaChunkData<BF16>*)data_ + head * chunks + chunk;
+    auto* const forward = (Forward*)forward_ + head * blocks + block;
+    auto* const backward = (DeltaBackward*)backward_ + head * blocks + block;
+    if (part == 0) {
+      const double last = sums[kDeltaBlock - 1];
+      const float early = (float)exp(sum), late = (float)exp(last - sum), whole = (float)exp(last);
+      forward->early[lane] = early, forward->late[lane] = late * beta;
+      if (lane == 0) forward->whole[0] = whole;
+      if constexpr (BACK) {
+        backward->early[lane] = early, backward->late[lane] = late, backward->beta[lane] = beta;
+        if (lane == 0) backward->whole[0] = whole;
+      }
+    }
+    const double my_sum = sums[i0 + l31];
+    const float my_rate = rates[i0 + l31];
     float w[16], r[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const int j = result_row(i, h);
-      const float d = exp2_fast((float)((sum - sums[j]) * 1.4426950408889634));
-      w[i] = j < l31 ? d * kk[i] : 0.f;                 // L
-      r[i] = j <= l31 ? d * qk[i] * a.scale : 0.f;
+      const float d = exp2_fast((float)((my_sum - sums[j0 + j]) * 1.4426950408889634));
+      const bool across = part == 2;
+      w[i] = across || j < l31 ? d * kk[i] : 0.f;
+      r[i] = across || j <= l31 ? d * qk[i] * a.scale : 0.f;
     }
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const int j = result_row(i, h);
-      A[l31 * kPitch + j] = w[i] * rates[j];
-      W[l31 * kPitch + j] = j <= l31 ? r[i] * rates[j] : 0.f;
+      const float beta_j = rates[j0 + j];
+      A[l31 * kPitch + j] = part == 2 || j < l31 ? w[i] * beta_j : 0.f;
+      W[l31 * kPitch + j] = part == 2 || j <= l31 ? r[i] * beta_j : 0.f;
     }
     wave_lds_fence();
-    put_operand<DeltaChunkData<BF16>::kPair, false>(W, data->pairs);
-    wave_lds_fence();
-    invert(A, X, W);
-    put_operand<3, false>(X, data->inverse);
-    if (h == 0) data->early[l31] = early, data->late[l31] = late * beta;
-    if (lane == 0) data->whole[0] = whole;
+    const int which = part == 0 ? 0 : part == 1 ? 2 : 1;
+    put_operand<Forward::kPair, false>(W, forward->pairs[which]);
+    if (part == 2) {
+      put_operand<3, false>(A, forward->below);
+    } else {
+      wave_lds_fence();
+      invert(A, X, W);
+      put_operand<3, false>(X, forward->inverse[part]);
+    }
     if constexpr (BACK) {
-      auto* const back = (DeltaChunkBack<BF16>*)back_ + head * chunks + chunk;
       wave_lds_fence();
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const int j = result_row(i, h);
-        A[l31 * kPitch + j] = w[i] * beta;
+        A[l31 * kPitch + j] = part == 2 || j < l31 ? w[i] * my_rate : 0.f;
         W[l31 * kPitch + j] = r[i];
       }
       wave_lds_fence();
-      put_operand<3, true>(W, back->pairs);
-      wave_lds_fence();
-      invert(A, X, W);
-      put_operand<3, true>(X, back->inverse);
-      if (h == 0) back->early[l31] = early, back->late[l31] = late, back->beta[l31] = beta;
-      if (lane == 0) back->whole[0] = whole;
+      put_operand<3, true>(W, backward->pairs[which]);
+      if (part == 2) {
+        put_operand<3, true>(A, backward->below);
+      } else {
+        wave_lds_fence();
+        invert(A, X, W);
+        put_operand<3, true>(X, backward->inverse[part]);
+      }
     }
   }
 }
 
 template <typename T, bool BACK>
-hipError_t launch(const DeltaArgs& a, void* data, void* back, hipStream_t s) {
-  const dim3 grid((a.n + C - 1) / C, a.heads / a.G);
+hipError_t launch(const DeltaArgs& a, void* forward, void* backward, hipStream_t s) {
+  const dim3 grid((a.n + kDeltaBlock - 1) / kDeltaBlock * 3, a.heads / a.G);
   switch ((a.dk + 31) / 32) {
-    case 1: hipLaunchKernelGGL((delta_pairs_kernel<T, 1, BACK>), grid, dim3(64), 0, s, a, data, back); break;
-    case 2: hipLaunchKernelGGL((delta_pairs_kernel<T, 2, BACK>), grid, dim3(64), 0, s, a, data, back); break;
-    case 3: hipLaunchKernelGGL((delta_pairs_kernel<T, 3, BACK>), grid, dim3(64), 0, s, a, data, back); break;
-    default: hipLaunchKernelGGL((delta_pairs_kernel<T, 4, BACK>), grid, dim3(64), 0, s, a, data, back); break;
+    case 1: hipLaunchKernelGGL((delta_pairs_kernel<T, 1, BACK>), grid, dim3(64), 0, s, a, forward, backward); break;
+    case 2: hipLaunchKernelGGL((delta_pairs_kernel<T, 2, BACK>), grid, dim3(64), 0, s, a, forward, backward); break;
+    case 3: hipLaunchKernelGGL((delta_pairs_kernel<T, 3, BACK>), grid, dim3(64), 0, s, a, forward, backward); break;
+    default: hipLaunchKernelGGL((delta_pairs_kernel<T, 4, BACK>), grid, dim3(64), 0, s, a, forward, backward); break;
   }
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_delta_pairs(const DeltaArgs& a, bool bf16, void* data, void* back, hipStream_t s) {
-  if (back) return bf16 ? launch<u16, true>(a, data, back, s) : launch<float, true>(a, data, back, s);
-  return bf16 ? launch<u16, false>(a, data, back, s) : launch<float, false>(a, data, back, s);
+hipError_t launch_delta_pairs(const DeltaArgs& a, bool bf16, void* forward, void* backward, hipStream_t s) {
+  if (backward) return bf16 ? launch<u16, true>(a, forward, backward, s) : launch<float, true>(a, forward, backward, s);
+  return bf16 ? launch<u16, false>(a, forward, backward, s) : launch<float, false>(a, forward, backward, s);
 }
 
-size_t delta_data_bytes(bool bf16, int heads, int n) {
-  const size_t chunks = (size_t)heads * ((n + C - 1) / C);
-  return chunks * (bf16 ? sizeof(DeltaChunkData<true>) : sizeof(DeltaChunkData<false>));
+size_t delta_forward_bytes(bool bf16, int heads, int n) {
+  const size_t blocks = (size_t)heads * ((n + kDeltaBlock - 1) / kDeltaBlock);
+  return blocks * (bf16 ? sizeof(DeltaForward<true>) : sizeof(DeltaForward<false>));
 }
 
 }  // namespace sata

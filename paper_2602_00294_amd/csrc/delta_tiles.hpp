@@ -1,11 +1,13 @@
-// What the delta rule's kernels share: 16 x 16 products over 32 entries, and what a chunk's pairs leave for the scans.
+// What the delta rule's kernels share: 16 x 16 products over 32 entries, and what the pairs of a block's tokens leave for
+// the scans.
 //
-// With G_i the sum of a chunk's log decays up to token i, S the state before the chunk and E the errors
-// e_i - k_i S' of its tokens (u = beta E),
-//     L_ij = exp(G_i - G_j) k_i.k_j (j < i),   E = (I + L beta)^-1 (v - exp(G) k S),
-//     y    = c exp(G) q S + P E,  P_ij = c exp(G_i - G_j) q_i.k_j beta_j (j <= i),
+// A block is 64 tokens, two halves of 32.  With G_i the sum of its log decays up to token i, S the state before it and
+// E_i = v_i - k_i S' the errors of its tokens (u = beta E),
+//     L_ij = exp(G_i - G_j) beta_j k_i.k_j (j < i),   E = (I + L)^-1 (v - exp(G) k S): half by half,
+//     E_1  = (I + L_11)^-1 (v_1 - exp(G) k_1 S),      E_2 = (I + L_22)^-1 (v_2 - exp(G) k_2 S - L_21 E_1),
+//     y    = c exp(G) q S + P E,  P_ij = c exp(G_i - G_j) beta_j q_i.k_j (j <= i),
 //     S    = exp(G_C) S + sum_j exp(G_C - G_j) beta_j k_j (x) E_j,
-// so that a chunk's tokens need one triangular inverse and products.  Differences of sums of logarithms are at
+// so that a block's tokens need triangular inverses of 32 x 32 and products.  Differences of sums of logarithms are at
 // most 0: no factor overflows, however strong the decay.
 //
 // Products are v_mfma_f32_16x16x32_bf16.  Lane l (l15 = l % 16, t4 = l / 16) holds row (left operand) or column
@@ -23,8 +25,7 @@
 
 namespace sata {
 
-constexpr int kDeltaChunk = 32;
-constexpr int kDeltaBlock = 64;  // tokens between the states that a gradient keeps
+constexpr int kDeltaBlock = 64;
 
 __device__ __forceinline__ f32x4 zero4() { return f32x4{0.f, 0.f, 0.f, 0.f}; }
 
@@ -39,13 +40,29 @@ __device__ __forceinline__ f32x4 dot_planes16(const uint4 (&a)[NA], const uint4 
   return c;
 }
 
-// eight values as an operand
+// Eight values as an operand of PL bfloat16 numbers each; x becomes what they leave out.  What two numbers leave out is
+// one v_dot2_f32_bf16 each, x - (first, 0) or - (0, second): exact, and it takes the place of unpacking and subtracting.
+// (An infinity makes NaN of its neighbour too.  The factors lie in registers: as an inline constant the first
+// would be multiplied with both numbers.)
 template <int PL>
 __device__ __forceinline__ void operand_of(float (&x)[8], uint4 (&op)[PL]) {
-  uint4 w[1][PL];
-  to_planes<PL>(x, w);
+  uint32_t first = 0x0000bf80u, second = 0xbf800000u;
+  asm("" : "+s"(first), "+s"(second));
+  typedef __bf16 pair __attribute__((ext_vector_type(2)));
 #pragma unroll
-  for (int p = 0; p < PL; ++p) op[p] = w[0][p];
+  for (int p = 0; p < PL; ++p) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      w[i] = pack2(x[2 * i], x[2 * i + 1]);
+      if (p + 1 < PL) {
+        const pair v = __builtin_bit_cast(pair, w[i]);
+        x[2 * i] = __builtin_amdgcn_fdot2_f32_bf16(v, __builtin_bit_cast(pair, first), x[2 * i], false);
+        x[2 * i + 1] = __builtin_amdgcn_fdot2_f32_bf16(v, __builtin_bit_cast(pair, second), x[2 * i + 1], false);
+      }
+    }
+    op[p] = uint4{w[0], w[1], w[2], w[3]};
+  }
 }
 template <int PL>
 __device__ __forceinline__ void operand_of(const f32x4& a, const f32x4& b, uint4 (&op)[PL]) {
@@ -86,26 +103,27 @@ __device__ __forceinline__ void columns16(const u16* t, int r0, int j, uint4 (&o
   for (int i = 0; i < L::kPl; ++i) op[i] = read_transposed(a + i * L::kPlane, (int)(b - a));
 }
 
-// What the pairs of a chunk leave, in the order in which lanes load it: operands [number][16 rows][lane].
+// What the pairs of a block leave, in the order in which lanes load it: operands [number][16 rows][lane] of 32 rows.
+typedef uint4 DeltaOperand[2][64];
 template <bool BF16>
-struct DeltaChunkData {
-  static constexpr int kInverse = 3;            // numbers of an inverse's entry
-  static constexpr int kPair = BF16 ? 2 : 3;    // of a pair's weight in the outputs
-  uint4 inverse[kInverse][2][64];               // (I + L beta)^-1, rows i
-  uint4 pairs[kPair][2][64];                    // P, rows i
-  float early[32], late[32];                    // exp(G_i), beta_j exp(G_C - G_j)
-  float whole[4];                               // exp(G_C)
+struct DeltaForward {
+  static constexpr int kPair = BF16 ? 2 : 3;  // numbers of a pair's weight in the outputs
+  DeltaOperand inverse[2][3];                 // (I + L_11)^-1, (I + L_22)^-1, rows i
+  DeltaOperand below[3];                      // L_21, rows i
+  DeltaOperand pairs[3][kPair];               // P_11, P_21, P_22, rows i
+  float early[kDeltaBlock], late[kDeltaBlock];  // exp(G_i), beta_j exp(G_C - G_j)
+  float whole[4];                             // exp(G_C)
 };
-// The same for gradients; `pairs` stays without use.
-template <bool BF16>
-struct DeltaChunkBack {
-  uint4 inverse[3][2][64];  // (I + beta L)^-1 transposed, rows j
-  uint4 pairs[3][2][64];    // c exp(G_i - G_j) q_i.k_j transposed, rows j
-  float early[32], late[32], beta[32];  // exp(G_i), exp(G_C - G_j)
+// For gradients, transposed: beta belongs to the other side there, M_ij = exp(G_i - G_j) beta_i k_i.k_j.
+struct DeltaBackward {
+  DeltaOperand inverse[2][3];  // (I + M_11)^-T, (I + M_22)^-T, rows j
+  DeltaOperand below[3];       // M_21^T, rows j
+  DeltaOperand pairs[3][3];    // P_11^T, P_21^T, P_22^T without beta, rows j
+  float early[kDeltaBlock], late[kDeltaBlock], beta[kDeltaBlock];  // exp(G_i), exp(G_C - G_j)
   float whole[4];
 };
 
-// The records of a head's chunks on their way into LDS.  (Loads have no branches: behind a branch the compiler waits for
+// The records of a head's blocks on their way into LDS.  (Loads have no branches: behind a branch the compiler waits for
 // all that are on their way.)
 template <typename D, int THREADS>
 struct DataStage {
@@ -129,14 +147,14 @@ struct DataStage {
   }
 };
 
-// One column of a head's [rows][pitch] entries, a lane its own: entries of rows t0 + 16 x + 4 t4 .. +3 (x = 0, 1), zero behind
+// One column of a head's [rows][width] entries, a lane its own: entries of rows t0 + 16 x + 4 t4 .. +3 (x = 0 .. 3), zero behind
 // the last row and where the lane has no column.  Stores there are dropped.
 template <typename T>
 struct ColumnStage {
   __amdgpu_buffer_rsrc_t rsrc;
   uint32_t off, pitch;
   int left;  // columns from this lane's on
-  uint32_t r[8];
+  uint32_t r[16];
   __device__ __forceinline__ void init(const T* head, int rows, int width, int col) {
     rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(head), 0, rows * width * (int)sizeof(T), 0x00020000);
     pitch = (uint32_t)(width * (int)sizeof(T));
@@ -148,7 +166,7 @@ struct ColumnStage {
     const uint32_t place = off + (uint32_t)(t0 + 16 * (e >> 2) + (e & 3)) * pitch + (uint32_t)(ahead * (int)sizeof(T));
     return ahead < left ? place : kNoVector;
   }
-  template <int COUNT = 8>
+  template <int COUNT = 16>
   __device__ __forceinline__ void fetch(int t0, int ahead = 0) {
 #pragma unroll
     for (int e = 0; e < COUNT; ++e) {
@@ -177,9 +195,10 @@ __device__ __forceinline__ bool delta_place(int heads, int slices, int& head, in
 }
 inline unsigned delta_grid(int heads, int slices) { return (unsigned)((heads >= 8 ? (heads + 7) / 8 * 8 : heads) * slices); }
 
-hipError_t launch_delta_pairs(const DeltaArgs& a, bool bf16, void* data, void* back, hipStream_t s);
+// Records [head][block] of DeltaForward and, where `backward`, DeltaBackward.
+hipError_t launch_delta_pairs(const DeltaArgs& a, bool bf16, void* forward, void* backward, hipStream_t s);
+size_t delta_forward_bytes(bool bf16, int heads, int n);
 // The states before every block and the errors E of a call's tokens: what gradients start from.
-hipError_t launch_delta_states(const DeltaArgs& a, bool bf16, const void* data, float* states, float* errors, hipStream_t s);
-size_t delta_data_bytes(bool bf16, int heads, int n);
+hipError_t launch_delta_states(const DeltaArgs& a, bool bf16, const void* forward, float* states, float* errors, hipStream_t s);
 
 }  // namespace sata
