@@ -23,83 +23,90 @@ namespace {
 constexpr int kBlock = kDeltaBlock;
 constexpr int kBackWaves = 4, kBackThreads = 64 * kBackWaves;
 
-// ---- from the last token back: a wave has 16 columns of U, as the forward scan of S
+// ---- from the last token back: a wave has 16 columns of U, as the forward scan of S, and four more bring blocks into LDS
+constexpr int kBackScanThreads = 2 * kBackThreads;
 template <typename T, int ND>
 struct BackLds {
-  using L = PairTile<T, ND, kBlock>;
+  using L = DeltaTile<T, ND, kBlock>;
+  using Y = SliceStage<T, kBackThreads>;
   static constexpr int kBuffers = sizeof(T) == 2 ? 2 : 1;
-  static constexpr int kBuffer = 2 * L::kBytes + (int)sizeof(DeltaBackward);
+  static constexpr int kBuffer = 2 * L::kBytes + (int)sizeof(DeltaBackward) + Y::kBytes;
   static constexpr int kBytes = kBuffers * kBuffer;
-  static_assert(kBytes <= 160 * 1024, "LDS of one workgroup");
+  static_assert(kBytes <= 160 * 1024 && kBuffer % 16 == 0, "LDS of one workgroup");
 };
 
 template <typename T, int ND>
-__global__ void __launch_bounds__(kBackThreads, 1) delta_back_kernel(DeltaArgs a, const void* data_, float* behind, float* zs, int slices) {
+__global__ void __launch_bounds__(kBackScanThreads, 2) delta_back_kernel(DeltaArgs a, const void* data_, float* behind, float* zs, int slices) {
   extern __shared__ __attribute__((aligned(16))) u16 smem16[];
   using D = BackLds<T, ND>;
   using L = typename D::L;
   using Data = DeltaBackward;
+  using Y = typename D::Y;
   int head, slice;
   if (!delta_place(a.heads, slices, head, slice)) return;
   const int tid = threadIdx.x, lane = tid & 63, l15 = lane & 15, t4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t shared = head / a.G;
   const int len = tokens_of(a.lengths, head / (a.Hk * a.G), a.n), blocks = (len + kBlock - 1) / kBlock;
-  const int col = 16 * (kBackWaves * slice + wave) + l15;
-  const bool on = col < a.dv;
-  const int64_t size = (int64_t)a.dk * a.dv;
-  f32x4 U[2 * ND];
-#pragma unroll
-  for (int j = 0; j < 2 * ND; ++j)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int row = 16 * j + 4 * t4 + i;
-      U[j][i] = a.dS && on && row < a.dk ? a.dS[head * size + (int64_t)row * a.dv + col] : 0.f;
-    }
-  auto put_state = [&](float* to) {
-#pragma unroll
-    for (int j = 0; j < 2 * ND; ++j)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int row = 16 * j + 4 * t4 + i;
-        if (on && row < a.dk) to[(int64_t)row * a.dv + col] = U[j][i];
-      }
-  };
-  const int64_t all_blocks = (a.n + kBlock - 1) / kBlock;
-  if (blocks > 0) {
-    TileStage<T, ND, kBlock, kBackThreads> sq, sk;
-    sq.init((const T*)a.q + shared * a.n * a.dk, len, a.dk, tid);
-    sk.init((const T*)a.k + shared * a.n * a.dk, len, a.dk, tid);
+  const int64_t all_blocks = (a.n + kBlock - 1) / kBlock, head0 = (int64_t)head * a.n * a.dv;
+  auto buffer = [&](int c) { return smem16 + (D::kBuffers == 2 && (c & 1) ? D::kBuffer / 2 : 0); };
+  if (wave >= kBackWaves) {  // ---- the next block into LDS
+    const int id = tid - kBackThreads;
+    DeltaStage<T, ND, kBlock, kBackThreads> sq, sk;
     DataStage<Data, kBackThreads> sd;
-    ColumnStage<T> sy, sv;
-    ColumnStage<float> sz;
-    const int64_t head0 = (int64_t)head * a.n * a.dv;
-    sd.init((const Data*)data_ + head * all_blocks, blocks, tid);
-    sy.init((const T*)a.dy + head0, len, a.dv, col);
-    sv.init((const T*)a.dv_out + head0, len, a.dv, col);
-    sz.init(zs + head0, len, a.dv, col);
+    Y sy;
+    sq.init((const T*)a.q + shared * a.n * a.dk, len, a.dk, id);
+    sk.init((const T*)a.k + shared * a.n * a.dk, len, a.dk, id);
+    sd.init((const Data*)data_ + head * all_blocks, blocks, id);
+    sy.init((const T*)a.dy + head0, len, a.dv, 64 * slice, id);
     auto fetch = [&](int c) {
       sk.fetch(c * kBlock);
       sq.fetch(c * kBlock);
       sd.fetch(c);
       sy.fetch(c * kBlock);
     };
-    fetch(blocks - 1);
+    if (blocks > 0) fetch(blocks - 1);
+    for (int c = blocks - 1; c >= 0; --c) {
+      u16* const tk = buffer(c);
+      if (D::kBuffers == 1 && c + 1 < blocks) __syncthreads();  // (the block behind has been read)
+      sk.put(tk, c * kBlock);
+      sq.put(tk + L::kElems, c * kBlock);
+      sd.put((Data*)(tk + 2 * L::kElems));
+      sy.put((T*)((Data*)(tk + 2 * L::kElems) + 1), c * kBlock);
+      __syncthreads();
+      if (c > 0) fetch(c - 1);
+    }
+    return;
+  }
+  const int col = 16 * (kBackWaves * slice + wave) + l15;
+  const bool on = col < a.dv;
+  const int64_t size = (int64_t)a.dk * a.dv;
+  f32x4 U[2 * ND];
+#pragma unroll
+  for (int j = 0; j < 2 * ND; ++j) U[j] = zero4();
+  StateColumns state;
+  if (a.dS) {
+    state.init(a.dS + head * size, a.dk, a.dv, col);
+    state.load(U);
+  }
+  {
+    ColumnStage<T> sv;
+    ColumnStage<float> sz;
+    sv.init((const T*)a.dv_out + head0, len, a.dv, col);
+    sz.init(zs + head0, len, a.dv, col);
     for (int c = blocks - 1; c >= 0; --c) {
       const int t0 = c * kBlock;
-      u16* const tk = smem16 + (D::kBuffers == 2 && (c & 1) ? D::kBuffer / 2 : 0);
-      u16* const tq = tk + L::kElems;
-      Data& d = *(Data*)(tq + L::kElems);
-      if (D::kBuffers == 1) __syncthreads();
-      sk.put(tk, t0);
-      sq.put(tq, t0);
-      sd.put(&d);
+      const u16* const tk = buffer(c);
+      const u16* const tq = tk + L::kElems;
+      const Data& d = *(const Data*)(tq + L::kElems);
+      if (D::kBuffers == 1 && c + 1 < blocks) __syncthreads();
       __syncthreads();
+      const T* const ys = (const T*)(&d + 1) + 16 * wave + l15;
       float y[16];
 #pragma unroll
-      for (int e = 0; e < 16; ++e) y[e] = sy.value(e);
-      if (c > 0) fetch(c - 1);
-      put_state(behind + (head * all_blocks + c) * size);
+      for (int e = 0; e < 16; ++e) y[e] = entry_of(ys, (16 * (e >> 2) + 4 * t4 + (e & 3)) * Y::kPitch);
+      state.init(behind + (head * all_blocks + c) * size, a.dk, a.dv, col);
+      state.store(U);
       auto operand = [&](const DeltaOperand* p, int x, uint4 (&op)[3]) {
 #pragma unroll
         for (int i = 0; i < 3; ++i) op[i] = p[i][x][lane];
@@ -112,19 +119,14 @@ __global__ void __launch_bounds__(kBackThreads, 1) delta_back_kernel(DeltaArgs a
         beta[x] = *(const f32x4*)(d.beta + 16 * x + 4 * t4);
       }
       const float whole = d.whole[0];
-      uint4 st[ND][3];
+      f32x4 R[4] = {zero4(), zero4(), zero4(), zero4()}, z[4];
 #pragma unroll
-      for (int b = 0; b < ND; ++b) operand_of<3>(U[2 * b], U[2 * b + 1], st[b]);
-      f32x4 R[4], z[4];
+      for (int b = 0; b < ND; ++b) {
+        uint4 st[3], e[4][L::kPl];
+        operand_of<3>(U[2 * b], U[2 * b + 1], st);
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        R[x] = zero4();
-#pragma unroll
-        for (int b = 0; b < ND; ++b) {
-          uint4 e[L::kPl];
-          rows16_as_results<L>(tk, 16 * x, b, e);
-          R[x] = dot_planes16(e, st[b], R[x]);
-        }
+        for (int x = 0; x < 4; ++x) rows16<L>(tk, 16 * x, b, e[x]);
+        dots_left16(e, st, R);
       }
       uint4 yp[2][L::kPl], ep[2][3], zp[3], wp[2][3];
 #pragma unroll
@@ -138,37 +140,48 @@ __global__ void __launch_bounds__(kBackThreads, 1) delta_back_kernel(DeltaArgs a
         operand_of<L::kPl>(x8, yp[h]);
         operand_of<3>(e8, ep[h]);
       }
+#pragma unroll
+      for (int j = 0; j < 2 * ND; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) U[j][i] *= whole;
       // the second half first: the first one's updates are seen by its keys
 #pragma unroll
       for (int h = 1; h >= 0; --h) {
-        f32x4 du[2];
+        f32x4 du[2] = {zero4(), zero4()};
+        uint4 p[2][3];
+        auto load = [&](const DeltaOperand* from) {
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          uint4 p[3];
-          operand(d.pairs[2 * h], x, p);
-          du[x] = dot_planes16(p, yp[h], zero4());
-          if (h == 0) {
-            operand(d.pairs[1], x, p);
-            du[x] = dot_planes16(p, yp[1], du[x]);
-          }
+          for (int x = 0; x < 2; ++x) operand(from, x, p[x]);
+        };
+        if (h == 0) {
+          load(d.below);
+          dots_left16(p, zp, du);
+#pragma unroll
+          for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) du[x][i] = -du[x][i];
+          load(d.pairs[1]);
+          dots_left16(p, yp[1], du);
+        }
+        load(d.pairs[2 * h]);
+        dots_left16(p, yp[h], du);
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
 #pragma unroll
           for (int i = 0; i < 4; ++i) du[x][i] = fmaf(late[2 * h + x][i], R[2 * h + x][i], du[x][i]);
-          if (h == 0) {
-            operand(d.below, x, p);
-            const f32x4 m = dot_planes16(p, zp, zero4());
-#pragma unroll
-            for (int i = 0; i < 4; ++i) du[x][i] -= m[i];
-          }
-        }
         uint4 dp[3];
         operand_of<3>(du[0], du[1], dp);
+        load(d.inverse[h]);
+        f32x4 w[2] = {zero4(), zero4()};
+        dots_left16(p, dp, w);
+        {  // (between the products that wait for each other)
+          uint4 e[2 * ND][L::kPl];
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          uint4 p[3];
-          operand(d.inverse[h], x, p);
-          z[2 * h + x] = dot_planes16(p, dp, zero4());
+          for (int j = 0; j < 2 * ND; ++j) state_columns16<L>(tq, 32 * h, j, e[j]);
+          dots_left16(e, ep[h], U);
         }
-        if (h == 1) operand_of<3>(z[2], z[3], zp);
+        z[2 * h] = w[0], z[2 * h + 1] = w[1];
+        if (h == 1) operand_of<3>(w[0], w[1], zp);
       }
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -184,22 +197,19 @@ __global__ void __launch_bounds__(kBackThreads, 1) delta_back_kernel(DeltaArgs a
         operand_of<3>(w, wp[h]);
       }
 #pragma unroll
-      for (int j = 0; j < 2 * ND; ++j) {
+      for (int h = 0; h < 2; ++h) {
+        uint4 e[2 * ND][L::kPl];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) U[j][i] *= whole;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint4 e[L::kPl];
-          columns16<L>(tq, 32 * h, j, e);
-          U[j] = dot_planes16(e, ep[h], U[j]);
-          columns16<L>(tk, 32 * h, j, e);
-          U[j] = dot_planes16(e, wp[h], U[j]);
-        }
+        for (int j = 0; j < 2 * ND; ++j) state_columns16<L>(tk, 32 * h, j, e[j]);
+        dots_left16(e, wp[h], U);
       }
       settle_mfma();
     }
   }
-  if (a.dS_in) put_state(a.dS_in + head * size);
+  if (a.dS_in) {
+    state.init(a.dS_in + head * size, a.dk, a.dv, col);
+    state.store(U);
+  }
   if (on) {
     T* const dv = (T*)a.dv_out + (int64_t)head * a.n * a.dv + col;
     for (int t = len + t4; t < a.n; t += 4) dv[(int64_t)t * a.dv] = (T)0;
@@ -213,9 +223,9 @@ __global__ void __launch_bounds__(kBackThreads, 1) delta_back_kernel(DeltaArgs a
 // weight is formed in both places, once for each side's rows, so that it is an operand where it is formed.
 template <typename T, int ND>
 struct BlockLds {
-  using W = PairTile<float, ND, kBlock>;  // errors, z, or gradients of the outputs; rows of a state
-  using L = PairTile<T, ND, kBlock>;      // queries or keys
-  using Half = PairTile<float, ND, 32>;
+  using W = DeltaTile<float, ND, kBlock>;  // errors, z, or gradients of the outputs; rows of a state
+  using L = DeltaTile<T, ND, kBlock>;      // queries or keys
+  using Half = DeltaTile<float, ND, 32>;
   static constexpr int kBytes = W::kBytes + L::kBytes;
 };
 
@@ -325,7 +335,7 @@ delta_blocks_kernel(DeltaArgs a, const float* states, const float* behind, const
   ck.init(k, len, a.dk, l15);
   gq.init((T*)a.dq + row0 * a.dk, len, a.dk, l15);
   gk.init((T*)a.dk_out + row0 * a.dk, len, a.dk, l15);
-  TileStage<T, ND, kBlock, kBackThreads> sb;
+  DeltaStage<T, ND, kBlock, kBackThreads> sb;
   auto fetch_keys = [&](const T* x) {
     sb.init(x, len, a.dk, tid);
     sb.fetch(t0);
@@ -340,7 +350,7 @@ delta_blocks_kernel(DeltaArgs a, const float* states, const float* behind, const
     const T* const dy = (const T*)a.dy + row * a.dv;
     const float* const S = states + (head * blocks + block) * size;
     const float* const U = behind + (head * blocks + block) * size;
-    TileStage<float, ND, kBlock, kBackThreads> sa;
+    DeltaStage<float, ND, kBlock, kBackThreads> sa;
     sa.init(E, len, a.dv, tid);
     sa.fetch(t0);
     fetch_keys(k);
@@ -410,7 +420,7 @@ delta_blocks_kernel(DeltaArgs a, const float* states, const float* behind, const
       float early[4];
 #pragma unroll
       for (int r = 0; r < 4; ++r) early[r] = decay(sums[own + 4 * t4 + r]);
-      TileStage<float, ND, 32, kBackThreads> ss;
+      DeltaStage<float, ND, 32, kBackThreads> ss;
       ss.init(S, a.dk, a.dv, tid);
       ss.fetch(0);
 #pragma unroll
@@ -458,7 +468,7 @@ delta_blocks_kernel(DeltaArgs a, const float* states, const float* behind, const
     // ---- pairs of tokens i with this wave's j <= i: columns of one, then of two
     uint4 e_own[ND][3];
     {
-      TileStage<T, ND, kBlock, kBackThreads> sy;
+      DeltaStage<T, ND, kBlock, kBackThreads> sy;
       sy.init(dy, len, a.dv, tid);
       sy.fetch(t0);
       fetch_keys(q);
@@ -541,7 +551,7 @@ delta_blocks_kernel(DeltaArgs a, const float* states, const float* behind, const
       float late[4];
 #pragma unroll
       for (int r = 0; r < 4; ++r) late[r] = decay(end - sums[own + 4 * t4 + r]) * rate[r];
-      TileStage<float, ND, 32, kBackThreads> ss, su;
+      DeltaStage<float, ND, 32, kBackThreads> ss, su;
       ss.init(S, a.dk, a.dv, tid);
       su.init(U, a.dk, a.dv, tid);
       su.fetch(0);
@@ -654,7 +664,7 @@ hipError_t launch_back(const DeltaArgs& a, const void* data, float* behind, floa
   hipError_t e = raise_lds(kern, bytes);
   if (e != hipSuccess) return e;
   const int slices = (a.dv + 16 * kBackWaves - 1) / (16 * kBackWaves);
-  hipLaunchKernelGGL(kern, dim3(delta_grid(a.heads, slices)), dim3(kBackThreads), bytes, s, a, data, behind, zs, slices);
+  hipLaunchKernelGGL(kern, dim3(delta_grid(a.heads, slices)), dim3(kBackScanThreads), bytes, s, a, data, behind, zs, slices);
   return hipGetLastError();
 }
 

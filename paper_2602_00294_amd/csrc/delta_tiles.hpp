@@ -29,6 +29,21 @@ constexpr int kDeltaBlock = 64;
 
 __device__ __forceinline__ f32x4 zero4() { return f32x4{0.f, 0.f, 0.f, 0.f}; }
 
+// Rows in LDS as PairTile has them, with the 16-byte units of a row in places of their own: here 32 lanes read 16 rows of
+// one unit or, transposed, 8 rows of two neighbouring ones, and each meets every bank once.
+template <typename T, int ND, int ROWS>
+struct DeltaTile : PairTile<T, ND, ROWS> {
+  using P = PairTile<T, ND, ROWS>;
+  __device__ static __forceinline__ int swap(int row) {
+    if constexpr (P::kUnits == 16) return ((row & 7) << 1) | ((row >> 3) & 1);
+    else if constexpr (P::kUnits == 8) return (((row >> 1) & 3) << 1) | ((row >> 3) & 1);
+    else return (((row >> 2) & 1) << 1) | ((row >> 3) & 1);
+  }
+  __device__ static __forceinline__ int at(int row, int col) { return row * P::kRow + 8 * ((col >> 3) ^ swap(row)) + (col & 7); }
+};
+template <typename T, int ND, int ROWS, int THREADS>
+using DeltaStage = TileStage<T, ND, ROWS, THREADS, DeltaTile<T, ND, ROWS>>;
+
 // sum of the products a[i] b[j] with i + j <= MAX, smallest first
 template <int MAX = 2, int NA, int NB>
 __device__ __forceinline__ f32x4 dot_planes16(const uint4 (&a)[NA], const uint4 (&b)[NB], f32x4 c) {
@@ -38,6 +53,28 @@ __device__ __forceinline__ f32x4 dot_planes16(const uint4 (&a)[NA], const uint4 
     for (int i = 0; i <= t; ++i)
       if (i < NA && t - i < NB) c = mfma_bf16(a[i], b[t - i], c);
   return c;
+}
+
+// The same for N results at once, product by product: a result's own products wait for each other.
+template <int MAX = 2, int N, int NA, int NB>
+__device__ __forceinline__ void dots_left16(const uint4 (&a)[N][NA], const uint4 (&b)[NB], f32x4 (&c)[N]) {
+#pragma unroll
+  for (int t = MAX; t >= 0; --t)
+#pragma unroll
+    for (int i = 0; i <= t; ++i)
+      if (i < NA && t - i < NB)
+#pragma unroll
+        for (int x = 0; x < N; ++x) c[x] = mfma_bf16(a[x][i], b[t - i], c[x]);
+}
+template <int MAX = 2, int N, int NA, int NB>
+__device__ __forceinline__ void dots_right16(const uint4 (&a)[NA], const uint4 (&b)[N][NB], f32x4 (&c)[N]) {
+#pragma unroll
+  for (int t = MAX; t >= 0; --t)
+#pragma unroll
+    for (int i = 0; i <= t; ++i)
+      if (i < NA && t - i < NB)
+#pragma unroll
+        for (int x = 0; x < N; ++x) c[x] = mfma_bf16(a[i], b[x][t - i], c[x]);
 }
 
 // Eight values as an operand of PL bfloat16 numbers each; x becomes what they leave out.  What two numbers leave out is
@@ -70,8 +107,8 @@ __device__ __forceinline__ void operand_of(const f32x4& a, const f32x4& b, uint4
   operand_of<PL>(x, op);
 }
 
-// Operands out of a tile of rows (L: PairTile).
-// Rows r0 .. +15, entries 32 s .. +31 in their order.
+// Operands out of a tile of rows (L: DeltaTile).
+// Rows r0 .. +15, entries 32 s .. +31: lane t4 has entries 32 s + 8 t4 .. +7.
 template <typename L>
 __device__ __forceinline__ void rows16(const u16* t, int r0, int s, uint4 (&op)[L::kPl]) {
   const int lane = threadIdx.x & 63, row = r0 + (lane & 15), t4 = lane >> 4;
@@ -79,24 +116,24 @@ __device__ __forceinline__ void rows16(const u16* t, int r0, int s, uint4 (&op)[
 #pragma unroll
   for (int i = 0; i < L::kPl; ++i) op[i] = *(const uint4*)(p + i * L::kPlane);
 }
-// The same in the order of a result's rows.
-template <typename L>
-__device__ __forceinline__ void rows16_as_results(const u16* t, int r0, int s, uint4 (&op)[L::kPl]) {
-  const int lane = threadIdx.x & 63, row = r0 + (lane & 15), t4 = lane >> 4;
-  const u16* const p = t + row * L::kRow + 4 * (t4 & 1);
-  const u16* const a = p + 8 * ((4 * s + (t4 >> 1)) ^ L::swap(row));
-  const u16* const b = p + 8 * ((4 * s + 2 + (t4 >> 1)) ^ L::swap(row));
-#pragma unroll
-  for (int i = 0; i < L::kPl; ++i) {
-    const uint2 x = *(const uint2*)(a + i * L::kPlane), y = *(const uint2*)(b + i * L::kPlane);
-    op[i] = uint4{x.x, x.y, y.x, y.y};
-  }
-}
 // Columns 16 j .. +15 over rows r0 .. +31 in the order of a result's rows.
 template <typename L>
 __device__ __forceinline__ void columns16(const u16* t, int r0, int j, uint4 (&op)[L::kPl]) {
   const int lane = threadIdx.x & 63, l15 = lane & 15, t4 = lane >> 4;
   const int row = r0 + 4 * t4 + (l15 >> 2), unit = 2 * j + ((l15 & 3) >> 1), half = 4 * (l15 & 1);
+  const u16* const a = t + row * L::kRow + 8 * (unit ^ L::swap(row)) + half;
+  const u16* const b = t + (row + 16) * L::kRow + 8 * (unit ^ L::swap(row + 16)) + half;
+#pragma unroll
+  for (int i = 0; i < L::kPl; ++i) op[i] = read_transposed(a + i * L::kPlane, (int)(b - a));
+}
+// The scans' states have rows of their own order: row r of tile 2 b + x is entry 32 b + 8 (r / 4) + 4 x + r % 4 of a key, so that
+// two tiles' numbers contract with a key's entries in the order in which rows16 reads them.
+__device__ __forceinline__ int state_row(int j, int i, int t4) { return 32 * (j >> 1) + 8 * t4 + 4 * (j & 1) + i; }
+// The entries of tile j over rows r0 .. +31 in the order of a result's rows.
+template <typename L>
+__device__ __forceinline__ void state_columns16(const u16* t, int r0, int j, uint4 (&op)[L::kPl]) {
+  const int lane = threadIdx.x & 63, l15 = lane & 15, t4 = lane >> 4;
+  const int row = r0 + 4 * t4 + (l15 >> 2), unit = 4 * (j >> 1) + (l15 & 3), half = 4 * (j & 1);
   const u16* const a = t + row * L::kRow + 8 * (unit ^ L::swap(row)) + half;
   const u16* const b = t + (row + 16) * L::kRow + 8 * (unit ^ L::swap(row + 16)) + half;
 #pragma unroll
@@ -178,6 +215,75 @@ struct ColumnStage {
   __device__ __forceinline__ void store(int t0, int e, float x, int ahead = 0) const {
     if constexpr (sizeof(T) == 4) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(x), rsrc, (int)at(t0, e, ahead), 0, 0);
     else __builtin_amdgcn_raw_buffer_store_b16((unsigned short)(pack2(x, 0.f) & 0xffffu), rsrc, (int)at(t0, e, ahead), 0, 0);
+  }
+};
+
+// 64 rows of a slice of 64 columns of a head's [rows][width] entries on their way into LDS, as they are.
+template <typename T, int THREADS>
+struct SliceStage {
+  static constexpr int kPitch = 68;  // entries of a row in LDS: the four rows that a wave reads at once lie in other banks
+  static constexpr int kBytes = kDeltaBlock * kPitch * (int)sizeof(T);
+  static constexpr int kEV = 16 / (int)sizeof(T), kUnits = 64 / kEV, kIt = kDeltaBlock * kUnits / THREADS;
+  const T* base;
+  VectorReader read;
+  int rows, width, c0, tid;
+  bool vec;
+  uint32_t off, pitch;
+  uint4 r[kIt];
+  __device__ __forceinline__ void init(const T* head, int rows_, int width_, int c0_, int tid_) {
+    base = head, rows = rows_, width = width_, c0 = c0_, tid = tid_;
+    vec = width % kEV == 0 && ((uintptr_t)head & 15) == 0;
+    read = VectorReader(head, vec ? (int64_t)rows * width * (int)sizeof(T) : 0);
+    pitch = (uint32_t)(width * (int)sizeof(T));
+    const int col = c0 + tid % kUnits * kEV;
+    off = col < width ? (uint32_t)(tid / kUnits) * pitch + (uint32_t)(col * (int)sizeof(T)) : kNoVector;
+  }
+  __device__ __forceinline__ void fetch(int t0) {
+#pragma unroll
+    for (int i = 0; i < kIt; ++i) r[i] = read(off + (uint32_t)(t0 + i * (THREADS / kUnits)) * pitch);
+  }
+  __device__ __forceinline__ void put(T* t, int t0) const {
+    if (vec) {
+#pragma unroll
+      for (int i = 0; i < kIt; ++i) {
+        T* const p = t + (tid / kUnits + i * (THREADS / kUnits)) * kPitch + tid % kUnits * kEV;
+        *(uint2*)p = uint2{r[i].x, r[i].y};
+        *(uint2*)(p + kEV / 2) = uint2{r[i].z, r[i].w};
+      }
+    } else {
+      for (int i = tid; i < kDeltaBlock * 64; i += THREADS) {
+        const int row = i / 64, col = i % 64;
+        t[row * kPitch + col] = t0 + row < rows && c0 + col < width ? base[(int64_t)(t0 + row) * width + c0 + col] : (T)0;
+      }
+    }
+  }
+};
+
+// A state of [dk][dv] entries, its tiles j of a wave's 16 columns from memory and back.
+struct StateColumns {
+  __amdgpu_buffer_rsrc_t rsrc;
+  uint32_t off, pitch;
+  __device__ __forceinline__ void init(const float* state, int dk, int dv, int col) {
+    rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(state), 0, dk * dv * 4, 0x00020000);
+    pitch = (uint32_t)dv * 4u;
+    off = col < dv ? (uint32_t)col * 4u : kNoVector;
+  }
+  __device__ __forceinline__ int at(int j, int i) const {
+    return (int)(off + (uint32_t)state_row(j, i, (threadIdx.x & 63) >> 4) * pitch);
+  }
+  template <int N>
+  __device__ __forceinline__ void load(f32x4 (&S)[N]) const {
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) S[j][i] = __uint_as_float((uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rsrc, at(j, i), 0, 0));
+  }
+  template <int N>
+  __device__ __forceinline__ void store(const f32x4 (&S)[N]) const {
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(S[j][i]), rsrc, at(j, i), 0, 0);
   }
 };
 

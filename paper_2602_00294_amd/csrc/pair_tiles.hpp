@@ -230,9 +230,9 @@ __device__ __forceinline__ bool tile_not_finite(const u16* t, int r0) {
 // where rows allow them (width a multiple of a vector, base aligned), else entries.  Rows
 // at and behind `rows` and columns at and behind the width read as zero.  A thread has
 // one vector's place in a row, in every kPer-th row.
-template <typename T, int ND, int ROWS, int THREADS>
+template <typename T, int ND, int ROWS, int THREADS, typename TILE = PairTile<T, ND, ROWS>>
 struct TileStage {
-  using L = PairTile<T, ND, ROWS>;
+  using L = TILE;
   static constexpr int kEV = 16 / sizeof(T);
   static constexpr int kU = L::kRow / kEV;  // vectors in a row
   static constexpr int kPer = THREADS / kU;
