@@ -229,51 +229,6 @@ struct BlockLds {
   static constexpr int kBytes = W::kBytes + L::kBytes;
 };
 
-// Entries 32 s + 8 t4 .. +7 of a row in float32, zero behind `width`.
-__device__ __forceinline__ void load_eight(const float* p, int c0, bool ok, int width, bool vec, float (&x)[8]) {
-#pragma unroll
-  for (int h = 0; h < 8; h += 4) {
-    float4 w = {0.f, 0.f, 0.f, 0.f};
-    if (vec) {
-      if (ok && c0 + h < width) w = *(const float4*)(p + c0 + h);
-    } else if (ok) {
-      if (c0 + h < width) w.x = p[c0 + h];
-      if (c0 + h + 1 < width) w.y = p[c0 + h + 1];
-      if (c0 + h + 2 < width) w.z = p[c0 + h + 2];
-      if (c0 + h + 3 < width) w.w = p[c0 + h + 3];
-    }
-    x[h] = w.x, x[h + 1] = w.y, x[h + 2] = w.z, x[h + 3] = w.w;
-  }
-}
-// A row's entries 32 s + 8 t4 .. +7 as operands
-template <typename T, int ND>
-__device__ __forceinline__ void load_own16(const T* p, bool ok, int width, uint4 (&f)[ND][sizeof(T) == 4 ? 3 : 1]) {
-  constexpr int kEV = 16 / sizeof(T);
-  const int t4 = (threadIdx.x & 63) >> 4;
-  const bool vec = width % kEV == 0 && ((uintptr_t)p & 15) == 0;
-#pragma unroll
-  for (int s = 0; s < ND; ++s) {
-    const int c0 = 32 * s + 8 * t4;
-    if constexpr (sizeof(T) == 4) {
-      float x[8];
-      load_eight(p, c0, ok, width, vec, x);
-      operand_of<3>(x, f[s]);
-    } else {
-      uint4 w = {0u, 0u, 0u, 0u};
-      if (vec) {
-        if (ok && c0 < width) w = *(const uint4*)(p + c0);
-      } else if (ok) {
-        uint32_t u[4] = {0u, 0u, 0u, 0u};
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (c0 + j < width) u[j >> 1] |= (uint32_t)p[c0 + j] << (16 * (j & 1));
-        w = uint4{u[0], u[1], u[2], u[3]};
-      }
-      f[s][0] = w;
-    }
-  }
-}
-
 // Sums over the lanes up to (or from) a lane's own.
 __device__ __forceinline__ double sum_up_to(double x) {
   const int lane = threadIdx.x & 63;
@@ -296,10 +251,47 @@ __device__ __forceinline__ double sum_from(double x) {
   return x;
 }
 
-// MANY: several value heads to a query and key head, whose dq and dk are summed.
+// A lane's entry of a staged tile, of row r0 + 4 t4 + r and column 16 j + l15.
+template <typename L>
+__device__ __forceinline__ float tile_entry(const u16* t, int row, int col) {
+  const u16* const p = t + L::at(row, col);
+  float x = __uint_as_float((uint32_t)p[0] << 16);
+#pragma unroll
+  for (int i = 1; i < L::kPl; ++i) x += __uint_as_float((uint32_t)p[i * L::kPlane] << 16);
+  return x;
+}
+
+// A wave's results of 16 tokens by 32 ND columns, through LDS into rows: row(i, c0, x) for eight columns at a time.  `buf`: the wave's
+// own; 16 rows of 32 ND + 4 floats.  (Results lie by columns: of 16 tokens each lane would write two bytes at a time.)
+template <int ND, typename F>
+__device__ __forceinline__ void by_rows(const f32x4 (&x)[2 * ND], float* buf, F&& row) {
+  constexpr int kPitch = 32 * ND + 4, kLanes = ND == 1 ? 4 : ND == 2 ? 8 : 16;
+  const int lane = threadIdx.x & 63, l15 = lane & 15, t4 = lane >> 4;
+  wave_lds_fence();
+#pragma unroll
+  for (int j = 0; j < 2 * ND; ++j)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) buf[(4 * t4 + r) * kPitch + 16 * j + l15] = x[j][r];
+  wave_lds_fence();
+#pragma unroll
+  for (int i = 0; i < kLanes / 4; ++i) {
+    const int token = i * (64 / kLanes) + lane / kLanes, c0 = 8 * (lane % kLanes);
+    float y[8];
+#pragma unroll
+    for (int h = 0; h < 8; h += 4) {
+      const float4 f = c0 < 32 * ND ? *(const float4*)(buf + token * kPitch + c0 + h) : float4{0.f, 0.f, 0.f, 0.f};
+      y[h] = f.x, y[h + 1] = f.y, y[h + 2] = f.z, y[h + 3] = f.w;
+    }
+    row(token, c0, y);
+  }
+}
+template <int ND>
+constexpr int by_rows_lanes() { return ND == 1 ? 4 : ND == 2 ? 8 : 16; }
+
+// MANY: several value heads to a query and key head, whose dq and dk are summed (in `sums`, [2][query and key heads][n][dk]).
 template <typename T, int ND, bool MANY>
 __global__ void __launch_bounds__(kBackThreads, sizeof(T) == 2 ? 2 : 1)
-delta_blocks_kernel(DeltaArgs a, const float* states, const float* behind, const float* errors, const float* zs) {
+delta_blocks_kernel(DeltaArgs a, const float* states, const float* behind, const float* errors, const float* zs, float* sums_) {
   extern __shared__ __attribute__((aligned(16))) u16 smem16[];
   using D = BlockLds<T, ND>;
   using W = typename D::W;
@@ -310,7 +302,7 @@ delta_blocks_kernel(DeltaArgs a, const float* states, const float* behind, const
   __shared__ float rates[kBlock], terms[kBlock], parts[kBackWaves];
   u16* const ta = smem16;
   u16* const tb = smem16 + W::kElems;
-  const int tid = threadIdx.x, lane = tid & 63, l15 = lane & 15, t4 = lane >> 4;
+  const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int blocks = (a.n + kBlock - 1) / kBlock, block = blockIdx.x, shared = blockIdx.y, t0 = block * kBlock;
   const int len = tokens_of(a.lengths, shared / a.Hk, a.n), own = 16 * wave, last = min(a.n, t0 + kBlock);
@@ -327,33 +319,30 @@ delta_blocks_kernel(DeltaArgs a, const float* states, const float* behind, const
       a.dg[at] = a.dbeta[at] = 0.f;
     }
   if (t0 >= len) return;
-  const T* const q = (const T*)a.q + row0 * a.dk;
-  const T* const k = (const T*)a.k + row0 * a.dk;
-  // (a column of queries, keys and their gradients, as results have it)
-  ColumnStage<T> cq, ck, gq, gk;
-  cq.init(q, len, a.dk, l15);
-  ck.init(k, len, a.dk, l15);
-  gq.init((T*)a.dq + row0 * a.dk, len, a.dk, l15);
-  gk.init((T*)a.dk_out + row0 * a.dk, len, a.dk, l15);
-  DeltaStage<T, ND, kBlock, kBackThreads> sb;
-  auto fetch_keys = [&](const T* x) {
-    sb.init(x, len, a.dk, tid);
-    sb.fetch(t0);
-  };
-  f32x4 all_q[MANY ? 2 * ND : 1], all_k[MANY ? 2 * ND : 1];
-#pragma unroll
-  for (int j = 0; j < (MANY ? 2 * ND : 1); ++j) all_q[j] = all_k[j] = zero4();
-  for (int v = 0; v < a.G; ++v) {
+  float* const buf = (float*)ta + wave * 16 * (32 * ND + 4);
+  static_assert(kBackWaves * 16 * (32 * ND + 4) * 4 <= W::kBytes, "results lie in the errors' place");
+  const int members = MANY ? a.G : 1;
+#pragma unroll 1
+  for (int v = 0; v < members; ++v) {
+    int id = tid;
+    if (MANY) asm volatile("" : "+v"(id));  // (what hangs on it is not kept over the loop)
+    const int l15 = id & 15, t4 = (id & 63) >> 4;
+    const T* const q = (const T*)a.q + row0 * a.dk;
+    const T* const k = (const T*)a.k + row0 * a.dk;
     const int64_t head = (int64_t)shared * a.G + v, row = head * a.n;
-    const float* const E = errors + row * a.dv;
-    const float* const Z = zs + row * a.dv;
-    const T* const dy = (const T*)a.dy + row * a.dv;
     const float* const S = states + (head * blocks + block) * size;
     const float* const U = behind + (head * blocks + block) * size;
+    RowAccess<float> E, Z;
+    RowAccess<T> dy;
+    E.init(errors + row * a.dv, len, a.dv);
+    Z.init(zs + row * a.dv, len, a.dv);
+    dy.init((const T*)a.dy + row * a.dv, len, a.dv);
+    DeltaStage<T, ND, kBlock, kBackThreads> sb;
     DeltaStage<float, ND, kBlock, kBackThreads> sa;
-    sa.init(E, len, a.dv, tid);
+    sa.init(errors + row * a.dv, len, a.dv, id);
     sa.fetch(t0);
-    fetch_keys(k);
+    sb.init(k, len, a.dk, id);
+    sb.fetch(t0);
     __syncthreads();  // (the last value head's readers are done)
     if (wave == 0) {
       const bool there = t0 + lane < len;
@@ -364,14 +353,36 @@ delta_blocks_kernel(DeltaArgs a, const float* states, const float* behind, const
     sb.put(tb, t0);
     __syncthreads();
     const int mine = own + l15;  // a token of this wave's, in the block
-    const bool there = t0 + mine < len;
     const double my_sum = sums[mine];
     const float my_rate = rates[mine];
     auto decay = [&](double d) { return exp2_fast((float)(d * 1.4426950408889634)); };
-    float rate[4];  // of tokens own + 4 t4 .. +3
+    // dots of this wave's tokens' rows, of by_rows: sums over a row's lanes to `terms`
+    auto add_term = [&](float x, int token) {
 #pragma unroll
-    for (int r = 0; r < 4; ++r) rate[r] = rates[own + 4 * t4 + r];
-    float at[4] = {0.f, 0.f, 0.f, 0.f};  // what counts for a token's sum of log decays
+      for (int d = 1; d < by_rows_lanes<ND>(); d *= 2) x += __shfl_xor(x, d);
+      if (lane % by_rows_lanes<ND>() == 0) terms[own + token] += x;
+    };
+    // a finished gradient's rows: summed over the value heads, or written
+    auto finish = [&](int which, int token, int c0, float (&x)[8]) {
+      if constexpr (MANY) {
+        RowAccess<float> total;
+        total.init(sums_ + ((int64_t)which * (a.heads / a.G) + shared) * a.n * a.dk, len, a.dk);
+        if (v > 0) {
+          float y[8];
+          total.load(t0 + own + token, c0, y);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] += y[i];
+        }
+        if (v + 1 < members) {
+          total.store(t0 + own + token, c0, x);
+          return;
+        }
+      }
+      RowAccess<T> out;
+      out.init((const T*)(which ? a.dk_out : a.dq) + row0 * a.dk, len, a.dk);
+      out.store(t0 + own + token, c0, x);
+    };
+    float asked_at[4] = {0.f, 0.f, 0.f, 0.f};  // k.asked of tokens own + 4 t4 .. +3, this lane's part
     f32x4 sum_k[2 * ND];
 #pragma unroll
     for (int j = 0; j < 2 * ND; ++j) sum_k[j] = zero4();
@@ -380,48 +391,53 @@ delta_blocks_kernel(DeltaArgs a, const float* states, const float* behind, const
 #pragma unroll
       for (int j = 0; j < 2 * ND; ++j) dq[j] = zero4();
       uint4 y[ND][kPl], z[ND][3];
-      load_own16<T, ND>(dy + (int64_t)(t0 + mine) * a.dv, there, a.dv, y);
-      load_own16<float, ND>(Z + (int64_t)(t0 + mine) * a.dv, there, a.dv, z);
+#pragma unroll
+      for (int s = 0; s < ND; ++s) {
+        dy.template operand<kPl>(t0 + mine, 32 * s + 8 * t4, y[s]);
+        Z.template operand<3>(t0 + mine, 32 * s + 8 * t4, z[s]);
+      }
       // ---- pairs of this wave's tokens i with j <= i: rows of one and two
 #pragma unroll 1
       for (int jb = 0; 32 * jb <= own; ++jb) {
         float one[8], two[8];
+        f32x4 p[2] = {zero4(), zero4()}, r[2] = {zero4(), zero4()};
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          f32x4 p = zero4(), r = zero4();
+        for (int s = 0; s < ND; ++s) {
+          uint4 e[2][3];
 #pragma unroll
-          for (int s = 0; s < ND; ++s) {
-            uint4 e[3];
-            rows16<W>(ta, 32 * jb + 16 * x, s, e);
-            p = dot_planes16(e, y[s], p);
-            r = dot_planes16(e, z[s], r);
-          }
+          for (int x = 0; x < 2; ++x) rows16<W>(ta, 32 * jb + 16 * x, s, e[x]);
+          dots_left16(e, y[s], p);
+          dots_left16(e, z[s], r);
+        }
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int j = 32 * jb + 16 * x + 4 * t4 + i;
-            const float d = decay(my_sum - sums[j]) * rates[j];
-            one[4 * x + i] = j <= mine ? p[i] * d * a.scale : 0.f;
-            two[4 * x + i] = j < mine ? -(r[i] * d * my_rate) : 0.f;
-          }
+        for (int e = 0; e < 8; ++e) {
+          const int j = 32 * jb + 16 * (e >> 2) + 4 * t4 + (e & 3);
+          const float d = decay(my_sum - sums[j]) * rates[j];
+          one[e] = j <= mine ? p[e >> 2][e & 3] * d * a.scale : 0.f;
+          two[e] = j < mine ? -(r[e >> 2][e & 3] * d * my_rate) : 0.f;
         }
         uint4 op[3], tp[3];
         operand_of<3>(one, op);
         operand_of<3>(two, tp);
 #pragma unroll
-        for (int j = 0; j < 2 * ND; ++j) {
-          uint4 e[kPl];
-          columns16<L>(tb, 32 * jb, j, e);
-          dq[j] = dot_planes16(op, e, dq[j]);
-          sum_k[j] = dot_planes16(tp, e, sum_k[j]);
+        for (int j = 0; j < 2 * ND; j += 2) {
+          __builtin_amdgcn_sched_barrier(0);
+          uint4 e[2][kPl];
+          f32x4 w[2] = {dq[j], dq[j + 1]}, u[2] = {sum_k[j], sum_k[j + 1]};
+#pragma unroll
+          for (int x = 0; x < 2; ++x) columns16<L>(tb, 32 * jb, j + x, e[x]);
+          dots_right16(op, e, w);
+          dots_right16(tp, e, u);
+          dq[j] = w[0], dq[j + 1] = w[1], sum_k[j] = u[0], sum_k[j + 1] = u[1];
         }
         settle_mfma();
       }
       // ---- the state before the block, 32 rows at a time
-      float early[4];
+      float early[4], rate[4];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) early[r] = decay(sums[own + 4 * t4 + r]);
+      for (int r = 0; r < 4; ++r) early[r] = decay(sums[own + 4 * t4 + r]), rate[r] = rates[own + 4 * t4 + r];
       DeltaStage<float, ND, 32, kBackThreads> ss;
-      ss.init(S, a.dk, a.dv, tid);
+      ss.init(S, a.dk, a.dv, id);
       ss.fetch(0);
 #pragma unroll
       for (int b = 0; b < ND; ++b)
@@ -430,64 +446,64 @@ delta_blocks_kernel(DeltaArgs a, const float* states, const float* behind, const
           ss.put(ta, 32 * b);
           __syncthreads();
           if (32 * b + 32 < a.dk) ss.fetch(32 * b + 32);
+          f32x4 of_y[2] = {zero4(), zero4()}, of_z[2] = {zero4(), zero4()};
 #pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            f32x4 of_y = zero4(), of_z = zero4();
+          for (int s = 0; s < ND; ++s) {
+            uint4 e[2][3];
 #pragma unroll
-            for (int s = 0; s < ND; ++s) {
-              uint4 e[3];
-              rows16<Half>(ta, 16 * x, s, e);
-              of_y = dot_planes16(y[s], e, of_y);
-              of_z = dot_planes16(z[s], e, of_z);
-            }
+            for (int x = 0; x < 2; ++x) rows16<Half>(ta, 16 * x, s, e[x]);
+            dots_right16(y[s], e, of_y);
+            dots_right16(z[s], e, of_z);
+          }
+#pragma unroll
+          for (int x = 0; x < 2; ++x)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-              dq[2 * b + x][r] = fmaf(of_y[r], early[r] * a.scale, dq[2 * b + x][r]);
-              sum_k[2 * b + x][r] = fmaf(-of_z[r], early[r] * rate[r], sum_k[2 * b + x][r]);
+              dq[2 * b + x][r] = fmaf(of_y[x][r], early[r] * a.scale, dq[2 * b + x][r]);
+              sum_k[2 * b + x][r] = fmaf(-of_z[x][r], early[r] * rate[r], sum_k[2 * b + x][r]);
             }
-          }
           settle_mfma();
         }
-      // (asked counts twice here: with kept it is taken off once)
+      // ---- dq is done; asked with the keys
 #pragma unroll
-      for (int j = 0; j < 2 * ND; ++j) {
-        cq.template fetch<4>(t0 + own, 16 * j);
-        ck.template fetch<4>(t0 + own, 16 * j);
+      for (int j = 0; j < 2 * ND; ++j)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) at[r] = fmaf(cq.value(r), dq[j][r], fmaf(2.f * ck.value(r), sum_k[j][r], at[r]));
-        if constexpr (MANY) {
+        for (int r = 0; r < 4; ++r)
+          asked_at[r] = fmaf(tile_entry<L>(tb, own + 4 * t4 + r, 16 * j + l15), sum_k[j][r], asked_at[r]);
+      if (lane < 16) terms[own + lane] = 0.f;
+      __syncthreads();
+      RowAccess<T> rq;
+      rq.init(q, len, a.dk);
+      by_rows<ND>(dq, buf, [&](int token, int c0, float (&x)[8]) {
+        float w[8], dot = 0.f;
+        rq.load(t0 + own + token, c0, w);
 #pragma unroll
-          for (int r = 0; r < 4; ++r) all_q[j][r] += dq[j][r];
-          dq[j] = all_q[j];
-        }
-        if (!MANY || v + 1 == a.G)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) gq.store(t0 + own, r, dq[j][r], 16 * j);
-      }
+        for (int i = 0; i < 8; ++i) dot = fmaf(w[i], x[i], dot);
+        add_term(dot, token);
+        finish(0, token, c0, x);
+      });
     }
     // ---- pairs of tokens i with this wave's j <= i: columns of one, then of two
     uint4 e_own[ND][3];
     {
       DeltaStage<T, ND, kBlock, kBackThreads> sy;
-      sy.init(dy, len, a.dv, tid);
+      sy.init((const T*)a.dy + row * a.dv, len, a.dv, id);
       sy.fetch(t0);
-      fetch_keys(q);
-      const float* const pe = E + (int64_t)(t0 + mine) * a.dv;
-      const float* const pz = Z + (int64_t)(t0 + mine) * a.dv;
-      const bool vec = a.dv % 4 == 0 && (((uintptr_t)pe | (uintptr_t)pz) & 15) == 0;
+      sb.init(q, len, a.dk, id);
+      sb.fetch(t0);
       float dot = 0.f;
 #pragma unroll
       for (int s = 0; s < ND; ++s) {
         float x[8], w[8];
-        load_eight(pe, 32 * s + 8 * t4, there, a.dv, vec, x);
-        load_eight(pz, 32 * s + 8 * t4, there, a.dv, vec, w);
+        E.load(t0 + mine, 32 * s + 8 * t4, x);
+        Z.load(t0 + mine, 32 * s + 8 * t4, w);
 #pragma unroll
         for (int i = 0; i < 8; ++i) dot = fmaf(x[i], w[i], dot);
         operand_of<3>(x, e_own[s]);
       }
       dot += __shfl_xor(dot, 16);
       dot += __shfl_xor(dot, 32);
-      if (t4 == 0 && there) a.dbeta[row + t0 + mine] = dot;
+      if (t4 == 0 && t0 + mine < len) a.dbeta[row + t0 + mine] = dot;
       __syncthreads();
       sy.put(ta, t0);
       sb.put(tb, t0);
@@ -496,9 +512,10 @@ delta_blocks_kernel(DeltaArgs a, const float* states, const float* behind, const
 #pragma unroll 1
     for (int turn = 0; turn < 2; ++turn) {
       if (turn == 1) {
-        sa.init(Z, len, a.dv, tid);
+        sa.init(zs + row * a.dv, len, a.dv, id);
         sa.fetch(t0);
-        fetch_keys(k);
+        sb.init(k, len, a.dk, id);
+        sb.fetch(t0);
         __syncthreads();
         sa.put(ta, t0);
         sb.put(tb, t0);
@@ -507,39 +524,42 @@ delta_blocks_kernel(DeltaArgs a, const float* states, const float* behind, const
 #pragma unroll 1
       for (int ib = own / 32; ib < 2; ++ib) {
         float w[8];
+        f32x4 p[2] = {zero4(), zero4()};
+        if (turn == 0) {
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          f32x4 p = zero4();
-          if (turn == 0) {
+          for (int s = 0; s < ND; ++s) {
+            uint4 e[2][kPl];
 #pragma unroll
-            for (int s = 0; s < ND; ++s) {
-              uint4 e[kPl];
-              rows16<L>(ta, 32 * ib + 16 * x, s, e);
-              p = dot_planes16(e, e_own[s], p);
-            }
-          } else {
-#pragma unroll
-            for (int s = 0; s < ND; ++s) {
-              uint4 e[3];
-              rows16<W>(ta, 32 * ib + 16 * x, s, e);
-              p = dot_planes16(e, e_own[s], p);
-            }
+            for (int x = 0; x < 2; ++x) rows16<L>(ta, 32 * ib + 16 * x, s, e[x]);
+            dots_left16(e, e_own[s], p);
           }
-          settle_mfma();
+        } else {
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int i = 32 * ib + 16 * x + 4 * t4 + r;
-            const float d = p[r] * (decay(sums[i] - my_sum) * my_rate);
-            w[4 * x + r] = turn == 0 ? (i >= mine ? d * a.scale : 0.f) : i > mine ? -(d * rates[i]) : 0.f;
+          for (int s = 0; s < ND; ++s) {
+            uint4 e[2][3];
+#pragma unroll
+            for (int x = 0; x < 2; ++x) rows16<W>(ta, 32 * ib + 16 * x, s, e[x]);
+            dots_left16(e, e_own[s], p);
           }
+        }
+        settle_mfma();
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int i = 32 * ib + 16 * (e >> 2) + 4 * t4 + (e & 3);
+          const float d = p[e >> 2][e & 3] * (decay(sums[i] - my_sum) * my_rate);
+          w[e] = turn == 0 ? (i >= mine ? d * a.scale : 0.f) : i > mine ? -(d * rates[i]) : 0.f;
         }
         uint4 op[3];
         operand_of<3>(w, op);
 #pragma unroll
-        for (int j = 0; j < 2 * ND; ++j) {
-          uint4 e[kPl];
-          columns16<L>(tb, 32 * ib, j, e);
-          sum_k[j] = dot_planes16(op, e, sum_k[j]);
+        for (int j = 0; j < 2 * ND; j += 2) {
+          __builtin_amdgcn_sched_barrier(0);
+          uint4 e[2][kPl];
+          f32x4 u[2] = {sum_k[j], sum_k[j + 1]};
+#pragma unroll
+          for (int x = 0; x < 2; ++x) columns16<L>(tb, 32 * ib, j + x, e[x]);
+          dots_right16(op, e, u);
+          sum_k[j] = u[0], sum_k[j + 1] = u[1];
         }
         settle_mfma();
       }
@@ -550,10 +570,10 @@ delta_blocks_kernel(DeltaArgs a, const float* states, const float* behind, const
       const double end = sums[kBlock - 1];
       float late[4];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) late[r] = decay(end - sums[own + 4 * t4 + r]) * rate[r];
+      for (int r = 0; r < 4; ++r) late[r] = decay(end - sums[own + 4 * t4 + r]) * rates[own + 4 * t4 + r];
       DeltaStage<float, ND, 32, kBackThreads> ss, su;
-      ss.init(S, a.dk, a.dv, tid);
-      su.init(U, a.dk, a.dv, tid);
+      ss.init(S, a.dk, a.dv, id);
+      su.init(U, a.dk, a.dv, id);
       su.fetch(0);
       ss.fetch(0);
 #pragma unroll
@@ -578,47 +598,44 @@ delta_blocks_kernel(DeltaArgs a, const float* states, const float* behind, const
             su.fetch(32 * b + 32);
             ss.fetch(32 * b + 32);
           }
+          f32x4 of_e[2] = {zero4(), zero4()};
 #pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            f32x4 of_e = zero4();
+          for (int s = 0; s < ND; ++s) {
+            uint4 e[2][3];
 #pragma unroll
-            for (int s = 0; s < ND; ++s) {
-              uint4 e[3];
-              rows16<Half>(ta, 16 * x, s, e);
-              of_e = dot_planes16(e_own[s], e, of_e);
-            }
-            ck.template fetch<4>(t0 + own, 32 * b + 16 * x);
+            for (int x = 0; x < 2; ++x) rows16<Half>(ta, 16 * x, s, e[x]);
+            dots_right16(e_own[s], e, of_e);
+          }
+#pragma unroll
+          for (int x = 0; x < 2; ++x)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-              const float e = of_e[r] * late[r];
-              late_terms = fmaf(ck.value(r), e, late_terms);
+              const float e = of_e[x][r] * late[r];
+              late_terms = fmaf(tile_entry<L>(tb, own + 4 * t4 + r, 32 * b + 16 * x + l15), e, late_terms);
               sum_k[2 * b + x][r] += e;
             }
-          }
           settle_mfma();
         }
       inner *= decay(end);
     }
-    // ---- dk, and the gradient of g
+    // ---- dk, and the gradient of g (asked counts for it: with kept it has been taken off)
+    __syncthreads();
+    RowAccess<T> rk;
+    rk.init(k, len, a.dk);
+    by_rows<ND>(sum_k, buf, [&](int token, int c0, float (&x)[8]) {
+      float w[8], dot = 0.f;
+      rk.load(t0 + own + token, c0, w);
 #pragma unroll
-    for (int j = 0; j < 2 * ND; ++j) {
-      ck.template fetch<4>(t0 + own, 16 * j);
-#pragma unroll
-      for (int r = 0; r < 4; ++r) at[r] = fmaf(-ck.value(r), sum_k[j][r], at[r]);
-      if constexpr (MANY) {
-#pragma unroll
-        for (int r = 0; r < 4; ++r) all_k[j][r] += sum_k[j][r];
-        sum_k[j] = all_k[j];
-      }
-      if (!MANY || v + 1 == a.G)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) gk.store(t0 + own, r, sum_k[j][r], 16 * j);
-    }
+      for (int i = 0; i < 8; ++i) dot = fmaf(w[i], x[i], dot);
+      add_term(-dot, token);
+      finish(1, token, c0, x);
+    });
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
 #pragma unroll
-      for (int d = 1; d < 16; d *= 2) at[r] += __shfl_xor(at[r], d);
-      if (l15 == r) terms[own + 4 * t4 + r] = at[r];
+      for (int d = 1; d < 16; d *= 2) asked_at[r] += __shfl_xor(asked_at[r], d);
+      wave_lds_fence();
+      if (l15 == r) terms[own + 4 * t4 + r] += 2.f * asked_at[r];
     }
     inner += late_terms;
 #pragma unroll
@@ -636,9 +653,9 @@ delta_blocks_kernel(DeltaArgs a, const float* states, const float* behind, const
 
 // Where a call's scratch goes.
 struct Places {
-  size_t data, back, states, behind, errors, zs, bytes;
+  size_t data, back, states, behind, errors, zs, sums, bytes;
 };
-Places places_of(bool bf16, int heads, int n, int dk, int dv) {
+Places places_of(bool bf16, int heads, int G, int n, int dk, int dv) {
   const size_t blocks = (size_t)heads * ((n + kBlock - 1) / kBlock);
   auto whole = [](size_t x) { return (x + 255) / 256 * 256; };
   Places p;
@@ -648,7 +665,8 @@ Places places_of(bool bf16, int heads, int n, int dk, int dv) {
   p.behind = p.states + whole(blocks * dk * dv * sizeof(float));
   p.errors = p.behind + whole(blocks * dk * dv * sizeof(float));
   p.zs = p.errors + whole((size_t)heads * n * dv * sizeof(float));
-  p.bytes = p.zs + whole((size_t)heads * n * dv * sizeof(float));
+  p.sums = p.zs + whole((size_t)heads * n * dv * sizeof(float));
+  p.bytes = p.sums + (G > 1 ? 2 * whole((size_t)(heads / G) * n * dk * sizeof(float)) : 0);
   return p;
 }
 
@@ -670,27 +688,27 @@ hipError_t launch_back(const DeltaArgs& a, const void* data, float* behind, floa
 
 template <typename T, int ND, bool MANY>
 hipError_t launch_blocks_of(const DeltaArgs& a, const float* states, const float* behind, const float* errors, const float* zs,
-                            hipStream_t s) {
+                            float* sums, hipStream_t s) {
   constexpr int bytes = BlockLds<T, ND>::kBytes;
   static_assert(bytes <= 158 * 1024, "LDS of one workgroup");
   auto kern = delta_blocks_kernel<T, ND, MANY>;
   hipError_t e = raise_lds(kern, bytes);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(kern, dim3((a.n + kBlock - 1) / kBlock, a.heads / a.G), dim3(kBackThreads), bytes, s, a, states, behind, errors, zs);
+  hipLaunchKernelGGL(kern, dim3((a.n + kBlock - 1) / kBlock, a.heads / a.G), dim3(kBackThreads), bytes, s, a, states, behind, errors, zs, sums);
   return hipGetLastError();
 }
 template <typename T, int ND>
 hipError_t launch_blocks(const DeltaArgs& a, const float* states, const float* behind, const float* errors, const float* zs,
-                         hipStream_t s) {
-  return a.G > 1 ? launch_blocks_of<T, ND, true>(a, states, behind, errors, zs, s)
-                 : launch_blocks_of<T, ND, false>(a, states, behind, errors, zs, s);
+                         float* sums, hipStream_t s) {
+  return a.G > 1 ? launch_blocks_of<T, ND, true>(a, states, behind, errors, zs, sums, s)
+                 : launch_blocks_of<T, ND, false>(a, states, behind, errors, zs, sums, s);
 }
 
 template <typename T>
 hipError_t launch(const DeltaArgs& a, char* scratch, hipStream_t s) {
-  const Places p = places_of(sizeof(T) == 2, a.heads, a.n, a.dk, a.dv);
+  const Places p = places_of(sizeof(T) == 2, a.heads, a.G, a.n, a.dk, a.dv);
   float *states = (float*)(scratch + p.states), *behind = (float*)(scratch + p.behind);
-  float *errors = (float*)(scratch + p.errors), *zs = (float*)(scratch + p.zs);
+  float *errors = (float*)(scratch + p.errors), *zs = (float*)(scratch + p.zs), *sums = (float*)(scratch + p.sums);
   hipError_t e = launch_delta_pairs(a, sizeof(T) == 2, scratch + p.data, scratch + p.back, s);
   if (e == hipSuccess) e = launch_delta_states(a, sizeof(T) == 2, scratch + p.data, states, errors, s);
   if (e != hipSuccess) return e;
@@ -702,10 +720,10 @@ hipError_t launch(const DeltaArgs& a, char* scratch, hipStream_t s) {
   }
   if (e != hipSuccess) return e;
   switch ((std::max(a.dk, a.dv) + 31) / 32) {
-    case 1: return launch_blocks<T, 1>(a, states, behind, errors, zs, s);
-    case 2: return launch_blocks<T, 2>(a, states, behind, errors, zs, s);
-    case 3: return launch_blocks<T, 3>(a, states, behind, errors, zs, s);
-    default: return launch_blocks<T, 4>(a, states, behind, errors, zs, s);
+    case 1: return launch_blocks<T, 1>(a, states, behind, errors, zs, sums, s);
+    case 2: return launch_blocks<T, 2>(a, states, behind, errors, zs, sums, s);
+    case 3: return launch_blocks<T, 3>(a, states, behind, errors, zs, sums, s);
+    default: return launch_blocks<T, 4>(a, states, behind, errors, zs, sums, s);
   }
 }
 
@@ -716,8 +734,8 @@ __global__ void __launch_bounds__(256) delta_no_tokens_kernel(const float* dS, f
 
 }  // namespace
 
-size_t delta_backward_scratch(bool bf16, int heads, int, int n, int dk, int dv) {
-  return n == 0 ? 0 : places_of(bf16, heads, n, dk, dv).bytes;
+size_t delta_backward_scratch(bool bf16, int heads, int G, int n, int dk, int dv) {
+  return n == 0 ? 0 : places_of(bf16, heads, G, n, dk, dv).bytes;
 }
 
 hipError_t launch_delta_backward(const DeltaArgs& a, bool bf16, void* scratch, hipStream_t s) {

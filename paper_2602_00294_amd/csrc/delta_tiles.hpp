@@ -184,37 +184,95 @@ struct DataStage {
   }
 };
 
-// One column of a head's [rows][width] entries, a lane its own: entries of rows t0 + 16 x + 4 t4 .. +3 (x = 0 .. 3), zero behind
-// the last row and where the lane has no column.  Stores there are dropped.
+// A lane's own column of a head's [rows][width] entries: entries of rows t0 + 16 x + 4 t4 .. +3 (x = 0 .. 3) are written, those behind
+// the last row and of a lane without a column dropped.
 template <typename T>
 struct ColumnStage {
   __amdgpu_buffer_rsrc_t rsrc;
   uint32_t off, pitch;
-  int left;  // columns from this lane's on
-  uint32_t r[16];
   __device__ __forceinline__ void init(const T* head, int rows, int width, int col) {
     rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(head), 0, rows * width * (int)sizeof(T), 0x00020000);
     pitch = (uint32_t)(width * (int)sizeof(T));
-    left = width - col;
-    off = (uint32_t)((threadIdx.x & 63) >> 4) * 4u * pitch + (uint32_t)(col * (int)sizeof(T));
+    off = col < width ? (uint32_t)((threadIdx.x & 63) >> 4) * 4u * pitch + (uint32_t)(col * (int)sizeof(T)) : kNoVector;
   }
-  // (of the column `ahead` further on, of which the lane may have none)
-  __device__ __forceinline__ uint32_t at(int t0, int e, int ahead) const {
-    const uint32_t place = off + (uint32_t)(t0 + 16 * (e >> 2) + (e & 3)) * pitch + (uint32_t)(ahead * (int)sizeof(T));
-    return ahead < left ? place : kNoVector;
+  __device__ __forceinline__ int at(int t0, int e) const { return (int)(off + (uint32_t)(t0 + 16 * (e >> 2) + (e & 3)) * pitch); }
+  __device__ __forceinline__ void store(int t0, int e, float x) const {
+    if constexpr (sizeof(T) == 4) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(x), rsrc, at(t0, e), 0, 0);
+    else __builtin_amdgcn_raw_buffer_store_b16((unsigned short)(pack2(x, 0.f) & 0xffffu), rsrc, at(t0, e), 0, 0);
   }
-  template <int COUNT = 16>
-  __device__ __forceinline__ void fetch(int t0, int ahead = 0) {
+};
+
+// Eight entries c0 .. +7 of a row of a head's [rows][width]: by vectors where the rows allow them.  Rows behind the last and
+// columns behind the width read as zero and are not written.  (No branch but the one on `vec`, the same for all.)
+template <typename T>
+struct RowAccess {
+  __amdgpu_buffer_rsrc_t rsrc;
+  int width;
+  bool vec;
+  typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+  __device__ __forceinline__ void init(const T* head, int rows, int width_) {
+    width = width_;
+    vec = width * (int)sizeof(T) % 16 == 0 && ((uintptr_t)head & 15) == 0;
+    rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(head), 0, rows * width * (int)sizeof(T), 0x00020000);
+  }
+  __device__ __forceinline__ int at(int row, int col) const {
+    return (int)(col < width ? (uint32_t)(row * width + col) * (uint32_t)sizeof(T) : kNoVector);
+  }
+  __device__ __forceinline__ uint4 quad(int offset) const {
+    return __builtin_bit_cast(uint4, (u32x4)__builtin_amdgcn_raw_buffer_load_b128(rsrc, offset, 0, 0));
+  }
+  // (the bits of bfloat16 ones)
+  __device__ __forceinline__ uint4 load_bits(int row, int c0) const {
+    if (vec) return quad(at(row, c0));
+    uint32_t u[8];
 #pragma unroll
-    for (int e = 0; e < COUNT; ++e) {
-      if constexpr (sizeof(T) == 4) r[e] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rsrc, (int)at(t0, e, ahead), 0, 0);
-      else r[e] = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rsrc, (int)at(t0, e, ahead), 0, 0);
+    for (int i = 0; i < 8; ++i) u[i] = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rsrc, at(row, c0 + i), 0, 0);
+    return uint4{u[0] | u[1] << 16, u[2] | u[3] << 16, u[4] | u[5] << 16, u[6] | u[7] << 16};
+  }
+  __device__ __forceinline__ void load(int row, int c0, float (&x)[8]) const {
+    if constexpr (sizeof(T) == 2) {
+      const uint4 w = load_bits(row, c0);
+      const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[2 * i] = lo_f32(u[i]), x[2 * i + 1] = hi_f32(u[i]);
+    } else if (vec) {
+      const uint4 w = quad(at(row, c0)), v = quad(at(row, c0 + 4));
+      x[0] = __uint_as_float(w.x), x[1] = __uint_as_float(w.y), x[2] = __uint_as_float(w.z), x[3] = __uint_as_float(w.w);
+      x[4] = __uint_as_float(v.x), x[5] = __uint_as_float(v.y), x[6] = __uint_as_float(v.z), x[7] = __uint_as_float(v.w);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = __uint_as_float((uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rsrc, at(row, c0 + i), 0, 0));
     }
   }
-  __device__ __forceinline__ float value(int e) const { return __uint_as_float(sizeof(T) == 4 ? r[e] : r[e] << 16); }
-  __device__ __forceinline__ void store(int t0, int e, float x, int ahead = 0) const {
-    if constexpr (sizeof(T) == 4) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(x), rsrc, (int)at(t0, e, ahead), 0, 0);
-    else __builtin_amdgcn_raw_buffer_store_b16((unsigned short)(pack2(x, 0.f) & 0xffffu), rsrc, (int)at(t0, e, ahead), 0, 0);
+  template <int PL>
+  __device__ __forceinline__ void operand(int row, int c0, uint4 (&op)[PL]) const {
+    if constexpr (sizeof(T) == 2) {
+      op[0] = load_bits(row, c0);
+    } else {
+      float x[8];
+      load(row, c0, x);
+      operand_of<PL>(x, op);
+    }
+  }
+  __device__ __forceinline__ void put_quad(int offset, uint32_t a, uint32_t b, uint32_t c, uint32_t d) const {
+    __builtin_amdgcn_raw_buffer_store_b128(u32x4{a, b, c, d}, rsrc, offset, 0, 0);
+  }
+  __device__ __forceinline__ void store(int row, int c0, const float (&x)[8]) const {
+    if (vec) {
+      if constexpr (sizeof(T) == 2) {
+        put_quad(at(row, c0), pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7]));
+      } else {
+#pragma unroll
+        for (int h = 0; h < 8; h += 4)
+          put_quad(at(row, c0 + h), __float_as_uint(x[h]), __float_as_uint(x[h + 1]), __float_as_uint(x[h + 2]), __float_as_uint(x[h + 3]));
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b16((unsigned short)(pack2(x[i], 0.f) & 0xffffu), rsrc, at(row, c0 + i), 0, 0);
+        else __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(x[i]), rsrc, at(row, c0 + i), 0, 0);
+      }
+    }
   }
 };
 
