@@ -21,14 +21,45 @@ __device__ __forceinline__ uint32_t group_params(float least, float most, bool f
   // (halves: as written down for programs that form such rows on their own; no difference of them overflows)
   return fine ? pack2((0.5f * most - 0.5f * least) / 7.5f, least) : 0x7fc07fc0u;
 }
-__device__ __forceinline__ uint32_t code_of(float x, uint32_t params) {
-  const float half = 0.5f * lo_f32(params), low = 0.5f * hi_f32(params);
-  // (a scale of NaN is not above zero)
-  return half > 0.f ? (uint32_t)fminf(fmaxf(rintf((0.5f * x - low) / half), 0.f), 15.f) : 0u;
-}
+// What the codes of a group's entries take: (x / 2 - least / 2) / (scale / 2) as float32 division rounds it, then to the nearest.
+// 1 / (scale / 2) is rounded to the nearest by one Newton step (of all 128 significands of a bfloat16, from any start two
+// units off), so that a quotient and one correction give the nearest quotient too, but for scales so small that the
+// correction's rest would not be a normal number: those divide.
+struct GroupCode {
+  float half, low, inverse;
+  bool divide;
+  __device__ __forceinline__ explicit GroupCode(uint32_t params) {
+    half = 0.5f * lo_f32(params), low = 0.5f * hi_f32(params);
+    const float r = __builtin_amdgcn_rcpf(half);
+    inverse = fmaf(fmaf(-half, r, 1.f), r, r);
+    divide = half < 0x1p-90f;
+  }
+  __device__ __forceinline__ uint32_t operator()(float x) const {
+    const float a = 0.5f * x - low;
+    float q = a * inverse;
+    q = fmaf(fmaf(-q, half, a), inverse, q);
+    if (__builtin_expect(divide, 0)) q = a / half;
+    // (a scale of zero or NaN is not above zero)
+    return half > 0.f ? (uint32_t)fminf(fmaxf(rintf(q), 0.f), 15.f) : 0u;
+  }
+};
 __device__ __forceinline__ float value_of(uint32_t code, uint32_t params) {
   return fmaf((float)code, lo_f32(params), hi_f32(params));
 }
+
+// The least and the most of 16 lanes' values.
+template <int CTRL>
+__device__ __forceinline__ float turned_row(float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ void ends_of_row(float& least, float& most) {
+  least = fminf(least, turned_row<0x128>(least)), most = fmaxf(most, turned_row<0x128>(most));  // by 8, 4, 2, 1 lanes
+  least = fminf(least, turned_row<0x124>(least)), most = fmaxf(most, turned_row<0x124>(most));
+  least = fminf(least, turned_row<0x122>(least)), most = fmaxf(most, turned_row<0x122>(most));
+  least = fminf(least, turned_row<0x121>(least)), most = fmaxf(most, turned_row<0x121>(most));
+}
+// What an entry counts as for a group's ends: one out of range as infinity, which tells.
+__device__ __forceinline__ float for_ends(float x) { return fabsf(x) <= 0x1p120f ? x : INFINITY; }
 
 // 16 lanes with the entries 32 g + a and 32 g + 16 + a of a row of width d, a = the lane: this lane's G bytes of codes,
 // and the groups' scales and least values (the same in all lanes).
@@ -39,17 +70,12 @@ __device__ __forceinline__ uint32_t pack_row(int a, int d, F&& entry, uint32_t (
   for (int g = 0; g < G; ++g) {
     const int i = 32 * g + a, j = i + 16;
     const float x = i < d ? entry(i) : 0.f, y = j < d ? entry(j) : 0.f;
-    float least = i < d ? x : INFINITY, most = i < d ? x : -INFINITY;
-    if (j < d) least = fminf(least, y), most = fmaxf(most, y);
-    int fine = fabsf(x) <= 0x1p120f && fabsf(y) <= 0x1p120f;
-#pragma unroll
-    for (int m = 1; m < 16; m *= 2) {
-      least = fminf(least, __shfl_xor(least, m));
-      most = fmaxf(most, __shfl_xor(most, m));
-      fine &= __shfl_xor(fine, m);
-    }
-    params[g] = 32 * g < d ? group_params(least, most, fine) : 0u;
-    codes |= ((i < d ? code_of(x, params[g]) : 0u) | (j < d ? code_of(y, params[g]) : 0u) << 4) << (8 * g);
+    float least = i < d ? for_ends(x) : INFINITY, most = i < d ? for_ends(x) : -INFINITY;
+    if (j < d) least = fminf(least, for_ends(y)), most = fmaxf(most, for_ends(y));
+    ends_of_row(least, most);
+    params[g] = 32 * g < d ? group_params(least, most, most < INFINITY) : 0u;
+    const GroupCode code(params[g]);
+    codes |= ((i < d ? code(x) : 0u) | (j < d ? code(y) : 0u) << 4) << (8 * g);
   }
   return codes;
 }

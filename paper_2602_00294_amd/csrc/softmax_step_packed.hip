@@ -2,15 +2,18 @@
 // caches becomes k and v in those bits, then y = sum_{s<=lengths[b]} p_s v_s with p = softmax(c q.k_s), k_s and v_s
 // being what the caches' rows stand for.
 //
-// Rows are never unpacked into numbers of their own.  A bfloat16 with the code's four bits on top of its
-// fraction, 0x4180 | code << 3, is 16 + code, exactly, so two codes become operands of a product by a shift and
-// one and-or.  With s and m a group's scale and least value, X the sums over such operands,
-//     q.k_t = sum_g s_tg X_tg + (m_tg - 16 s_tg) (sum of q's entries in g),   X_tg = sum_i (16 + code_ti) q_i
-//     y     = sum_t (p_t s_tg) (16 + code_tj) + sum_t p_t (m_tg - 16 s_tg).
+// Rows are never unpacked into numbers of their own.  A bfloat16 with the code's four bits as the last of its
+// fraction, 0x4300 | code, is 128 + code, exactly, so two codes become operands of a product by a shift (half of them) and
+// one and-or.  With s and m a group's scale and least value, X the sums over such operands, o = 128,
+//     q.k_t = sum_g s_tg X_tg + (m_tg - o s_tg) (sum of q's entries in g),   X_tg = sum_i (o + code_ti) q_i
+//     y     = sum_t (p_t s_tg) (o + code_tj) + sum_t p_t (m_tg - o s_tg).
+// What the offset takes from the sums, seven bits of 24, bfloat16 calls do not feel; float32 calls take
+// 0x4180 | code << 3, o = 16, for a shift more.
 // Products are v_mfma_f32_16x16x32_bf16 with the query heads of a group as columns: of keys a group of 32 entries
 // at a time, rows being 16 tokens; of values 16 columns at a time over 32 tokens.  A lane reads of a key's row the bytes of
 // four a (packed_rows.hpp), of a value's row those of one; scores' tokens, four a lane, are the
-// weights' places in the second product, so they never leave their lanes.
+// weights' places in the second product, so they never leave their lanes.  Scales go through LDS: a lane needs eight
+// tokens' and reads one's or two's.
 //
 // Bound: the cache is read once, 5 (d_k + d_v) / 8 bytes a key.
 //
@@ -20,6 +23,7 @@
 
 #include <algorithm>
 
+#include "delta_tiles.hpp"
 #include "device_common.hpp"
 #include "kernels.hpp"
 #include "packed_rows.hpp"
@@ -70,17 +74,94 @@ __device__ __forceinline__ void group_bytes(const KeyCodes<G>& c, int g, uint32_
     second = __builtin_amdgcn_perm(0u, c.w[0], 0x0c030c02u);
   }
 }
-// 16 + the code in bits 0..3 (or 4..7) of each half
-__device__ __forceinline__ uint32_t low_codes(uint32_t x) { return ((x << 3) & 0x00780078u) | 0x41804180u; }
-__device__ __forceinline__ uint32_t high_codes(uint32_t x) { return ((x >> 1) & 0x00780078u) | 0x41804180u; }
+// What codes count from, and the code in bits 0..3 (or 4..7) of each half as that much more.  (Both constants in registers:
+// one instruction.)
+template <typename T>
+struct Codes {
+  static constexpr float kOffset = sizeof(T) == 2 ? 128.f : 16.f;
+  uint32_t mask = sizeof(T) == 2 ? 0x000f000fu : 0x00780078u, tag = sizeof(T) == 2 ? 0x43004300u : 0x41804180u;
+  __device__ __forceinline__ Codes() { asm("" : "+v"(mask), "+v"(tag)); }
+  __device__ __forceinline__ uint32_t low(uint32_t x) const { return ((sizeof(T) == 2 ? x : x << 3) & mask) | tag; }
+  __device__ __forceinline__ uint32_t high(uint32_t x) const { return ((sizeof(T) == 2 ? x >> 4 : x >> 1) & mask) | tag; }
+};
 
-__device__ __forceinline__ f32x4 zero4() { return f32x4{0.f, 0.f, 0.f, 0.f}; }
+// N floats of LDS
+template <int N>
+struct Floats {
+  float f[N];
+};
+template <int N>
+__device__ __forceinline__ Floats<N> load_floats(const float* p) {
+  Floats<N> x;
+  if constexpr (N == 4) {
+    const float4 v = *(const float4*)p;
+    x.f[0] = v.x, x.f[1] = v.y, x.f[2] = v.z, x.f[3] = v.w;
+  } else if constexpr (N == 2) {
+    const float2 v = *(const float2*)p;
+    x.f[0] = v.x, x.f[1] = v.y;
+  } else {
+    x.f[0] = *p;
+  }
+  return x;
+}
+template <int N>
+__device__ __forceinline__ void store_floats(float* p, const float (&x)[N]) {
+  if constexpr (N == 4) *(float4*)p = float4{x[0], x[1], x[2], x[3]};
+  else if constexpr (N == 2) *(float2*)p = float2{x[0], x[1]};
+  else *p = x[0];
+}
+
+// A lane's part of 32 rows: codes and parameters of keys 16 x + l15, codes of values 4 t4 + i and 16 + 4 t4 + i,
+// parameters of value l31.
+template <int GK, int GV>
+struct PackedTile {
+  KeyCodes<GK> kc[2], kp[2];
+  uint32_t vc[8];
+  KeyCodes<GV> vp;
+  // rows r0 .. r0 + 31, all before the last one
+  __device__ __forceinline__ void load(const uint8_t* K, const uint8_t* V, int r0) {
+    const int lane = threadIdx.x & 63, l15 = lane & 15, t4 = lane >> 4, l31 = lane & 31;
+    const uint8_t* const k = K + (int64_t)r0 * (20 * GK) + l15 * (20 * GK);
+    const uint8_t* const v = V + (int64_t)r0 * (20 * GV);
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      kc[x] = load_key<GK>(k + 16 * x * (20 * GK) + 4 * GK * t4);
+      kp[x] = load_params<GK>(k + 16 * x * (20 * GK));
+    }
+    const uint8_t* const c = v + 4 * t4 * (20 * GV) + l15 * GV;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) vc[i] = load_packed<GV>(c + (16 * (i >> 2) + (i & 3)) * (20 * GV), 0);
+    vp = load_params<GV>(v + l31 * (20 * GV));
+  }
+  // The same where row `at` is the last: rows behind it are read as that one, which others may be writing and which lies in
+  // LDS (`fresh`, the value's 80 bytes on).
+  __device__ __forceinline__ void load_last(const uint8_t* K, const uint8_t* V, int r0, int at, const uint8_t* fresh) {
+    const int lane = threadIdx.x & 63, l15 = lane & 15, t4 = lane >> 4, l31 = lane & 31;
+    auto key = [&](int r) { return K + (int64_t)min(r, at) * (20 * GK); };
+    auto value = [&](int r) { return V + (int64_t)min(r, at) * (20 * GV); };
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const int r = r0 + 16 * x + l15;
+      kc[x] = load_key<GK>(key(r) + 4 * GK * t4);
+      kp[x] = load_params<GK>(key(r));
+      if (r >= at) kc[x] = load_key<GK>(fresh + 4 * GK * t4), kp[x] = load_params<GK>(fresh);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int r = r0 + 4 * t4 + 16 * (i >> 2) + (i & 3);
+      vc[i] = load_packed<GV>(value(r), l15);
+      if (r >= at) vc[i] = load_packed<GV>(fresh + 80, l15);
+    }
+    vp = load_params<GV>(value(r0 + l31));
+    if (r0 + l31 >= at) vp = load_params<GV>(fresh + 80);
+  }
+};
 
 // GK, GV: groups of keys and values.
 template <typename T, int GK, int GV>
 __device__ __forceinline__ void packed_stretch_rows(const SoftmaxStepArgs& a, int64_t kvh, int block, int at, int first, int end,
                                                     float* part, float* sums, StepState (*state)[kPackedMembers],
-                                                    uint8_t* fresh) {
+                                                    uint8_t* fresh, float* scales) {
   constexpr int kPl = sizeof(T) == 4 ? 3 : 1;    // numbers of a query's entry
   constexpr int kWeight = sizeof(T) == 4 ? 3 : 2;  // of a weight
   constexpr int kKey = 20 * GK, kValue = 20 * GV, kThreads = 64 * kStepWaves;
@@ -143,7 +224,7 @@ __device__ __forceinline__ void packed_stretch_rows(const SoftmaxStepArgs& a, in
     }
     float x[8];
 #pragma unroll
-    for (int g = 0; g < 4; ++g) x[2 * g] = g < GK ? -16.f * total[g] : 0.f, x[2 * g + 1] = g < GK ? total[g] : 0.f;
+    for (int g = 0; g < 4; ++g) x[2 * g] = g < GK ? -Codes<T>::kOffset * total[g] : 0.f, x[2 * g + 1] = g < GK ? total[g] : 0.f;
     uint4 w[1][3];
     to_planes<3>(x, w);
     qsum = t4 == 0 ? w[0][0] : t4 == 1 ? w[0][1] : t4 == 2 ? w[0][2] : uint4{0u, 0u, 0u, 0u};
@@ -157,70 +238,70 @@ __device__ __forceinline__ void packed_stretch_rows(const SoftmaxStepArgs& a, in
   float top = -3.4028234e38f, sum = 0.f;
   const float c = a.scale * kLog2e;
   constexpr int kStep = 32 * kStepWaves;
+  const Codes<T> codes;
+  // this wave's: scales of keys [32][GK], of values [32][GV], and least values less the codes' offset
+  float* const kscale = scales + wave * 32 * (GK + 2 * GV);
+  float* const vscale = kscale + 32 * GK;
+  float* const vbase = vscale + 32 * GV;
+  PackedTile<GK, GV> tile;
+  auto load = [&](int r0) {
+    if (r0 + 32 <= at) tile.load(K, V, r0);
+    else tile.load_last(K, V, r0, at, fresh);
+  };
+  int r0 = first + 32 * wave;
+  if (r0 < end) load(r0);
 #pragma unroll 1
-  for (int r0 = first + 32 * wave; r0 < end; r0 += kStep) {
-    // Rows behind the last one are read as the last one, and the last one, which others may be writing, from LDS.
-    const bool last = at < r0 + 32;
-    auto key_row = [&](int r) -> const uint8_t* { return K + (int64_t)min(r, at) * kKey; };
-    auto value_row = [&](int r) -> const uint8_t* { return V + (int64_t)min(r, at) * kValue; };
-    KeyCodes<GK> kc[2], kp[2], ks[2][4];
-    uint32_t vc[8];
-    KeyCodes<GV> vp[8];
+  for (; r0 < end; r0 += kStep) {
+    const PackedTile<GK, GV> now = tile;
+    wave_lds_fence();  // (the last tile's scales have been read)
+    if (t4 < 2) {
+      float k[GK], v[GV], base[GV];
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const uint8_t* const row = key_row(r0 + 16 * x + l15);
-      kc[x] = load_key<GK>(row + 4 * GK * t4);
-      kp[x] = load_params<GK>(row);
+      for (int g = 0; g < GK; ++g) k[g] = lo_f32(t4 ? now.kp[1].w[g] : now.kp[0].w[g]);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) ks[x][i] = load_params<GK>(key_row(r0 + 16 * x + 4 * t4 + i));
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const uint8_t* const row = value_row(r0 + 4 * t4 + 16 * (i >> 2) + (i & 3));
-      vc[i] = load_packed<GV>(row, l15);
-      vp[i] = load_params<GV>(row);
-    }
-    if (last) {
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        if (r0 + 16 * x + l15 >= at) kc[x] = load_key<GK>(fresh + 4 * GK * t4), kp[x] = load_params<GK>(fresh);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (r0 + 16 * x + 4 * t4 + i >= at) ks[x][i] = load_params<GK>(fresh);
+      for (int g = 0; g < GV; ++g) {
+        v[g] = lo_f32(now.vp.w[g]);
+        base[g] = fmaf(-Codes<T>::kOffset, v[g], hi_f32(now.vp.w[g]));
       }
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (r0 + 4 * t4 + 16 * (i >> 2) + (i & 3) >= at) vc[i] = load_packed<GV>(fresh + 80, l15), vp[i] = load_params<GV>(fresh + 80);
+      store_floats<GK>(kscale + lane * GK, k);
+      store_floats<GV>(vscale + lane * GV, v);
+      store_floats<GV>(vbase + lane * GV, base);
     }
+    wave_lds_fence();
+    if (r0 + kStep < end) load(r0 + kStep);
     // ---- scores of tokens 4 t4 .. +3 and 16 + 4 t4 .. +3 with query head l15
     float s[8];
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
       uint4 m = {0u, 0u, 0u, 0u};
-      m.x = kp[x].w[0];
-      if constexpr (GK >= 2) m.y = kp[x].w[1];
-      if constexpr (GK == 4) m.z = kp[x].w[2], m.w = kp[x].w[3];
-      f32x4 score = mfma_bf16(m, qsum, zero4());
+      m.x = now.kp[x].w[0];
+      if constexpr (GK >= 2) m.y = now.kp[x].w[1];
+      if constexpr (GK == 4) m.z = now.kp[x].w[2], m.w = now.kp[x].w[3];
+      f32x4 score = mfma_bf16(m, qsum, zero4()), acc[GK];
 #pragma unroll
       for (int g = 0; g < GK; ++g) {
         uint32_t u, w;
-        group_bytes<GK>(kc[x], g, u, w);
-        const uint4 e = {low_codes(u), low_codes(w), high_codes(u), high_codes(w)};
-        f32x4 acc = zero4();
+        group_bytes<GK>(now.kc[x], g, u, w);
+        const uint4 e = {codes.low(u), codes.low(w), codes.high(u), codes.high(w)};
+        acc[g] = zero4();
 #pragma unroll
-        for (int p = kPl - 1; p >= 0; --p) acc = mfma_bf16(e, qf[g][p], acc);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) score[i] = fmaf(lo_f32(ks[x][i].w[g]), acc[i], score[i]);
+        for (int p = kPl - 1; p >= 0; --p) acc[g] = mfma_bf16(e, qf[g][p], acc[g]);
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s[4 * x + i] = score[i];
-    }
-    float most = -INFINITY;
+      for (int i = 0; i < 4; ++i) {
+        const Floats<GK> scale = load_floats<GK>(kscale + (16 * x + 4 * t4 + i) * GK);
+        s[4 * x + i] = score[i];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      s[i] = r0 + 4 * t4 + 16 * (i >> 2) + (i & 3) > at ? -INFINITY : s[i];
-      most = fmaxf(most, s[i]);
+        for (int g = 0; g < GK; ++g) s[4 * x + i] = fmaf(scale.f[g], acc[g][i], s[4 * x + i]);
+      }
     }
+    if (at < r0 + 31) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s[i] = r0 + 4 * t4 + 16 * (i >> 2) + (i & 3) > at ? -INFINITY : s[i];
+    }
+    float most = s[0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) most = fmaxf(most, s[i]);
     most *= c;
     if (__ballot(most > top + 8.f)) {
       float next = fmaxf(most, __shfl_xor(most, 16));
@@ -236,39 +317,39 @@ __device__ __forceinline__ void packed_stretch_rows(const SoftmaxStepArgs& a, in
       for (int g = 0; g < GV; ++g) base[g] *= keep;
     }
     // ---- weights, times the scales, and the values
-    float z[8];
+    float z[8], y[GV][8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       z[i] = exp2_fast(fmaf(s[i], c, -top));
       sum += z[i];
+      const int row = 4 * t4 + 16 * (i >> 2) + (i & 3);
+      const Floats<GV> scale = load_floats<GV>(vscale + row * GV), least = load_floats<GV>(vbase + row * GV);
+#pragma unroll
+      for (int g = 0; g < GV; ++g) {
+        y[g][i] = z[i] * scale.f[g];
+        base[g] = fmaf(z[i], least.f[g], base[g]);
+      }
     }
     uint32_t pairs[4][2];  // bytes of tokens 2 i and 2 i + 1, groups 0, 1 and 2, 3
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      pairs[i][0] = __builtin_amdgcn_perm(vc[2 * i + 1], vc[2 * i], 0x05040100);
-      pairs[i][1] = __builtin_amdgcn_perm(vc[2 * i + 1], vc[2 * i], 0x07060302);
+      pairs[i][0] = __builtin_amdgcn_perm(now.vc[2 * i + 1], now.vc[2 * i], 0x05040100);
+      pairs[i][1] = __builtin_amdgcn_perm(now.vc[2 * i + 1], now.vc[2 * i], 0x07060302);
     }
 #pragma unroll
     for (int g = 0; g < GV; ++g) {
-      float y[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float scale = lo_f32(vp[i].w[g]);
-        y[i] = z[i] * scale;
-        base[g] = fmaf(z[i], fmaf(-16.f, scale, hi_f32(vp[i].w[g])), base[g]);
-      }
-      uint4 w[1][kWeight];
-      to_planes<kWeight>(y, w);
+      uint4 w[kWeight];
+      operand_of<kWeight>(y[g], w);
       uint32_t lo[4], hi[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const uint32_t x = pairs[i][g >> 1] >> (8 * (g & 1));
-        lo[i] = low_codes(x), hi[i] = high_codes(x);
+        const uint32_t x = g & 1 ? pairs[i][g >> 1] >> 8 : pairs[i][g >> 1];
+        lo[i] = codes.low(x), hi[i] = codes.high(x);
       }
 #pragma unroll
       for (int p = kWeight - 1; p >= 0; --p) {
-        o[2 * g] = mfma_bf16(uint4{lo[0], lo[1], lo[2], lo[3]}, w[0][p], o[2 * g]);
-        o[2 * g + 1] = mfma_bf16(uint4{hi[0], hi[1], hi[2], hi[3]}, w[0][p], o[2 * g + 1]);
+        o[2 * g] = mfma_bf16(uint4{lo[0], lo[1], lo[2], lo[3]}, w[p], o[2 * g]);
+        o[2 * g + 1] = mfma_bf16(uint4{hi[0], hi[1], hi[2], hi[3]}, w[p], o[2 * g + 1]);
       }
     }
   }
@@ -321,6 +402,7 @@ __global__ void __launch_bounds__(64 * kStepWaves, 2) softmax_step_packed_kernel
   extern __shared__ float sums_of[];  // [wave][member][dv]
   __shared__ StepState state[kStepWaves][kPackedMembers];
   __shared__ __attribute__((aligned(16))) uint8_t fresh[160];  // the new rows
+  __shared__ __attribute__((aligned(16))) float scales[kStepWaves * 32 * (GK + 2 * GV)];
   StepPlace f;
   if (!find_stretch(a, p, f)) return;
   const int id = blockIdx.x, heads_of = a.H * p.blocks, head = f.hb / p.blocks;
@@ -332,7 +414,7 @@ __global__ void __launch_bounds__(64 * kStepWaves, 2) softmax_step_packed_kernel
   packed_stretch_rows<T, GK, GV>(a, (int64_t)f.b * a.H + head, f.hb - head * p.blocks, at, first,
                                  min(at + 1, first + f.len * p.unit),
                                  f.count == 1 ? nullptr : sums + (int64_t)id * min(kPackedMembers, a.G) * (a.dv_ + 2), sums_of,
-                                 state, fresh);
+                                 state, fresh, scales);
 }
 
 template <typename T, int GK, int GV>
