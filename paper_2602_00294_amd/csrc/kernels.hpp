@@ -262,7 +262,7 @@ struct SoftmaxStepPlan {
   int unit = 128, least = 2, places = 0, workgroups = 0, blocks = 1, members = 32, fixed = 0, fixed_len = 0;
   size_t bytes = 0;
 };
-SoftmaxStepPlan plan_softmax_step(bool bf16, int heads, int H, int G, int capacity, int dv, int members = 32);
+SoftmaxStepPlan plan_softmax_step(bool bf16, int heads, int H, int G, int capacity, int dv, int members = 32, int places = 0);
 struct SoftmaxStepArgs {
   void *K, *V;         // [heads][capacity][d]
   const int* lengths;  // [heads / H]

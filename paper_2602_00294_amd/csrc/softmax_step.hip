@@ -193,12 +193,12 @@ hipError_t launch_step(const SoftmaxStepArgs& a, const SoftmaxStepPlan& p, hipSt
 
 }  // namespace
 
-SoftmaxStepPlan plan_softmax_step(bool bf16, int heads, int H, int G, int capacity, int dv, int members) {
+SoftmaxStepPlan plan_softmax_step(bool bf16, int heads, int H, int G, int capacity, int dv, int members, int places) {
   SoftmaxStepPlan p;
   p.members = members;
   p.blocks = (G + members - 1) / members;
   const int count = heads * p.blocks, units = (capacity + p.unit - 1) / p.unit, B = heads / H;
-  p.places = bf16 ? 512 : 256;
+  p.places = places ? places : bf16 ? 512 : 256;
   if ((int64_t)count * ((units + p.least - 1) / p.least) <= p.places) {
     p.fixed_len = p.least;  // (all find a place)
   } else if (B > 384) {

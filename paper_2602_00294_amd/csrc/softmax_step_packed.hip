@@ -34,6 +34,13 @@ namespace sata {
 
 namespace {
 
+// Workgroups of a CU.  Waves wait for loads more than they compute; the scheduling barriers below keep a tile's
+// parts apart so that three bfloat16 workgroups have registers enough (168 each, 14 of d_k = d_v = 128 in scratch).
+// 16 sequences, 8 key heads, caches of 16384 rows of 128 entries, ragged: 49.6 us with three, 53.2 with two, without the barriers 114
+// with three.  A float32 call's third plane takes the room of one.
+template <typename T>
+constexpr int kAtOnce = sizeof(T) == 2 ? 3 : 2;
+
 // G bytes for each of four a, as they lie in a key's row.
 template <int G>
 struct KeyCodes {
@@ -111,6 +118,36 @@ __device__ __forceinline__ void store_floats(float* p, const float (&x)[N]) {
   else *p = x[0];
 }
 
+// A cache of rows of 20 G bytes, read at a lane's offset from a row that is the same for the wave.
+template <int G>
+struct RowReader {
+  static constexpr int kRow = 20 * G;
+  __amdgpu_buffer_rsrc_t rsrc;
+  __device__ __forceinline__ RowReader(const uint8_t* p, int rows)
+      : rsrc(__builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), 0, rows * kRow, 0x00020000)) {}
+  __device__ __forceinline__ KeyCodes<G> dwords(int offset, int row) const {
+    typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+    typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+    KeyCodes<G> c;
+    if constexpr (G == 4) {
+      const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(rsrc, offset, row * kRow, 0);
+      c.w[0] = x.x, c.w[1] = x.y, c.w[2] = x.z, c.w[3] = x.w;
+    } else if constexpr (G == 2) {
+      const u32x2 x = __builtin_amdgcn_raw_buffer_load_b64(rsrc, offset, row * kRow, 0);
+      c.w[0] = x.x, c.w[1] = x.y;
+    } else {
+      c.w[0] = __builtin_amdgcn_raw_buffer_load_b32(rsrc, offset, row * kRow, 0);
+    }
+    return c;
+  }
+  // the G bytes of one a
+  __device__ __forceinline__ uint32_t bytes(int offset, int row) const {
+    if constexpr (G == 4) return __builtin_amdgcn_raw_buffer_load_b32(rsrc, offset, row * kRow, 0);
+    else if constexpr (G == 2) return (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rsrc, offset, row * kRow, 0);
+    else return (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(rsrc, offset, row * kRow, 0);
+  }
+};
+
 // A lane's part of 32 rows: codes and parameters of keys 16 x + l15, codes of values 4 t4 + i and 16 + 4 t4 + i,
 // parameters of value l31.
 template <int GK, int GV>
@@ -119,40 +156,41 @@ struct PackedTile {
   uint32_t vc[8];
   KeyCodes<GV> vp;
   // rows r0 .. r0 + 31, all before the last one
-  __device__ __forceinline__ void load(const uint8_t* K, const uint8_t* V, int r0) {
-    const int lane = threadIdx.x & 63, l15 = lane & 15, t4 = lane >> 4, l31 = lane & 31;
-    const uint8_t* const k = K + (int64_t)r0 * (20 * GK) + l15 * (20 * GK);
-    const uint8_t* const v = V + (int64_t)r0 * (20 * GV);
+  __device__ __forceinline__ void load_keys(const RowReader<GK>& K, int r0) {
+    const int lane = threadIdx.x & 63, l15 = lane & 15, t4 = lane >> 4;
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
-      kc[x] = load_key<GK>(k + 16 * x * (20 * GK) + 4 * GK * t4);
-      kp[x] = load_params<GK>(k + 16 * x * (20 * GK));
+      kc[x] = K.dwords(l15 * (20 * GK) + 4 * GK * t4 + 16 * x * (20 * GK), r0);
+      kp[x] = K.dwords(l15 * (20 * GK) + 16 * GK + 16 * x * (20 * GK), r0);
     }
-    const uint8_t* const c = v + 4 * t4 * (20 * GV) + l15 * GV;
+  }
+  __device__ __forceinline__ void load_values(const RowReader<GV>& V, int r0) {
+    const int lane = threadIdx.x & 63, l15 = lane & 15, t4 = lane >> 4, l31 = lane & 31;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) vc[i] = load_packed<GV>(c + (16 * (i >> 2) + (i & 3)) * (20 * GV), 0);
-    vp = load_params<GV>(v + l31 * (20 * GV));
+    for (int i = 0; i < 8; ++i) vc[i] = V.bytes(4 * t4 * (20 * GV) + l15 * GV + (16 * (i >> 2) + (i & 3)) * (20 * GV), r0);
+    vp = V.dwords(l31 * (20 * GV) + 16 * GV, r0);
   }
   // The same where row `at` is the last: rows behind it are read as that one, which others may be writing and which lies in
   // LDS (`fresh`, the value's 80 bytes on).
-  __device__ __forceinline__ void load_last(const uint8_t* K, const uint8_t* V, int r0, int at, const uint8_t* fresh) {
-    const int lane = threadIdx.x & 63, l15 = lane & 15, t4 = lane >> 4, l31 = lane & 31;
-    auto key = [&](int r) { return K + (int64_t)min(r, at) * (20 * GK); };
-    auto value = [&](int r) { return V + (int64_t)min(r, at) * (20 * GV); };
+  __device__ __forceinline__ void load_last_keys(const RowReader<GK>& K, int r0, int at, const uint8_t* fresh) {
+    const int lane = threadIdx.x & 63, l15 = lane & 15, t4 = lane >> 4;
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
-      const int r = r0 + 16 * x + l15;
-      kc[x] = load_key<GK>(key(r) + 4 * GK * t4);
-      kp[x] = load_params<GK>(key(r));
-      if (r >= at) kc[x] = load_key<GK>(fresh + 4 * GK * t4), kp[x] = load_params<GK>(fresh);
+      const int r = 16 * x + l15, row = min(r, at - r0) * (20 * GK);
+      kc[x] = K.dwords(row + 4 * GK * t4, r0);
+      kp[x] = K.dwords(row + 16 * GK, r0);
+      if (r0 + r >= at) kc[x] = load_key<GK>(fresh + 4 * GK * t4), kp[x] = load_params<GK>(fresh);
     }
+  }
+  __device__ __forceinline__ void load_last_values(const RowReader<GV>& V, int r0, int at, const uint8_t* fresh) {
+    const int lane = threadIdx.x & 63, l15 = lane & 15, t4 = lane >> 4, l31 = lane & 31;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const int r = r0 + 4 * t4 + 16 * (i >> 2) + (i & 3);
-      vc[i] = load_packed<GV>(value(r), l15);
-      if (r >= at) vc[i] = load_packed<GV>(fresh + 80, l15);
+      const int r = 4 * t4 + 16 * (i >> 2) + (i & 3);
+      vc[i] = V.bytes(min(r, at - r0) * (20 * GV) + l15 * GV, r0);
+      if (r0 + r >= at) vc[i] = load_packed<GV>(fresh + 80, l15);
     }
-    vp = load_params<GV>(value(r0 + l31));
+    vp = V.dwords(min(l31, at - r0) * (20 * GV) + 16 * GV, r0);
     if (r0 + l31 >= at) vp = load_params<GV>(fresh + 80);
   }
 };
@@ -244,44 +282,52 @@ __device__ __forceinline__ void packed_stretch_rows(const SoftmaxStepArgs& a, in
   float* const vscale = kscale + 32 * GK;
   float* const vbase = vscale + 32 * GV;
   PackedTile<GK, GV> tile;
-  auto load = [&](int r0) {
-    if (r0 + 32 <= at) tile.load(K, V, r0);
-    else tile.load_last(K, V, r0, at, fresh);
+  const RowReader<GK> keys(K, a.capacity);
+  const RowReader<GV> values(V, a.capacity);
+  auto load_keys = [&](int r0) {
+    if (r0 + 32 <= at) tile.load_keys(keys, r0);
+    else tile.load_last_keys(keys, r0, at, fresh);
+  };
+  auto load_values = [&](int r0) {
+    if (r0 + 32 <= at) tile.load_values(values, r0);
+    else tile.load_last_values(values, r0, at, fresh);
   };
   int r0 = first + 32 * wave;
-  if (r0 < end) load(r0);
+  if (r0 < end) {
+    load_keys(r0);
+    load_values(r0);
+  }
 #pragma unroll 1
   for (; r0 < end; r0 += kStep) {
-    const PackedTile<GK, GV> now = tile;
     wave_lds_fence();  // (the last tile's scales have been read)
     if (t4 < 2) {
       float k[GK], v[GV], base[GV];
 #pragma unroll
-      for (int g = 0; g < GK; ++g) k[g] = lo_f32(t4 ? now.kp[1].w[g] : now.kp[0].w[g]);
+      for (int g = 0; g < GK; ++g) k[g] = lo_f32(t4 ? tile.kp[1].w[g] : tile.kp[0].w[g]);
 #pragma unroll
       for (int g = 0; g < GV; ++g) {
-        v[g] = lo_f32(now.vp.w[g]);
-        base[g] = fmaf(-Codes<T>::kOffset, v[g], hi_f32(now.vp.w[g]));
+        v[g] = lo_f32(tile.vp.w[g]);
+        base[g] = fmaf(-Codes<T>::kOffset, v[g], hi_f32(tile.vp.w[g]));
       }
       store_floats<GK>(kscale + lane * GK, k);
       store_floats<GV>(vscale + lane * GV, v);
       store_floats<GV>(vbase + lane * GV, base);
     }
     wave_lds_fence();
-    if (r0 + kStep < end) load(r0 + kStep);
     // ---- scores of tokens 4 t4 .. +3 and 16 + 4 t4 .. +3 with query head l15
     float s[8];
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
+      __builtin_amdgcn_sched_barrier(0);
       uint4 m = {0u, 0u, 0u, 0u};
-      m.x = now.kp[x].w[0];
-      if constexpr (GK >= 2) m.y = now.kp[x].w[1];
-      if constexpr (GK == 4) m.z = now.kp[x].w[2], m.w = now.kp[x].w[3];
+      m.x = tile.kp[x].w[0];
+      if constexpr (GK >= 2) m.y = tile.kp[x].w[1];
+      if constexpr (GK == 4) m.z = tile.kp[x].w[2], m.w = tile.kp[x].w[3];
       f32x4 score = mfma_bf16(m, qsum, zero4()), acc[GK];
 #pragma unroll
       for (int g = 0; g < GK; ++g) {
         uint32_t u, w;
-        group_bytes<GK>(now.kc[x], g, u, w);
+        group_bytes<GK>(tile.kc[x], g, u, w);
         const uint4 e = {codes.low(u), codes.low(w), codes.high(u), codes.high(w)};
         acc[g] = zero4();
 #pragma unroll
@@ -299,6 +345,7 @@ __device__ __forceinline__ void packed_stretch_rows(const SoftmaxStepArgs& a, in
 #pragma unroll
       for (int i = 0; i < 8; ++i) s[i] = r0 + 4 * t4 + 16 * (i >> 2) + (i & 3) > at ? -INFINITY : s[i];
     }
+    if (r0 + kStep < end) load_keys(r0 + kStep);
     float most = s[0];
 #pragma unroll
     for (int i = 1; i < 8; ++i) most = fmaxf(most, s[i]);
@@ -317,39 +364,51 @@ __device__ __forceinline__ void packed_stretch_rows(const SoftmaxStepArgs& a, in
       for (int g = 0; g < GV; ++g) base[g] *= keep;
     }
     // ---- weights, times the scales, and the values
-    float z[8], y[GV][8];
+    __builtin_amdgcn_sched_barrier(0);
+    uint32_t pairs[4][2];  // bytes of tokens 2 i and 2 i + 1, groups 0, 1 and 2, 3
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      pairs[i][0] = __builtin_amdgcn_perm(tile.vc[2 * i + 1], tile.vc[2 * i], 0x05040100);
+      pairs[i][1] = __builtin_amdgcn_perm(tile.vc[2 * i + 1], tile.vc[2 * i], 0x07060302);
+    }
+    if (r0 + kStep < end) load_values(r0 + kStep);
+    float z[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       z[i] = exp2_fast(fmaf(s[i], c, -top));
       sum += z[i];
-      const int row = 4 * t4 + 16 * (i >> 2) + (i & 3);
-      const Floats<GV> scale = load_floats<GV>(vscale + row * GV), least = load_floats<GV>(vbase + row * GV);
-#pragma unroll
-      for (int g = 0; g < GV; ++g) {
-        y[g][i] = z[i] * scale.f[g];
-        base[g] = fmaf(z[i], least.f[g], base[g]);
-      }
     }
-    uint32_t pairs[4][2];  // bytes of tokens 2 i and 2 i + 1, groups 0, 1 and 2, 3
+    constexpr int kAt = GV < 2 ? GV : 2;  // groups at a time
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      pairs[i][0] = __builtin_amdgcn_perm(now.vc[2 * i + 1], now.vc[2 * i], 0x05040100);
-      pairs[i][1] = __builtin_amdgcn_perm(now.vc[2 * i + 1], now.vc[2 * i], 0x07060302);
-    }
+    for (int g0 = 0; g0 < GV; g0 += kAt) {
+      __builtin_amdgcn_sched_barrier(0);
+      float y[kAt][8];
 #pragma unroll
-    for (int g = 0; g < GV; ++g) {
-      uint4 w[kWeight];
-      operand_of<kWeight>(y[g], w);
-      uint32_t lo[4], hi[4];
+      for (int i = 0; i < 8; ++i) {
+        const int row = (4 * t4 + 16 * (i >> 2) + (i & 3)) * GV + g0;
+        const Floats<kAt> scale = load_floats<kAt>(vscale + row), least = load_floats<kAt>(vbase + row);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t x = g & 1 ? pairs[i][g >> 1] >> 8 : pairs[i][g >> 1];
-        lo[i] = codes.low(x), hi[i] = codes.high(x);
+        for (int g = 0; g < kAt; ++g) {
+          y[g][i] = z[i] * scale.f[g];
+          base[g0 + g] = fmaf(z[i], least.f[g], base[g0 + g]);
+        }
       }
 #pragma unroll
-      for (int p = kWeight - 1; p >= 0; --p) {
-        o[2 * g] = mfma_bf16(uint4{lo[0], lo[1], lo[2], lo[3]}, w[p], o[2 * g]);
-        o[2 * g + 1] = mfma_bf16(uint4{hi[0], hi[1], hi[2], hi[3]}, w[p], o[2 * g + 1]);
+      for (int g = 0; g < kAt; ++g) {
+        uint4 w[kWeight];
+        operand_of<kWeight>(y[g], w);
+        uint32_t lo[4], hi[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t x = g & 1 ? pairs[i][g0 >> 1] >> 8 : pairs[i][g0 >> 1];
+          lo[i] = codes.low(x), hi[i] = codes.high(x);
+        }
+        f32x4 &a0 = o[2 * (g0 + g)], &a1 = o[2 * (g0 + g) + 1];
+#pragma unroll
+        for (int p = kWeight - 1; p >= 0; --p) {
+          a0 = mfma_bf16(uint4{lo[0], lo[1], lo[2], lo[3]}, w[p], a0);
+          a1 = mfma_bf16(uint4{hi[0], hi[1], hi[2], hi[3]}, w[p], a1);
+        }
       }
     }
   }
@@ -398,7 +457,7 @@ __device__ __forceinline__ void packed_stretch_rows(const SoftmaxStepArgs& a, in
 }
 
 template <typename T, int GK, int GV>
-__global__ void __launch_bounds__(64 * kStepWaves, 2) softmax_step_packed_kernel(SoftmaxStepArgs a, SoftmaxStepPlan p) {
+__global__ void __launch_bounds__(64 * kStepWaves, kAtOnce<T>) softmax_step_packed_kernel(SoftmaxStepArgs a, SoftmaxStepPlan p) {
   extern __shared__ float sums_of[];  // [wave][member][dv]
   __shared__ StepState state[kStepWaves][kPackedMembers];
   __shared__ __attribute__((aligned(16))) uint8_t fresh[160];  // the new rows
@@ -447,7 +506,7 @@ hipError_t launch_keys(const SoftmaxStepArgs& a, const SoftmaxStepPlan& p, hipSt
 }  // namespace
 
 SoftmaxStepPlan plan_softmax_step_packed(bool bf16, int heads, int H, int G, int capacity, int dv) {
-  return plan_softmax_step(bf16, heads, H, G, capacity, dv, kPackedMembers);
+  return plan_softmax_step(bf16, heads, H, G, capacity, dv, kPackedMembers, 256 * (bf16 ? kAtOnce<uint16_t> : kAtOnce<float>));
 }
 
 hipError_t launch_softmax_step_packed(const SoftmaxStepArgs& a, bool bf16, hipStream_t s) {
