@@ -14,77 +14,6 @@ namespace sata {
 
 namespace {
 
-// Token by token: a thread has a column of the state in registers, the tokens' queries and keys lie in LDS.
-constexpr int kRows = 16;  // tokens staged at once
-
-template <typename T, int ND>
-__global__ void __launch_bounds__(64) delta_tokens_kernel(DeltaArgs a) {
-  constexpr int kD = 32 * ND;
-  __shared__ __attribute__((aligned(16))) float ks[kRows][kD], qs[kRows][kD];
-  __shared__ float decays[kRows], rates[kRows];
-  const int head = blockIdx.x, tid = threadIdx.x, col = blockIdx.y * 64 + tid;
-  const int64_t shared = head / a.G;
-  const bool on = col < a.dv;
-  const int len = tokens_of(a.lengths, head / (a.Hk * a.G), a.n);
-  const T* const q = (const T*)a.q + shared * a.n * a.dk;
-  const T* const k = (const T*)a.k + shared * a.n * a.dk;
-  const T* const v = (const T*)a.v + (int64_t)head * a.n * a.dv;
-  T* const y = (T*)a.y + (int64_t)head * a.n * a.dv;
-  float S[kD];
-#pragma unroll
-  for (int i = 0; i < kD; ++i) S[i] = a.S_in && on && i < a.dk ? a.S_in[((int64_t)head * a.dk + i) * a.dv + col] : 0.f;
-  for (int t0 = 0; t0 < len; t0 += kRows) {
-    const int m = min(kRows, len - t0);
-    __syncthreads();
-    for (int i = tid; i < m * kD; i += 64) {
-      const int r = i / kD, e = i % kD;
-      ks[r][e] = e < a.dk ? entry_of(k, (int64_t)(t0 + r) * a.dk + e) : 0.f;
-      qs[r][e] = e < a.dk ? entry_of(q, (int64_t)(t0 + r) * a.dk + e) : 0.f;
-    }
-    if (tid < m) {
-      decays[tid] = (float)exp(delta_rate(a.g[(int64_t)head * a.n + t0 + tid]));
-      rates[tid] = a.beta[(int64_t)head * a.n + t0 + tid];
-    }
-    __syncthreads();
-    for (int r = 0; r < m; ++r) {
-      const float lam = decays[r];
-      float p0 = 0.f, p1 = 0.f;
-#pragma unroll
-      for (int i = 0; i < kD; i += 2) {
-        S[i] *= lam, S[i + 1] *= lam;
-        p0 = fmaf(ks[r][i], S[i], p0), p1 = fmaf(ks[r][i + 1], S[i + 1], p1);
-      }
-      const float u = on ? rates[r] * (entry_of(v, (int64_t)(t0 + r) * a.dv + col) - (p0 + p1)) : 0.f;
-      p0 = p1 = 0.f;
-#pragma unroll
-      for (int i = 0; i < kD; i += 2) {
-        S[i] = fmaf(ks[r][i], u, S[i]), S[i + 1] = fmaf(ks[r][i + 1], u, S[i + 1]);
-        p0 = fmaf(qs[r][i], S[i], p0), p1 = fmaf(qs[r][i + 1], S[i + 1], p1);
-      }
-      if (on) y[(int64_t)(t0 + r) * a.dv + col] = rounded<T>((p0 + p1) * a.scale);
-    }
-  }
-  if (on) {
-    for (int t = len; t < a.n; ++t) y[(int64_t)t * a.dv + col] = (T)0;
-    if (a.S_out)
-#pragma unroll
-      for (int i = 0; i < kD; ++i)
-        if (i < a.dk) a.S_out[((int64_t)head * a.dk + i) * a.dv + col] = S[i];
-  }
-}
-
-template <typename T>
-hipError_t launch_tokens(const DeltaArgs& a, hipStream_t s) {
-  const dim3 grid(a.heads, (a.dv + 63) / 64);
-  switch ((a.dk + 31) / 32) {
-    case 1: hipLaunchKernelGGL((delta_tokens_kernel<T, 1>), grid, dim3(64), 0, s, a); break;
-    case 2: hipLaunchKernelGGL((delta_tokens_kernel<T, 2>), grid, dim3(64), 0, s, a); break;
-    case 3: hipLaunchKernelGGL((delta_tokens_kernel<T, 3>), grid, dim3(64), 0, s, a); break;
-    default: hipLaunchKernelGGL((delta_tokens_kernel<T, 4>), grid, dim3(64), 0, s, a); break;
-  }
-  return hipGetLastError();
-}
-
 // ---- block by block
 //
 // A wave has 16 columns of the state for a head's whole sequence, in the tiles of state_row; four of them share the staged
@@ -93,6 +22,9 @@ hipError_t launch_tokens(const DeltaArgs& a, hipStream_t s) {
 //     y = c early q S + P E,  S = whole S + k^T (late E),
 // each a product whose right operand is what the one before left in this lane.  Four more waves bring the next block
 // into LDS: issuing its loads costs a wave 3300 cycles of the 13000 that a block then took.
+//
+// A few tokens cost what a block costs, and still less than one by one with a column of the state a thread: 32 heads of 128,
+// pairs and scan, 13.7 us for 1 to 64 tokens, the other form 22.9 for one and 154 for 64.
 constexpr int kScanWaves = 4, kScanThreads = 2 * 64 * kScanWaves;
 
 // One of the buffers in LDS: a block's keys, queries, what its pairs left, and values of the workgroup's columns.
@@ -406,9 +338,10 @@ size_t delta_prefill_scratch(bool bf16, int heads, int, int n, int, int) {
 }
 
 hipError_t launch_delta_prefill(const DeltaArgs& a, bool bf16, void* scratch, hipStream_t s) {
-  if (a.n == 0) return bf16 ? launch_tokens<u16>(a, s) : launch_tokens<float>(a, s);
-  hipError_t e = launch_delta_pairs(a, bf16, scratch, nullptr, s);
-  if (e != hipSuccess) return e;
+  if (a.n > 0) {  // (without tokens, the states alone go on)
+    hipError_t e = launch_delta_pairs(a, bf16, scratch, nullptr, s);
+    if (e != hipSuccess) return e;
+  }
   return bf16 ? launch_scan_t<u16, false>(a, scratch, nullptr, nullptr, s) : launch_scan_t<float, false>(a, scratch, nullptr, nullptr, s);
 }
 
