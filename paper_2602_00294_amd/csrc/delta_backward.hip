@@ -13,6 +13,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "delta_tiles.hpp"
 
@@ -218,15 +219,14 @@ __global__ void __launch_bounds__(kBackScanThreads, 2) delta_back_kernel(DeltaAr
 
 // ---- block by block: a wave has 16 of 64 tokens and all columns of their dq and dk
 //
-// First dq and asked, which take what lies before a token (pairs with tokens j <= i, the state before the block); then, on top
+// float32 calls: first dq and asked, which take what lies before a token (pairs with tokens j <= i, the state before the block); then, on top
 // of asked, kept, which takes what lies behind (pairs with i >= j, the gradient of the state behind the block).  A pair's
 // weight is formed in both places, once for each side's rows, so that it is an operand where it is formed.
-template <typename T, int ND>
+template <int ND>
 struct BlockLds {
-  using W = DeltaTile<float, ND, kBlock>;  // errors, z, or gradients of the outputs; rows of a state
-  using L = DeltaTile<T, ND, kBlock>;      // queries or keys
+  using L = DeltaTile<float, ND, kBlock>;  // errors, z, gradients of the outputs or rows of a state; queries or keys
   using Half = DeltaTile<float, ND, 32>;
-  static constexpr int kBytes = W::kBytes + L::kBytes;
+  static constexpr int kBytes = 2 * L::kBytes;
 };
 
 // Sums over the lanes up to (or from) a lane's own.
@@ -288,366 +288,669 @@ __device__ __forceinline__ void by_rows(const f32x4 (&x)[2 * ND], float* buf, F&
 template <int ND>
 constexpr int by_rows_lanes() { return ND == 1 ? 4 : ND == 2 ? 8 : 16; }
 
-// MANY: several value heads to a query and key head, whose dq and dk are summed (in `sums`, [2][query and key heads][n][dk]).
-template <typename T, int ND, bool MANY>
-__global__ void __launch_bounds__(kBackThreads, sizeof(T) == 2 ? 2 : 1)
+// MANY: several value heads to a query and key head, whose dq and dk are each written to `sums`, [2][value heads][n][dk].
+template <int ND, bool MANY>
+__global__ void __launch_bounds__(kBackThreads, 1)
 delta_blocks_kernel(DeltaArgs a, const float* states, const float* behind, const float* errors, const float* zs, float* sums_) {
   extern __shared__ __attribute__((aligned(16))) u16 smem16[];
-  using D = BlockLds<T, ND>;
-  using W = typename D::W;
+  using T = float;
+  using D = BlockLds<ND>;
   using L = typename D::L;
   using Half = typename D::Half;
   constexpr int kPl = L::kPl;
   __shared__ double sums[kBlock];
   __shared__ float rates[kBlock], terms[kBlock], parts[kBackWaves];
   u16* const ta = smem16;
-  u16* const tb = smem16 + W::kElems;
+  u16* const tb = smem16 + L::kElems;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int blocks = (a.n + kBlock - 1) / kBlock, block = blockIdx.x, shared = blockIdx.y, t0 = block * kBlock;
+  const int blocks = (a.n + kBlock - 1) / kBlock, block = blockIdx.x, head = blockIdx.y, shared = MANY ? head / a.G : head, t0 = block * kBlock;
   const int len = tokens_of(a.lengths, shared / a.Hk, a.n), own = 16 * wave, last = min(a.n, t0 + kBlock);
-  const int64_t size = (int64_t)a.dk * a.dv, row0 = (int64_t)shared * a.n;
-  // rows behind the sequence
+  const int64_t size = (int64_t)a.dk * a.dv, row0 = (int64_t)shared * a.n, row = (int64_t)head * a.n;
+  // rows behind the sequence (several heads' sums: delta_sums_kernel)
   const int rest = max(t0, min(len, last));
-  for (int i = tid; i < (last - rest) * a.dk; i += kBackThreads) {
-    const int64_t at = (row0 + rest) * a.dk + i;
-    ((T*)a.dq)[at] = ((T*)a.dk_out)[at] = (T)0;
-  }
-  if (tid < kBlock && t0 + tid < last && t0 + tid >= len)
-    for (int v = 0; v < a.G; ++v) {
-      const int64_t at = ((int64_t)shared * a.G + v) * a.n + t0 + tid;
-      a.dg[at] = a.dbeta[at] = 0.f;
+  if (!MANY)
+    for (int i = tid; i < (last - rest) * a.dk; i += kBackThreads) {
+      const int64_t at = (row0 + rest) * a.dk + i;
+      ((T*)a.dq)[at] = ((T*)a.dk_out)[at] = (T)0;
     }
+  if (tid < kBlock && t0 + tid < last && t0 + tid >= len) a.dg[row + t0 + tid] = a.dbeta[row + t0 + tid] = 0.f;
   if (t0 >= len) return;
   float* const buf = (float*)ta + wave * 16 * (32 * ND + 4);
-  static_assert(kBackWaves * 16 * (32 * ND + 4) * 4 <= W::kBytes, "results lie in the errors' place");
-  const int members = MANY ? a.G : 1;
-#pragma unroll 1
-  for (int v = 0; v < members; ++v) {
-    int id = tid;
-    if (MANY) asm volatile("" : "+v"(id));  // (what hangs on it is not kept over the loop)
-    const int l15 = id & 15, t4 = (id & 63) >> 4;
-    const T* const q = (const T*)a.q + row0 * a.dk;
-    const T* const k = (const T*)a.k + row0 * a.dk;
-    const int64_t head = (int64_t)shared * a.G + v, row = head * a.n;
-    const float* const S = states + (head * blocks + block) * size;
-    const float* const U = behind + (head * blocks + block) * size;
-    RowAccess<float> E, Z;
-    RowAccess<T> dy;
-    E.init(errors + row * a.dv, len, a.dv);
-    Z.init(zs + row * a.dv, len, a.dv);
-    dy.init((const T*)a.dy + row * a.dv, len, a.dv);
-    DeltaStage<T, ND, kBlock, kBackThreads> sb;
-    DeltaStage<float, ND, kBlock, kBackThreads> sa;
-    sa.init(errors + row * a.dv, len, a.dv, id);
-    sa.fetch(t0);
-    sb.init(k, len, a.dk, id);
-    sb.fetch(t0);
-    __syncthreads();  // (the last value head's readers are done)
-    if (wave == 0) {
-      const bool there = t0 + lane < len;
-      sums[lane] = sum_up_to(there ? delta_rate(a.g[row + t0 + lane]) : 0.0);
-      rates[lane] = there ? a.beta[row + t0 + lane] : 0.f;
+  static_assert(kBackWaves * 16 * (32 * ND + 4) * 4 <= L::kBytes, "results lie in the errors' place");
+  const int l15 = lane & 15, t4 = lane >> 4;
+  const T* const q = (const T*)a.q + row0 * a.dk;
+  const T* const k = (const T*)a.k + row0 * a.dk;
+  const float* const S = states + ((int64_t)head * blocks + block) * size;
+  const float* const U = behind + ((int64_t)head * blocks + block) * size;
+  RowAccess<float> E, Z;
+  RowAccess<T> dy;
+  E.init(errors + row * a.dv, len, a.dv);
+  Z.init(zs + row * a.dv, len, a.dv);
+  dy.init((const T*)a.dy + row * a.dv, len, a.dv);
+  DeltaStage<T, ND, kBlock, kBackThreads> sb;
+  DeltaStage<float, ND, kBlock, kBackThreads> sa;
+  sa.init(errors + row * a.dv, len, a.dv, tid);
+  sa.fetch(t0);
+  sb.init(k, len, a.dk, tid);
+  sb.fetch(t0);
+  if (wave == 0) {
+    const bool there = t0 + lane < len;
+    sums[lane] = sum_up_to(there ? delta_rate(a.g[row + t0 + lane]) : 0.0);
+    rates[lane] = there ? a.beta[row + t0 + lane] : 0.f;
+  }
+  sa.put(ta, t0);
+  sb.put(tb, t0);
+  __syncthreads();
+  const int mine = own + l15;  // a token of this wave's, in the block
+  const double my_sum = sums[mine];
+  const float my_rate = rates[mine];
+  auto decay = [&](double d) { return exp2_fast((float)(d * 1.4426950408889634)); };
+  // dots of this wave's tokens' rows, of by_rows: sums over a row's lanes to `terms`
+  auto add_term = [&](float x, int token) {
+#pragma unroll
+    for (int d = 1; d < by_rows_lanes<ND>(); d *= 2) x += __shfl_xor(x, d);
+    if (lane % by_rows_lanes<ND>() == 0) terms[own + token] += x;
+  };
+  // a finished gradient's rows
+  auto finish = [&](int which, int token, int c0, float (&x)[8]) {
+    RowAccess<std::conditional_t<MANY, float, T>> out;
+    if constexpr (MANY) out.init(sums_ + ((int64_t)which * a.heads + head) * a.n * a.dk, len, a.dk);
+    else out.init((const T*)(which ? a.dk_out : a.dq) + row0 * a.dk, len, a.dk);
+    out.store(t0 + own + token, c0, x);
+  };
+  float asked_at[4] = {0.f, 0.f, 0.f, 0.f};  // k.asked of tokens own + 4 t4 .. +3, this lane's part
+  f32x4 sum_k[2 * ND];
+#pragma unroll
+  for (int j = 0; j < 2 * ND; ++j) sum_k[j] = zero4();
+  {
+    f32x4 dq[2 * ND];
+#pragma unroll
+    for (int j = 0; j < 2 * ND; ++j) dq[j] = zero4();
+    uint4 y[ND][kPl], z[ND][3];
+#pragma unroll
+    for (int s = 0; s < ND; ++s) {
+      dy.template operand<kPl>(t0 + mine, 32 * s + 8 * t4, y[s]);
+      Z.template operand<3>(t0 + mine, 32 * s + 8 * t4, z[s]);
     }
-    sa.put(ta, t0);
-    sb.put(tb, t0);
-    __syncthreads();
-    const int mine = own + l15;  // a token of this wave's, in the block
-    const double my_sum = sums[mine];
-    const float my_rate = rates[mine];
-    auto decay = [&](double d) { return exp2_fast((float)(d * 1.4426950408889634)); };
-    // dots of this wave's tokens' rows, of by_rows: sums over a row's lanes to `terms`
-    auto add_term = [&](float x, int token) {
-#pragma unroll
-      for (int d = 1; d < by_rows_lanes<ND>(); d *= 2) x += __shfl_xor(x, d);
-      if (lane % by_rows_lanes<ND>() == 0) terms[own + token] += x;
-    };
-    // a finished gradient's rows: summed over the value heads, or written
-    auto finish = [&](int which, int token, int c0, float (&x)[8]) {
-      if constexpr (MANY) {
-        RowAccess<float> total;
-        total.init(sums_ + ((int64_t)which * (a.heads / a.G) + shared) * a.n * a.dk, len, a.dk);
-        if (v > 0) {
-          float y[8];
-          total.load(t0 + own + token, c0, y);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) x[i] += y[i];
-        }
-        if (v + 1 < members) {
-          total.store(t0 + own + token, c0, x);
-          return;
-        }
-      }
-      RowAccess<T> out;
-      out.init((const T*)(which ? a.dk_out : a.dq) + row0 * a.dk, len, a.dk);
-      out.store(t0 + own + token, c0, x);
-    };
-    float asked_at[4] = {0.f, 0.f, 0.f, 0.f};  // k.asked of tokens own + 4 t4 .. +3, this lane's part
-    f32x4 sum_k[2 * ND];
-#pragma unroll
-    for (int j = 0; j < 2 * ND; ++j) sum_k[j] = zero4();
-    {
-      f32x4 dq[2 * ND];
-#pragma unroll
-      for (int j = 0; j < 2 * ND; ++j) dq[j] = zero4();
-      uint4 y[ND][kPl], z[ND][3];
+    // ---- pairs of this wave's tokens i with j <= i: rows of one and two
+#pragma unroll 1
+    for (int jb = 0; 32 * jb <= own; ++jb) {
+      float one[8], two[8];
+      f32x4 p[2] = {zero4(), zero4()}, r[2] = {zero4(), zero4()};
 #pragma unroll
       for (int s = 0; s < ND; ++s) {
-        dy.template operand<kPl>(t0 + mine, 32 * s + 8 * t4, y[s]);
-        Z.template operand<3>(t0 + mine, 32 * s + 8 * t4, z[s]);
+        uint4 e[2][3];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) rows16<L>(ta, 32 * jb + 16 * x, s, e[x]);
+        dots_left16(e, y[s], p);
+        dots_left16(e, z[s], r);
       }
-      // ---- pairs of this wave's tokens i with j <= i: rows of one and two
-#pragma unroll 1
-      for (int jb = 0; 32 * jb <= own; ++jb) {
-        float one[8], two[8];
-        f32x4 p[2] = {zero4(), zero4()}, r[2] = {zero4(), zero4()};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int j = 32 * jb + 16 * (e >> 2) + 4 * t4 + (e & 3);
+        const float d = decay(my_sum - sums[j]) * rates[j];
+        one[e] = j <= mine ? p[e >> 2][e & 3] * d * a.scale : 0.f;
+        two[e] = j < mine ? -(r[e >> 2][e & 3] * d * my_rate) : 0.f;
+      }
+      uint4 op[3], tp[3];
+      operand_of<3>(one, op);
+      operand_of<3>(two, tp);
+#pragma unroll
+      for (int j = 0; j < 2 * ND; j += 2) {
+        __builtin_amdgcn_sched_barrier(0);
+        uint4 e[2][kPl];
+        f32x4 w[2] = {dq[j], dq[j + 1]}, u[2] = {sum_k[j], sum_k[j + 1]};
+#pragma unroll
+        for (int x = 0; x < 2; ++x) columns16<L>(tb, 32 * jb, j + x, e[x]);
+        dots_right16(op, e, w);
+        dots_right16(tp, e, u);
+        dq[j] = w[0], dq[j + 1] = w[1], sum_k[j] = u[0], sum_k[j + 1] = u[1];
+      }
+      settle_mfma();
+    }
+    // ---- the state before the block, 32 rows at a time
+    float early[4], rate[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) early[r] = decay(sums[own + 4 * t4 + r]), rate[r] = rates[own + 4 * t4 + r];
+    DeltaStage<float, ND, 32, kBackThreads> ss;
+    ss.init(S, a.dk, a.dv, tid);
+    ss.fetch(0);
+#pragma unroll
+    for (int b = 0; b < ND; ++b)
+      if (32 * b < a.dk) {
+        __syncthreads();
+        ss.put(ta, 32 * b);
+        __syncthreads();
+        if (32 * b + 32 < a.dk) ss.fetch(32 * b + 32);
+        f32x4 of_y[2] = {zero4(), zero4()}, of_z[2] = {zero4(), zero4()};
 #pragma unroll
         for (int s = 0; s < ND; ++s) {
           uint4 e[2][3];
 #pragma unroll
-          for (int x = 0; x < 2; ++x) rows16<W>(ta, 32 * jb + 16 * x, s, e[x]);
-          dots_left16(e, y[s], p);
-          dots_left16(e, z[s], r);
+          for (int x = 0; x < 2; ++x) rows16<Half>(ta, 16 * x, s, e[x]);
+          dots_right16(y[s], e, of_y);
+          dots_right16(z[s], e, of_z);
         }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int j = 32 * jb + 16 * (e >> 2) + 4 * t4 + (e & 3);
-          const float d = decay(my_sum - sums[j]) * rates[j];
-          one[e] = j <= mine ? p[e >> 2][e & 3] * d * a.scale : 0.f;
-          two[e] = j < mine ? -(r[e >> 2][e & 3] * d * my_rate) : 0.f;
-        }
-        uint4 op[3], tp[3];
-        operand_of<3>(one, op);
-        operand_of<3>(two, tp);
+        for (int x = 0; x < 2; ++x)
 #pragma unroll
-        for (int j = 0; j < 2 * ND; j += 2) {
-          __builtin_amdgcn_sched_barrier(0);
-          uint4 e[2][kPl];
-          f32x4 w[2] = {dq[j], dq[j + 1]}, u[2] = {sum_k[j], sum_k[j + 1]};
-#pragma unroll
-          for (int x = 0; x < 2; ++x) columns16<L>(tb, 32 * jb, j + x, e[x]);
-          dots_right16(op, e, w);
-          dots_right16(tp, e, u);
-          dq[j] = w[0], dq[j + 1] = w[1], sum_k[j] = u[0], sum_k[j + 1] = u[1];
-        }
+          for (int r = 0; r < 4; ++r) {
+            dq[2 * b + x][r] = fmaf(of_y[x][r], early[r] * a.scale, dq[2 * b + x][r]);
+            sum_k[2 * b + x][r] = fmaf(-of_z[x][r], early[r] * rate[r], sum_k[2 * b + x][r]);
+          }
         settle_mfma();
       }
-      // ---- the state before the block, 32 rows at a time
-      float early[4], rate[4];
+    // ---- dq is done; asked with the keys
 #pragma unroll
-      for (int r = 0; r < 4; ++r) early[r] = decay(sums[own + 4 * t4 + r]), rate[r] = rates[own + 4 * t4 + r];
-      DeltaStage<float, ND, 32, kBackThreads> ss;
-      ss.init(S, a.dk, a.dv, id);
-      ss.fetch(0);
+    for (int j = 0; j < 2 * ND; ++j)
 #pragma unroll
-      for (int b = 0; b < ND; ++b)
-        if (32 * b < a.dk) {
-          __syncthreads();
-          ss.put(ta, 32 * b);
-          __syncthreads();
-          if (32 * b + 32 < a.dk) ss.fetch(32 * b + 32);
-          f32x4 of_y[2] = {zero4(), zero4()}, of_z[2] = {zero4(), zero4()};
+      for (int r = 0; r < 4; ++r)
+        asked_at[r] = fmaf(tile_entry<L>(tb, own + 4 * t4 + r, 16 * j + l15), sum_k[j][r], asked_at[r]);
+    if (lane < 16) terms[own + lane] = 0.f;
+    __syncthreads();
+    RowAccess<T> rq;
+    rq.init(q, len, a.dk);
+    by_rows<ND>(dq, buf, [&](int token, int c0, float (&x)[8]) {
+      float w[8], dot = 0.f;
+      rq.load(t0 + own + token, c0, w);
 #pragma unroll
-          for (int s = 0; s < ND; ++s) {
-            uint4 e[2][3];
+      for (int i = 0; i < 8; ++i) dot = fmaf(w[i], x[i], dot);
+      add_term(dot, token);
+      finish(0, token, c0, x);
+    });
+  }
+  // ---- pairs of tokens i with this wave's j <= i: columns of one, then of two
+  uint4 e_own[ND][3];
+  {
+    DeltaStage<T, ND, kBlock, kBackThreads> sy;
+    sy.init((const T*)a.dy + row * a.dv, len, a.dv, tid);
+    sy.fetch(t0);
+    sb.init(q, len, a.dk, tid);
+    sb.fetch(t0);
+    float dot = 0.f;
 #pragma unroll
-            for (int x = 0; x < 2; ++x) rows16<Half>(ta, 16 * x, s, e[x]);
-            dots_right16(y[s], e, of_y);
-            dots_right16(z[s], e, of_z);
-          }
+    for (int s = 0; s < ND; ++s) {
+      float x[8], w[8];
+      E.load(t0 + mine, 32 * s + 8 * t4, x);
+      Z.load(t0 + mine, 32 * s + 8 * t4, w);
 #pragma unroll
-          for (int x = 0; x < 2; ++x)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              dq[2 * b + x][r] = fmaf(of_y[x][r], early[r] * a.scale, dq[2 * b + x][r]);
-              sum_k[2 * b + x][r] = fmaf(-of_z[x][r], early[r] * rate[r], sum_k[2 * b + x][r]);
-            }
-          settle_mfma();
-        }
-      // ---- dq is done; asked with the keys
-#pragma unroll
-      for (int j = 0; j < 2 * ND; ++j)
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-          asked_at[r] = fmaf(tile_entry<L>(tb, own + 4 * t4 + r, 16 * j + l15), sum_k[j][r], asked_at[r]);
-      if (lane < 16) terms[own + lane] = 0.f;
-      __syncthreads();
-      RowAccess<T> rq;
-      rq.init(q, len, a.dk);
-      by_rows<ND>(dq, buf, [&](int token, int c0, float (&x)[8]) {
-        float w[8], dot = 0.f;
-        rq.load(t0 + own + token, c0, w);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) dot = fmaf(w[i], x[i], dot);
-        add_term(dot, token);
-        finish(0, token, c0, x);
-      });
+      for (int i = 0; i < 8; ++i) dot = fmaf(x[i], w[i], dot);
+      operand_of<3>(x, e_own[s]);
     }
-    // ---- pairs of tokens i with this wave's j <= i: columns of one, then of two
-    uint4 e_own[ND][3];
-    {
-      DeltaStage<T, ND, kBlock, kBackThreads> sy;
-      sy.init((const T*)a.dy + row * a.dv, len, a.dv, id);
-      sy.fetch(t0);
-      sb.init(q, len, a.dk, id);
+    dot += __shfl_xor(dot, 16);
+    dot += __shfl_xor(dot, 32);
+    if (t4 == 0 && t0 + mine < len) a.dbeta[row + t0 + mine] = dot;
+    __syncthreads();
+    sy.put(ta, t0);
+    sb.put(tb, t0);
+    __syncthreads();
+  }
+#pragma unroll 1
+  for (int turn = 0; turn < 2; ++turn) {
+    if (turn == 1) {
+      sa.init(zs + row * a.dv, len, a.dv, tid);
+      sa.fetch(t0);
+      sb.init(k, len, a.dk, tid);
       sb.fetch(t0);
-      float dot = 0.f;
-#pragma unroll
-      for (int s = 0; s < ND; ++s) {
-        float x[8], w[8];
-        E.load(t0 + mine, 32 * s + 8 * t4, x);
-        Z.load(t0 + mine, 32 * s + 8 * t4, w);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) dot = fmaf(x[i], w[i], dot);
-        operand_of<3>(x, e_own[s]);
-      }
-      dot += __shfl_xor(dot, 16);
-      dot += __shfl_xor(dot, 32);
-      if (t4 == 0 && t0 + mine < len) a.dbeta[row + t0 + mine] = dot;
       __syncthreads();
-      sy.put(ta, t0);
+      sa.put(ta, t0);
       sb.put(tb, t0);
       __syncthreads();
     }
 #pragma unroll 1
-    for (int turn = 0; turn < 2; ++turn) {
-      if (turn == 1) {
-        sa.init(zs + row * a.dv, len, a.dv, id);
-        sa.fetch(t0);
-        sb.init(k, len, a.dk, id);
-        sb.fetch(t0);
-        __syncthreads();
-        sa.put(ta, t0);
-        sb.put(tb, t0);
-        __syncthreads();
+    for (int ib = own / 32; ib < 2; ++ib) {
+      float w[8];
+      f32x4 p[2] = {zero4(), zero4()};
+#pragma unroll
+      for (int s = 0; s < ND; ++s) {
+        uint4 e[2][3];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) rows16<L>(ta, 32 * ib + 16 * x, s, e[x]);
+        dots_left16(e, e_own[s], p);
       }
-#pragma unroll 1
-      for (int ib = own / 32; ib < 2; ++ib) {
-        float w[8];
-        f32x4 p[2] = {zero4(), zero4()};
-        if (turn == 0) {
+      settle_mfma();
 #pragma unroll
-          for (int s = 0; s < ND; ++s) {
-            uint4 e[2][kPl];
+      for (int e = 0; e < 8; ++e) {
+        const int i = 32 * ib + 16 * (e >> 2) + 4 * t4 + (e & 3);
+        const float d = p[e >> 2][e & 3] * (decay(sums[i] - my_sum) * my_rate);
+        w[e] = turn == 0 ? (i >= mine ? d * a.scale : 0.f) : i > mine ? -(d * rates[i]) : 0.f;
+      }
+      uint4 op[3];
+      operand_of<3>(w, op);
 #pragma unroll
-            for (int x = 0; x < 2; ++x) rows16<L>(ta, 32 * ib + 16 * x, s, e[x]);
-            dots_left16(e, e_own[s], p);
+      for (int j = 0; j < 2 * ND; j += 2) {
+        __builtin_amdgcn_sched_barrier(0);
+        uint4 e[2][kPl];
+        f32x4 u[2] = {sum_k[j], sum_k[j + 1]};
+#pragma unroll
+        for (int x = 0; x < 2; ++x) columns16<L>(tb, 32 * ib, j + x, e[x]);
+        dots_right16(op, e, u);
+        sum_k[j] = u[0], sum_k[j + 1] = u[1];
+      }
+      settle_mfma();
+    }
+  }
+  // ---- the gradient of the state behind the block
+  float inner = 0.f, late_terms = 0.f;
+  {
+    const double end = sums[kBlock - 1];
+    float late[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) late[r] = decay(end - sums[own + 4 * t4 + r]) * rates[own + 4 * t4 + r];
+    DeltaStage<float, ND, 32, kBackThreads> ss, su;
+    ss.init(S, a.dk, a.dv, tid);
+    su.init(U, a.dk, a.dv, tid);
+    su.fetch(0);
+    ss.fetch(0);
+#pragma unroll
+    for (int b = 0; b < ND; ++b)
+      if (32 * b < a.dk) {
+        __syncthreads();
+        su.put(ta, 32 * b);
+        if (su.vec && ss.vec) {
+#pragma unroll
+          for (int i = 0; i < su.kIt; ++i) {
+            inner = fmaf(__uint_as_float(ss.r[i].x), __uint_as_float(su.r[i].x), inner);
+            inner = fmaf(__uint_as_float(ss.r[i].y), __uint_as_float(su.r[i].y), inner);
+            inner = fmaf(__uint_as_float(ss.r[i].z), __uint_as_float(su.r[i].z), inner);
+            inner = fmaf(__uint_as_float(ss.r[i].w), __uint_as_float(su.r[i].w), inner);
           }
         } else {
+          for (int i = tid; i < min(32, a.dk - 32 * b) * a.dv; i += kBackThreads)
+            inner = fmaf(S[(int64_t)32 * b * a.dv + i], U[(int64_t)32 * b * a.dv + i], inner);
+        }
+        __syncthreads();
+        if (32 * b + 32 < a.dk) {
+          su.fetch(32 * b + 32);
+          ss.fetch(32 * b + 32);
+        }
+        f32x4 of_e[2] = {zero4(), zero4()};
 #pragma unroll
-          for (int s = 0; s < ND; ++s) {
-            uint4 e[2][3];
+        for (int s = 0; s < ND; ++s) {
+          uint4 e[2][3];
 #pragma unroll
-            for (int x = 0; x < 2; ++x) rows16<W>(ta, 32 * ib + 16 * x, s, e[x]);
-            dots_left16(e, e_own[s], p);
+          for (int x = 0; x < 2; ++x) rows16<Half>(ta, 16 * x, s, e[x]);
+          dots_right16(e_own[s], e, of_e);
+        }
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const float e = of_e[x][r] * late[r];
+            late_terms = fmaf(tile_entry<L>(tb, own + 4 * t4 + r, 32 * b + 16 * x + l15), e, late_terms);
+            sum_k[2 * b + x][r] += e;
           }
-        }
-        settle_mfma();
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int i = 32 * ib + 16 * (e >> 2) + 4 * t4 + (e & 3);
-          const float d = p[e >> 2][e & 3] * (decay(sums[i] - my_sum) * my_rate);
-          w[e] = turn == 0 ? (i >= mine ? d * a.scale : 0.f) : i > mine ? -(d * rates[i]) : 0.f;
-        }
-        uint4 op[3];
-        operand_of<3>(w, op);
-#pragma unroll
-        for (int j = 0; j < 2 * ND; j += 2) {
-          __builtin_amdgcn_sched_barrier(0);
-          uint4 e[2][kPl];
-          f32x4 u[2] = {sum_k[j], sum_k[j + 1]};
-#pragma unroll
-          for (int x = 0; x < 2; ++x) columns16<L>(tb, 32 * ib, j + x, e[x]);
-          dots_right16(op, e, u);
-          sum_k[j] = u[0], sum_k[j + 1] = u[1];
-        }
         settle_mfma();
       }
+    inner *= decay(end);
+  }
+  // ---- dk, and the gradient of g (asked counts for it: with kept it has been taken off)
+  __syncthreads();
+  RowAccess<T> rk;
+  rk.init(k, len, a.dk);
+  by_rows<ND>(sum_k, buf, [&](int token, int c0, float (&x)[8]) {
+    float w[8], dot = 0.f;
+    rk.load(t0 + own + token, c0, w);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) dot = fmaf(w[i], x[i], dot);
+    add_term(-dot, token);
+    finish(1, token, c0, x);
+  });
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+#pragma unroll
+    for (int d = 1; d < 16; d *= 2) asked_at[r] += __shfl_xor(asked_at[r], d);
+    wave_lds_fence();
+    if (l15 == r) terms[own + 4 * t4 + r] += 2.f * asked_at[r];
+  }
+  inner += late_terms;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) inner += __shfl_xor(inner, d);
+  if (lane == 0) parts[wave] = inner;
+  __syncthreads();
+  if (wave == 0) {
+    double sum = sum_from(terms[lane]);
+#pragma unroll
+    for (int w = 0; w < kBackWaves; ++w) sum += parts[w];
+    if (t0 + lane < len) a.dg[row + t0 + lane] = (float)sum;
+  }
+}
+
+// ---- the same for bfloat16 calls, whose tiles of a block lie in LDS together: eight waves, each with 16 tokens and one of the two
+// parts.  The first four form dq and asked: pairs with tokens j <= i, the state before the block; the others
+// kept: pairs with i >= j, the gradient behind it.  A block's rows are read once, its states once, 32 rows of both at
+// a time, and the two parts of dk meet in LDS.  (Of a SIMD's two waves one has the longer part of the pairs, the other the shorter.)
+template <int ND>
+struct SplitLds {
+  using W = DeltaTile<float, ND, kBlock>;  // errors, z; later rows of the states
+  using L = DeltaTile<u16, ND, kBlock>;    // gradients of the outputs, keys, queries
+  using Half = DeltaTile<float, ND, 32>;
+  static constexpr int kRows = 16 * (32 * ND + 4);  // floats of a wave's place in by_rows
+  static constexpr int kBytes = 2 * W::kBytes + 3 * L::kBytes;
+  static_assert(2 * Half::kBytes <= W::kBytes, "rows of both states lie in the errors' place, or z's");
+  static_assert(kBackWaves * 2 * ND * 1024 + 2 * kBackWaves * kRows * 4 <= 2 * W::kBytes + L::kBytes, "results lie in front of the keys");
+};
+constexpr int kSplitThreads = 2 * kBackThreads;
+
+template <int ND, bool MANY>
+__global__ void __launch_bounds__(kSplitThreads, 2)
+delta_split_kernel(DeltaArgs a, const float* states, const float* behind, const float* errors, const float* zs, float* sums_) {
+  extern __shared__ __attribute__((aligned(16))) u16 smem16[];
+  using T = u16;
+  using D = SplitLds<ND>;
+  using W = typename D::W;
+  using L = typename D::L;
+  using Half = typename D::Half;
+  __shared__ double sums[kBlock];
+  __shared__ float rates[kBlock], terms[2][kBlock], parts[2 * kBackWaves];
+  u16 *const te = smem16, *const tz = te + W::kElems, *const ty = tz + W::kElems, *const tk = ty + L::kElems, *const tq = tk + L::kElems;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), own = 16 * (wave % kBackWaves);
+  const bool asks = wave < kBackWaves;
+  const int blocks = (a.n + kBlock - 1) / kBlock, block = blockIdx.x, head = blockIdx.y, shared = MANY ? head / a.G : head, t0 = block * kBlock;
+  const int len = tokens_of(a.lengths, shared / a.Hk, a.n), last = min(a.n, t0 + kBlock);
+  const int64_t size = (int64_t)a.dk * a.dv, row0 = (int64_t)shared * a.n, row = (int64_t)head * a.n;
+  // rows behind the sequence (several heads' sums: delta_sums_kernel)
+  const int rest = max(t0, min(len, last));
+  if (!MANY)
+    for (int i = tid; i < (last - rest) * a.dk; i += kSplitThreads) {
+      const int64_t at = (row0 + rest) * a.dk + i;
+      ((T*)a.dq)[at] = ((T*)a.dk_out)[at] = (T)0;
     }
-    // ---- the gradient of the state behind the block
-    float inner = 0.f, late_terms = 0.f;
-    {
-      const double end = sums[kBlock - 1];
-      float late[4];
-#pragma unroll
-      for (int r = 0; r < 4; ++r) late[r] = decay(end - sums[own + 4 * t4 + r]) * rates[own + 4 * t4 + r];
-      DeltaStage<float, ND, 32, kBackThreads> ss, su;
-      ss.init(S, a.dk, a.dv, id);
-      su.init(U, a.dk, a.dv, id);
-      su.fetch(0);
-      ss.fetch(0);
-#pragma unroll
-      for (int b = 0; b < ND; ++b)
-        if (32 * b < a.dk) {
-          __syncthreads();
-          su.put(ta, 32 * b);
-          if (su.vec && ss.vec) {
-#pragma unroll
-            for (int i = 0; i < su.kIt; ++i) {
-              inner = fmaf(__uint_as_float(ss.r[i].x), __uint_as_float(su.r[i].x), inner);
-              inner = fmaf(__uint_as_float(ss.r[i].y), __uint_as_float(su.r[i].y), inner);
-              inner = fmaf(__uint_as_float(ss.r[i].z), __uint_as_float(su.r[i].z), inner);
-              inner = fmaf(__uint_as_float(ss.r[i].w), __uint_as_float(su.r[i].w), inner);
-            }
-          } else {
-            for (int i = tid; i < min(32, a.dk - 32 * b) * a.dv; i += kBackThreads)
-              inner = fmaf(S[(int64_t)32 * b * a.dv + i], U[(int64_t)32 * b * a.dv + i], inner);
-          }
-          __syncthreads();
-          if (32 * b + 32 < a.dk) {
-            su.fetch(32 * b + 32);
-            ss.fetch(32 * b + 32);
-          }
-          f32x4 of_e[2] = {zero4(), zero4()};
-#pragma unroll
-          for (int s = 0; s < ND; ++s) {
-            uint4 e[2][3];
-#pragma unroll
-            for (int x = 0; x < 2; ++x) rows16<Half>(ta, 16 * x, s, e[x]);
-            dots_right16(e_own[s], e, of_e);
-          }
-#pragma unroll
-          for (int x = 0; x < 2; ++x)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              const float e = of_e[x][r] * late[r];
-              late_terms = fmaf(tile_entry<L>(tb, own + 4 * t4 + r, 32 * b + 16 * x + l15), e, late_terms);
-              sum_k[2 * b + x][r] += e;
-            }
-          settle_mfma();
-        }
-      inner *= decay(end);
+  if (tid < kBlock && t0 + tid < last && t0 + tid >= len) a.dg[row + t0 + tid] = a.dbeta[row + t0 + tid] = 0.f;
+  if (t0 >= len) return;
+  const int l15 = lane & 15, t4 = lane >> 4;
+  const float* const S = states + ((int64_t)head * blocks + block) * size;
+  const float* const U = behind + ((int64_t)head * blocks + block) * size;
+  DeltaStage<float, ND, 32, kSplitThreads> ss, su;
+  ss.init(S, a.dk, a.dv, tid);
+  su.init(U, a.dk, a.dv, tid);
+  {
+    DeltaStage<float, ND, kBlock, kSplitThreads> se, sz;
+    DeltaStage<T, ND, kBlock, kSplitThreads> sy, sk, sq;
+    se.init(errors + row * a.dv, len, a.dv, tid);
+    se.fetch(t0);
+    sy.init((const T*)a.dy + row * a.dv, len, a.dv, tid);
+    sy.fetch(t0);
+    sz.init(zs + row * a.dv, len, a.dv, tid);
+    sz.fetch(t0);
+    sk.init((const T*)a.k + row0 * a.dk, len, a.dk, tid);
+    sq.init((const T*)a.q + row0 * a.dk, len, a.dk, tid);
+    sk.fetch(t0);
+    sq.fetch(t0);
+      if (wave == 0) {
+      const bool there = t0 + lane < len;
+      sums[lane] = sum_up_to(there ? delta_rate(a.g[row + t0 + lane]) : 0.0);
+      rates[lane] = there ? a.beta[row + t0 + lane] : 0.f;
     }
-    // ---- dk, and the gradient of g (asked counts for it: with kept it has been taken off)
-    __syncthreads();
-    RowAccess<T> rk;
-    rk.init(k, len, a.dk);
-    by_rows<ND>(sum_k, buf, [&](int token, int c0, float (&x)[8]) {
-      float w[8], dot = 0.f;
-      rk.load(t0 + own + token, c0, w);
+    se.put(te, t0);
+    sy.put(ty, t0);
+    sz.put(tz, t0);
+    sk.put(tk, t0);
+    sq.put(tq, t0);
+  }
+  ss.fetch(0);
+  su.fetch(0);
+  __syncthreads();
+  const int mine = own + l15;  // a token of this wave's, in the block
+  const double my_sum = sums[mine];
+  const float my_rate = rates[mine];
+  auto decay = [&](double d) { return exp2_fast((float)(d * 1.4426950408889634)); };
+  // Rows of the states, 32 at a time, from registers into the errors' and z's places in turn.
+  float inner = 0.f;  // this thread's part of <S, U>
+  const bool vec = su.vec && ss.vec;
+  auto next_rows = [&](int b) {
+    u16* const to = b & 1 ? tz : te;
+    if (b == 0) __syncthreads();  // (the errors and z have been read)
+    ss.put(to, 32 * b);
+    su.put(to + Half::kElems, 32 * b);
+    if (vec) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) dot = fmaf(w[i], x[i], dot);
-      add_term(-dot, token);
-      finish(1, token, c0, x);
-    });
+      for (int i = 0; i < su.kIt; ++i) {
+        inner = fmaf(__uint_as_float(ss.r[i].x), __uint_as_float(su.r[i].x), inner);
+        inner = fmaf(__uint_as_float(ss.r[i].y), __uint_as_float(su.r[i].y), inner);
+        inner = fmaf(__uint_as_float(ss.r[i].z), __uint_as_float(su.r[i].z), inner);
+        inner = fmaf(__uint_as_float(ss.r[i].w), __uint_as_float(su.r[i].w), inner);
+      }
+    } else {
+      for (int i = tid; i < min(32, a.dk - 32 * b) * a.dv; i += kSplitThreads)
+        inner = fmaf(S[(int64_t)32 * b * a.dv + i], U[(int64_t)32 * b * a.dv + i], inner);
+    }
+    __syncthreads();  // (and the rows before the last ones have been read)
+    if (32 * b + 32 < a.dk) {
+      ss.fetch(32 * b + 32);
+      su.fetch(32 * b + 32);
+    }
+    return to;
+  };
+  // what a wave's sums over columns add to its tokens' terms
+  auto add_terms = [&](float (&x)[4]) {
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
 #pragma unroll
-      for (int d = 1; d < 16; d *= 2) asked_at[r] += __shfl_xor(asked_at[r], d);
-      wave_lds_fence();
-      if (l15 == r) terms[own + 4 * t4 + r] += 2.f * asked_at[r];
+      for (int d = 1; d < 16; d *= 2) x[r] += __shfl_xor(x[r], d);
+      if (l15 == r) terms[asks ? 0 : 1][own + 4 * t4 + r] = x[r];
     }
-    inner += late_terms;
+  };
+  f32x4* const meet = (f32x4*)smem16 + own / 16 * 2 * ND * 64;
+  float* const buf = (float*)smem16 + kBackWaves * 2 * ND * 256 + wave * D::kRows;
+  // a finished gradient's rows
+  auto finish = [&](int which, int token, int c0, float (&x)[8]) {
+    RowAccess<std::conditional_t<MANY, float, T>> out;
+    if constexpr (MANY) out.init(sums_ + ((int64_t)which * a.heads + head) * a.n * a.dk, len, a.dk);
+    else out.init((const T*)(which ? a.dk_out : a.dq) + row0 * a.dk, len, a.dk);
+    out.store(t0 + own + token, c0, x);
+  };
+  if (asks) {
+    f32x4 dq[2 * ND], asked[2 * ND];
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) inner += __shfl_xor(inner, d);
-    if (lane == 0) parts[wave] = inner;
+    for (int j = 0; j < 2 * ND; ++j) dq[j] = asked[j] = zero4();
+    uint4 y[ND][1], z[ND][3];
+#pragma unroll
+    for (int s = 0; s < ND; ++s) {
+      rows16<L>(ty, own, s, y[s]);
+      rows16<W>(tz, own, s, z[s]);
+    }
+#pragma unroll 1
+    for (int jb = 0; 32 * jb <= own; ++jb) {
+      float one[8], two[8];
+      f32x4 p[2] = {zero4(), zero4()}, r[2] = {zero4(), zero4()};
+#pragma unroll
+      for (int s = 0; s < ND; ++s) {
+        uint4 e[2][3];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) rows16<W>(te, 32 * jb + 16 * x, s, e[x]);
+        dots_left16(e, y[s], p);
+        dots_left16(e, z[s], r);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int j = 32 * jb + 16 * (e >> 2) + 4 * t4 + (e & 3);
+        const float d = decay(my_sum - sums[j]) * rates[j];
+        one[e] = j <= mine ? p[e >> 2][e & 3] * d * a.scale : 0.f;
+        two[e] = j < mine ? -(r[e >> 2][e & 3] * d * my_rate) : 0.f;
+        if (j == mine && t0 + mine < len) a.dbeta[row + t0 + mine] = r[e >> 2][e & 3];  // (z.E of one token)
+      }
+      uint4 op[3], tp[3];
+      operand_of<3>(one, op);
+      operand_of<3>(two, tp);
+#pragma unroll
+      for (int j = 0; j < 2 * ND; j += 2) {
+        __builtin_amdgcn_sched_barrier(0);
+        uint4 e[2][1];
+        f32x4 w[2] = {dq[j], dq[j + 1]}, u[2] = {asked[j], asked[j + 1]};
+#pragma unroll
+        for (int x = 0; x < 2; ++x) columns16<L>(tk, 32 * jb, j + x, e[x]);
+        dots_right16(op, e, w);
+        dots_right16(tp, e, u);
+        dq[j] = w[0], dq[j + 1] = w[1], asked[j] = u[0], asked[j + 1] = u[1];
+      }
+      settle_mfma();
+    }
+    // ---- the state before the block
+    float early[4], rate[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) early[r] = decay(sums[own + 4 * t4 + r]), rate[r] = rates[own + 4 * t4 + r];
+#pragma unroll
+    for (int b = 0; b < ND; ++b)
+      if (32 * b < a.dk) {
+        const u16* const rows = next_rows(b);
+        f32x4 of_y[2] = {zero4(), zero4()}, of_z[2] = {zero4(), zero4()};
+#pragma unroll
+        for (int s = 0; s < ND; ++s) {
+          uint4 e[2][3];
+#pragma unroll
+          for (int x = 0; x < 2; ++x) rows16<Half>(rows, 16 * x, s, e[x]);
+          dots_right16(y[s], e, of_y);
+          dots_right16(z[s], e, of_z);
+        }
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            dq[2 * b + x][r] = fmaf(of_y[x][r], early[r] * a.scale, dq[2 * b + x][r]);
+            asked[2 * b + x][r] = fmaf(-of_z[x][r], early[r] * rate[r], asked[2 * b + x][r]);
+          }
+        settle_mfma();
+      }
+    float at[4] = {0.f, 0.f, 0.f, 0.f};  // q.dq + k.asked
+#pragma unroll
+    for (int j = 0; j < 2 * ND; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        at[r] = fmaf(tile_entry<L>(tq, own + 4 * t4 + r, 16 * j + l15), dq[j][r], at[r]);
+        at[r] = fmaf(tile_entry<L>(tk, own + 4 * t4 + r, 16 * j + l15), asked[j][r], at[r]);
+      }
+    add_terms(at);
+    __syncthreads();  // (the states have been read)
+#pragma unroll
+    for (int j = 0; j < 2 * ND; ++j) meet[j * 64 + lane] = asked[j];
     __syncthreads();
-    if (wave == 0) {
-      double sum = sum_from(terms[lane]);
+    by_rows<ND>(dq, buf, [&](int token, int c0, float (&x)[8]) { finish(0, token, c0, x); });
+  } else {
+    f32x4 kept[2 * ND];
 #pragma unroll
-      for (int w = 0; w < kBackWaves; ++w) sum += parts[w];
-      if (t0 + lane < len) a.dg[row + t0 + lane] = (float)sum;
+    for (int j = 0; j < 2 * ND; ++j) kept[j] = zero4();
+    uint4 e_own[ND][3];
+#pragma unroll
+    for (int s = 0; s < ND; ++s) rows16<W>(te, own, s, e_own[s]);
+#pragma unroll 1
+    for (int ib = own / 32; ib < 2; ++ib) {
+      float one[8], two[8];
+      f32x4 p[2] = {zero4(), zero4()}, r[2] = {zero4(), zero4()};
+#pragma unroll
+      for (int s = 0; s < ND; ++s) {
+        uint4 y[2][1], z[2][3];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          rows16<L>(ty, 32 * ib + 16 * x, s, y[x]);
+          rows16<W>(tz, 32 * ib + 16 * x, s, z[x]);
+        }
+        dots_left16(y, e_own[s], p);
+        dots_left16(z, e_own[s], r);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int i = 32 * ib + 16 * (e >> 2) + 4 * t4 + (e & 3);
+        const float d = decay(sums[i] - my_sum) * my_rate;
+        one[e] = i >= mine ? p[e >> 2][e & 3] * d * a.scale : 0.f;
+        two[e] = i > mine ? -(r[e >> 2][e & 3] * d * rates[i]) : 0.f;
+      }
+      uint4 op[3], tp[3];
+      operand_of<3>(one, op);
+      operand_of<3>(two, tp);
+#pragma unroll
+      for (int j = 0; j < 2 * ND; j += 2) {
+        __builtin_amdgcn_sched_barrier(0);
+        uint4 q[2][1], k[2][1];
+        f32x4 u[2] = {kept[j], kept[j + 1]};
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          columns16<L>(tq, 32 * ib, j + x, q[x]);
+          columns16<L>(tk, 32 * ib, j + x, k[x]);
+        }
+        dots_right16(op, q, u);
+        dots_right16(tp, k, u);
+        kept[j] = u[0], kept[j + 1] = u[1];
+      }
+      settle_mfma();
     }
+    // ---- the gradient of the state behind the block
+    const double end = sums[kBlock - 1];
+    float late[4], late_terms = 0.f;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) late[r] = decay(end - sums[own + 4 * t4 + r]) * rates[own + 4 * t4 + r];
+#pragma unroll
+    for (int b = 0; b < ND; ++b)
+      if (32 * b < a.dk) {
+        const u16* const rows = next_rows(b) + Half::kElems;
+        f32x4 of_e[2] = {zero4(), zero4()};
+#pragma unroll
+        for (int s = 0; s < ND; ++s) {
+          uint4 e[2][3];
+#pragma unroll
+          for (int x = 0; x < 2; ++x) rows16<Half>(rows, 16 * x, s, e[x]);
+          dots_right16(e_own[s], e, of_e);
+        }
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const float e = of_e[x][r] * late[r];
+            late_terms = fmaf(tile_entry<L>(tk, own + 4 * t4 + r, 32 * b + 16 * x + l15), e, late_terms);
+            kept[2 * b + x][r] += e;
+          }
+        settle_mfma();
+      }
+    float at[4] = {0.f, 0.f, 0.f, 0.f};  // -k.kept
+#pragma unroll
+    for (int j = 0; j < 2 * ND; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) at[r] = fmaf(-tile_entry<L>(tk, own + 4 * t4 + r, 16 * j + l15), kept[j][r], at[r]);
+    add_terms(at);
+    inner = fmaf(inner, decay(end), late_terms);
+    __syncthreads();
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < 2 * ND; ++j) kept[j] += meet[j * 64 + lane];
+    by_rows<ND>(kept, buf, [&](int token, int c0, float (&x)[8]) { finish(1, token, c0, x); });
+  }
+  if (asks) inner *= decay(sums[kBlock - 1]);
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) inner += __shfl_xor(inner, d);
+  if (lane == 0) parts[wave] = inner;
+  __syncthreads();
+  if (wave == 0) {  // the gradient of g
+    double sum = sum_from(terms[0][lane] + terms[1][lane]);
+#pragma unroll
+    for (int w = 0; w < 2 * kBackWaves; ++w) sum += parts[w];
+    if (t0 + lane < len) a.dg[row + t0 + lane] = (float)sum;
+  }
+}
+
+// dq and dk of query and key heads, sums over the value heads' in their order; zero behind a sequence.  x: entries at once.
+template <typename T, int X>
+__global__ void __launch_bounds__(256) delta_sums_kernel(DeltaArgs a, const float* sums) {
+  const int64_t count = (int64_t)a.n * a.dk, heads = a.heads / a.G;
+  const int shared = blockIdx.y % heads, which = blockIdx.y / heads;
+  const int64_t end = (int64_t)tokens_of(a.lengths, shared / a.Hk, a.n) * a.dk;
+  for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * X; i < count; i += (int64_t)gridDim.x * 256 * X) {
+    const float* const from = sums + ((int64_t)which * a.heads + (int64_t)shared * a.G) * count + i;
+    T* const to = (T*)(which ? a.dk_out : a.dq) + shared * count + i;
+    float x[X] = {};
+    if (i < end)
+      for (int v = 0; v < a.G; ++v) {
+        if constexpr (X == 4) {
+          const float4 f = *(const float4*)(from + v * count);
+          x[0] += f.x, x[1] += f.y, x[2] += f.z, x[3] += f.w;
+        } else {
+          x[0] += from[v * count];
+        }
+      }
+    if constexpr (X == 4 && sizeof(T) == 2) *(uint2*)to = uint2{pack2(x[0], x[1]), pack2(x[2], x[3])};
+    else if constexpr (X == 4) *(float4*)to = float4{x[0], x[1], x[2], x[3]};
+    else to[0] = rounded<T>(x[0]);
   }
 }
 
@@ -666,7 +969,7 @@ Places places_of(bool bf16, int heads, int G, int n, int dk, int dv) {
   p.errors = p.behind + whole(blocks * dk * dv * sizeof(float));
   p.zs = p.errors + whole((size_t)heads * n * dv * sizeof(float));
   p.sums = p.zs + whole((size_t)heads * n * dv * sizeof(float));
-  p.bytes = p.sums + (G > 1 ? 2 * whole((size_t)(heads / G) * n * dk * sizeof(float)) : 0);
+  p.bytes = p.sums + (G > 1 ? 2 * (size_t)heads * n * dk * sizeof(float) : 0);
   return p;
 }
 
@@ -689,19 +992,34 @@ hipError_t launch_back(const DeltaArgs& a, const void* data, float* behind, floa
 template <typename T, int ND, bool MANY>
 hipError_t launch_blocks_of(const DeltaArgs& a, const float* states, const float* behind, const float* errors, const float* zs,
                             float* sums, hipStream_t s) {
-  constexpr int bytes = BlockLds<T, ND>::kBytes;
-  static_assert(bytes <= 158 * 1024, "LDS of one workgroup");
-  auto kern = delta_blocks_kernel<T, ND, MANY>;
-  hipError_t e = raise_lds(kern, bytes);
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(kern, dim3((a.n + kBlock - 1) / kBlock, a.heads / a.G), dim3(kBackThreads), bytes, s, a, states, behind, errors, zs, sums);
-  return hipGetLastError();
+  const dim3 grid((a.n + kBlock - 1) / kBlock, a.heads);
+  auto start = [&](auto kern, int threads, int bytes) {
+    hipError_t e = raise_lds(kern, bytes);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(kern, grid, dim3(threads), bytes, s, a, states, behind, errors, zs, sums);
+    return hipGetLastError();
+  };
+  if constexpr (sizeof(T) == 2) {
+    static_assert(SplitLds<ND>::kBytes <= 158 * 1024, "LDS of one workgroup");
+    return start(delta_split_kernel<ND, MANY>, kSplitThreads, SplitLds<ND>::kBytes);
+  } else {
+    static_assert(BlockLds<ND>::kBytes <= 158 * 1024, "LDS of one workgroup");
+    return start(delta_blocks_kernel<ND, MANY>, kBackThreads, BlockLds<ND>::kBytes);
+  }
 }
 template <typename T, int ND>
 hipError_t launch_blocks(const DeltaArgs& a, const float* states, const float* behind, const float* errors, const float* zs,
                          float* sums, hipStream_t s) {
-  return a.G > 1 ? launch_blocks_of<T, ND, true>(a, states, behind, errors, zs, sums, s)
-                 : launch_blocks_of<T, ND, false>(a, states, behind, errors, zs, sums, s);
+  if (a.G == 1) return launch_blocks_of<T, ND, false>(a, states, behind, errors, zs, sums, s);
+  hipError_t e = launch_blocks_of<T, ND, true>(a, states, behind, errors, zs, sums, s);
+  if (e != hipSuccess) return e;
+  const bool fours = a.dk % 4 == 0 && (((uintptr_t)a.dq | (uintptr_t)a.dk_out) & (4 * sizeof(T) - 1)) == 0;
+  const int64_t vectors = (int64_t)a.n * a.dk / (fours ? 4 : 1);
+  const int rows = 2 * (a.heads / a.G);
+  const dim3 grid((unsigned)std::min<int64_t>((vectors + 255) / 256, std::max(1, (1 << 22) / rows)), rows);
+  if (fours) hipLaunchKernelGGL((delta_sums_kernel<T, 4>), grid, dim3(256), 0, s, a, sums);
+  else hipLaunchKernelGGL((delta_sums_kernel<T, 1>), grid, dim3(256), 0, s, a, sums);
+  return hipGetLastError();
 }
 
 template <typename T>
