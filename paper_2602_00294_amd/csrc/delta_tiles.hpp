@@ -346,15 +346,15 @@ struct StateColumns {
 };
 
 // Workgroups to heads and slices of columns: an XCD takes whole heads, whose queries and keys are then read through one L2.
-__device__ __forceinline__ bool delta_place(int heads, int slices, int& head, int& slice) {
+__device__ __forceinline__ bool delta_place(int workgroup, int heads, int slices, int& head, int& slice) {
   if (heads >= 8) {
-    const int j = blockIdx.x >> 3;
-    head = j / slices * 8 + (int)(blockIdx.x & 7);
+    const int j = workgroup >> 3;
+    head = j / slices * 8 + (workgroup & 7);
     slice = j % slices;
     return head < heads;
   }
-  head = blockIdx.x / slices;
-  slice = blockIdx.x % slices;
+  head = workgroup / slices;
+  slice = workgroup % slices;
   return true;
 }
 inline unsigned delta_grid(int heads, int slices) { return (unsigned)((heads >= 8 ? (heads + 7) / 8 * 8 : heads) * slices); }
@@ -362,7 +362,5 @@ inline unsigned delta_grid(int heads, int slices) { return (unsigned)((heads >= 
 // Records [head][block] of DeltaForward and, where `backward`, DeltaBackward.
 hipError_t launch_delta_pairs(const DeltaArgs& a, bool bf16, void* forward, void* backward, hipStream_t s);
 size_t delta_forward_bytes(bool bf16, int heads, int n);
-// The states before every block and the errors E of a call's tokens: what gradients start from.
-hipError_t launch_delta_states(const DeltaArgs& a, bool bf16, const void* forward, float* states, float* errors, hipStream_t s);
 
 }  // namespace sata
