@@ -7,6 +7,7 @@ not been built, loading fails with an error; there is no fallback.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 import re
 from typing import Optional, Tuple
@@ -152,18 +153,24 @@ def feature_index(d: int, P: int, f: int) -> Tuple[int, ...]:
 
 # ------------------------------------------------------------------ tensor calls
 
+_torch_module = None
+
+
 def _torch():
-    import torch
-    return torch
+    global _torch_module
+    if _torch_module is None:
+        import torch
+        _torch_module = torch
+    return _torch_module
 
 
 def _dtype_code(t) -> int:
-    torch = _torch()
-    if t.dtype == torch.float32:
+    torch, dtype = _torch(), t.dtype
+    if dtype == torch.float32:
         return SATA_F32
-    if t.dtype == torch.bfloat16:
+    if dtype == torch.bfloat16:
         return SATA_BF16
-    raise TypeError(f"unsupported dtype {t.dtype}; use float32 or bfloat16")
+    raise TypeError(f"unsupported dtype {dtype}; use float32 or bfloat16")
 
 
 def _check_tensor(t, name: str, device=None):
@@ -176,13 +183,14 @@ def _check_tensor(t, name: str, device=None):
 
 
 def _check_same_dtype(ref, **tensors):
+    dtype = ref.dtype
     for name, t in tensors.items():
-        if t.dtype != ref.dtype:
-            raise TypeError(f"{name} is {t.dtype}, expected {ref.dtype} like q")
+        if t.dtype != dtype:
+            raise TypeError(f"{name} is {t.dtype}, expected {dtype} like q")
 
 
 def _check_shape(t, name: str, shape):
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape and tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
 
 
@@ -210,13 +218,12 @@ def _raw_stream(index: int) -> int:
 def _invoke(name: str, device, *args):
     """Calls a function of the library on `device` and its current stream.  (A token's call is a few
     microseconds of work: the device is changed only where it has to be.)"""
-    torch = _torch()
-    func = getattr(load_library(), name)
-    if torch.cuda.current_device() == device.index:
-        _check(func(*args, _raw_stream(device.index)), name)
+    func, index = getattr(load_library(), name), device.index
+    if _torch().cuda.current_device() == index:
+        _check(func(*args, _raw_stream(index)), name)
     else:
-        with torch.cuda.device(device):
-            _check(func(*args, _raw_stream(device.index)), name)
+        with _torch().cuda.device(device):
+            _check(func(*args, _raw_stream(index)), name)
 
 
 def _at(t):
@@ -491,9 +498,8 @@ def decode_step_grouped(S, q, k, v, P: int, y=None):
 
 def _check_sizes(*sizes):
     """ctypes hands the library the low 32 bits of a size, whatever it is."""
-    for size in sizes:
-        if size >= 1 << 31:
-            raise ValueError(f"a size of {size} does not fit in 32 bits")
+    if max(sizes) >= 1 << 31:
+        raise ValueError(f"a size of {max(sizes)} does not fit in 32 bits")
 
 
 def _prompt_sizes(q, k, v):
@@ -538,8 +544,9 @@ def _check_as(t, name: str, dtype, shape):
 
 
 def _check_tensors(device, **tensors):
+    index = device.index  # (asked for by its number, a tensor's device takes half the time)
     for name, t in tensors.items():
-        if t is not None:
+        if t is not None and (t.get_device() != index or not t.is_contiguous()):
             _check_tensor(t, name, device)
 
 
@@ -682,17 +689,16 @@ def _delta_sizes(q, k, v, dims: int):
     """(dtype code, B, H_qk, G, n, d_k, d_v) of q, k [B, H_qk(, n), d_k] and v [B, G*H_qk(, n), d_v] of `dims` dimensions."""
     code = _dtype_code(q)
     _check_same_dtype(q, k=k, v=v)
-    rows = ", n" if dims == 4 else ""
-    if q.dim() != dims or k.dim() != dims or v.dim() != dims:
+    qs, vs = q.shape, v.shape
+    if not len(qs) == len(vs) == k.dim() == dims:
+        rows = ", n" if dims == 4 else ""
         raise ValueError(f"q, k [B, H_qk{rows}, d_k] and v [B, G*H_qk{rows}, d_v] expected")
-    B, H, dk = q.shape[0], q.shape[1], q.shape[-1]
-    Hv, dv = v.shape[1], v.shape[-1]
+    B, H, dk, Hv, dv = qs[0], qs[1], qs[-1], vs[1], vs[-1]
     if H < 1 or Hv % H or Hv < H:
         raise ValueError("the value head count must be a multiple of the query and key head count")
-    n = q.shape[2] if dims == 4 else 1
-    tokens = (n,) if dims == 4 else ()
-    _check_shape(k, "k", (B, H, *tokens, dk))
-    _check_shape(v, "v", (B, Hv, *tokens, dv))
+    n = qs[2] if dims == 4 else 1
+    _check_shape(k, "k", qs)
+    _check_shape(v, "v", (B, Hv, *qs[2:-1], dv))
     _check_sizes(B, Hv, n, dk, dv)
     return code, B, H, Hv // H, n, dk, dv
 
@@ -716,7 +722,7 @@ def delta_prefill(q, k, v, g, beta, lengths=None, S_in=None, want_state: bool = 
     _check_as(S, "S", torch.float32, (B, G * H, dk, dv))
     _check_tensors(q.device, q=q, k=k, v=v, g=g, beta=beta, lengths=lengths, S_in=S_in, y=y, S=S)
     if y is None:
-        y = torch.empty(B, G * H, n, dv, dtype=q.dtype, device=q.device)
+        y = torch.empty_like(v)
     if want_state and S is None:
         S = torch.empty(B, G * H, dk, dv, dtype=torch.float32, device=q.device)
     scratch = _scratch(load_library().sata_delta_scratch(0, code, B, H, G, n, dk, dv), q.device)
@@ -736,7 +742,7 @@ def delta_step(S, q, k, v, g, beta, y=None):
     _check_as(y, "y", q.dtype, (B, G * H, dv))
     _check_tensors(q.device, S=S, q=q, k=k, v=v, g=g, beta=beta, y=y)
     if y is None:
-        y = torch.empty(B, G * H, dv, dtype=q.dtype, device=q.device)
+        y = torch.empty_like(v)
     _invoke("sata_delta_step", q.device, _at(S), _at(q), _at(k), _at(v), _at(g), _at(beta), code, B, H, G, dk, dv, _at(y))
     return y
 
@@ -834,6 +840,7 @@ def rotary_backward(dq, dk, positions, inv_freq, interleaved: bool = False, scal
 
 # ------------------------------------------------------------------ caches of 4 bits an entry
 
+@functools.lru_cache(maxsize=None)
 def packed_row_bytes(d: int) -> int:
     """Bytes of a row of d entries (1 to 128) in a cache of 4 bits an entry, a scale and a least value for every 32."""
     _check_sizes(d)
@@ -844,13 +851,19 @@ def packed_row_bytes(d: int) -> int:
 
 
 def _check_packed(cache, name: str, B, H, d):
-    torch = _torch()
-    if cache.dtype != torch.uint8:
+    if cache.dtype != _torch().uint8:
         raise TypeError(f"{name} is {cache.dtype}, expected torch.uint8")
     if cache.dim() != 4:
         raise ValueError(f"{name} must be [B, H_kv, capacity, row bytes]")
-    _check_sizes(cache.shape[2])
-    _check_shape(cache, name, (B, H, cache.shape[2], packed_row_bytes(d)))
+    capacity = cache.shape[2]
+    _check_sizes(capacity)
+    _check_shape(cache, name, (B, H, capacity, packed_row_bytes(d)))
+
+
+@functools.lru_cache(maxsize=1024)
+def _packed_scratch(B: int, H: int, G: int, capacity: int, dv: int) -> int:
+    """(Asked for once for a call's sizes: the question costs as much as a tenth of the call.)"""
+    return int(load_library().sata_softmax_step_packed_scratch(B, H, G, capacity, dv))
 
 
 def packed_write(K, V, first, k, v, counts=None):
@@ -917,7 +930,7 @@ def softmax_step_packed(K, V, lengths, q, k, v, y=None):
     _check_tensors(q.device, K=K, V=V, lengths=lengths, q=q, k=k, v=v, y=y)
     if y is None:
         y = torch.empty(B, G * H, dv, dtype=q.dtype, device=q.device)
-    scratch = _scratch(load_library().sata_softmax_step_packed_scratch(B, H, G, cap, dv), q.device)
+    scratch = _scratch(_packed_scratch(B, H, G, cap, dv), q.device)
     _invoke("sata_softmax_step_packed", q.device, _at(K), _at(V), cap, _at(lengths), _at(q), _at(k), _at(v), code, B, H, G,
             dk, dv, _at(y), _at(scratch))
     return y
