@@ -243,3 +243,52 @@ def test_off_whole_vectors(sata, B, H, G, n, dk, dv, dtype):
     assert torch.equal(y, y2) and torch.equal(S1, S2)
     for a, b in zip(grads, sata.delta_backward(*o, _off(dy), S_in=_off(S), dS=_off(S1))):
         assert torch.equal(a, b)
+
+
+def test_most_heads(sata):
+    """65535 heads, the most that a call takes: some of them as alone, bit by bit; one more is refused."""
+    most = 65535
+    print("most heads", file=sys.stderr, flush=True)
+    for B, Hk, G in ((most, 1, 1), (1, most // 3, 3)):
+        q, k, v, g, beta, S = (x.cuda() for x in ref.draw(41, B, Hk, G, 2, 4, 3, "f32", state=True))
+        y, S1 = sata.delta_prefill(q, k, v, g, beta, S_in=S)
+        grads = sata.delta_backward(q, k, v, g, beta, v, S_in=S, dS=S1)
+        S2 = S1.clone()
+        tokens = [x[:, :, 1].contiguous() for x in (q, k, v, g, beta)]
+        yt = sata.delta_step(S2, *tokens)
+        for h in (0, 255, 256, most // G - 1):
+            part = (slice(h, h + 1), slice(None)) if B > 1 else (slice(None), slice(h, h + 1))
+            many = part if B > 1 else (slice(None), slice(G * h, G * h + G))
+            a = [x[part].contiguous() for x in (q, k)] + [x[many].contiguous() for x in (v, g, beta)]
+            o, T = sata.delta_prefill(*a, S_in=S[many].contiguous())
+            assert torch.equal(o, y[many]) and torch.equal(T, S1[many])
+            alone = sata.delta_backward(*a, a[2], S_in=S[many].contiguous(), dS=T)
+            for i, (x, z) in enumerate(zip(alone, grads)):
+                assert torch.equal(x, z[part if i < 2 else many]), (h, i)
+            assert torch.equal(sata.delta_step(T, *(x[:, :, 1].contiguous() for x in a)), yt[many])
+    x = torch.randn(1, most, 1, 8, device="cuda")
+    pos = torch.full((1, 1), 7, dtype=torch.int32, device="cuda")
+    freq, _ = sata.rotary_frequencies(4)
+    tq, tk = sata.rotary(x, x, pos, freq)
+    assert torch.equal(tq, tk) and torch.equal(tq[:, -1:], sata.rotary(x[:, -1:].contiguous(), None, pos, freq)[0])
+    cK, cV = (torch.zeros(1, most, 3, sata.packed_row_bytes(8), dtype=torch.uint8, device="cuda") for _ in range(2))
+    sata.packed_write(cK, cV, None, x, x)
+    at = torch.ones(1, dtype=torch.int32, device="cuda")
+    one = x[:, :, 0].contiguous()
+    y = sata.softmax_step_packed(cK, cV, at, one, one, one)
+    last = [c[:, -1:].contiguous() for c in (cK, cV)]
+    assert torch.equal(y[:, -1:], sata.softmax_step_packed(*last, at, *(one[:, -1:].contiguous() for _ in range(3))))
+    assert torch.equal(sata.packed_read(cK, None, 2, 8, torch.float32)[:, :, 0], sata.packed_read(cK, None, 2, 8, torch.float32)[:, :, 1])
+    with pytest.raises(sata.SataError):
+        z = torch.zeros(1, most + 1, 1, 8, device="cuda")
+        sata.delta_prefill(z, z, z, z[..., 0].contiguous(), z[..., 0].contiguous())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_gradients_with_lengths_out_of_range(sata, dtype):
+    q, k, v, g, beta, S = (x.cuda() for x in ref.draw(51, 3, 1, 2, 70, 16, 16, dtype, state=True))
+    out = [sata.delta_backward(q, k, v, g, beta, v, lengths=torch.tensor(L, dtype=torch.int32, device="cuda"), S_in=S, dS=S)
+           for L in ([-3, 1000, 66], [0, 70, 66])]
+    for a, b in zip(*out):
+        assert torch.equal(a, b)
+    assert torch.equal(out[0][5][0], S[0])
