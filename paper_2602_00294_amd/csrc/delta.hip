@@ -41,7 +41,7 @@ hipError_t launch_scan_t(const DeltaArgs& a, const void* data, hipStream_t s) {
 
 }  // namespace
 
-size_t delta_prefill_scratch(bool bf16, int heads, int, int n, int, int) {
+size_t delta_prefill_scratch(bool bf16, int heads, int n) {
   return delta_forward_bytes(bf16, heads, n);
 }
 

@@ -1,6 +1,6 @@
 // Gradients of the gated delta rule, in four passes: what the blocks' pairs leave (delta_pairs.hip), forward for the
-// states before every 64 tokens and the errors E = v - k S' (delta.hip), backward for the states' gradients U
-// and z = dL/du, and then, all blocks of 64 tokens side by side, what a block's tokens
+// states before every 64 tokens and the errors E = v - k S' (delta_scan.hpp), backward for the states' gradients U
+// and z = dL/du, in the same launch, and then, all blocks of 64 tokens side by side, what a block's tokens
 // make of these.  With the letters of delta_tiles.hpp, D = -beta z, S the state before a block and U the gradient behind it:
 //     du  = P^T dy + exp(G_C - G) (k U),   P_ij = c exp(G_i - G_j) q_i.k_j (j <= i)
 //     z   = (I + M)^-T du,   M_ij = exp(G_i - G_j) beta_i k_i.k_j (j < i),   dv = beta z,   dbeta = z.E
@@ -232,9 +232,11 @@ delta_scans_kernel(DeltaArgs a, const void* data, const void* back, float* state
 
 // ---- block by block: a wave has 16 of 64 tokens and all columns of their dq and dk
 //
-// float32 calls: first dq and asked, which take what lies before a token (pairs with tokens j <= i, the state before the block); then, on top
-// of asked, kept, which takes what lies behind (pairs with i >= j, the gradient of the state behind the block).  A pair's
-// weight is formed in both places, once for each side's rows, so that it is an operand where it is formed.
+// float32 calls: first dq and asked, which take what lies before a token (pairs with tokens j <= i, the state before the
+// block); then, on top of asked, kept, which takes what lies behind (pairs with i >= j, the gradient of the state behind the
+// block).  A pair's weight is formed in both places, once for each side's rows, so that it is an operand where it is formed.
+// A block's five tiles of three numbers an entry would take 240 KB of LDS: two lie there at a time.  6 heads x 555
+// tokens, d_k = 48, d_v = 32: 24 us, one workgroup's phases behind one another on 108 of the CUs.
 template <int ND>
 struct BlockLds {
   using L = DeltaTile<float, ND, kBlock>;  // errors, z, gradients of the outputs or rows of a state; queries or keys
@@ -633,8 +635,10 @@ delta_blocks_kernel(DeltaArgs a, const float* states, const float* behind, const
 // ---- the same for bfloat16 calls, whose tiles of a block lie in LDS together: eight waves, each with 16 tokens and one of the two
 // parts.  The first four form dq and asked: pairs with tokens j <= i, the state before the block; the others
 // kept: pairs with i >= j, the gradient behind it.  A block's rows are read once, its states once, 32 rows of both at
-// a time, and the two parts of dk meet in LDS.  64 heads x 2048 tokens of 128: 208 us for 557 MB (vector issue 37%, LDS 34%,
-// matrix cores 26% of the cycles; four waves that did one part after the other, two workgroups a CU: 320).  (Of a SIMD's two waves one has the longer part of the pairs, the other the shorter.)
+// a time, and the two parts of dk meet in LDS.  (Of a SIMD's two waves one has the longer part of the pairs, the other
+// the shorter.)
+// 64 heads x 2048 tokens of 128: 208 us for 557 MB, vector issue 37%, LDS 34%, matrix cores 26% of the cycles; four waves
+// that did one part after the other, two workgroups a CU: 320.
 template <int ND>
 struct SplitLds {
   using W = DeltaTile<float, ND, kBlock>;  // errors, z; later rows of the states

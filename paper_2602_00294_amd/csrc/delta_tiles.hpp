@@ -44,18 +44,8 @@ struct DeltaTile : PairTile<T, ND, ROWS> {
 template <typename T, int ND, int ROWS, int THREADS>
 using DeltaStage = TileStage<T, ND, ROWS, THREADS, DeltaTile<T, ND, ROWS>>;
 
-// sum of the products a[i] b[j] with i + j <= MAX, smallest first
-template <int MAX = 2, int NA, int NB>
-__device__ __forceinline__ f32x4 dot_planes16(const uint4 (&a)[NA], const uint4 (&b)[NB], f32x4 c) {
-#pragma unroll
-  for (int t = MAX; t >= 0; --t)
-#pragma unroll
-    for (int i = 0; i <= t; ++i)
-      if (i < NA && t - i < NB) c = mfma_bf16(a[i], b[t - i], c);
-  return c;
-}
-
-// The same for N results at once, product by product: a result's own products wait for each other.
+// Sums of the products a[i] b[j] with i + j <= MAX, smallest first, for N results at once, product by product: a result's own
+// products wait for each other.
 template <int MAX = 2, int N, int NA, int NB>
 __device__ __forceinline__ void dots_left16(const uint4 (&a)[N][NA], const uint4 (&b)[NB], f32x4 (&c)[N]) {
 #pragma unroll

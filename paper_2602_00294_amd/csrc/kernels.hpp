@@ -322,7 +322,7 @@ struct DeltaArgs {
   float scale;
 };
 hipError_t launch_delta_prefill(const DeltaArgs& a, bool bf16, void* scratch, hipStream_t s);
-size_t delta_prefill_scratch(bool bf16, int heads, int G, int n, int dk, int dv);
+size_t delta_prefill_scratch(bool bf16, int heads, int n);
 hipError_t launch_delta_step(const DeltaArgs& a, float* S, bool bf16, hipStream_t s);
 hipError_t launch_delta_backward(const DeltaArgs& a, bool bf16, void* scratch, hipStream_t s);
 size_t delta_backward_scratch(bool bf16, int heads, int G, int n, int dk, int dv);

@@ -1151,7 +1151,7 @@ int64_t sata_delta_scratch(int gradients, sata_dtype dt, int B, int H_qk, int G,
   if (check_delta_args(dt, B, H_qk, G, n, d_k, d_v) != SATA_OK) return -1;
   const int heads = B * H_qk * G;
   return (int64_t)(gradients ? sata::delta_backward_scratch(dt == SATA_BF16, heads, G, n, d_k, d_v)
-                             : sata::delta_prefill_scratch(dt == SATA_BF16, heads, G, n, d_k, d_v));
+                             : sata::delta_prefill_scratch(dt == SATA_BF16, heads, n));
 }
 
 sata_status sata_delta_prefill(const void* q, const void* k, const void* v, const float* g, const float* beta,
@@ -1163,7 +1163,7 @@ sata_status sata_delta_prefill(const void* q, const void* k, const void* v, cons
   if (S_in && S_in == S_out) return fail(SATA_ERR_INVALID_ARG, "S_out must not be S_in");
   if (n == 0 && !S_out) return ok();
   sata::DeltaArgs a = delta_args(q, k, v, g, beta, B, H_qk, G, n, d_k, d_v, lengths);
-  if ((st = check_scratch(scratch, sata::delta_prefill_scratch(dt == SATA_BF16, a.heads, G, n, d_k, d_v))) != SATA_OK) return st;
+  if ((st = check_scratch(scratch, sata::delta_prefill_scratch(dt == SATA_BF16, a.heads, n))) != SATA_OK) return st;
   a.S_in = S_in, a.y = y, a.S_out = S_out;
   hipError_t e = sata::launch_delta_prefill(a, dt == SATA_BF16, scratch, (hipStream_t)stream);
   if (e != hipSuccess) return hip_fail(e, "delta prefill launch");
