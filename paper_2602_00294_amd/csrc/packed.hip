@@ -1,15 +1,15 @@
 // Rows into caches of 4 bits an entry, and back out of them as the values they stand for.
 //
-// Bound: memory, 2 or 4 bytes an entry on one side and 5 bits on the other.  A lane has a group of 32 entries, which it reads or
-// writes by whole vectors, and finds their ends and codes without another; the row's bytes, of which each group has every
-// G-th, change lanes (DPP) and places (v_perm) once.
+// Bound: memory, 2 or 4 bytes an entry on one side and 5 bits on the other.  Writing, a lane has a group of 32 entries, which it
+// reads by whole vectors, and finds their ends and codes without another; the row's bytes, of which each group has every
+// G-th, change lanes (DPP) and places (v_perm) once.  Reading, a lane has eight entries and writes whole vectors side by
+// side with its neighbours'.
 // Keys and values of 32 heads x 4000 rows of 128 bfloat16 entries (86 MB): written in 16.8 us, of which vector
 // instructions take 92% (a lane's division and rounding of 32 entries; 16 lanes to a group, as a token's row
-// is packed, took 36); read back in 15.8 us each.
+// is packed, took 36); read back in 10.3 us each, 4.2 TB/s (a lane a group, as they are written, took 15.8).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
-#include <type_traits>
 
 #include "kernels.hpp"
 #include "packed_rows.hpp"
@@ -49,34 +49,24 @@ __device__ __forceinline__ void across_bytes(uint32_t (&x)[4]) {
   x[0] = __builtin_amdgcn_perm(c, a, 0x05040100), x[1] = __builtin_amdgcn_perm(c, a, 0x07060302);
   x[2] = __builtin_amdgcn_perm(d, b, 0x05040100), x[3] = __builtin_amdgcn_perm(d, b, 0x07060302);
 }
-// A group's 16 bytes, dword w of a = 4 w .. +3, from the 16 bytes that this lane has of its row (lane g of G: of a = 16 g / G on), or
-// the other way (TO_ROW).
-template <int G, bool TO_ROW>
-__device__ __forceinline__ void change_places(uint32_t (&x)[4], int g) {
+// A group's 16 bytes, dword w of a = 4 w .. +3, become the 16 bytes that this lane, g of G, has of its row: of a = 16 g / G on.
+template <int G>
+__device__ __forceinline__ void to_row(uint32_t (&x)[4], int g) {
   if constexpr (G == 4) {
-    if (TO_ROW) across_four(x, g);
+    across_four(x, g);
     across_bytes(x);
-    if (!TO_ROW) across_four(x, g);
   } else if constexpr (G == 2) {
-    if constexpr (TO_ROW) {
-      // (the other lane's dwords of this lane's a)
-      const uint32_t a = neighbour<0xb1>(g ? x[0] : x[2]), b = neighbour<0xb1>(g ? x[1] : x[3]);
-      const uint32_t own0 = g ? x[2] : x[0], own1 = g ? x[3] : x[1];
-      const uint32_t f0 = g ? a : own0, s0 = g ? own0 : a, f1 = g ? b : own1, s1 = g ? own1 : b;  // of groups 0 and 1
-      x[0] = __builtin_amdgcn_perm(s0, f0, 0x05010400), x[1] = __builtin_amdgcn_perm(s0, f0, 0x07030602);
-      x[2] = __builtin_amdgcn_perm(s1, f1, 0x05010400), x[3] = __builtin_amdgcn_perm(s1, f1, 0x07030602);
-    } else {
-      const uint32_t f0 = __builtin_amdgcn_perm(x[1], x[0], 0x06040200), s0 = __builtin_amdgcn_perm(x[1], x[0], 0x07050301);
-      const uint32_t f1 = __builtin_amdgcn_perm(x[3], x[2], 0x06040200), s1 = __builtin_amdgcn_perm(x[3], x[2], 0x07050301);
-      const uint32_t a = neighbour<0xb1>(g ? f0 : s0), b = neighbour<0xb1>(g ? f1 : s1);
-      if (g) x[0] = a, x[1] = b, x[2] = s0, x[3] = s1;
-      else x[0] = f0, x[1] = f1, x[2] = a, x[3] = b;
-    }
+    // (the other lane's dwords of this lane's a)
+    const uint32_t a = neighbour<0xb1>(g ? x[0] : x[2]), b = neighbour<0xb1>(g ? x[1] : x[3]);
+    const uint32_t own0 = g ? x[2] : x[0], own1 = g ? x[3] : x[1];
+    const uint32_t f0 = g ? a : own0, s0 = g ? own0 : a, f1 = g ? b : own1, s1 = g ? own1 : b;  // of groups 0 and 1
+    x[0] = __builtin_amdgcn_perm(s0, f0, 0x05010400), x[1] = __builtin_amdgcn_perm(s0, f0, 0x07030602);
+    x[2] = __builtin_amdgcn_perm(s1, f1, 0x05010400), x[3] = __builtin_amdgcn_perm(s1, f1, 0x07030602);
   }
 }
 
-template <typename T, int G, bool WRITE>
-__device__ __forceinline__ void rows_of(const PackedArgs& p, const PackedRows& r) {
+template <typename T, int G>
+__device__ __forceinline__ void write_rows(const PackedArgs& p, const PackedRows& r) {
   constexpr int kEV = 16 / (int)sizeof(T), kRows = kPackThreads / G;
   const int g = threadIdx.x % G, d = r.d, left = d - 32 * g;  // entries from this group on
   const int64_t rows = (int64_t)p.heads * p.n;
@@ -90,123 +80,145 @@ __device__ __forceinline__ void rows_of(const PackedArgs& p, const PackedRows& r
     T* const x = (T*)r.x + i * d + 32 * g;
     float f[32];
     uint32_t w[4], params = 0u;
-    // 16 bytes of the row as it lies: rows of 80 bytes are aligned to 16, of 40 to 8, of 20 to 4
-    auto row_dwords = [&](auto&& each) {
-      uint8_t* const q = row + 16 * g;
-      if constexpr (G == 4) each((uint4*)q);
-      else if constexpr (G == 2) each((uint2*)q);
-      else each((uint32_t*)q);
-    };
-    if constexpr (WRITE) {
-      if (!there) continue;  // (the same for the lanes of a row)
-      if (vec) {
+    if (!there) continue;  // (the same for the lanes of a row)
+    if (vec) {
 #pragma unroll
-        for (int c = 0; c < 32; c += kEV) {
-          uint4 v = {0u, 0u, 0u, 0u};
-          if (c < left) v = *(const uint4*)(x + c);
-          const uint32_t u[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            if constexpr (sizeof(T) == 2) f[c + 2 * e] = lo_f32(u[e]), f[c + 2 * e + 1] = hi_f32(u[e]);
-            else f[c + e] = __uint_as_float(u[e]);
-          }
-        }
-      } else {
-#pragma unroll
-        for (int e = 0; e < 32; ++e) f[e] = e < left ? f32_of(x[e]) : 0.f;
-      }
-      float least = INFINITY, most = -INFINITY;
-#pragma unroll
-      for (int e = 0; e < 32; ++e) {
-        const float y = for_ends(f[e]);
-        least = fminf(least, e < left ? y : INFINITY), most = fmaxf(most, e < left ? y : -INFINITY);
-      }
-      params = left > 0 ? group_params(least, most, most < INFINITY) : 0u;
-      const GroupCode code(params);
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        w[q] = 0u;
+      for (int c = 0; c < 32; c += kEV) {
+        uint4 v = {0u, 0u, 0u, 0u};
+        if (c < left) v = *(const uint4*)(x + c);
+        const uint32_t u[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int lo = 4 * q + e, hi = lo + 16;
-          w[q] |= ((lo < left ? code(f[lo]) : 0u) | (hi < left ? code(f[hi]) : 0u) << 4) << (8 * e);
+          if constexpr (sizeof(T) == 2) f[c + 2 * e] = lo_f32(u[e]), f[c + 2 * e + 1] = hi_f32(u[e]);
+          else f[c + e] = __uint_as_float(u[e]);
         }
       }
-      change_places<G, true>(w, g);
-      row_dwords([&](auto* q) {
-        using V = std::remove_pointer_t<decltype(q)>;
-#pragma unroll
-        for (int e = 0; e < 16 / (int)sizeof(V); ++e) {
-          if constexpr (sizeof(V) == 16) q[e] = uint4{w[0], w[1], w[2], w[3]};
-          else if constexpr (sizeof(V) == 8) q[e] = uint2{w[2 * e], w[2 * e + 1]};
-          else q[e] = w[e];
-        }
-      });
-      ((uint32_t*)(row + 16 * G))[g] = params;
     } else {
-      w[0] = w[1] = w[2] = w[3] = 0u;
-      if (there) {
-        row_dwords([&](auto* q) {
-          using V = std::remove_pointer_t<decltype(q)>;
 #pragma unroll
-          for (int e = 0; e < 16 / (int)sizeof(V); ++e) {
-            const V v = q[e];
-            if constexpr (sizeof(V) == 16) w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
-            else if constexpr (sizeof(V) == 8) w[2 * e] = v.x, w[2 * e + 1] = v.y;
-            else w[e] = v;
-          }
-        });
-        params = ((const uint32_t*)(row + 16 * G))[g];
+      for (int e = 0; e < 32; ++e) f[e] = e < left ? f32_of(x[e]) : 0.f;
+    }
+    float least = INFINITY, most = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < 32; ++e) {
+      const float y = for_ends(f[e]);
+      least = fminf(least, e < left ? y : INFINITY), most = fmaxf(most, e < left ? y : -INFINITY);
+    }
+    params = left > 0 ? group_params(least, most, most < INFINITY) : 0u;
+    const GroupCode code(params);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      w[i] = 0u;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int lo = 4 * i + e, hi = lo + 16;
+        w[i] |= ((lo < left ? code(f[lo]) : 0u) | (hi < left ? code(f[hi]) : 0u) << 4) << (8 * e);
       }
-      change_places<G, false>(w, g);
+    }
+    to_row<G>(w, g);
+    uint8_t* const q = row + 16 * g;  // (rows of 80 bytes are aligned to 16, of 40 to 8, of 20 to 4)
+    if constexpr (G == 4) {
+      *(uint4*)q = uint4{w[0], w[1], w[2], w[3]};
+    } else if constexpr (G == 2) {
+      ((uint2*)q)[0] = uint2{w[0], w[1]}, ((uint2*)q)[1] = uint2{w[2], w[3]};
+    } else {
 #pragma unroll
-      for (int e = 0; e < 32; ++e) f[e] = value_of((w[(e & 15) / 4] >> (8 * (e & 3) + 4 * (e >> 4))) & 15u, params);
-      if (vec) {
+      for (int e = 0; e < 4; ++e) ((uint32_t*)q)[e] = w[e];
+    }
+    ((uint32_t*)(row + 16 * G))[g] = params;
+  }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kPackThreads) packed_write_kernel(PackedArgs p) {
+  const PackedRows& r = p.rows[blockIdx.y];
+  switch (packed_groups(r.d)) {
+    case 1: return write_rows<T, 1>(p, r);
+    case 2: return write_rows<T, 2>(p, r);
+    default: return write_rows<T, 4>(p, r);
+  }
+}
+
+// Eight entries a lane: their bytes lie G apart in 8 G bytes, which the lanes of the other groups and halves read too.
+template <typename T, int G>
+__global__ void __launch_bounds__(kPackThreads) packed_read_kernel(PackedArgs p) {
+  const PackedRows& r = p.rows[0];
+  const int d = r.d, head = blockIdx.y;
+  const uint32_t parts = (uint32_t)(d + 7) / 8, all = (uint32_t)p.n * parts;
+  const bool vec = d % 8 == 0 && ((uintptr_t)r.x & 15) == 0;
+  const int64_t first = p.first ? p.first[head / p.H] : 0;
+  const uint8_t* const cache = r.cache + (int64_t)head * p.capacity * (20 * G);
+  for (uint32_t i = blockIdx.x * kPackThreads + threadIdx.x; i < all; i += gridDim.x * kPackThreads) {
+    const uint32_t t = i / parts;
+    const int e0 = 8 * (int)(i - t * parts), g = e0 / 32, high = e0 % 32 / 16;
+    const int64_t at = first + t;
+    uint32_t w[2 * G] = {}, params = 0u;
+    if (at >= 0 && at < p.capacity) {
+      const uint8_t* const row = cache + at * (20 * G);
+      const uint8_t* const q = row + e0 % 16 * G;  // (aligned as the row: to 16, 8 or 4 bytes)
 #pragma unroll
-        for (int c = 0; c < 32; c += kEV) {
-          uint4 v;
-          if constexpr (sizeof(T) == 2) v = uint4{pack2(f[c], f[c + 1]), pack2(f[c + 2], f[c + 3]), pack2(f[c + 4], f[c + 5]), pack2(f[c + 6], f[c + 7])};
-          else v = uint4{__float_as_uint(f[c]), __float_as_uint(f[c + 1]), __float_as_uint(f[c + 2]), __float_as_uint(f[c + 3])};
-          if (c < left) *(uint4*)(x + c) = v;
+      for (int x = 0; x < 2; ++x) {
+        if constexpr (G == 4) {
+          const uint4 v = ((const uint4*)q)[x];
+          w[4 * x] = v.x, w[4 * x + 1] = v.y, w[4 * x + 2] = v.z, w[4 * x + 3] = v.w;
+        } else if constexpr (G == 2) {
+          const uint2 v = ((const uint2*)q)[x];
+          w[2 * x] = v.x, w[2 * x + 1] = v.y;
+        } else {
+          w[x] = ((const uint32_t*)q)[x];
         }
-      } else {
-#pragma unroll
-        for (int e = 0; e < 32; ++e)
-          if (e < left) {
-            if constexpr (sizeof(T) == 4) x[e] = f[e];
-            else x[e] = (T)(pack2(f[e], 0.f) & 0xffffu);
-          }
       }
+      params = ((const uint32_t*)(row + 16 * G))[g];
+    }
+    float f[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = value_of((w[e * G / 4] >> (8 * (e * G % 4 + g) + 4 * high)) & 15u, params);
+    T* const x = (T*)r.x + ((int64_t)head * p.n + t) * d + e0;
+    if (vec) {
+      if constexpr (sizeof(T) == 2) {
+        *(uint4*)x = uint4{pack2(f[0], f[1]), pack2(f[2], f[3]), pack2(f[4], f[5]), pack2(f[6], f[7])};
+      } else {
+        ((float4*)x)[0] = float4{f[0], f[1], f[2], f[3]};
+        ((float4*)x)[1] = float4{f[4], f[5], f[6], f[7]};
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e0 + e < d) {
+          if constexpr (sizeof(T) == 4) x[e] = f[e];
+          else x[e] = (T)(pack2(f[e], 0.f) & 0xffffu);
+        }
     }
   }
 }
 
-template <typename T, bool WRITE>
-__global__ void __launch_bounds__(kPackThreads) packed_kernel(PackedArgs p) {
-  const PackedRows& r = p.rows[blockIdx.y];
-  switch (packed_groups(r.d)) {
-    case 1: return rows_of<T, 1, WRITE>(p, r);
-    case 2: return rows_of<T, 2, WRITE>(p, r);
-    default: return rows_of<T, 4, WRITE>(p, r);
-  }
-}
-
-template <typename T, bool WRITE>
-hipError_t launch(const PackedArgs& p, hipStream_t s) {
+template <typename T>
+hipError_t launch_write(const PackedArgs& p, hipStream_t s) {
   const int d = p.tensors > 1 ? std::max(p.rows[0].d, p.rows[1].d) : p.rows[0].d, each = kPackThreads / packed_groups(d);
   const int64_t blocks = ((int64_t)p.heads * p.n + each - 1) / each;
-  hipLaunchKernelGGL((packed_kernel<T, WRITE>), dim3((unsigned)std::min<int64_t>(blocks, 1 << 20), p.tensors),
-                     dim3(kPackThreads), 0, s, p);
+  hipLaunchKernelGGL((packed_write_kernel<T>), dim3((unsigned)std::min<int64_t>(blocks, 1 << 20), p.tensors), dim3(kPackThreads), 0, s, p);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_read(const PackedArgs& p, hipStream_t s) {
+  const int64_t blocks = ((int64_t)p.n * ((p.rows[0].d + 7) / 8) + kPackThreads - 1) / kPackThreads;
+  // (a launch has fewer than 2^32 threads)
+  const dim3 grid((unsigned)std::min<int64_t>(blocks, (1 << 23) / p.heads), p.heads);
+  switch (packed_groups(p.rows[0].d)) {
+    case 1: hipLaunchKernelGGL((packed_read_kernel<T, 1>), grid, dim3(kPackThreads), 0, s, p); break;
+    case 2: hipLaunchKernelGGL((packed_read_kernel<T, 2>), grid, dim3(kPackThreads), 0, s, p); break;
+    default: hipLaunchKernelGGL((packed_read_kernel<T, 4>), grid, dim3(kPackThreads), 0, s, p); break;
+  }
   return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_packed_write(const PackedArgs& a, bool bf16, hipStream_t s) {
-  return bf16 ? launch<u16, true>(a, s) : launch<float, true>(a, s);
+  return bf16 ? launch_write<u16>(a, s) : launch_write<float>(a, s);
 }
 hipError_t launch_packed_read(const PackedArgs& a, bool bf16, hipStream_t s) {
-  return bf16 ? launch<u16, false>(a, s) : launch<float, false>(a, s);
+  return bf16 ? launch_read<u16>(a, s) : launch_read<float>(a, s);
 }
 
 }  // namespace sata
