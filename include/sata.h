@@ -480,7 +480,8 @@ sata_status sata_packed_read(const void* cache, int capacity, const int32_t* fir
 
 /* sata_softmax_step over such caches, the new rows among them: k and v count as what their four bits stand for.  Idle
  * sequences, unused rows, sizes and scratch as there; scratch of sata_softmax_step_packed_scratch bytes.  (A weight
- * times a scale enters its product with 16 bits in bfloat16 calls.)  A row's NaN makes NaN of the outputs that see it. */
+ * times a scale enters its product with 16 bits in bfloat16 calls.)  A row's NaN makes NaN of the outputs that see it;
+ * rows of finite entries up to 2^120 give finite outputs, where q.k has a sum in float32. */
 int64_t sata_softmax_step_packed_scratch(int B, int H_kv, int G, int capacity, int d_v);
 sata_status sata_softmax_step_packed(void* K, void* V, int capacity, const int32_t* lengths, const void* q, const void* k,
                                      const void* v, sata_dtype dt, int B, int H_kv, int G, int d_k, int d_v, void* y,

@@ -5,8 +5,8 @@
 // of every 16 in what it reads at once, and four lanes of keys' 16 bytes are a whole group's contraction.
 //
 // scale = (most - least) / 15, least the smallest entry, both rounded to bfloat16; codes are the nearest, to those
-// rounded numbers, ties to the even one.  A group with an entry that is not finite, or beyond 2^120 in size (31
-// scales have to be a number), stands for NaN.
+// rounded numbers, ties to the even one.  A group with an entry that is not finite, or beyond 2^120 in size (what
+// softmax_step_packed.hip can still take sums of), stands for NaN.
 #pragma once
 
 #include <hip/hip_runtime.h>

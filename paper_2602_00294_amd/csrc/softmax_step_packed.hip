@@ -92,6 +92,13 @@ struct Codes {
   __device__ __forceinline__ uint32_t high(uint32_t x) const { return ((sizeof(T) == 2 ? x >> 4 : x >> 1) & mask) | tag; }
 };
 
+// Entries go up to 2^120 (packed_rows.hpp), and sums over (o + code) q or weights and those over least values that
+// belong to them are larger than what is left of them, by (o + 15) / 7.5 at most, a score's by twice that.
+// Queries enter 2^8 times smaller: where a query's and a key's entries have a product at all, so have these.
+// Sums over 2^21 rows of weights up to 2^8 hold scales and least values of up to 2^88; from the first larger
+// ones on, a wave takes all 2^32 times smaller.  (Means of stretches, not sums, are joined.)
+constexpr float kSmaller = 0x1p-8f, kFar = 0x1p88f, kFarSmaller = 0x1p-32f;
+
 // N floats of LDS
 template <int N>
 struct Floats {
@@ -250,7 +257,7 @@ __device__ __forceinline__ void packed_stretch_rows(const SoftmaxStepArgs& a, in
       for (int i = 0; i < 8; ++i) {
         // (dwords in the order of the products' operands: low codes of a = 0, 1, then of 2, 3, then the high ones)
         const int e = 32 * g + 4 * t4 + (i & 3) + 16 * (i >> 2);
-        x[i] = l15 < members && e < dk ? entry_of(q, e) : 0.f;
+        x[i] = l15 < members && e < dk ? kSmaller * entry_of(q, e) : 0.f;
         total[g] += x[i];
       }
       total[g] += __shfl_xor(total[g], 16);
@@ -274,7 +281,8 @@ __device__ __forceinline__ void packed_stretch_rows(const SoftmaxStepArgs& a, in
 #pragma unroll
   for (int g = 0; g < GV; ++g) base[g] = 0.f;
   float top = -3.4028234e38f, sum = 0.f;
-  const float c = a.scale * kLog2e;
+  float smaller = 1.f;  // what values enter the sums with, the same for the wave
+  const float c = a.scale * (kLog2e / kSmaller);
   constexpr int kStep = 32 * kStepWaves;
   const Codes<T> codes;
   // this wave's: scales of keys [32][GK], of values [32][GV], and least values less the codes' offset
@@ -300,18 +308,35 @@ __device__ __forceinline__ void packed_stretch_rows(const SoftmaxStepArgs& a, in
 #pragma unroll 1
   for (; r0 < end; r0 += kStep) {
     wave_lds_fence();  // (the last tile's scales have been read)
+    float vs[GV], vb[GV], far = 0.f;
+#pragma unroll
+    for (int g = 0; g < GV; ++g) {
+      vs[g] = lo_f32(tile.vp.w[g]);
+      vb[g] = fmaf(-Codes<T>::kOffset, vs[g], hi_f32(tile.vp.w[g]));
+      far = fmaxf(far, fmaxf(vs[g], fabsf(vb[g])));
+    }
+    if (__builtin_expect(smaller != 1.f || __ballot(far > kFar) != 0, 0)) {
+      stay_in_branch();
+      if (smaller == 1.f) {
+        smaller = kFarSmaller;
+        settle_mfma();
+#pragma unroll
+        for (int j = 0; j < 2 * GV; ++j)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[j][i] *= smaller;
+#pragma unroll
+        for (int g = 0; g < GV; ++g) base[g] *= smaller;
+      }
+#pragma unroll
+      for (int g = 0; g < GV; ++g) vs[g] *= smaller, vb[g] *= smaller;
+    }
     if (t4 < 2) {
-      float k[GK], v[GV], base[GV];
+      float k[GK];
 #pragma unroll
       for (int g = 0; g < GK; ++g) k[g] = lo_f32(t4 ? tile.kp[1].w[g] : tile.kp[0].w[g]);
-#pragma unroll
-      for (int g = 0; g < GV; ++g) {
-        v[g] = lo_f32(tile.vp.w[g]);
-        base[g] = fmaf(-Codes<T>::kOffset, v[g], hi_f32(tile.vp.w[g]));
-      }
       store_floats<GK>(kscale + lane * GK, k);
-      store_floats<GV>(vscale + lane * GV, v);
-      store_floats<GV>(vbase + lane * GV, base);
+      store_floats<GV>(vscale + lane * GV, vs);
+      store_floats<GV>(vbase + lane * GV, vb);
     }
     wave_lds_fence();
     // ---- scores of tokens 4 t4 .. +3 and 16 + 4 t4 .. +3 with query head l15
@@ -339,6 +364,7 @@ __device__ __forceinline__ void packed_stretch_rows(const SoftmaxStepArgs& a, in
         s[4 * x + i] = score[i];
 #pragma unroll
         for (int g = 0; g < GK; ++g) s[4 * x + i] = fmaf(scale.f[g], acc[g][i], s[4 * x + i]);
+        s[4 * x + i] *= c;  // (rounded before the largest is taken off: what is left of two sizes of 10^10 is no small number)
       }
     }
     if (at < r0 + 31) {
@@ -349,7 +375,6 @@ __device__ __forceinline__ void packed_stretch_rows(const SoftmaxStepArgs& a, in
     float most = s[0];
 #pragma unroll
     for (int i = 1; i < 8; ++i) most = fmaxf(most, s[i]);
-    most *= c;
     if (__ballot(most > top + 8.f)) {
       float next = fmaxf(most, __shfl_xor(most, 16));
       next = fmaxf(top, fmaxf(next, __shfl_xor(next, 32)));
@@ -375,7 +400,7 @@ __device__ __forceinline__ void packed_stretch_rows(const SoftmaxStepArgs& a, in
     float z[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      z[i] = exp2_fast(fmaf(s[i], c, -top));
+      z[i] = exp2_fast(s[i] - top);
       sum += z[i];
     }
     constexpr int kAt = GV < 2 ? GV : 2;  // groups at a time
@@ -421,16 +446,18 @@ __device__ __forceinline__ void packed_stretch_rows(const SoftmaxStepArgs& a, in
     base[g] += __shfl_xor(base[g], 32);
   }
 
-  // ---- the waves' sums joined, in their order
+  // ---- the waves' means joined, in their order, each with its part of the weights (sums of the largest values would
+  // not be numbers)
   if (t4 == 0) state[wave][l15] = StepState{top, sum};
   if (l15 < members) {
     float* const row = sums + (wave * members + l15) * dv;
+    const float inverse = sum == 0.f ? 0.f : 1.f / sum / smaller;  // (0: a wave without rows)
 #pragma unroll
     for (int j = 0; j < 2 * GV; ++j)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int col = 16 * j + 4 * t4 + i;
-        if (col < dv) row[col] = o[j][i] + base[j / 2];
+        if (col < dv) row[col] = (o[j][i] + base[j / 2]) * inverse;
       }
   }
   __syncthreads();
@@ -439,15 +466,17 @@ __device__ __forceinline__ void packed_stretch_rows(const SoftmaxStepArgs& a, in
     float most = state[0][m].top;
 #pragma unroll
     for (int w = 1; w < kStepWaves; ++w) most = fmaxf(most, state[w][m].top);
-    float x = 0.f, l = 0.f;
+    float x = 0.f, l = 0.f, k[kStepWaves];
 #pragma unroll
     for (int w = 0; w < kStepWaves; ++w) {
-      const float k = exp2_fast(state[w][m].top - most);
-      x = fmaf(sums[(w * members + m) * dv + col], k, x);
-      l = fmaf(state[w][m].sum, k, l);
+      k[w] = state[w][m].sum * exp2_fast(state[w][m].top - most);
+      l += k[w];
     }
+    const float inverse = 1.f / l;
+#pragma unroll
+    for (int w = 0; w < kStepWaves; ++w) x = fmaf(sums[(w * members + m) * dv + col], k[w] * inverse, x);
     if (!part) {
-      ((T*)a.y)[(q0 + m) * dv + col] = rounded<T>(x / l);
+      ((T*)a.y)[(q0 + m) * dv + col] = rounded<T>(x);
     } else {
       float* const out = part + m * (dv + 2);
       out[col] = x;
@@ -482,7 +511,7 @@ hipError_t launch_step(const SoftmaxStepArgs& a, const SoftmaxStepPlan& p, hipSt
   hipLaunchKernelGGL((softmax_step_packed_kernel<T, GK, GV>), dim3(p.workgroups), dim3(64 * kStepWaves), bytes, s, a, p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.bytes == 0) return e;
-  hipLaunchKernelGGL(softmax_join_kernel<T>, dim3(a.heads * a.G), dim3((a.dv_ + 63) / 64 * 64), 0, s, a, p);
+  hipLaunchKernelGGL((softmax_join_kernel<T, true>), dim3(a.heads * a.G), dim3((a.dv_ + 63) / 64 * 64), 0, s, a, p);
   return hipGetLastError();
 }
 

@@ -115,7 +115,8 @@ __device__ __forceinline__ void to_positive_pairs(const float (&x)[16], uint4 (&
 // The sums of one query head's stretches joined, in their order; one thread per column.  (Each wave has all
 // tops at once and four stretches' sums on their way: 512 query heads of up to 12
 // stretches 4.6 us, where each block counting stretches and loading one sum after the other took 7.6.)
-template <typename T>
+// MEANS: stretches left their means in the sums' place.
+template <typename T, bool MEANS = false>
 __global__ void __launch_bounds__(kMaxPairDim) softmax_join_kernel(SoftmaxStepArgs a, SoftmaxStepPlan p) {
   const int qh = blockIdx.x, kvh = qh / a.G, member = qh - kvh * a.G;
   const int dv = a.dv_, col = threadIdx.x, lane = col & 63;
@@ -128,6 +129,19 @@ __global__ void __launch_bounds__(kMaxPairDim) softmax_join_kernel(SoftmaxStepAr
   for (int w = lane; w < first.y; w += 64) most = fmaxf(most, in[w * pitch + dv]);
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
+  if constexpr (MEANS) {
+    float all = 0.f, x = 0.f;
+    for (int w = lane; w < first.y; w += 64) all = fmaf(in[w * pitch + dv + 1], exp2_fast(in[w * pitch + dv] - most), all);
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) all += __shfl_xor(all, d);
+    if (col >= dv) return;
+    const float inverse = 1.f / all;
+#pragma unroll 4
+    for (int w = 0; w < first.y; ++w)
+      x = fmaf(in[w * pitch + col], in[w * pitch + dv + 1] * exp2_fast(in[w * pitch + dv] - most) * inverse, x);
+    ((T*)a.y)[(int64_t)qh * dv + col] = rounded<T>(x);
+    return;
+  }
   if (col >= dv) return;
   float x = 0.f, l = 0.f;
 #pragma unroll 4

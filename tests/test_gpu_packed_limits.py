@@ -1,0 +1,150 @@
+"""Single tokens over caches of 4 bits an entry with entries near the largest that a row holds, against float64."""
+import math
+import sys
+
+import pytest
+
+import delta_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+LARGEST = 1.3e36  # a little below 2^120
+
+
+@pytest.fixture(scope="module")
+def sata():
+    if not torch.cuda.is_available():
+        pytest.fail("no GPU visible")
+    import paper_2602_00294_amd as m
+    m.load_library()
+    return m
+
+
+def _dtype(name):
+    return torch.bfloat16 if name == "bf16" else torch.float32
+
+
+def _stands(x):
+    """(values, scales, sizes of the least values) [.., d] float64 of rows made from x."""
+    rows, values = ref.pack(x.float().numpy())
+    d, groups = x.shape[-1], rows.shape[-1] // 20
+    p = torch.from_numpy(rows[..., 16 * groups:].copy()).view(torch.bfloat16).double()
+    each = lambda j: p[..., j::2].repeat_interleave(32, dim=-1)[..., :d]  # noqa: E731
+    return torch.from_numpy(values).double(), each(0).abs(), each(1).abs()
+
+
+def _token(sata, k, v, q):
+    """The call over caches of all rows of k and v but the last, which are the token's."""
+    B, H, e, dk = k.shape
+    K, V = (torch.zeros(B, H, e + 3, sata.packed_row_bytes(x.shape[-1]), dtype=torch.uint8, device="cuda") for x in (k, v))
+    sata.packed_write(K, V, None, k[:, :, :e - 1].contiguous().cuda(), v[:, :, :e - 1].contiguous().cuda())
+    lengths = torch.full((B,), e - 1, dtype=torch.int32, device="cuda")
+    return sata.softmax_step_packed(K, V, lengths, q.cuda(), k[:, :, -1].contiguous().cuda(),
+                                    v[:, :, -1].contiguous().cuda()).double().cpu()
+
+
+def _bound(k, v, q, dtype):
+    """float64 outputs, and what they may be off: their rounding; a weight times a scale, which is two bfloat16 numbers (2^-18
+    of it off) or three, times the codes; scores, sums over (offset + code) q and least values of at most 80 float32 roundings,
+    which count in a weight and in the sum of weights; sums over the rows of (offset + code) weights in float32, whose
+    roundings, two matrix products of two weight numbers for every 32 rows, add up as a root."""
+    (K, ks, km), (V, vs, vm) = _stands(k), _stands(v)
+    B, H, e, dk = K.shape
+    G = q.shape[1] // H
+    y, tol = (torch.zeros(B, H * G, V.shape[-1], dtype=torch.float64) for _ in range(2))
+    eps, weight, offset = (2.0 ** -8, 2.0 ** -18, 128) if dtype == "bf16" else (2.0 ** -24, 2.0 ** -23, 16)
+    for b in range(B):
+        for h in range(H):
+            for m in range(G):
+                x = q[b, h * G + m].double()
+                p = torch.softmax(K[b, h] @ x / math.sqrt(dk), -1)
+                y[b, h * G + m] = p @ V[b, h]
+                size = ((offset + 15) * ks[b, h] + km[b, h]) @ x.abs() / math.sqrt(dk)
+                off = p @ (15 * vs[b, h]) * weight
+                off = off + p @ (15 * vs[b, h] + vm[b, h]) * 2.0 ** -24 * (2 * 80 * size.max() + 8)
+                off = off + p @ ((offset + 15) * vs[b, h] + vm[b, h]) * 2.0 ** -24 * (16 + 2 * math.sqrt(e / 8))
+                tol[b, h * G + m] = eps * y[b, h * G + m].abs() + off
+    return y, tol
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("G,e,dk,dv", [(1, 1, 32, 32), (2, 300, 64, 128), (17, 3000, 33, 70)])
+@pytest.mark.parametrize("rising", [False, True])
+def test_largest_values(sata, rising, G, e, dk, dv, dtype):
+    """Values of all sizes up to the largest: sums of (offset + code) weights, with weights that are all alike, or that rise
+    by 2^7 along the cache."""
+    print("largest values", rising, G, e, dk, dv, dtype, file=sys.stderr, flush=True)
+    gen = torch.Generator().manual_seed(e + dv)
+    v = (torch.rand(2, 1, e, dv, generator=gen) * 2 - 1) * LARGEST
+    v[1, 0, e // 2:, : dv // 2] *= 1e-20  # (some groups and rows of ordinary size beside them)
+    v[:, 0, -1, 0], v[:, 0, -1, 1] = LARGEST, -LARGEST
+    q = torch.full((2, G, dk), 0.25)
+    k = torch.zeros(2, 1, e, dk)
+    if rising:  # (constant rows are exact but for their rounding to bfloat16)
+        k += (torch.arange(e) / e * (7 * math.log(2.0)) * math.sqrt(dk) / (0.25 * dk))[:, None]
+    q, k, v = (x.to(_dtype(dtype)) for x in (q, k, v))
+    y = _token(sata, k, v, q)
+    want, tol = _bound(k, v, q, dtype)
+    assert torch.isfinite(y).all()
+    assert ((y - want).abs() <= tol).all(), ((y - want).abs() / tol).max()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("size", [1.0, 30.0])
+@pytest.mark.parametrize("G,e,dk,dv", [(2, 40, 32, 32), (2, 700, 128, 64), (1, 5, 65, 40)])
+def test_largest_keys(sata, G, e, dk, dv, size, dtype):
+    """Keys up to the largest: scores of some 10^36 are numbers, and the key of the largest has all the weight."""
+    print("largest keys", G, e, dk, dv, size, dtype, file=sys.stderr, flush=True)
+    gen = torch.Generator().manual_seed(e + dk + 1)
+    k = ((torch.rand(2, 2, e, dk, generator=gen) * 2 - 1) * LARGEST).to(_dtype(dtype))
+    v, q = torch.randn(2, 2, e, dv, generator=gen), size * torch.randn(2, 2 * G, dk, generator=gen)
+    v, q = v.to(_dtype(dtype)), q.to(_dtype(dtype))
+    (K, ks, km), (V, _, _) = _stands(k), _stands(v)
+    want = torch.zeros(2, 2 * G, dv, dtype=torch.float64)
+    for b in range(2):
+        for h in range(2 * G):
+            x = q[b, h].double()
+            s = (K[b, h // G] @ x).sort(descending=True)
+            # (the two largest are further apart than all roundings of their sums)
+            off = ((143 * ks + km)[b, h // G] @ x.abs()).max() * 100 * 2.0 ** -24
+            assert s.values[0] - s.values[1] > 4 * off > 1e20
+            want[b, h] = V[b, h // G, s.indices[0]]
+    y = _token(sata, k, v, q)
+    eps = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -24
+    sizes = (143 * _stands(v)[1] + _stands(v)[2]).amax(2).repeat_interleave(G, dim=1)
+    assert ((y - want).abs() <= eps * want.abs() + 8 * 2.0 ** -24 * sizes).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_largest_keys_and_values(sata, dtype):
+    """As many equal scores of some 10^37 as there are rows, over the largest values."""
+    e, d = 500, 64
+    gen = torch.Generator().manual_seed(9)
+    k = torch.full((1, 1, e, d), 1.0) * LARGEST
+    v = torch.rand(1, 1, e, d, generator=gen) * LARGEST
+    q = torch.ones(1, 1, d)
+    q, k, v = (x.to(_dtype(dtype)) for x in (q, k, v))
+    y = _token(sata, k, v, q)
+    V, vs, vm = _stands(v)
+    want = V.mean(2)
+    eps, offset = (2.0 ** -8, 128) if dtype == "bf16" else (2.0 ** -24, 16)
+    tol = eps * want.abs() + (((offset + 15) * vs + vm).mean(2)) * 2.0 ** -24 * (16 + 2 * math.sqrt(e / 8))
+    assert ((y - want).abs() <= tol).all(), ((y - want).abs() / tol).max()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_large_values_behind_ordinary_ones(sata, dtype):
+    """128 rows of ordinary size and 128 of the largest in turn; and the same with the largest of little weight."""
+    e, d = 2000, 128
+    gen = torch.Generator().manual_seed(12)
+    large = (torch.arange(e) // 128 % 2 == 1)[:, None]
+    v = torch.where(large, LARGEST, 1.0) * (torch.rand(2, 1, e, d, generator=gen) * 2 - 1)
+    k = torch.zeros(2, 1, e, d)
+    k[1] -= large * 60.0 / math.sqrt(d)  # (weights of exp(-60))
+    q = torch.ones(2, 2, d)
+    q, k, v = (x.to(_dtype(dtype)) for x in (q, k, v))
+    y = _token(sata, k, v, q)
+    want, tol = _bound(k, v, q, dtype)
+    assert ((y - want).abs() <= tol).all(), ((y - want).abs() / tol).max()
