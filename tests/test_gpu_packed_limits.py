@@ -148,3 +148,29 @@ def test_large_values_behind_ordinary_ones(sata, dtype):
     y = _token(sata, k, v, q)
     want, tol = _bound(k, v, q, dtype)
     assert ((y - want).abs() <= tol).all(), ((y - want).abs() / tol).max()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_values_that_cancel(sata, dtype):
+    """A key twice, with values of both signs: their sum is zero, and what is left of it is a weight's rounding times
+    the codes, not times what codes are counted from."""
+    B, H, d = 16, 4, 128
+    gen = torch.Generator().manual_seed(13)
+    code = torch.randint(0, 16, (B, H, d), generator=gen)
+    code[..., ::32], code[..., 1::32] = 0, 15
+    step = (9 + 2 * torch.randint(0, 4, (B, H, 4), generator=gen)).repeat_interleave(32, dim=-1) / 8.0
+    x = step * (code - 7.5)  # (least value and scale are bfloat16 numbers, of -x too)
+    v = torch.stack((x, -x, torch.zeros_like(x)), 2)
+    k = torch.zeros(B, H, 3, d)
+    k[:, :, :2] = -torch.rand(B, H, 1, 1, generator=gen).bfloat16().float()
+    q = torch.full((B, H, d), 0.125)
+    q, k, v = (a.to(_dtype(dtype)) for a in (q, k, v))
+    V, vs, vm = _stands(v)
+    assert torch.equal(V[:, :, 0], -V[:, :, 1]) and torch.equal(V[:, :, 0].float(), x)
+    p = torch.softmax((_stands(k)[0] @ q.double()[..., None])[..., 0] / math.sqrt(d), -1)[..., None]
+    weight, offset = (2.0 ** -18, 128) if dtype == "bf16" else (2.0 ** -25, 16)
+    # (16: the roundings of one wave's four matrix products of eight partial sums each, and of a few sums behind them, as a root
+    # of 64 and twice that)
+    tol = (p * 15 * vs).sum(2) * weight + (p * ((offset + 15) * vs + vm)).sum(2) * 16 * 2.0 ** -24
+    y = _token(sata, k, v, q)
+    assert (y.abs() <= tol).all(), (y.abs() / tol).max()
