@@ -448,8 +448,12 @@ typedef enum {
   SATA_ROTARY_LINEAR = 1,  /* all divided by the factor (positions brought closer together)        */
   SATA_ROTARY_BASE = 2,    /* base * factor^(pairs / (pairs - 1)): the slowest divided by the factor */
   SATA_ROTARY_BY_TURNS = 3 /* those of 32 turns and more in `original` tokens as they are, of one and
-                              fewer divided by the factor, in between in proportion; scale 0.1 ln factor + 1 */
+                              fewer divided by the factor, in between in proportion to the turns (the share
+                              (turns - 1) / 31 as they are, the rest divided); scale 0.1 ln factor + 1 */
 } sata_rotary_scaling;
+/* (Weights expect the frequencies that they were trained with.  Programs that go between the same two ends in proportion to
+ * a pair's number, not to its turns, have middle frequencies up to three times as large as BY_TURNS: for such weights, and
+ * for other ends, form the frequencies yourself; sata_rotary takes any.) */
 /* Host only.  inv_freq: [pairs] and scale: [1] (host, written), for sata_rotary; scale is 1 but BY_TURNS. */
 sata_status sata_rotary_frequencies(int pairs, double base, sata_rotary_scaling scaling, double factor, double original,
                                     float* inv_freq, float* scale);

@@ -777,7 +777,8 @@ def rotary_frequencies(pairs: int, base: float = 10000.0, scaling: str = "plain"
     """Frequencies base^(-i / pairs) of `pairs` pairs, [pairs] float32 on `device`, and the outputs' scale, for rotary().
     scaling, for contexts `factor` times as long as trained: "linear" divides all by the factor; "base" raises the
     base so that the slowest is divided by it; "by_turns" keeps those of 32 turns and more in `original` tokens, divides those
-    of one and fewer, goes from the ones to the others in proportion, and scales by 0.1 ln(factor) + 1."""
+    of one and fewer, goes from the ones to the others in proportion to the turns, and scales by 0.1 ln(factor) + 1
+    (weights that were trained with another way between the two need their own frequencies: rotary() takes any)."""
     if scaling not in ROTARY_SCALINGS:
         raise ValueError(f"unknown scaling {scaling!r}; one of {', '.join(ROTARY_SCALINGS)}")
     _check_sizes(pairs)
