@@ -1215,6 +1215,7 @@ sata_status sata_rotary_frequencies(int pairs, double base, sata_rotary_scaling 
     return fail(SATA_ERR_INVALID_ARG, "original=%g must be at least 1", original);
   if (scaling == SATA_ROTARY_BASE && pairs < 2) return fail(SATA_ERR_INVALID_ARG, "a scaled base takes two pairs at least");
   if (scaling == SATA_ROTARY_BASE) base *= std::pow(factor, (double)pairs / (pairs - 1));
+  if (!std::isfinite(base)) return fail(SATA_ERR_INVALID_ARG, "the base scaled by factor=%g is no number", factor);
   for (int i = 0; i < pairs; ++i) {
     double f = std::pow(base, -(double)i / pairs);
     if (scaling == SATA_ROTARY_LINEAR) f /= factor;

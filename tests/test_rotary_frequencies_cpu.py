@@ -20,3 +20,11 @@ def test_by_turns_in_between(pairs, base, original, factor):
         want.append(keep * x + (1.0 - keep) * x / factor)
     assert np.allclose(f.numpy(), want, rtol=2.0 ** -24 * (1 + 1e-6), atol=0.0)
     assert math.isclose(s, 0.1 * math.log(factor) + 1.0, rel_tol=2.0 ** -24)
+
+
+def test_a_scaled_base_that_is_no_number_is_refused():
+    """base * factor^(pairs / (pairs - 1)) beyond 64 bits would leave all pairs but the first unturned."""
+    with pytest.raises(bnd.SataError):
+        bnd.rotary_frequencies(64, 1e300, "base", 1e300, device="cpu")
+    with pytest.raises(bnd.SataError):
+        bnd.rotary_frequencies(2, 1e10, "base", 1e200, device="cpu")
