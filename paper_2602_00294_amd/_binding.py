@@ -782,7 +782,7 @@ def rotary_frequencies(pairs: int, base: float = 10000.0, scaling: str = "plain"
     if scaling not in ROTARY_SCALINGS:
         raise ValueError(f"unknown scaling {scaling!r}; one of {', '.join(ROTARY_SCALINGS)}")
     _check_sizes(pairs)
-    freq, scale = (ctypes.c_float * max(1, pairs))(), ctypes.c_float()
+    freq, scale = (ctypes.c_float * min(max(1, pairs), 128))(), ctypes.c_float()  # (more pairs are refused)
     _check(load_library().sata_rotary_frequencies(pairs, base, ROTARY_SCALINGS[scaling], factor, original, freq,
                                                   ctypes.byref(scale)), "sata_rotary_frequencies")
     return _torch().tensor(list(freq), dtype=_torch().float32).to(device), scale.value

@@ -28,3 +28,13 @@ def test_a_scaled_base_that_is_no_number_is_refused():
         bnd.rotary_frequencies(64, 1e300, "base", 1e300, device="cpu")
     with pytest.raises(bnd.SataError):
         bnd.rotary_frequencies(2, 1e10, "base", 1e200, device="cpu")
+
+
+def test_too_many_pairs_take_no_memory():
+    import tracemalloc
+    tracemalloc.start()
+    with pytest.raises(bnd.SataError):
+        bnd.rotary_frequencies(1 << 24, device="cpu")
+    peak = tracemalloc.get_traced_memory()[1]
+    tracemalloc.stop()
+    assert peak < 1 << 20
