@@ -120,7 +120,7 @@ __device__ __forceinline__ void delta_back(const DeltaArgs& a, const void* data_
         late[x] = *(const f32x4*)(d.late + 16 * x + 4 * t4);
         beta[x] = *(const f32x4*)(d.beta + 16 * x + 4 * t4);
       }
-      const float whole = d.whole[0];
+      const FloatPair whole = d.whole;
       f32x4 R[4] = {zero4(), zero4(), zero4(), zero4()}, z[4];
 #pragma unroll
       for (int b = 0; b < ND; ++b) {
@@ -145,7 +145,7 @@ __device__ __forceinline__ void delta_back(const DeltaArgs& a, const void* data_
 #pragma unroll
       for (int j = 0; j < 2 * ND; ++j)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) U[j][i] *= whole;
+        for (int i = 0; i < 4; ++i) U[j][i] = times(U[j][i], whole);
       // the second half first: the first one's updates are seen by its keys
 #pragma unroll
       for (int h = 1; h >= 0; --h) {

@@ -148,12 +148,13 @@ __global__ void __launch_bounds__(64) delta_pairs_kernel(DeltaArgs a, void* forw
     auto* const backward = (DeltaBackward*)backward_ + head * blocks + block;
     if (part == 0) {
       const double last = sums[kDeltaBlock - 1];
-      const float early = (float)exp(sum), late = (float)exp(last - sum), whole = (float)exp(last);
+      const float early = (float)exp(sum), late = (float)exp(last - sum);
+      const FloatPair whole = float_pair(exp(last));
       forward->early[lane] = early, forward->late[lane] = late * beta;
-      if (lane == 0) forward->whole[0] = whole;
+      if (lane == 0) forward->whole = whole;
       if constexpr (BACK) {
         backward->early[lane] = early, backward->late[lane] = late, backward->beta[lane] = beta;
-        if (lane == 0) backward->whole[0] = whole;
+        if (lane == 0) backward->whole = whole;
       }
     }
     const double my_sum = sums[i0 + l31];

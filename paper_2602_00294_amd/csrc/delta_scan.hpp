@@ -174,7 +174,7 @@ __device__ __forceinline__ void delta_scan(const DeltaArgs& a, const void* data_
         early[x] = *(const f32x4*)(d.early + 16 * x + 4 * t4);
         late[x] = *(const f32x4*)(d.late + 16 * x + 4 * t4);
       }
-      const float whole = d.whole[0];
+      const FloatPair whole = d.whole;
       auto operand = [&](const DeltaOperand* p, int x, auto& op) {
 #pragma unroll
         for (int i = 0; i < (int)(sizeof(op) / sizeof(op[0])); ++i) op[i] = p[i][x][lane];
@@ -278,7 +278,7 @@ __device__ __forceinline__ void delta_scan(const DeltaArgs& a, const void* data_
 #pragma unroll
       for (int j = 0; j < 2 * ND; ++j)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) S[j][i] *= whole;
+        for (int i = 0; i < 4; ++i) S[j][i] = times(S[j][i], whole);
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         uint4 e[2 * ND][L::kPl];

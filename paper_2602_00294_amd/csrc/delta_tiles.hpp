@@ -139,7 +139,8 @@ struct DeltaForward {
   DeltaOperand below[3];                      // L_21, rows i
   DeltaOperand pairs[3][kPair];               // P_11, P_21, P_22, rows i
   float early[kDeltaBlock], late[kDeltaBlock];  // exp(G_i), beta_j exp(G_C - G_j)
-  float whole[4];                             // exp(G_C)
+  FloatPair whole;                            // exp(G_C), of which a state takes one for every block
+  float none[2];
 };
 // For gradients, transposed: beta belongs to the other side there, M_ij = exp(G_i - G_j) beta_i k_i.k_j.
 struct DeltaBackward {
@@ -147,7 +148,8 @@ struct DeltaBackward {
   DeltaOperand below[3];       // M_21^T, rows j
   DeltaOperand pairs[3][3];    // P_11^T, P_21^T, P_22^T without beta, rows j
   float early[kDeltaBlock], late[kDeltaBlock], beta[kDeltaBlock];  // exp(G_i), exp(G_C - G_j)
-  float whole[4];
+  FloatPair whole;
+  float none[2];
 };
 
 // The records of a head's blocks on their way into LDS.  (Loads have no branches: behind a branch the compiler waits for
