@@ -47,7 +47,8 @@ __device__ __forceinline__ void delta_one_by_one(const DeltaArgs& a, int head, i
   const T* const q = (const T*)a.q + shared * a.n * a.dk;
   const T* const k = (const T*)a.k + shared * a.n * a.dk;
   for (int t = t0; t < t0 + m; ++t) {
-    const float lam = (float)exp(delta_rate(a.g[(int64_t)head * a.n + t])), beta = a.beta[(int64_t)head * a.n + t];
+    const FloatPair lam = float_pair(exp(delta_rate(a.g[(int64_t)head * a.n + t])));
+    const float beta = a.beta[(int64_t)head * a.n + t];
     float p = 0.f;
 #pragma unroll 1
     for (int j = 0; j < 2 * ND; ++j) {
@@ -57,7 +58,7 @@ __device__ __forceinline__ void delta_one_by_one(const DeltaArgs& a, int head, i
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int row = state_row(j, i, t4);
-        s[i] *= lam;
+        s[i] = times(s[i], lam);
         p = row < a.dk ? fmaf(entry_of(k, (int64_t)t * a.dk + row), s[i], p) : p;
       }
 #pragma unroll

@@ -48,3 +48,25 @@ def test_a_constant_decay_over_many_tokens(sata):
         # (2048 products, each rounded to the nearest: their errors, of either sign, add up as a root; four times that)
         err = ((got[:, :, dk // 2:].double().cpu() - want) / want).abs().max()
         assert err <= 4 * 2.0 ** -24 * math.sqrt(2048), err / (2.0 ** -24 * math.sqrt(2048))
+
+
+def test_a_constant_decay_beside_a_column_of_nan(sata):
+    """The same where a column of values is NaN, whose neighbours go on token by token: factors of one token each."""
+    n, dk, dv = 3000, 24, 20
+    g0, off = _inexact(-2e-6, -1e-6, 1)
+    assert off > 0.9 * 2.0 ** -25
+    print("constant decay beside NaN", n, g0, file=sys.stderr, flush=True)
+    q, k, v, _, beta, S0 = ref.draw(3, 1, 1, 1, n, dk, dv, "f32", state=True)
+    q[..., dk // 2:], k[..., dk // 2:] = 0.0, 0.0
+    v[0, 0, 0, 3] = math.nan
+    g = torch.full((1, 1, n), g0)
+    y, S = sata.delta_prefill(*(x.cuda() for x in (q, k, v, g, beta)), S_in=S0.cuda())
+    others = [c for c in range(dv) if c != 3]
+    assert torch.isnan(y[..., 3]).all() and torch.isnan(S[..., 3]).all() and torch.isfinite(y[..., others]).all()
+    want = (S0[:, :, dk // 2:].double() * math.exp(n * float(torch.tensor(g0))))[..., others]
+    got = S[:, :, dk // 2:].double().cpu()[..., others]
+    err = ((got - want) / want).abs().max()
+    # (A token's product is rounded by at most 2^-24.  These roundings are not of either sign: a token takes off some 12 to 25
+    # units in the last place, a number whose fraction changes by 4e-5 a token, so for thousands of tokens all are rounded the
+    # same way, and their errors add up to n of them at most.  A factor that is itself 2^-25 off would add half as much.)
+    assert err <= n * 2.0 ** -24, err / (n * 2.0 ** -24)
