@@ -5,6 +5,7 @@ import sys
 import pytest
 
 import delta_ref as ref
+from test_gpu_delta import check_gradients, check_rows, gradient_reference, state_tol
 
 pytestmark = pytest.mark.gpu
 
@@ -70,3 +71,44 @@ def test_a_constant_decay_beside_a_column_of_nan(sata):
     # units in the last place, a number whose fraction changes by 4e-5 a token, so for thousands of tokens all are rounded the
     # same way, and their errors add up to n of them at most.  A factor that is itself 2^-25 off would add half as much.)
     assert err <= n * 2.0 ** -24, err / (n * 2.0 ** -24)
+
+
+def _alike(seed, B, H, G, n, dk, dv, dtype):
+    """Keys that are nearly one another, with rates near 1: the pairs of a block are nearly all ones, what is right of
+    their triangular inverse is small."""
+    q, k, v, g, beta, S0 = ref.draw(seed, B, H, G, n, dk, dv, dtype, decay=1e-3, state=True)
+    k = k.float() * 0.05 + torch.randn(B, H, 1, dk, generator=torch.Generator().manual_seed(seed + 1)) / math.sqrt(dk)
+    k = (k / k.norm(dim=-1, keepdim=True) * (1 - 2.0 ** -8)).to(q.dtype)  # (rounded, none is longer than one)
+    return q, k, v, g, 1.0 - 0.02 * beta, S0
+
+
+SIZES = [(1, 1, 1, 2500, 64, 48, "f32"), (1, 1, 2, 2500, 128, 16, "bf16"), (2, 1, 1, 1100, 33, 20, "f32")]
+
+
+@pytest.mark.parametrize("case", SIZES, ids=str)
+@pytest.mark.parametrize("alike", [False, True])
+def test_long_prompts(sata, alike, case):
+    B, H, G, n, dk, dv, dtype = case
+    print("long prompt", alike, case, file=sys.stderr, flush=True)
+    draw = _alike if alike else lambda *a: ref.draw(*a, decay=1e-3, state=True)
+    q, k, v, g, beta, S0 = draw(n, *case)
+    want, S, states = ref.delta(*ref.to64(q, k, v, g, beta), None, S0.double())
+    y, got = sata.delta_prefill(*(x.cuda() for x in (q, k, v, g, beta)), S_in=S0.cuda())
+    tol = state_tol(n, dk)
+    off = (got.double().cpu() - S).flatten(2).norm(dim=-1) / S.flatten(2).norm(dim=-1)
+    assert (off <= tol).all(), off / tol
+    check_rows(y, want, q.float(), states, dk, dtype, tol)
+
+
+@pytest.mark.parametrize("case", [(1, 1, 1, 700, 64, 48, "f32"), (1, 1, 2, 700, 64, 64, "bf16"), (2, 1, 1, 333, 33, 20, "f32")], ids=str)
+@pytest.mark.parametrize("alike", [False, True])
+def test_long_gradients(sata, alike, case):
+    B, H, G, n, dk, dv, dtype = case
+    print("long gradients", alike, case, file=sys.stderr, flush=True)
+    draw = _alike if alike else lambda *a: ref.draw(*a, decay=1e-3, state=True)
+    q, k, v, g, beta, S0 = draw(n + 1, *case)
+    gen = torch.Generator().manual_seed(n)
+    dy, dS = torch.randn(v.shape, generator=gen).to(q.dtype), torch.randn(S0.shape, generator=gen)
+    want, size = gradient_reference(q, k, v, g, beta, dy, None, S0, dS)
+    got = sata.delta_backward(*(x.cuda() for x in (q, k, v, g, beta, dy)), S_in=S0.cuda(), dS=dS.cuda())
+    check_gradients(got, want, size, n, dk, dv, dtype, G)
