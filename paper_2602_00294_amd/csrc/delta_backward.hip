@@ -276,11 +276,15 @@ __device__ __forceinline__ float tile_entry(const u16* t, int row, int col) {
   return x;
 }
 
+// Lanes to a row of by_rows.
+template <int ND>
+constexpr int by_rows_lanes() { return ND == 1 ? 4 : ND == 2 ? 8 : 16; }
+
 // A wave's results of 16 tokens by 32 ND columns, through LDS into rows: row(i, c0, x) for eight columns at a time.  `buf`: the wave's
 // own; 16 rows of 32 ND + 4 floats.  (Results lie by columns: of 16 tokens each lane would write two bytes at a time.)
 template <int ND, typename F>
 __device__ __forceinline__ void by_rows(const f32x4 (&x)[2 * ND], float* buf, F&& row) {
-  constexpr int kPitch = 32 * ND + 4, kLanes = ND == 1 ? 4 : ND == 2 ? 8 : 16;
+  constexpr int kPitch = 32 * ND + 4, kLanes = by_rows_lanes<ND>();
   const int lane = threadIdx.x & 63, l15 = lane & 15, t4 = lane >> 4;
   wave_lds_fence();
 #pragma unroll
@@ -300,8 +304,6 @@ __device__ __forceinline__ void by_rows(const f32x4 (&x)[2 * ND], float* buf, F&
     row(token, c0, y);
   }
 }
-template <int ND>
-constexpr int by_rows_lanes() { return ND == 1 ? 4 : ND == 2 ? 8 : 16; }
 
 // MANY: several value heads to a query and key head, whose dq and dk are each written to `sums`, [2][value heads][n][dk].
 template <int ND, bool MANY>
@@ -697,7 +699,7 @@ delta_split_kernel(DeltaArgs a, const float* states, const float* behind, const 
     sq.init((const T*)a.q + row0 * a.dk, len, a.dk, tid);
     sk.fetch(t0);
     sq.fetch(t0);
-      if (wave == 0) {
+    if (wave == 0) {
       const bool there = t0 + lane < len;
       sums[lane] = sum_up_to(there ? delta_rate(a.g[row + t0 + lane]) : 0.0);
       rates[lane] = there ? a.beta[row + t0 + lane] : 0.f;

@@ -213,21 +213,10 @@ struct RowAccess {
   __device__ __forceinline__ uint4 quad(int offset) const {
     return __builtin_bit_cast(uint4, (u32x4)__builtin_amdgcn_raw_buffer_load_b128(rsrc, offset, 0, 0));
   }
-  // (the bits of bfloat16 ones)
-  __device__ __forceinline__ uint4 load_bits(int row, int c0) const {
-    if (vec) return quad(at(row, c0));
-    uint32_t u[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) u[i] = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rsrc, at(row, c0 + i), 0, 0);
-    return uint4{u[0] | u[1] << 16, u[2] | u[3] << 16, u[4] | u[5] << 16, u[6] | u[7] << 16};
-  }
+  // (float32 rows alone are read here: blocks of bfloat16 ones go through LDS)
   __device__ __forceinline__ void load(int row, int c0, float (&x)[8]) const {
-    if constexpr (sizeof(T) == 2) {
-      const uint4 w = load_bits(row, c0);
-      const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-      for (int i = 0; i < 4; ++i) x[2 * i] = lo_f32(u[i]), x[2 * i + 1] = hi_f32(u[i]);
-    } else if (vec) {
+    static_assert(sizeof(T) == 4, "float32 rows");
+    if (vec) {
       const uint4 w = quad(at(row, c0)), v = quad(at(row, c0 + 4));
       x[0] = __uint_as_float(w.x), x[1] = __uint_as_float(w.y), x[2] = __uint_as_float(w.z), x[3] = __uint_as_float(w.w);
       x[4] = __uint_as_float(v.x), x[5] = __uint_as_float(v.y), x[6] = __uint_as_float(v.z), x[7] = __uint_as_float(v.w);
@@ -238,13 +227,9 @@ struct RowAccess {
   }
   template <int PL>
   __device__ __forceinline__ void operand(int row, int c0, uint4 (&op)[PL]) const {
-    if constexpr (sizeof(T) == 2) {
-      op[0] = load_bits(row, c0);
-    } else {
-      float x[8];
-      load(row, c0, x);
-      operand_of<PL>(x, op);
-    }
+    float x[8];
+    load(row, c0, x);
+    operand_of<PL>(x, op);
   }
   __device__ __forceinline__ void put_quad(int offset, uint32_t a, uint32_t b, uint32_t c, uint32_t d) const {
     __builtin_amdgcn_raw_buffer_store_b128(u32x4{a, b, c, d}, rsrc, offset, 0, 0);

@@ -73,7 +73,7 @@ template <int G>
 __device__ __forceinline__ void group_bytes(const KeyCodes<G>& c, int g, uint32_t& first, uint32_t& second) {
   if constexpr (G == 4) {
     const uint32_t sel = 0x0c000c04u + 0x00010001u * g;  // byte g of the second and of the first
-    first = __builtin_amdgcn_perm(c.w[0], c.w[1], 0x0c000c04u + 0x00010001u * g);
+    first = __builtin_amdgcn_perm(c.w[0], c.w[1], sel);
     second = __builtin_amdgcn_perm(c.w[2], c.w[3], sel);
   } else if constexpr (G == 2) {
     first = g ? (c.w[0] >> 8) & 0x00ff00ffu : c.w[0] & 0x00ff00ffu;
