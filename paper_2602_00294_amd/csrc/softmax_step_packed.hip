@@ -6,11 +6,12 @@
 // fraction, 0x4300 | code, is 128 + code, exactly, so two codes become operands of a product by a shift (half of them) and
 // one and-or.  With s and m a group's scale and least value, X the sums over such operands, o = 128,
 //     q.k_t = sum_g s_tg X_tg + (m_tg - o s_tg) (sum of q's entries in g),   X_tg = sum_i (o + code_ti) q_i
-//     y     = sum_t (p_t s_tg) (o + code_tj) - sum_t (p_t s_tg) o + sum_t p_t m_tg,
-// the second sum by products of the very operands that enter the first: the rounding of p s, 2^-18 of it in bfloat16 calls,
-// counts as often as the code says, not o times as well (1.6 us of the time below).
-// What the offset takes from the sums, seven bits of 24, bfloat16 calls do not feel; float32 calls take
-// 0x4180 | code << 3, o = 16, for a shift more.
+//     y     = sum_t (p_t s_tg) (o + code_tj) - sum_t (p_t s_tg) (o + 8) + sum_t p_t (m_tg + 8 s_tg),
+// the second sum by products of the very operands that enter the first, product by product: a weight's rounding, 2^-18 of it in
+// bfloat16 calls, counts as often as code - 8 says, not o times as well (2 us of the time below), and m + 8 s, the middle of a
+// group, is no larger than its values, where sums of least values would have to cancel with sums of codes.
+// What the offset takes from the scores, seven bits of 24, bfloat16 calls do not feel; float32 calls take
+// 0x4180 | code << 3, o = 16, for a shift more, and take o + 8 off their scores in the same way.
 // Products are v_mfma_f32_16x16x32_bf16 with the query heads of a group as columns: of keys a group of 32 entries
 // at a time, rows being 16 tokens; of values 16 columns at a time over 32 tokens.  A lane reads of a key's row the bytes of
 // four a (packed_rows.hpp), of a value's row those of one; scores' tokens, four a lane, are the
@@ -37,9 +38,9 @@ namespace sata {
 namespace {
 
 // Workgroups of a CU.  Waves wait for loads more than they compute; the scheduling barriers below keep a tile's
-// parts apart so that three bfloat16 workgroups have registers enough (168 each, 14 of d_k = d_v = 128 in scratch).
-// 16 sequences, 8 key heads, caches of 16384 rows of 128 entries, ragged: 49.6 us with three, 53.2 with two, without the barriers 114
-// with three.  A float32 call's third plane takes the room of one.
+// parts apart so that three bfloat16 workgroups have registers enough (168 each, 15 of d_k = d_v = 128 in scratch).
+// 16 sequences, 8 key heads, caches of 16384 rows of 128 entries, ragged, step and join: 58.2 us with three, 60.1 with two,
+// without the barriers 74 with three.  A float32 call's third plane takes the room of one.
 template <typename T>
 constexpr int kAtOnce = sizeof(T) == 2 ? 3 : 2;
 
@@ -89,16 +90,16 @@ template <typename T>
 struct Codes {
   static constexpr float kOffset = sizeof(T) == 2 ? 128.f : 16.f;
   uint32_t mask = sizeof(T) == 2 ? 0x000f000fu : 0x00780078u, tag = sizeof(T) == 2 ? 0x43004300u : 0x41804180u;
-  uint32_t less = tag | 0x80008000u;  // (less the offset, twice)
+  uint32_t less = sizeof(T) == 2 ? 0xc308c308u : 0xc1c0c1c0u;  // -(kOffset + 8), twice
   __device__ __forceinline__ Codes() { asm("" : "+v"(mask), "+v"(tag), "+v"(less)); }
   __device__ __forceinline__ uint32_t low(uint32_t x) const { return ((sizeof(T) == 2 ? x : x << 3) & mask) | tag; }
   __device__ __forceinline__ uint32_t high(uint32_t x) const { return ((sizeof(T) == 2 ? x >> 4 : x >> 1) & mask) | tag; }
 };
 
-// Entries go up to 2^120 (packed_rows.hpp), and sums over (o + code) q or weights and those over least values that
-// belong to them are larger than what is left of them, by (o + 15) / 7.5 at most, a score's by twice that.
+// Entries go up to 2^120 (packed_rows.hpp), and sums over (o + code) q or weights are larger than what is left of them, by
+// (o + 15) / 7.5 at most, a score's by twice that.
 // Queries enter 2^8 times smaller: where a query's and a key's entries have a product at all, so have these.
-// Sums over 2^21 rows of weights up to 2^8 hold scales and least values of up to 2^88; from the first larger
+// Sums over 2^21 rows of weights up to 2^8 hold scales and middles of up to 2^88; from the first larger
 // ones on, a wave takes all 2^32 times smaller.  (Means of stretches, not sums, are joined.)
 constexpr float kSmaller = 0x1p-8f, kFar = 0x1p88f, kFarSmaller = 0x1p-32f;
 
@@ -212,6 +213,7 @@ __device__ __forceinline__ void packed_stretch_rows(const SoftmaxStepArgs& a, in
                                                     uint8_t* fresh, float* scales) {
   constexpr int kPl = sizeof(T) == 4 ? 3 : 1;    // numbers of a query's entry
   constexpr int kWeight = sizeof(T) == 4 ? 3 : 2;  // of a weight
+  constexpr bool kExact = sizeof(T) == 4;
   constexpr int kKey = 20 * GK, kValue = 20 * GV, kThreads = 64 * kStepWaves;
   const int tid = threadIdx.x, lane = tid & 63, l15 = lane & 15, t4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -272,7 +274,7 @@ __device__ __forceinline__ void packed_stretch_rows(const SoftmaxStepArgs& a, in
     }
     float x[8];
 #pragma unroll
-    for (int g = 0; g < 4; ++g) x[2 * g] = g < GK ? -Codes<T>::kOffset * total[g] : 0.f, x[2 * g + 1] = g < GK ? total[g] : 0.f;
+    for (int g = 0; g < 4; ++g) x[2 * g] = g < GK ? (kExact ? 8.f : -Codes<T>::kOffset) * total[g] : 0.f, x[2 * g + 1] = g < GK ? total[g] : 0.f;
     uint4 w[1][3];
     to_planes<3>(x, w);
     qsum = t4 == 0 ? w[0][0] : t4 == 1 ? w[0][1] : t4 == 2 ? w[0][2] : uint4{0u, 0u, 0u, 0u};
@@ -288,10 +290,11 @@ __device__ __forceinline__ void packed_stretch_rows(const SoftmaxStepArgs& a, in
   const float c = a.scale * (kLog2e / kSmaller);
   constexpr int kStep = 32 * kStepWaves;
   const Codes<T> codes;
-  // this wave's: scales of keys [32][GK], of values [32][GV], and least values
+  const uint4 less = {codes.less, codes.less, codes.less, codes.less};
+  // this wave's: scales of keys [32][GK], of values [32][GV], and the middles of their groups
   float* const kscale = scales + wave * 32 * (GK + 2 * GV);
   float* const vscale = kscale + 32 * GK;
-  float* const vleast = vscale + 32 * GV;
+  float* const vmiddle = vscale + 32 * GV;
   PackedTile<GK, GV> tile;
   const RowReader<GK> keys(K, a.capacity);
   const RowReader<GV> values(V, a.capacity);
@@ -311,12 +314,12 @@ __device__ __forceinline__ void packed_stretch_rows(const SoftmaxStepArgs& a, in
 #pragma unroll 1
   for (; r0 < end; r0 += kStep) {
     wave_lds_fence();  // (the last tile's scales have been read)
-    float vs[GV], least[GV], far = 0.f;
+    float vs[GV], middle[GV], far = 0.f;
 #pragma unroll
     for (int g = 0; g < GV; ++g) {
       vs[g] = lo_f32(tile.vp.w[g]);
-      least[g] = hi_f32(tile.vp.w[g]);
-      far = fmaxf(far, fmaxf(vs[g], fabsf(least[g])));
+      middle[g] = fmaf(8.f, vs[g], hi_f32(tile.vp.w[g]));
+      far = fmaxf(far, fmaxf(vs[g], fabsf(middle[g])));
     }
     if (__builtin_expect(smaller != 1.f || __ballot(far > kFar) != 0, 0)) {
       stay_in_branch();
@@ -331,7 +334,7 @@ __device__ __forceinline__ void packed_stretch_rows(const SoftmaxStepArgs& a, in
         for (int g = 0; g < GV; ++g) base[g] *= smaller;
       }
 #pragma unroll
-      for (int g = 0; g < GV; ++g) vs[g] *= smaller, least[g] *= smaller;
+      for (int g = 0; g < GV; ++g) vs[g] *= smaller, middle[g] *= smaller;
     }
     if (t4 < 2) {
       float k[GK];
@@ -339,7 +342,7 @@ __device__ __forceinline__ void packed_stretch_rows(const SoftmaxStepArgs& a, in
       for (int g = 0; g < GK; ++g) k[g] = lo_f32(t4 ? tile.kp[1].w[g] : tile.kp[0].w[g]);
       store_floats<GK>(kscale + lane * GK, k);
       store_floats<GV>(vscale + lane * GV, vs);
-      store_floats<GV>(vleast + lane * GV, least);
+      store_floats<GV>(vmiddle + lane * GV, middle);
     }
     wave_lds_fence();
     // ---- scores of tokens 4 t4 .. +3 and 16 + 4 t4 .. +3 with query head l15
@@ -359,7 +362,10 @@ __device__ __forceinline__ void packed_stretch_rows(const SoftmaxStepArgs& a, in
         const uint4 e = {codes.low(u), codes.low(w), codes.high(u), codes.high(w)};
         acc[g] = zero4();
 #pragma unroll
-        for (int p = kPl - 1; p >= 0; --p) acc[g] = mfma_bf16(e, qf[g][p], acc[g]);
+        for (int p = 0; p < kPl; ++p) {
+          if constexpr (kExact) acc[g] = mfma_bf16(less, qf[g][p], acc[g]);
+          acc[g] = mfma_bf16(e, qf[g][p], acc[g]);
+        }
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -414,11 +420,11 @@ __device__ __forceinline__ void packed_stretch_rows(const SoftmaxStepArgs& a, in
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const int row = (4 * t4 + 16 * (i >> 2) + (i & 3)) * GV + g0;
-        const Floats<kAt> scale = load_floats<kAt>(vscale + row), least = load_floats<kAt>(vleast + row);
+        const Floats<kAt> scale = load_floats<kAt>(vscale + row), middle = load_floats<kAt>(vmiddle + row);
 #pragma unroll
         for (int g = 0; g < kAt; ++g) {
           y[g][i] = z[i] * scale.f[g];
-          base[g0 + g] = fmaf(z[i], least.f[g], base[g0 + g]);
+          base[g0 + g] = fmaf(z[i], middle.f[g], base[g0 + g]);
         }
       }
 #pragma unroll
@@ -431,16 +437,20 @@ __device__ __forceinline__ void packed_stretch_rows(const SoftmaxStepArgs& a, in
           const uint32_t x = g & 1 ? pairs[i][g0 >> 1] >> 8 : pairs[i][g0 >> 1];
           lo[i] = codes.low(x), hi[i] = codes.high(x);
         }
-        f32x4 &a0 = o[2 * (g0 + g)], &a1 = o[2 * (g0 + g) + 1];
+        f32x4 &o0 = o[2 * (g0 + g)], &o1 = o[2 * (g0 + g) + 1];
+        f32x4 a0 = kExact ? zero4() : o0, a1 = kExact ? zero4() : o1;
 #pragma unroll
-        for (int p = kWeight - 1; p >= 0; --p) {
+        for (int p = 0; p < kWeight; ++p) {
+          a0 = mfma_bf16(less, w[p], a0);
+          a1 = mfma_bf16(less, w[p], a1);
           a0 = mfma_bf16(uint4{lo[0], lo[1], lo[2], lo[3]}, w[p], a0);
           a1 = mfma_bf16(uint4{hi[0], hi[1], hi[2], hi[3]}, w[p], a1);
         }
+        if constexpr (kExact) {
 #pragma unroll
-        for (int p = kWeight - 1; p >= 0; --p) {
-          a0 = mfma_bf16(uint4{codes.less, codes.less, codes.less, codes.less}, w[p], a0);
-          a1 = mfma_bf16(uint4{codes.less, codes.less, codes.less, codes.less}, w[p], a1);
+          for (int i = 0; i < 4; ++i) o0[i] += a0[i], o1[i] += a1[i];
+        } else {
+          o0 = a0, o1 = a1;
         }
       }
     }

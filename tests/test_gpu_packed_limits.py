@@ -174,3 +174,20 @@ def test_values_that_cancel(sata, dtype):
     tol = (p * 15 * vs).sum(2) * weight + (p * ((offset + 15) * vs + vm)).sum(2) * 16 * 2.0 ** -24
     y = _token(sata, k, v, q)
     assert (y.abs() <= tol).all(), (y.abs() / tol).max()
+
+
+@pytest.mark.parametrize("e,d", [(20, 64), (100, 32), (1000, 128), (3000, 64)])
+def test_float32_precision(sata, e, d):
+    """Values of both signs, whose sum is small beside its terms: the outputs' errors are those of the weights, as if each row's
+    values had been formed first.  A score, of some 4 at most, is a sum that goes through about a dozen roundings of up to 2^-24
+    of that (rms 0.3: 4 units of 2^-24); its exponential has 2 more, sums of the values as they are 2 or 3: 5 as a root, and
+    twice that for a batch of few heads.  (What codes are counted from, and least values, are 6 times a row's values and
+    up to 100 times a mean of them: left to cancel in sums over the rows, their roundings are 20 to 40 units.)"""
+    print("float32 precision", e, d, file=sys.stderr, flush=True)
+    gen = torch.Generator().manual_seed(e)
+    k, v, q = torch.randn(4, 4, e, d, generator=gen), torch.randn(4, 4, e, d, generator=gen), torch.randn(4, 4, d, generator=gen)
+    K, V = _stands(k)[0], _stands(v)[0]
+    p = torch.softmax((K @ q.double()[..., None])[..., 0] / math.sqrt(d), -1)
+    want = (p[..., None, :] @ V)[..., 0, :]
+    err = (_token(sata, k, v, q) - want).norm() / want.norm()
+    assert err <= 10 * 2.0 ** -24, err / 2.0 ** -24
