@@ -465,7 +465,8 @@ sata_status sata_rotary_frequencies(int pairs, double base, sata_rotary_scaling 
  * bits and of entry 32 g + 16 + a in its high ones; from byte 16 G on follow for each group its scale and its least value
  * in bfloat16.  An entry stands for least + scale * code (rounded once to float32).  For entries x of a group,
  *     least = bf16(min x),  scale = bf16((max x / 2 - min x / 2) / 7.5),  code = nearest of (x - least) / scale in 0..15
- * (0 where scale is 0), ties to the even one.  A group with an entry that is not finite or beyond 2^120 in size stands
+ * (0 where scale is 0), ties to the even one, in float32: half the range times the nearest float32 to 1 / 7.5, and
+ * (x / 2 - least / 2) / (scale / 2) as float32 division rounds it.  A group with an entry that is not finite or beyond 2^120 in size stands
  * for NaN.  Entries and groups behind d are zero.
  * A cache is [B][H_kv][capacity][row bytes], aligned to 4 G bytes (SATA_ERR_INVALID_ARG otherwise). */
 int64_t sata_packed_row_bytes(int d);

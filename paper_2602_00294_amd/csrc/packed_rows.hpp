@@ -18,8 +18,9 @@ namespace sata {
 
 // scale (low half) and least value (high half) of a group with these extremes; `fine`: all entries are in range
 __device__ __forceinline__ uint32_t group_params(float least, float most, bool fine) {
-  // (halves: as written down for programs that form such rows on their own; no difference of them overflows)
-  return fine ? pack2((0.5f * most - 0.5f * least) / 7.5f, least) : 0x7fc07fc0u;
+  // (halves: as written down for programs that form such rows on their own; no difference of them overflows.  The nearest
+  // float32 to 1 / 7.5, not a division: torch multiplies too where a program on the GPU divides by a number)
+  return fine ? pack2((0.5f * most - 0.5f * least) * (1.f / 7.5f), least) : 0x7fc07fc0u;
 }
 // What the codes of a group's entries take: (x / 2 - least / 2) / (scale / 2) as float32 division rounds it, then to the nearest.
 // 1 / (scale / 2) is rounded to the nearest by one Newton step (of all 128 significands of a bfloat16, from any start two

@@ -2,6 +2,7 @@
 import math
 import sys
 
+import numpy as np
 import pytest
 
 import delta_ref as ref
@@ -27,12 +28,21 @@ def _dtype(name):
 
 
 def _stands(x):
-    """(values, scales, sizes of the least values) [.., d] float64 of rows made from x."""
-    rows, values = ref.pack(x.float().numpy())
-    d, groups = x.shape[-1], rows.shape[-1] // 20
-    p = torch.from_numpy(rows[..., 16 * groups:].copy()).view(torch.bfloat16).double()
-    each = lambda j: p[..., j::2].repeat_interleave(32, dim=-1)[..., :d]  # noqa: E731
-    return torch.from_numpy(values).double(), each(0).abs(), each(1).abs()
+    """(values, scales, sizes of the least values) [.., d] float64 of what rows made from x stand for, in float32 as include/sata.h
+    has it."""
+    x = x.float().numpy()
+    out = [torch.empty(x.shape, dtype=torch.float64) for _ in range(3)]
+    half = np.float32(0.5)
+    for g in range(0, x.shape[-1], 32):
+        f = x[..., g:g + 32]
+        low, high = f.min(-1, keepdims=True), f.max(-1, keepdims=True)
+        scale, least = ref.bf16((half * high - half * low) * np.float32(1 / 7.5)), ref.bf16(low)
+        step = half * scale
+        code = np.clip(np.rint((half * f - half * least) / np.where(step > 0, step, np.float32(1))), 0, 15)
+        code = np.where(step > 0, code, 0).astype(np.float64)
+        for o, a in zip(out, (least + scale.astype(np.float64) * code, scale, np.abs(least))):
+            o[..., g:g + 32] = torch.from_numpy(np.broadcast_to(a, f.shape).astype(np.float64))
+    return out
 
 
 def _token(sata, k, v, q):
