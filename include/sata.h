@@ -289,7 +289,8 @@ sata_status sata_decode_step_grouped(float* S, const void* q, const void* k, con
  *  - Values that are not finite reach what depends on them only: not earlier
  *    tokens' outputs, nor other sequences or heads.  In softmax attention an infinity
  *    counts as in float32 arithmetic: a key whose score is minus infinity has no
- *    weight, and an infinite entry of v is an infinity in the outputs' column.
+ *    weight, and an infinite entry of v is an infinity in the outputs' column.  (Finite scores beyond 2^30 in size, whose
+ *    differences float32 has no digits for, may give NaN; over 4-bit caches they do not.)
  *    Gradients, and the decay's outputs and states, that it reaches are infinite or NaN.
  *  - float32 calls carry 24 bits throughout: inputs, weights, states and sums.  In bfloat16
  *    calls states, scores, statistics and sums are float32 and outputs are rounded

@@ -6,7 +6,7 @@
 //     y = c early q S + P E,  S = whole S + k^T (late E),
 // each a product whose right operand is what the one before left in this lane.  Four more waves bring the next block
 // into LDS: issuing its loads costs a wave 3300 cycles of the 13000 that a block then took.
-// 128 heads x 4096 tokens, d_k = d_v = 128, bfloat16: 253 us, 4 a block; matrix cores 38%, vector issue 39%, LDS 37% of
+// 128 heads x 4096 tokens, d_k = d_v = 128, bfloat16: 255 us, 4 a block; matrix cores 37%, vector issue 40%, LDS 36% of
 // the cycles, which one computing wave a SIMD overlaps only in part.  (16 columns are a product's least, and a head's
 // states would have to be joined over waves if its rows were shared out: no second wave to a SIMD at 128 heads.)
 //

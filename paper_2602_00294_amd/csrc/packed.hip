@@ -4,9 +4,10 @@
 // reads by whole vectors, and finds their ends and codes without another; the row's bytes, of which each group has every
 // G-th, change lanes (DPP) and places (v_perm) once.  Reading, a lane has eight entries and writes whole vectors side by
 // side with its neighbours'.
-// Keys and values of 32 heads x 4000 rows of 128 bfloat16 entries (86 MB): written in 16.8 us, of which vector
+// Keys and values of 32 heads x 4000 rows of 128 entries: bfloat16 (86 MB) written in 22.7 us, 3.8 TB/s, float32 (151 MB) in
+// 32, 4.7 TB/s; half of the bfloat16 rows, as padded prompts have them (43 MB), in 17 to 18, of which vector
 // instructions take 92% (a lane's division and rounding of 32 entries; 16 lanes to a group, as a token's row
-// is packed, took 36); read back in 10.3 us each, 4.2 TB/s (a lane a group, as they are written, took 15.8).
+// is packed, took 36); all read back in 10.3 us each, 4.2 TB/s (a lane a group, as they are written, took 15.8).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
