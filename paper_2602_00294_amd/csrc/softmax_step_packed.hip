@@ -20,7 +20,7 @@
 //
 // Bound: the cache is read once, 5 (d_k + d_v) / 8 bytes a key.
 //
-// Precision: codes, scales and least values are exact operands; scores, statistics and sums are float32; a weight times a
+// Precision: codes and scales are exact operands; middles, scores, statistics and sums are float32; a weight times a
 // scale is two bfloat16 numbers in bfloat16 calls, three in float32 ones.
 #include <hip/hip_runtime.h>
 

@@ -1,4 +1,5 @@
-"""Single tokens over caches of 4 bits an entry with entries near the largest that a row holds, against float64."""
+"""Single tokens over caches of 4 bits an entry, against float64: entries near the largest that a row holds, and what sums over codes
+may lose."""
 import math
 import sys
 
